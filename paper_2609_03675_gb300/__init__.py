@@ -16,8 +16,9 @@ import torch
 
 from . import _abi
 from ._abi import (KEEP_DROP, KEEP_FIRST, KEEP_GAP, KEEP_NOVELTY, NGFFError)  # noqa: F401
+from .kv import KVCache, Rotary
 
-__all__ = ["NGFF", "QER", "NGFFError", "KEEP_DROP", "KEEP_NOVELTY", "KEEP_GAP", "KEEP_FIRST", "library_path"]
+__all__ = ["NGFF", "QER", "KVCache", "Rotary", "NGFFError", "KEEP_DROP", "KEEP_NOVELTY", "KEEP_GAP", "KEEP_FIRST", "library_path"]
 
 
 def library_path() -> str:

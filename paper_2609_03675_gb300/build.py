@@ -20,7 +20,7 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libcofie_ngff.so")
 SOURCES = ["ngff_api.cu", "ngff_hist.cu", "ngff_features.cu", "ngff_select.cu", "ngff_chain.cu", "ngff_lazy.cu",
            "ngff_finalize.cu",
-           "ngff_static.cu", "qer.cu"]
+           "ngff_static.cu", "qer.cu", "rotary.cu", "kv_pages.cu", "kv_attend.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 
@@ -37,9 +37,9 @@ def _flags(extra=()):
 
 
 def _inputs():
-    headers = ["ngff_common.cuh", "ngff_device.cuh"]
+    headers = ["ngff_common.cuh", "ngff_device.cuh", "kv_common.cuh", "kv_rows.cuh", "kv_handle.cuh"]
     files = ([os.path.join(CSRC, s) for s in SOURCES + headers]
-             + [os.path.join(INCLUDE, "cofie_ngff.h"), __file__])
+             + [os.path.join(INCLUDE, h) for h in ("cofie_ngff.h", "cofie_kv.h")] + [__file__])
     return files
 
 

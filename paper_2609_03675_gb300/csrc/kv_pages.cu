@@ -1,0 +1,368 @@
+// The paged cache: its handle, appending to it and reading it back.
+#include <algorithm>
+#include <cstring>
+#include <new>
+
+#include "kv_handle.cuh"
+
+namespace cofie {
+namespace {
+
+constexpr int kThreads = 256;
+thread_local std::string g_kv_error;
+
+struct CodesArgs {
+  RowsArgs rows;  // queries, if any, as strided rows
+  const char* in[2];  // keys, values
+  int64_t in_token[2], in_head[2];
+  uint32_t* codes[2];
+  uint16_t* words[2];
+  uint32_t kv_heads, q_parts;
+};
+
+// Appends to 4-bit pages. CTAs of gridDim.y below q_parts rotate the queries;
+// the others take a share of the (key or value, head) rows of their tokens.
+// Eight values of a row to a lane, a group's 64 to eight lanes, which find its
+// extremes by shuffles.
+template <typename T, int V, int D>
+__global__ void __launch_bounds__(kThreads) append_codes(const __grid_constant__ CodesArgs a, const __grid_constant__ RotaryTable tab) {
+  extern __shared__ float2 cs[];
+  const RowsArgs& r = a.rows;
+  int64_t* place = reinterpret_cast<int64_t*>(cs + r.tile * tab.half);
+  int32_t* offs = reinterpret_cast<int32_t*>(place + r.tile);
+  const uint32_t t0 = blockIdx.x * r.tile, n = min(r.tile, r.n_tokens - t0);
+  pdl_trigger();
+  pdl_wait();
+  rows_set_up(r, tab, t0, n, cs, place, offs);
+  if (blockIdx.y < a.q_parts) {
+    const uint32_t per = (r.heads + a.q_parts - 1) / a.q_parts, h0 = blockIdx.y * per;
+    if (h0 < r.heads) rows_run<T, V>(r, tab, t0, n, h0, min(per, r.heads - h0), cs, place);
+    return;
+  }
+  constexpr uint32_t kLanes = D / 8;  // of a row
+  const uint32_t parts = gridDim.y - a.q_parts, part = blockIdx.y - a.q_parts;
+  const uint32_t per = (2 * a.kv_heads + parts - 1) / parts, k0 = part * per;
+  if (k0 >= 2 * a.kv_heads) return;
+  const uint32_t kinds = min(per, 2 * a.kv_heads - k0);
+  const uint32_t lane = threadIdx.x % kLanes, rows = n * kinds;
+  // whole warps stay in the loop, for the shuffles
+  for (uint32_t base = 0; base < rows; base += kThreads / kLanes) {
+    const uint32_t row = base + threadIdx.x / kLanes;
+    const bool live = row < rows;
+    const uint32_t t = live ? row / kinds : 0, kind = live ? k0 + row - t * kinds : 0;
+    const uint32_t v = kind >= a.kv_heads, head = kind - v * a.kv_heads;
+    const int64_t p = live ? place[t] : -1;
+    float x[8];
+    if (p >= 0) {
+      const T* in = reinterpret_cast<const T*>(a.in[v]) + static_cast<int64_t>(t0 + t) * a.in_token[v] + head * a.in_head[v];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t d = lane * 8 + i;
+        x[i] = Elem<T>::to(in[d]);
+        if (!v && d < 2 * tab.half) {
+          const bool by_half = tab.layout == COFIE_ROTARY_HALF;
+          const bool second = by_half ? d >= tab.half : d & 1;
+          const uint32_t pair = by_half ? (second ? d - tab.half : d) : d / 2;
+          const float other = Elem<T>::to(in[by_half ? (second ? d - tab.half : d + tab.half) : d ^ 1]);
+          const float2 c = cs[t * tab.half + pair];
+          x[i] = second ? x[i] * c.x + other * c.y : x[i] * c.x - other * c.y;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = 0.f;
+    }
+    float lo = 0.f, hi = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      lo = fminf(lo, x[i]);
+      hi = fmaxf(hi, x[i]);
+      if (!(fabsf(x[i]) <= 3.402823466e38f)) hi = INFINITY;  // fmax drops a NaN
+    }
+#pragma unroll
+    for (int o = 1; o < 8; o <<= 1) {
+      lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
+      hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
+    }
+    const float scale = group_scale(lo, hi);
+    // x / scale to the nearest, halves away from zero: the product with the
+    // reciprocal made a little too large (2^-21, more than its rounding) is
+    // never a half where the quotient is one, and no quotient of 16-bit x
+    // lies that close to a half without being one
+    const float inv = scale > 0.f ? __fmul_rn(__fdiv_rn(1.f, scale), 1.f + 0x1p-21f) : 0.f;
+    const float zero = fminf(rintf(-lo * inv), 15.f);
+    uint32_t word = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float q = fminf(fmaxf(rintf(x[i] * inv) + zero, 0.f), 15.f);
+      word |= static_cast<uint32_t>(q) << (4 * i);
+    }
+    if (p >= 0) {
+      const uint64_t out = page_row(r.batch, p, head);
+      a.codes[v][out * kLanes + lane] = word;
+      if (lane % 8 == 0)
+        a.words[v][out * (D / kGroup) + lane / 8] =
+            static_cast<uint16_t>((__float_as_uint(scale) >> 16) | static_cast<uint32_t>(zero));
+    }
+  }
+}
+
+struct ReadArgs {
+  BatchArg batch;
+  const char* pages[2];
+  const uint16_t* words[2];
+  uint4* out[2];
+};
+
+// Eight values of a (token, key or value, head) row to a thread.
+template <typename T, int D, int BITS>
+__global__ void __launch_bounds__(kThreads) read_pages(const ReadArgs a) {
+  constexpr uint32_t kLanes = D / 8;
+  pdl_trigger();
+  pdl_wait();
+  const uint64_t per_token = 2ull * a.batch.kv_heads * kLanes;
+  const uint64_t total = a.batch.n_tokens * per_token;
+  for (uint64_t e = blockIdx.x * static_cast<uint64_t>(kThreads) + threadIdx.x; e < total; e += static_cast<uint64_t>(gridDim.x) * kThreads) {
+    const uint32_t t = static_cast<uint32_t>(e / per_token), x = static_cast<uint32_t>(e - t * per_token);
+    const uint32_t lane = x % kLanes, kind = x / kLanes;
+    const uint32_t v = kind >= a.batch.kv_heads, head = kind - v * a.batch.kv_heads;
+    const int64_t p = place_of(a.batch, a.batch.offsets, t);
+    uint4 val = make_uint4(0, 0, 0, 0);
+    if (p >= 0) {
+      const uint64_t row = page_row(a.batch, p, head);
+      if (BITS == 16) {
+        val = reinterpret_cast<const uint4*>(a.pages[v])[row * kLanes + lane];
+      } else {
+        const uint32_t codes = reinterpret_cast<const uint32_t*>(a.pages[v])[row * kLanes + lane];
+        const uint32_t word = a.words[v][row * (D / kGroup) + lane / 8];
+        RowVec<T, 8> y;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y.v[i] = Elem<T>::from(code_value(codes >> (4 * i) & 15u, word));
+        val = *reinterpret_cast<uint4*>(&y);
+      }
+    }
+    a.out[v][(static_cast<uint64_t>(t) * a.batch.kv_heads + head) * kLanes + lane] = val;
+  }
+}
+
+template <typename T, int D>
+cudaError_t launch_codes(CodesArgs a, const RotaryTable& tab, bool queries, cudaStream_t st) {
+  RowsArgs& r = a.rows;
+  const uint32_t v = queries ? rows_vector(r, tab, D, 2) : 8;
+  r.units = D / (2 * v);
+  r.rotary_units = tab.half / v;
+  r.offsets_in_smem = r.batch.offsets && r.batch.n_seqs <= kOffsetsInSmem;
+  r.tile = r.n_tokens >= sm_count() * 16 ? 8 : 1;
+  const uint32_t tiles = (r.n_tokens + r.tile - 1) / r.tile;
+  const uint32_t parts = std::max(1u, std::min(2 * a.kv_heads, sm_count() * 4 / tiles));
+  a.q_parts = queries ? std::max(1u, std::min(r.heads, sm_count() * 4 / tiles)) : 0;
+  const dim3 grid(tiles, parts + a.q_parts);
+  const size_t smem = rows_smem(r.tile, tab.half, r.batch.n_seqs, r.offsets_in_smem);
+  const auto go = [&](auto kernel) { return launch_dependent(true, kernel, grid, dim3(kThreads), smem, st, a, tab); };
+  return v == 8   ? go(append_codes<T, 8, D>)
+         : v == 4 ? go(append_codes<T, 4, D>)
+         : v == 2 ? go(append_codes<T, 2, D>)
+                  : go(append_codes<T, 1, D>);
+}
+
+template <typename T, int D>
+cudaError_t launch_read(const ReadArgs& a, uint32_t bits, cudaStream_t st) {
+  const uint64_t total = 2ull * a.batch.n_tokens * a.batch.kv_heads * (D / 8);
+  const dim3 grid(static_cast<uint32_t>(std::min<uint64_t>((total + kThreads - 1) / kThreads, sm_count() * 64ull)));
+  return bits == 4 ? launch_dependent(true, read_pages<T, D, 4>, grid, dim3(kThreads), 0, st, a)
+                   : launch_dependent(true, read_pages<T, D, 16>, grid, dim3(kThreads), 0, st, a);
+}
+
+bool on_device(const void* p, int dev) {
+  cudaPointerAttributes a;
+  if (cudaPointerGetAttributes(&a, p) != cudaSuccess) {
+    cudaGetLastError();
+    return false;
+  }
+  return (a.type == cudaMemoryTypeDevice || a.type == cudaMemoryTypeManaged) && a.device == dev;
+}
+
+void kv_free(cofie_kv* h) {
+  if (!h) return;
+  DeviceGuard g(h->device);
+  cudaDeviceSynchronize();
+  if (h->d_err) cudaFree(h->d_err);
+  delete h;
+}
+
+}  // namespace
+
+int check_batch(cofie_kv* h, const cofie_kv_batch* b) {
+  if (!b) return h->fail(COFIE_EINVAL, "the batch is NULL");
+  if (b->n_tokens > 0x7fffffffu || b->n_seqs > 0x7fffffffu) return h->fail(COFIE_EINVAL, "n_tokens and n_seqs must be below 2^31");
+  if (b->n_tokens == 0) return COFIE_OK;
+  if (b->n_seqs == 0) return h->fail(COFIE_EINVAL, "a batch with tokens needs sequences");
+  if (!b->table || !b->lengths) return h->fail(COFIE_EINVAL, "table and lengths are required");
+  if (b->table_stride < 1 || b->table_stride > 0x7fffffffu / h->p.page_size)
+    return h->fail(COFIE_EINVAL, "table_stride x page_size must be in [page_size, 2^31)");
+  if (!b->offsets && b->n_tokens != b->n_seqs) return h->fail(COFIE_EINVAL, "without offsets every sequence has one new token");
+  return COFIE_OK;
+}
+
+int check_rows(cofie_kv* h, const cofie_rows* r, uint32_t heads, bool has_out, const char* name) {
+  const std::string n(name);
+  if (!r->in || (has_out && !r->out)) return h->fail(COFIE_EINVAL, n + " is NULL");
+  if (r->heads != heads) return h->fail(COFIE_EINVAL, n + " must have " + std::to_string(heads) + " heads");
+  if (reinterpret_cast<uintptr_t>(r->in) % 2 || (has_out && reinterpret_cast<uintptr_t>(r->out) % 2))
+    return h->fail(COFIE_EINVAL, n + " is not aligned to its type");
+  return COFIE_OK;
+}
+
+BatchArg batch_arg(const cofie_kv* h, const cofie_kv_batch* b) {
+  return {b->table, b->lengths, b->offsets, b->n_seqs, b->n_tokens, b->table_stride, h->p.n_pages, h->page_shift, h->p.n_kv_heads, h->d_err};
+}
+
+int launched(cofie_kv* h, cudaError_t e, const char* what) {
+  if (e == cudaSuccess) return COFIE_OK;
+  cudaGetLastError();
+  return h->fail(COFIE_ECUDA, std::string(what) + ": " + cudaGetErrorString(e));
+}
+
+}  // namespace cofie
+
+using namespace cofie;
+
+extern "C" {
+
+int cofie_kv_create(const cofie_kv_params* p, cofie_kv_t** out) {
+  const auto bad = [](const char* m) { return g_kv_error = m, COFIE_EINVAL; };
+  if (!p || !out) return bad("params or out is NULL");
+  if (p->n_pages < 1 || p->n_pages > 0x7fffffffu) return bad("n_pages must be in [1, 2^31)");
+  uint32_t shift = 4;
+  while (shift <= 8 && (1u << shift) != p->page_size) ++shift;
+  if (shift > 8) return bad("page_size must be 16, 32, 64, 128 or 256");
+  if (p->n_heads < 1 || p->n_kv_heads < 1 || p->n_heads > 1024 || p->n_heads % p->n_kv_heads)
+    return bad("n_kv_heads must divide n_heads, at most 1024");
+  if (p->head_dim != 64 && p->head_dim != 128) return bad("head_dim must be 64 or 128");
+  if (p->dtype != COFIE_BF16 && p->dtype != COFIE_FP16) return bad("dtype must be COFIE_BF16 or COFIE_FP16");
+  if (p->bits != 16 && p->bits != 4) return bad("bits must be 16 or 4");
+  if (!p->k_pages || !p->v_pages || (p->bits == 4 && (!p->k_scales || !p->v_scales)))
+    return bad("the pages (and for 4 bits the scales) are required");
+  for (const void* x : {static_cast<const void*>(p->k_pages), static_cast<const void*>(p->v_pages),
+                        static_cast<const void*>(p->k_scales), static_cast<const void*>(p->v_scales)})
+    if (reinterpret_cast<uintptr_t>(x) % 16) return bad("pages and scales must be 16-byte aligned");
+  int dev = p->device;
+  if (dev < 0 && cudaGetDevice(&dev) != cudaSuccess) return g_kv_error = "no CUDA device", COFIE_ECUDA;
+  int count = 0;
+  if (cudaGetDeviceCount(&count) != cudaSuccess || dev >= count) {
+    cudaGetLastError();
+    return g_kv_error = "cannot select the device", COFIE_ECUDA;
+  }
+  DeviceGuard g(dev);
+  if (!on_device(p->k_pages, dev) || !on_device(p->v_pages, dev) ||
+      (p->bits == 4 && (!on_device(p->k_scales, dev) || !on_device(p->v_scales, dev))))
+    return bad("the pages must be device memory on the handle's device");
+  cofie_kv* h = new (std::nothrow) cofie_kv();
+  if (!h) return g_kv_error = "host allocation failed", COFIE_ENOMEM;
+  h->p = *p;
+  h->device = dev;
+  h->page_shift = shift;
+  cudaError_t e = injected_alloc_failure() ? cudaErrorMemoryAllocation : cudaMalloc(&h->d_err, sizeof(uint32_t));
+  if (e == cudaSuccess) e = cudaMemset(h->d_err, 0, sizeof(uint32_t));
+  if (e != cudaSuccess) {
+    g_kv_error = std::string("cache set-up failed: ") + cudaGetErrorString(e);
+    cudaGetLastError();
+    kv_free(h);
+    return e == cudaErrorMemoryAllocation ? COFIE_ENOMEM : COFIE_ECUDA;
+  }
+  *out = h;
+  return COFIE_OK;
+}
+
+void cofie_kv_destroy(cofie_kv_t* h) { kv_free(h); }
+
+int cofie_kv_append(cofie_kv_t* h, const cofie_kv_batch* b, const cofie_rows* k, const cofie_rows* v, const cofie_rows* q,
+                    const cofie_rotary_t* rotary, const int32_t* positions, void* cuda_stream) {
+  if (!h) return COFIE_EINVAL;
+  if (const int rc = check_batch(h, b)) return rc;
+  if (b->n_tokens == 0) return COFIE_OK;
+  if (!k || !v) return h->fail(COFIE_EINVAL, "k and v are required");
+  if (const int rc = check_rows(h, k, h->p.n_kv_heads, false, "k")) return rc;
+  if (const int rc = check_rows(h, v, h->p.n_kv_heads, false, "v")) return rc;
+  if (q) {
+    if (!rotary) return h->fail(COFIE_EINVAL, "q without rotary has nothing to be done to it");
+    if (const int rc = check_rows(h, q, h->p.n_heads, true, "q")) return rc;
+    if (q->in == q->out && (q->in_token != q->out_token || q->in_head != q->out_head))
+      return h->fail(COFIE_EINVAL, "in place, the strides of q's in and out must be the same");
+  }
+  if (rotary && rotary_head_dim(rotary) != h->p.head_dim) return h->fail(COFIE_EINVAL, "rotary's head_dim is not the cache's");
+  if (rotary && !positions) return h->fail(COFIE_EINVAL, "positions is required with rotary");
+  DeviceGuard g(h->device);
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  static const RotaryTable none{};
+  const RotaryTable& tab = rotary ? rotary_table(rotary) : none;
+  RowsArgs a{};
+  a.n_tokens = b->n_tokens;
+  a.positions = positions;
+  a.paged = 1;
+  a.batch = batch_arg(h, b);
+  const auto rows = [](const cofie_rows* r, void* out, uint32_t kind) {
+    return RowsArg{static_cast<const char*>(r->in), static_cast<char*>(out), r->in_token, r->in_head, r->out_token, r->out_head, r->heads, kind};
+  };
+  if (q) a.rows[a.n_rows++] = rows(q, q->out, kRotate);
+  cudaError_t e;
+  if (h->p.bits == 16) {
+    cofie_rows kr = *k, vr = *v;
+    kr.out_token = kr.out_head = vr.out_token = vr.out_head = 0;
+    a.rows[a.n_rows++] = rows(&kr, h->p.k_pages, kRotatePage);
+    a.rows[a.n_rows++] = rows(&vr, h->p.v_pages, kCopyPage);
+    for (uint32_t i = 0; i < a.n_rows; ++i) a.heads += a.rows[i].heads;
+    e = launch_rows(a, tab, h->p.head_dim, h->p.dtype, st);
+  } else {
+    a.heads = q ? h->p.n_heads : 0;
+    CodesArgs c{a,
+                {static_cast<const char*>(k->in), static_cast<const char*>(v->in)},
+                {k->in_token, v->in_token},
+                {k->in_head, v->in_head},
+                {static_cast<uint32_t*>(h->p.k_pages), static_cast<uint32_t*>(h->p.v_pages)},
+                {h->p.k_scales, h->p.v_scales},
+                h->p.n_kv_heads,
+                0};
+    if (h->p.dtype == COFIE_BF16)
+      e = h->p.head_dim == 64 ? launch_codes<__nv_bfloat16, 64>(c, tab, q != nullptr, st) : launch_codes<__nv_bfloat16, 128>(c, tab, q != nullptr, st);
+    else
+      e = h->p.head_dim == 64 ? launch_codes<__half, 64>(c, tab, q != nullptr, st) : launch_codes<__half, 128>(c, tab, q != nullptr, st);
+  }
+  return launched(h, e, "append");
+}
+
+int cofie_kv_read(cofie_kv_t* h, const cofie_kv_batch* b, void* k_out, void* v_out, void* cuda_stream) {
+  if (!h) return COFIE_EINVAL;
+  if (const int rc = check_batch(h, b)) return rc;
+  if (b->n_tokens == 0) return COFIE_OK;
+  if (!k_out || !v_out || reinterpret_cast<uintptr_t>(k_out) % 16 || reinterpret_cast<uintptr_t>(v_out) % 16)
+    return h->fail(COFIE_EINVAL, "k_out and v_out are required, 16-byte aligned");
+  DeviceGuard g(h->device);
+  const ReadArgs a{batch_arg(h, b),
+                   {static_cast<const char*>(h->p.k_pages), static_cast<const char*>(h->p.v_pages)},
+                   {h->p.k_scales, h->p.v_scales},
+                   {static_cast<uint4*>(k_out), static_cast<uint4*>(v_out)}};
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const bool bf = h->p.dtype == COFIE_BF16;
+  const cudaError_t e = h->p.head_dim == 64 ? (bf ? launch_read<__nv_bfloat16, 64>(a, h->p.bits, st) : launch_read<__half, 64>(a, h->p.bits, st))
+                                            : (bf ? launch_read<__nv_bfloat16, 128>(a, h->p.bits, st) : launch_read<__half, 128>(a, h->p.bits, st));
+  return launched(h, e, "read");
+}
+
+int cofie_kv_status(cofie_kv_t* h, void* cuda_stream) {
+  if (!h) return COFIE_EINVAL;
+  DeviceGuard g(h->device);
+  cudaError_t e = cudaStreamSynchronize(static_cast<cudaStream_t>(cuda_stream));
+  uint32_t word = 0;
+  if (e == cudaSuccess) e = cudaMemcpy(&word, h->d_err, sizeof word, cudaMemcpyDeviceToHost);
+  if (e == cudaSuccess && word) e = cudaMemset(h->d_err, 0, sizeof word);
+  if (e != cudaSuccess) return launched(h, e, "status");
+  if (word & kKvErrWait) return h->fail(COFIE_ETIMEOUT, "a device-side wait of the attention kernel ran out");
+  if (word & kKvErrPage) return h->fail(COFIE_EDEVICE, "a page number in the table is not below n_pages");
+  if (word) return h->fail(COFIE_EDEVICE, "a length or an offset of the batch is out of range");
+  return COFIE_OK;
+}
+
+const char* cofie_kv_last_error(const cofie_kv_t* h) { return h ? h->err.c_str() : g_kv_error.c_str(); }
+
+}  // extern "C"

@@ -1,0 +1,343 @@
+"""Answering from the selected frames: rotary positions, a paged key/value
+cache of 16-bit values or 4-bit codes, and attention over it.
+
+    from paper_2609_03675_gb300 import KVCache, Rotary
+    rotary = Rotary(128, base=1e6)
+    cache = KVCache(n_pages, 64, 32, 8, 128, bits=4, rotary=rotary)
+    q = cache.append(k, v, table, lengths, offsets, positions=positions, q=q)
+    out, lse = cache.attend(q, table, lengths, offsets, max_new=longest_question)
+
+Thin binding of the entry points that include/cofie_kv.h declares (the layout
+of pages and codes is described there); every value is computed in the
+library's CUDA kernels.
+"""
+from __future__ import annotations
+
+import contextlib
+import ctypes
+
+import torch
+
+from . import _abi
+from ._abi import NGFFError
+
+__all__ = ["KVCache", "Rotary"]
+
+_DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+_LAYOUTS = {"half": 0, "interleaved": 1}
+_SCALINGS = {"none": 0, "linear": 1, "base": 2, "yarn": 3}
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+
+
+class _RotaryParams(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_uint32), ("rotary_dim", ctypes.c_uint32), ("layout", ctypes.c_uint32),
+                ("scaling", ctypes.c_uint32), ("base", ctypes.c_double), ("factor", ctypes.c_double),
+                ("original_len", ctypes.c_double), ("beta_fast", ctypes.c_double), ("beta_slow", ctypes.c_double),
+                ("n_axes", ctypes.c_uint32), ("axes", ctypes.c_char_p)]
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("src", ctypes.c_void_p), ("out", ctypes.c_void_p), ("heads", ctypes.c_uint32), ("in_token", ctypes.c_int64),
+                ("in_head", ctypes.c_int64), ("out_token", ctypes.c_int64), ("out_head", ctypes.c_int64)]
+
+
+class _KVParams(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_uint32), ("page_size", ctypes.c_uint32), ("n_heads", ctypes.c_uint32),
+                ("n_kv_heads", ctypes.c_uint32), ("head_dim", ctypes.c_uint32), ("dtype", ctypes.c_uint32),
+                ("bits", ctypes.c_uint32), ("device", ctypes.c_int32), ("k_pages", ctypes.c_void_p),
+                ("v_pages", ctypes.c_void_p), ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p)]
+
+
+class _Batch(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_uint32), ("n_tokens", ctypes.c_uint32), ("max_new", ctypes.c_uint32),
+                ("table_stride", ctypes.c_uint32), ("table", ctypes.c_void_p), ("lengths", ctypes.c_void_p),
+                ("offsets", ctypes.c_void_p)]
+
+
+# Every symbol include/cofie_kv.h declares.
+EXPORTS = ("cofie_rotary_create", "cofie_rotary_destroy", "cofie_rotary_run", "cofie_rotary_last_error", "cofie_kv_create",
+           "cofie_kv_destroy", "cofie_kv_append", "cofie_kv_read", "cofie_kv_attend", "cofie_kv_status", "cofie_kv_last_error")
+
+_bound = None
+
+
+def _load():
+    global _bound
+    lib = _abi.load()
+    if _bound is lib:
+        return lib
+    vp, u32, u64, P = ctypes.c_void_p, ctypes.c_uint32, ctypes.c_uint64, ctypes.POINTER
+    for name, res, args in (
+            ("cofie_rotary_create", ctypes.c_int, [P(_RotaryParams), P(vp)]),
+            ("cofie_rotary_destroy", None, [vp]),
+            ("cofie_rotary_run", ctypes.c_int, [vp, P(_Rows), u32, u32, vp, u32, ctypes.c_int, vp]),
+            ("cofie_rotary_last_error", ctypes.c_char_p, [vp]),
+            ("cofie_kv_create", ctypes.c_int, [P(_KVParams), P(vp)]),
+            ("cofie_kv_destroy", None, [vp]),
+            ("cofie_kv_append", ctypes.c_int, [vp, P(_Batch), P(_Rows), P(_Rows), P(_Rows), vp, vp, vp]),
+            ("cofie_kv_read", ctypes.c_int, [vp, P(_Batch), vp, vp, vp]),
+            ("cofie_kv_attend", ctypes.c_int, [vp, P(_Batch), P(_Rows), vp, vp, u64, ctypes.c_int, ctypes.c_float, vp]),
+            ("cofie_kv_status", ctypes.c_int, [vp, vp]),
+            ("cofie_kv_last_error", ctypes.c_char_p, [vp])):
+        f = getattr(lib, name)
+        f.restype, f.argtypes = res, args
+    _bound = lib
+    return lib
+
+
+def _stream_of(cuda_stream, index):
+    if cuda_stream is None:
+        return _raw_stream(index)
+    return cuda_stream.cuda_stream if isinstance(cuda_stream, torch.cuda.Stream) else int(cuda_stream)
+
+
+def _allocating(cuda_stream, index):
+    """Outputs made for a call on another stream than the current one belong to that stream."""
+    if cuda_stream is None:
+        return contextlib.nullcontext()
+    if not isinstance(cuda_stream, torch.cuda.Stream):
+        cuda_stream = torch.cuda.ExternalStream(int(cuda_stream), device=index)
+    return torch.cuda.stream(cuda_stream)
+
+
+def _heads(x, dtype, index, what):
+    """(data_ptr, tokens, heads, token stride, head stride) of a [tokens, heads, head_dim] tensor."""
+    if x.dtype != dtype or x.dim() != 3 or x.get_device() != index:
+        raise ValueError(f"{what} must be a {dtype} tensor [tokens, heads, head_dim] on cuda:{index}")
+    n, h, d = x.shape
+    t, s, one = x.stride()
+    if one != 1 and d > 1:
+        raise ValueError(f"{what}: a head's values must be contiguous")
+    return x.data_ptr(), n, h, t, s
+
+
+def _int32(x, index, what, shape=None):
+    if x.dtype != torch.int32 or x.get_device() != index or not x.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous int32 tensor on cuda:{index}")
+    if shape is not None and tuple(x.shape) != shape:
+        raise ValueError(f"{what} must have the shape {shape}")
+    return x.data_ptr()
+
+
+class Rotary:
+    """Rotates heads to their positions.
+
+    layout: "half" pairs x[i] with x[i + rotary_dim / 2], "interleaved" x[2 i] with x[2 i + 1]; what lies past rotary_dim
+    passes through. scaling: "none", "linear", "base" or "yarn" (with original_len, the trained length), by ``factor``.
+    axes: None, or one axis number for each pair, where positions have several axes (frame, row, column)."""
+
+    def __init__(self, head_dim: int, *, rotary_dim: int | None = None, base: float = 10000.0, layout: str = "half",
+                 scaling: str = "none", factor: float = 1.0, original_len: float = 0.0, beta_fast: float = 32.0,
+                 beta_slow: float = 1.0, axes=None):
+        if layout not in _LAYOUTS or scaling not in _SCALINGS:
+            raise ValueError(f"layout is one of {sorted(_LAYOUTS)}, scaling one of {sorted(_SCALINGS)}")
+        rotary_dim = head_dim if rotary_dim is None else rotary_dim
+        if axes is not None:
+            axes = bytes(axes)
+            if len(axes) != rotary_dim // 2:
+                raise ValueError("axes has one entry for each of the rotary_dim / 2 pairs")
+        self.head_dim, self.rotary_dim, self.layout = head_dim, rotary_dim, layout
+        self.n_axes = max(axes) + 1 if axes else 1
+        lib = _load()
+        p = _RotaryParams(head_dim, rotary_dim, _LAYOUTS[layout], _SCALINGS[scaling], base, factor, original_len, beta_fast,
+                          beta_slow, self.n_axes, axes)
+        h = ctypes.c_void_p()
+        rc = lib.cofie_rotary_create(ctypes.byref(p), ctypes.byref(h))
+        if rc != _abi.OK:
+            raise NGFFError(rc, lib.cofie_rotary_last_error(None).decode())
+        self._lib, self._h = lib, h
+
+    def _positions(self, positions, n, index):
+        shape = (n,) if positions.dim() == 1 and self.n_axes == 1 else (self.n_axes, n)
+        return _int32(positions, index, "positions", shape)
+
+    def _run(self, x, positions, out, transpose, cuda_stream):
+        xs = (x,) if isinstance(x, torch.Tensor) else tuple(x)
+        if not 1 <= len(xs) <= 4:
+            raise ValueError("one to four tensors of the same tokens")
+        index, dtype, n = xs[0].get_device(), xs[0].dtype, xs[0].shape[0]
+        if index < 0 or dtype not in _DTYPES:
+            raise ValueError("the tensors must be bfloat16, float16 or float32, on a CUDA device")
+        if out is None:
+            with _allocating(cuda_stream, index):
+                outs = tuple(torch.empty(y.shape, dtype=dtype, device=y.device) for y in xs)
+        else:
+            outs = (out,) if isinstance(out, torch.Tensor) else tuple(out)
+        if len(outs) != len(xs):
+            raise ValueError("out has a tensor for each input")
+        rows = (_Rows * len(xs))()
+        for r, y, o in zip(rows, xs, outs):
+            if y.shape[0] != n or y.shape[-1] != self.head_dim or o.shape != y.shape:
+                raise ValueError(f"every tensor is [tokens, heads, {self.head_dim}], and its out as large")
+            r.src, _, r.heads, r.in_token, r.in_head = _heads(y, dtype, index, "x")
+            r.out, _, _, r.out_token, r.out_head = _heads(o, dtype, index, "out")
+        at = self._positions(positions, n, index)
+        with contextlib.nullcontext() if index == torch.cuda.current_device() else torch.cuda.device(index):
+            rc = self._lib.cofie_rotary_run(self._h, rows, len(xs), n, at, _DTYPES[dtype], transpose,
+                                            _stream_of(cuda_stream, index))
+        if rc != _abi.OK:
+            raise NGFFError(rc, self._lib.cofie_rotary_last_error(self._h).decode())
+        return outs[0] if isinstance(x, torch.Tensor) else outs
+
+    def apply(self, x, positions, *, out=None, cuda_stream=None):
+        """x (a tensor [tokens, heads, head_dim], or up to four of the same tokens) rotated; positions int32 [tokens], or
+        [axes, tokens]. ``out`` may be x itself."""
+        return self._run(x, positions, out, 0, cuda_stream)
+
+    def backward(self, grad, positions, *, out=None, cuda_stream=None):
+        """The gradient of apply()'s input, from that of its output: the transposed rotation."""
+        return self._run(grad, positions, out, 1, cuda_stream)
+
+    def close(self):
+        if getattr(self, "_h", None):
+            self._lib.cofie_rotary_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:  # noqa: BLE001 -- interpreter shutdown
+            pass
+
+
+class KVCache:
+    """Paged keys and values of one layer, n_pages pages of page_size tokens.
+
+    The pages are k_pages, v_pages (and k_scales, v_scales for 4 bits), made here unless given. Sequence s of a batch holds
+    lengths[s] tokens; token i lies in page table[s, i // page_size]. A batch's new tokens are rows offsets[s] to
+    offsets[s + 1] of every per-token argument, the last of the sequence's lengths[s] (offsets=None: one each)."""
+
+    def __init__(self, n_pages: int, page_size: int, n_heads: int, n_kv_heads: int, head_dim: int, *,
+                 dtype: torch.dtype = torch.bfloat16, bits: int = 16, rotary: Rotary | None = None, device: int | None = None,
+                 k_pages=None, v_pages=None, k_scales=None, v_scales=None):
+        lib = _load()
+        if dtype not in (torch.bfloat16, torch.float16) or bits not in (4, 16):
+            raise ValueError("dtype is bfloat16 or float16, bits 16 or 4")
+        index = device if device is not None else k_pages.get_device() if k_pages is not None else torch.cuda.current_device()
+        self.device = torch.device("cuda", index)
+        lead = (n_pages, n_kv_heads, page_size)
+        row, scale, kind = (lead + (head_dim,), None, dtype) if bits == 16 else (lead + (head_dim // 2,), lead + (head_dim // 64,), torch.uint8)
+
+        def pages(x, shape, dt):
+            if shape is None:
+                return None
+            if x is None:
+                return torch.zeros(shape, dtype=dt, device=self.device)
+            if x.dtype != dt or tuple(x.shape) != shape or not x.is_contiguous() or x.get_device() != index:
+                raise ValueError(f"pages must be contiguous {dt} of shape {shape} on cuda:{index}")
+            return x
+
+        self.k_pages, self.v_pages = pages(k_pages, row, kind), pages(v_pages, row, kind)
+        self.k_scales, self.v_scales = pages(k_scales, scale, torch.int16), pages(v_scales, scale, torch.int16)
+        ptr = lambda x: x.data_ptr() if x is not None else None  # noqa: E731
+        p = _KVParams(n_pages, page_size, n_heads, n_kv_heads, head_dim, _DTYPES[dtype], bits, index, ptr(self.k_pages),
+                      ptr(self.v_pages), ptr(self.k_scales), ptr(self.v_scales))
+        h = ctypes.c_void_p()
+        rc = lib.cofie_kv_create(ctypes.byref(p), ctypes.byref(h))
+        if rc != _abi.OK:
+            raise NGFFError(rc, lib.cofie_kv_last_error(None).decode())
+        self._lib, self._h, self._index = lib, h, index
+        self.n_pages, self.page_size, self.n_heads, self.n_kv_heads, self.head_dim = n_pages, page_size, n_heads, n_kv_heads, head_dim
+        self.dtype, self.bits, self.rotary = dtype, bits, rotary
+
+    def _check(self, rc):
+        if rc != _abi.OK:
+            raise NGFFError(rc, self._lib.cofie_kv_last_error(self._h).decode())
+
+    def _batch(self, table, lengths, offsets, n, max_new):
+        index = self._index
+        if table.dim() != 2 or table.dtype != torch.int32 or table.get_device() != index or table.stride(1) != 1 and table.shape[1] > 1:
+            raise ValueError(f"table must be an int32 tensor [sequences, pages] on cuda:{index} with contiguous rows")
+        seqs = table.shape[0]
+        if seqs > 1 and table.stride(0) != table.shape[1]:
+            raise ValueError("table must be contiguous")
+        return _Batch(seqs, n, max_new, table.shape[1], table.data_ptr(), _int32(lengths, index, "lengths", (seqs,)),
+                      None if offsets is None else _int32(offsets, index, "offsets", (seqs + 1,)))
+
+    def _rows(self, x, heads, what, n=None, out=None):
+        p, t, h, st, sh = _heads(x, self.dtype, self._index, what)
+        if h != heads or x.shape[2] != self.head_dim or n is not None and t != n:
+            raise ValueError(f"{what} must be [{'tokens' if n is None else n}, {heads}, {self.head_dim}]")
+        if out is None:
+            return _Rows(p, None, h, st, sh, 0, 0)
+        if out.shape != x.shape:
+            raise ValueError(f"the output of {what} must have its shape")
+        po, _, _, ot, oh = _heads(out, self.dtype, self._index, "the output of " + what)
+        return _Rows(p, po, h, st, sh, ot, oh)
+
+    def append(self, k, v, table, lengths, offsets=None, *, positions=None, q=None, q_out=None, cuda_stream=None):
+        """Puts the batch's new keys (rotated, where the cache has a rotary) and values into their pages; lengths count them
+        already. With q, its rotated copy is returned (in q_out, which may be q)."""
+        n = k.shape[0]
+        b = self._batch(table, lengths, offsets, n, 0)
+        kr, vr = self._rows(k, self.n_kv_heads, "k"), self._rows(v, self.n_kv_heads, "v", n)
+        if (self.rotary is None) != (positions is None):
+            raise ValueError("positions go with a cache that has a rotary")
+        qr = None
+        if q is not None:
+            if self.rotary is None:
+                raise ValueError("q goes with a cache that has a rotary")
+            if q_out is None:
+                with _allocating(cuda_stream, self._index):
+                    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            qr = ctypes.byref(self._rows(q, self.n_heads, "q", n, q_out))
+        at = None if positions is None else self.rotary._positions(positions, n, self._index)
+        self._check(self._lib.cofie_kv_append(self._h, ctypes.byref(b), ctypes.byref(kr), ctypes.byref(vr), qr,
+                                              None if self.rotary is None else self.rotary._h, at,
+                                              _stream_of(cuda_stream, self._index)))
+        return q_out if q is not None else None
+
+    def read(self, table, lengths, offsets=None, *, n_tokens=None, out=None, cuda_stream=None):
+        """(keys, values) [tokens, kv heads, head_dim] as the cache holds them at the batch's new tokens. The count of
+        tokens is that of ``out`` (a pair of tensors), n_tokens, or the sequences'."""
+        if out is None:
+            n = n_tokens if n_tokens is not None else table.shape[0]
+            with _allocating(cuda_stream, self._index):
+                out = tuple(torch.empty((n, self.n_kv_heads, self.head_dim), dtype=self.dtype, device=self.device) for _ in range(2))
+        k, v = out
+        n = k.shape[0]
+        for x in (k, v):
+            if x.dtype != self.dtype or tuple(x.shape) != (n, self.n_kv_heads, self.head_dim) or not x.is_contiguous() or x.get_device() != self._index:
+                raise ValueError(f"out must be contiguous {self.dtype} [tokens, {self.n_kv_heads}, {self.head_dim}] on cuda:{self._index}")
+        b = self._batch(table, lengths, offsets, n, 0)
+        self._check(self._lib.cofie_kv_read(self._h, ctypes.byref(b), k.data_ptr(), v.data_ptr(), _stream_of(cuda_stream, self._index)))
+        return k, v
+
+    def attend(self, q, table, lengths, offsets=None, *, max_new=0, mask=None, causal=True, scale=0.0, out=None, lse=None,
+               cuda_stream=None):
+        """(out, lse) of the batch's new queries over their sequences' cached tokens; out like q, lse fp32 [tokens, heads].
+        max_new: at least the largest count of new tokens (the fewer, the better the kernel chosen). mask: uint8
+        [sequences, >= the longest], nonzero where a cached token may be seen. scale 0: head_dim ** -0.5."""
+        n = q.shape[0]
+        if out is None or lse is None:
+            with _allocating(cuda_stream, self._index):
+                out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
+                lse = torch.empty((n, self.n_heads), dtype=torch.float32, device=q.device) if lse is None else lse
+        b = self._batch(table, lengths, offsets, n, 1 if offsets is None else max_new)
+        r = self._rows(q, self.n_heads, "q", None, out)
+        if lse.dtype != torch.float32 or tuple(lse.shape) != (n, self.n_heads) or not lse.is_contiguous() or lse.get_device() != self._index:
+            raise ValueError(f"lse must be a contiguous float32 tensor [{n}, {self.n_heads}] on cuda:{self._index}")
+        at, stride = None, 0
+        if mask is not None:
+            if mask.dtype not in (torch.uint8, torch.bool) or mask.dim() != 2 or mask.shape[0] != table.shape[0] or not mask.is_contiguous() \
+                    or mask.get_device() != self._index:
+                raise ValueError(f"mask must be a contiguous uint8 or bool tensor [{table.shape[0]}, tokens] on cuda:{self._index}")
+            at, stride = mask.data_ptr(), mask.shape[1]
+        self._check(self._lib.cofie_kv_attend(self._h, ctypes.byref(b), ctypes.byref(r), lse.data_ptr(), at, stride, causal, scale,
+                                              _stream_of(cuda_stream, self._index)))
+        return out, lse
+
+    def status(self, cuda_stream=None):
+        """Synchronises and raises NGFFError if a kernel met a page, a length or an offset out of range."""
+        self._check(self._lib.cofie_kv_status(self._h, _stream_of(cuda_stream, self._index)))
+
+    def close(self):
+        if getattr(self, "_h", None):
+            self._lib.cofie_kv_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:  # noqa: BLE001 -- interpreter shutdown
+            pass

@@ -1,105 +1,98 @@
-// Attention over the paged cache.
+// Attention over the paged cache: the entry point, the tiles that a mask
+// leaves, and the choice of the kernel.
 #include <algorithm>
 #include <cmath>
 
-#include "kv_handle.cuh"
+#include "kv_split.cuh"
 
 namespace cofie {
 namespace {
 
-constexpr int kWarps = 8;
+constexpr int kMaskThreads = 1024;
 
-struct AttendArgs {
-  BatchArg batch;
-  RowsArg q;
-  float* lse;
-  const uint8_t* mask;
-  uint64_t mask_stride;
-  const char* k;
-  const char* v;
-  const uint16_t* k_words;
-  const uint16_t* v_words;
-  uint32_t heads, group, causal;
-  float scale;
-};
-
-// D / 32 values of a cached row for this lane, in fp32.
-template <typename T, int D, int BITS>
-__device__ __forceinline__ void cached_values(const char* pages, const uint16_t* words, uint64_t row, uint32_t lane, float* x) {
-  constexpr int N = D / 32;
-  const uint32_t d = lane * N;
-  if (BITS == 16) {
-    const T* p = reinterpret_cast<const T*>(pages) + row * D + d;
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = Elem<T>::to(p[i]);
-  } else {
-    const uint8_t* p = reinterpret_cast<const uint8_t*>(pages) + (row * D + d) / 2;
-    const uint32_t word = words[row * (D / kGroup) + d / kGroup];
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = code_value(p[i / 2] >> (4 * (i % 2)) & 15u, word);
-  }
-}
-
-// A warp to a (token, head) row, one cached token after the other.
-template <typename T, int D, int BITS>
-__global__ void __launch_bounds__(32 * kWarps) attend_rows(const AttendArgs a) {
-  constexpr int N = D / 32;
+// The tiles of 64 cached tokens of which the mask leaves one at least, in
+// order, a CTA to a sequence: a thread looks at a tile, a scan gives it its place.
+__global__ void __launch_bounds__(kMaskThreads) visible_tiles(const BatchArg b, const uint8_t* mask, uint64_t mask_stride, uint32_t* tiles,
+                                                              uint32_t* count, uint32_t tile_stride) {
+  __shared__ uint32_t warps[kMaskThreads / 32];
   pdl_trigger();
   pdl_wait();
-  const uint32_t lane = threadIdx.x % 32;
-  const uint64_t row = blockIdx.x * static_cast<uint64_t>(kWarps) + threadIdx.x / 32;
-  if (row >= static_cast<uint64_t>(a.batch.n_tokens) * a.heads) return;
-  const uint32_t t = static_cast<uint32_t>(row / a.heads), head = static_cast<uint32_t>(row % a.heads);
-  const BatchArg& b = a.batch;
-  const uint32_t s = b.offsets ? sequence_of(b.offsets, b.n_seqs, t) : t;
-  if (s >= b.n_seqs) return;
-  const Span span = sequence_span(b, s);
-  if (t - span.first >= span.count) return;
-  const int64_t n = span.count, i = t - span.first, m = span.length;
-  const int64_t end = a.causal ? min(m, m - n + i + 1) : m;
-  const T* q = reinterpret_cast<const T*>(a.q.in) + t * a.q.in_token + head * a.q.in_head + lane * N;
-  float x[N], o[N], y[N], top = -INFINITY, sum = 0.f;
+  const uint32_t seq = blockIdx.x, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  const uint64_t length = min(static_cast<uint64_t>(sequence_span(b, seq).length), mask_stride);
+  const uint8_t* row = mask + seq * mask_stride;
+  const bool wide = reinterpret_cast<uintptr_t>(row) % 16 == 0;
+  uint32_t n = 0;
+  for (uint32_t t0 = 0; t0 * static_cast<uint64_t>(kTile) < length; t0 += kMaskThreads) {
+    const uint64_t first = (t0 + threadIdx.x) * static_cast<uint64_t>(kTile), end = min(length, first + kTile);
+    bool some = false;
+    if (wide && first + kTile <= length) {
 #pragma unroll
-  for (int e = 0; e < N; ++e) {
-    x[e] = Elem<T>::to(q[e]) * a.scale;
-    o[e] = 0.f;
-  }
-  for (int64_t j = 0; j < end; ++j) {
-    if (a.mask && (static_cast<uint64_t>(j) >= a.mask_stride || !a.mask[s * a.mask_stride + j])) continue;
-    const uint32_t page = static_cast<uint32_t>(b.table[static_cast<uint64_t>(s) * b.table_stride + (j >> b.page_shift)]);
-    if (page >= b.n_pages) {
-      if (lane == 0) atomicOr(b.err, kKvErrPage);
-      continue;
+      for (int i = 0; i < 4; ++i) {
+        const uint4 x = reinterpret_cast<const uint4*>(row + first)[i];
+        some |= (x.x | x.y | x.z | x.w) != 0;
+      }
+    } else {
+      for (uint64_t i = first; i < end; ++i) some |= row[i] != 0;
     }
-    const uint64_t r = page_row(b, (static_cast<int64_t>(page) << b.page_shift) | (j & ((1 << b.page_shift) - 1)), head / a.group);
-    cached_values<T, D, BITS>(a.k, a.k_words, r, lane, y);
-    float dot = 0.f;
-#pragma unroll
-    for (int e = 0; e < N; ++e) dot += x[e] * y[e];
-#pragma unroll
-    for (int w = 16; w > 0; w >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, w);
-    const float next = fmaxf(top, dot), keep = expf(top - next), p = expf(dot - next);
-    top = next;
-    sum = sum * keep + p;
-    cached_values<T, D, BITS>(a.v, a.v_words, r, lane, y);
-#pragma unroll
-    for (int e = 0; e < N; ++e) o[e] = o[e] * keep + p * y[e];
+    const uint32_t bits = __ballot_sync(0xffffffffu, some);
+    if (lane == 0) warps[warp] = __popc(bits);
+    __syncthreads();
+    uint32_t before = n, all = 0;
+    for (uint32_t w = 0; w < kMaskThreads / 32; ++w) {
+      if (w < warp) before += warps[w];
+      all += warps[w];
+    }
+    if (some) tiles[static_cast<uint64_t>(seq) * tile_stride + before + __popc(bits & ((1u << lane) - 1))] = t0 + threadIdx.x;
+    n += all;
+    __syncthreads();
   }
-  T* out = reinterpret_cast<T*>(a.q.out) + t * a.q.out_token + head * a.q.out_head + lane * N;
-#pragma unroll
-  for (int e = 0; e < N; ++e) out[e] = Elem<T>::from(sum > 0.f ? o[e] / sum : (sum == 0.f ? 0.f : sum));
-  if (a.lse && lane == 0) a.lse[row] = top + logf(sum);
+  if (threadIdx.x == 0) count[seq] = n;
 }
 
-template <typename T, int D>
-cudaError_t launch_attend(const AttendArgs& a, uint32_t bits, cudaStream_t st) {
-  const uint64_t rows = static_cast<uint64_t>(a.batch.n_tokens) * a.heads;
-  const dim3 grid(static_cast<uint32_t>((rows + kWarps - 1) / kWarps)), block(32 * kWarps);
-  return bits == 4 ? launch_dependent(true, attend_rows<T, D, 4>, grid, block, 0, st, a)
-                   : launch_dependent(true, attend_rows<T, D, 16>, grid, block, 0, st, a);
+template <typename F>
+auto for_type(const cofie_kv_params& p, F f) {
+  if (p.dtype == COFIE_BF16) return f(__nv_bfloat16());
+  return f(__half());
+}
+
+// The kernel of the handle's type, head length and pages, for 8 << i rows.
+using SplitKernel = void (*)(AttendArgs);
+template <typename T, int D, int BITS>
+SplitKernel split_kernel(int i, size_t* smem) {
+  *smem = i == 0 ? split_smem<D, BITS, 1>() : i == 1 ? split_smem<D, BITS, 2>() : split_smem<D, BITS, 4>();
+  return i == 0 ? attend_split<T, D, BITS, 1> : i == 1 ? attend_split<T, D, BITS, 2> : attend_split<T, D, BITS, 4>;
+}
+SplitKernel split_kernel(const cofie_kv_params& p, int i, size_t* smem) {
+  return for_type(p, [&](auto x) {
+    using T = decltype(x);
+    if (p.head_dim == 64) return p.bits == 4 ? split_kernel<T, 64, 4>(i, smem) : split_kernel<T, 64, 16>(i, smem);
+    return p.bits == 4 ? split_kernel<T, 128, 4>(i, smem) : split_kernel<T, 128, 16>(i, smem);
+  });
 }
 
 }  // namespace
+
+cudaError_t attend_set_up(cofie_kv* h) {
+  cudaError_t e = cudaSuccess;
+  size_t rows = 0, ctas = 0;
+  for (int i = 0; i < 3 && e == cudaSuccess; ++i) {
+    size_t smem = 0;
+    const SplitKernel k = split_kernel(h->p, i, &smem);
+    int per_sm = 0;
+    e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, k, kSplitThreads, smem);
+    if (e == cudaSuccess && per_sm < 1) e = cudaErrorInvalidConfiguration;
+    h->split_ctas[i] = sm_count() * static_cast<uint32_t>(per_sm);
+    ctas = std::max<size_t>(ctas, h->split_ctas[i]);
+    rows = std::max<size_t>(rows, 2ull * h->split_ctas[i] * (8u << i));
+  }
+  if (e == cudaSuccess) e = cudaMalloc(&h->d_part, rows * h->p.head_dim * sizeof(float));
+  if (e == cudaSuccess) e = cudaMalloc(&h->d_part_ms, rows * sizeof(float2));
+  if (e == cudaSuccess) e = cudaMalloc(&h->d_done, ctas * sizeof(uint32_t));
+  if (e == cudaSuccess) e = cudaMemset(h->d_done, 0, ctas * sizeof(uint32_t));
+  return e;
+}
+
 }  // namespace cofie
 
 using namespace cofie;
@@ -113,22 +106,58 @@ extern "C" int cofie_kv_attend(cofie_kv_t* h, const cofie_kv_batch* b, const cof
   if (const int rc = check_rows(h, q, h->p.n_heads, true, "q")) return rc;
   if (!(scale >= 0.f && std::isfinite(scale))) return h->fail(COFIE_EINVAL, "scale must be finite and not negative");
   DeviceGuard g(h->device);
-  const AttendArgs a{batch_arg(h, b),
-                     {static_cast<const char*>(q->in), static_cast<char*>(q->out), q->in_token, q->in_head, q->out_token, q->out_head, q->heads, kRotate},
-                     lse,
-                     mask,
-                     mask_stride,
-                     static_cast<const char*>(h->p.k_pages),
-                     static_cast<const char*>(h->p.v_pages),
-                     h->p.k_scales,
-                     h->p.v_scales,
-                     h->p.n_heads,
-                     h->p.n_heads / h->p.n_kv_heads,
-                     causal != 0,
-                     scale > 0.f ? scale : 1.f / std::sqrt(static_cast<float>(h->p.head_dim))};
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  const bool bf = h->p.dtype == COFIE_BF16;
-  const cudaError_t e = h->p.head_dim == 64 ? (bf ? launch_attend<__nv_bfloat16, 64>(a, h->p.bits, st) : launch_attend<__half, 64>(a, h->p.bits, st))
-                                            : (bf ? launch_attend<__nv_bfloat16, 128>(a, h->p.bits, st) : launch_attend<__half, 128>(a, h->p.bits, st));
-  return launched(h, e, "attend");
+  const auto aligned = [](const void* p, int64_t token, int64_t head, uint32_t elems) {
+    return reinterpret_cast<uintptr_t>(p) % (2 * elems) == 0 && token % elems == 0 && head % elems == 0;
+  };
+  AttendArgs a{};
+  a.batch = batch_arg(h, b);
+  a.q = {static_cast<const char*>(q->in), static_cast<char*>(q->out), q->in_token, q->in_head, q->out_token, q->out_head, q->heads, kRotate};
+  a.lse = lse;
+  a.mask = mask;
+  a.mask_stride = mask_stride;
+  a.k = static_cast<const char*>(h->p.k_pages);
+  a.v = static_cast<const char*>(h->p.v_pages);
+  a.k_words = h->p.k_scales;
+  a.v_words = h->p.v_scales;
+  a.heads = h->p.n_heads;
+  a.group = h->p.n_heads / h->p.n_kv_heads;
+  a.causal = causal != 0;
+  a.q_wide = aligned(q->in, q->in_token, q->in_head, 8);
+  a.out_wide = aligned(q->out, q->out_token, q->out_head, 4);
+  a.scale = scale > 0.f ? scale : 1.f / std::sqrt(static_cast<float>(h->p.head_dim));
+  a.part = h->d_part;
+  a.part_ms = h->d_part_ms;
+  a.done = h->d_done;
+  if (mask) {
+    a.tile_stride = (b->table_stride << h->page_shift) / kTile + 1;
+    const size_t room = static_cast<size_t>(b->n_seqs) * (a.tile_stride + 1);
+    if (room > h->tiles_room) {
+      cudaStreamCaptureStatus cs = cudaStreamCaptureStatusNone;
+      if (cudaStreamIsCapturing(st, &cs) != cudaSuccess || cs != cudaStreamCaptureStatusNone) {
+        cudaGetLastError();
+        return h->fail(COFIE_EINVAL, "the first masked call of this size must come before the capture");
+      }
+      uint32_t* more = nullptr;
+      const cudaError_t e = injected_alloc_failure() ? cudaErrorMemoryAllocation : cudaMalloc(&more, room * sizeof(uint32_t));
+      if (e != cudaSuccess) {
+        cudaGetLastError();
+        return h->fail(e == cudaErrorMemoryAllocation ? COFIE_ENOMEM : COFIE_ECUDA, "no room for the list of the mask's tiles");
+      }
+      cudaFree(h->d_tiles);  // waits for the calls that read it
+      h->d_tiles = more;
+      h->tiles_room = room;
+    }
+    a.tiles = h->d_tiles;
+    a.tile_count = h->d_tiles + static_cast<size_t>(b->n_seqs) * a.tile_stride;
+    if (const int rc = launched(h, launch_dependent(true, visible_tiles, dim3(b->n_seqs), dim3(kMaskThreads), 0, st, a.batch, mask, mask_stride,
+                                                    h->d_tiles, const_cast<uint32_t*>(a.tile_count), a.tile_stride),
+                                "attend"))
+      return rc;
+  }
+  const uint64_t rows = static_cast<uint64_t>(b->offsets ? (b->max_new ? b->max_new : b->n_tokens) : 1) * a.group;
+  const int i = rows <= 8 ? 0 : rows <= 16 ? 1 : 2;
+  size_t smem = 0;
+  const SplitKernel k = split_kernel(h->p, i, &smem);
+  return launched(h, launch_dependent(true, k, dim3(h->split_ctas[i]), dim3(kSplitThreads), smem, st, a), "attend");
 }

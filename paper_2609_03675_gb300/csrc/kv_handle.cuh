@@ -10,6 +10,14 @@ struct cofie_kv {
   int device = 0;
   uint32_t page_shift = 0;
   uint32_t* d_err = nullptr;
+  // attention: CTAs that fit the GPU at once for 8, 16 and 32 rows each, the
+  // parts that they leave, and the tiles that a mask leaves (grown on demand)
+  uint32_t split_ctas[3] = {0, 0, 0};
+  float* d_part = nullptr;
+  float2* d_part_ms = nullptr;
+  uint32_t* d_done = nullptr;
+  uint32_t* d_tiles = nullptr;
+  size_t tiles_room = 0;
   std::string err;
   int fail(int code, const std::string& m) {
     err = m;
@@ -35,6 +43,9 @@ int check_batch(cofie_kv* h, const cofie_kv_batch* b);
 int check_rows(cofie_kv* h, const cofie_rows* r, uint32_t heads, bool has_out, const char* name);
 BatchArg batch_arg(const cofie_kv* h, const cofie_kv_batch* b);
 int launched(cofie_kv* h, cudaError_t e, const char* what);
+
+// Allocates the attention's scratch (the handle's other fields are set).
+cudaError_t attend_set_up(cofie_kv* h);
 
 cudaError_t launch_rows(RowsArgs a, const RotaryTable& tab, uint32_t head_dim, uint32_t dtype, cudaStream_t st);
 

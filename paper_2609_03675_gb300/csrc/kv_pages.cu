@@ -186,7 +186,9 @@ void kv_free(cofie_kv* h) {
   if (!h) return;
   DeviceGuard g(h->device);
   cudaDeviceSynchronize();
-  if (h->d_err) cudaFree(h->d_err);
+  for (void* x : {static_cast<void*>(h->d_err), static_cast<void*>(h->d_part), static_cast<void*>(h->d_part_ms), static_cast<void*>(h->d_done),
+                  static_cast<void*>(h->d_tiles)})
+    if (x) cudaFree(x);
   delete h;
 }
 
@@ -264,6 +266,7 @@ int cofie_kv_create(const cofie_kv_params* p, cofie_kv_t** out) {
   h->page_shift = shift;
   cudaError_t e = injected_alloc_failure() ? cudaErrorMemoryAllocation : cudaMalloc(&h->d_err, sizeof(uint32_t));
   if (e == cudaSuccess) e = cudaMemset(h->d_err, 0, sizeof(uint32_t));
+  if (e == cudaSuccess) e = attend_set_up(h);
   if (e != cudaSuccess) {
     g_kv_error = std::string("cache set-up failed: ") + cudaGetErrorString(e);
     cudaGetLastError();

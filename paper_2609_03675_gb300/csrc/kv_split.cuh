@@ -15,12 +15,25 @@
 // memory after the codes are unpacked.) S^T leaves the tensor core as a
 // fragment of tokens by rows; movmatrix turns it into P^T's.
 //
-// 4-bit codes enter the products without being scaled. A code n becomes the
-// 16-bit number 128 + n (bf16) or 1024 + n (fp16) by one logic operation on two
-// codes. For keys, whose scale is one factor of a score's 64 terms, the score
-// is s (sum q (128 + n) - (128 + z) sum q), in fp32. Values have a scale for
-// each token, inside the sum: (n - z) s is formed, exactly, in two more
-// operations on two values.
+// 4-bit codes enter the products as they are: a 16-bit number whose low four
+// bits are the code and whose others are clear is the fp16 number n 2^-24 (a
+// subnormal, which the tensor cores take like any other), and with the code
+// four bits higher 16 n 2^-24. So one logic operation unpacks two codes, and
+// one shift in eight of them; the 16 and the 2^24 are taken off q and the
+// results. Everything else is on the side of the few rows:
+//   q      is brought to fp16 by a power of two for each row (its largest
+//          value in [128, 256)), which keeps bf16's and fp16's bits;
+//   keys   score = s (sum q n - z sum q), s one factor of a group's 64 terms;
+//          z sum q comes from one more product, whose operands are the zero
+//          points and sum q as three fp16 numbers;
+//   values the sum over tokens has a scale for each: p s is rounded to fp16,
+//          after a power of two that keeps the largest scale met so far below
+//          2^15 (raised, and the output so far brought down, when a larger one
+//          comes). z is taken off the code, in fp16, exactly: taken off the
+//          sums, as the keys' is, it would cost half the operations, but a sum
+//          of values near zero would carry the rounding of sums of codes.
+// 262144 tokens, 8 heads of 128, 4 query heads each: unpacked to (n - z) s for
+// values and 128 + n for keys the kernel took 108 us, its ALU pipe 70 % busy.
 #pragma once
 
 #include "kv_plan.cuh"
@@ -33,9 +46,6 @@ constexpr int kSplitThreads = 32 * kSplitWarps;
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool live) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src, bool live) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(live ? 4 : 0) : "memory");
 }
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -84,21 +94,10 @@ template <typename T>
 struct Pair;  // two 16-bit values in a register
 template <>
 struct Pair<__nv_bfloat16> {
-  static constexpr uint32_t kMagic = 0x43004300u;  // 128 + n
-  static constexpr float kExcess = 128.f;
   static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
     const __nv_bfloat162 x = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&x);
   }
-  static __device__ __forceinline__ uint32_t sub(uint32_t a, uint32_t b) {
-    const __nv_bfloat162 x = __hsub2(*reinterpret_cast<__nv_bfloat162*>(&a), *reinterpret_cast<__nv_bfloat162*>(&b));
-    return *reinterpret_cast<const uint32_t*>(&x);
-  }
-  static __device__ __forceinline__ uint32_t mul(uint32_t a, uint32_t b) {
-    const __nv_bfloat162 x = __hmul2(*reinterpret_cast<__nv_bfloat162*>(&a), *reinterpret_cast<__nv_bfloat162*>(&b));
-    return *reinterpret_cast<const uint32_t*>(&x);
-  }
-  static __device__ __forceinline__ uint32_t scales(uint32_t w) { return w & 0xFFF0FFF0u; }
   static __device__ __forceinline__ float lo(uint32_t x) { return __uint_as_float(x << 16); }
   static __device__ __forceinline__ float hi(uint32_t x) { return __uint_as_float(x & 0xFFFF0000u); }
   static __device__ __forceinline__ void mma(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
@@ -110,8 +109,6 @@ struct Pair<__nv_bfloat16> {
 };
 template <>
 struct Pair<__half> {
-  static constexpr uint32_t kMagic = 0x64006400u;  // 1024 + n
-  static constexpr float kExcess = 1024.f;
   static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
     const __half2 x = __floats2half2_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&x);
@@ -119,13 +116,6 @@ struct Pair<__half> {
   static __device__ __forceinline__ uint32_t sub(uint32_t a, uint32_t b) {
     const __half2 x = __hsub2(*reinterpret_cast<__half2*>(&a), *reinterpret_cast<__half2*>(&b));
     return *reinterpret_cast<const uint32_t*>(&x);
-  }
-  static __device__ __forceinline__ uint32_t mul(uint32_t a, uint32_t b) {
-    const __half2 x = __hmul2(*reinterpret_cast<__half2*>(&a), *reinterpret_cast<__half2*>(&b));
-    return *reinterpret_cast<const uint32_t*>(&x);
-  }
-  static __device__ __forceinline__ uint32_t scales(uint32_t w) {  // bf16 words to fp16
-    return pack(__uint_as_float((w & 0xFFF0u) << 16), __uint_as_float(w & 0xFFF00000u));
   }
   static __device__ __forceinline__ float lo(uint32_t x) { return __half2float(__ushort_as_half(static_cast<unsigned short>(x))); }
   static __device__ __forceinline__ float hi(uint32_t x) { return __half2float(__ushort_as_half(static_cast<unsigned short>(x >> 16))); }
@@ -136,6 +126,10 @@ struct Pair<__half> {
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
   }
 };
+
+// The scales of a register of two words (the high half's, the low half's).
+__device__ __forceinline__ float scale_hi(uint32_t w) { return __uint_as_float(w & 0xFFF00000u); }
+__device__ __forceinline__ float scale_lo(uint32_t w) { return __uint_as_float((w << 16) & 0xFFF00000u); }
 
 // Sizes of one warp's ring. Chunks of 32 tokens of codes, 16 of 16-bit values.
 template <int D, int BITS>
@@ -165,12 +159,13 @@ __device__ __forceinline__ uint32_t unit_at(uint32_t t, uint32_t u) {
 template <typename T, int D, int BITS, int NT>
 __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) attend_split(const __grid_constant__ AttendArgs a) {
   using P = Pair<T>;
+  using H = Pair<__half>;
   using R = Ring<D, BITS>;
   constexpr int kRows = 8 * NT, kGroups = D / 64, kM = R::kTokens / 16, kPerTile = kTile / R::kTokens;
   extern __shared__ __align__(128) char smem[];
   __shared__ Plan<kSplitThreads> plan;
   __shared__ float warp_m[kSplitWarps][kRows], warp_l[kSplitWarps][kRows];
-  __shared__ uint32_t seen_bits[kSplitWarps][R::kStages];
+  __shared__ uint2 stages[kSplitWarps][R::kStages];  // the bits of the tokens that are seen, and the first one's place
   __shared__ uint32_t last_here;
   pdl_trigger();
   pdl_wait();
@@ -179,15 +174,15 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
   Walk<kSplitThreads> walk(a, plan, kRows, range);
   const uint32_t ring = shared_address(smem) + warp * R::kWarp;
   const BatchArg& b = a.batch;
-  const float scale = a.scale * 1.4426950408889634f;  // scores in base 2
   Item it;
   while (walk.next(it)) {
     const uint32_t row0 = it.rb * kRows;
     const uint32_t rows = min(static_cast<uint32_t>(kRows), it.span.count * a.group - row0);
     // ---- queries: fragments of Q^T, the columns of this lane's dims in the order in which the keys' lie in registers
     uint32_t qf[NT][D / 16][2];
-    float qsum[NT][2][kGroups];  // 4-bit: sum of q over a group, of rows 2c and 2c + 1
-    int32_t seen[NT][2];         // tokens that rows 2c and 2c + 1 may see
+    uint32_t qz[BITS == 4 ? NT : 1];  // a part of -sum q over the two groups, for the zero points
+    float by[NT][2];                  // what takes the scores of rows 2c and 2c + 1 to base 2
+    int32_t seen[NT][2];              // tokens that they may see
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const uint32_t r = nt * 8 + g;
@@ -196,52 +191,84 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
       const T* q = reinterpret_cast<const T*>(a.q.in) + (real ? static_cast<int64_t>(it.span.first + i) * a.q.in_token +
                                                                     static_cast<int64_t>(it.head * a.group + j) * a.q.in_head
                                                               : 0);
+      uint4 x[D / 32];
 #pragma unroll
       for (int e = 0; e < D / 32; ++e) {
         // eight dims: 16-bit keys: unit 4 e + c of the row; codes: word e % 2 of the lane's two words in group e / 2
         const uint32_t d = BITS == 16 ? (4 * e + c) * 8 : (e / 2) * 64 + c * 16 + (e % 2) * 8;
-        uint4 x = make_uint4(0, 0, 0, 0);
+        x[e] = make_uint4(0, 0, 0, 0);
         if (real) {
           if (a.q_wide) {
-            x = *reinterpret_cast<const uint4*>(q + d);
+            x[e] = *reinterpret_cast<const uint4*>(q + d);
           } else {
             RowVec<T, 8> y;
 #pragma unroll
             for (int f = 0; f < 8; ++f) y.v[f] = q[d + f];
-            x = *reinterpret_cast<uint4*>(&y);
+            x[e] = *reinterpret_cast<uint4*>(&y);
           }
         }
-        if (BITS == 16) {
-          qf[nt][2 * e][0] = x.x;
-          qf[nt][2 * e][1] = x.y;
-          qf[nt][2 * e + 1][0] = x.z;
-          qf[nt][2 * e + 1][1] = x.w;
-        } else {  // codes come out of a word as (0, 4), (1, 5), (2, 6), (3, 7)
-          qf[nt][2 * e][0] = __byte_perm(x.x, x.z, 0x5410);
-          qf[nt][2 * e][1] = __byte_perm(x.x, x.z, 0x7632);
-          qf[nt][2 * e + 1][0] = __byte_perm(x.y, x.w, 0x5410);
-          qf[nt][2 * e + 1][1] = __byte_perm(x.y, x.w, 0x7632);
-        }
       }
-      if (BITS == 4) {
+      const float scale = a.scale * 1.4426950408889634f;
+      if (BITS == 16) {
 #pragma unroll
-        for (int gr = 0; gr < kGroups; ++gr) {
+        for (int e = 0; e < D / 32; ++e) {
+          qf[nt][2 * e][0] = x[e].x;
+          qf[nt][2 * e][1] = x[e].y;
+          qf[nt][2 * e + 1][0] = x[e].z;
+          qf[nt][2 * e + 1][1] = x[e].w;
+        }
+        by[nt][0] = by[nt][1] = scale;
+      } else {
+        float most = 0.f, sum[kGroups];
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) {
+          const uint32_t w[4] = {x[e].x, x[e].y, x[e].z, x[e].w};
           float s = 0.f;
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
+          for (int f = 0; f < 4; ++f) {
+            most = fmaxf(most, fmaxf(fabsf(P::lo(w[f])), fabsf(P::hi(w[f]))));
+            s += P::lo(w[f]) + P::hi(w[f]);
+          }
+          sum[e / 2] = e % 2 ? sum[e / 2] + s : s;
+        }
+        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+        // the power of two that brings `most` to [128, 256); 1 for a row of zeros or with an infinity
+        const int ex = most > 0.f && most <= 3.402823466e38f ? max(static_cast<int>(__float_as_uint(most) >> 23) - 127, -100) : 7;
+        const float up = __uint_as_float(static_cast<uint32_t>(127 + 7 - ex) << 23), odd = up * 0.0625f;
 #pragma unroll
-            for (int f = 0; f < 2; ++f) s += P::lo(qf[nt][4 * gr + e][f]) + P::hi(qf[nt][4 * gr + e][f]);
+        for (int e = 0; e < D / 32; ++e) {
+          // codes come out of a word as (0, 4), 16 (1, 5), (2, 6), 16 (3, 7)
+          qf[nt][2 * e][0] = H::pack(P::lo(x[e].x) * up, P::lo(x[e].z) * up);
+          qf[nt][2 * e][1] = H::pack(P::hi(x[e].x) * odd, P::hi(x[e].z) * odd);
+          qf[nt][2 * e + 1][0] = H::pack(P::lo(x[e].y) * up, P::lo(x[e].w) * up);
+          qf[nt][2 * e + 1][1] = H::pack(P::hi(x[e].y) * odd, P::hi(x[e].w) * odd);
+        }
+        // column slots 2c (first group) and 2c + 1 (second) of the zero points' product: a third of -sum q to each of
+        // three lanes
+        uint32_t parts[3] = {0, 0, 0};
+#pragma unroll
+        for (int gr = 0; gr < kGroups; ++gr) {
+          float s = -sum[gr] * up;
           s += __shfl_xor_sync(0xffffffffu, s, 1);
           s += __shfl_xor_sync(0xffffffffu, s, 2);
-          qsum[nt][0][gr] = __shfl_sync(0xffffffffu, s, 8 * c);
-          qsum[nt][1][gr] = __shfl_sync(0xffffffffu, s, 8 * c + 4);
+#pragma unroll
+          for (int f = 0; f < 3; ++f) {
+            const __half p = __float2half_rn(s);
+            s -= __half2float(p);
+            parts[f] |= static_cast<uint32_t>(__half_as_ushort(p)) << (16 * gr);
+          }
         }
+        qz[nt] = c == 0 ? parts[0] : c == 1 ? parts[1] : c == 2 ? parts[2] : 0u;
+        const float back = scale * __uint_as_float(static_cast<uint32_t>(127 - 7 + ex) << 23) * 0x1p24f;
+        by[nt][0] = __shfl_sync(0xffffffffu, back, 8 * c);
+        by[nt][1] = __shfl_sync(0xffffffffu, back, 8 * c + 4);
       }
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const uint32_t x = nt * 8 + 2 * c + e;
-        const int64_t n = a.causal ? static_cast<int64_t>(it.span.length) - it.span.count + (row0 + x) / a.group + 1 : it.span.length;
-        seen[nt][e] = x < rows && n > 0 ? static_cast<int32_t>(n) : 0;
+        const uint32_t y = nt * 8 + 2 * c + e;
+        const int64_t n = a.causal ? static_cast<int64_t>(it.span.length) - it.span.count + (row0 + y) / a.group + 1 : it.span.length;
+        seen[nt][e] = y < rows && n > 0 ? static_cast<int32_t>(n) : 0;
       }
     }
     // the fewest tokens that a row sees: below it, only the mask matters
@@ -251,6 +278,8 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
       all_see = n > 0 ? static_cast<int32_t>(n) : 0;
     }
     float o[NT][D / 16][4], m[NT][2], l[NT][2];
+    float v_up = 1.f;               // 4-bit: the power of two on p s
+    uint32_t v_most = 0x000F000Fu;  // words up to which it holds, twice
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -259,63 +288,78 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
       l[nt][0] = l[nt][1] = 0.f;
     }
 
-    // ---- the warp's chunks: warp, warp + 8, ... of the item's part
+    // ---- the warp's chunks: warp, warp + 8, ... of the item's part. A chunk's blocks of 16 tokens lie in one page each,
+    // one behind the other.
     const uint32_t chunks = (it.hi - it.lo) * kPerTile;
     const int32_t* table = b.table + static_cast<uint64_t>(it.seq) * b.table_stride;
-    const auto chunk_pos = [&](uint32_t ch) {
-      const uint32_t t = it.lo + ch / kPerTile;
-      return (a.mask ? a.tiles[static_cast<uint64_t>(it.seq) * a.tile_stride + t] : t) * kTile + (ch % kPerTile) * R::kTokens;
+    const uint8_t* mask = a.mask + it.seq * a.mask_stride;
+    struct Ahead {
+      uint32_t pos, page[kM];  // page: n_pages and above where there is none
+      bool seen;               // this lane's token
     };
-    // the row in the pages of this lane's token of a chunk, -1 where there is nothing to see
-    const auto token_row = [&](uint32_t ch) -> int64_t {
-      if (ch >= chunks) return -1;
-      const uint32_t pos = chunk_pos(ch) + lane % R::kTokens;
-      if (pos >= it.span.length) return -1;
-      if (a.mask && (pos >= a.mask_stride || !a.mask[it.seq * a.mask_stride + pos])) return -1;
-      const uint32_t page = static_cast<uint32_t>(table[pos >> b.page_shift]);
-      if (page >= b.n_pages) {
-        atomicOr(b.err, kKvErrPage);
-        return -1;
+    const auto look = [&](uint32_t ch) {
+      Ahead x;
+      x.pos = 0;
+      x.seen = false;
+#pragma unroll
+      for (int mt = 0; mt < kM; ++mt) x.page[mt] = ~0u;
+      if (ch < chunks) {
+        const uint32_t t = it.lo + ch / kPerTile;
+        x.pos = (a.mask ? a.tiles[static_cast<uint64_t>(it.seq) * a.tile_stride + t] : t) * kTile + (ch % kPerTile) * R::kTokens;
+#pragma unroll
+        for (int mt = 0; mt < kM; ++mt)
+          if (x.pos + 16 * mt < it.span.length) x.page[mt] = static_cast<uint32_t>(table[(x.pos + 16 * mt) >> b.page_shift]);
+        const uint32_t p = x.pos + lane % R::kTokens;
+        x.seen = p < it.span.length && (!a.mask || (p < a.mask_stride && mask[p] != 0));
       }
-      return static_cast<int64_t>(page_row(b, (static_cast<int64_t>(page) << b.page_shift) | (pos & ((1u << b.page_shift) - 1)), it.head));
+      return x;
     };
-    const auto issue = [&](uint32_t stage, int64_t row) {
+    const auto issue = [&](uint32_t stage, const Ahead& x) {
       const uint32_t base = ring + stage * R::kStage;
-      const uint32_t bits = __ballot_sync(0xffffffffu, row >= 0);
-      if (lane == 0) seen_bits[warp][stage] = bits;
+      uint32_t bits = __ballot_sync(0xffffffffu, x.seen);
       if (bits) {
 #pragma unroll
-        for (int i = 0; i < R::kTokens * R::kUnits / 32; ++i) {
-          const uint32_t x = i * 32 + lane, t = x / R::kUnits, u = x % R::kUnits;
-          const int64_t r = __shfl_sync(0xffffffffu, row, t);
-          const uint64_t off = r < 0 ? 0 : static_cast<uint64_t>(r) * R::kRow + u * 16;
-          cp_async16(base + unit_at<D, BITS, false>(t, u), a.k + off, r >= 0);
-          cp_async16(base + R::kTokens * R::kRow + unit_at<D, BITS, true>(t, u), a.v + off, r >= 0);
-        }
-        if (BITS == 4) {
-          const uint32_t dst = base + 2 * R::kTokens * R::kRow + lane * 4;
-          if (D == 128) {
-            const uint64_t off = row < 0 ? 0 : static_cast<uint64_t>(row) * 2;
-            cp_async4(dst, a.k_words + off, row >= 0);
-            cp_async4(dst + R::kWords, a.v_words + off, row >= 0);
-          } else {  // the words of two tokens, which lie in one page, to a lane
-            const int64_t r0 = __shfl_sync(0xffffffffu, row, lane * 2 % 32), r1 = __shfl_sync(0xffffffffu, row, (lane * 2 + 1) % 32);
-            const int64_t r = r0 >= 0 ? r0 : r1 - 1;
-            if (lane < 16) {
-              cp_async4(dst, a.k_words + (r < 0 ? 0 : r), r >= 0);
-              cp_async4(dst + R::kWords, a.v_words + (r < 0 ? 0 : r), r >= 0);
+        for (int mt = 0; mt < kM; ++mt) {
+          const uint32_t half = 0xFFFFu << (16 * mt);
+          if ((bits & half) && x.page[mt] >= b.n_pages) {
+            if (lane == 0) atomicOr(b.err, kKvErrPage);
+            bits &= BITS == 16 ? 0u : ~half;
+          }
+          const bool there = (bits & half) != 0;
+          if (BITS == 4 && !there) continue;  // what the ring holds there is masked below
+          const uint64_t row = there ? ((static_cast<uint64_t>(x.page[mt]) * b.kv_heads + it.head) << b.page_shift) +
+                                           ((x.pos + 16 * mt) & ((1u << b.page_shift) - 1))
+                                     : 0;
+          const char* k = a.k + row * R::kRow + lane * 16;
+          const char* v = a.v + row * R::kRow + lane * 16;
+#pragma unroll
+          for (int i = 0; i < R::kUnits / 2; ++i) {  // 32 units of 16 bytes
+            const uint32_t t = (i * 32 + lane) / R::kUnits, u = lane % R::kUnits;
+            // 16-bit values that nobody sees become zeros (a NaN among them would pass through a product with 0)
+            const bool live = BITS == 4 || ((bits >> t) & 1u);
+            cp_async16(base + unit_at<D, BITS, false>(16 * mt + t, u), k + i * 512, live);
+            cp_async16(base + R::kTokens * R::kRow + unit_at<D, BITS, true>(16 * mt + t, u), v + i * 512, live);
+          }
+          if (BITS == 4) {  // the block's words: D / 2 bytes of the keys', as many of the values'
+            constexpr uint32_t kLanes = D / 32;
+            static_assert(R::kWords / kM == 16 * kLanes || BITS == 16, "16 bytes to a lane");
+            if (lane < 2 * kLanes) {
+              const uint32_t v2 = lane / kLanes, u = lane % kLanes;
+              cp_async16(base + 2 * R::kTokens * R::kRow + v2 * R::kWords + mt * (R::kWords / kM) + u * 16,
+                         (v2 ? a.v_words : a.k_words) + row * (D / 64) + u * 8, true);
             }
           }
         }
       }
+      if (lane == 0) stages[warp][stage] = make_uint2(bits, x.pos);
       cp_async_commit();
     };
-    int64_t ahead;
+    Ahead ahead;
     {
-      int64_t first[R::kStages - 1];
+      Ahead first[R::kStages - 1];
 #pragma unroll
-      for (int s = 0; s < R::kStages - 1; ++s) first[s] = token_row(warp + s * kSplitWarps);
-      ahead = token_row(warp + (R::kStages - 1) * kSplitWarps);
+      for (int s = 0; s < R::kStages - 1; ++s) first[s] = look(warp + s * kSplitWarps);
+      ahead = look(warp + (R::kStages - 1) * kSplitWarps);
 #pragma unroll
       for (int s = 0; s < R::kStages - 1; ++s) issue(s, first[s]);
     }
@@ -323,12 +367,12 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
     for (uint32_t ch = warp; ch < chunks; ch += kSplitWarps) {
       cp_async_wait<R::kStages - 2>();
       __syncwarp();
-      const uint32_t base = ring + stage * R::kStage, bits = seen_bits[warp][stage];
+      const uint32_t base = ring + stage * R::kStage, bits = stages[warp][stage].x;
+      const int32_t pos = static_cast<int32_t>(stages[warp][stage].y);
       issue(stage == 0 ? R::kStages - 1 : stage - 1, ahead);  // the stage read in the iteration before
-      ahead = token_row(ch + R::kStages * kSplitWarps);
+      ahead = look(ch + R::kStages * kSplitWarps);
       if (++stage == R::kStages) stage = 0;
       if (bits == 0) continue;
-      const int32_t pos = static_cast<int32_t>(chunk_pos(ch));
       const bool whole = (BITS == 4 ? bits == 0xffffffffu : (bits & 0xffffu) == 0xffffu);
       const uint32_t vbase = base + R::kTokens * R::kRow, kw = base + 2 * R::kTokens * R::kRow, vw = kw + R::kWords;
 
@@ -352,10 +396,6 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
               P::mma(s[nt][mt], f1, qf[nt][2 * e + 1][0], qf[nt][2 * e + 1][1]);
             }
           }
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[nt][mt][e] *= scale;
         } else {
           uint32_t w0, w1;  // the words of tokens t0 and t0 + 8
           if (D == 128) {
@@ -370,26 +410,26 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
             const uint2 x = lds64(base + unit_at<D, BITS, false>(t0, gr * 2 + c / 2) + (c % 2) * 8);
             const uint2 y = lds64(base + unit_at<D, BITS, false>(t0 + 8, gr * 2 + c / 2) + (c % 2) * 8);
             float acc[NT][4];
+            const uint32_t only = gr == 0 ? 0x0000000Fu : 0x000F0000u;  // the group's zero point, in its slot
+            const uint32_t z[4] = {w0 & only, w1 & only, 0u, 0u};
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) acc[nt][0] = acc[nt][1] = acc[nt][2] = acc[nt][3] = 0.f;
+            for (int nt = 0; nt < NT; ++nt) {
+              acc[nt][0] = acc[nt][1] = acc[nt][2] = acc[nt][3] = 0.f;
+              H::mma(acc[nt], z, qz[nt], 0u);
+            }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const uint32_t u = (e < 2 ? x.x : x.y) >> (8 * (e % 2)), v = (e < 2 ? y.x : y.y) >> (8 * (e % 2));
-              const uint32_t f[4] = {(u & 0x000F000Fu) | P::kMagic, (v & 0x000F000Fu) | P::kMagic, ((u >> 4) & 0x000F000Fu) | P::kMagic,
-                                     ((v >> 4) & 0x000F000Fu) | P::kMagic};
+              const uint32_t f[4] = {u & 0x000F000Fu, v & 0x000F000Fu, u & 0x00F000F0u, v & 0x00F000F0u};
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt) P::mma(acc[nt], f, qf[nt][4 * gr + e][0], qf[nt][4 * gr + e][1]);
+              for (int nt = 0; nt < NT; ++nt) H::mma(acc[nt], f, qf[nt][4 * gr + e][0], qf[nt][4 * gr + e][1]);
             }
-            const uint32_t h0 = D == 128 && gr == 1 ? w0 >> 16 : w0 & 0xFFFFu, h1 = D == 128 && gr == 1 ? w1 >> 16 : w1 & 0xFFFFu;
-            const float s0 = __uint_as_float((h0 & 0xFFF0u) << 16) * scale, s1 = __uint_as_float((h1 & 0xFFF0u) << 16) * scale;
-            const float z0 = -P::kExcess - static_cast<float>(h0 & 15u), z1 = -P::kExcess - static_cast<float>(h1 & 15u);
+            const float s0 = gr == 0 ? scale_lo(w0) : scale_hi(w0), s1 = gr == 0 ? scale_lo(w1) : scale_hi(w1);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const float t = fmaf(e < 2 ? z0 : z1, qsum[nt][e % 2][gr], acc[nt][e]);
-                s[nt][mt][e] = gr == 0 ? (e < 2 ? s0 : s1) * t : fmaf(e < 2 ? s0 : s1, t, s[nt][mt][e]);
-              }
+              for (int e = 0; e < 4; ++e)
+                s[nt][mt][e] = gr == 0 ? (e < 2 ? s0 : s1) * acc[nt][e] : fmaf(e < 2 ? s0 : s1, acc[nt][e], s[nt][mt][e]);
           }
         }
       }
@@ -406,7 +446,7 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
           }
       }
       // ---- running maximum, sum and probabilities
-      uint32_t pf[NT][kM][2];
+      float p[NT][kM][4];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         float x0 = fmaxf(s[nt][0][0], s[nt][0][2]), x1 = fmaxf(s[nt][0][1], s[nt][0][3]);
@@ -420,8 +460,8 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
           x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, w));
           x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, w));
         }
-        x0 = fmaxf(x0, m[nt][0]);
-        x1 = fmaxf(x1, m[nt][1]);
+        x0 = fmaxf(x0 * by[nt][0], m[nt][0]);
+        x1 = fmaxf(x1 * by[nt][1], m[nt][1]);
         if (__any_sync(0xffffffffu, x0 != m[nt][0] || x1 != m[nt][1])) {
           const float k0 = m[nt][0] == -INFINITY ? 0.f : exp2_fast(m[nt][0] - x0), k1 = m[nt][1] == -INFINITY ? 0.f : exp2_fast(m[nt][1] - x1);
           m[nt][0] = x0;
@@ -439,46 +479,100 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
         const float u0 = x0 == -INFINITY ? 0.f : x0, u1 = x1 == -INFINITY ? 0.f : x1;
 #pragma unroll
         for (int mt = 0; mt < kM; ++mt) {
-          const float p0 = exp2_fast(s[nt][mt][0] - u0), p1 = exp2_fast(s[nt][mt][1] - u1), p2 = exp2_fast(s[nt][mt][2] - u0),
-                      p3 = exp2_fast(s[nt][mt][3] - u1);
-          l[nt][0] += p0 + p2;
-          l[nt][1] += p1 + p3;
-          pf[nt][mt][0] = transpose8x8(P::pack(p0, p1));
-          pf[nt][mt][1] = transpose8x8(P::pack(p2, p3));
+#pragma unroll
+          for (int e = 0; e < 4; ++e) p[nt][mt][e] = exp2_fast(fmaf(s[nt][mt][e], by[nt][e % 2], e % 2 ? -u1 : -u0));
+          l[nt][0] += p[nt][mt][0] + p[nt][mt][2];
+          l[nt][1] += p[nt][mt][1] + p[nt][mt][3];
         }
       }
       // ---- values
+      if (BITS == 16) {
 #pragma unroll
-      for (int mt = 0; mt < kM; ++mt) {
-        if (BITS == 16) {
+        for (int mt = 0; mt < kM; ++mt) {
+          uint32_t pf[NT][2];
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            pf[nt][0] = transpose8x8(P::pack(p[nt][mt][0], p[nt][mt][1]));
+            pf[nt][1] = transpose8x8(P::pack(p[nt][mt][2], p[nt][mt][3]));
+          }
           const uint32_t t = mt * 16 + (lane & 7u) + ((lane >> 4) & 1u) * 8;
 #pragma unroll
           for (int e = 0; e < D / 16; ++e) {
             uint32_t f[4];
             ldmatrix_trans(f, vbase + unit_at<D, BITS, true>(t, 2 * e + ((lane >> 3) & 1u)));
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) P::mma(o[nt][e], f, pf[nt][mt][0], pf[nt][mt][1]);
+            for (int nt = 0; nt < NT; ++nt) P::mma(o[nt][e], f, pf[nt][0], pf[nt][1]);
           }
-        } else {
+        }
+      } else {
+        uint32_t ws[kM][2];  // the words of tokens t0 and t0 + 8, whose probabilities this lane has
+#pragma unroll
+        for (int mt = 0; mt < kM; ++mt) {
+          const uint32_t t0 = mt * 16 + tk;
+          if (D == 128) {
+            ws[mt][0] = lds32(vw + t0 * 4);
+            ws[mt][1] = lds32(vw + t0 * 4 + 32);
+          } else {
+            ws[mt][0] = lds16(vw + t0 * 2);
+            ws[mt][1] = lds16(vw + t0 * 2 + 16);
+          }
+          if (!whole) {  // what nobody sees may be anything
+            if (!((bits >> t0) & 1u)) ws[mt][0] = 0;
+            if (!((bits >> (t0 + 8)) & 1u)) ws[mt][1] = 0;
+          }
+        }
+        uint32_t most = __vmaxu2(ws[0][0], ws[0][1]);
+#pragma unroll
+        for (int mt = 1; mt < kM; ++mt) most = __vmaxu2(most, __vmaxu2(ws[mt][0], ws[mt][1]));
+        if (__any_sync(0xffffffffu, __vmaxu2(most, v_most) != v_most)) {  // a scale above all before
+          float x = 0.f;
+#pragma unroll
+          for (int mt = 0; mt < kM; ++mt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) x = fmaxf(x, fmaxf(scale_lo(ws[mt][e]), scale_hi(ws[mt][e])));  // a NaN is passed over
+#pragma unroll
+          for (int w = 1; w < 32; w <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, w));
+          // scales below 2^(ex + 5) are then below 2^15, those at hand below 2^11
+          const int ex = max(static_cast<int>(__float_as_uint(x) >> 23) - 127, -100);
+          const uint32_t upto = static_cast<uint32_t>(min(ex + 4 + 127, 254)) << 7 | 0x7Fu;
+          if (x > 0.f && (upto | upto << 16) > v_most) {
+            const float up = __uint_as_float(static_cast<uint32_t>(127 + 10 - ex) << 23), k = v_most == 0x000F000Fu ? 1.f : up / v_up;
+            v_up = up;
+            v_most = upto | upto << 16;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+              for (int e = 0; e < D / 16; ++e) {
+                o[nt][e][0] *= k;
+                o[nt][e][1] *= k;
+                o[nt][e][2] *= k;
+                o[nt][e][3] *= k;
+              }
+            }
+          }
+        }
+#pragma unroll
+        for (int mt = 0; mt < kM; ++mt) {
           const uint32_t swap = c >> 1;  // slots 2c and 2c + 1 are tokens 2c and 2c + 1, or the other way round
           const uint32_t ta = mt * 16 + 2 * c + swap, tb = mt * 16 + 2 * c + (swap ^ 1u);
-          uint32_t wa, wb, wc, wd;  // scale words of the tokens in slots 2c, 2c + 1, 2c + 8, 2c + 9
+          uint32_t wa, wb, wc, wd;  // words of the tokens in slots 2c, 2c + 1, 2c + 8, 2c + 9, for their zero points
           if (D == 128) {
             wa = lds32(vw + ta * 4), wb = lds32(vw + tb * 4), wc = lds32(vw + ta * 4 + 32), wd = lds32(vw + tb * 4 + 32);
           } else {
             wa = lds16(vw + ta * 2), wb = lds16(vw + tb * 2), wc = lds16(vw + ta * 2 + 16), wd = lds16(vw + tb * 2 + 16);
           }
-          if (!whole) {  // a token that is not there may have a neighbour's word
-            if (!((bits >> ta) & 1u)) wa = 0;
-            if (!((bits >> tb) & 1u)) wb = 0;
-            if (!((bits >> (ta + 8)) & 1u)) wc = 0;
-            if (!((bits >> (tb + 8)) & 1u)) wd = 0;
-          }
 #pragma unroll
           for (int gr = 0; gr < kGroups; ++gr) {
-            const uint32_t w01 = __byte_perm(wa, wb, gr == 0 ? 0x5410 : 0x7632), w23 = __byte_perm(wc, wd, gr == 0 ? 0x5410 : 0x7632);
-            const uint32_t z01 = (w01 & 0x000F000Fu) | P::kMagic, z23 = (w23 & 0x000F000Fu) | P::kMagic;
-            const uint32_t s01 = P::scales(w01), s23 = P::scales(w23);
+            const float s0 = (gr == 0 ? scale_lo(ws[mt][0]) : scale_hi(ws[mt][0])) * v_up;
+            const float s1 = (gr == 0 ? scale_lo(ws[mt][1]) : scale_hi(ws[mt][1])) * v_up;
+            uint32_t pf[NT][2];
+            const uint32_t z01 = __byte_perm(wa, wb, gr == 0 ? 0x5410 : 0x7632) & 0x000F000Fu,
+                           z23 = __byte_perm(wc, wd, gr == 0 ? 0x5410 : 0x7632) & 0x000F000Fu;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              pf[nt][0] = transpose8x8(H::pack(p[nt][mt][0] * s0, p[nt][mt][1] * s0));
+              pf[nt][1] = transpose8x8(H::pack(p[nt][mt][2] * s1, p[nt][mt][3] * s1));
+            }
             const uint32_t unit = gr * 2 + g / 4, at = (g % 4) * 4;
             const uint32_t xa = lds32(vbase + unit_at<D, BITS, true>(ta, unit) + at), xb = lds32(vbase + unit_at<D, BITS, true>(tb, unit) + at);
             const uint32_t xc = lds32(vbase + unit_at<D, BITS, true>(ta + 8, unit) + at), xd = lds32(vbase + unit_at<D, BITS, true>(tb + 8, unit) + at);
@@ -488,16 +582,24 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
 #pragma unroll
               for (int e = 0; e < 2; ++e) {
                 const uint32_t ue = u >> (8 * e), ve = v >> (8 * e);
-                const uint32_t f[4] = {
-                    P::mul(P::sub((ue & 0x000F000Fu) | P::kMagic, z01), s01), P::mul(P::sub(((ue >> 4) & 0x000F000Fu) | P::kMagic, z01), s01),
-                    P::mul(P::sub((ve & 0x000F000Fu) | P::kMagic, z23), s23), P::mul(P::sub(((ve >> 4) & 0x000F000Fu) | P::kMagic, z23), s23)};
+                const uint32_t f[4] = {H::sub(ue & 0x000F000Fu, z01), H::sub(ue & 0x00F000F0u, z01 * 16), H::sub(ve & 0x000F000Fu, z23),
+                                       H::sub(ve & 0x00F000F0u, z23 * 16)};
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) P::mma(o[nt][gr * 4 + h * 2 + e], f, pf[nt][mt][0], pf[nt][mt][1]);
+                for (int nt = 0; nt < NT; ++nt) H::mma(o[nt][gr * 4 + h * 2 + e], f, pf[nt][0], pf[nt][1]);
               }
             }
           }
         }
       }
+    }
+    if (BITS == 4) {  // to values: the powers of two back
+      const float back = 0x1p24f / v_up;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < D / 16; ++e)
+#pragma unroll
+          for (int f = 0; f < 4; ++f) o[nt][e][f] *= f < 2 ? back : back * 0.0625f;
     }
     cp_async_wait<0>();
     __syncthreads();  // every warp is done with its ring

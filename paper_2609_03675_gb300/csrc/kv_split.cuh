@@ -54,25 +54,9 @@ __device__ __forceinline__ void cp_async_wait() {
 }
 __device__ __forceinline__ uint32_t shared_address(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
 
-__device__ __forceinline__ uint32_t lds32(uint32_t a) {
-  uint32_t x;
-  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(x) : "r"(a));
-  return x;
-}
-__device__ __forceinline__ uint32_t lds16(uint32_t a) {
-  uint16_t x;
-  asm volatile("ld.shared.b16 %0, [%1];" : "=h"(x) : "r"(a));
-  return x;
-}
-__device__ __forceinline__ uint2 lds64(uint32_t a) {
-  uint2 x;
-  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(x.x), "=r"(x.y) : "r"(a));
-  return x;
-}
-__device__ __forceinline__ uint4 lds128(uint32_t a) {
-  uint4 x;
-  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(a));
-  return x;
+template <typename T>
+__device__ __forceinline__ T at(const char* p) {
+  return *reinterpret_cast<const T*>(p);
 }
 __device__ __forceinline__ void ldmatrix_trans(uint32_t* r, uint32_t a) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
@@ -101,7 +85,7 @@ struct Pair<__nv_bfloat16> {
   static __device__ __forceinline__ float lo(uint32_t x) { return __uint_as_float(x << 16); }
   static __device__ __forceinline__ float hi(uint32_t x) { return __uint_as_float(x & 0xFFFF0000u); }
   static __device__ __forceinline__ void mma(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
-    asm volatile(
+    asm(
         "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
@@ -120,12 +104,19 @@ struct Pair<__half> {
   static __device__ __forceinline__ float lo(uint32_t x) { return __half2float(__ushort_as_half(static_cast<unsigned short>(x))); }
   static __device__ __forceinline__ float hi(uint32_t x) { return __half2float(__ushort_as_half(static_cast<unsigned short>(x >> 16))); }
   static __device__ __forceinline__ void mma(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
-    asm volatile(
+    asm(
         "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
   }
 };
+
+// The first product of a sum, in fp16.
+__device__ __forceinline__ void mma_first(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+      : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
 
 // The scales of a register of two words (the high half's, the low half's).
 __device__ __forceinline__ float scale_hi(uint32_t w) { return __uint_as_float(w & 0xFFF00000u); }
@@ -144,7 +135,7 @@ struct Ring {
 };
 
 template <int D, int BITS, int NT>
-constexpr size_t split_smem() {
+__host__ __device__ constexpr size_t split_smem() {
   const size_t ring = static_cast<size_t>(kSplitWarps) * Ring<D, BITS>::kWarp, join = static_cast<size_t>(kSplitWarps) * 8 * NT * D * 4;
   return ring > join ? ring : join;
 }
@@ -172,7 +163,7 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, c = lane % 4;
   const uint64_t range = plan.set_up(a, kRows);
   Walk<kSplitThreads> walk(a, plan, kRows, range);
-  const uint32_t ring = shared_address(smem) + warp * R::kWarp;
+  const char* const ring = smem + warp * R::kWarp;
   const BatchArg& b = a.batch;
   Item it;
   while (walk.next(it)) {
@@ -315,7 +306,7 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
       return x;
     };
     const auto issue = [&](uint32_t stage, const Ahead& x) {
-      const uint32_t base = ring + stage * R::kStage;
+      const uint32_t base = shared_address(ring + stage * R::kStage);
       uint32_t bits = __ballot_sync(0xffffffffu, x.seen);
       if (bits) {
 #pragma unroll
@@ -367,14 +358,15 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
     for (uint32_t ch = warp; ch < chunks; ch += kSplitWarps) {
       cp_async_wait<R::kStages - 2>();
       __syncwarp();
-      const uint32_t base = ring + stage * R::kStage, bits = stages[warp][stage].x;
+      const char* const base = ring + stage * R::kStage;
+      const uint32_t bits = stages[warp][stage].x;
       const int32_t pos = static_cast<int32_t>(stages[warp][stage].y);
       issue(stage == 0 ? R::kStages - 1 : stage - 1, ahead);  // the stage read in the iteration before
       ahead = look(ch + R::kStages * kSplitWarps);
       if (++stage == R::kStages) stage = 0;
       if (bits == 0) continue;
       const bool whole = (BITS == 4 ? bits == 0xffffffffu : (bits & 0xffffu) == 0xffffu);
-      const uint32_t vbase = base + R::kTokens * R::kRow, kw = base + 2 * R::kTokens * R::kRow, vw = kw + R::kWords;
+      const char *const vbase = base + R::kTokens * R::kRow, *const kw = base + 2 * R::kTokens * R::kRow, *const vw = kw + R::kWords;
 
       // ---- scores. Row slots of a 16-token operand hold tokens in this order (4-bit: so that both operands' reads
       // are free of conflicts): slot s is token s ^ ((s >> 2) & 1) of its eight
@@ -388,7 +380,7 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
           for (int nt = 0; nt < NT; ++nt) s[nt][mt][0] = s[nt][mt][1] = s[nt][mt][2] = s[nt][mt][3] = 0.f;
 #pragma unroll
           for (int e = 0; e < D / 32; ++e) {
-            const uint4 x = lds128(base + unit_at<D, BITS, false>(t0, 4 * e + c)), y = lds128(base + unit_at<D, BITS, false>(t0 + 8, 4 * e + c));
+            const uint4 x = at<uint4>(base + unit_at<D, BITS, false>(t0, 4 * e + c)), y = at<uint4>(base + unit_at<D, BITS, false>(t0 + 8, 4 * e + c));
             const uint32_t f0[4] = {x.x, y.x, x.y, y.y}, f1[4] = {x.z, y.z, x.w, y.w};
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
@@ -399,24 +391,21 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
         } else {
           uint32_t w0, w1;  // the words of tokens t0 and t0 + 8
           if (D == 128) {
-            w0 = lds32(kw + t0 * 4);
-            w1 = lds32(kw + t0 * 4 + 32);
+            w0 = at<uint32_t>(kw + t0 * 4);
+            w1 = at<uint32_t>(kw + t0 * 4 + 32);
           } else {
-            w0 = lds16(kw + t0 * 2);
-            w1 = lds16(kw + t0 * 2 + 16);
+            w0 = at<uint16_t>(kw + t0 * 2);
+            w1 = at<uint16_t>(kw + t0 * 2 + 16);
           }
 #pragma unroll
           for (int gr = 0; gr < kGroups; ++gr) {
-            const uint2 x = lds64(base + unit_at<D, BITS, false>(t0, gr * 2 + c / 2) + (c % 2) * 8);
-            const uint2 y = lds64(base + unit_at<D, BITS, false>(t0 + 8, gr * 2 + c / 2) + (c % 2) * 8);
+            const uint2 x = at<uint2>(base + unit_at<D, BITS, false>(t0, gr * 2 + c / 2) + (c % 2) * 8);
+            const uint2 y = at<uint2>(base + unit_at<D, BITS, false>(t0 + 8, gr * 2 + c / 2) + (c % 2) * 8);
             float acc[NT][4];
             const uint32_t only = gr == 0 ? 0x0000000Fu : 0x000F0000u;  // the group's zero point, in its slot
             const uint32_t z[4] = {w0 & only, w1 & only, 0u, 0u};
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              acc[nt][0] = acc[nt][1] = acc[nt][2] = acc[nt][3] = 0.f;
-              H::mma(acc[nt], z, qz[nt], 0u);
-            }
+            for (int nt = 0; nt < NT; ++nt) mma_first(acc[nt], z, qz[nt], 0u);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const uint32_t u = (e < 2 ? x.x : x.y) >> (8 * (e % 2)), v = (e < 2 ? y.x : y.y) >> (8 * (e % 2));
@@ -499,7 +488,7 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
 #pragma unroll
           for (int e = 0; e < D / 16; ++e) {
             uint32_t f[4];
-            ldmatrix_trans(f, vbase + unit_at<D, BITS, true>(t, 2 * e + ((lane >> 3) & 1u)));
+            ldmatrix_trans(f, shared_address(vbase + unit_at<D, BITS, true>(t, 2 * e + ((lane >> 3) & 1u))));
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) P::mma(o[nt][e], f, pf[nt][0], pf[nt][1]);
           }
@@ -510,11 +499,11 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
         for (int mt = 0; mt < kM; ++mt) {
           const uint32_t t0 = mt * 16 + tk;
           if (D == 128) {
-            ws[mt][0] = lds32(vw + t0 * 4);
-            ws[mt][1] = lds32(vw + t0 * 4 + 32);
+            ws[mt][0] = at<uint32_t>(vw + t0 * 4);
+            ws[mt][1] = at<uint32_t>(vw + t0 * 4 + 32);
           } else {
-            ws[mt][0] = lds16(vw + t0 * 2);
-            ws[mt][1] = lds16(vw + t0 * 2 + 16);
+            ws[mt][0] = at<uint16_t>(vw + t0 * 2);
+            ws[mt][1] = at<uint16_t>(vw + t0 * 2 + 16);
           }
           if (!whole) {  // what nobody sees may be anything
             if (!((bits >> t0) & 1u)) ws[mt][0] = 0;
@@ -557,9 +546,9 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
           const uint32_t ta = mt * 16 + 2 * c + swap, tb = mt * 16 + 2 * c + (swap ^ 1u);
           uint32_t wa, wb, wc, wd;  // words of the tokens in slots 2c, 2c + 1, 2c + 8, 2c + 9, for their zero points
           if (D == 128) {
-            wa = lds32(vw + ta * 4), wb = lds32(vw + tb * 4), wc = lds32(vw + ta * 4 + 32), wd = lds32(vw + tb * 4 + 32);
+            wa = at<uint32_t>(vw + ta * 4), wb = at<uint32_t>(vw + tb * 4), wc = at<uint32_t>(vw + ta * 4 + 32), wd = at<uint32_t>(vw + tb * 4 + 32);
           } else {
-            wa = lds16(vw + ta * 2), wb = lds16(vw + tb * 2), wc = lds16(vw + ta * 2 + 16), wd = lds16(vw + tb * 2 + 16);
+            wa = at<uint16_t>(vw + ta * 2), wb = at<uint16_t>(vw + tb * 2), wc = at<uint16_t>(vw + ta * 2 + 16), wd = at<uint16_t>(vw + tb * 2 + 16);
           }
 #pragma unroll
           for (int gr = 0; gr < kGroups; ++gr) {
@@ -573,9 +562,9 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
               pf[nt][0] = transpose8x8(H::pack(p[nt][mt][0] * s0, p[nt][mt][1] * s0));
               pf[nt][1] = transpose8x8(H::pack(p[nt][mt][2] * s1, p[nt][mt][3] * s1));
             }
-            const uint32_t unit = gr * 2 + g / 4, at = (g % 4) * 4;
-            const uint32_t xa = lds32(vbase + unit_at<D, BITS, true>(ta, unit) + at), xb = lds32(vbase + unit_at<D, BITS, true>(tb, unit) + at);
-            const uint32_t xc = lds32(vbase + unit_at<D, BITS, true>(ta + 8, unit) + at), xd = lds32(vbase + unit_at<D, BITS, true>(tb + 8, unit) + at);
+            const uint32_t unit = gr * 2 + g / 4, in = (g % 4) * 4;
+            const uint32_t xa = at<uint32_t>(vbase + unit_at<D, BITS, true>(ta, unit) + in), xb = at<uint32_t>(vbase + unit_at<D, BITS, true>(tb, unit) + in);
+            const uint32_t xc = at<uint32_t>(vbase + unit_at<D, BITS, true>(ta + 8, unit) + in), xd = at<uint32_t>(vbase + unit_at<D, BITS, true>(tb + 8, unit) + in);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {  // dims 8 g .. + 3, and the four after them
               const uint32_t u = __byte_perm(xa, xb, h == 0 ? 0x5410 : 0x7632), v = __byte_perm(xc, xd, h == 0 ? 0x5410 : 0x7632);
@@ -678,22 +667,54 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
       __syncthreads();
       if (last_here) {
         __threadfence();
-        for (uint32_t x = threadIdx.x; x < rows * (D / 4); x += kSplitThreads) {
-          const uint32_t r = x / (D / 4), d = x % (D / 4) * 4;
-          float top = -INFINITY, sum = 0.f;
-          float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-          for (uint32_t ct = it.first_cta; ct <= it.last_cta; ++ct)
-            top = fmaxf(top, __ldcg(&a.part_ms[(2ull * ct + (ct == it.first_cta)) * kRows + r]).x);
-#pragma unroll 4
-          for (uint32_t ct = it.first_cta; ct <= it.last_cta; ++ct) {
-            const uint64_t at = (2ull * ct + (ct == it.first_cta)) * kRows + r;
-            const float2 ms = __ldcg(&a.part_ms[at]);
-            const float4 z = __ldcg(reinterpret_cast<const float4*>(a.part + at * D + d));
-            const float k = ms.x == -INFINITY ? (ms.y == 0.f ? 0.f : 1.f) : exp2_fast(ms.x - top);
-            sum += k * ms.y;
-            y.x += k * z.x, y.y += k * z.y, y.z += k * z.z, y.w += k * z.w;
+        // each part's factor for each row, kJoin parts at a time; the maximum over all parts first
+        const uint32_t parts = it.last_cta - it.first_cta + 1;
+        const auto part_at = [&](uint32_t i, uint32_t r) { return (2ull * (it.first_cta + i) + (i == 0)) * kRows + r; };
+        float2* ms = reinterpret_cast<float2*>(smem);  // [part][row]
+        constexpr uint32_t kJoin = split_smem<D, BITS, NT>() / (kRows * sizeof(float2));
+        float top = -INFINITY, sum = 0.f;  // of row threadIdx.x
+        for (uint32_t p0 = 0; p0 < parts; p0 += kJoin) {
+          const uint32_t n = min(kJoin, parts - p0);
+          __syncthreads();
+          for (uint32_t x = threadIdx.x; x < n * kRows; x += kSplitThreads) ms[x] = __ldcg(&a.part_ms[part_at(p0 + x / kRows, x % kRows)]);
+          __syncthreads();
+          if (threadIdx.x < rows)
+            for (uint32_t i = 0; i < n; ++i) top = fmaxf(top, ms[i * kRows + threadIdx.x].x);
+        }
+        if (threadIdx.x < kRows) warp_m[0][threadIdx.x] = top;
+        constexpr int kMost = (kRows * (D / 4) + kSplitThreads - 1) / kSplitThreads;
+        float4 y[kMost];
+#pragma unroll
+        for (int q = 0; q < kMost; ++q) y[q] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (uint32_t p0 = 0; p0 < parts; p0 += kJoin) {
+          const uint32_t n = min(kJoin, parts - p0);
+          __syncthreads();
+          for (uint32_t x = threadIdx.x; x < n * kRows; x += kSplitThreads) {
+            const float2 z = __ldcg(&a.part_ms[part_at(p0 + x / kRows, x % kRows)]);
+            const float k = z.x == -INFINITY ? (z.y == 0.f ? 0.f : 1.f) : exp2_fast(z.x - warp_m[0][x % kRows]);
+            ms[x] = make_float2(k, z.y == 0.f ? 0.f : k * z.y);
           }
-          write(r, d, y, top, sum);
+          __syncthreads();
+          if (threadIdx.x < rows)
+            for (uint32_t i = 0; i < n; ++i) sum += ms[i * kRows + threadIdx.x].y;
+#pragma unroll
+          for (int q = 0; q < kMost; ++q) {
+            const uint32_t x = threadIdx.x + q * kSplitThreads, r = x / (D / 4), d = x % (D / 4) * 4;
+            if (r >= rows) break;
+#pragma unroll 8
+            for (uint32_t i = 0; i < n; ++i) {
+              const float k = ms[i * kRows + r].x;
+              const float4 z = __ldcg(reinterpret_cast<const float4*>(a.part + part_at(p0 + i, r) * D + d));
+              y[q].x += k * z.x, y[q].y += k * z.y, y[q].z += k * z.z, y[q].w += k * z.w;
+            }
+          }
+        }
+        if (threadIdx.x < kRows) warp_l[0][threadIdx.x] = sum;
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < kMost; ++q) {
+          const uint32_t x = threadIdx.x + q * kSplitThreads, r = x / (D / 4), d = x % (D / 4) * 4;
+          if (r < rows) write(r, d, y[q], warp_m[0][r], warp_l[0][r]);
         }
       }
     }

@@ -38,7 +38,7 @@ def _flags(extra=()):
 
 def _inputs():
     headers = ["ngff_common.cuh", "ngff_device.cuh", "kv_common.cuh", "kv_rows.cuh", "kv_handle.cuh", "kv_plan.cuh",
-               "kv_split.cuh"]
+               "kv_split.cuh", "kv_rows_tc.cuh"]
     files = ([os.path.join(CSRC, s) for s in SOURCES + headers]
              + [os.path.join(INCLUDE, h) for h in ("cofie_ngff.h", "cofie_kv.h")] + [__file__])
     return files

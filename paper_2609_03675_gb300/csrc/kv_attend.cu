@@ -3,7 +3,7 @@
 #include <algorithm>
 #include <cmath>
 
-#include "kv_split.cuh"
+#include "kv_rows_tc.cuh"
 
 namespace cofie {
 namespace {
@@ -70,6 +70,18 @@ SplitKernel split_kernel(const cofie_kv_params& p, int i, size_t* smem) {
   });
 }
 
+template <typename T, int D>
+SplitKernel rows_kernel(uint32_t bits, size_t* smem) {
+  *smem = tc_smem<D>();
+  return bits == 4 ? attend_rows_tc<T, D, 4> : attend_rows_tc<T, D, 16>;
+}
+SplitKernel rows_kernel(const cofie_kv_params& p, size_t* smem) {
+  return for_type(p, [&](auto x) {
+    using T = decltype(x);
+    return p.head_dim == 64 ? rows_kernel<T, 64>(p.bits, smem) : rows_kernel<T, 128>(p.bits, smem);
+  });
+}
+
 }  // namespace
 
 cudaError_t attend_set_up(cofie_kv* h) {
@@ -85,6 +97,12 @@ cudaError_t attend_set_up(cofie_kv* h) {
     h->split_ctas[i] = sm_count() * static_cast<uint32_t>(per_sm);
     ctas = std::max<size_t>(ctas, h->split_ctas[i]);
     rows = std::max<size_t>(rows, 2ull * h->split_ctas[i] * (8u << i));
+  }
+  size_t smem = 0;
+  if (e == cudaSuccess) {
+    const SplitKernel k = rows_kernel(h->p, &smem);
+    e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    rows = std::max<size_t>(rows, 2ull * sm_count() * kTcRows);
   }
   if (e == cudaSuccess) e = cudaMalloc(&h->d_part, rows * h->p.head_dim * sizeof(float));
   if (e == cudaSuccess) e = cudaMalloc(&h->d_part_ms, rows * sizeof(float2));
@@ -156,8 +174,12 @@ extern "C" int cofie_kv_attend(cofie_kv_t* h, const cofie_kv_batch* b, const cof
       return rc;
   }
   const uint64_t rows = static_cast<uint64_t>(b->offsets ? (b->max_new ? b->max_new : b->n_tokens) : 1) * a.group;
-  const int i = rows <= 8 ? 0 : rows <= 16 ? 1 : 2;
   size_t smem = 0;
+  if (rows > 16) {
+    const SplitKernel k = rows_kernel(h->p, &smem);
+    return launched(h, launch_dependent(true, k, dim3(sm_count()), dim3(kTcThreads), smem, st, a), "attend");
+  }
+  const int i = rows <= 8 ? 0 : 1;
   const SplitKernel k = split_kernel(h->p, i, &smem);
   return launched(h, launch_dependent(true, k, dim3(h->split_ctas[i]), dim3(kSplitThreads), smem, st, a), "attend");
 }

@@ -1,0 +1,703 @@
+// Attention of many query rows over the cache (questions, prompts): the
+// products bound it, so both run on tcgen05.
+//
+// A CTA takes up to 256 query rows (new tokens x heads of the group) of one
+// key/value head as two tiles of 128, and the cached tokens 128 at a time:
+//   producers  four warps: keys and values of the next tokens into shared memory
+//              (128-byte swizzle), copied (16 bits) or unpacked to (n - z) s,
+//              which the 16-bit types hold exactly (4 bits); a thread to a token
+//   MMA        one thread: S = Q K^T into tensor memory (128 x 128 fp32 a tile),
+//              and O += P V with P read from tensor memory
+//   softmax    four warps a tile, a thread to a row: maximum, exponentials, P
+//              back into S's place in 16 bits; at the end O out
+// While one tile's softmax runs, the other's products do. The running maximum
+// that exponentials refer to is raised only when the true one passes it by 2^8
+// (then O is brought down in tensor memory), which seldom happens after the
+// first tokens.
+//
+// Tensor memory: S0 S1 O0 O1, 128 columns each, P in the first 64 of its S. P V
+// of a tile has to be done before Q K^T of the next tokens writes there.
+//
+// For each 256 x 128 block of the scores the tensor core needs 2048 cycles (head
+// of 128), shared memory 1536 for its operands and 512 for writing them, the
+// exponentials 1024 and more.
+#pragma once
+
+#include <type_traits>
+
+#include "kv_split.cuh"
+#include "ngff_device.cuh"
+
+namespace cofie {
+namespace {
+
+constexpr int kTcRows = 256;
+constexpr int kTcKeys = 128;
+constexpr int kTcSoftmax = 256;                  // threads: warps 0 to 7
+constexpr int kTcProducers = 128;                // warps 8 to 11
+constexpr int kTcThreads = kTcSoftmax + kTcProducers + 32;  // and the MMA warp
+constexpr int kTcStages = 2;
+constexpr int kTcInfo = 4;
+constexpr float kTcRaise = 8.f;
+constexpr uint64_t kTcTimeout = 1000000000ull;
+
+struct TcInfo {
+  uint32_t bits[4];  // tokens that some row may see
+  int32_t pos[2];    // first token of each 64
+  uint32_t plain;    // every token is seen by every row
+};
+
+template <int D>
+struct TcSmem {
+  static constexpr int kBlock = 128 * 128;               // 128 rows of 64 values
+  static constexpr int kTileBytes = kBlock * (D / 64);   // 128 rows of D values
+  char q[2][kTileBytes];
+  char k[kTcStages][kTileBytes];
+  char v[kTcStages][kTileBytes];
+  Plan<kTcThreads> plan;
+  TcInfo info[kTcInfo];
+  uint64_t row_of[kTcStages][kTcKeys];  // 16 bits: the tokens' rows in the pages, ~0 where there is nothing to see
+  float top[kTcRows], sum[kTcRows];
+  uint64_t k_full[kTcStages], k_empty[kTcStages], v_full[kTcStages], v_empty[kTcStages];
+  uint64_t info_full[kTcInfo], q_full[2], s_full[2], p_full[2], o_full[2], drained;
+  uint32_t tmem, stop, last_here;
+};
+
+// A wait for a barrier's phase that ends, with false, when it runs out or another's has.
+__device__ __noinline__ bool tc_wait_slow(uint32_t bar, uint32_t parity, volatile uint32_t* stop) {
+  const uint64_t t0 = globaltimer_ns();
+  for (;;) {
+#pragma unroll 1
+    for (int i = 0; i < 16; ++i)
+      if (mbar_try_wait(bar, parity)) return true;
+    if (*stop) return false;
+    if (globaltimer_ns() - t0 > kTcTimeout) {
+      *stop = 1;
+      return false;
+    }
+  }
+}
+__device__ __forceinline__ bool tc_wait(const uint64_t* bar, uint32_t parity, uint32_t* stop) {
+  const uint32_t b = shared_address(bar);
+  return mbar_try_wait(b, parity & 1) || tc_wait_slow(b, parity & 1, stop);
+}
+
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+template <int ID, int THREADS>
+__device__ __forceinline__ void bar_sync() {
+  asm volatile("bar.sync %0, %1;" ::"n"(ID), "n"(THREADS) : "memory");
+}
+
+// Operand in shared memory, 128-byte swizzle, eight rows of 128 bytes to an
+// atom of 1024. K-major: rows are M or N, the 64 values of a row are K; the
+// leading offset is not used. MN-major: rows are K, the 64 values M or N, the
+// next 64 lie `leading` bytes on.
+__device__ __forceinline__ uint64_t tc_desc(uint32_t addr, uint32_t leading) {
+  uint64_t d = (addr >> 4) & 0x3FFFu;
+  d |= static_cast<uint64_t>(leading >> 4) << 16;
+  d |= static_cast<uint64_t>(1024u >> 4) << 32;
+  d |= 1ull << 46;
+  d |= 2ull << 61;
+  return d;
+}
+// fp32 sums of products of 16-bit values; B K-major or MN-major.
+template <typename T>
+__device__ __forceinline__ constexpr uint32_t tc_idesc(uint32_t m, uint32_t n, bool b_mn) {
+  const uint32_t type = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
+  return (1u << 4) | (type << 7) | (type << 10) | ((b_mn ? 1u : 0u) << 16) | ((n >> 3) << 17) | ((m >> 4) << 24);
+}
+__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(acc)
+      : "memory");
+}
+__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"(acc)
+      : "memory");
+}
+__device__ __forceinline__ void tc_commit(uint64_t* bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(shared_address(bar)) : "memory");
+}
+__device__ __forceinline__ void tc_ld32(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+      : "r"(taddr));
+}
+__device__ __forceinline__ void tc_st32(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::"r"(r[0]),
+      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+      "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]),
+      "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]),
+      "r"(taddr)
+      : "memory");
+}
+__device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t* r) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(
+          r[0]),
+      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+      "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
+      : "memory");
+}
+// Waits for this thread's loads from tensor memory; the registers they fill pass through it, so that no use of them
+// can be moved before it.
+__device__ __forceinline__ void tc_wait_ld(uint32_t* r) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]), "+r"(r[8]),
+                 "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]), "+r"(r[16]),
+                 "+r"(r[17]), "+r"(r[18]), "+r"(r[19]), "+r"(r[20]), "+r"(r[21]), "+r"(r[22]), "+r"(r[23]), "+r"(r[24]),
+                 "+r"(r[25]), "+r"(r[26]), "+r"(r[27]), "+r"(r[28]), "+r"(r[29]), "+r"(r[30]), "+r"(r[31])::"memory");
+}
+__device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Eight codes to (n - z) s, in the order (0, 4), (1, 5), (2, 6), (3, 7).
+template <typename T>
+struct Unpack;
+template <>
+struct Unpack<__nv_bfloat16> {
+  __nv_bfloat162 z, s;
+  __device__ __forceinline__ explicit Unpack(uint32_t word) {
+    const uint32_t a = (word & 15u) | 0x4300u, b = word & 0xFFF0u;  // 128 + z
+    const uint32_t aa = a | a << 16, bb = b | b << 16;
+    z = *reinterpret_cast<const __nv_bfloat162*>(&aa);
+    s = *reinterpret_cast<const __nv_bfloat162*>(&bb);
+  }
+  __device__ __forceinline__ uint4 operator()(uint32_t w) const {
+    uint32_t r[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t x = ((w >> (4 * i)) & 0x000F000Fu) | 0x43004300u;  // 128 + n
+      const __nv_bfloat162 y = __hmul2(__hsub2(*reinterpret_cast<const __nv_bfloat162*>(&x), z), s);
+      r[i] = *reinterpret_cast<const uint32_t*>(&y);
+    }
+    return make_uint4(r[0], r[1], r[2], r[3]);
+  }
+};
+template <>
+struct Unpack<__half> {
+  __half2 z, z16, s;
+  __device__ __forceinline__ explicit Unpack(uint32_t word) {
+    const float f = static_cast<float>(word & 15u);
+    z = __float2half2_rn(1024.f + f);
+    z16 = __float2half2_rn(-64.f - f);
+    s = __float2half2_rn(__uint_as_float((word & 0xFFF0u) << 16));
+  }
+  __device__ __forceinline__ uint4 operator()(uint32_t w) const {
+    uint32_t r[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t x = ((w >> (8 * (i / 2))) & (i % 2 ? 0x00F000F0u : 0x000F000Fu)) | 0x64006400u;  // 1024 + n, 1024 + 16 n
+      const __half2 h = *reinterpret_cast<const __half2*>(&x);
+      const __half2 y = __hmul2(i % 2 ? __hfma2(h, __float2half2_rn(0.0625f), z16) : __hsub2(h, z), s);
+      r[i] = *reinterpret_cast<const uint32_t*>(&y);
+    }
+    return make_uint4(r[0], r[1], r[2], r[3]);
+  }
+};
+
+template <typename T, int D, int BITS>
+__global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_constant__ AttendArgs a) {
+  using P = Pair<T>;
+  using S = TcSmem<D>;
+  extern __shared__ char raw[];
+  S& sm = *reinterpret_cast<S*>(raw + (1024u - (shared_address(raw) & 1023u)) % 1024u);
+  pdl_trigger();
+  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kTcStages; ++i) {
+      mbar_init(shared_address(&sm.k_full[i]), kTcProducers);
+      mbar_init(shared_address(&sm.v_full[i]), kTcProducers);
+      mbar_init(shared_address(&sm.k_empty[i]), 1);
+      mbar_init(shared_address(&sm.v_empty[i]), 1);
+    }
+    for (int i = 0; i < kTcInfo; ++i) mbar_init(shared_address(&sm.info_full[i]), kTcProducers);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(shared_address(&sm.q_full[i]), 128);
+      mbar_init(shared_address(&sm.s_full[i]), 1);
+      mbar_init(shared_address(&sm.p_full[i]), 128);
+      mbar_init(shared_address(&sm.o_full[i]), 1);
+    }
+    mbar_init(shared_address(&sm.drained), 1);
+    sm.stop = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  pdl_wait();
+  // only now: a kernel before this one may still hold tensor memory, or wait for it
+  if (warp == kTcThreads / 32 - 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(shared_address(&sm.tmem)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    tc_fence_before();
+  }
+  const uint64_t range = sm.plan.set_up(a, kTcRows);  // ends with a barrier
+  tc_fence_after();
+  const uint32_t tmem = sm.tmem;
+  Walk<kTcThreads> walk(a, sm.plan, kTcRows, range);
+  const BatchArg& b = a.batch;
+  Item it;
+  uint32_t* stop = &sm.stop;
+  bool ok = true;
+
+  if (warp < kTcSoftmax / 32) {
+    // ---------------------------------------------------------------- softmax: thread r of tile t has row r of it
+    const uint32_t t = warp / 4, r = threadIdx.x % 128;
+    const uint32_t lanes = (warp % 4) * 32u << 16;
+    const uint32_t s_col = tmem + lanes + t * 128, o_col = tmem + lanes + 256 + t * 128;
+    const float by = a.scale * 1.4426950408889634f;
+    uint32_t s_n = 0, o_n = 0, info_n = 0;  // phases
+    while (walk.next(it)) {  // to the end even when a wait ran out: the barriers below count on all
+      const uint32_t row0 = it.rb * kTcRows + t * 128, all = it.span.count * a.group;
+      const uint32_t tiles = (it.hi - it.lo + 1) / 2;
+      const bool active = row0 < all, real = row0 + r < all;
+      const uint32_t token = real ? (row0 + r) / a.group : 0, head = it.head * a.group + (real ? (row0 + r) % a.group : 0);
+      int32_t seen = 0;
+      if (real) {
+        const int64_t n = a.causal ? static_cast<int64_t>(it.span.length) - it.span.count + token + 1 : it.span.length;
+        seen = n > 0 ? static_cast<int32_t>(n) : 0;
+      }
+      float m = -INFINITY, l = 0.f;
+      if (active && tiles) {
+        {  // the row of Q into shared memory; codes' products come in the order in which they are unpacked
+          const T* q = reinterpret_cast<const T*>(a.q.in) + static_cast<int64_t>(it.span.first + token) * a.q.in_token +
+                       static_cast<int64_t>(head) * a.q.in_head;
+#pragma unroll
+          for (int e = 0; e < D / 8; ++e) {
+            uint4 x = make_uint4(0, 0, 0, 0);
+            if (real) {
+              if (a.q_wide) {
+                x = *reinterpret_cast<const uint4*>(q + e * 8);
+              } else {
+                RowVec<T, 8> y;
+#pragma unroll
+                for (int f = 0; f < 8; ++f) y.v[f] = q[e * 8 + f];
+                x = *reinterpret_cast<uint4*>(&y);
+              }
+            }
+            if (BITS == 4)
+              x = make_uint4(__byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632), __byte_perm(x.y, x.w, 0x5410),
+                             __byte_perm(x.y, x.w, 0x7632));
+            *reinterpret_cast<uint4*>(sm.q[t] + (e / 8) * S::kBlock + r * 128 + ((e % 8) ^ (r & 7)) * 16) = x;
+          }
+          fence_async_shared();
+          mbar_arrive(shared_address(&sm.q_full[t]));
+        }
+        for (uint32_t j = 0; ok && j < tiles; ++j) {
+          const TcInfo& info = sm.info[info_n % kTcInfo];
+          ok = tc_wait(&sm.info_full[info_n % kTcInfo], info_n / kTcInfo, stop) && tc_wait(&sm.s_full[t], s_n++, stop);
+          ++info_n;
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          tc_fence_after();
+          const bool plain = info.plain != 0;
+          const auto masked = [&](uint32_t col) {  // whether this row does not see the tile's token col
+            const int32_t pos = info.pos[col / 64] + static_cast<int32_t>(col % 64);
+            return !((info.bits[col / 32] >> (col % 32)) & 1u) || pos >= seen;
+          };
+          // the maximum
+          float top = -INFINITY;
+          uint32_t x[2][32];
+          tc_ld32(s_col, x[0]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            tc_wait_ld(x[e % 2]);
+            if (e < 3) tc_ld32(s_col + 32 * (e + 1), x[(e + 1) % 2]);
+            if (!plain) {
+#pragma unroll
+              for (int f = 0; f < 32; ++f)
+                if (masked(32 * e + f)) x[e % 2][f] = 0xff800000u;
+            }
+            float top2 = -INFINITY;
+#pragma unroll
+            for (int f = 0; f < 32; f += 2) {
+              top = fmaxf(top, __uint_as_float(x[e % 2][f]));
+              top2 = fmaxf(top2, __uint_as_float(x[e % 2][f + 1]));
+            }
+            top = fmaxf(top, top2);
+          }
+          top *= by;
+          const bool raise = top > m + kTcRaise || (m == -INFINITY && top > -INFINITY);
+          if (__any_sync(0xffffffffu, raise)) {
+            const float to = raise ? top : m, k = m == -INFINITY ? 0.f : exp2_fast(m - to);
+            if (j > 0) {  // O as it is after the tokens before
+              ok = tc_wait(&sm.o_full[t], o_n, stop);
+              ok = __all_sync(0xffffffffu, ok);
+              if (!ok) break;
+              tc_fence_after();
+              uint32_t y[32];
+#pragma unroll 1
+              for (int e = 0; e < D / 32; ++e) {
+                tc_ld32(o_col + 32 * e, y);
+                tc_wait_ld(y);
+#pragma unroll
+                for (int f = 0; f < 32; ++f) y[f] = __float_as_uint(__uint_as_float(y[f]) * k);
+                tc_st32(o_col + 32 * e, y);
+              }
+              tc_wait_st();
+            }
+            l *= k;
+            m = to;
+          }
+          if (j > 0) ++o_n;  // the phase of the tokens before, waited for or not
+          // the exponentials
+          const float from = m == -INFINITY ? 0.f : -m;
+          float l2 = 0.f;
+          tc_ld32(s_col, x[0]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            tc_wait_ld(x[e % 2]);
+            if (e < 3) tc_ld32(s_col + 32 * (e + 1), x[(e + 1) % 2]);
+            if (!plain) {
+#pragma unroll
+              for (int f = 0; f < 32; ++f)
+                if (masked(32 * e + f)) x[e % 2][f] = 0xff800000u;
+            }
+            uint32_t y[16];
+#pragma unroll
+            for (int f = 0; f < 16; ++f) {
+              const float p0 = exp2_fast(fmaf(__uint_as_float(x[e % 2][2 * f]), by, from));
+              const float p1 = exp2_fast(fmaf(__uint_as_float(x[e % 2][2 * f + 1]), by, from));
+              l += p0;
+              l2 += p1;
+              y[f] = P::pack(p0, p1);
+            }
+            // S's columns up to 32 e + 31 are read, P's from 16 e are written
+            tc_st16(s_col + 16 * e, y);
+          }
+          l += l2;
+          tc_wait_st();
+          tc_fence_before();
+          mbar_arrive(shared_address(&sm.p_full[t]));
+        }
+        if (ok) {
+          ok = tc_wait(&sm.o_full[t], o_n++, stop);
+          ok = __all_sync(0xffffffffu, ok);
+          tc_fence_after();
+        }
+      }
+      // info of tiles that this half does not use
+      if (!active) info_n += tiles;
+      const bool alone = it.first_cta == it.last_cta;
+      const uint32_t lr = t * 128 + r;  // row of the item's 256
+      const uint64_t part = (2ull * blockIdx.x + (blockIdx.x == it.first_cta ? 1 : 0)) * kTcRows;
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      T* out = reinterpret_cast<T*>(a.q.out) + static_cast<int64_t>(it.span.first + token) * a.q.out_token +
+               static_cast<int64_t>(head) * a.q.out_head;
+      if (active) {
+#pragma unroll 1
+        for (int e = 0; e < D / 32; ++e) {
+          uint32_t y[32];
+          if (tiles) {
+            tc_ld32(o_col + 32 * e, y);
+            tc_wait_ld(y);
+          } else {
+#pragma unroll
+            for (int f = 0; f < 32; ++f) y[f] = 0;
+          }
+          if (real) {
+#pragma unroll
+            for (int f = 0; f < 4; ++f) {  // eight columns, and the dims that they are
+              constexpr int order[8] = {0, 4, 1, 5, 2, 6, 3, 7};
+              float z[8];
+#pragma unroll
+              for (int i = 0; i < 8; ++i) z[BITS == 4 ? order[i] : i] = __uint_as_float(y[8 * f + i]);
+              if (l == 0.f)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) z[i] = 0.f;
+              const int d = 32 * e + 8 * f;
+              if (!alone) {
+                float* to = a.part + (part + lr) * D + d;
+                *reinterpret_cast<float4*>(to) = make_float4(z[0], z[1], z[2], z[3]);
+                *reinterpret_cast<float4*>(to + 4) = make_float4(z[4], z[5], z[6], z[7]);
+              } else {
+                const uint32_t w[4] = {P::pack(z[0] * inv, z[1] * inv), P::pack(z[2] * inv, z[3] * inv), P::pack(z[4] * inv, z[5] * inv),
+                                       P::pack(z[6] * inv, z[7] * inv)};
+                if (a.out_wide) {
+                  *reinterpret_cast<uint2*>(out + d) = make_uint2(w[0], w[1]);
+                  *reinterpret_cast<uint2*>(out + d + 4) = make_uint2(w[2], w[3]);
+                } else {
+#pragma unroll
+                  for (int i = 0; i < 8; ++i) out[d + i] = Elem<T>::from(z[i] * inv);
+                }
+              }
+            }
+          }
+        }
+        if (real) {
+          if (!alone) a.part_ms[part + lr] = make_float2(m, l);
+          else if (a.lse) a.lse[static_cast<uint64_t>(it.span.first + token) * a.heads + head] = (m + log2f(l)) * 0.6931471805599453f;
+        }
+      }
+      tc_fence_before();  // O is read before the next item's products are let through (by q_full)
+      if (!alone) {
+        __threadfence();
+        bar_sync<1, kTcSoftmax>();
+        const uint32_t parts = it.last_cta - it.first_cta + 1;
+        if (threadIdx.x == 0) {
+          sm.last_here = atomicAdd(a.done + it.first_cta, 1u) == parts - 1;
+          if (sm.last_here) a.done[it.first_cta] = 0;
+        }
+        bar_sync<1, kTcSoftmax>();
+        if (sm.last_here) {
+          __threadfence();
+          const auto part_at = [&](uint32_t i, uint32_t row) { return (2ull * (it.first_cta + i) + (i == 0)) * kTcRows + row; };
+          float top = -INFINITY, sum = 0.f;
+          if (real) {
+            for (uint32_t i = 0; i < parts; ++i) top = fmaxf(top, __ldcg(&a.part_ms[part_at(i, lr)]).x);
+            for (uint32_t i = 0; i < parts; ++i) {
+              const float2 z = __ldcg(&a.part_ms[part_at(i, lr)]);
+              sum += z.y == 0.f ? 0.f : (z.x == -INFINITY ? 1.f : exp2_fast(z.x - top)) * z.y;
+            }
+            if (a.lse) a.lse[static_cast<uint64_t>(it.span.first + token) * a.heads + head] = (top + log2f(sum)) * 0.6931471805599453f;
+          }
+          sm.top[lr] = top;
+          sm.sum[lr] = sum;
+          bar_sync<1, kTcSoftmax>();
+          const uint32_t rows = min(static_cast<uint32_t>(kTcRows), all - it.rb * kTcRows);
+          for (uint32_t x = threadIdx.x; x < rows * (D / 4); x += kTcSoftmax) {
+            const uint32_t row = x / (D / 4), d = x % (D / 4) * 4;
+            const float mine = sm.top[row], total = sm.sum[row], by_total = total == 0.f ? 0.f : 1.f / total;
+            float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+            for (uint32_t i = 0; i < parts; ++i) {
+              const uint64_t at = part_at(i, row);
+              const float2 ms = __ldcg(&a.part_ms[at]);
+              const float4 z = __ldcg(reinterpret_cast<const float4*>(a.part + at * D + d));
+              const float k = ms.x == -INFINITY ? (ms.y == 0.f ? 0.f : 1.f) : exp2_fast(ms.x - mine);
+              y.x += k * z.x, y.y += k * z.y, y.z += k * z.z, y.w += k * z.w;
+            }
+            const uint32_t tok = (it.rb * kTcRows + row) / a.group, hd = it.head * a.group + (it.rb * kTcRows + row) % a.group;
+            T* o = reinterpret_cast<T*>(a.q.out) + static_cast<int64_t>(it.span.first + tok) * a.q.out_token +
+                   static_cast<int64_t>(hd) * a.q.out_head + d;
+            if (a.out_wide) {
+              *reinterpret_cast<uint2*>(o) = make_uint2(P::pack(y.x * by_total, y.y * by_total), P::pack(y.z * by_total, y.w * by_total));
+            } else {
+              o[0] = Elem<T>::from(y.x * by_total);
+              o[1] = Elem<T>::from(y.y * by_total);
+              o[2] = Elem<T>::from(y.z * by_total);
+              o[3] = Elem<T>::from(y.w * by_total);
+            }
+          }
+          bar_sync<1, kTcSoftmax>();
+        }
+      }
+    }
+  } else if (warp < (kTcSoftmax + kTcProducers) / 32) {
+    // ---------------------------------------------------------------- producers: a thread to a token
+    const uint32_t p = threadIdx.x - kTcSoftmax;
+    uint32_t n = 0;  // tiles so far
+    while (walk.next(it)) {  // to the end, as above
+      const uint32_t units = it.hi - it.lo, tiles = (units + 1) / 2;
+      const int32_t* table = b.table + static_cast<uint64_t>(it.seq) * b.table_stride;
+      // the fewest tokens that a row of the item sees
+      int32_t all_see = it.span.length;
+      if (a.causal) {
+        const int64_t x = static_cast<int64_t>(it.span.length) - it.span.count + it.rb * kTcRows / a.group + 1;
+        all_see = x > 0 ? static_cast<int32_t>(x) : 0;
+      }
+      struct Token {
+        uint32_t pos;   // of the first of its 64
+        bool some;      // there is such a 64
+        uint64_t row;   // in the pages; ~0 where there is nothing to see
+      };
+      const auto look = [&](uint32_t j) {
+        Token x{0, false, ~0ull};
+        const uint32_t unit = it.lo + 2 * j + p / 64;
+        if (unit >= it.hi) return x;
+        x.some = true;
+        x.pos = (a.mask ? a.tiles[static_cast<uint64_t>(it.seq) * a.tile_stride + unit] : unit) * kTile;
+        const uint32_t pos = x.pos + p % 64;
+        if (pos >= it.span.length) return x;
+        if (a.mask && (pos >= a.mask_stride || !a.mask[it.seq * a.mask_stride + pos])) return x;
+        const uint32_t page = static_cast<uint32_t>(table[pos >> b.page_shift]);
+        if (page >= b.n_pages) {
+          atomicOr(b.err, kKvErrPage);
+          return x;
+        }
+        x.row = page_row(b, (static_cast<int64_t>(page) << b.page_shift) | (pos & ((1u << b.page_shift) - 1)), it.head);
+        return x;
+      };
+      const auto tell = [&](const Token& x) {  // the tile's info, and where its tokens' rows are
+        TcInfo& info = sm.info[n % kTcInfo];
+        const uint32_t bits = __ballot_sync(0xffffffffu, x.row != ~0ull);
+        if (lane == 0) info.bits[p / 32] = bits;
+        if (p % 64 == 0) info.pos[p / 64] = static_cast<int32_t>(x.pos);
+        sm.row_of[n % kTcStages][p] = x.row;
+        const bool see = x.row != ~0ull && static_cast<int32_t>(x.pos + p % 64) < all_see;
+        uint32_t plain;
+        asm volatile(
+            "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\t"
+            "barrier.cta.red.and.pred q, 2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+            : "=r"(plain)
+            : "r"(static_cast<uint32_t>(see))
+            : "memory");
+        if (p == 0) info.plain = plain;
+        mbar_arrive(shared_address(&sm.info_full[n % kTcInfo]));
+      };
+      if (BITS == 4) {
+        uint4 kc[D / 32], vc[D / 32];
+        uint32_t kw = 0, vw = 0;
+        Token x = look(0);
+        const auto fetch = [&](const char* pages, const uint16_t* words, const Token& y, uint4* c, uint32_t& w) {
+          w = 0;
+          if (y.row == ~0ull) return;  // the scale of nothing is zero
+          const uint4* from = reinterpret_cast<const uint4*>(pages + y.row * (D / 2));
+#pragma unroll
+          for (int e = 0; e < D / 32; ++e) c[e] = __ldg(from + e);
+          w = D == 128 ? __ldg(reinterpret_cast<const uint32_t*>(words) + y.row) : __ldg(words + y.row);
+        };
+        const auto unpack = [&](char* to, const uint4* c, uint32_t w) {
+#pragma unroll
+          for (int gr = 0; gr < D / 64; ++gr) {
+            const Unpack<T> u(gr == 0 ? w & 0xFFFFu : w >> 16);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const uint4 y = c[2 * gr + e];
+              const uint32_t ws[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+              for (int f = 0; f < 4; ++f)
+                *reinterpret_cast<uint4*>(to + gr * S::kBlock + p * 128 + ((4 * e + f) ^ (p & 7)) * 16) = u(ws[f]);
+            }
+          }
+          fence_async_shared();
+        };
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) kc[e] = vc[e] = make_uint4(0, 0, 0, 0);
+        fetch(a.k, a.k_words, x, kc, kw);
+        for (uint32_t j = 0; j < tiles; ++j, ++n) {
+          const uint32_t st = n % kTcStages, round = n / kTcStages;
+          fetch(a.v, a.v_words, x, vc, vw);
+          const Token next = look(j + 1);
+          tell(x);
+          if (round > 0) ok = ok && tc_wait(&sm.k_empty[st], round - 1, stop);
+          if (ok) {
+            unpack(sm.k[st], kc, kw);
+            mbar_arrive(shared_address(&sm.k_full[st]));
+          }
+          fetch(a.k, a.k_words, next, kc, kw);
+          if (round > 0) ok = ok && tc_wait(&sm.v_empty[st], round - 1, stop);
+          if (ok) {
+            unpack(sm.v[st], vc, vw);
+            mbar_arrive(shared_address(&sm.v_full[st]));
+          }
+          x = next;
+        }
+      } else {
+        constexpr uint32_t kUnits = D / 8;  // 16-byte units of a token
+        const auto copy = [&](char* to, const char* pages, uint32_t slot) {
+#pragma unroll 4
+          for (uint32_t i = 0; i < kUnits; ++i) {
+            const uint32_t e = i * 128 + p, tok = e / kUnits, u = e % kUnits;
+            const uint64_t row = sm.row_of[slot][tok];
+            const bool live = row != ~0ull;
+            cp_async16(shared_address(to) + (u / 8) * S::kBlock + tok * 128 + ((u % 8) ^ (tok & 7)) * 16,
+                       pages + (live ? row * (D * 2) + u * 16 : 0), live);
+          }
+          cp_async_commit();
+        };
+        Token x = look(0);
+        for (uint32_t j = 0; j < tiles; ++j, ++n) {
+          const uint32_t st = n % kTcStages, round = n / kTcStages;
+          const Token next = look(j + 1);
+          tell(x);
+          if (round > 0) ok = ok && tc_wait(&sm.k_empty[st], round - 1, stop);
+          if (ok) copy(sm.k[st], a.k, st);
+          if (ok && j > 0) {  // the values of the tile before
+            cp_async_wait<1>();
+            fence_async_shared();
+            mbar_arrive(shared_address(&sm.v_full[(n - 1) % kTcStages]));
+          }
+          if (round > 0) ok = ok && tc_wait(&sm.v_empty[st], round - 1, stop);
+          if (ok) {
+            copy(sm.v[st], a.v, st);
+            cp_async_wait<1>();
+            fence_async_shared();
+            mbar_arrive(shared_address(&sm.k_full[st]));
+          }
+          x = next;
+        }
+        cp_async_wait<0>();
+        if (ok && tiles) {
+          fence_async_shared();
+          mbar_arrive(shared_address(&sm.v_full[(n - 1) % kTcStages]));
+        }
+      }
+    }
+    cp_async_wait<0>();
+  } else if (lane == 0) {
+    // ---------------------------------------------------------------- products
+    constexpr uint32_t kQK = tc_idesc<T>(128, kTcKeys, false), kPV = tc_idesc<T>(128, D, true);
+    uint32_t n = 0, q_n[2] = {0, 0}, p_n[2] = {0, 0}, o_n[2] = {0, 0};
+    while (ok && walk.next(it)) {
+      const uint32_t tiles = (it.hi - it.lo + 1) / 2;
+      if (tiles == 0) continue;
+      const uint32_t halves = it.span.count * a.group - it.rb * kTcRows > 128 ? 2 : 1;
+      const auto qk = [&](uint32_t t, uint32_t j) {
+        const uint32_t st = (n + j) % kTcStages;
+        if (j == 0) ok = ok && tc_wait(&sm.q_full[t], q_n[t]++, stop);
+        // S's place holds the P of the tokens before
+        if (j > 0) ok = ok && tc_wait(&sm.o_full[t], o_n[t]++, stop);
+        ok = ok && tc_wait(&sm.k_full[st], (n + j) / kTcStages, stop);
+        if (!ok) return;
+        tc_fence_after();
+        const uint32_t q = shared_address(sm.q[t]), k = shared_address(sm.k[st]);
+#pragma unroll
+        for (int e = 0; e < D / 16; ++e)
+          tc_mma_ss(tmem + t * 128, tc_desc(q + (e / 4) * S::kBlock + (e % 4) * 32, 16), tc_desc(k + (e / 4) * S::kBlock + (e % 4) * 32, 16), kQK, e > 0);
+        tc_commit(&sm.s_full[t]);
+        if (t + 1 == halves) tc_commit(&sm.k_empty[st]);
+      };
+      const auto pv = [&](uint32_t t, uint32_t j) {
+        const uint32_t st = (n + j) % kTcStages;
+        ok = ok && tc_wait(&sm.p_full[t], p_n[t]++, stop) && tc_wait(&sm.v_full[st], (n + j) / kTcStages, stop);
+        if (!ok) return;
+        tc_fence_after();
+        const uint32_t v = shared_address(sm.v[st]);
+#pragma unroll
+        for (int e = 0; e < kTcKeys / 16; ++e)
+          tc_mma_ts(tmem + 256 + t * 128, tmem + t * 128 + e * 8, tc_desc(v + e * 2048, S::kBlock), kPV, j > 0 || e > 0);
+        tc_commit(&sm.o_full[t]);
+        if (t + 1 == halves) tc_commit(&sm.v_empty[st]);
+      };
+      for (uint32_t t = 0; t < halves; ++t) qk(t, 0);
+      for (uint32_t j = 0; ok && j < tiles; ++j)
+        for (uint32_t t = 0; ok && t < halves; ++t) {
+          pv(t, j);
+          if (j + 1 < tiles) qk(t, j + 1);
+        }
+      for (uint32_t t = 0; t < halves; ++t) ++o_n[t];  // the last phase, which the softmax waits for
+      n += tiles;
+    }
+    // what was issued, and its arrivals, finish before the tensor memory goes and the CTA ends
+    tc_commit(&sm.drained);
+    if (!mbar_wait_bounded(shared_address(&sm.drained), 0, kTcTimeout)) atomicOr(b.err, kKvErrWait);
+  }
+  if (!ok) atomicOr(b.err, kKvErrWait);
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kTcThreads / 32 - 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  }
+}
+
+// One CTA to an SM, whose tensor memory it takes whole: more than half of its shared memory.
+template <int D>
+constexpr size_t tc_smem() {
+  return sizeof(TcSmem<D>) + 1024 > 120 * 1024 ? sizeof(TcSmem<D>) + 1024 : 120 * 1024;
+}
+
+}  // namespace
+}  // namespace cofie

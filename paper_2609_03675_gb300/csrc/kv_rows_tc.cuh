@@ -36,8 +36,7 @@ constexpr int kTcKeys = 128;
 constexpr int kTcSoftmax = 256;                  // threads: warps 0 to 7
 constexpr int kTcProducers = 128;                // warps 8 to 11
 constexpr int kTcThreads = kTcSoftmax + kTcProducers + 32;  // and the MMA warp
-constexpr int kTcStages = 2;
-constexpr int kTcInfo = 4;
+constexpr int kTcInfo = 8;  // more than the stages: a tile is told before its place is free
 constexpr float kTcRaise = 8.f;
 constexpr uint64_t kTcTimeout = 1000000000ull;
 
@@ -51,14 +50,15 @@ template <int D>
 struct TcSmem {
   static constexpr int kBlock = 128 * 128;               // 128 rows of 64 values
   static constexpr int kTileBytes = kBlock * (D / 64);   // 128 rows of D values
+  static constexpr int kStages = D == 64 ? 4 : 2;        // of keys, and of values
   char q[2][kTileBytes];
-  char k[kTcStages][kTileBytes];
-  char v[kTcStages][kTileBytes];
+  char k[kStages][kTileBytes];
+  char v[kStages][kTileBytes];
   Plan<kTcThreads> plan;
   TcInfo info[kTcInfo];
-  uint64_t row_of[kTcStages][kTcKeys];  // 16 bits: the tokens' rows in the pages, ~0 where there is nothing to see
+  uint64_t row_of[kStages][kTcKeys];  // 16 bits: the tokens' rows in the pages, ~0 where there is nothing to see
   float top[kTcRows], sum[kTcRows];
-  uint64_t k_full[kTcStages], k_empty[kTcStages], v_full[kTcStages], v_empty[kTcStages];
+  uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
   uint64_t info_full[kTcInfo], q_full[2], s_full[2], p_full[2], o_full[2], drained;
   uint32_t tmem, stop, last_here;
 };
@@ -209,6 +209,16 @@ struct Unpack<__half> {
   }
 };
 
+__device__ __forceinline__ float most_of(const uint32_t* x, float top) {
+  float a = top, b = __uint_as_float(x[0]);
+#pragma unroll
+  for (int f = 1; f < 31; f += 2) {
+    a = fmaxf(a, __uint_as_float(x[f]));
+    b = fmaxf(b, __uint_as_float(x[f + 1]));
+  }
+  return fmaxf(fmaxf(a, __uint_as_float(x[31])), b);
+}
+
 template <typename T, int D, int BITS>
 __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_constant__ AttendArgs a) {
   using P = Pair<T>;
@@ -218,7 +228,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
   pdl_trigger();
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kTcStages; ++i) {
+    for (int i = 0; i < S::kStages; ++i) {
       mbar_init(shared_address(&sm.k_full[i]), kTcProducers);
       mbar_init(shared_address(&sm.v_full[i]), kTcProducers);
       mbar_init(shared_address(&sm.k_empty[i]), 1);
@@ -302,30 +312,29 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
           if (!ok) break;
           tc_fence_after();
           const bool plain = info.plain != 0;
-          const auto masked = [&](uint32_t col) {  // whether this row does not see the tile's token col
-            const int32_t pos = info.pos[col / 64] + static_cast<int32_t>(col % 64);
-            return !((info.bits[col / 32] >> (col % 32)) & 1u) || pos >= seen;
+          // hides those of 32 tokens that this row does not see
+          const auto hide = [&](uint32_t e, uint32_t* y) {
+            const int32_t n = seen - info.pos[e / 2] - static_cast<int32_t>(e % 2) * 32;  // the row sees the first n
+            const uint32_t see = info.bits[e] & (n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1);
+            if (__all_sync(0xffffffffu, see == ~0u)) return;
+#pragma unroll
+            for (int f = 0; f < 32; ++f)
+              if (!(see & (1u << f))) y[f] = 0xff800000u;
           };
           // the maximum
           float top = -INFINITY;
-          uint32_t x[2][32];
-          tc_ld32(s_col, x[0]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            tc_wait_ld(x[e % 2]);
-            if (e < 3) tc_ld32(s_col + 32 * (e + 1), x[(e + 1) % 2]);
-            if (!plain) {
-#pragma unroll
-              for (int f = 0; f < 32; ++f)
-                if (masked(32 * e + f)) x[e % 2][f] = 0xff800000u;
-            }
-            float top2 = -INFINITY;
-#pragma unroll
-            for (int f = 0; f < 32; f += 2) {
-              top = fmaxf(top, __uint_as_float(x[e % 2][f]));
-              top2 = fmaxf(top2, __uint_as_float(x[e % 2][f + 1]));
-            }
-            top = fmaxf(top, top2);
+          uint32_t x[32], y[32];
+          tc_ld32(s_col, x);
+#pragma unroll 1
+          for (uint32_t e = 0; e < 4; e += 2) {
+            tc_wait_ld(x);
+            tc_ld32(s_col + 32 * (e + 1), y);
+            if (!plain) hide(e, x);
+            top = most_of(x, top);
+            tc_wait_ld(y);
+            if (e == 0) tc_ld32(s_col + 64, x);
+            if (!plain) hide(e + 1, y);
+            top = most_of(y, top);
           }
           top *= by;
           const bool raise = top > m + kTcRaise || (m == -INFINITY && top > -INFINITY);
@@ -336,7 +345,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
               ok = __all_sync(0xffffffffu, ok);
               if (!ok) break;
               tc_fence_after();
-              uint32_t y[32];
 #pragma unroll 1
               for (int e = 0; e < D / 32; ++e) {
                 tc_ld32(o_col + 32 * e, y);
@@ -351,32 +359,34 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
             m = to;
           }
           if (j > 0) ++o_n;  // the phase of the tokens before, waited for or not
-          // the exponentials
+          // the exponentials. S's columns up to 32 e + 31 are read when P's from 16 e are written
           const float from = m == -INFINITY ? 0.f : -m;
-          float l2 = 0.f;
-          tc_ld32(s_col, x[0]);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            tc_wait_ld(x[e % 2]);
-            if (e < 3) tc_ld32(s_col + 32 * (e + 1), x[(e + 1) % 2]);
-            if (!plain) {
-#pragma unroll
-              for (int f = 0; f < 32; ++f)
-                if (masked(32 * e + f)) x[e % 2][f] = 0xff800000u;
-            }
-            uint32_t y[16];
+          const auto exponentials = [&](uint32_t e, const uint32_t* z) {
+            uint32_t w[16];
+            float l2 = 0.f;
 #pragma unroll
             for (int f = 0; f < 16; ++f) {
-              const float p0 = exp2_fast(fmaf(__uint_as_float(x[e % 2][2 * f]), by, from));
-              const float p1 = exp2_fast(fmaf(__uint_as_float(x[e % 2][2 * f + 1]), by, from));
+              const float p0 = exp2_fast(fmaf(__uint_as_float(z[2 * f]), by, from));
+              const float p1 = exp2_fast(fmaf(__uint_as_float(z[2 * f + 1]), by, from));
               l += p0;
               l2 += p1;
-              y[f] = P::pack(p0, p1);
+              w[f] = P::pack(p0, p1);
             }
-            // S's columns up to 32 e + 31 are read, P's from 16 e are written
-            tc_st16(s_col + 16 * e, y);
+            l += l2;
+            tc_st16(s_col + 16 * e, w);
+          };
+          tc_ld32(s_col, x);
+#pragma unroll 1
+          for (uint32_t e = 0; e < 4; e += 2) {
+            tc_wait_ld(x);
+            tc_ld32(s_col + 32 * (e + 1), y);
+            if (!plain) hide(e, x);
+            exponentials(e, x);
+            tc_wait_ld(y);
+            if (e == 0) tc_ld32(s_col + 64, x);
+            if (!plain) hide(e + 1, y);
+            exponentials(e + 1, y);
           }
-          l += l2;
           tc_wait_st();
           tc_fence_before();
           mbar_arrive(shared_address(&sm.p_full[t]));
@@ -534,7 +544,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
         const uint32_t bits = __ballot_sync(0xffffffffu, x.row != ~0ull);
         if (lane == 0) info.bits[p / 32] = bits;
         if (p % 64 == 0) info.pos[p / 64] = static_cast<int32_t>(x.pos);
-        sm.row_of[n % kTcStages][p] = x.row;
+        sm.row_of[n % S::kStages][p] = x.row;
         const bool see = x.row != ~0ull && static_cast<int32_t>(x.pos + p % 64) < all_see;
         uint32_t plain;
         asm volatile(
@@ -547,52 +557,59 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
         mbar_arrive(shared_address(&sm.info_full[n % kTcInfo]));
       };
       if (BITS == 4) {
-        uint4 kc[D / 32], vc[D / 32];
-        uint32_t kw = 0, vw = 0;
-        Token x = look(0);
-        const auto fetch = [&](const char* pages, const uint16_t* words, const Token& y, uint4* c, uint32_t& w) {
-          w = 0;
-          if (y.row == ~0ull) return;  // the scale of nothing is zero
-          const uint4* from = reinterpret_cast<const uint4*>(pages + y.row * (D / 2));
-#pragma unroll
-          for (int e = 0; e < D / 32; ++e) c[e] = __ldg(from + e);
-          w = D == 128 ? __ldg(reinterpret_cast<const uint32_t*>(words) + y.row) : __ldg(words + y.row);
+        // Keys and values in turn, a step each, through one piece of code (three roles' code is more than the
+        // instruction cache likes); codes are fetched three steps ahead, into registers.
+        struct Codes {
+          uint4 c[D / 32];
+          uint32_t w;
         };
-        const auto unpack = [&](char* to, const uint4* c, uint32_t w) {
+        const auto fetch = [&](uint32_t step, const Token& y) {
+          Codes z;
 #pragma unroll
-          for (int gr = 0; gr < D / 64; ++gr) {
-            const Unpack<T> u(gr == 0 ? w & 0xFFFFu : w >> 16);
+          for (int e = 0; e < D / 32; ++e) z.c[e] = make_uint4(0, 0, 0, 0);
+          z.w = 0;  // the scale of nothing is zero
+          if (y.row != ~0ull) {
+            const uint4* from = reinterpret_cast<const uint4*>((step % 2 ? a.v : a.k) + y.row * (D / 2));
+            const uint16_t* words = step % 2 ? a.v_words : a.k_words;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const uint4 y = c[2 * gr + e];
-              const uint32_t ws[4] = {y.x, y.y, y.z, y.w};
+            for (int e = 0; e < D / 32; ++e) z.c[e] = __ldg(from + e);
+            z.w = D == 128 ? __ldg(reinterpret_cast<const uint32_t*>(words) + y.row) : __ldg(words + y.row);
+          }
+          return z;
+        };
+        Token x0 = look(0), x1 = look(1), x2 = look(2);
+        Codes c0 = fetch(0, x0), c1 = fetch(1, x0), c2 = fetch(2, x1);
+#pragma unroll 1
+        for (uint32_t step = 0; step < 2 * tiles; ++step) {
+          const uint32_t st = n % S::kStages, round = n / S::kStages, v = step % 2;
+          if (!v) tell(x0);
+          if (round > 0) ok = ok && tc_wait(v ? &sm.v_empty[st] : &sm.k_empty[st], round - 1, stop);
+          if (ok) {
+            char* to = v ? sm.v[st] : sm.k[st];
 #pragma unroll
-              for (int f = 0; f < 4; ++f)
-                *reinterpret_cast<uint4*>(to + gr * S::kBlock + p * 128 + ((4 * e + f) ^ (p & 7)) * 16) = u(ws[f]);
+            for (int gr = 0; gr < D / 64; ++gr) {
+              const Unpack<T> u(gr == 0 ? c0.w & 0xFFFFu : c0.w >> 16);
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                const uint4 y = c0.c[2 * gr + e];
+                const uint32_t ws[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                for (int f = 0; f < 4; ++f)
+                  *reinterpret_cast<uint4*>(to + gr * S::kBlock + p * 128 + ((4 * e + f) ^ (p & 7)) * 16) = u(ws[f]);
+              }
             }
+            fence_async_shared();
+            mbar_arrive(shared_address(v ? &sm.v_full[st] : &sm.k_full[st]));
           }
-          fence_async_shared();
-        };
-#pragma unroll
-        for (int e = 0; e < D / 32; ++e) kc[e] = vc[e] = make_uint4(0, 0, 0, 0);
-        fetch(a.k, a.k_words, x, kc, kw);
-        for (uint32_t j = 0; j < tiles; ++j, ++n) {
-          const uint32_t st = n % kTcStages, round = n / kTcStages;
-          fetch(a.v, a.v_words, x, vc, vw);
-          const Token next = look(j + 1);
-          tell(x);
-          if (round > 0) ok = ok && tc_wait(&sm.k_empty[st], round - 1, stop);
-          if (ok) {
-            unpack(sm.k[st], kc, kw);
-            mbar_arrive(shared_address(&sm.k_full[st]));
+          c0 = c1;
+          c1 = c2;
+          c2 = fetch(step + 3, v ? x2 : x1);  // step + 3: values of the next tile, or keys of the one after
+          if (v) {
+            x0 = x1;
+            x1 = x2;
+            x2 = look(step / 2 + 3);
+            ++n;
           }
-          fetch(a.k, a.k_words, next, kc, kw);
-          if (round > 0) ok = ok && tc_wait(&sm.v_empty[st], round - 1, stop);
-          if (ok) {
-            unpack(sm.v[st], vc, vw);
-            mbar_arrive(shared_address(&sm.v_full[st]));
-          }
-          x = next;
         }
       } else {
         constexpr uint32_t kUnits = D / 8;  // 16-byte units of a token
@@ -609,7 +626,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
         };
         Token x = look(0);
         for (uint32_t j = 0; j < tiles; ++j, ++n) {
-          const uint32_t st = n % kTcStages, round = n / kTcStages;
+          const uint32_t st = n % S::kStages, round = n / S::kStages;
           const Token next = look(j + 1);
           tell(x);
           if (round > 0) ok = ok && tc_wait(&sm.k_empty[st], round - 1, stop);
@@ -617,7 +634,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
           if (ok && j > 0) {  // the values of the tile before
             cp_async_wait<1>();
             fence_async_shared();
-            mbar_arrive(shared_address(&sm.v_full[(n - 1) % kTcStages]));
+            mbar_arrive(shared_address(&sm.v_full[(n - 1) % S::kStages]));
           }
           if (round > 0) ok = ok && tc_wait(&sm.v_empty[st], round - 1, stop);
           if (ok) {
@@ -631,7 +648,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
         cp_async_wait<0>();
         if (ok && tiles) {
           fence_async_shared();
-          mbar_arrive(shared_address(&sm.v_full[(n - 1) % kTcStages]));
+          mbar_arrive(shared_address(&sm.v_full[(n - 1) % S::kStages]));
         }
       }
     }
@@ -645,11 +662,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
       if (tiles == 0) continue;
       const uint32_t halves = it.span.count * a.group - it.rb * kTcRows > 128 ? 2 : 1;
       const auto qk = [&](uint32_t t, uint32_t j) {
-        const uint32_t st = (n + j) % kTcStages;
+        const uint32_t st = (n + j) % S::kStages;
         if (j == 0) ok = ok && tc_wait(&sm.q_full[t], q_n[t]++, stop);
         // S's place holds the P of the tokens before
         if (j > 0) ok = ok && tc_wait(&sm.o_full[t], o_n[t]++, stop);
-        ok = ok && tc_wait(&sm.k_full[st], (n + j) / kTcStages, stop);
+        ok = ok && tc_wait(&sm.k_full[st], (n + j) / S::kStages, stop);
         if (!ok) return;
         tc_fence_after();
         const uint32_t q = shared_address(sm.q[t]), k = shared_address(sm.k[st]);
@@ -660,8 +677,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
         if (t + 1 == halves) tc_commit(&sm.k_empty[st]);
       };
       const auto pv = [&](uint32_t t, uint32_t j) {
-        const uint32_t st = (n + j) % kTcStages;
-        ok = ok && tc_wait(&sm.p_full[t], p_n[t]++, stop) && tc_wait(&sm.v_full[st], (n + j) / kTcStages, stop);
+        const uint32_t st = (n + j) % S::kStages;
+        ok = ok && tc_wait(&sm.p_full[t], p_n[t]++, stop) && tc_wait(&sm.v_full[st], (n + j) / S::kStages, stop);
         if (!ok) return;
         tc_fence_after();
         const uint32_t v = shared_address(sm.v[st]);

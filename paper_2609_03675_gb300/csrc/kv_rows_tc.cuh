@@ -54,6 +54,9 @@ struct TcSmem {
   char q[2][kTileBytes];
   char k[kStages][kTileBytes];
   char v[kStages][kTileBytes];
+  static constexpr int kRaw = 3;                         // of codes as they lie in the pages
+  char raw[kRaw][128 * (D / 2)];
+  uint32_t raw_word[kRaw][128];
   Plan<kTcThreads> plan;
   TcInfo info[kTcInfo];
   uint64_t row_of[kStages][kTcKeys];  // 16 bits: the tokens' rows in the pages, ~0 where there is nothing to see
@@ -85,6 +88,9 @@ __device__ __forceinline__ bool tc_wait(const uint64_t* bar, uint32_t parity, ui
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
 template <int ID, int THREADS>
 __device__ __forceinline__ void bar_sync() {
   asm volatile("bar.sync %0, %1;" ::"n"(ID), "n"(THREADS) : "memory");
@@ -558,40 +564,42 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
       };
       if (BITS == 4) {
         // Keys and values in turn, a step each, through one piece of code (three roles' code is more than the
-        // instruction cache likes); codes are fetched three steps ahead, into registers.
-        struct Codes {
-          uint4 c[D / 32];
-          uint32_t w;
-        };
+        // instruction cache likes); codes are fetched three steps ahead, each thread's to places of its own.
         const auto fetch = [&](uint32_t step, const Token& y) {
-          Codes z;
-#pragma unroll
-          for (int e = 0; e < D / 32; ++e) z.c[e] = make_uint4(0, 0, 0, 0);
-          z.w = 0;  // the scale of nothing is zero
           if (y.row != ~0ull) {
-            const uint4* from = reinterpret_cast<const uint4*>((step % 2 ? a.v : a.k) + y.row * (D / 2));
-            const uint16_t* words = step % 2 ? a.v_words : a.k_words;
+            const char* from = (step % 2 ? a.v : a.k) + y.row * (D / 2);
+            const uint32_t to = shared_address(sm.raw[step % S::kRaw]) + p * 16;
 #pragma unroll
-            for (int e = 0; e < D / 32; ++e) z.c[e] = __ldg(from + e);
-            z.w = D == 128 ? __ldg(reinterpret_cast<const uint32_t*>(words) + y.row) : __ldg(words + y.row);
+            for (int e = 0; e < D / 32; ++e) cp_async16(to + e * 2048, from + e * 16, true);
+            // the word, or two, of the token; with one, of it and its neighbour (an even token's row is even)
+            const uint16_t* words = (step % 2 ? a.v_words : a.k_words) + (D == 128 ? 2 * y.row : y.row & ~1ull);
+            cp_async4(shared_address(&sm.raw_word[step % S::kRaw][p]), words);
+          } else {
+            sm.raw_word[step % S::kRaw][p] = 0;  // the scale of nothing is zero
           }
-          return z;
+          cp_async_commit();
         };
         Token x0 = look(0), x1 = look(1), x2 = look(2);
-        Codes c0 = fetch(0, x0), c1 = fetch(1, x0), c2 = fetch(2, x1);
+        static_assert(S::kRaw == 3, "three steps ahead");
+        fetch(0, x0);
+        fetch(1, x0);
+        fetch(2, x1);
 #pragma unroll 1
         for (uint32_t step = 0; step < 2 * tiles; ++step) {
           const uint32_t st = n % S::kStages, round = n / S::kStages, v = step % 2;
           if (!v) tell(x0);
           if (round > 0) ok = ok && tc_wait(v ? &sm.v_empty[st] : &sm.k_empty[st], round - 1, stop);
+          cp_async_wait<S::kRaw - 1>();
           if (ok) {
             char* to = v ? sm.v[st] : sm.k[st];
+            const char* from = sm.raw[step % S::kRaw] + p * 16;
+            const uint32_t w = sm.raw_word[step % S::kRaw][p];
 #pragma unroll
             for (int gr = 0; gr < D / 64; ++gr) {
-              const Unpack<T> u(gr == 0 ? c0.w & 0xFFFFu : c0.w >> 16);
+              const Unpack<T> u((D == 64 && p % 2) || gr == 1 ? w >> 16 : w & 0xFFFFu);
 #pragma unroll
               for (int e = 0; e < 2; ++e) {
-                const uint4 y = c0.c[2 * gr + e];
+                const uint4 y = *reinterpret_cast<const uint4*>(from + (2 * gr + e) * 2048);
                 const uint32_t ws[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
                 for (int f = 0; f < 4; ++f)
@@ -601,9 +609,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
             fence_async_shared();
             mbar_arrive(shared_address(v ? &sm.v_full[st] : &sm.k_full[st]));
           }
-          c0 = c1;
-          c1 = c2;
-          c2 = fetch(step + 3, v ? x2 : x1);  // step + 3: values of the next tile, or keys of the one after
+          fetch(step + 3, v ? x2 : x1);  // step + 3: values of the next tile, or keys of the one after
           if (v) {
             x0 = x1;
             x1 = x2;
@@ -611,6 +617,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
             ++n;
           }
         }
+        cp_async_wait<0>();
       } else {
         constexpr uint32_t kUnits = D / 8;  // 16-byte units of a token
         const auto copy = [&](char* to, const char* pages, uint32_t slot) {

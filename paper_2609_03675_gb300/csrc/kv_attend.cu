@@ -72,7 +72,7 @@ SplitKernel split_kernel(const cofie_kv_params& p, int i, size_t* smem) {
 
 template <typename T, int D>
 SplitKernel rows_kernel(uint32_t bits, size_t* smem) {
-  *smem = tc_smem<D>();
+  *smem = bits == 4 ? tc_smem<D, 4>() : tc_smem<D, 16>();
   return bits == 4 ? attend_rows_tc<T, D, 4> : attend_rows_tc<T, D, 16>;
 }
 SplitKernel rows_kernel(const cofie_kv_params& p, size_t* smem) {

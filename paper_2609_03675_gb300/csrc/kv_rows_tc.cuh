@@ -2,24 +2,26 @@
 // products bound it, so both run on tcgen05.
 //
 // A CTA takes up to 256 query rows (new tokens x heads of the group) of one
-// key/value head as two tiles of 128, and the cached tokens 128 at a time:
-//   producers  four warps: keys and values of the next tokens into shared memory
-//              (128-byte swizzle), copied (16 bits) or unpacked to (n - z) s,
-//              which the 16-bit types hold exactly (4 bits); a thread to a token
-//   MMA        one thread: S = Q K^T into tensor memory (128 x 128 fp32 a tile),
-//              and O += P V with P read from tensor memory
+// key/value head as two tiles of 128, and the cached tokens 64 at a time:
 //   softmax    four warps a tile, a thread to a row: maximum, exponentials, P
 //              back into S's place in 16 bits; at the end O out
-// While one tile's softmax runs, the other's products do. The running maximum
-// that exponentials refer to is raised only when the true one passes it by 2^8
-// (then O is brought down in tensor memory), which seldom happens after the
-// first tokens.
+//   producers  four warps for keys, four for values: the next tokens into shared
+//              memory (128-byte swizzle), copied (16 bits) or unpacked to
+//              (n - z) s, which the 16-bit types hold exactly (4 bits)
+//   MMA        one thread: S = Q K^T into tensor memory (128 x 64 fp32 a tile),
+//              and O += P V with P read from tensor memory
+// The running maximum that exponentials refer to is raised only when the true
+// one passes it by 2^8 (then O is brought down in tensor memory), which seldom
+// happens after the first tokens.
 //
-// Tensor memory: S0 S1 O0 O1, 128 columns each, P in the first 64 of its S. P V
-// of a tile has to be done before Q K^T of the next tokens writes there.
+// Tensor memory: O0 O1 (D columns each) and for each tile two S of 64 columns,
+// P in the first 32 of its S: while the softmax works on one S, the products
+// of the next tokens fill the other. With one S of 128 tokens a tile, the
+// softmax waited 2300 of 5900 cycles for P V and the next Q K^T to be done
+// (256 new tokens over 65792 cached ones of 4 bits: 376 us).
 //
 // For each 256 x 128 block of the scores the tensor core needs 2048 cycles (head
-// of 128), shared memory 1536 for its operands and 512 for writing them, the
+// of 128), shared memory 2048 for its operands and 512 for writing them, the
 // exponentials 1024 and more.
 #pragma once
 
@@ -32,42 +34,44 @@ namespace cofie {
 namespace {
 
 constexpr int kTcRows = 256;
-constexpr int kTcKeys = 128;
-constexpr int kTcSoftmax = 256;                  // threads: warps 0 to 7
-constexpr int kTcProducers = 128;                // warps 8 to 11
-constexpr int kTcThreads = kTcSoftmax + kTcProducers + 32;  // and the MMA warp
-constexpr int kTcInfo = 8;  // more than the stages: a tile is told before its place is free
+constexpr int kTcSoftmax = 256;    // threads: warps 0 to 7
+constexpr int kTcProducers = 128;  // for keys, and as many for values
+constexpr int kTcThreads = kTcSoftmax + 2 * kTcProducers + 128;  // and a group of four warps with the one that issues
+constexpr int kTcStages = 4;       // of keys, and of values
+constexpr int kTcInfo = 8;         // more than the stages: a tile is told before its place is free
+constexpr int kTcRaw = 3;          // codes as they lie in the pages
 constexpr float kTcRaise = 8.f;
 constexpr uint64_t kTcTimeout = 1000000000ull;
+// Registers: all threads start with 96; 256 x 144 + 256 x 72 + 128 x 40 is less than 640 x 96.
+constexpr int kTcRegsSoftmax = 144, kTcRegsProducer = 72, kTcRegsIssuer = 40;
 
 struct TcInfo {
-  uint32_t bits[4];  // tokens that some row may see
-  int32_t pos[2];    // first token of each 64
+  uint32_t bits[2];  // tokens that some row may see
+  int32_t pos;       // the first token
   uint32_t plain;    // every token is seen by every row
 };
 
-template <int D>
+template <int D, int BITS>
 struct TcSmem {
-  static constexpr int kBlock = 128 * 128;               // 128 rows of 64 values
-  static constexpr int kTileBytes = kBlock * (D / 64);   // 128 rows of D values
-  static constexpr int kStages = D == 64 ? 4 : 2;        // of keys, and of values
-  char q[2][kTileBytes];
-  char k[kStages][kTileBytes];
-  char v[kStages][kTileBytes];
-  static constexpr int kRaw = 3;                         // of codes as they lie in the pages
-  char raw[kRaw][128 * (D / 2)];
-  uint32_t raw_word[kRaw][128];
+  static constexpr int kBlockQ = 128 * 128;  // 128 rows of 64 values
+  static constexpr int kBlock = kTile * 128;  // 64 rows of 64 values
+  char q[2][kBlockQ * (D / 64)];
+  char kv[2][kTcStages][kBlock * (D / 64)];  // keys, values
+  char raw[2][BITS == 4 ? kTcRaw : 1][BITS == 4 ? kTile * (D / 2) : 16];
+  uint32_t raw_word[2][kTcRaw][kTile];
+  uint64_t row_of[2][BITS == 4 ? 1 : kTcStages][kTile];  // 16 bits: the tokens' rows in the pages, ~0 where there is nothing
   Plan<kTcThreads> plan;
   TcInfo info[kTcInfo];
-  uint64_t row_of[kStages][kTcKeys];  // 16 bits: the tokens' rows in the pages, ~0 where there is nothing to see
   float top[kTcRows], sum[kTcRows];
-  uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
-  uint64_t info_full[kTcInfo], q_full[2], s_full[2], p_full[2], o_full[2], drained;
+  uint64_t full[2][kTcStages], empty[2][kTcStages];  // keys, values
+  // A barrier's phase can be told from the one before only. O is ready twice before anyone has to look, so it has a
+  // barrier for even tiles and one for odd ones, as S and P have.
+  uint64_t info_full[kTcInfo], q_full[2], s_full[2][2], p_full[2][2], o_full[2][2], drained;
   uint32_t tmem, stop, last_here;
 };
 
 // A wait for a barrier's phase that ends, with false, when it runs out or another's has.
-__device__ __noinline__ bool tc_wait_slow(uint32_t bar, uint32_t parity, volatile uint32_t* stop) {
+__device__ __forceinline__ bool tc_wait_slow(uint32_t bar, uint32_t parity, volatile uint32_t* stop) {
   const uint64_t t0 = globaltimer_ns();
   for (;;) {
 #pragma unroll 1
@@ -100,36 +104,46 @@ __device__ __forceinline__ void bar_sync() {
 // atom of 1024. K-major: rows are M or N, the 64 values of a row are K; the
 // leading offset is not used. MN-major: rows are K, the 64 values M or N, the
 // next 64 lie `leading` bytes on.
-__device__ __forceinline__ uint64_t tc_desc(uint32_t addr, uint32_t leading) {
-  uint64_t d = (addr >> 4) & 0x3FFFu;
-  d |= static_cast<uint64_t>(leading >> 4) << 16;
-  d |= static_cast<uint64_t>(1024u >> 4) << 32;
-  d |= 1ull << 46;
-  d |= 2ull << 61;
-  return d;
-}
+// (The descriptor's upper half is the same for all: eight rows' 1024 bytes, the version, the swizzle.)
+__device__ __forceinline__ uint32_t tc_desc(uint32_t addr, uint32_t leading) { return (addr >> 4) | (leading >> 4) << 16; }
+constexpr uint32_t kTcDescUpper = (1024u >> 4) | 1u << 14 | 2u << 29;
 // fp32 sums of products of 16-bit values; B K-major or MN-major.
 template <typename T>
 __device__ __forceinline__ constexpr uint32_t tc_idesc(uint32_t m, uint32_t n, bool b_mn) {
   const uint32_t type = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
   return (1u << 4) | (type << 7) | (type << 10) | ((b_mn ? 1u : 0u) << 16) | ((n >> 3) << 17) | ((m >> 4) << 24);
 }
-__device__ __forceinline__ void tc_mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+// One thread of the warp, chosen once. The products are written for a whole warp, of which that thread issues: in code
+// that a single thread runs, the operands' way into uniform registers took 125 cycles a product.
+__device__ __forceinline__ uint32_t tc_leader() {
+  uint32_t x;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(x));
+  return x;
+}
+__device__ __forceinline__ void tc_mma_ss(uint32_t leader, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t acc) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"(acc)
+      "{\n\t.reg .pred p, q;\n\t.reg .b64 x, y;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "mov.b64 x, {%1, %6};\n\tmov.b64 y, {%2, %6};\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"(acc), "r"(leader), "n"(kTcDescUpper)
       : "memory");
 }
-__device__ __forceinline__ void tc_mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+__device__ __forceinline__ void tc_mma_ts(uint32_t leader, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t acc) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-      "r"(a), "l"(b), "r"(idesc), "r"(acc)
+      "{\n\t.reg .pred p, q;\n\t.reg .b64 y;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "mov.b64 y, {%2, %6};\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"(acc), "r"(leader), "n"(kTcDescUpper)
       : "memory");
 }
-__device__ __forceinline__ void tc_commit(uint64_t* bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(shared_address(bar)) : "memory");
+__device__ __forceinline__ void tc_commit(uint32_t leader, uint64_t* bar) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(shared_address(bar)),
+      "r"(leader)
+      : "memory");
 }
 __device__ __forceinline__ void tc_ld32(uint32_t taddr, uint32_t* r) {
   asm volatile(
@@ -141,22 +155,22 @@ __device__ __forceinline__ void tc_ld32(uint32_t taddr, uint32_t* r) {
         "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(taddr));
 }
-__device__ __forceinline__ void tc_st32(uint32_t taddr, const uint32_t* r) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::"r"(r[0]),
-      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
-      "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]),
-      "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]),
-      "r"(taddr)
-      : "memory");
-}
 __device__ __forceinline__ void tc_st16(uint32_t taddr, const uint32_t* r) {
   asm volatile(
       "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(
           r[0]),
       "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
       "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
+      : "memory");
+}
+// 16 columns, waited for.
+__device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+      "tcgen05.wait::ld.sync.aligned;"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr)
       : "memory");
 }
 // Waits for this thread's loads from tensor memory; the registers they fill pass through it, so that no use of them
@@ -215,37 +229,57 @@ struct Unpack<__half> {
   }
 };
 
-__device__ __forceinline__ float most_of(const uint32_t* x, float top) {
-  float a = top, b = __uint_as_float(x[0]);
+// The largest of 64 values and `top`.
+__device__ __forceinline__ float most_of(const uint32_t* x, const uint32_t* y, float top) {
+  float a = top, b = __uint_as_float(y[0]);
 #pragma unroll
-  for (int f = 1; f < 31; f += 2) {
-    a = fmaxf(a, __uint_as_float(x[f]));
-    b = fmaxf(b, __uint_as_float(x[f + 1]));
-  }
-  return fmaxf(fmaxf(a, __uint_as_float(x[31])), b);
+  for (int f = 0; f < 32; f += 2) a = fmaxf(fmaxf(__uint_as_float(x[f]), __uint_as_float(x[f + 1])), a);
+#pragma unroll
+  for (int f = 0; f < 32; f += 2) b = fmaxf(fmaxf(__uint_as_float(y[f]), __uint_as_float(y[f + 1])), b);
+  return fmaxf(a, b);
+}
+// Two fp32 operations at once.
+__device__ __forceinline__ uint64_t two(uint32_t lo, uint32_t hi) {
+  uint64_t x;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "r"(lo), "r"(hi));
+  return x;
+}
+__device__ __forceinline__ uint64_t two(float lo, float hi) { return two(__float_as_uint(lo), __float_as_uint(hi)); }
+__device__ __forceinline__ void apart(uint64_t x, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(x)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t x;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(x) : "l"(a), "l"(b), "l"(c));
+  return x;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t x;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(x) : "l"(a), "l"(b));
+  return x;
 }
 
 template <typename T, int D, int BITS>
 __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_constant__ AttendArgs a) {
   using P = Pair<T>;
-  using S = TcSmem<D>;
+  using S = TcSmem<D, BITS>;
   extern __shared__ char raw[];
   S& sm = *reinterpret_cast<S*>(raw + (1024u - (shared_address(raw) & 1023u)) % 1024u);
   pdl_trigger();
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  constexpr uint32_t kIssuer = (kTcSoftmax + 2 * kTcProducers) / 32;
   if (threadIdx.x == 0) {
-    for (int i = 0; i < S::kStages; ++i) {
-      mbar_init(shared_address(&sm.k_full[i]), kTcProducers);
-      mbar_init(shared_address(&sm.v_full[i]), kTcProducers);
-      mbar_init(shared_address(&sm.k_empty[i]), 1);
-      mbar_init(shared_address(&sm.v_empty[i]), 1);
-    }
+    for (int i = 0; i < kTcStages; ++i)
+      for (int v = 0; v < 2; ++v) {
+        mbar_init(shared_address(&sm.full[v][i]), kTcProducers);
+        mbar_init(shared_address(&sm.empty[v][i]), 1);
+      }
     for (int i = 0; i < kTcInfo; ++i) mbar_init(shared_address(&sm.info_full[i]), kTcProducers);
     for (int i = 0; i < 2; ++i) {
       mbar_init(shared_address(&sm.q_full[i]), 128);
-      mbar_init(shared_address(&sm.s_full[i]), 1);
-      mbar_init(shared_address(&sm.p_full[i]), 128);
-      mbar_init(shared_address(&sm.o_full[i]), 1);
+      for (int j = 0; j < 2; ++j) {
+        mbar_init(shared_address(&sm.o_full[i][j]), 1);
+        mbar_init(shared_address(&sm.s_full[i][j]), 1);
+        mbar_init(shared_address(&sm.p_full[i][j]), 128);
+      }
     }
     mbar_init(shared_address(&sm.drained), 1);
     sm.stop = 0;
@@ -253,7 +287,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
   }
   pdl_wait();
   // only now: a kernel before this one may still hold tensor memory, or wait for it
-  if (warp == kTcThreads / 32 - 1) {
+  if (warp == kIssuer) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(shared_address(&sm.tmem)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     tc_fence_before();
@@ -261,6 +295,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
   const uint64_t range = sm.plan.set_up(a, kTcRows);  // ends with a barrier
   tc_fence_after();
   const uint32_t tmem = sm.tmem;
+  const auto o_at = [&](uint32_t t) { return tmem + t * D; };
+  const auto s_at = [&](uint32_t t, uint32_t i) { return tmem + 2 * D + (2 * t + i % 2) * kTile; };
   Walk<kTcThreads> walk(a, sm.plan, kTcRows, range);
   const BatchArg& b = a.batch;
   Item it;
@@ -269,27 +305,28 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
 
   if (warp < kTcSoftmax / 32) {
     // ---------------------------------------------------------------- softmax: thread r of tile t has row r of it
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kTcRegsSoftmax));
     const uint32_t t = warp / 4, r = threadIdx.x % 128;
     const uint32_t lanes = (warp % 4) * 32u << 16;
-    const uint32_t s_col = tmem + lanes + t * 128, o_col = tmem + lanes + 256 + t * 128;
+    const uint32_t o_col = o_at(t) + lanes;
     const float by = a.scale * 1.4426950408889634f;
-    uint32_t s_n = 0, o_n = 0, info_n = 0;  // phases
+    uint32_t n = 0, s_n = 0;  // tiles told; tiles of this half
     while (walk.next(it)) {  // to the end even when a wait ran out: the barriers below count on all
       const uint32_t row0 = it.rb * kTcRows + t * 128, all = it.span.count * a.group;
-      const uint32_t tiles = (it.hi - it.lo + 1) / 2;
+      const uint32_t tiles = it.hi - it.lo;
       const bool active = row0 < all, real = row0 + r < all;
       const uint32_t token = real ? (row0 + r) / a.group : 0, head = it.head * a.group + (real ? (row0 + r) % a.group : 0);
       int32_t seen = 0;
       if (real) {
-        const int64_t n = a.causal ? static_cast<int64_t>(it.span.length) - it.span.count + token + 1 : it.span.length;
-        seen = n > 0 ? static_cast<int32_t>(n) : 0;
+        const int64_t x = a.causal ? static_cast<int64_t>(it.span.length) - it.span.count + token + 1 : it.span.length;
+        seen = x > 0 ? static_cast<int32_t>(x) : 0;
       }
       float m = -INFINITY, l = 0.f;
       if (active && tiles) {
         {  // the row of Q into shared memory; codes' products come in the order in which they are unpacked
           const T* q = reinterpret_cast<const T*>(a.q.in) + static_cast<int64_t>(it.span.first + token) * a.q.in_token +
                        static_cast<int64_t>(head) * a.q.in_head;
-#pragma unroll
+#pragma unroll 4
           for (int e = 0; e < D / 8; ++e) {
             uint4 x = make_uint4(0, 0, 0, 0);
             if (real) {
@@ -305,106 +342,97 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
             if (BITS == 4)
               x = make_uint4(__byte_perm(x.x, x.z, 0x5410), __byte_perm(x.x, x.z, 0x7632), __byte_perm(x.y, x.w, 0x5410),
                              __byte_perm(x.y, x.w, 0x7632));
-            *reinterpret_cast<uint4*>(sm.q[t] + (e / 8) * S::kBlock + r * 128 + ((e % 8) ^ (r & 7)) * 16) = x;
+            *reinterpret_cast<uint4*>(sm.q[t] + (e / 8) * S::kBlockQ + r * 128 + ((e % 8) ^ (r & 7)) * 16) = x;
           }
           fence_async_shared();
           mbar_arrive(shared_address(&sm.q_full[t]));
         }
-        for (uint32_t j = 0; ok && j < tiles; ++j) {
-          const TcInfo& info = sm.info[info_n % kTcInfo];
-          ok = tc_wait(&sm.info_full[info_n % kTcInfo], info_n / kTcInfo, stop) && tc_wait(&sm.s_full[t], s_n++, stop);
-          ++info_n;
+#pragma unroll 1
+        for (uint32_t j = 0; j < tiles; ++j, ++n, ++s_n) {
+          const TcInfo& info = sm.info[n % kTcInfo];
+          ok = ok && tc_wait(&sm.info_full[n % kTcInfo], n / kTcInfo, stop) && tc_wait(&sm.s_full[t][s_n % 2], s_n / 2, stop);
           ok = __all_sync(0xffffffffu, ok);
-          if (!ok) break;
+          if (!ok) {
+            n += tiles - j;
+            break;
+          }
           tc_fence_after();
-          const bool plain = info.plain != 0;
-          // hides those of 32 tokens that this row does not see
-          const auto hide = [&](uint32_t e, uint32_t* y) {
-            const int32_t n = seen - info.pos[e / 2] - static_cast<int32_t>(e % 2) * 32;  // the row sees the first n
-            const uint32_t see = info.bits[e] & (n >= 32 ? ~0u : n <= 0 ? 0u : (1u << n) - 1);
-            if (__all_sync(0xffffffffu, see == ~0u)) return;
-#pragma unroll
-            for (int f = 0; f < 32; ++f)
-              if (!(see & (1u << f))) y[f] = 0xff800000u;
-          };
-          // the maximum
-          float top = -INFINITY;
+          const uint32_t s_col = s_at(t, s_n) + lanes;
           uint32_t x[32], y[32];
           tc_ld32(s_col, x);
-#pragma unroll 1
-          for (uint32_t e = 0; e < 4; e += 2) {
-            tc_wait_ld(x);
-            tc_ld32(s_col + 32 * (e + 1), y);
-            if (!plain) hide(e, x);
-            top = most_of(x, top);
-            tc_wait_ld(y);
-            if (e == 0) tc_ld32(s_col + 64, x);
-            if (!plain) hide(e + 1, y);
-            top = most_of(y, top);
+          tc_ld32(s_col + 32, y);
+          tc_wait_ld(x);
+          tc_wait_ld(y);
+          if (!info.plain) {
+            // hides those of 32 tokens that this row does not see
+            const int32_t k = seen - info.pos;  // the row sees the first k
+            const uint32_t see0 = info.bits[0] & (k >= 32 ? ~0u : k <= 0 ? 0u : (1u << k) - 1);
+            const uint32_t see1 = info.bits[1] & (k >= 64 ? ~0u : k <= 32 ? 0u : (1u << (k - 32)) - 1);
+            if (!__all_sync(0xffffffffu, (see0 & see1) == ~0u)) {
+#pragma unroll
+              for (int f = 0; f < 32; ++f) {
+                if (!(see0 & (1u << f))) x[f] = 0xff800000u;
+                if (!(see1 & (1u << f))) y[f] = 0xff800000u;
+              }
+            }
           }
-          top *= by;
+          const float top = most_of(x, y, -INFINITY) * by;
           const bool raise = top > m + kTcRaise || (m == -INFINITY && top > -INFINITY);
           if (__any_sync(0xffffffffu, raise)) {
             const float to = raise ? top : m, k = m == -INFINITY ? 0.f : exp2_fast(m - to);
             if (j > 0) {  // O as it is after the tokens before
-              ok = tc_wait(&sm.o_full[t], o_n, stop);
+              ok = tc_wait(&sm.o_full[t][(s_n - 1) % 2], (s_n - 1) / 2, stop);
               ok = __all_sync(0xffffffffu, ok);
-              if (!ok) break;
               tc_fence_after();
+              uint32_t z[16];
 #pragma unroll 1
-              for (int e = 0; e < D / 32; ++e) {
-                tc_ld32(o_col + 32 * e, y);
-                tc_wait_ld(y);
+              for (int e = 0; e < D / 16; ++e) {
+                tc_ld16(o_col + 16 * e, z);
 #pragma unroll
-                for (int f = 0; f < 32; ++f) y[f] = __float_as_uint(__uint_as_float(y[f]) * k);
-                tc_st32(o_col + 32 * e, y);
+                for (int f = 0; f < 16; ++f) z[f] = __float_as_uint(__uint_as_float(z[f]) * k);
+                tc_st16(o_col + 16 * e, z);
               }
               tc_wait_st();
             }
             l *= k;
             m = to;
           }
-          if (j > 0) ++o_n;  // the phase of the tokens before, waited for or not
-          // the exponentials. S's columns up to 32 e + 31 are read when P's from 16 e are written
           const float from = m == -INFINITY ? 0.f : -m;
-          const auto exponentials = [&](uint32_t e, const uint32_t* z) {
+          const uint64_t by2 = two(by, by), from2 = two(from, from);
+          uint64_t l2 = two(l, 0.f), l3 = two(0.f, 0.f);
+          const auto exponentials = [&](const uint32_t* z, uint32_t col) {
             uint32_t w[16];
-            float l2 = 0.f;
 #pragma unroll
-            for (int f = 0; f < 16; ++f) {
-              const float p0 = exp2_fast(fmaf(__uint_as_float(z[2 * f]), by, from));
-              const float p1 = exp2_fast(fmaf(__uint_as_float(z[2 * f + 1]), by, from));
-              l += p0;
-              l2 += p1;
+            for (int f = 0; f < 16; f += 2) {
+              float p0, p1, p2, p3;
+              apart(fma2(two(z[2 * f], z[2 * f + 1]), by2, from2), p0, p1);
+              apart(fma2(two(z[2 * f + 2], z[2 * f + 3]), by2, from2), p2, p3);
+              p0 = exp2_fast(p0);
+              p1 = exp2_fast(p1);
+              p2 = exp2_fast(p2);
+              p3 = exp2_fast(p3);
+              l2 = add2(l2, two(p0, p1));
+              l3 = add2(l3, two(p2, p3));
               w[f] = P::pack(p0, p1);
+              w[f + 1] = P::pack(p2, p3);
             }
-            l += l2;
-            tc_st16(s_col + 16 * e, w);
+            tc_st16(col, w);
           };
-          tc_ld32(s_col, x);
-#pragma unroll 1
-          for (uint32_t e = 0; e < 4; e += 2) {
-            tc_wait_ld(x);
-            tc_ld32(s_col + 32 * (e + 1), y);
-            if (!plain) hide(e, x);
-            exponentials(e, x);
-            tc_wait_ld(y);
-            if (e == 0) tc_ld32(s_col + 64, x);
-            if (!plain) hide(e + 1, y);
-            exponentials(e + 1, y);
-          }
+          exponentials(x, s_col);
+          exponentials(y, s_col + 16);
+          float l0, l1;
+          apart(add2(l2, l3), l0, l1);
+          l = l0 + l1;
           tc_wait_st();
           tc_fence_before();
-          mbar_arrive(shared_address(&sm.p_full[t]));
+          mbar_arrive(shared_address(&sm.p_full[t][s_n % 2]));
         }
-        if (ok) {
-          ok = tc_wait(&sm.o_full[t], o_n++, stop);
-          ok = __all_sync(0xffffffffu, ok);
-          tc_fence_after();
-        }
+        if (ok) ok = tc_wait(&sm.o_full[t][(s_n - 1) % 2], (s_n - 1) / 2, stop);
+        ok = __all_sync(0xffffffffu, ok);
+        tc_fence_after();
       }
       // info of tiles that this half does not use
-      if (!active) info_n += tiles;
+      if (!active) n += tiles;
       const bool alone = it.first_cta == it.last_cta;
       const uint32_t lr = t * 128 + r;  // row of the item's 256
       const uint64_t part = (2ull * blockIdx.x + (blockIdx.x == it.first_cta ? 1 : 0)) * kTcRows;
@@ -510,12 +538,16 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
         }
       }
     }
-  } else if (warp < (kTcSoftmax + kTcProducers) / 32) {
-    // ---------------------------------------------------------------- producers: a thread to a token
-    const uint32_t p = threadIdx.x - kTcSoftmax;
+  } else if (warp < kIssuer) {
+    // ---------------------------------------------------------------- producers of keys (v = 0) and of values (v = 1)
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kTcRegsProducer));
+    const uint32_t v = warp / 4 - kTcSoftmax / 128, p = threadIdx.x % kTcProducers;
+    const uint32_t tok = p % kTile, half = p / kTile;  // two threads to a token
+    const char* const pages = v ? a.v : a.k;
+    const uint16_t* const words = v ? a.v_words : a.k_words;
     uint32_t n = 0;  // tiles so far
     while (walk.next(it)) {  // to the end, as above
-      const uint32_t units = it.hi - it.lo, tiles = (units + 1) / 2;
+      const uint32_t tiles = it.hi - it.lo;
       const int32_t* table = b.table + static_cast<uint64_t>(it.seq) * b.table_stride;
       // the fewest tokens that a row of the item sees
       int32_t all_see = it.span.length;
@@ -524,17 +556,15 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
         all_see = x > 0 ? static_cast<int32_t>(x) : 0;
       }
       struct Token {
-        uint32_t pos;   // of the first of its 64
-        bool some;      // there is such a 64
-        uint64_t row;   // in the pages; ~0 where there is nothing to see
+        uint32_t pos;  // of the tile's first
+        uint64_t row;  // in the pages; ~0 where there is nothing to see
       };
       const auto look = [&](uint32_t j) {
-        Token x{0, false, ~0ull};
-        const uint32_t unit = it.lo + 2 * j + p / 64;
-        if (unit >= it.hi) return x;
-        x.some = true;
+        Token x{0, ~0ull};
+        if (j >= tiles) return x;
+        const uint32_t unit = it.lo + j;
         x.pos = (a.mask ? a.tiles[static_cast<uint64_t>(it.seq) * a.tile_stride + unit] : unit) * kTile;
-        const uint32_t pos = x.pos + p % 64;
+        const uint32_t pos = x.pos + tok;
         if (pos >= it.span.length) return x;
         if (a.mask && (pos >= a.mask_stride || !a.mask[it.seq * a.mask_stride + pos])) return x;
         const uint32_t page = static_cast<uint32_t>(table[pos >> b.page_shift]);
@@ -545,182 +575,188 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
         x.row = page_row(b, (static_cast<int64_t>(page) << b.page_shift) | (pos & ((1u << b.page_shift) - 1)), it.head);
         return x;
       };
-      const auto tell = [&](const Token& x) {  // the tile's info, and where its tokens' rows are
-        TcInfo& info = sm.info[n % kTcInfo];
-        const uint32_t bits = __ballot_sync(0xffffffffu, x.row != ~0ull);
-        if (lane == 0) info.bits[p / 32] = bits;
-        if (p % 64 == 0) info.pos[p / 64] = static_cast<int32_t>(x.pos);
-        sm.row_of[n % S::kStages][p] = x.row;
-        const bool see = x.row != ~0ull && static_cast<int32_t>(x.pos + p % 64) < all_see;
-        uint32_t plain;
+      const auto tell = [&](const Token& x, uint32_t i) {  // what the softmax has to know of tile i
+        TcInfo& info = sm.info[i % kTcInfo];
+        const bool there = x.row != ~0ull;
+        const uint32_t bits = __ballot_sync(0xffffffffu, there);
+        const uint32_t plain = __all_sync(0xffffffffu, there && static_cast<int32_t>(x.pos + tok) < all_see);
+        if (lane == 0 && half == 0) info.bits[tok / 32] = bits;
+        if (p == 0) info.pos = static_cast<int32_t>(x.pos);
+        uint32_t every;
         asm volatile(
             "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\t"
             "barrier.cta.red.and.pred q, 2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-            : "=r"(plain)
-            : "r"(static_cast<uint32_t>(see))
+            : "=r"(every)
+            : "r"(plain)
             : "memory");
-        if (p == 0) info.plain = plain;
-        mbar_arrive(shared_address(&sm.info_full[n % kTcInfo]));
+        if (p == 0) info.plain = every;
+        mbar_arrive(shared_address(&sm.info_full[i % kTcInfo]));
       };
       if (BITS == 4) {
-        // Keys and values in turn, a step each, through one piece of code (three roles' code is more than the
-        // instruction cache likes); codes are fetched three steps ahead, each thread's to places of its own.
-        const auto fetch = [&](uint32_t step, const Token& y) {
+        // Codes are fetched three tiles ahead, each thread's to places of its own.
+        constexpr uint32_t kPart = D / 64;  // 16-byte pieces of a thread: a quarter of D codes is D / 4 bytes
+        const auto fetch = [&](uint32_t i, const Token& y) {
           if (y.row != ~0ull) {
-            const char* from = (step % 2 ? a.v : a.k) + y.row * (D / 2);
-            const uint32_t to = shared_address(sm.raw[step % S::kRaw]) + p * 16;
+            const char* from = pages + y.row * (D / 2) + half * (D / 4);
+            const uint32_t to = shared_address(sm.raw[v][i % kTcRaw]) + p * 16;
 #pragma unroll
-            for (int e = 0; e < D / 32; ++e) cp_async16(to + e * 2048, from + e * 16, true);
+            for (int e = 0; e < static_cast<int>(kPart); ++e) cp_async16(to + e * 2048, from + e * 16, true);
             // the word, or two, of the token; with one, of it and its neighbour (an even token's row is even)
-            const uint16_t* words = (step % 2 ? a.v_words : a.k_words) + (D == 128 ? 2 * y.row : y.row & ~1ull);
-            cp_async4(shared_address(&sm.raw_word[step % S::kRaw][p]), words);
-          } else {
-            sm.raw_word[step % S::kRaw][p] = 0;  // the scale of nothing is zero
+            if (half == 0) cp_async4(shared_address(&sm.raw_word[v][i % kTcRaw][tok]), words + (D == 128 ? 2 * y.row : y.row & ~1ull));
+          } else if (half == 0) {
+            sm.raw_word[v][i % kTcRaw][tok] = 0;  // the scale of nothing is zero
           }
           cp_async_commit();
         };
-        Token x0 = look(0), x1 = look(1), x2 = look(2);
-        static_assert(S::kRaw == 3, "three steps ahead");
-        fetch(0, x0);
-        fetch(1, x0);
-        fetch(2, x1);
+        Token x[4] = {look(0), look(1), look(2), look(3)};
+        fetch(n, x[0]);
+        fetch(n + 1, x[1]);
+        fetch(n + 2, x[2]);
 #pragma unroll 1
-        for (uint32_t step = 0; step < 2 * tiles; ++step) {
-          const uint32_t st = n % S::kStages, round = n / S::kStages, v = step % 2;
-          if (!v) tell(x0);
-          if (round > 0) ok = ok && tc_wait(v ? &sm.v_empty[st] : &sm.k_empty[st], round - 1, stop);
-          cp_async_wait<S::kRaw - 1>();
+        for (uint32_t j = 0; j < tiles; ++j, ++n) {
+          const uint32_t st = n % kTcStages, round = n / kTcStages;
+          if (v == 0) tell(x[0], n);
+          const Token next = look(j + 4);
+          cp_async_wait<kTcRaw - 1>();
+          // the word was another thread's to fetch
+          if (v == 0) bar_sync<2, kTcProducers>();
+          else bar_sync<3, kTcProducers>();
+          if (round > 0) ok = ok && tc_wait(&sm.empty[v][st], round - 1, stop);
           if (ok) {
-            char* to = v ? sm.v[st] : sm.k[st];
-            const char* from = sm.raw[step % S::kRaw] + p * 16;
-            const uint32_t w = sm.raw_word[step % S::kRaw][p];
+            const char* from = sm.raw[v][n % kTcRaw] + p * 16;
+            const uint32_t w = sm.raw_word[v][n % kTcRaw][tok];
+            const Unpack<T> u(D == 64 ? (tok % 2 ? w >> 16 : w & 0xFFFFu) : (half ? w >> 16 : w & 0xFFFFu));
+            char* to = sm.kv[v][st] + (D == 128 ? half * S::kBlock : 0) + tok * 128;
 #pragma unroll
-            for (int gr = 0; gr < D / 64; ++gr) {
-              const Unpack<T> u((D == 64 && p % 2) || gr == 1 ? w >> 16 : w & 0xFFFFu);
+            for (int e = 0; e < static_cast<int>(kPart); ++e) {
+              const uint4 y = *reinterpret_cast<const uint4*>(from + e * 2048);
+              const uint32_t ws[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                const uint4 y = *reinterpret_cast<const uint4*>(from + (2 * gr + e) * 2048);
-                const uint32_t ws[4] = {y.x, y.y, y.z, y.w};
-#pragma unroll
-                for (int f = 0; f < 4; ++f)
-                  *reinterpret_cast<uint4*>(to + gr * S::kBlock + p * 128 + ((4 * e + f) ^ (p & 7)) * 16) = u(ws[f]);
-              }
+              for (int f = 0; f < 4; ++f)
+                *reinterpret_cast<uint4*>(to + (((D == 64 ? 4 * half : 0) + 4 * e + f) ^ (tok & 7)) * 16) = u(ws[f]);
             }
             fence_async_shared();
-            mbar_arrive(shared_address(v ? &sm.v_full[st] : &sm.k_full[st]));
+            mbar_arrive(shared_address(&sm.full[v][st]));
           }
-          fetch(step + 3, v ? x2 : x1);  // step + 3: values of the next tile, or keys of the one after
-          if (v) {
-            x0 = x1;
-            x1 = x2;
-            x2 = look(step / 2 + 3);
-            ++n;
-          }
+          // every thread has its word before the next one comes to its place
+          if (v == 0) bar_sync<2, kTcProducers>();
+          else bar_sync<3, kTcProducers>();
+          fetch(n + 3, x[3]);
+          x[0] = x[1], x[1] = x[2], x[2] = x[3], x[3] = next;
         }
         cp_async_wait<0>();
+        if (v == 0) bar_sync<2, kTcProducers>();
+        else bar_sync<3, kTcProducers>();
       } else {
+        // Copies of three tiles are on their way at a time.
         constexpr uint32_t kUnits = D / 8;  // 16-byte units of a token
-        const auto copy = [&](char* to, const char* pages, uint32_t slot) {
+        constexpr uint32_t kAhead = kTcStages - 1;
+        Token x = look(0);
+#pragma unroll 1
+        for (uint32_t j = 0; j < tiles + kAhead - 1; ++j) {
+          const uint32_t i = n + j, st = i % kTcStages, round = i / kTcStages;
+          if (j < tiles) {
+            const Token next = look(j + 1);
+            if (half == 0) sm.row_of[v][st][tok] = x.row;
+            if (v == 0) tell(x, i);
+            else bar_sync<3, kTcProducers>();
+            if (round > 0) ok = ok && tc_wait(&sm.empty[v][st], round - 1, stop);
+            if (ok) {
+              const uint32_t to = shared_address(sm.kv[v][st]);
 #pragma unroll 4
-          for (uint32_t i = 0; i < kUnits; ++i) {
-            const uint32_t e = i * 128 + p, tok = e / kUnits, u = e % kUnits;
-            const uint64_t row = sm.row_of[slot][tok];
-            const bool live = row != ~0ull;
-            cp_async16(shared_address(to) + (u / 8) * S::kBlock + tok * 128 + ((u % 8) ^ (tok & 7)) * 16,
-                       pages + (live ? row * (D * 2) + u * 16 : 0), live);
+              for (uint32_t e = p; e < kTile * kUnits; e += kTcProducers) {
+                const uint32_t tk = e / kUnits, u = e % kUnits;
+                const uint64_t row = sm.row_of[v][st][tk];
+                const bool live = row != ~0ull;
+                cp_async16(to + (u / 8) * S::kBlock + tk * 128 + ((u % 8) ^ (tk & 7)) * 16, pages + (live ? row * (D * 2) + u * 16 : 0), live);
+              }
+            }
+            x = next;
           }
           cp_async_commit();
-        };
-        Token x = look(0);
-        for (uint32_t j = 0; j < tiles; ++j, ++n) {
-          const uint32_t st = n % S::kStages, round = n / S::kStages;
-          const Token next = look(j + 1);
-          tell(x);
-          if (round > 0) ok = ok && tc_wait(&sm.k_empty[st], round - 1, stop);
-          if (ok) copy(sm.k[st], a.k, st);
-          if (ok && j > 0) {  // the values of the tile before
-            cp_async_wait<1>();
-            fence_async_shared();
-            mbar_arrive(shared_address(&sm.v_full[(n - 1) % S::kStages]));
+          if (j + 1 >= kAhead) {  // the tile of two steps before is there
+            cp_async_wait<kAhead - 1>();
+            if (ok) {
+              fence_async_shared();
+              mbar_arrive(shared_address(&sm.full[v][(i + 1 - kAhead) % kTcStages]));
+            }
           }
-          if (round > 0) ok = ok && tc_wait(&sm.v_empty[st], round - 1, stop);
-          if (ok) {
-            copy(sm.v[st], a.v, st);
-            cp_async_wait<1>();
-            fence_async_shared();
-            mbar_arrive(shared_address(&sm.k_full[st]));
-          }
-          x = next;
         }
-        cp_async_wait<0>();
-        if (ok && tiles) {
-          fence_async_shared();
-          mbar_arrive(shared_address(&sm.v_full[(n - 1) % S::kStages]));
-        }
+        n += tiles;
       }
     }
     cp_async_wait<0>();
-  } else if (lane == 0) {
-    // ---------------------------------------------------------------- products
-    constexpr uint32_t kQK = tc_idesc<T>(128, kTcKeys, false), kPV = tc_idesc<T>(128, D, true);
-    uint32_t n = 0, q_n[2] = {0, 0}, p_n[2] = {0, 0}, o_n[2] = {0, 0};
-    while (ok && walk.next(it)) {
-      const uint32_t tiles = (it.hi - it.lo + 1) / 2;
-      if (tiles == 0) continue;
-      const uint32_t halves = it.span.count * a.group - it.rb * kTcRows > 128 ? 2 : 1;
-      const auto qk = [&](uint32_t t, uint32_t j) {
-        const uint32_t st = (n + j) % S::kStages;
-        if (j == 0) ok = ok && tc_wait(&sm.q_full[t], q_n[t]++, stop);
-        // S's place holds the P of the tokens before
-        if (j > 0) ok = ok && tc_wait(&sm.o_full[t], o_n[t]++, stop);
-        ok = ok && tc_wait(&sm.k_full[st], (n + j) / S::kStages, stop);
-        if (!ok) return;
-        tc_fence_after();
-        const uint32_t q = shared_address(sm.q[t]), k = shared_address(sm.k[st]);
+  } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kTcRegsIssuer));
+    if (warp == kIssuer) {
+      // -------------------------------------------------------------- products
+      constexpr uint32_t kQK = tc_idesc<T>(128, kTile, false), kPV = tc_idesc<T>(128, D, true);
+      const uint32_t leader = tc_leader();
+      uint32_t n = 0, q_n[2] = {0, 0}, s_n[2] = {0, 0};  // tiles so far; items and tiles of each half
+      while (ok && walk.next(it)) {
+        const uint32_t tiles = it.hi - it.lo;
+        if (tiles == 0) continue;
+        const uint32_t halves = it.span.count * a.group - it.rb * kTcRows > 128 ? 2 : 1;
+        const auto qk = [&](uint32_t t, uint32_t j) {
+          const uint32_t st = (n + j) % kTcStages;
+          if (j == 0) ok = ok && tc_wait(&sm.q_full[t], q_n[t]++, stop);
+          // this S holds the P of two tiles before
+          if (j > 1) ok = ok && tc_wait(&sm.o_full[t][(s_n[t] + j) % 2], (s_n[t] + j) / 2 - 1, stop);
+          ok = ok && tc_wait(&sm.full[0][st], (n + j) / kTcStages, stop);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) return;
+          tc_fence_after();
+          const uint32_t q = shared_address(sm.q[t]), k = shared_address(sm.kv[0][st]);
 #pragma unroll
-        for (int e = 0; e < D / 16; ++e)
-          tc_mma_ss(tmem + t * 128, tc_desc(q + (e / 4) * S::kBlock + (e % 4) * 32, 16), tc_desc(k + (e / 4) * S::kBlock + (e % 4) * 32, 16), kQK, e > 0);
-        tc_commit(&sm.s_full[t]);
-        if (t + 1 == halves) tc_commit(&sm.k_empty[st]);
-      };
-      const auto pv = [&](uint32_t t, uint32_t j) {
-        const uint32_t st = (n + j) % S::kStages;
-        ok = ok && tc_wait(&sm.p_full[t], p_n[t]++, stop) && tc_wait(&sm.v_full[st], (n + j) / S::kStages, stop);
-        if (!ok) return;
-        tc_fence_after();
-        const uint32_t v = shared_address(sm.v[st]);
+          for (int e = 0; e < D / 16; ++e)
+            tc_mma_ss(leader, s_at(t, s_n[t] + j), tc_desc(q + (e / 4) * S::kBlockQ + (e % 4) * 32, 16), tc_desc(k + (e / 4) * S::kBlock + (e % 4) * 32, 16),
+                      kQK, e > 0);
+          tc_commit(leader, &sm.s_full[t][(s_n[t] + j) % 2]);
+          if (t + 1 == halves) tc_commit(leader, &sm.empty[0][st]);
+        };
+        const auto pv = [&](uint32_t t, uint32_t j) {
+          const uint32_t st = (n + j) % kTcStages, i = s_n[t] + j;
+          ok = ok && tc_wait(&sm.p_full[t][i % 2], i / 2, stop) && tc_wait(&sm.full[1][st], (n + j) / kTcStages, stop);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) return;
+          tc_fence_after();
+          const uint32_t v = shared_address(sm.kv[1][st]);
 #pragma unroll
-        for (int e = 0; e < kTcKeys / 16; ++e)
-          tc_mma_ts(tmem + 256 + t * 128, tmem + t * 128 + e * 8, tc_desc(v + e * 2048, S::kBlock), kPV, j > 0 || e > 0);
-        tc_commit(&sm.o_full[t]);
-        if (t + 1 == halves) tc_commit(&sm.v_empty[st]);
-      };
-      for (uint32_t t = 0; t < halves; ++t) qk(t, 0);
-      for (uint32_t j = 0; ok && j < tiles; ++j)
-        for (uint32_t t = 0; ok && t < halves; ++t) {
-          pv(t, j);
-          if (j + 1 < tiles) qk(t, j + 1);
+          for (int e = 0; e < static_cast<int>(kTile) / 16; ++e)
+            tc_mma_ts(leader, o_at(t), s_at(t, i) + e * 8, tc_desc(v + e * 2048, S::kBlock), kPV, j > 0 || e > 0);
+          tc_commit(leader, &sm.o_full[t][i % 2]);
+          if (t + 1 == halves) tc_commit(leader, &sm.empty[1][st]);
+        };
+        for (uint32_t j = 0; j < 2 && j < tiles; ++j)
+          for (uint32_t t = 0; t < halves; ++t) qk(t, j);
+#pragma unroll 1
+        for (uint32_t j = 0; ok && j < tiles; ++j) {
+          for (uint32_t t = 0; t < halves; ++t) pv(t, j);
+          if (j + 2 < tiles)
+            for (uint32_t t = 0; t < halves; ++t) qk(t, j + 2);
         }
-      for (uint32_t t = 0; t < halves; ++t) ++o_n[t];  // the last phase, which the softmax waits for
-      n += tiles;
+        for (uint32_t t = 0; t < halves; ++t) s_n[t] += tiles;
+        n += tiles;
+      }
+      // what was issued, and its arrivals, finish before the tensor memory goes and the CTA ends
+      tc_commit(leader, &sm.drained);
+      if (!tc_wait(&sm.drained, 0, stop)) atomicOr(b.err, kKvErrWait);
+      __syncwarp();
     }
-    // what was issued, and its arrivals, finish before the tensor memory goes and the CTA ends
-    tc_commit(&sm.drained);
-    if (!mbar_wait_bounded(shared_address(&sm.drained), 0, kTcTimeout)) atomicOr(b.err, kKvErrWait);
   }
   if (!ok) atomicOr(b.err, kKvErrWait);
   tc_fence_before();
   __syncthreads();
-  if (warp == kTcThreads / 32 - 1) {
+  if (warp == kIssuer) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
   }
 }
 
 // One CTA to an SM, whose tensor memory it takes whole: more than half of its shared memory.
-template <int D>
+template <int D, int BITS>
 constexpr size_t tc_smem() {
-  return sizeof(TcSmem<D>) + 1024 > 120 * 1024 ? sizeof(TcSmem<D>) + 1024 : 120 * 1024;
+  return sizeof(TcSmem<D, BITS>) + 1024 > 120 * 1024 ? sizeof(TcSmem<D, BITS>) + 1024 : 120 * 1024;
 }
 
 }  // namespace

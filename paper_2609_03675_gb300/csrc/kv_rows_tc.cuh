@@ -8,7 +8,7 @@
 //   producers  four warps for keys, four for values: the next tokens into shared
 //              memory (128-byte swizzle), copied (16 bits) or unpacked to
 //              (n - z) s, which the 16-bit types hold exactly (4 bits)
-//   MMA        one thread: S = Q K^T into tensor memory (128 x 64 fp32 a tile),
+//   MMA        a warp for each tile: S = Q K^T into tensor memory (128 x 64 fp32 a tile),
 //              and O += P V with P read from tensor memory
 // The running maximum that exponentials refer to is raised only when the true
 // one passes it by 2^8 (then O is brought down in tensor memory), which seldom
@@ -42,8 +42,8 @@ constexpr int kTcInfo = 8;         // more than the stages: a tile is told befor
 constexpr int kTcRaw = 3;          // codes as they lie in the pages
 constexpr float kTcRaise = 8.f;
 constexpr uint64_t kTcTimeout = 1000000000ull;
-// Registers: all threads start with 96; 256 x 144 + 256 x 72 + 128 x 40 is less than 640 x 96.
-constexpr int kTcRegsSoftmax = 144, kTcRegsProducer = 72, kTcRegsIssuer = 40;
+// Registers: all threads start with 96; 256 x 136 + 256 x 72 + 128 x 64 is 640 x 96.
+constexpr int kTcRegsSoftmax = 136, kTcRegsProducer = 72, kTcRegsIssuer = 64;
 
 struct TcInfo {
   uint32_t bits[2];  // tokens that some row may see
@@ -270,7 +270,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
     for (int i = 0; i < kTcStages; ++i)
       for (int v = 0; v < 2; ++v) {
         mbar_init(shared_address(&sm.full[v][i]), kTcProducers);
-        mbar_init(shared_address(&sm.empty[v][i]), 1);
+        mbar_init(shared_address(&sm.empty[v][i]), 2);  // both issuers
       }
     for (int i = 0; i < kTcInfo; ++i) mbar_init(shared_address(&sm.info_full[i]), kTcProducers);
     for (int i = 0; i < 2; ++i) {
@@ -281,7 +281,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
         mbar_init(shared_address(&sm.p_full[i][j]), 128);
       }
     }
-    mbar_init(shared_address(&sm.drained), 1);
+    mbar_init(shared_address(&sm.drained), 2);
     sm.stop = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -688,54 +688,52 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
     cp_async_wait<0>();
   } else {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kTcRegsIssuer));
-    if (warp == kIssuer) {
-      // -------------------------------------------------------------- products
+    if (warp < kIssuer + 2) {
+      // -------------------------------------------------------------- products: a warp for each tile
       constexpr uint32_t kQK = tc_idesc<T>(128, kTile, false), kPV = tc_idesc<T>(128, D, true);
-      const uint32_t leader = tc_leader();
-      uint32_t n = 0, q_n[2] = {0, 0}, s_n[2] = {0, 0};  // tiles so far; items and tiles of each half
+      const uint32_t leader = tc_leader(), t = warp - kIssuer;
+      uint32_t n = 0, q_n = 0, s_n = 0;  // tiles so far; items and tiles of this half
       while (ok && walk.next(it)) {
-        const uint32_t tiles = it.hi - it.lo;
+        const uint32_t tiles = it.hi - it.lo, halves = it.span.count * a.group - it.rb * kTcRows > 128 ? 2 : 1;
+        if (t >= halves) {  // the other warp stands in for this one
+          n += tiles;
+          continue;
+        }
         if (tiles == 0) continue;
-        const uint32_t halves = it.span.count * a.group - it.rb * kTcRows > 128 ? 2 : 1;
-        const auto qk = [&](uint32_t t, uint32_t j) {
-          const uint32_t st = (n + j) % kTcStages;
-          if (j == 0) ok = ok && tc_wait(&sm.q_full[t], q_n[t]++, stop);
+        const auto qk = [&](uint32_t j) {
+          const uint32_t st = (n + j) % kTcStages, i = s_n + j;
+          if (j == 0) ok = ok && tc_wait(&sm.q_full[t], q_n++, stop);
           // this S holds the P of two tiles before
-          if (j > 1) ok = ok && tc_wait(&sm.o_full[t][(s_n[t] + j) % 2], (s_n[t] + j) / 2 - 1, stop);
+          if (j > 1) ok = ok && tc_wait(&sm.o_full[t][i % 2], i / 2 - 1, stop);
           ok = ok && tc_wait(&sm.full[0][st], (n + j) / kTcStages, stop);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) return;
           tc_fence_after();
-          const uint32_t q = shared_address(sm.q[t]), k = shared_address(sm.kv[0][st]);
+          const uint32_t q = tc_desc(shared_address(sm.q[t]), 16), k = tc_desc(shared_address(sm.kv[0][st]), 16), d = s_at(t, i);
 #pragma unroll
           for (int e = 0; e < D / 16; ++e)
-            tc_mma_ss(leader, s_at(t, s_n[t] + j), tc_desc(q + (e / 4) * S::kBlockQ + (e % 4) * 32, 16), tc_desc(k + (e / 4) * S::kBlock + (e % 4) * 32, 16),
-                      kQK, e > 0);
-          tc_commit(leader, &sm.s_full[t][(s_n[t] + j) % 2]);
-          if (t + 1 == halves) tc_commit(leader, &sm.empty[0][st]);
+            tc_mma_ss(leader, d, q + (e / 4) * (S::kBlockQ / 16) + (e % 4) * 2, k + (e / 4) * (S::kBlock / 16) + (e % 4) * 2, kQK, e > 0);
+          tc_commit(leader, &sm.s_full[t][i % 2]);
+          tc_commit(leader, &sm.empty[0][st]);
+          if (halves == 1) tc_commit(leader, &sm.empty[0][st]);
         };
-        const auto pv = [&](uint32_t t, uint32_t j) {
-          const uint32_t st = (n + j) % kTcStages, i = s_n[t] + j;
-          ok = ok && tc_wait(&sm.p_full[t][i % 2], i / 2, stop) && tc_wait(&sm.full[1][st], (n + j) / kTcStages, stop);
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) return;
-          tc_fence_after();
-          const uint32_t v = shared_address(sm.kv[1][st]);
-#pragma unroll
-          for (int e = 0; e < static_cast<int>(kTile) / 16; ++e)
-            tc_mma_ts(leader, o_at(t), s_at(t, i) + e * 8, tc_desc(v + e * 2048, S::kBlock), kPV, j > 0 || e > 0);
-          tc_commit(leader, &sm.o_full[t][i % 2]);
-          if (t + 1 == halves) tc_commit(leader, &sm.empty[1][st]);
-        };
-        for (uint32_t j = 0; j < 2 && j < tiles; ++j)
-          for (uint32_t t = 0; t < halves; ++t) qk(t, j);
+        for (uint32_t j = 0; j < 2 && j < tiles; ++j) qk(j);
 #pragma unroll 1
         for (uint32_t j = 0; ok && j < tiles; ++j) {
-          for (uint32_t t = 0; t < halves; ++t) pv(t, j);
-          if (j + 2 < tiles)
-            for (uint32_t t = 0; t < halves; ++t) qk(t, j + 2);
+          const uint32_t st = (n + j) % kTcStages, i = s_n + j;
+          ok = tc_wait(&sm.p_full[t][i % 2], i / 2, stop) && tc_wait(&sm.full[1][st], (n + j) / kTcStages, stop);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t v = tc_desc(shared_address(sm.kv[1][st]), S::kBlock), p = s_at(t, i);
+#pragma unroll
+          for (int e = 0; e < static_cast<int>(kTile) / 16; ++e) tc_mma_ts(leader, o_at(t), p + e * 8, v + e * (2048 / 16), kPV, j > 0 || e > 0);
+          tc_commit(leader, &sm.o_full[t][i % 2]);
+          tc_commit(leader, &sm.empty[1][st]);
+          if (halves == 1) tc_commit(leader, &sm.empty[1][st]);
+          if (j + 2 < tiles) qk(j + 2);
         }
-        for (uint32_t t = 0; t < halves; ++t) s_n[t] += tiles;
+        s_n += tiles;
         n += tiles;
       }
       // what was issued, and its arrivals, finish before the tensor memory goes and the CTA ends

@@ -48,19 +48,21 @@ constexpr int kTcRegsSoftmax = 136, kTcRegsProducer = 72, kTcRegsIssuer = 64;
 struct TcInfo {
   uint32_t bits[2];  // tokens that some row may see
   int32_t pos;       // the first token
-  uint32_t plain;    // every token is seen by every row
+  uint32_t plain[2]; // every token of the half is seen by every row
 };
 
 template <int D, int BITS>
 struct TcSmem {
   static constexpr int kBlockQ = 128 * 128;  // 128 rows of 64 values
   static constexpr int kBlock = kTile * 128;  // 64 rows of 64 values
-  char q[2][kBlockQ * (D / 64)];
+  union {
+    char q[2][kBlockQ * (D / 64)];
+    Plan<kTcThreads> plan;  // until every thread has its walk
+  };
   char kv[2][kTcStages][kBlock * (D / 64)];  // keys, values
   char raw[2][BITS == 4 ? kTcRaw : 1][BITS == 4 ? kTile * (D / 2) : 16];
-  uint32_t raw_word[2][kTcRaw][kTile];
+  uint32_t raw_word[2][kTcRaw][kTcProducers];
   uint64_t row_of[2][BITS == 4 ? 1 : kTcStages][kTile];  // 16 bits: the tokens' rows in the pages, ~0 where there is nothing
-  Plan<kTcThreads> plan;
   TcInfo info[kTcInfo];
   float top[kTcRows], sum[kTcRows];
   uint64_t full[2][kTcStages], empty[2][kTcStages];  // keys, values
@@ -94,6 +96,12 @@ __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+// What the warp has done before comes before the barrier's phase: one arrival for all its threads (128 arrivals at one
+// address one after the other would cost more than the wait).
+__device__ __forceinline__ void warp_arrive(uint64_t* bar) {
+  __syncwarp();
+  if (threadIdx.x % 32 == 0) mbar_arrive(shared_address(bar));
 }
 template <int ID, int THREADS>
 __device__ __forceinline__ void bar_sync() {
@@ -269,16 +277,16 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
   if (threadIdx.x == 0) {
     for (int i = 0; i < kTcStages; ++i)
       for (int v = 0; v < 2; ++v) {
-        mbar_init(shared_address(&sm.full[v][i]), kTcProducers);
+        mbar_init(shared_address(&sm.full[v][i]), kTcProducers / 32);
         mbar_init(shared_address(&sm.empty[v][i]), 2);  // both issuers
       }
-    for (int i = 0; i < kTcInfo; ++i) mbar_init(shared_address(&sm.info_full[i]), kTcProducers);
+    for (int i = 0; i < kTcInfo; ++i) mbar_init(shared_address(&sm.info_full[i]), 2);
     for (int i = 0; i < 2; ++i) {
-      mbar_init(shared_address(&sm.q_full[i]), 128);
+      mbar_init(shared_address(&sm.q_full[i]), 4);
       for (int j = 0; j < 2; ++j) {
         mbar_init(shared_address(&sm.o_full[i][j]), 1);
         mbar_init(shared_address(&sm.s_full[i][j]), 1);
-        mbar_init(shared_address(&sm.p_full[i][j]), 128);
+        mbar_init(shared_address(&sm.p_full[i][j]), 4);
       }
     }
     mbar_init(shared_address(&sm.drained), 2);
@@ -298,6 +306,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
   const auto o_at = [&](uint32_t t) { return tmem + t * D; };
   const auto s_at = [&](uint32_t t, uint32_t i) { return tmem + 2 * D + (2 * t + i % 2) * kTile; };
   Walk<kTcThreads> walk(a, sm.plan, kTcRows, range);
+  __syncthreads();
   const BatchArg& b = a.batch;
   Item it;
   uint32_t* stop = &sm.stop;
@@ -345,7 +354,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
             *reinterpret_cast<uint4*>(sm.q[t] + (e / 8) * S::kBlockQ + r * 128 + ((e % 8) ^ (r & 7)) * 16) = x;
           }
           fence_async_shared();
-          mbar_arrive(shared_address(&sm.q_full[t]));
+          warp_arrive(&sm.q_full[t]);
         }
 #pragma unroll 1
         for (uint32_t j = 0; j < tiles; ++j, ++n, ++s_n) {
@@ -363,7 +372,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
           tc_ld32(s_col + 32, y);
           tc_wait_ld(x);
           tc_wait_ld(y);
-          if (!info.plain) {
+          if (!(info.plain[0] & info.plain[1])) {
             // hides those of 32 tokens that this row does not see
             const int32_t k = seen - info.pos;  // the row sees the first k
             const uint32_t see0 = info.bits[0] & (k >= 32 ? ~0u : k <= 0 ? 0u : (1u << k) - 1);
@@ -425,7 +434,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
           l = l0 + l1;
           tc_wait_st();
           tc_fence_before();
-          mbar_arrive(shared_address(&sm.p_full[t][s_n % 2]));
+          warp_arrive(&sm.p_full[t][s_n % 2]);
         }
         if (ok) ok = tc_wait(&sm.o_full[t][(s_n - 1) % 2], (s_n - 1) / 2, stop);
         ok = __all_sync(0xffffffffu, ok);
@@ -576,21 +585,17 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
         return x;
       };
       const auto tell = [&](const Token& x, uint32_t i) {  // what the softmax has to know of tile i
+        if (v || half) return;
         TcInfo& info = sm.info[i % kTcInfo];
         const bool there = x.row != ~0ull;
         const uint32_t bits = __ballot_sync(0xffffffffu, there);
         const uint32_t plain = __all_sync(0xffffffffu, there && static_cast<int32_t>(x.pos + tok) < all_see);
-        if (lane == 0 && half == 0) info.bits[tok / 32] = bits;
-        if (p == 0) info.pos = static_cast<int32_t>(x.pos);
-        uint32_t every;
-        asm volatile(
-            "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\t"
-            "barrier.cta.red.and.pred q, 2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-            : "=r"(every)
-            : "r"(plain)
-            : "memory");
-        if (p == 0) info.plain = every;
-        mbar_arrive(shared_address(&sm.info_full[i % kTcInfo]));
+        if (lane == 0) {
+          info.bits[tok / 32] = bits;
+          info.plain[tok / 32] = plain;
+          if (tok == 0) info.pos = static_cast<int32_t>(x.pos);
+          mbar_arrive(shared_address(&sm.info_full[i % kTcInfo]));
+        }
       };
       if (BITS == 4) {
         // Codes are fetched three tiles ahead, each thread's to places of its own.
@@ -602,9 +607,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
 #pragma unroll
             for (int e = 0; e < static_cast<int>(kPart); ++e) cp_async16(to + e * 2048, from + e * 16, true);
             // the word, or two, of the token; with one, of it and its neighbour (an even token's row is even)
-            if (half == 0) cp_async4(shared_address(&sm.raw_word[v][i % kTcRaw][tok]), words + (D == 128 ? 2 * y.row : y.row & ~1ull));
-          } else if (half == 0) {
-            sm.raw_word[v][i % kTcRaw][tok] = 0;  // the scale of nothing is zero
+            cp_async4(shared_address(&sm.raw_word[v][i % kTcRaw][p]), words + (D == 128 ? 2 * y.row : y.row & ~1ull));
+          } else {
+            sm.raw_word[v][i % kTcRaw][p] = 0;  // the scale of nothing is zero
           }
           cp_async_commit();
         };
@@ -615,16 +620,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
 #pragma unroll 1
         for (uint32_t j = 0; j < tiles; ++j, ++n) {
           const uint32_t st = n % kTcStages, round = n / kTcStages;
-          if (v == 0) tell(x[0], n);
+          tell(x[0], n);
           const Token next = look(j + 4);
           cp_async_wait<kTcRaw - 1>();
-          // the word was another thread's to fetch
-          if (v == 0) bar_sync<2, kTcProducers>();
-          else bar_sync<3, kTcProducers>();
           if (round > 0) ok = ok && tc_wait(&sm.empty[v][st], round - 1, stop);
           if (ok) {
             const char* from = sm.raw[v][n % kTcRaw] + p * 16;
-            const uint32_t w = sm.raw_word[v][n % kTcRaw][tok];
+            const uint32_t w = sm.raw_word[v][n % kTcRaw][p];
             const Unpack<T> u(D == 64 ? (tok % 2 ? w >> 16 : w & 0xFFFFu) : (half ? w >> 16 : w & 0xFFFFu));
             char* to = sm.kv[v][st] + (D == 128 ? half * S::kBlock : 0) + tok * 128;
 #pragma unroll
@@ -636,17 +638,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
                 *reinterpret_cast<uint4*>(to + (((D == 64 ? 4 * half : 0) + 4 * e + f) ^ (tok & 7)) * 16) = u(ws[f]);
             }
             fence_async_shared();
-            mbar_arrive(shared_address(&sm.full[v][st]));
           }
-          // every thread has its word before the next one comes to its place
-          if (v == 0) bar_sync<2, kTcProducers>();
-          else bar_sync<3, kTcProducers>();
+          ok = __all_sync(0xffffffffu, ok);
+          if (ok) warp_arrive(&sm.full[v][st]);
           fetch(n + 3, x[3]);
           x[0] = x[1], x[1] = x[2], x[2] = x[3], x[3] = next;
         }
         cp_async_wait<0>();
-        if (v == 0) bar_sync<2, kTcProducers>();
-        else bar_sync<3, kTcProducers>();
       } else {
         // Copies of three tiles are on their way at a time.
         constexpr uint32_t kUnits = D / 8;  // 16-byte units of a token
@@ -658,7 +656,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
           if (j < tiles) {
             const Token next = look(j + 1);
             if (half == 0) sm.row_of[v][st][tok] = x.row;
-            if (v == 0) tell(x, i);
+            tell(x, i);
+            if (v == 0) bar_sync<2, kTcProducers>();
             else bar_sync<3, kTcProducers>();
             if (round > 0) ok = ok && tc_wait(&sm.empty[v][st], round - 1, stop);
             if (ok) {
@@ -676,10 +675,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
           cp_async_commit();
           if (j + 1 >= kAhead) {  // the tile of two steps before is there
             cp_async_wait<kAhead - 1>();
-            if (ok) {
-              fence_async_shared();
-              mbar_arrive(shared_address(&sm.full[v][(i + 1 - kAhead) % kTcStages]));
-            }
+            fence_async_shared();
+            ok = __all_sync(0xffffffffu, ok);
+            if (ok) warp_arrive(&sm.full[v][(i + 1 - kAhead) % kTcStages]);
           }
         }
         n += tiles;

@@ -53,8 +53,7 @@ __device__ __forceinline__ uint32_t block_tiles(const AttendArgs& a, const Span&
   return (end + kTile - 1) / kTile;
 }
 
-__device__ __forceinline__ uint64_t sequence_slots(const AttendArgs& a, uint32_t rows_per_block, uint32_t seq) {
-  const Span sp = sequence_span(a.batch, seq);
+__device__ __forceinline__ uint64_t sequence_slots(const AttendArgs& a, uint32_t rows_per_block, uint32_t seq, const Span& sp) {
   const uint32_t blocks = (sp.count * a.group + rows_per_block - 1) / rows_per_block;
   uint64_t n = 0;
   if (a.causal && !a.mask)
@@ -73,17 +72,23 @@ struct Item {
   uint32_t first_cta, last_cta;
 };
 
+constexpr uint32_t kSpans = 256;  // sequences that are looked up once and kept in shared memory
+
 // Walks the items of one CTA's range. THREADS threads share the sequences.
 template <int THREADS>
 struct Plan {
   uint64_t before[THREADS + 1];  // slots before the sequences of each thread
 
   // All threads; ends with a barrier. The slots of a range.
-  __device__ __forceinline__ uint64_t set_up(const AttendArgs& a, uint32_t rows_per_block) {
+  __device__ __forceinline__ uint64_t set_up(const AttendArgs& a, uint32_t rows_per_block, Span* spans) {
     const uint32_t per = (a.batch.n_seqs + THREADS - 1) / THREADS;
     const uint32_t t = threadIdx.x, lane = t % 32;
     uint64_t n = 0;
-    for (uint32_t s = t * per; s < min(a.batch.n_seqs, (t + 1) * per); ++s) n += sequence_slots(a, rows_per_block, s);
+    for (uint32_t s = t * per; s < min(a.batch.n_seqs, (t + 1) * per); ++s) {
+      const Span sp = sequence_span(a.batch, s);
+      if (s < kSpans) spans[s] = sp;
+      n += sequence_slots(a, rows_per_block, s, sp);
+    }
     uint64_t sum = n;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -109,13 +114,14 @@ struct Walk {
   const AttendArgs& a;
   const uint32_t rows_per_block;
   const uint64_t range;
+  const Span* spans;
   uint64_t at, end;    // what is left of the CTA's range
   uint64_t item_at;    // slot at which the next item begins
   uint32_t seq, rb, head, blocks;
   Span span;
 
-  __device__ __forceinline__ Walk(const AttendArgs& args, const Plan<THREADS>& plan, uint32_t rows, uint64_t range_slots)
-      : a(args), rows_per_block(rows), range(range_slots) {
+  __device__ __forceinline__ Walk(const AttendArgs& args, const Plan<THREADS>& plan, const Span* kept, uint32_t rows, uint64_t range_slots)
+      : a(args), rows_per_block(rows), range(range_slots), spans(kept) {
     const uint64_t total = plan.before[THREADS];
     at = min(total, static_cast<uint64_t>(blockIdx.x) * range);
     end = min(total, at + range);
@@ -129,7 +135,7 @@ struct Walk {
     seq = lo * ((a.batch.n_seqs + THREADS - 1) / THREADS);
     item_at = plan.before[lo];
     for (;; ++seq) {
-      const uint64_t n = sequence_slots(a, rows_per_block, seq);
+      const uint64_t n = sequence_slots(a, rows_per_block, seq, span_of(seq));
       if (item_at + n > at || seq + 1 >= a.batch.n_seqs) break;
       item_at += n;
     }
@@ -147,8 +153,10 @@ struct Walk {
     }
   }
 
+  __device__ __forceinline__ Span span_of(uint32_t s) const { return s < kSpans ? spans[s] : sequence_span(a.batch, s); }
+
   __device__ __forceinline__ void enter() {
-    span = sequence_span(a.batch, seq);
+    span = span_of(seq);
     blocks = (span.count * a.group + rows_per_block - 1) / rows_per_block;
   }
 

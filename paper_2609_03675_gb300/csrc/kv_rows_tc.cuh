@@ -63,6 +63,7 @@ struct TcSmem {
   char raw[2][BITS == 4 ? kTcRaw : 1][BITS == 4 ? kTile * (D / 2) : 16];
   uint32_t raw_word[2][kTcRaw][kTcProducers];
   uint64_t row_of[2][BITS == 4 ? 1 : kTcStages][kTile];  // 16 bits: the tokens' rows in the pages, ~0 where there is nothing
+  Span spans[kSpans];
   TcInfo info[kTcInfo];
   float top[kTcRows], sum[kTcRows];
   uint64_t full[2][kTcStages], empty[2][kTcStages];  // keys, values
@@ -300,12 +301,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     tc_fence_before();
   }
-  const uint64_t range = sm.plan.set_up(a, kTcRows);  // ends with a barrier
+  const uint64_t range = sm.plan.set_up(a, kTcRows, sm.spans);  // ends with a barrier
   tc_fence_after();
   const uint32_t tmem = sm.tmem;
   const auto o_at = [&](uint32_t t) { return tmem + t * D; };
   const auto s_at = [&](uint32_t t, uint32_t i) { return tmem + 2 * D + (2 * t + i % 2) * kTile; };
-  Walk<kTcThreads> walk(a, sm.plan, kTcRows, range);
+  Walk<kTcThreads> walk(a, sm.plan, sm.spans, kTcRows, range);
   __syncthreads();
   const BatchArg& b = a.batch;
   Item it;
@@ -519,28 +520,49 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
           sm.sum[lr] = sum;
           bar_sync<1, kTcSoftmax>();
           const uint32_t rows = min(static_cast<uint32_t>(kTcRows), all - it.rb * kTcRows);
-          for (uint32_t x = threadIdx.x; x < rows * (D / 4); x += kTcSoftmax) {
-            const uint32_t row = x / (D / 4), d = x % (D / 4) * 4;
-            const float mine = sm.top[row], total = sm.sum[row], by_total = total == 0.f ? 0.f : 1.f / total;
-            float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
+          // eight units of four values to a thread at a time, whose loads are all on their way together
+          constexpr int kUnits = 8;
+          for (uint32_t x0 = threadIdx.x; x0 < rows * (D / 4); x0 += kTcSoftmax * kUnits) {
+            float4 y[kUnits];
+#pragma unroll
+            for (int u = 0; u < kUnits; ++u) y[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
             for (uint32_t i = 0; i < parts; ++i) {
-              const uint64_t at = part_at(i, row);
-              const float2 ms = __ldcg(&a.part_ms[at]);
-              const float4 z = __ldcg(reinterpret_cast<const float4*>(a.part + at * D + d));
-              const float k = ms.x == -INFINITY ? (ms.y == 0.f ? 0.f : 1.f) : exp2_fast(ms.x - mine);
-              y.x += k * z.x, y.y += k * z.y, y.z += k * z.z, y.w += k * z.w;
+              float4 z[kUnits];
+              float k[kUnits];
+#pragma unroll
+              for (int u = 0; u < kUnits; ++u) {
+                const uint32_t x = min(x0 + u * kTcSoftmax, rows * (D / 4) - 1), row = x / (D / 4);
+                const uint64_t at = part_at(i, row);
+                z[u] = __ldcg(reinterpret_cast<const float4*>(a.part + at * D + x % (D / 4) * 4));
+                const float2 ms = __ldcg(&a.part_ms[at]);
+                k[u] = ms.x == -INFINITY ? (ms.y == 0.f ? 0.f : 1.f) : exp2_fast(ms.x - sm.top[row]);
+              }
+#pragma unroll
+              for (int u = 0; u < kUnits; ++u) {
+                y[u].x += k[u] * z[u].x;
+                y[u].y += k[u] * z[u].y;
+                y[u].z += k[u] * z[u].z;
+                y[u].w += k[u] * z[u].w;
+              }
             }
-            const uint32_t tok = (it.rb * kTcRows + row) / a.group, hd = it.head * a.group + (it.rb * kTcRows + row) % a.group;
-            T* o = reinterpret_cast<T*>(a.q.out) + static_cast<int64_t>(it.span.first + tok) * a.q.out_token +
-                   static_cast<int64_t>(hd) * a.q.out_head + d;
-            if (a.out_wide) {
-              *reinterpret_cast<uint2*>(o) = make_uint2(P::pack(y.x * by_total, y.y * by_total), P::pack(y.z * by_total, y.w * by_total));
-            } else {
-              o[0] = Elem<T>::from(y.x * by_total);
-              o[1] = Elem<T>::from(y.y * by_total);
-              o[2] = Elem<T>::from(y.z * by_total);
-              o[3] = Elem<T>::from(y.w * by_total);
+#pragma unroll
+            for (int u = 0; u < kUnits; ++u) {
+              const uint32_t x = x0 + u * kTcSoftmax, row = x / (D / 4), d = x % (D / 4) * 4;
+              if (x >= rows * (D / 4)) break;
+              const float total = sm.sum[row], by_total = total == 0.f ? 0.f : 1.f / total;
+              const uint32_t tok = (it.rb * kTcRows + row) / a.group, hd = it.head * a.group + (it.rb * kTcRows + row) % a.group;
+              T* o = reinterpret_cast<T*>(a.q.out) + static_cast<int64_t>(it.span.first + tok) * a.q.out_token +
+                     static_cast<int64_t>(hd) * a.q.out_head + d;
+              if (a.out_wide) {
+                *reinterpret_cast<uint2*>(o) =
+                    make_uint2(P::pack(y[u].x * by_total, y[u].y * by_total), P::pack(y[u].z * by_total, y[u].w * by_total));
+              } else {
+                o[0] = Elem<T>::from(y[u].x * by_total);
+                o[1] = Elem<T>::from(y[u].y * by_total);
+                o[2] = Elem<T>::from(y[u].z * by_total);
+                o[3] = Elem<T>::from(y[u].w * by_total);
+              }
             }
           }
           bar_sync<1, kTcSoftmax>();

@@ -155,14 +155,15 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
   constexpr int kRows = 8 * NT, kGroups = D / 64, kM = R::kTokens / 16, kPerTile = kTile / R::kTokens;
   extern __shared__ __align__(128) char smem[];
   __shared__ Plan<kSplitThreads> plan;
+  __shared__ Span spans[kSpans];
   __shared__ float warp_m[kSplitWarps][kRows], warp_l[kSplitWarps][kRows];
   __shared__ uint2 stages[kSplitWarps][R::kStages];  // the bits of the tokens that are seen, and the first one's place
   __shared__ uint32_t last_here;
   pdl_trigger();
   pdl_wait();
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, c = lane % 4;
-  const uint64_t range = plan.set_up(a, kRows);
-  Walk<kSplitThreads> walk(a, plan, kRows, range);
+  const uint64_t range = plan.set_up(a, kRows, spans);
+  Walk<kSplitThreads> walk(a, plan, spans, kRows, range);
   const char* const ring = smem + warp * R::kWarp;
   const BatchArg& b = a.batch;
   Item it;

@@ -177,9 +177,11 @@ extern "C" int cofie_kv_attend(cofie_kv_t* h, const cofie_kv_batch* b, const cof
   size_t smem = 0;
   if (rows > 16) {
     const SplitKernel k = rows_kernel(h->p, &smem);
+    a.item_slots = 16;
     return launched(h, launch_dependent(true, k, dim3(sm_count()), dim3(kTcThreads), smem, st, a), "attend");
   }
   const int i = rows <= 8 ? 0 : 1;
+  a.item_slots = 4;
   const SplitKernel k = split_kernel(h->p, i, &smem);
   return launched(h, launch_dependent(true, k, dim3(h->split_ctas[i]), dim3(kSplitThreads), smem, st, a), "attend");
 }

@@ -2,7 +2,7 @@
 //
 // An item is one block of a sequence's query rows (row = new token x group +
 // head of the group) over one key/value head; its cached tokens come in tiles
-// of 64. All items, laid end to end, a slot for each tile and one more for the
+// of 64. All items, laid end to end, a slot for each tile and some more for the
 // item's fixed cost, are cut into equal ranges, one for each CTA, so that long
 // and short sequences, many heads and one, fill the GPU alike. A CTA works
 // through its range item by item. An item that lies in several ranges leaves a
@@ -28,6 +28,7 @@ struct AttendArgs {
   const uint16_t* k_words;
   const uint16_t* v_words;
   uint32_t heads, group, causal;
+  uint32_t item_slots;  // slots that an item costs beside those of its tiles
   uint32_t q_wide, out_wide;  // rows of q (16-byte vectors) and of the output (8-byte) are aligned
   float scale;
   // tiles that the mask leaves, in order, and their count, for each sequence (with a mask)
@@ -57,9 +58,9 @@ __device__ __forceinline__ uint64_t sequence_slots(const AttendArgs& a, uint32_t
   const uint32_t blocks = (sp.count * a.group + rows_per_block - 1) / rows_per_block;
   uint64_t n = 0;
   if (a.causal && !a.mask)
-    for (uint32_t rb = 0; rb < blocks; ++rb) n += block_tiles(a, sp, rows_per_block, rb, seq) + 1;
+    for (uint32_t rb = 0; rb < blocks; ++rb) n += block_tiles(a, sp, rows_per_block, rb, seq) + a.item_slots;
   else if (blocks)
-    n = static_cast<uint64_t>(blocks) * (block_tiles(a, sp, rows_per_block, 0, seq) + 1);
+    n = static_cast<uint64_t>(blocks) * (block_tiles(a, sp, rows_per_block, 0, seq) + a.item_slots);
   return n * a.batch.kv_heads;
 }
 
@@ -142,7 +143,7 @@ struct Walk {
     rb = head = 0;
     enter();
     for (;;) {  // row blocks of the sequence, then heads
-      const uint64_t n = block_tiles(a, span, rows_per_block, rb, seq) + 1;
+      const uint64_t n = block_tiles(a, span, rows_per_block, rb, seq) + a.item_slots;
       if (item_at + n * a.batch.kv_heads > at) {
         head = static_cast<uint32_t>((at - item_at) / n);
         item_at += n * head;
@@ -164,9 +165,9 @@ struct Walk {
   __device__ __forceinline__ bool next(Item& it) {
     while (at < end) {
       const uint32_t tiles = block_tiles(a, span, rows_per_block, rb, seq);
-      const uint64_t first = item_at + 1, past = first + tiles;  // the tiles' slots
+      const uint64_t first = item_at + a.item_slots, past = first + tiles;  // the tiles' slots
       const uint64_t lo = max(at, first), hi = min(end, past);
-      const bool mine = tiles ? hi > lo : at <= item_at;
+      const bool mine = tiles ? hi > lo : at <= item_at;  // an item without tiles belongs to its first slot
       if (mine) {
         it.seq = seq;
         it.rb = rb;

@@ -360,7 +360,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
 #pragma unroll 1
         for (uint32_t j = 0; j < tiles; ++j, ++n, ++s_n) {
           const TcInfo& info = sm.info[n % kTcInfo];
-          ok = ok && tc_wait(&sm.info_full[n % kTcInfo], n / kTcInfo, stop) && tc_wait(&sm.s_full[t][s_n % 2], s_n / 2, stop);
+          // S first: after an item in which this half had no rows, info may be some phases behind until then
+          ok = ok && tc_wait(&sm.s_full[t][s_n % 2], s_n / 2, stop) && tc_wait(&sm.info_full[n % kTcInfo], n / kTcInfo, stop);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) {
             n += tiles - j;
@@ -715,8 +716,13 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
       uint32_t n = 0, q_n = 0, s_n = 0;  // tiles so far; items and tiles of this half
       while (ok && walk.next(it)) {
         const uint32_t tiles = it.hi - it.lo, halves = it.span.count * a.group - it.rb * kTcRows > 128 ? 2 : 1;
-        if (t >= halves) {  // the other warp stands in for this one
-          n += tiles;
+        if (t >= halves) {  // nothing to issue, but to stay in step: a barrier's phases are told apart by their parity
+          for (uint32_t j = 0; j < tiles; ++j, ++n)
+            for (uint32_t v = 0; v < 2; ++v) {
+              ok = ok && tc_wait(&sm.full[v][n % kTcStages], n / kTcStages, stop);
+              ok = __all_sync(0xffffffffu, ok);
+              if (ok) warp_arrive(&sm.empty[v][n % kTcStages]);
+            }
           continue;
         }
         if (tiles == 0) continue;
@@ -735,7 +741,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
             tc_mma_ss(leader, d, q + (e / 4) * (S::kBlockQ / 16) + (e % 4) * 2, k + (e / 4) * (S::kBlock / 16) + (e % 4) * 2, kQK, e > 0);
           tc_commit(leader, &sm.s_full[t][i % 2]);
           tc_commit(leader, &sm.empty[0][st]);
-          if (halves == 1) tc_commit(leader, &sm.empty[0][st]);
         };
         for (uint32_t j = 0; j < 2 && j < tiles; ++j) qk(j);
 #pragma unroll 1
@@ -750,7 +755,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
           for (int e = 0; e < static_cast<int>(kTile) / 16; ++e) tc_mma_ts(leader, o_at(t), p + e * 8, v + e * (2048 / 16), kPV, j > 0 || e > 0);
           tc_commit(leader, &sm.o_full[t][i % 2]);
           tc_commit(leader, &sm.empty[1][st]);
-          if (halves == 1) tc_commit(leader, &sm.empty[1][st]);
           if (j + 2 < tiles) qk(j + 2);
         }
         s_n += tiles;

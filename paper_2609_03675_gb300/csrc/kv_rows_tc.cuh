@@ -65,7 +65,7 @@ struct TcSmem {
   uint64_t row_of[2][BITS == 4 ? 1 : kTcStages][kTile];  // 16 bits: the tokens' rows in the pages, ~0 where there is nothing
   Span spans[kSpans];
   TcInfo info[kTcInfo];
-  float top[kTcRows], sum[kTcRows];
+  float by_sum[kTcRows];
   uint64_t full[2][kTcStages], empty[2][kTcStages];  // keys, values
   // A barrier's phase can be told from the one before only. O is ready twice before anyone has to look, so it has a
   // barrier for even tiles and one for odd ones, as S and P have.
@@ -510,34 +510,40 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
           const auto part_at = [&](uint32_t i, uint32_t row) { return (2ull * (it.first_cta + i) + (i == 0)) * kTcRows + row; };
           float top = -INFINITY, sum = 0.f;
           if (real) {
+#pragma unroll 4
             for (uint32_t i = 0; i < parts; ++i) top = fmaxf(top, __ldcg(&a.part_ms[part_at(i, lr)]).x);
+#pragma unroll 4
             for (uint32_t i = 0; i < parts; ++i) {
-              const float2 z = __ldcg(&a.part_ms[part_at(i, lr)]);
-              sum += z.y == 0.f ? 0.f : (z.x == -INFINITY ? 1.f : exp2_fast(z.x - top)) * z.y;
+              float2* at = &a.part_ms[part_at(i, lr)];
+              const float2 z = __ldcg(at);
+              const float k = z.x == -INFINITY ? (z.y == 0.f ? 0.f : 1.f) : exp2_fast(z.x - top);
+              sum += z.y == 0.f ? 0.f : k * z.y;
+              __stcg(&at->x, k);  // the part's factor, for the threads that join it
             }
             if (a.lse) a.lse[static_cast<uint64_t>(it.span.first + token) * a.heads + head] = (top + log2f(sum)) * 0.6931471805599453f;
           }
-          sm.top[lr] = top;
-          sm.sum[lr] = sum;
+          sm.by_sum[lr] = sum == 0.f ? 0.f : 1.f / sum;
           bar_sync<1, kTcSoftmax>();
           const uint32_t rows = min(static_cast<uint32_t>(kTcRows), all - it.rb * kTcRows);
-          // eight units of four values to a thread at a time, whose loads are all on their way together
-          constexpr int kUnits = 8;
-          for (uint32_t x0 = threadIdx.x; x0 < rows * (D / 4); x0 += kTcSoftmax * kUnits) {
+          // eight units of four values to a thread at a time, whose loads are all on their way together (a unit's row is
+          // the same for a whole warp, or half of it)
+          constexpr uint32_t kUnits = 8;
+          const uint32_t all_units = rows * (D / 4);
+          for (uint32_t x0 = threadIdx.x; x0 < all_units; x0 += kTcSoftmax * kUnits) {
             float4 y[kUnits];
 #pragma unroll
             for (int u = 0; u < kUnits; ++u) y[u] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 2
             for (uint32_t i = 0; i < parts; ++i) {
+              const float4* from = reinterpret_cast<const float4*>(a.part + part_at(i, 0) * D) + x0;
+              const float2* factor = a.part_ms + part_at(i, x0 / (D / 4));
               float4 z[kUnits];
               float k[kUnits];
 #pragma unroll
               for (int u = 0; u < kUnits; ++u) {
-                const uint32_t x = min(x0 + u * kTcSoftmax, rows * (D / 4) - 1), row = x / (D / 4);
-                const uint64_t at = part_at(i, row);
-                z[u] = __ldcg(reinterpret_cast<const float4*>(a.part + at * D + x % (D / 4) * 4));
-                const float2 ms = __ldcg(&a.part_ms[at]);
-                k[u] = ms.x == -INFINITY ? (ms.y == 0.f ? 0.f : 1.f) : exp2_fast(ms.x - sm.top[row]);
+                const bool there = x0 + u * kTcSoftmax < all_units;
+                z[u] = there ? __ldcg(from + u * kTcSoftmax) : make_float4(0.f, 0.f, 0.f, 0.f);
+                k[u] = there ? __ldcg(&factor[u * (kTcSoftmax / (D / 4))].x) : 0.f;
               }
 #pragma unroll
               for (int u = 0; u < kUnits; ++u) {
@@ -550,8 +556,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
 #pragma unroll
             for (int u = 0; u < kUnits; ++u) {
               const uint32_t x = x0 + u * kTcSoftmax, row = x / (D / 4), d = x % (D / 4) * 4;
-              if (x >= rows * (D / 4)) break;
-              const float total = sm.sum[row], by_total = total == 0.f ? 0.f : 1.f / total;
+              if (x >= all_units) break;
+              const float by_total = sm.by_sum[row];
               const uint32_t tok = (it.rb * kTcRows + row) / a.group, hd = it.head * a.group + (it.rb * kTcRows + row) % a.group;
               T* o = reinterpret_cast<T*>(a.q.out) + static_cast<int64_t>(it.span.first + tok) * a.q.out_token +
                      static_cast<int64_t>(hd) * a.q.out_head + d;

@@ -22,9 +22,11 @@ struct CodesArgs {
 
 // Appends to 4-bit pages. CTAs of gridDim.y below q_parts rotate the queries;
 // the others take a share of the (key or value, head) rows of their tokens.
-// Eight values of a row to a lane, a group's 64 to eight lanes, which find its
-// extremes by shuffles.
-template <typename T, int V, int D>
+// Sixteen values of a row to a lane, a group's 64 to four lanes, which find its
+// extremes by shuffles. WIDE: rows are read 16 bytes at a time, and what a
+// value is rotated with lies in as many pieces (sizes and strides that allow
+// it); else value by value.
+template <typename T, int V, int D, bool WIDE>
 __global__ void __launch_bounds__(kThreads) append_codes(const __grid_constant__ CodesArgs a, const __grid_constant__ RotaryTable tab) {
   extern __shared__ float2 cs[];
   const RowsArgs& r = a.rows;
@@ -39,12 +41,13 @@ __global__ void __launch_bounds__(kThreads) append_codes(const __grid_constant__
     if (h0 < r.heads) rows_run<T, V>(r, tab, t0, n, h0, min(per, r.heads - h0), cs, place);
     return;
   }
-  constexpr uint32_t kLanes = D / 8;  // of a row
+  constexpr uint32_t kLanes = D / 16;  // of a row
   const uint32_t parts = gridDim.y - a.q_parts, part = blockIdx.y - a.q_parts;
   const uint32_t per = (2 * a.kv_heads + parts - 1) / parts, k0 = part * per;
   if (k0 >= 2 * a.kv_heads) return;
   const uint32_t kinds = min(per, 2 * a.kv_heads - k0);
   const uint32_t lane = threadIdx.x % kLanes, rows = n * kinds;
+  const bool by_half = tab.layout == COFIE_ROTARY_HALF;
   // whole warps stay in the loop, for the shuffles
   for (uint32_t base = 0; base < rows; base += kThreads / kLanes) {
     const uint32_t row = base + threadIdx.x / kLanes;
@@ -52,57 +55,96 @@ __global__ void __launch_bounds__(kThreads) append_codes(const __grid_constant__
     const uint32_t t = live ? row / kinds : 0, kind = live ? k0 + row - t * kinds : 0;
     const uint32_t v = kind >= a.kv_heads, head = kind - v * a.kv_heads;
     const int64_t p = live ? place[t] : -1;
-    float x[8];
+    float x[16];
     if (p >= 0) {
       const T* in = reinterpret_cast<const T*>(a.in[v]) + static_cast<int64_t>(t0 + t) * a.in_token[v] + head * a.in_head[v];
+      const uint32_t d0 = lane * 16;
+      const float2* c = cs + t * tab.half;
+      if (WIDE) {
+        const auto read = [&](uint32_t d, float* y) {
+          const RowVec<T, 8> w = *reinterpret_cast<const RowVec<T, 8>*>(in + d);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const uint32_t d = lane * 8 + i;
-        x[i] = Elem<T>::to(in[d]);
-        if (!v && d < 2 * tab.half) {
-          const bool by_half = tab.layout == COFIE_ROTARY_HALF;
-          const bool second = by_half ? d >= tab.half : d & 1;
-          const uint32_t pair = by_half ? (second ? d - tab.half : d) : d / 2;
-          const float other = Elem<T>::to(in[by_half ? (second ? d - tab.half : d + tab.half) : d ^ 1]);
-          const float2 c = cs[t * tab.half + pair];
-          x[i] = second ? x[i] * c.x + other * c.y : x[i] * c.x - other * c.y;
+          for (int i = 0; i < 8; ++i) y[i] = Elem<T>::to(w.v[i]);
+        };
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const uint32_t d = d0 + 8 * e;
+          float* const xe = x + 8 * e;
+          read(d, xe);
+          if (v || d >= 2 * tab.half) continue;
+          if (by_half) {
+            const bool second = d >= tab.half;
+            const uint32_t o = second ? d - tab.half : d;
+            float y[8];
+            read(second ? o : d + tab.half, y);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float2 z = c[o + i];
+              xe[i] = xe[i] * z.x + y[i] * (second ? z.y : -z.y);
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+              const float2 z = c[d / 2 + i / 2];
+              const float f = xe[i], g = xe[i + 1];
+              xe[i] = f * z.x - g * z.y;
+              xe[i + 1] = g * z.x + f * z.y;
+            }
+          }
+        }
+      } else {
+#pragma unroll 4
+        for (int i = 0; i < 16; ++i) {
+          const uint32_t d = d0 + i;
+          float f = Elem<T>::to(in[d]);
+          if (!v && d < 2 * tab.half) {
+            const bool second = by_half ? d >= tab.half : d & 1;
+            const uint32_t pair = by_half ? (second ? d - tab.half : d) : d / 2;
+            const float other = Elem<T>::to(in[by_half ? (second ? d - tab.half : d + tab.half) : d ^ 1]);
+            const float2 z = c[pair];
+            f = second ? f * z.x + other * z.y : f * z.x - other * z.y;
+          }
+          x[i] = f;
         }
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = 0.f;
+      for (int i = 0; i < 16; ++i) x[i] = 0.f;
     }
-    float lo = 0.f, hi = 0.f;
+    float lo = 0.f, hi = 0.f, none = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 16; ++i) {
       lo = fminf(lo, x[i]);
       hi = fmaxf(hi, x[i]);
-      if (!(fabsf(x[i]) <= 3.402823466e38f)) hi = INFINITY;  // fmax drops a NaN
+      none = fmaf(x[i], 0.f, none);  // fmin and fmax drop a NaN
     }
+    if (!(none == 0.f)) hi = INFINITY;
 #pragma unroll
-    for (int o = 1; o < 8; o <<= 1) {
+    for (int o = 1; o < 4; o <<= 1) {
       lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
       hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
     }
     const float scale = group_scale(lo, hi);
-    // x / scale to the nearest, halves away from zero: the product with the
-    // reciprocal made a little too large (2^-21, more than its rounding) is
-    // never a half where the quotient is one, and no quotient of 16-bit x
-    // lies that close to a half without being one
-    const float inv = scale > 0.f ? __fmul_rn(__fdiv_rn(1.f, scale), 1.f + 0x1p-21f) : 0.f;
-    const float zero = fminf(rintf(-lo * inv), 15.f);
-    uint32_t word = 0;
+    // x / scale to the nearest, halves away from zero: the reciprocal is taken
+    // a little above its value, so that no half stays one, and the product and
+    // the zero point are summed and rounded once, to the last bit of 1.5 2^23.
+    // (No quotient of 16-bit x lies that close to a half without being one.)
+    const float inv = scale > 0.f ? __uint_as_float(__float_as_uint(__frcp_ru(scale)) + 1) : 0.f;
+    const float zero = fminf(__fmaf_rn(-lo, inv, 12582912.f), 12582927.f);
+    uint32_t word[2];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float q = fminf(fmaxf(rintf(x[i] * inv) + zero, 0.f), 15.f);
-      word |= static_cast<uint32_t>(q) << (4 * i);
+    for (int e = 0; e < 2; ++e) {
+      // codes are the low bits of 0x4B400000 + code, whose sum's share is taken off at the end
+      uint32_t w = 0;
+#pragma unroll
+      for (int i = 7; i >= 0; --i) w = w * 16 + __float_as_uint(fminf(__fmaf_rn(x[8 * e + i], inv, zero), 12582927.f));
+      word[e] = w - 0x4B400000u * 0x11111111u;
     }
     if (p >= 0) {
       const uint64_t out = page_row(r.batch, p, head);
-      a.codes[v][out * kLanes + lane] = word;
-      if (lane % 8 == 0)
-        a.words[v][out * (D / kGroup) + lane / 8] =
-            static_cast<uint16_t>((__float_as_uint(scale) >> 16) | static_cast<uint32_t>(zero));
+      reinterpret_cast<uint2*>(a.codes[v])[out * kLanes + lane] = make_uint2(word[0], word[1]);
+      if (lane % 4 == 0)
+        a.words[v][out * (D / kGroup) + lane / 4] = static_cast<uint16_t>((__float_as_uint(scale) >> 16) | (__float_as_uint(zero) & 15u));
     }
   }
 }
@@ -114,41 +156,48 @@ struct ReadArgs {
   uint4* out[2];
 };
 
+constexpr uint32_t kReadTile = 16;  // tokens of a CTA
+
 // Eight values of a (token, key or value, head) row to a thread.
 template <typename T, int D, int BITS>
 __global__ void __launch_bounds__(kThreads) read_pages(const ReadArgs a) {
   constexpr uint32_t kLanes = D / 8;
+  __shared__ int64_t place[kReadTile];
   pdl_trigger();
   pdl_wait();
-  const uint64_t per_token = 2ull * a.batch.kv_heads * kLanes;
-  const uint64_t total = a.batch.n_tokens * per_token;
-  for (uint64_t e = blockIdx.x * static_cast<uint64_t>(kThreads) + threadIdx.x; e < total; e += static_cast<uint64_t>(gridDim.x) * kThreads) {
-    const uint32_t t = static_cast<uint32_t>(e / per_token), x = static_cast<uint32_t>(e - t * per_token);
-    const uint32_t lane = x % kLanes, kind = x / kLanes;
+  const uint32_t t0 = blockIdx.x * kReadTile, n = min(kReadTile, a.batch.n_tokens - t0);
+  if (threadIdx.x < n) place[threadIdx.x] = place_of(a.batch, a.batch.offsets, t0 + threadIdx.x);
+  __syncthreads();
+  const uint32_t lane = threadIdx.x % kLanes, kinds = 2 * a.batch.kv_heads;
+#pragma unroll 4
+  for (uint32_t row = threadIdx.x / kLanes; row < n * kinds; row += kThreads / kLanes) {
+    const uint32_t t = row / kinds, kind = row - t * kinds;
     const uint32_t v = kind >= a.batch.kv_heads, head = kind - v * a.batch.kv_heads;
-    const int64_t p = place_of(a.batch, a.batch.offsets, t);
+    const int64_t p = place[t];
     uint4 val = make_uint4(0, 0, 0, 0);
     if (p >= 0) {
-      const uint64_t row = page_row(a.batch, p, head);
+      const uint64_t at = page_row(a.batch, p, head);
       if (BITS == 16) {
-        val = reinterpret_cast<const uint4*>(a.pages[v])[row * kLanes + lane];
+        val = reinterpret_cast<const uint4*>(a.pages[v])[at * kLanes + lane];
       } else {
-        const uint32_t codes = reinterpret_cast<const uint32_t*>(a.pages[v])[row * kLanes + lane];
-        const uint32_t word = a.words[v][row * (D / kGroup) + lane / 8];
-        RowVec<T, 8> y;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) y.v[i] = Elem<T>::from(code_value(codes >> (4 * i) & 15u, word));
-        val = *reinterpret_cast<uint4*>(&y);
+        const Unpack<T> u(a.words[v][at * (D / kGroup) + lane / 8]);
+        const uint4 y = u(reinterpret_cast<const uint32_t*>(a.pages[v])[at * kLanes + lane]);  // (0, 4), (1, 5), (2, 6), (3, 7)
+        val = make_uint4(__byte_perm(y.x, y.y, 0x5410), __byte_perm(y.z, y.w, 0x5410), __byte_perm(y.x, y.y, 0x7632),
+                         __byte_perm(y.z, y.w, 0x7632));
       }
     }
-    a.out[v][(static_cast<uint64_t>(t) * a.batch.kv_heads + head) * kLanes + lane] = val;
+    a.out[v][(static_cast<uint64_t>(t0 + t) * a.batch.kv_heads + head) * kLanes + lane] = val;
   }
 }
 
 template <typename T, int D>
 cudaError_t launch_codes(CodesArgs a, const RotaryTable& tab, bool queries, cudaStream_t st) {
   RowsArgs& r = a.rows;
-  const uint32_t v = queries ? rows_vector(r, tab, D, 2) : 8;
+  uint32_t v = queries ? rows_vector(r, tab, D, 2) : 8;
+  bool wide = v == 8 && tab.half % (tab.layout == COFIE_ROTARY_HALF ? 8 : 4) == 0;
+  for (int i = 0; i < 2; ++i)
+    wide = wide && reinterpret_cast<uintptr_t>(a.in[i]) % 16 == 0 && a.in_token[i] % 8 == 0 && a.in_head[i] % 8 == 0;
+  if (!wide) v = v >= 2 ? 2 : 1;
   r.units = D / (2 * v);
   r.rotary_units = tab.half / v;
   r.offsets_in_smem = r.batch.offsets && r.batch.n_seqs <= kOffsetsInSmem;
@@ -159,16 +208,13 @@ cudaError_t launch_codes(CodesArgs a, const RotaryTable& tab, bool queries, cuda
   const dim3 grid(tiles, parts + a.q_parts);
   const size_t smem = rows_smem(r.tile, tab.half, r.batch.n_seqs, r.offsets_in_smem);
   const auto go = [&](auto kernel) { return launch_dependent(true, kernel, grid, dim3(kThreads), smem, st, a, tab); };
-  return v == 8   ? go(append_codes<T, 8, D>)
-         : v == 4 ? go(append_codes<T, 4, D>)
-         : v == 2 ? go(append_codes<T, 2, D>)
-                  : go(append_codes<T, 1, D>);
+  if (wide) return go(append_codes<T, 8, D, true>);
+  return v == 2 ? go(append_codes<T, 2, D, false>) : go(append_codes<T, 1, D, false>);
 }
 
 template <typename T, int D>
 cudaError_t launch_read(const ReadArgs& a, uint32_t bits, cudaStream_t st) {
-  const uint64_t total = 2ull * a.batch.n_tokens * a.batch.kv_heads * (D / 8);
-  const dim3 grid(static_cast<uint32_t>(std::min<uint64_t>((total + kThreads - 1) / kThreads, sm_count() * 64ull)));
+  const dim3 grid((a.batch.n_tokens + kReadTile - 1) / kReadTile);
   return bits == 4 ? launch_dependent(true, read_pages<T, D, 4>, grid, dim3(kThreads), 0, st, a)
                    : launch_dependent(true, read_pages<T, D, 16>, grid, dim3(kThreads), 0, st, a);
 }

@@ -193,51 +193,6 @@ __device__ __forceinline__ void tc_wait_ld(uint32_t* r) {
 }
 __device__ __forceinline__ void tc_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// Eight codes to (n - z) s, in the order (0, 4), (1, 5), (2, 6), (3, 7).
-template <typename T>
-struct Unpack;
-template <>
-struct Unpack<__nv_bfloat16> {
-  __nv_bfloat162 z, s;
-  __device__ __forceinline__ explicit Unpack(uint32_t word) {
-    const uint32_t a = (word & 15u) | 0x4300u, b = word & 0xFFF0u;  // 128 + z
-    const uint32_t aa = a | a << 16, bb = b | b << 16;
-    z = *reinterpret_cast<const __nv_bfloat162*>(&aa);
-    s = *reinterpret_cast<const __nv_bfloat162*>(&bb);
-  }
-  __device__ __forceinline__ uint4 operator()(uint32_t w) const {
-    uint32_t r[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t x = ((w >> (4 * i)) & 0x000F000Fu) | 0x43004300u;  // 128 + n
-      const __nv_bfloat162 y = __hmul2(__hsub2(*reinterpret_cast<const __nv_bfloat162*>(&x), z), s);
-      r[i] = *reinterpret_cast<const uint32_t*>(&y);
-    }
-    return make_uint4(r[0], r[1], r[2], r[3]);
-  }
-};
-template <>
-struct Unpack<__half> {
-  __half2 z, z16, s;
-  __device__ __forceinline__ explicit Unpack(uint32_t word) {
-    const float f = static_cast<float>(word & 15u);
-    z = __float2half2_rn(1024.f + f);
-    z16 = __float2half2_rn(-64.f - f);
-    s = __float2half2_rn(__uint_as_float((word & 0xFFF0u) << 16));
-  }
-  __device__ __forceinline__ uint4 operator()(uint32_t w) const {
-    uint32_t r[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t x = ((w >> (8 * (i / 2))) & (i % 2 ? 0x00F000F0u : 0x000F000Fu)) | 0x64006400u;  // 1024 + n, 1024 + 16 n
-      const __half2 h = *reinterpret_cast<const __half2*>(&x);
-      const __half2 y = __hmul2(i % 2 ? __hfma2(h, __float2half2_rn(0.0625f), z16) : __hsub2(h, z), s);
-      r[i] = *reinterpret_cast<const uint32_t*>(&y);
-    }
-    return make_uint4(r[0], r[1], r[2], r[3]);
-  }
-};
-
 // The largest of 64 values and `top`.
 __device__ __forceinline__ float most_of(const uint32_t* x, const uint32_t* y, float top) {
   float a = top, b = __uint_as_float(y[0]);

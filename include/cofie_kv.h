@@ -92,7 +92,7 @@ typedef struct {
 typedef struct {
   const void* in; /* device memory */
   void* out;      /* device memory; may be `in` itself with the same strides, else must not overlap it */
-  uint32_t heads;
+  uint32_t heads; /* 1..4096 */
   int64_t in_token, in_head, out_token, out_head;
 } cofie_rows;
 

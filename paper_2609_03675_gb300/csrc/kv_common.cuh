@@ -160,6 +160,28 @@ __device__ __forceinline__ float group_scale(float lo, float hi) {
   return __uint_as_float((__float_as_uint(raw) + 0xFFFFFu) & ~0xFFFFFu);
 }
 
+// Two 16-bit values in a register.
+template <typename T>
+struct Two;
+template <>
+struct Two<__nv_bfloat16> {
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    const __nv_bfloat162 x = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&x);
+  }
+  static __device__ __forceinline__ float lo(uint32_t x) { return __uint_as_float(x << 16); }
+  static __device__ __forceinline__ float hi(uint32_t x) { return __uint_as_float(x & 0xFFFF0000u); }
+};
+template <>
+struct Two<__half> {
+  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    const __half2 x = __floats2half2_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&x);
+  }
+  static __device__ __forceinline__ float lo(uint32_t x) { return __half2float(__ushort_as_half(static_cast<unsigned short>(x))); }
+  static __device__ __forceinline__ float hi(uint32_t x) { return __half2float(__ushort_as_half(static_cast<unsigned short>(x >> 16))); }
+};
+
 // Eight codes to (n - z) s, in the order (0, 4), (1, 5), (2, 6), (3, 7).
 template <typename T>
 struct Unpack;

@@ -62,9 +62,9 @@ __global__ void __launch_bounds__(kThreads) append_codes(const __grid_constant__
       const float2* c = cs + t * tab.half;
       if (WIDE) {
         const auto read = [&](uint32_t d, float* y) {
-          const RowVec<T, 8> w = *reinterpret_cast<const RowVec<T, 8>*>(in + d);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) y[i] = Elem<T>::to(w.v[i]);
+          RowVec<T, 8> w;
+          w.load(in + d);
+          w.to(y);
         };
 #pragma unroll
         for (int e = 0; e < 2; ++e) {

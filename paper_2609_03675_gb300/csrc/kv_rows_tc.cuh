@@ -298,10 +298,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
               if (a.q_wide) {
                 x = *reinterpret_cast<const uint4*>(q + e * 8);
               } else {
-                RowVec<T, 8> y;
-#pragma unroll
-                for (int f = 0; f < 8; ++f) y.v[f] = q[e * 8 + f];
-                x = *reinterpret_cast<uint4*>(&y);
+                x = gather8(q + e * 8);
               }
             }
             if (BITS == 4)

@@ -75,37 +75,23 @@ __device__ __forceinline__ float exp2_fast(float x) {
 }
 
 template <typename T>
-struct Pair;  // two 16-bit values in a register
+struct Pair;  // and their products
 template <>
-struct Pair<__nv_bfloat16> {
-  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
-    const __nv_bfloat162 x = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&x);
-  }
-  static __device__ __forceinline__ float lo(uint32_t x) { return __uint_as_float(x << 16); }
-  static __device__ __forceinline__ float hi(uint32_t x) { return __uint_as_float(x & 0xFFFF0000u); }
+struct Pair<__nv_bfloat16> : Two<__nv_bfloat16> {
   static __device__ __forceinline__ void mma(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
-    asm(
-        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
   }
 };
 template <>
-struct Pair<__half> {
-  static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
-    const __half2 x = __floats2half2_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&x);
-  }
+struct Pair<__half> : Two<__half> {
   static __device__ __forceinline__ uint32_t sub(uint32_t a, uint32_t b) {
     const __half2 x = __hsub2(*reinterpret_cast<__half2*>(&a), *reinterpret_cast<__half2*>(&b));
     return *reinterpret_cast<const uint32_t*>(&x);
   }
-  static __device__ __forceinline__ float lo(uint32_t x) { return __half2float(__ushort_as_half(static_cast<unsigned short>(x))); }
-  static __device__ __forceinline__ float hi(uint32_t x) { return __half2float(__ushort_as_half(static_cast<unsigned short>(x >> 16))); }
   static __device__ __forceinline__ void mma(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
-    asm(
-        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
   }
@@ -193,10 +179,7 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
           if (a.q_wide) {
             x[e] = *reinterpret_cast<const uint4*>(q + d);
           } else {
-            RowVec<T, 8> y;
-#pragma unroll
-            for (int f = 0; f < 8; ++f) y.v[f] = q[d + f];
-            x[e] = *reinterpret_cast<uint4*>(&y);
+            x[e] = gather8(q + d);
           }
         }
       }

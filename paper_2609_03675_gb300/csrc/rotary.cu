@@ -141,7 +141,7 @@ int cofie_rotary_run(cofie_rotary_t* h, const cofie_rows* rows, uint32_t n_rows,
   for (uint32_t i = 0; i < n_rows; ++i) {
     const cofie_rows& r = rows[i];
     if (!r.in || !r.out) return h->fail(COFIE_EINVAL, "a tensor's in or out is NULL");
-    if (r.heads < 1 || r.heads > 65536) return h->fail(COFIE_EINVAL, "heads must be in [1, 65536]");
+    if (r.heads < 1 || r.heads > 4096) return h->fail(COFIE_EINVAL, "heads must be in [1, 4096]");
     if (reinterpret_cast<uintptr_t>(r.in) % size || reinterpret_cast<uintptr_t>(r.out) % size)
       return h->fail(COFIE_EINVAL, "a tensor is not aligned to its type");
     if (r.in == r.out && (r.in_token != r.out_token || r.in_head != r.out_head))

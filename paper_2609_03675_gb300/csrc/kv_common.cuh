@@ -151,13 +151,27 @@ struct Elem<float> {
   static __device__ __forceinline__ float from(float x) { return x; }
 };
 
-// The scale of a group from its extremes: (hi - lo) / 15 rounded up to 4
-// significant bits; NaN where that is not finite.
+// fmin and fmax that pass a NaN on.
+__device__ __forceinline__ float min_nan(float a, float b) {
+  float x;
+  asm("min.NaN.f32 %0, %1, %2;" : "=f"(x) : "f"(a), "f"(b));
+  return x;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float x;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(x) : "f"(a), "f"(b));
+  return x;
+}
+
+// The scale of a group from its extremes: the smallest number of 4 significant
+// bits that 15 times reach hi - lo with (the product is exact); NaN where that
+// is not finite.
 __device__ __forceinline__ float group_scale(float lo, float hi) {
-  const float raw = __fdiv_rn(__fsub_rn(hi, lo), 15.f);
-  if (!(raw <= 0x1.ep127f)) return __int_as_float(0x7FC00000);
-  if (raw < 0x1p-100f) return 0.f;
-  return __uint_as_float((__float_as_uint(raw) + 0xFFFFFu) & ~0xFFFFFu);
+  const float range = __fsub_rn(hi, lo), near = range * (1.f / 15.f);
+  float s = __uint_as_float(__float_as_uint(near) & ~0xFFFFFu);
+  if (15.f * s < range) s = __uint_as_float(__float_as_uint(s) + 0x100000u);
+  if (near < 0x1p-100f) s = 0.f;
+  return range <= 3.402823466e38f ? s : __int_as_float(0x7FC00000);
 }
 
 // Two 16-bit values in a register.

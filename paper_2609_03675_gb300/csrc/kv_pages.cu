@@ -22,15 +22,16 @@ struct CodesArgs {
 
 // Appends to 4-bit pages. CTAs of gridDim.y below q_parts rotate the queries;
 // the others take a share of the (key or value, head) rows of their tokens.
-// Sixteen values of a row to a lane, a group's 64 to four lanes, which find its
-// extremes by shuffles. WIDE: rows are read 16 bytes at a time, and what a
+// Sixteen values of a row to a lane, eight from either half of the head, so that
+// where all of it rotates in the half layout a lane holds both of a pair; the
+// lanes of a group find its extremes by shuffles. WIDE: rows are read 16 bytes at a time, and what a
 // value is rotated with lies in as many pieces (sizes and strides that allow
 // it); else value by value.
 template <typename T, int V, int D, bool WIDE>
 __global__ void __launch_bounds__(kThreads) append_codes(const __grid_constant__ CodesArgs a, const __grid_constant__ RotaryTable tab) {
-  extern __shared__ float2 cs[];
+  extern __shared__ __align__(16) float2 cs[];
   const RowsArgs& r = a.rows;
-  int64_t* place = reinterpret_cast<int64_t*>(cs + r.tile * tab.half);
+  int64_t* place = reinterpret_cast<int64_t*>(cs + r.tile * cs_stride(tab.half));
   int32_t* offs = reinterpret_cast<int32_t*>(place + r.tile);
   const uint32_t t0 = blockIdx.x * r.tile, n = min(r.tile, r.n_tokens - t0);
   pdl_trigger();
@@ -43,108 +44,128 @@ __global__ void __launch_bounds__(kThreads) append_codes(const __grid_constant__
   }
   constexpr uint32_t kLanes = D / 16;  // of a row
   const uint32_t parts = gridDim.y - a.q_parts, part = blockIdx.y - a.q_parts;
-  const uint32_t per = (2 * a.kv_heads + parts - 1) / parts, k0 = part * per;
-  if (k0 >= 2 * a.kv_heads) return;
-  const uint32_t kinds = min(per, 2 * a.kv_heads - k0);
-  const uint32_t lane = threadIdx.x % kLanes, rows = n * kinds;
+  const uint32_t per = (2 * a.kv_heads + parts - 1) / parts, k0 = part * per, k1 = min(k0 + per, 2 * a.kv_heads);
+  const uint32_t lane = threadIdx.x % kLanes, mine = threadIdx.x % 32 / kLanes;
   const bool by_half = tab.layout == COFIE_ROTARY_HALF;
-  // whole warps stay in the loop, for the shuffles
-  for (uint32_t base = 0; base < rows; base += kThreads / kLanes) {
-    const uint32_t row = base + threadIdx.x / kLanes;
-    const bool live = row < rows;
-    const uint32_t t = live ? row / kinds : 0, kind = live ? k0 + row - t * kinds : 0;
+  // a warp takes the keys or the values of a head, several tokens at a time
+  for (uint32_t kind = k0 + threadIdx.x / 32; kind < k1; kind += kThreads / 32) {
     const uint32_t v = kind >= a.kv_heads, head = kind - v * a.kv_heads;
-    const int64_t p = live ? place[t] : -1;
-    float x[16];
-    if (p >= 0) {
-      const T* in = reinterpret_cast<const T*>(a.in[v]) + static_cast<int64_t>(t0 + t) * a.in_token[v] + head * a.in_head[v];
-      const uint32_t d0 = lane * 16;
-      const float2* c = cs + t * tab.half;
-      if (WIDE) {
-        const auto read = [&](uint32_t d, float* y) {
-          RowVec<T, 8> w;
-          w.load(in + d);
-          w.to(y);
-        };
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const uint32_t d = d0 + 8 * e;
-          float* const xe = x + 8 * e;
-          read(d, xe);
-          if (v || d >= 2 * tab.half) continue;
-          if (by_half) {
-            const bool second = d >= tab.half;
-            const uint32_t o = second ? d - tab.half : d;
-            float y[8];
-            read(second ? o : d + tab.half, y);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const float2 z = c[o + i];
-              xe[i] = xe[i] * z.x + y[i] * (second ? z.y : -z.y);
-            }
-          } else {
-#pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-              const float2 z = c[d / 2 + i / 2];
-              const float f = xe[i], g = xe[i + 1];
-              xe[i] = f * z.x - g * z.y;
-              xe[i + 1] = g * z.x + f * z.y;
-            }
-          }
-        }
-      } else {
-#pragma unroll 4
-        for (int i = 0; i < 16; ++i) {
-          const uint32_t d = d0 + i;
-          float f = Elem<T>::to(in[d]);
-          if (!v && d < 2 * tab.half) {
-            const bool second = by_half ? d >= tab.half : d & 1;
-            const uint32_t pair = by_half ? (second ? d - tab.half : d) : d / 2;
-            const float other = Elem<T>::to(in[by_half ? (second ? d - tab.half : d + tab.half) : d ^ 1]);
-            const float2 z = c[pair];
-            f = second ? f * z.x + other * z.y : f * z.x - other * z.y;
-          }
-          x[i] = f;
-        }
-      }
-    } else {
+    const T* const in0 = reinterpret_cast<const T*>(a.in[v]) + static_cast<int64_t>(t0) * a.in_token[v] + head * a.in_head[v];
+    const int64_t in_token = a.in_token[v];
+    uint32_t* const codes = a.codes[v] + static_cast<uint64_t>(head << r.batch.page_shift) * (D / 8);
+    uint16_t* const words = a.words[v] + static_cast<uint64_t>(head << r.batch.page_shift) * (D / kGroup);
+    const uint32_t turned = v ? 0 : 2 * tab.half;  // values that are rotated
+    for (uint32_t t1 = 0; t1 < n; t1 += 32 / kLanes) {  // whole warps stay in the loop, for the shuffles
+      const uint32_t t = t1 + mine;
+      const int64_t p = t < n ? place[t] : -1;
+      float x[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) x[i] = 0.f;
-    }
-    float lo = 0.f, hi = 0.f, none = 0.f;
+      if (p >= 0) {
+        const T* in = in0 + t * in_token;
+        const float2* c = cs + t * cs_stride(tab.half);
+        if (WIDE) {
+          RowVec<T, 8> w[2];
+          w[0].load(in + lane * 8);
+          w[1].load(in + D / 2 + lane * 8);
+          w[0].to(x);
+          w[1].to(x + 8);
+          if (turned == D && by_half) {
+            float2 z[8];
+            load_cs<8>(c, lane * 8, z);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      lo = fminf(lo, x[i]);
-      hi = fmaxf(hi, x[i]);
-      none = fmaf(x[i], 0.f, none);  // fmin and fmax drop a NaN
-    }
-    if (!(none == 0.f)) hi = INFINITY;
+            for (int i = 0; i < 8; ++i) turn_pair(x[i], x[8 + i], z[i]);
+          } else {
 #pragma unroll
-    for (int o = 1; o < 4; o <<= 1) {
-      lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-      hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-    }
-    const float scale = group_scale(lo, hi);
-    // x / scale to the nearest, halves away from zero: the reciprocal is taken
-    // a little above its value, so that no half stays one, and the product and
-    // the zero point are summed and rounded once, to the last bit of 1.5 2^23.
-    // (No quotient of 16-bit x lies that close to a half without being one.)
-    const float inv = scale > 0.f ? __uint_as_float(__float_as_uint(__frcp_ru(scale)) + 1) : 0.f;
-    const float zero = fminf(__fmaf_rn(-lo, inv, 12582912.f), 12582927.f);
-    uint32_t word[2];
+            for (int e = 0; e < 2; ++e) {
+              const uint32_t d = e * (D / 2) + lane * 8;
+              if (d >= turned) continue;
+              if (by_half) {
+                const bool second = d >= tab.half;
+                const uint32_t o = second ? d - tab.half : d;
+                RowVec<T, 8> other;
+                other.load(in + (second ? o : d + tab.half));
+                float y[8];
+                float2 z[8];
+                other.to(y);
+                load_cs<8>(c, o, z);
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      // codes are the low bits of 0x4B400000 + code, whose sum's share is taken off at the end
-      uint32_t w = 0;
+                for (int i = 0; i < 8; ++i) x[8 * e + i] = x[8 * e + i] * z[i].x + y[i] * (second ? z[i].y : -z[i].y);
+              } else {
+                float2 z[4];
+                load_cs<4>(c, d / 2, z);
 #pragma unroll
-      for (int i = 7; i >= 0; --i) w = w * 16 + __float_as_uint(fminf(__fmaf_rn(x[8 * e + i], inv, zero), 12582927.f));
-      word[e] = w - 0x4B400000u * 0x11111111u;
-    }
-    if (p >= 0) {
-      const uint64_t out = page_row(r.batch, p, head);
-      reinterpret_cast<uint2*>(a.codes[v])[out * kLanes + lane] = make_uint2(word[0], word[1]);
-      if (lane % 4 == 0)
-        a.words[v][out * (D / kGroup) + lane / 4] = static_cast<uint16_t>((__float_as_uint(scale) >> 16) | (__float_as_uint(zero) & 15u));
+                for (int i = 0; i < 4; ++i) turn_pair(x[8 * e + 2 * i], x[8 * e + 2 * i + 1], z[i]);
+              }
+            }
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const uint32_t d = i / 8 * (D / 2) + lane * 8 + i % 8;
+            x[i] = Elem<T>::to(in[d]);
+            if (d < turned) {
+              const bool second = by_half ? d >= tab.half : d & 1;
+              const uint32_t pair = by_half ? (second ? d - tab.half : d) : d / 2;
+              const float other = Elem<T>::to(in[by_half ? (second ? d - tab.half : d + tab.half) : d ^ 1]);
+              float2 z;
+              load_cs<1>(c, pair, &z);
+              x[i] = x[i] * z.x + other * (second ? z.y : -z.y);
+            }
+          }
+        }
+      }
+      // the extremes of the lane's groups: its two eights are of one (D = 64) or of two
+      constexpr int kOwn = D / 64;
+      float lo[2] = {0.f, 0.f}, hi[2] = {0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int gr = kOwn == 1 ? 0 : i / 8;
+        lo[gr] = min_nan(lo[gr], x[i]);
+        hi[gr] = max_nan(hi[gr], x[i]);
+      }
+#pragma unroll
+      for (int o = 1; o < static_cast<int>(kLanes); o <<= 1)
+#pragma unroll
+        for (int gr = 0; gr < kOwn; ++gr) {
+          lo[gr] = min_nan(lo[gr], __shfl_xor_sync(0xffffffffu, lo[gr], o));
+          hi[gr] = max_nan(hi[gr], __shfl_xor_sync(0xffffffffu, hi[gr], o));
+        }
+      // x / scale to the nearest, halves away from zero: the reciprocal (good to
+      // a last place) is taken two above its value, so that no half stays one,
+      // and the product and the zero point are summed and rounded once, to the
+      // last bit of 1.5 2^23. (No quotient of 16-bit x lies that close to a half
+      // without being one.)
+      uint32_t word[2], codes8[2];
+      float inv[2], zero[2];
+#pragma unroll
+      for (int gr = 0; gr < kOwn; ++gr) {
+        const float scale = group_scale(lo[gr], hi[gr]);
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv[gr]) : "f"(scale));
+        inv[gr] = scale > 0.f ? __uint_as_float(__float_as_uint(inv[gr]) + 2) : 0.f;
+        zero[gr] = fminf(__fmaf_rn(-lo[gr], inv[gr], 12582912.f), 12582927.f);
+        word[gr] = (__float_as_uint(scale) >> 16) | (__float_as_uint(zero[gr]) & 15u);
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        // codes are the low bits of 0x4B400000 + code, whose sum's share is taken off at the end
+        uint32_t w = 0;
+        const int gr = kOwn == 1 ? 0 : e;
+#pragma unroll
+        for (int i = 7; i >= 0; --i) w = w * 16 + __float_as_uint(fminf(__fmaf_rn(x[8 * e + i], inv[gr], zero[gr]), 12582927.f));
+        codes8[e] = w - 0x4B400000u * 0x11111111u;
+      }
+      if (p >= 0) {
+        // the row of the page's first head, to which the head's places were added above
+        const uint64_t page = static_cast<uint64_t>(p) >> r.batch.page_shift;
+        const uint64_t at = ((page * a.kv_heads) << r.batch.page_shift) + (static_cast<uint32_t>(p) & ((1u << r.batch.page_shift) - 1));
+        codes[at * (D / 8) + lane] = codes8[0];
+        codes[at * (D / 8) + kLanes + lane] = codes8[1];
+        if (lane == 0) {
+          if (kOwn == 2) reinterpret_cast<uint32_t*>(words)[at] = word[0] | word[1] << 16;
+          else words[at] = static_cast<uint16_t>(word[0]);
+        }
+      }
     }
   }
 }
@@ -201,7 +222,7 @@ cudaError_t launch_codes(CodesArgs a, const RotaryTable& tab, bool queries, cuda
   r.units = D / (2 * v);
   r.rotary_units = tab.half / v;
   r.offsets_in_smem = r.batch.offsets && r.batch.n_seqs <= kOffsetsInSmem;
-  r.tile = r.n_tokens >= sm_count() * 16 ? 8 : 1;
+  r.tile = r.n_tokens >= sm_count() * 32 ? 16 : r.n_tokens >= sm_count() * 8 ? 4 : 1;
   const uint32_t tiles = (r.n_tokens + r.tile - 1) / r.tile;
   const uint32_t parts = std::max(1u, std::min(2 * a.kv_heads, sm_count() * 4 / tiles));
   a.q_parts = queries ? std::max(1u, std::min(r.heads, sm_count() * 4 / tiles)) : 0;

@@ -73,17 +73,36 @@ __device__ __forceinline__ uint4 gather8(const T* p) {
 
 constexpr uint32_t kOffsetsInSmem = 1024;  // sequences whose offsets a CTA copies
 
-inline __host__ __device__ size_t rows_smem(uint32_t tile, uint32_t half, uint32_t n_seqs, bool offsets) {
-  return static_cast<size_t>(tile) * (half * sizeof(float2) + sizeof(int64_t)) + (offsets ? (n_seqs + 1) * sizeof(int32_t) : 0);
+// The CTA's angles: each token's pairs, as cos and sin, in units of two pairs
+// (16 bytes) whose order lets eight neighbouring lanes that read eight pairs
+// each meet every bank once.
+inline __host__ __device__ uint32_t cs_stride(uint32_t half) { return (half + 15) & ~15u; }
+__device__ __forceinline__ uint32_t cs_unit(uint32_t unit) { return unit ^ (unit >> 2 & 3u) ^ (unit >> 2 & 4u); }
+template <int N>
+__device__ __forceinline__ void load_cs(const float2* c, uint32_t pair, float2* to) {
+  if (N % 2 == 0) {
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+      const float4 x = reinterpret_cast<const float4*>(c)[cs_unit(pair / 2 + i / 2)];
+      to[i] = make_float2(x.x, x.y);
+      to[i + 1] = make_float2(x.z, x.w);
+    }
+  } else {
+    to[0] = c[cs_unit(pair / 2) * 2 + pair % 2];
+  }
 }
 
-// Fills the CTA's angles [tile][half] and places [tile]; ends with a barrier.
+inline __host__ __device__ size_t rows_smem(uint32_t tile, uint32_t half, uint32_t n_seqs, bool offsets) {
+  return static_cast<size_t>(tile) * (cs_stride(half) * sizeof(float2) + sizeof(int64_t)) + (offsets ? (n_seqs + 1) * sizeof(int32_t) : 0);
+}
+
+// Fills the CTA's angles and places [tile]; ends with a barrier.
 __device__ __forceinline__ void rows_set_up(const RowsArgs& a, const RotaryTable& tab, uint32_t t0, uint32_t n, float2* cs,
                                             int64_t* place, int32_t* offs) {
   for (uint32_t e = threadIdx.x; e < n * tab.half; e += blockDim.x) {
     const uint32_t t = e / tab.half, i = e - t * tab.half;
     const int32_t pos = a.positions[static_cast<uint64_t>(tab.axis[i]) * a.n_tokens + t0 + t];
-    cs[e] = rotary_cs(tab.turn[i], pos, tab.amplitude, a.transpose != 0);
+    cs[t * cs_stride(tab.half) + cs_unit(i / 2) * 2 + i % 2] = rotary_cs(tab.turn[i], pos, tab.amplitude, a.transpose != 0);
   }
   if (a.paged) {
     const int32_t* offsets = a.batch.offsets;
@@ -104,8 +123,10 @@ __device__ __forceinline__ void turn_pair(float& a, float& b, float2 cs) {
 }
 
 template <typename T, int V>
-__device__ __forceinline__ void turn_unit(RowVec<T, V>& a, RowVec<T, V>& b, const float2* cs, uint32_t layout) {
+__device__ __forceinline__ void turn_unit(RowVec<T, V>& a, RowVec<T, V>& b, const float2* c, uint32_t pair, uint32_t layout) {
   float x[V], y[V];
+  float2 cs[V];
+  load_cs<V>(c, pair, cs);
   a.to(x);
   b.to(y);
   if (layout == COFIE_ROTARY_HALF || V == 1) {
@@ -166,14 +187,14 @@ __device__ __forceinline__ void rows_run(const RowsArgs& a, const RotaryTable& t
         } else {
           to[i] = out + t * x.out_token + h * x.out_head;
         }
-        at[i] = t * tab.half + u * V;
+        at[i] = t;
         y[i].load(from + o1);
         z[i].load(from + o2);
       }
 #pragma unroll
       for (int i = 0; i < kAtOnce; ++i) {
         if (!to[i]) continue;
-        if (turns) turn_unit<T, V>(y[i], z[i], cs + at[i], tab.layout);
+        if (turns) turn_unit<T, V>(y[i], z[i], cs + at[i] * cs_stride(tab.half), u * V, tab.layout);
         y[i].store(to[i] + o1);
         z[i].store(to[i] + o2);
       }

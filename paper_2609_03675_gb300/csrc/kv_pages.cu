@@ -28,7 +28,7 @@ struct CodesArgs {
 // value is rotated with lies in as many pieces (sizes and strides that allow
 // it); else value by value.
 template <typename T, int V, int D, bool WIDE>
-__global__ void __launch_bounds__(kThreads) append_codes(const __grid_constant__ CodesArgs a, const __grid_constant__ RotaryTable tab) {
+__global__ void __launch_bounds__(kThreads, 4) append_codes(const __grid_constant__ CodesArgs a, const __grid_constant__ RotaryTable tab) {
   extern __shared__ __align__(16) float2 cs[];
   const RowsArgs& r = a.rows;
   int64_t* place = reinterpret_cast<int64_t*>(cs + r.tile * cs_stride(tab.half));
@@ -55,9 +55,20 @@ __global__ void __launch_bounds__(kThreads) append_codes(const __grid_constant__
     uint32_t* const codes = a.codes[v] + static_cast<uint64_t>(head << r.batch.page_shift) * (D / 8);
     uint16_t* const words = a.words[v] + static_cast<uint64_t>(head << r.batch.page_shift) * (D / kGroup);
     const uint32_t turned = v ? 0 : 2 * tab.half;  // values that are rotated
+    RowVec<T, 8> w[2], ahead[2];                   // the lane's values, and those of the next tokens
+    const auto fetch = [&](uint32_t t1, RowVec<T, 8>* to) {
+      const uint32_t t = t1 + mine;
+      if (!WIDE || t >= n) return;
+      to[0].load(in0 + t * in_token + lane * 8);
+      to[1].load(in0 + t * in_token + D / 2 + lane * 8);
+    };
+    fetch(0, ahead);
     for (uint32_t t1 = 0; t1 < n; t1 += 32 / kLanes) {  // whole warps stay in the loop, for the shuffles
       const uint32_t t = t1 + mine;
       const int64_t p = t < n ? place[t] : -1;
+      w[0] = ahead[0];
+      w[1] = ahead[1];
+      fetch(t1 + 32 / kLanes, ahead);
       float x[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) x[i] = 0.f;
@@ -65,9 +76,6 @@ __global__ void __launch_bounds__(kThreads) append_codes(const __grid_constant__
         const T* in = in0 + t * in_token;
         const float2* c = cs + t * cs_stride(tab.half);
         if (WIDE) {
-          RowVec<T, 8> w[2];
-          w[0].load(in + lane * 8);
-          w[1].load(in + D / 2 + lane * 8);
           w[0].to(x);
           w[1].to(x + 8);
           if (turned == D && by_half) {

@@ -30,7 +30,7 @@ constexpr int kThreads = 256;
 thread_local std::string g_rotary_error;
 
 template <typename T, int V>
-__global__ void __launch_bounds__(kThreads) rotate_rows(const __grid_constant__ RowsArgs a, const __grid_constant__ RotaryTable tab) {
+__global__ void __launch_bounds__(kThreads, 4) rotate_rows(const __grid_constant__ RowsArgs a, const __grid_constant__ RotaryTable tab) {
   extern __shared__ __align__(16) float2 cs[];
   int64_t* place = reinterpret_cast<int64_t*>(cs + a.tile * cs_stride(tab.half));
   int32_t* offs = reinterpret_cast<int32_t*>(place + a.tile);

@@ -15,6 +15,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import struct
 
 import torch
 
@@ -26,6 +27,7 @@ __all__ = ["KVCache", "Rotary"]
 _DTYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 _LAYOUTS = {"half": 0, "interleaved": 1}
 _SCALINGS = {"none": 0, "linear": 1, "base": 2, "yarn": 3}
+_get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
 
 
@@ -54,6 +56,13 @@ class _Batch(ctypes.Structure):
                 ("offsets", ctypes.c_void_p)]
 
 
+# The calls' structs, packed in one go into a buffer that the handle keeps (a
+# ctypes field costs the host more than a tensor's stride; a step of single
+# tokens is bound by the host).
+_ROWS = struct.Struct("=QQI4xqqqq")
+_BATCH = struct.Struct("=IIIIQQQ")
+assert _ROWS.size == ctypes.sizeof(_Rows) and _BATCH.size == ctypes.sizeof(_Batch)
+
 # Every symbol include/cofie_kv.h declares.
 EXPORTS = ("cofie_rotary_create", "cofie_rotary_destroy", "cofie_rotary_run", "cofie_rotary_last_error", "cofie_kv_create",
            "cofie_kv_destroy", "cofie_kv_append", "cofie_kv_read", "cofie_kv_attend", "cofie_kv_status", "cofie_kv_last_error")
@@ -70,13 +79,13 @@ def _load():
     for name, res, args in (
             ("cofie_rotary_create", ctypes.c_int, [P(_RotaryParams), P(vp)]),
             ("cofie_rotary_destroy", None, [vp]),
-            ("cofie_rotary_run", ctypes.c_int, [vp, P(_Rows), u32, u32, vp, u32, ctypes.c_int, vp]),
+            ("cofie_rotary_run", ctypes.c_int, [vp, vp, u32, u32, vp, u32, ctypes.c_int, vp]),
             ("cofie_rotary_last_error", ctypes.c_char_p, [vp]),
             ("cofie_kv_create", ctypes.c_int, [P(_KVParams), P(vp)]),
             ("cofie_kv_destroy", None, [vp]),
-            ("cofie_kv_append", ctypes.c_int, [vp, P(_Batch), P(_Rows), P(_Rows), P(_Rows), vp, vp, vp]),
-            ("cofie_kv_read", ctypes.c_int, [vp, P(_Batch), vp, vp, vp]),
-            ("cofie_kv_attend", ctypes.c_int, [vp, P(_Batch), P(_Rows), vp, vp, u64, ctypes.c_int, ctypes.c_float, vp]),
+            ("cofie_kv_append", ctypes.c_int, [vp, vp, vp, vp, vp, vp, vp, vp]),
+            ("cofie_kv_read", ctypes.c_int, [vp, vp, vp, vp, vp]),
+            ("cofie_kv_attend", ctypes.c_int, [vp, vp, vp, vp, vp, u64, ctypes.c_int, ctypes.c_float, vp]),
             ("cofie_kv_status", ctypes.c_int, [vp, vp]),
             ("cofie_kv_last_error", ctypes.c_char_p, [vp])):
         f = getattr(lib, name)
@@ -100,22 +109,22 @@ def _allocating(cuda_stream, index):
     return torch.cuda.stream(cuda_stream)
 
 
-def _heads(x, dtype, index, what):
-    """(data_ptr, tokens, heads, token stride, head stride) of a [tokens, heads, head_dim] tensor."""
-    if x.dtype != dtype or x.dim() != 3 or x.get_device() != index:
-        raise ValueError(f"{what} must be a {dtype} tensor [tokens, heads, head_dim] on cuda:{index}")
-    n, h, d = x.shape
-    t, s, one = x.stride()
-    if one != 1 and d > 1:
+def _heads(x, dtype, index, what, tokens, heads, head_dim):
+    """Refuses a tensor that is not [tokens, heads, head_dim] as the call wants it (None: any); its strides."""
+    shape = x.shape
+    if x.dtype is not dtype or x.get_device() != index or len(shape) != 3 or (tokens is not None and shape[0] != tokens) \
+            or (heads is not None and shape[1] != heads) or shape[2] != head_dim:
+        want = f"[{'tokens' if tokens is None else tokens}, {'heads' if heads is None else heads}, {head_dim}]"
+        raise ValueError(f"{what} must be a {dtype} tensor {want} on cuda:{index}")
+    st = x.stride()
+    if st[2] != 1:
         raise ValueError(f"{what}: a head's values must be contiguous")
-    return x.data_ptr(), n, h, t, s
+    return st
 
 
-def _int32(x, index, what, shape=None):
-    if x.dtype != torch.int32 or x.get_device() != index or not x.is_contiguous():
-        raise ValueError(f"{what} must be a contiguous int32 tensor on cuda:{index}")
-    if shape is not None and tuple(x.shape) != shape:
-        raise ValueError(f"{what} must have the shape {shape}")
+def _int32(x, index, what, shape):
+    if x.dtype is not torch.int32 or x.get_device() != index or not x.is_contiguous() or x.shape != shape:
+        raise ValueError(f"{what} must be a contiguous int32 tensor {list(shape)} on cuda:{index}")
     return x.data_ptr()
 
 
@@ -146,38 +155,44 @@ class Rotary:
         if rc != _abi.OK:
             raise NGFFError(rc, lib.cofie_rotary_last_error(None).decode())
         self._lib, self._h = lib, h
+        self._buf = ctypes.create_string_buffer(4 * _ROWS.size)
+        self._at = ctypes.addressof(self._buf)
 
     def _positions(self, positions, n, index):
-        shape = (n,) if positions.dim() == 1 and self.n_axes == 1 else (self.n_axes, n)
-        return _int32(positions, index, "positions", shape)
+        return _int32(positions, index, "positions", (n,) if self.n_axes == 1 and positions.dim() == 1 else (self.n_axes, n))
 
     def _run(self, x, positions, out, transpose, cuda_stream):
-        xs = (x,) if isinstance(x, torch.Tensor) else tuple(x)
-        if not 1 <= len(xs) <= 4:
+        xs = (x,) if isinstance(x, torch.Tensor) else x
+        k = len(xs)
+        if not 1 <= k <= 4:
             raise ValueError("one to four tensors of the same tokens")
-        index, dtype, n = xs[0].get_device(), xs[0].dtype, xs[0].shape[0]
-        if index < 0 or dtype not in _DTYPES:
+        first = xs[0]
+        index, dtype, n = first.get_device(), first.dtype, first.shape[0]
+        code = _DTYPES.get(dtype)
+        if index < 0 or code is None:
             raise ValueError("the tensors must be bfloat16, float16 or float32, on a CUDA device")
         if out is None:
             with _allocating(cuda_stream, index):
                 outs = tuple(torch.empty(y.shape, dtype=dtype, device=y.device) for y in xs)
         else:
-            outs = (out,) if isinstance(out, torch.Tensor) else tuple(out)
-        if len(outs) != len(xs):
-            raise ValueError("out has a tensor for each input")
-        rows = (_Rows * len(xs))()
-        for r, y, o in zip(rows, xs, outs):
-            if y.shape[0] != n or y.shape[-1] != self.head_dim or o.shape != y.shape:
-                raise ValueError(f"every tensor is [tokens, heads, {self.head_dim}], and its out as large")
-            r.src, _, r.heads, r.in_token, r.in_head = _heads(y, dtype, index, "x")
-            r.out, _, _, r.out_token, r.out_head = _heads(o, dtype, index, "out")
-        at = self._positions(positions, n, index)
-        with contextlib.nullcontext() if index == torch.cuda.current_device() else torch.cuda.device(index):
-            rc = self._lib.cofie_rotary_run(self._h, rows, len(xs), n, at, _DTYPES[dtype], transpose,
-                                            _stream_of(cuda_stream, index))
-        if rc != _abi.OK:
+            outs = (out,) if isinstance(out, torch.Tensor) else out
+            if len(outs) != k:
+                raise ValueError("out has a tensor for each input")
+        d, buf, at = self.head_dim, self._buf, 0
+        for y, o in zip(xs, outs):
+            a, b = _heads(y, dtype, index, "x", n, None, d), _heads(o, dtype, index, "out", n, y.shape[1], d)
+            _ROWS.pack_into(buf, at, y.data_ptr(), o.data_ptr(), y.shape[1], a[0], a[1], b[0], b[1])
+            at += 56
+        where = self._positions(positions, n, index)
+        stream = _raw_stream(index) if cuda_stream is None else _stream_of(cuda_stream, index)
+        if index == _get_device():
+            rc = self._lib.cofie_rotary_run(self._h, self._at, k, n, where, code, transpose, stream)
+        else:
+            with torch.cuda.device(index):
+                rc = self._lib.cofie_rotary_run(self._h, self._at, k, n, where, code, transpose, stream)
+        if rc:
             raise NGFFError(rc, self._lib.cofie_rotary_last_error(self._h).decode())
-        return outs[0] if isinstance(x, torch.Tensor) else outs
+        return outs[0] if xs is not x else outs
 
     def apply(self, x, positions, *, out=None, cuda_stream=None):
         """x (a tensor [tokens, heads, head_dim], or up to four of the same tokens) rotated; positions int32 [tokens], or
@@ -239,68 +254,70 @@ class KVCache:
         self._lib, self._h, self._index = lib, h, index
         self.n_pages, self.page_size, self.n_heads, self.n_kv_heads, self.head_dim = n_pages, page_size, n_heads, n_kv_heads, head_dim
         self.dtype, self.bits, self.rotary = dtype, bits, rotary
+        self._buf = ctypes.create_string_buffer(_BATCH.size + 3 * _ROWS.size)  # a batch, and up to three tensors' rows
+        self._at = ctypes.addressof(self._buf)
 
     def _check(self, rc):
-        if rc != _abi.OK:
+        if rc:
             raise NGFFError(rc, self._lib.cofie_kv_last_error(self._h).decode())
 
     def _batch(self, table, lengths, offsets, n, max_new):
         index = self._index
-        if table.dim() != 2 or table.dtype != torch.int32 or table.get_device() != index or table.stride(1) != 1 and table.shape[1] > 1:
-            raise ValueError(f"table must be an int32 tensor [sequences, pages] on cuda:{index} with contiguous rows")
-        seqs = table.shape[0]
-        if seqs > 1 and table.stride(0) != table.shape[1]:
-            raise ValueError("table must be contiguous")
-        return _Batch(seqs, n, max_new, table.shape[1], table.data_ptr(), _int32(lengths, index, "lengths", (seqs,)),
-                      None if offsets is None else _int32(offsets, index, "offsets", (seqs + 1,)))
+        if table.dtype is not torch.int32 or table.get_device() != index or table.dim() != 2 or not table.is_contiguous():
+            raise ValueError(f"table must be a contiguous int32 tensor [sequences, pages] on cuda:{index}")
+        seqs, width = table.shape
+        _BATCH.pack_into(self._buf, 0, seqs, n, max_new, width, table.data_ptr(), _int32(lengths, index, "lengths", (seqs,)),
+                         0 if offsets is None else _int32(offsets, index, "offsets", (seqs + 1,)))
 
-    def _rows(self, x, heads, what, n=None, out=None):
-        p, t, h, st, sh = _heads(x, self.dtype, self._index, what)
-        if h != heads or x.shape[2] != self.head_dim or n is not None and t != n:
-            raise ValueError(f"{what} must be [{'tokens' if n is None else n}, {heads}, {self.head_dim}]")
+    def _rows(self, i, x, heads, what, n=None, out=None):
+        """Packs tensor i of the call; returns where."""
+        a = _heads(x, self.dtype, self._index, what, n, heads, self.head_dim)
+        at = 40 + 56 * i
         if out is None:
-            return _Rows(p, None, h, st, sh, 0, 0)
-        if out.shape != x.shape:
-            raise ValueError(f"the output of {what} must have its shape")
-        po, _, _, ot, oh = _heads(out, self.dtype, self._index, "the output of " + what)
-        return _Rows(p, po, h, st, sh, ot, oh)
+            _ROWS.pack_into(self._buf, at, x.data_ptr(), 0, heads, a[0], a[1], 0, 0)
+        else:
+            b = _heads(out, self.dtype, self._index, "the output of " + what, x.shape[0], heads, self.head_dim)
+            _ROWS.pack_into(self._buf, at, x.data_ptr(), out.data_ptr(), heads, a[0], a[1], b[0], b[1])
+        return self._at + at
 
     def append(self, k, v, table, lengths, offsets=None, *, positions=None, q=None, q_out=None, cuda_stream=None):
         """Puts the batch's new keys (rotated, where the cache has a rotary) and values into their pages; lengths count them
         already. With q, its rotated copy is returned (in q_out, which may be q)."""
-        n = k.shape[0]
-        b = self._batch(table, lengths, offsets, n, 0)
-        kr, vr = self._rows(k, self.n_kv_heads, "k"), self._rows(v, self.n_kv_heads, "v", n)
-        if (self.rotary is None) != (positions is None):
+        n, rotary, index = k.shape[0], self.rotary, self._index
+        kr, vr = self._rows(0, k, self.n_kv_heads, "k"), self._rows(1, v, self.n_kv_heads, "v", n)
+        self._batch(table, lengths, offsets, n, 0)
+        if (rotary is None) != (positions is None):
             raise ValueError("positions go with a cache that has a rotary")
-        qr = None
+        qr = at = handle = None
+        if rotary is not None:
+            handle, at = rotary._h, rotary._positions(positions, n, index)
         if q is not None:
-            if self.rotary is None:
+            if rotary is None:
                 raise ValueError("q goes with a cache that has a rotary")
             if q_out is None:
-                with _allocating(cuda_stream, self._index):
+                with _allocating(cuda_stream, index):
                     q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-            qr = ctypes.byref(self._rows(q, self.n_heads, "q", n, q_out))
-        at = None if positions is None else self.rotary._positions(positions, n, self._index)
-        self._check(self._lib.cofie_kv_append(self._h, ctypes.byref(b), ctypes.byref(kr), ctypes.byref(vr), qr,
-                                              None if self.rotary is None else self.rotary._h, at,
-                                              _stream_of(cuda_stream, self._index)))
+            qr = self._rows(2, q, self.n_heads, "q", n, q_out)
+        stream = _raw_stream(index) if cuda_stream is None else _stream_of(cuda_stream, index)
+        self._check(self._lib.cofie_kv_append(self._h, self._at, kr, vr, qr, handle, at, stream))
         return q_out if q is not None else None
 
     def read(self, table, lengths, offsets=None, *, n_tokens=None, out=None, cuda_stream=None):
         """(keys, values) [tokens, kv heads, head_dim] as the cache holds them at the batch's new tokens. The count of
         tokens is that of ``out`` (a pair of tensors), n_tokens, or the sequences'."""
+        index = self._index
         if out is None:
             n = n_tokens if n_tokens is not None else table.shape[0]
-            with _allocating(cuda_stream, self._index):
+            with _allocating(cuda_stream, index):
                 out = tuple(torch.empty((n, self.n_kv_heads, self.head_dim), dtype=self.dtype, device=self.device) for _ in range(2))
         k, v = out
         n = k.shape[0]
         for x in (k, v):
-            if x.dtype != self.dtype or tuple(x.shape) != (n, self.n_kv_heads, self.head_dim) or not x.is_contiguous() or x.get_device() != self._index:
-                raise ValueError(f"out must be contiguous {self.dtype} [tokens, {self.n_kv_heads}, {self.head_dim}] on cuda:{self._index}")
-        b = self._batch(table, lengths, offsets, n, 0)
-        self._check(self._lib.cofie_kv_read(self._h, ctypes.byref(b), k.data_ptr(), v.data_ptr(), _stream_of(cuda_stream, self._index)))
+            if x.dtype is not self.dtype or x.shape != (n, self.n_kv_heads, self.head_dim) or not x.is_contiguous() or x.get_device() != index:
+                raise ValueError(f"out must be contiguous {self.dtype} [tokens, {self.n_kv_heads}, {self.head_dim}] on cuda:{index}")
+        self._batch(table, lengths, offsets, n, 0)
+        stream = _raw_stream(index) if cuda_stream is None else _stream_of(cuda_stream, index)
+        self._check(self._lib.cofie_kv_read(self._h, self._at, k.data_ptr(), v.data_ptr(), stream))
         return k, v
 
     def attend(self, q, table, lengths, offsets=None, *, max_new=0, mask=None, causal=True, scale=0.0, out=None, lse=None,
@@ -308,23 +325,23 @@ class KVCache:
         """(out, lse) of the batch's new queries over their sequences' cached tokens; out like q, lse fp32 [tokens, heads].
         max_new: at least the largest count of new tokens (the fewer, the better the kernel chosen). mask: uint8
         [sequences, >= the longest], nonzero where a cached token may be seen. scale 0: head_dim ** -0.5."""
-        n = q.shape[0]
+        n, index = q.shape[0], self._index
         if out is None or lse is None:
-            with _allocating(cuda_stream, self._index):
+            with _allocating(cuda_stream, index):
                 out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out
                 lse = torch.empty((n, self.n_heads), dtype=torch.float32, device=q.device) if lse is None else lse
-        b = self._batch(table, lengths, offsets, n, 1 if offsets is None else max_new)
-        r = self._rows(q, self.n_heads, "q", None, out)
-        if lse.dtype != torch.float32 or tuple(lse.shape) != (n, self.n_heads) or not lse.is_contiguous() or lse.get_device() != self._index:
-            raise ValueError(f"lse must be a contiguous float32 tensor [{n}, {self.n_heads}] on cuda:{self._index}")
+        r = self._rows(0, q, self.n_heads, "q", None, out)
+        self._batch(table, lengths, offsets, n, 1 if offsets is None else max_new)
+        if lse.dtype is not torch.float32 or lse.shape != (n, self.n_heads) or not lse.is_contiguous() or lse.get_device() != index:
+            raise ValueError(f"lse must be a contiguous float32 tensor [{n}, {self.n_heads}] on cuda:{index}")
         at, stride = None, 0
         if mask is not None:
             if mask.dtype not in (torch.uint8, torch.bool) or mask.dim() != 2 or mask.shape[0] != table.shape[0] or not mask.is_contiguous() \
-                    or mask.get_device() != self._index:
-                raise ValueError(f"mask must be a contiguous uint8 or bool tensor [{table.shape[0]}, tokens] on cuda:{self._index}")
+                    or mask.get_device() != index:
+                raise ValueError(f"mask must be a contiguous uint8 or bool tensor [{table.shape[0]}, tokens] on cuda:{index}")
             at, stride = mask.data_ptr(), mask.shape[1]
-        self._check(self._lib.cofie_kv_attend(self._h, ctypes.byref(b), ctypes.byref(r), lse.data_ptr(), at, stride, causal, scale,
-                                              _stream_of(cuda_stream, self._index)))
+        stream = _raw_stream(index) if cuda_stream is None else _stream_of(cuda_stream, index)
+        self._check(self._lib.cofie_kv_attend(self._h, self._at, r, lse.data_ptr(), at, stride, causal, scale, stream))
         return out, lse
 
     def status(self, cuda_stream=None):

@@ -71,9 +71,9 @@ def test_rotary_checks_its_rows_on_the_host(lib):
         for k, v in change.items():
             setattr(x, k, v)
         rows[0] = x
-        assert lib.cofie_rotary_run(r._h, *args[:4], args[4], 0, None) == _abi.EINVAL
+        assert lib.cofie_rotary_run(r._h, ctypes.addressof(rows), *args[1:4], args[4], 0, None) == _abi.EINVAL
         assert msg in lib.cofie_rotary_last_error(r._h), msg
-    assert lib.cofie_rotary_run(r._h, rows, 1, 0, None, 0, 0, None) == _abi.OK  # no tokens
+    assert lib.cofie_rotary_run(r._h, ctypes.addressof(rows), 1, 0, None, 0, 0, None) == _abi.OK  # no tokens
 
 
 @pytest.mark.parametrize("field,value,msg", [

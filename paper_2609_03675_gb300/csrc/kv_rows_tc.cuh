@@ -549,21 +549,32 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
         uint32_t pos;  // of the tile's first
         uint64_t row;  // in the pages; ~0 where there is nothing to see
       };
-      const auto look = [&](uint32_t j) {
-        Token x{0, ~0ull};
-        if (j >= tiles) return x;
-        const uint32_t unit = it.lo + j;
-        x.pos = (a.mask ? a.tiles[static_cast<uint64_t>(it.seq) * a.tile_stride + unit] : unit) * kTile;
+      // A token's row takes two loads one after the other where there is a mask (the tile's number, then the page and the
+      // mask): each is used a tile after it was asked for, so that nobody waits for it.
+      struct Page {
+        uint32_t pos, page, seen;
+      };
+      const auto unit_of = [&](uint32_t j) {
+        return j >= tiles ? ~0u : a.mask ? __ldg(&a.tiles[static_cast<uint64_t>(it.seq) * a.tile_stride + it.lo + j]) : it.lo + j;
+      };
+      const auto page_of = [&](uint32_t unit) {
+        Page x{unit == ~0u ? 0u : unit * kTile, 0, 0};
         const uint32_t pos = x.pos + tok;
-        if (pos >= it.span.length) return x;
-        if (a.mask && (pos >= a.mask_stride || !a.mask[it.seq * a.mask_stride + pos])) return x;
-        const uint32_t page = static_cast<uint32_t>(table[pos >> b.page_shift]);
-        if (page >= b.n_pages) {
-          atomicOr(b.err, kKvErrPage);
-          return x;
+        if (unit != ~0u && pos < it.span.length) {
+          x.page = static_cast<uint32_t>(__ldg(&table[pos >> b.page_shift]));
+          x.seen = !a.mask ? 1u : pos < a.mask_stride ? __ldg(&a.mask[it.seq * a.mask_stride + pos]) : 0u;
         }
-        x.row = page_row(b, (static_cast<int64_t>(page) << b.page_shift) | (pos & ((1u << b.page_shift) - 1)), it.head);
         return x;
+      };
+      const auto row_of = [&](const Page& x) {
+        Token y{x.pos, ~0ull};
+        if (x.seen) {
+          if (x.page < b.n_pages)
+            y.row = ((static_cast<uint64_t>(x.page) * b.kv_heads + it.head) << b.page_shift) + ((x.pos + tok) & ((1u << b.page_shift) - 1));
+          else
+            atomicOr(b.err, kKvErrPage);
+        }
+        return y;
       };
       const auto tell = [&](const Token& x, uint32_t i) {  // what the softmax has to know of tile i
         if (v || half) return;
@@ -594,7 +605,17 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
           }
           cp_async_commit();
         };
-        Token x[4] = {look(0), look(1), look(2), look(3)};
+        uint32_t unit[5];
+        Page page[4];
+        Token x[3];
+#pragma unroll
+        for (int i = 0; i < 5; ++i) unit[i] = unit_of(i);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) page[i] = page_of(unit[i]);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) x[i] = row_of(page[i]);
+        Page page_ahead = page[3];      // of tile j + 3
+        uint32_t unit_ahead = unit[4];  // of tile j + 4
         fetch(n, x[0]);
         fetch(n + 1, x[1]);
         fetch(n + 2, x[2]);
@@ -602,7 +623,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
         for (uint32_t j = 0; j < tiles; ++j, ++n) {
           const uint32_t st = n % kTcStages, round = n / kTcStages;
           tell(x[0], n);
-          const Token next = look(j + 4);
           cp_async_wait<kTcRaw - 1>();
           if (round > 0) ok = ok && tc_wait(&sm.empty[v][st], round - 1, stop);
           if (ok) {
@@ -622,20 +642,25 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
           }
           ok = __all_sync(0xffffffffu, ok);
           if (ok) warp_arrive(&sm.full[v][st]);
-          fetch(n + 3, x[3]);
-          x[0] = x[1], x[1] = x[2], x[2] = x[3], x[3] = next;
+          x[0] = x[1], x[1] = x[2], x[2] = row_of(page_ahead);
+          fetch(n + 3, x[2]);
+          page_ahead = page_of(unit_ahead);
+          unit_ahead = unit_of(j + 5);
         }
         cp_async_wait<0>();
       } else {
         // Copies of three tiles are on their way at a time.
         constexpr uint32_t kUnits = D / 8;  // 16-byte units of a token
         constexpr uint32_t kAhead = kTcStages - 1;
-        Token x = look(0);
+        uint32_t unit_ahead = unit_of(1);
+        Page page_ahead = page_of(unit_of(0));
 #pragma unroll 1
         for (uint32_t j = 0; j < tiles + kAhead - 1; ++j) {
           const uint32_t i = n + j, st = i % kTcStages, round = i / kTcStages;
           if (j < tiles) {
-            const Token next = look(j + 1);
+            const Token x = row_of(page_ahead);
+            page_ahead = page_of(unit_ahead);
+            unit_ahead = unit_of(j + 2);
             if (half == 0) sm.row_of[v][st][tok] = x.row;
             tell(x, i);
             if (v == 0) bar_sync<2, kTcProducers>();
@@ -651,7 +676,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
                 cp_async16(to + (u / 8) * S::kBlock + tk * 128 + ((u % 8) ^ (tk & 7)) * 16, pages + (live ? row * (D * 2) + u * 16 : 0), live);
               }
             }
-            x = next;
           }
           cp_async_commit();
           if (j + 1 >= kAhead) {  // the tile of two steps before is there

@@ -11,29 +11,48 @@ namespace {
 constexpr int kMaskThreads = 1024;
 
 // The tiles of 64 cached tokens of which the mask leaves one at least, in
-// order, a CTA to a sequence: a thread looks at a tile, a scan gives it its place.
+// order, a CTA to a sequence, 1024 tiles at a time: neighbouring lanes look at
+// a tile together (N bytes each, as the rows' alignment allows), then a thread
+// has a tile and a scan gives it its place.
+template <typename V>
+__device__ __forceinline__ bool any_set(const uint8_t* p) {
+  const V x = *reinterpret_cast<const V*>(p);
+  if constexpr (sizeof(V) == 16) return (x.x | x.y | x.z | x.w) != 0;
+  else return x != 0;
+}
+template <typename V>
 __global__ void __launch_bounds__(kMaskThreads) visible_tiles(const BatchArg b, const uint8_t* mask, uint64_t mask_stride, uint32_t* tiles,
                                                               uint32_t* count, uint32_t tile_stride) {
+  constexpr uint32_t kBytes = sizeof(V) > 1 ? sizeof(V) : 4, kLanes = kTile / kBytes;
   __shared__ uint32_t warps[kMaskThreads / 32];
+  __shared__ uint8_t flag[kMaskThreads];
   pdl_trigger();
   pdl_wait();
   const uint32_t seq = blockIdx.x, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   const uint64_t length = min(static_cast<uint64_t>(sequence_span(b, seq).length), mask_stride);
   const uint8_t* row = mask + seq * mask_stride;
-  const bool wide = reinterpret_cast<uintptr_t>(row) % 16 == 0;
   uint32_t n = 0;
-  for (uint32_t t0 = 0; t0 * static_cast<uint64_t>(kTile) < length; t0 += kMaskThreads) {
-    const uint64_t first = (t0 + threadIdx.x) * static_cast<uint64_t>(kTile), end = min(length, first + kTile);
-    bool some = false;
-    if (wide && first + kTile <= length) {
+  for (uint64_t t0 = 0; t0 * kTile < length; t0 += kMaskThreads) {
+    // whole warps stay in the loop, for the votes
+    const uint32_t here = static_cast<uint32_t>(min(static_cast<uint64_t>(kMaskThreads), (length + kTile - 1) / kTile - t0));
+#pragma unroll 4
+    for (uint32_t t1 = warp * (32 / kLanes); t1 < here; t1 += kMaskThreads / kLanes) {
+      const uint32_t t = t1 + lane / kLanes;
+      const uint64_t at = (t0 + t) * kTile + lane % kLanes * kBytes;
+      bool some = false;
+      if (t < here && at < length) {
+        if (sizeof(V) > 1 && at + kBytes <= length) {
+          some = any_set<V>(row + at);
+        } else {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint4 x = reinterpret_cast<const uint4*>(row + first)[i];
-        some |= (x.x | x.y | x.z | x.w) != 0;
+          for (uint32_t i = 0; i < kBytes; ++i) some |= at + i < length && row[at + i] != 0;
+        }
       }
-    } else {
-      for (uint64_t i = first; i < end; ++i) some |= row[i] != 0;
+      const uint32_t bits = __ballot_sync(0xffffffffu, some);
+      if (lane % kLanes == 0 && t < here) flag[t] = (bits >> lane & ((1u << kLanes) - 1)) != 0;
     }
+    __syncthreads();
+    const bool some = threadIdx.x < here && flag[threadIdx.x];
     const uint32_t bits = __ballot_sync(0xffffffffu, some);
     if (lane == 0) warps[warp] = __popc(bits);
     __syncthreads();
@@ -42,7 +61,8 @@ __global__ void __launch_bounds__(kMaskThreads) visible_tiles(const BatchArg b, 
       if (w < warp) before += warps[w];
       all += warps[w];
     }
-    if (some) tiles[static_cast<uint64_t>(seq) * tile_stride + before + __popc(bits & ((1u << lane) - 1))] = t0 + threadIdx.x;
+    if (some)
+      tiles[static_cast<uint64_t>(seq) * tile_stride + before + __popc(bits & ((1u << lane) - 1))] = static_cast<uint32_t>(t0) + threadIdx.x;
     n += all;
     __syncthreads();
   }
@@ -55,12 +75,12 @@ auto for_type(const cofie_kv_params& p, F f) {
   return f(__half());
 }
 
-// The kernel of the handle's type, head length and pages, for 8 << i rows.
+// The kernel of the handle's type, head length and pages, for 8 << i rows (i: 0 or 1).
 using SplitKernel = void (*)(AttendArgs);
 template <typename T, int D, int BITS>
 SplitKernel split_kernel(int i, size_t* smem) {
-  *smem = i == 0 ? split_smem<D, BITS, 1>() : i == 1 ? split_smem<D, BITS, 2>() : split_smem<D, BITS, 4>();
-  return i == 0 ? attend_split<T, D, BITS, 1> : i == 1 ? attend_split<T, D, BITS, 2> : attend_split<T, D, BITS, 4>;
+  *smem = i == 0 ? split_smem<D, BITS, 1>() : split_smem<D, BITS, 2>();
+  return i == 0 ? attend_split<T, D, BITS, 1> : attend_split<T, D, BITS, 2>;
 }
 SplitKernel split_kernel(const cofie_kv_params& p, int i, size_t* smem) {
   return for_type(p, [&](auto x) {
@@ -87,7 +107,7 @@ SplitKernel rows_kernel(const cofie_kv_params& p, size_t* smem) {
 cudaError_t attend_set_up(cofie_kv* h) {
   cudaError_t e = cudaSuccess;
   size_t rows = 0, ctas = 0;
-  for (int i = 0; i < 3 && e == cudaSuccess; ++i) {
+  for (int i = 0; i < 2 && e == cudaSuccess; ++i) {
     size_t smem = 0;
     const SplitKernel k = split_kernel(h->p, i, &smem);
     int per_sm = 0;
@@ -168,14 +188,21 @@ extern "C" int cofie_kv_attend(cofie_kv_t* h, const cofie_kv_batch* b, const cof
     }
     a.tiles = h->d_tiles;
     a.tile_count = h->d_tiles + static_cast<size_t>(b->n_seqs) * a.tile_stride;
-    if (const int rc = launched(h, launch_dependent(true, visible_tiles, dim3(b->n_seqs), dim3(kMaskThreads), 0, st, a.batch, mask, mask_stride,
+    const uintptr_t at = reinterpret_cast<uintptr_t>(mask) | (b->n_seqs > 1 ? mask_stride : 0);
+    const auto find = at % 16 == 0 ? visible_tiles<uint4> : at % 4 == 0 ? visible_tiles<uint32_t> : visible_tiles<uint8_t>;
+    if (const int rc = launched(h, launch_dependent(true, find, dim3(b->n_seqs), dim3(kMaskThreads), 0, st, a.batch, mask, mask_stride,
                                                     h->d_tiles, const_cast<uint32_t*>(a.tile_count), a.tile_stride),
                                 "attend"))
       return rc;
   }
   const uint64_t rows = static_cast<uint64_t>(b->offsets ? (b->max_new ? b->max_new : b->n_tokens) : 1) * a.group;
   size_t smem = 0;
-  if (rows > 16) {
+  // Up to 32 rows of a sequence and head, in blocks of 8 or 16, are left to the kernel that reads the cache for each
+  // block; more rows pay for tiles of 128 of them. Eight sequences of up to 60000 tokens, 32 heads over 8 of 128 (us,
+  // blocks / tiles): 20 rows 176 / 233 with 4 bits, 214 / 337 with 16; 32 rows 188 / 234, 262 / 339; 48 rows 266 / 234,
+  // 344 / 340. Up to 2000 tokens: 20 rows 25 / 28, 22 / 32; 48 rows 32 / 29, 27 / 34.
+  // What an item costs beside its tiles' slots: set-up, first loads, its part's joining.
+  if (rows > 32) {
     const SplitKernel k = rows_kernel(h->p, &smem);
     a.item_slots = 16;
     return launched(h, launch_dependent(true, k, dim3(sm_count()), dim3(kTcThreads), smem, st, a), "attend");

@@ -10,9 +10,9 @@ struct cofie_kv {
   int device = 0;
   uint32_t page_shift = 0;
   uint32_t* d_err = nullptr;
-  // attention: CTAs that fit the GPU at once for 8, 16 and 32 rows each, the
+  // attention: CTAs that fit the GPU at once for 8 and for 16 rows each, the
   // parts that they leave, and the tiles that a mask leaves (grown on demand)
-  uint32_t split_ctas[3] = {0, 0, 0};
+  uint32_t split_ctas[2] = {0, 0};
   float* d_part = nullptr;
   float2* d_part_ms = nullptr;
   uint32_t* d_done = nullptr;

@@ -299,6 +299,54 @@ def test_many_rows_over_a_long_cache(bits):
             _check_attend(cache, q, table, lengths, new, held, max_new=0)
 
 
+@pytest.mark.parametrize("h,kv,d", [(16, 8, 64), (16, 2, 128)])
+def test_row_blocks_of_one_and_of_two_tiles_in_turn(h, kv, d):
+    """Items whose second tile of 128 rows is empty between items where it is not, long enough that the roles of a CTA
+    run as far apart as they can; repeated, the same bits."""
+    G = h // kv
+    new, lengths = [300 // G, 100 // G, 600 // G, 40 // G + 5, 430 // G], [2500, 3000, 700, 2100, 5000]
+    g = torch.Generator().manual_seed(11)
+    table, n_pages = _table(lengths, 32, 1, g)
+    for bits in (16, 4):
+        cache = _cache(n_pages, 32, h, kv, d, torch.bfloat16, bits)
+        held = _fill(cache, table, lengths, g)
+        q = (2 * torch.randn((sum(new), h, d), generator=g)).to(torch.bfloat16).cuda()
+        _check_attend(cache, q, table, lengths, new, held)
+        lens, offsets = torch.tensor(lengths, dtype=torch.int32, device="cuda"), _offsets(new)
+        first = cache.attend(q, table, lens, offsets, max_new=max(new))
+        for _ in range(20):
+            again = cache.attend(q, table, lens, offsets, max_new=max(new))
+            assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+        cache.status()
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_pages_past_four_gigabytes(bits):
+    """Places whose byte offsets pass 32 bits: the last pages of a large pool, read, appended to and attended to."""
+    from paper_2609_03675_gb300 import Rotary
+    h, kv, d, page = 8, 4, 128, 64
+    each = kv * page * d * bits // 8
+    n_pages = (1 << 32) // each + 40
+    rotary = Rotary(d)
+    cache = _cache(n_pages, page, h, kv, d, torch.bfloat16, bits, rotary)
+    far = torch.arange(n_pages - 30, n_pages, dtype=torch.int32).view(2, 15).contiguous().cuda()
+    near = torch.arange(30, dtype=torch.int32).view(2, 15).contiguous().cuda()
+    g = torch.Generator(device="cuda").manual_seed(3)
+    for new in ([1, 1], [60, 45]):
+        lens = torch.tensor([900, 333], dtype=torch.int32, device="cuda")
+        x = torch.randn((1233, h + 2 * kv, d), generator=g, device="cuda").to(torch.bfloat16)
+        pos = torch.arange(1233, device="cuda", dtype=torch.int32)
+        whole = torch.tensor([0, 900, 1233], dtype=torch.int32, device="cuda")
+        got = []
+        for table in (far, near):
+            cache.append(x[:, h:h + kv], x[:, h + kv:], table, lens, whole, positions=pos)
+            q = x[:sum(new), :h].contiguous()
+            got.append((*cache.read(table, lens, whole, n_tokens=1233), *cache.attend(q, table, lens, _offsets(new), max_new=max(new))))
+        cache.status()
+        for a, b in zip(*got):
+            assert torch.equal(a, b)
+
+
 def test_large_scores_and_planted_keys():
     """Scores in the hundreds, rising along the sequence, so that the running maximum moves in every tile."""
     h, kv, d = 4, 2, 128

@@ -23,15 +23,14 @@
 // results. Everything else is on the side of the few rows:
 //   q      is brought to fp16 by a power of two for each row (its largest
 //          value in [128, 256)), which keeps bf16's and fp16's bits;
-//   keys   score = s (sum q n - z sum q), s one factor of a group's 64 terms;
-//          z sum q comes from one more product, whose operands are the zero
-//          points and sum q as three fp16 numbers;
+//   keys   a score is the sum over the groups of s sum q (n - z);
 //   values the sum over tokens has a scale for each: p s is rounded to fp16,
 //          after a power of two that keeps the largest scale met so far below
 //          2^15 (raised, and the output so far brought down, when a larger one
-//          comes). z is taken off the code, in fp16, exactly: taken off the
-//          sums, as the keys' is, it would cost half the operations, but a sum
-//          of values near zero would carry the rounding of sums of codes.
+//          comes).
+// z is taken off the codes, in fp16, exactly. Taken off the sums it would cost
+// half the operations, but sums near zero would carry the rounding of sums of
+// codes (log-sum-exps of few tokens were off by 3e-6 of their size, not 4e-7).
 // 262144 tokens, 8 heads of 128, 4 query heads each: unpacked to (n - z) s for
 // values and 128 + n for keys the kernel took 108 us, its ALU pipe 70 % busy.
 #pragma once
@@ -158,9 +157,8 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
     const uint32_t rows = min(static_cast<uint32_t>(kRows), it.span.count * a.group - row0);
     // ---- queries: fragments of Q^T, the columns of this lane's dims in the order in which the keys' lie in registers
     uint32_t qf[NT][D / 16][2];
-    uint32_t qz[BITS == 4 ? NT : 1];  // a part of -sum q over the two groups, for the zero points
-    float by[NT][2];                  // what takes the scores of rows 2c and 2c + 1 to base 2
-    int32_t seen[NT][2];              // tokens that they may see
+    float by[NT][2];      // what takes the scores of rows 2c and 2c + 1 to base 2
+    int32_t seen[NT][2];  // tokens that they may see
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const uint32_t r = nt * 8 + g;
@@ -194,17 +192,12 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
         }
         by[nt][0] = by[nt][1] = scale;
       } else {
-        float most = 0.f, sum[kGroups];
+        float most = 0.f;
 #pragma unroll
         for (int e = 0; e < D / 32; ++e) {
           const uint32_t w[4] = {x[e].x, x[e].y, x[e].z, x[e].w};
-          float s = 0.f;
 #pragma unroll
-          for (int f = 0; f < 4; ++f) {
-            most = fmaxf(most, fmaxf(fabsf(P::lo(w[f])), fabsf(P::hi(w[f]))));
-            s += P::lo(w[f]) + P::hi(w[f]);
-          }
-          sum[e / 2] = e % 2 ? sum[e / 2] + s : s;
+          for (int f = 0; f < 4; ++f) most = fmaxf(most, fmaxf(fabsf(P::lo(w[f])), fabsf(P::hi(w[f]))));
         }
         most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
         most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
@@ -219,22 +212,6 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
           qf[nt][2 * e + 1][0] = H::pack(P::lo(x[e].y) * up, P::lo(x[e].w) * up);
           qf[nt][2 * e + 1][1] = H::pack(P::hi(x[e].y) * odd, P::hi(x[e].w) * odd);
         }
-        // column slots 2c (first group) and 2c + 1 (second) of the zero points' product: a third of -sum q to each of
-        // three lanes
-        uint32_t parts[3] = {0, 0, 0};
-#pragma unroll
-        for (int gr = 0; gr < kGroups; ++gr) {
-          float s = -sum[gr] * up;
-          s += __shfl_xor_sync(0xffffffffu, s, 1);
-          s += __shfl_xor_sync(0xffffffffu, s, 2);
-#pragma unroll
-          for (int f = 0; f < 3; ++f) {
-            const __half p = __float2half_rn(s);
-            s -= __half2float(p);
-            parts[f] |= static_cast<uint32_t>(__half_as_ushort(p)) << (16 * gr);
-          }
-        }
-        qz[nt] = c == 0 ? parts[0] : c == 1 ? parts[1] : c == 2 ? parts[2] : 0u;
         const float back = scale * __uint_as_float(static_cast<uint32_t>(127 - 7 + ex) << 23) * 0x1p24f;
         by[nt][0] = __shfl_sync(0xffffffffu, back, 8 * c);
         by[nt][1] = __shfl_sync(0xffffffffu, back, 8 * c + 4);
@@ -386,16 +363,17 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
             const uint2 x = at<uint2>(base + unit_at<D, BITS, false>(t0, gr * 2 + c / 2) + (c % 2) * 8);
             const uint2 y = at<uint2>(base + unit_at<D, BITS, false>(t0 + 8, gr * 2 + c / 2) + (c % 2) * 8);
             float acc[NT][4];
-            const uint32_t only = gr == 0 ? 0x0000000Fu : 0x000F0000u;  // the group's zero point, in its slot
-            const uint32_t z[4] = {w0 & only, w1 & only, 0u, 0u};
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) mma_first(acc[nt], z, qz[nt], 0u);
+            const uint32_t z0 = __byte_perm(w0, w0, gr == 0 ? 0x1010 : 0x3232) & 0x000F000Fu, z1 = __byte_perm(w1, w1, gr == 0 ? 0x1010 : 0x3232) & 0x000F000Fu;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const uint32_t u = (e < 2 ? x.x : x.y) >> (8 * (e % 2)), v = (e < 2 ? y.x : y.y) >> (8 * (e % 2));
-              const uint32_t f[4] = {u & 0x000F000Fu, v & 0x000F000Fu, u & 0x00F000F0u, v & 0x00F000F0u};
+              const uint32_t f[4] = {H::sub(u & 0x000F000Fu, z0), H::sub(v & 0x000F000Fu, z1), H::sub(u & 0x00F000F0u, z0 * 16),
+                                     H::sub(v & 0x00F000F0u, z1 * 16)};
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt) H::mma(acc[nt], f, qf[nt][4 * gr + e][0], qf[nt][4 * gr + e][1]);
+              for (int nt = 0; nt < NT; ++nt) {
+                if (e == 0) mma_first(acc[nt], f, qf[nt][4 * gr][0], qf[nt][4 * gr][1]);
+                else H::mma(acc[nt], f, qf[nt][4 * gr + e][0], qf[nt][4 * gr + e][1]);
+              }
             }
             const float s0 = gr == 0 ? scale_lo(w0) : scale_hi(w0), s1 = gr == 0 ? scale_lo(w1) : scale_hi(w1);
 #pragma unroll

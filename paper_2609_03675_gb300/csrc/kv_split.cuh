@@ -155,6 +155,81 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
   while (walk.next(it)) {
     const uint32_t row0 = it.rb * kRows;
     const uint32_t rows = min(static_cast<uint32_t>(kRows), it.span.count * a.group - row0);
+    // ---- the warp's chunks: warp, warp + 8, ... of the item's part. A chunk's blocks of 16 tokens lie in one page each,
+    // one behind the other. The first are asked for before the queries are read.
+    const uint32_t chunks = (it.hi - it.lo) * kPerTile;
+    const int32_t* table = b.table + static_cast<uint64_t>(it.seq) * b.table_stride;
+    const uint8_t* mask = a.mask + it.seq * a.mask_stride;
+    struct Ahead {
+      uint32_t pos, page[kM];  // page: n_pages and above where there is none
+      bool seen;               // this lane's token
+    };
+    const auto look = [&](uint32_t ch) {
+      Ahead x;
+      x.pos = 0;
+      x.seen = false;
+#pragma unroll
+      for (int mt = 0; mt < kM; ++mt) x.page[mt] = ~0u;
+      if (ch < chunks) {
+        const uint32_t t = it.lo + ch / kPerTile;
+        x.pos = (a.mask ? a.tiles[static_cast<uint64_t>(it.seq) * a.tile_stride + t] : t) * kTile + (ch % kPerTile) * R::kTokens;
+#pragma unroll
+        for (int mt = 0; mt < kM; ++mt)
+          if (x.pos + 16 * mt < it.span.length) x.page[mt] = static_cast<uint32_t>(table[(x.pos + 16 * mt) >> b.page_shift]);
+        const uint32_t p = x.pos + lane % R::kTokens;
+        x.seen = p < it.span.length && (!a.mask || (p < a.mask_stride && mask[p] != 0));
+      }
+      return x;
+    };
+    const auto issue = [&](uint32_t stage, const Ahead& x) {
+      const uint32_t base = shared_address(ring + stage * R::kStage);
+      uint32_t bits = __ballot_sync(0xffffffffu, x.seen);
+      if (bits) {
+#pragma unroll
+        for (int mt = 0; mt < kM; ++mt) {
+          const uint32_t half = 0xFFFFu << (16 * mt);
+          if ((bits & half) && x.page[mt] >= b.n_pages) {
+            if (lane == 0) atomicOr(b.err, kKvErrPage);
+            bits &= BITS == 16 ? 0u : ~half;
+          }
+          const bool there = (bits & half) != 0;
+          if (BITS == 4 && !there) continue;  // what the ring holds there is masked below
+          const uint64_t row = there ? ((static_cast<uint64_t>(x.page[mt]) * b.kv_heads + it.head) << b.page_shift) +
+                                           ((x.pos + 16 * mt) & ((1u << b.page_shift) - 1))
+                                     : 0;
+          const char* k = a.k + row * R::kRow + lane * 16;
+          const char* v = a.v + row * R::kRow + lane * 16;
+#pragma unroll
+          for (int i = 0; i < R::kUnits / 2; ++i) {  // 32 units of 16 bytes
+            const uint32_t t = (i * 32 + lane) / R::kUnits, u = lane % R::kUnits;
+            // 16-bit values that nobody sees become zeros (a NaN among them would pass through a product with 0)
+            const bool live = BITS == 4 || ((bits >> t) & 1u);
+            cp_async16(base + unit_at<D, BITS, false>(16 * mt + t, u), k + i * 512, live);
+            cp_async16(base + R::kTokens * R::kRow + unit_at<D, BITS, true>(16 * mt + t, u), v + i * 512, live);
+          }
+          if (BITS == 4) {  // the block's words: D / 2 bytes of the keys', as many of the values'
+            constexpr uint32_t kLanes = D / 32;
+            static_assert(R::kWords / kM == 16 * kLanes || BITS == 16, "16 bytes to a lane");
+            if (lane < 2 * kLanes) {
+              const uint32_t v2 = lane / kLanes, u = lane % kLanes;
+              cp_async16(base + 2 * R::kTokens * R::kRow + v2 * R::kWords + mt * (R::kWords / kM) + u * 16,
+                         (v2 ? a.v_words : a.k_words) + row * (D / 64) + u * 8, true);
+            }
+          }
+        }
+      }
+      if (lane == 0) stages[warp][stage] = make_uint2(bits, x.pos);
+      cp_async_commit();
+    };
+    Ahead ahead;
+    {
+      Ahead first[R::kStages - 1];
+#pragma unroll
+      for (int s = 0; s < R::kStages - 1; ++s) first[s] = look(warp + s * kSplitWarps);
+      ahead = look(warp + (R::kStages - 1) * kSplitWarps);
+#pragma unroll
+      for (int s = 0; s < R::kStages - 1; ++s) issue(s, first[s]);
+    }
     // ---- queries: fragments of Q^T, the columns of this lane's dims in the order in which the keys' lie in registers
     uint32_t qf[NT][D / 16][2];
     float by[NT][2];      // what takes the scores of rows 2c and 2c + 1 to base 2
@@ -240,81 +315,6 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
       l[nt][0] = l[nt][1] = 0.f;
     }
 
-    // ---- the warp's chunks: warp, warp + 8, ... of the item's part. A chunk's blocks of 16 tokens lie in one page each,
-    // one behind the other.
-    const uint32_t chunks = (it.hi - it.lo) * kPerTile;
-    const int32_t* table = b.table + static_cast<uint64_t>(it.seq) * b.table_stride;
-    const uint8_t* mask = a.mask + it.seq * a.mask_stride;
-    struct Ahead {
-      uint32_t pos, page[kM];  // page: n_pages and above where there is none
-      bool seen;               // this lane's token
-    };
-    const auto look = [&](uint32_t ch) {
-      Ahead x;
-      x.pos = 0;
-      x.seen = false;
-#pragma unroll
-      for (int mt = 0; mt < kM; ++mt) x.page[mt] = ~0u;
-      if (ch < chunks) {
-        const uint32_t t = it.lo + ch / kPerTile;
-        x.pos = (a.mask ? a.tiles[static_cast<uint64_t>(it.seq) * a.tile_stride + t] : t) * kTile + (ch % kPerTile) * R::kTokens;
-#pragma unroll
-        for (int mt = 0; mt < kM; ++mt)
-          if (x.pos + 16 * mt < it.span.length) x.page[mt] = static_cast<uint32_t>(table[(x.pos + 16 * mt) >> b.page_shift]);
-        const uint32_t p = x.pos + lane % R::kTokens;
-        x.seen = p < it.span.length && (!a.mask || (p < a.mask_stride && mask[p] != 0));
-      }
-      return x;
-    };
-    const auto issue = [&](uint32_t stage, const Ahead& x) {
-      const uint32_t base = shared_address(ring + stage * R::kStage);
-      uint32_t bits = __ballot_sync(0xffffffffu, x.seen);
-      if (bits) {
-#pragma unroll
-        for (int mt = 0; mt < kM; ++mt) {
-          const uint32_t half = 0xFFFFu << (16 * mt);
-          if ((bits & half) && x.page[mt] >= b.n_pages) {
-            if (lane == 0) atomicOr(b.err, kKvErrPage);
-            bits &= BITS == 16 ? 0u : ~half;
-          }
-          const bool there = (bits & half) != 0;
-          if (BITS == 4 && !there) continue;  // what the ring holds there is masked below
-          const uint64_t row = there ? ((static_cast<uint64_t>(x.page[mt]) * b.kv_heads + it.head) << b.page_shift) +
-                                           ((x.pos + 16 * mt) & ((1u << b.page_shift) - 1))
-                                     : 0;
-          const char* k = a.k + row * R::kRow + lane * 16;
-          const char* v = a.v + row * R::kRow + lane * 16;
-#pragma unroll
-          for (int i = 0; i < R::kUnits / 2; ++i) {  // 32 units of 16 bytes
-            const uint32_t t = (i * 32 + lane) / R::kUnits, u = lane % R::kUnits;
-            // 16-bit values that nobody sees become zeros (a NaN among them would pass through a product with 0)
-            const bool live = BITS == 4 || ((bits >> t) & 1u);
-            cp_async16(base + unit_at<D, BITS, false>(16 * mt + t, u), k + i * 512, live);
-            cp_async16(base + R::kTokens * R::kRow + unit_at<D, BITS, true>(16 * mt + t, u), v + i * 512, live);
-          }
-          if (BITS == 4) {  // the block's words: D / 2 bytes of the keys', as many of the values'
-            constexpr uint32_t kLanes = D / 32;
-            static_assert(R::kWords / kM == 16 * kLanes || BITS == 16, "16 bytes to a lane");
-            if (lane < 2 * kLanes) {
-              const uint32_t v2 = lane / kLanes, u = lane % kLanes;
-              cp_async16(base + 2 * R::kTokens * R::kRow + v2 * R::kWords + mt * (R::kWords / kM) + u * 16,
-                         (v2 ? a.v_words : a.k_words) + row * (D / 64) + u * 8, true);
-            }
-          }
-        }
-      }
-      if (lane == 0) stages[warp][stage] = make_uint2(bits, x.pos);
-      cp_async_commit();
-    };
-    Ahead ahead;
-    {
-      Ahead first[R::kStages - 1];
-#pragma unroll
-      for (int s = 0; s < R::kStages - 1; ++s) first[s] = look(warp + s * kSplitWarps);
-      ahead = look(warp + (R::kStages - 1) * kSplitWarps);
-#pragma unroll
-      for (int s = 0; s < R::kStages - 1; ++s) issue(s, first[s]);
-    }
     uint32_t stage = 0;
     for (uint32_t ch = warp; ch < chunks; ch += kSplitWarps) {
       cp_async_wait<R::kStages - 2>();
@@ -652,7 +652,7 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
           const uint32_t n = min(kJoin, parts - p0);
           __syncthreads();
           for (uint32_t x = threadIdx.x; x < n * kRows; x += kSplitThreads) {
-            const float2 z = __ldcg(&a.part_ms[part_at(p0 + x / kRows, x % kRows)]);
+            const float2 z = parts <= kJoin ? ms[x] : __ldcg(&a.part_ms[part_at(p0 + x / kRows, x % kRows)]);
             const float k = z.x == -INFINITY ? (z.y == 0.f ? 0.f : 1.f) : exp2_fast(z.x - warp_m[0][x % kRows]);
             ms[x] = make_float2(k, z.y == 0.f ? 0.f : k * z.y);
           }

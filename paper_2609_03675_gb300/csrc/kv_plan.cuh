@@ -73,6 +73,21 @@ struct Item {
   uint32_t first_cta, last_cta;
 };
 
+// Called by one thread when the CTA has written its part of an item and a
+// barrier has brought the writes of the others before this: counts the part,
+// and says whether it was the last. Its fences are the CTA's: what its threads
+// wrote is visible before the count, and, after the barrier that follows, what
+// the other CTAs wrote is visible to all of them.
+__device__ __forceinline__ uint32_t part_done(const AttendArgs& a, const Item& it) {
+  __threadfence();
+  const uint32_t last = atomicAdd(a.done + it.first_cta, 1u) == it.last_cta - it.first_cta;
+  if (last) {
+    a.done[it.first_cta] = 0;
+    __threadfence();
+  }
+  return last;
+}
+
 constexpr uint32_t kSpans = 256;  // sequences that are looked up once and kept in shared memory
 
 // Walks the items of one CTA's range. THREADS threads share the sequences.

@@ -449,16 +449,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
       }
       tc_fence_before();  // O is read before the next item's products are let through (by q_full)
       if (!alone) {
-        __threadfence();
         bar_sync<1, kTcSoftmax>();
         const uint32_t parts = it.last_cta - it.first_cta + 1;
-        if (threadIdx.x == 0) {
-          sm.last_here = atomicAdd(a.done + it.first_cta, 1u) == parts - 1;
-          if (sm.last_here) a.done[it.first_cta] = 0;
-        }
+        if (threadIdx.x == 0) sm.last_here = part_done(a, it);
         bar_sync<1, kTcSoftmax>();
         if (sm.last_here) {
-          __threadfence();
           const auto part_at = [&](uint32_t i, uint32_t row) { return (2ull * (it.first_cta + i) + (i == 0)) * kTcRows + row; };
           float top = -INFINITY, sum = 0.f;
           if (real) {

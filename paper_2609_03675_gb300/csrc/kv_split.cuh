@@ -619,16 +619,10 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
       }
     }
     if (!alone) {
-      __threadfence();
       __syncthreads();
-      if (threadIdx.x == 0) {
-        const uint32_t parts = it.last_cta - it.first_cta + 1;
-        last_here = atomicAdd(a.done + it.first_cta, 1u) == parts - 1;
-        if (last_here) a.done[it.first_cta] = 0;
-      }
+      if (threadIdx.x == 0) last_here = part_done(a, it);
       __syncthreads();
       if (last_here) {
-        __threadfence();
         // each part's factor for each row, kJoin parts at a time; the maximum over all parts first
         const uint32_t parts = it.last_cta - it.first_cta + 1;
         const auto part_at = [&](uint32_t i, uint32_t r) { return (2ull * (it.first_cta + i) + (i == 0)) * kRows + r; };

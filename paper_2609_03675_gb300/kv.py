@@ -109,13 +109,10 @@ def _allocating(cuda_stream, index):
     return torch.cuda.stream(cuda_stream)
 
 
-def _heads(x, dtype, index, what, tokens, heads, head_dim):
-    """Refuses a tensor that is not [tokens, heads, head_dim] as the call wants it (None: any); its strides."""
-    shape = x.shape
-    if x.dtype is not dtype or x.get_device() != index or len(shape) != 3 or (tokens is not None and shape[0] != tokens) \
-            or (heads is not None and shape[1] != heads) or shape[2] != head_dim:
-        want = f"[{'tokens' if tokens is None else tokens}, {'heads' if heads is None else heads}, {head_dim}]"
-        raise ValueError(f"{what} must be a {dtype} tensor {want} on cuda:{index}")
+def _heads(x, dtype, index, what, shape):
+    """Refuses a tensor that is not of this shape, [tokens, heads, head_dim], as the call wants it; its strides."""
+    if x.shape != shape or x.dtype is not dtype or x.get_device() != index:
+        raise ValueError(f"{what} must be a {dtype} tensor {list(shape)} on cuda:{index}")
     st = x.stride()
     if st[2] != 1:
         raise ValueError(f"{what}: a head's values must be contiguous")
@@ -154,7 +151,7 @@ class Rotary:
         rc = lib.cofie_rotary_create(ctypes.byref(p), ctypes.byref(h))
         if rc != _abi.OK:
             raise NGFFError(rc, lib.cofie_rotary_last_error(None).decode())
-        self._lib, self._h = lib, h
+        self._lib, self._h = lib, h.value  # an integer: quicker to pass
         self._buf = ctypes.create_string_buffer(4 * _ROWS.size)
         self._at = ctypes.addressof(self._buf)
 
@@ -180,8 +177,9 @@ class Rotary:
                 raise ValueError("out has a tensor for each input")
         d, buf, at = self.head_dim, self._buf, 0
         for y, o in zip(xs, outs):
-            a, b = _heads(y, dtype, index, "x", n, None, d), _heads(o, dtype, index, "out", n, y.shape[1], d)
-            _ROWS.pack_into(buf, at, y.data_ptr(), o.data_ptr(), y.shape[1], a[0], a[1], b[0], b[1])
+            shape = (n, y.shape[1], d) if y.dim() == 3 else (n, 1, d)
+            a, b = _heads(y, dtype, index, "x", shape), _heads(o, dtype, index, "out", shape)
+            _ROWS.pack_into(buf, at, y.data_ptr(), o.data_ptr(), shape[1], a[0], a[1], b[0], b[1])
             at += 56
         where = self._positions(positions, n, index)
         stream = _raw_stream(index) if cuda_stream is None else _stream_of(cuda_stream, index)
@@ -251,7 +249,7 @@ class KVCache:
         rc = lib.cofie_kv_create(ctypes.byref(p), ctypes.byref(h))
         if rc != _abi.OK:
             raise NGFFError(rc, lib.cofie_kv_last_error(None).decode())
-        self._lib, self._h, self._index = lib, h, index
+        self._lib, self._h, self._index = lib, h.value, index
         self.n_pages, self.page_size, self.n_heads, self.n_kv_heads, self.head_dim = n_pages, page_size, n_heads, n_kv_heads, head_dim
         self.dtype, self.bits, self.rotary = dtype, bits, rotary
         self._buf = ctypes.create_string_buffer(_BATCH.size + 3 * _ROWS.size)  # a batch, and up to three tensors' rows
@@ -271,12 +269,13 @@ class KVCache:
 
     def _rows(self, i, x, heads, what, n=None, out=None):
         """Packs tensor i of the call; returns where."""
-        a = _heads(x, self.dtype, self._index, what, n, heads, self.head_dim)
+        shape = (x.shape[0] if n is None else n, heads, self.head_dim)
+        a = _heads(x, self.dtype, self._index, what, shape)
         at = 40 + 56 * i
         if out is None:
             _ROWS.pack_into(self._buf, at, x.data_ptr(), 0, heads, a[0], a[1], 0, 0)
         else:
-            b = _heads(out, self.dtype, self._index, "the output of " + what, x.shape[0], heads, self.head_dim)
+            b = _heads(out, self.dtype, self._index, "out", shape)
             _ROWS.pack_into(self._buf, at, x.data_ptr(), out.data_ptr(), heads, a[0], a[1], b[0], b[1])
         return self._at + at
 

@@ -187,35 +187,41 @@ struct ReadArgs {
 
 constexpr uint32_t kReadTile = 16;  // tokens of a CTA
 
-// Eight values of a (token, key or value, head) row to a thread.
+// A warp takes the keys or the values of a head, some tokens at a time, eight
+// values of a row to a lane.
 template <typename T, int D, int BITS>
-__global__ void __launch_bounds__(kThreads) read_pages(const ReadArgs a) {
-  constexpr uint32_t kLanes = D / 8;
+__global__ void __launch_bounds__(kThreads) read_pages(const __grid_constant__ ReadArgs a) {
+  constexpr uint32_t kLanes = D / 8, kStep = 32 / kLanes;
   __shared__ int64_t place[kReadTile];
   pdl_trigger();
   pdl_wait();
   const uint32_t t0 = blockIdx.x * kReadTile, n = min(kReadTile, a.batch.n_tokens - t0);
   if (threadIdx.x < n) place[threadIdx.x] = place_of(a.batch, a.batch.offsets, t0 + threadIdx.x);
   __syncthreads();
-  const uint32_t lane = threadIdx.x % kLanes, kinds = 2 * a.batch.kv_heads;
+  const uint32_t lane = threadIdx.x % kLanes, mine = threadIdx.x % 32 / kLanes, kv = a.batch.kv_heads, shift = a.batch.page_shift;
+  for (uint32_t kind = blockIdx.y * (kThreads / 32) + threadIdx.x / 32; kind < 2 * kv; kind += gridDim.y * (kThreads / 32)) {
+    const uint32_t v = kind >= kv, head = kind - v * kv;
+    // from the head's place in a page
+    const char* const pages = a.pages[v] + static_cast<uint64_t>(head << shift) * (D * BITS / 8) + lane * BITS;
+    const uint16_t* const words = a.words[v] + static_cast<uint64_t>(head << shift) * (D / kGroup) + lane / 8;
+    uint4* const out = a.out[v] + (static_cast<uint64_t>(t0) * kv + head) * kLanes + lane;
 #pragma unroll 4
-  for (uint32_t row = threadIdx.x / kLanes; row < n * kinds; row += kThreads / kLanes) {
-    const uint32_t t = row / kinds, kind = row - t * kinds;
-    const uint32_t v = kind >= a.batch.kv_heads, head = kind - v * a.batch.kv_heads;
-    const int64_t p = place[t];
-    uint4 val = make_uint4(0, 0, 0, 0);
-    if (p >= 0) {
-      const uint64_t at = page_row(a.batch, p, head);
-      if (BITS == 16) {
-        val = reinterpret_cast<const uint4*>(a.pages[v])[at * kLanes + lane];
-      } else {
-        const Unpack<T> u(a.words[v][at * (D / kGroup) + lane / 8]);
-        const uint4 y = u(reinterpret_cast<const uint32_t*>(a.pages[v])[at * kLanes + lane]);  // (0, 4), (1, 5), (2, 6), (3, 7)
-        val = make_uint4(__byte_perm(y.x, y.y, 0x5410), __byte_perm(y.z, y.w, 0x5410), __byte_perm(y.x, y.y, 0x7632),
-                         __byte_perm(y.z, y.w, 0x7632));
+    for (uint32_t t = mine; t < n; t += kStep) {
+      const int64_t p = place[t];
+      uint4 val = make_uint4(0, 0, 0, 0);
+      if (p >= 0) {
+        const uint64_t at = ((static_cast<uint64_t>(p) >> shift) * kv << shift) + (static_cast<uint32_t>(p) & ((1u << shift) - 1));
+        if (BITS == 16) {
+          val = *reinterpret_cast<const uint4*>(pages + at * (D * 2));
+        } else {
+          const Unpack<T> u(words[at * (D / kGroup)]);
+          const uint4 y = u(*reinterpret_cast<const uint32_t*>(pages + at * (D / 2)));  // (0, 4), (1, 5), (2, 6), (3, 7)
+          val = make_uint4(__byte_perm(y.x, y.y, 0x5410), __byte_perm(y.z, y.w, 0x5410), __byte_perm(y.x, y.y, 0x7632),
+                           __byte_perm(y.z, y.w, 0x7632));
+        }
       }
+      out[static_cast<uint64_t>(t) * kv * kLanes] = val;
     }
-    a.out[v][(static_cast<uint64_t>(t0 + t) * a.batch.kv_heads + head) * kLanes + lane] = val;
   }
 }
 
@@ -243,7 +249,8 @@ cudaError_t launch_codes(CodesArgs a, const RotaryTable& tab, bool queries, cuda
 
 template <typename T, int D>
 cudaError_t launch_read(const ReadArgs& a, uint32_t bits, cudaStream_t st) {
-  const dim3 grid((a.batch.n_tokens + kReadTile - 1) / kReadTile);
+  const uint32_t tiles = (a.batch.n_tokens + kReadTile - 1) / kReadTile, most = (2 * a.batch.kv_heads + kThreads / 32 - 1) / (kThreads / 32);
+  const dim3 grid(tiles, std::max(1u, std::min(most, sm_count() * 4 / tiles)));
   return bits == 4 ? launch_dependent(true, read_pages<T, D, 4>, grid, dim3(kThreads), 0, st, a)
                    : launch_dependent(true, read_pages<T, D, 16>, grid, dim3(kThreads), 0, st, a);
 }

@@ -51,7 +51,8 @@ cudaError_t launch_rows(RowsArgs a, const RotaryTable& tab, uint32_t head_dim, u
   a.units = head_dim / (2 * v);
   a.rotary_units = tab.half / v;
   a.offsets_in_smem = a.paged && a.batch.offsets && a.batch.n_seqs <= kOffsetsInSmem;
-  a.tile = a.n_tokens >= sm_count() * 16 ? 8 : 1;
+  // few tokens to a CTA where there would be few waves of CTAs, many where their set-up counts
+  a.tile = a.n_tokens >= sm_count() * 256 ? 8 : a.n_tokens >= sm_count() * 16 ? 4 : 1;
   const uint32_t tiles = (a.n_tokens + a.tile - 1) / a.tile;
   const uint32_t parts = std::max(1u, std::min(a.heads, sm_count() * 4 / tiles));
   const dim3 grid(tiles, parts);

@@ -30,7 +30,7 @@
  *   s = (hi - lo) / 15 rounded up to 4 significant bits (0 below 2^-100),
  *   z = min(15, [-lo / s]), n = min(15, max(0, [x / s] + z)), [] to the
  *   nearest, halves away from zero. A group that holds a NaN or an infinity,
- *   or whose s would pass bf16's range, reads as NaN.
+ *   or whose hi - lo passes fp32's range, reads as NaN.
  */
 #ifndef COFIE_KV_H
 #define COFIE_KV_H
@@ -171,7 +171,8 @@ int cofie_kv_read(cofie_kv_t* h, const cofie_kv_batch* b, void* k_out, void* v_o
  *   out = sum_j p_j v_j, p = softmax_j(scale <q, k_j>), lse = ln sum_j exp(scale <q, k_j>)
  * in fp32, out rounded once to the cache's type. A row that sees nothing gets
  * out = 0, lse = -infinity; what a masked or unwritten place holds (NaN too)
- * never matters.
+ * never matters. (A NaN or an infinity among a call's own new values may reach
+ * all new rows of its sequence, those before it too.)
  *   q     n_heads rows a token; `out` is the output.
  *   lse   NULL, or fp32 [n_tokens][n_heads], device memory.
  *   mask  NULL, or uint8 [n_seqs][mask_stride], device memory, mask_stride >= the longest sequence

@@ -201,14 +201,15 @@ extern "C" int cofie_kv_attend(cofie_kv_t* h, const cofie_kv_batch* b, const cof
   // block; more rows pay for tiles of 128 of them. Eight sequences of up to 60000 tokens, 32 heads over 8 of 128 (us,
   // blocks / tiles): 20 rows 176 / 233 with 4 bits, 214 / 337 with 16; 32 rows 188 / 234, 262 / 339; 48 rows 266 / 234,
   // 344 / 340. Up to 2000 tokens: 20 rows 25 / 28, 22 / 32; 48 rows 32 / 29, 27 / 34.
-  // What an item costs beside its tiles' slots: set-up, first loads, its part's joining.
+  // What an item costs beside its tiles' slots (set-up, first loads, its part's joining): with 6, 16 and 24 of them for
+  // many rows seven ragged questions took 98, 107 and 116 us; with 2, 4 and 6 for few, 24 streams' evidence 72, 67 and 63.
   if (rows > 32) {
     const SplitKernel k = rows_kernel(h->p, &smem);
-    a.item_slots = 16;
+    a.item_slots = 8;
     return launched(h, launch_dependent(true, k, dim3(sm_count()), dim3(kTcThreads), smem, st, a), "attend");
   }
   const int i = rows <= 8 ? 0 : 1;
-  a.item_slots = 4;
+  a.item_slots = 6;
   const SplitKernel k = split_kernel(h->p, i, &smem);
   return launched(h, launch_dependent(true, k, dim3(h->split_ctas[i]), dim3(kSplitThreads), smem, st, a), "attend");
 }

@@ -114,7 +114,7 @@ struct Ring {
   static constexpr int kRow = D * BITS / 8;                               // bytes of a token's keys
   static constexpr int kWords = BITS == 4 ? kTokens * (D / 64) * 2 : 0;   // bytes of its chunk's scale words
   static constexpr int kStage = 2 * (kTokens * kRow + kWords);
-  static constexpr int kStages = BITS == 4 ? 3 : 3;
+  static constexpr int kStages = 3;
   static constexpr int kWarp = kStages * kStage;
   static constexpr int kUnits = kRow / 16;                                // 16-byte units of a token
 };

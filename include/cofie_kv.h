@@ -179,7 +179,8 @@ int cofie_kv_read(cofie_kv_t* h, const cofie_kv_batch* b, void* k_out, void* v_o
  *         (a cached token past mask_stride counts as masked).
  *   scale 0: 1 / sqrt(head_dim).
  * May be captured, except for the first masked call of a larger n_seqs x
- * table_stride, which grows the handle's scratch.
+ * table_stride, which grows the handle's scratch. Calls captured before it are
+ * launched as before (what they use stays until cofie_kv_destroy).
  */
 int cofie_kv_attend(cofie_kv_t* h, const cofie_kv_batch* b, const cofie_rows* q, float* lse, const uint8_t* mask,
                     uint64_t mask_stride, int causal, float scale, void* cuda_stream);

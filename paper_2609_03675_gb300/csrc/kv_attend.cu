@@ -169,8 +169,9 @@ extern "C" int cofie_kv_attend(cofie_kv_t* h, const cofie_kv_batch* b, const cof
   a.done = h->d_done;
   if (mask) {
     a.tile_stride = (b->table_stride << h->page_shift) / kTile + 1;
-    const size_t room = static_cast<size_t>(b->n_seqs) * (a.tile_stride + 1);
-    if (room > h->tiles_room) {
+    const size_t need = static_cast<size_t>(b->n_seqs) * (a.tile_stride + 1);
+    if (need > h->tiles_room) {
+      const size_t room = std::max(need, 2 * h->tiles_room);
       cudaStreamCaptureStatus cs = cudaStreamCaptureStatusNone;
       if (cudaStreamIsCapturing(st, &cs) != cudaSuccess || cs != cudaStreamCaptureStatusNone) {
         cudaGetLastError();
@@ -182,7 +183,7 @@ extern "C" int cofie_kv_attend(cofie_kv_t* h, const cofie_kv_batch* b, const cof
         cudaGetLastError();
         return h->fail(e == cudaErrorMemoryAllocation ? COFIE_ENOMEM : COFIE_ECUDA, "no room for the list of the mask's tiles");
       }
-      cudaFree(h->d_tiles);  // waits for the calls that read it
+      if (h->d_tiles) h->d_tiles_before[h->n_tiles_before++] = h->d_tiles;  // graphs may have it
       h->d_tiles = more;
       h->tiles_room = room;
     }

@@ -11,13 +11,17 @@ struct cofie_kv {
   uint32_t page_shift = 0;
   uint32_t* d_err = nullptr;
   // attention: CTAs that fit the GPU at once for 8 and for 16 rows each, the
-  // parts that they leave, and the tiles that a mask leaves (grown on demand)
+  // parts that they leave, and the tiles that a mask leaves. That list grows on
+  // demand, to twice its size at least; those before it stay with the handle,
+  // because a captured call keeps the address that it was captured with.
   uint32_t split_ctas[2] = {0, 0};
   float* d_part = nullptr;
   float2* d_part_ms = nullptr;
   uint32_t* d_done = nullptr;
   uint32_t* d_tiles = nullptr;
   size_t tiles_room = 0;
+  uint32_t* d_tiles_before[64] = {};  // doublings that a size_t allows
+  uint32_t n_tiles_before = 0;
   std::string err;
   int fail(int code, const std::string& m) {
     err = m;

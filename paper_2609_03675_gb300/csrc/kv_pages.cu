@@ -271,6 +271,7 @@ void kv_free(cofie_kv* h) {
   for (void* x : {static_cast<void*>(h->d_err), static_cast<void*>(h->d_part), static_cast<void*>(h->d_part_ms), static_cast<void*>(h->d_done),
                   static_cast<void*>(h->d_tiles)})
     if (x) cudaFree(x);
+  for (uint32_t i = 0; i < h->n_tiles_before; ++i) cudaFree(h->d_tiles_before[i]);
   delete h;
 }
 

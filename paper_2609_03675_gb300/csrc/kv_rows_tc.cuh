@@ -286,7 +286,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
         const int64_t x = a.causal ? static_cast<int64_t>(it.span.length) - it.span.count + token + 1 : it.span.length;
         seen = x > 0 ? static_cast<int32_t>(x) : 0;
       }
-      float m = -INFINITY, l = 0.f;
+      // The sum of the weights, and what its roundings left out: a row's tokens may all come to one thread, and
+      // 262144 of them 17.5 below a first one, added to it as they came, were off by 1.7e-3 in the log-sum-exp.
+      float m = -INFINITY, l = 0.f, l_rest = 0.f;
       if (active && tiles) {
         {  // the row of Q into shared memory; codes' products come in the order in which they are unpacked
           const T* q = reinterpret_cast<const T*>(a.q.in) + static_cast<int64_t>(it.span.first + token) * a.q.in_token +
@@ -358,11 +360,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
               tc_wait_st();
             }
             l *= k;
+            l_rest *= k;
             m = to;
           }
           const float from = m == -INFINITY ? 0.f : -m;
           const uint64_t by2 = two(by, by), from2 = two(from, from);
-          uint64_t l2 = two(l, 0.f), l3 = two(0.f, 0.f);
+          uint64_t l2 = two(0.f, 0.f), l3 = two(0.f, 0.f);
           const auto exponentials = [&](const uint32_t* z, uint32_t col) {
             uint32_t w[16];
 #pragma unroll
@@ -385,7 +388,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
           exponentials(y, s_col + 16);
           float l0, l1;
           apart(add2(l2, l3), l0, l1);
-          l = l0 + l1;
+          {  // l + here, whose rounding is l - (sum - took) + (here - took) to the last bit
+            const float here = l0 + l1, sum = l + here, took = sum - l;
+            l_rest += (l - (sum - took)) + (here - took);
+            l = sum;
+          }
           tc_wait_st();
           tc_fence_before();
           warp_arrive(&sm.p_full[t][s_n % 2]);
@@ -393,6 +400,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
         if (ok) ok = tc_wait(&sm.o_full[t][(s_n - 1) % 2], (s_n - 1) / 2, stop);
         ok = __all_sync(0xffffffffu, ok);
         tc_fence_after();
+        l += l_rest;
       }
       // info of tiles that this half does not use
       if (!active) n += tiles;

@@ -1,0 +1,59 @@
+"""Long flat caches below one key. Each of the flat keys' weights is small beside the largest, together they are not:
+sums must not lose them. There are more sequences than the GPU holds at a time (they share their pages), so that few CTAs
+see a row: where many do, each has a maximum and sums of its own."""
+import functools
+
+import pytest
+import torch
+
+from tests import kv_bounds as B
+from tests import kv_oracle as K
+
+pytestmark = pytest.mark.gpu
+
+SEQS, D, PAGE = 304, 64, 256
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _cuda():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+
+
+@functools.lru_cache(maxsize=1)
+def _run(dtype, bits, n, above, value, M=262144, H=2):
+    """(outputs, log-sum-exps) of n new tokens that pass their bounds; key 1000 lies `above` the others, its value is
+    `value`, theirs are about 1."""
+    from paper_2609_03675_gb300 import KVCache
+    g = torch.Generator().manual_seed(n)
+    cache = KVCache(M // PAGE, PAGE, H, 1, D, dtype=dtype, bits=bits)
+    k = torch.zeros((M, 1, D), dtype=dtype)
+    k[1000, 0, 0] = 15.0
+    v = (1.0 + 0.25 * torch.randn((M, 1, D), generator=g)).to(dtype)
+    v[1000] = value
+    for x, pages, scales in ((k, cache.k_pages, cache.k_scales), (v, cache.v_pages, cache.v_scales)):
+        if bits == 16:
+            pages.copy_(x.view(M // PAGE, PAGE, 1, D).transpose(1, 2))
+        else:
+            b, w = K.pack(*K.quantise(x))
+            pages.copy_(b.view(M // PAGE, PAGE, 1, D // 2).transpose(1, 2))
+            scales.copy_(w.view(M // PAGE, PAGE, 1, D // 64).transpose(1, 2))
+    if bits == 4:
+        k, v = (K.unpack(*K.pack(*K.quantise(x)))[0] for x in (k, v))
+    q = (0.5 * torch.randn((n, H, D), generator=g)).to(dtype)
+    q[..., 0] = above * D ** 0.5 / 15.0
+    table = torch.arange(M // PAGE, dtype=torch.int32, device="cuda").repeat(SEQS, 1)
+    lens = torch.full((SEQS,), M, dtype=torch.int32, device="cuda")
+    offsets = torch.arange(SEQS + 1, dtype=torch.int32, device="cuda") * n
+    out, lse = cache.attend(q.cuda().repeat(SEQS, 1, 1), table, lens, offsets, max_new=n)
+    cache.status()
+    seen = torch.arange(M)[None] <= (M - n + torch.arange(n))[:, None]
+    return B.exceeds(out.view(SEQS, n, H, D), lse.view(SEQS, n, H), B.attend(q, k, v, seen, D ** -0.5, dtype))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("n", [1, 5, 17])
+@pytest.mark.parametrize("above", [0.0, 12.0, 17.5])
+def test_sum_of_the_weights(dtype, bits, n, above):
+    assert not bool(_run(dtype, bits, n, above, 0.0)[1].any())

@@ -304,7 +304,10 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
       const int64_t n = static_cast<int64_t>(it.span.length) - it.span.count + row0 / a.group + 1;
       all_see = n > 0 ? static_cast<int32_t>(n) : 0;
     }
-    float o[NT][D / 16][4], m[NT][2], l[NT][2];
+    // Weights are summed by kSumChunks chunks, and those sums into l: a lane may have the largest weight and, one by one
+    // onto it, 16384 of a million that are 2^-25 of it (the log-sum-exp was 4e-4 off).
+    constexpr uint32_t kSumChunks = 64;
+    float o[NT][D / 16][4], m[NT][2], l[NT][2], l_part[NT][2];
     float v_up = 1.f;               // 4-bit: the power of two on p s
     uint32_t v_most = 0x000F000Fu;  // words up to which it holds, twice
 #pragma unroll
@@ -312,7 +315,7 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
 #pragma unroll
       for (int e = 0; e < D / 16; ++e) o[nt][e][0] = o[nt][e][1] = o[nt][e][2] = o[nt][e][3] = 0.f;
       m[nt][0] = m[nt][1] = -INFINITY;
-      l[nt][0] = l[nt][1] = 0.f;
+      l[nt][0] = l[nt][1] = l_part[nt][0] = l_part[nt][1] = 0.f;
     }
 
     uint32_t stage = 0;
@@ -325,6 +328,14 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
       issue(stage == 0 ? R::kStages - 1 : stage - 1, ahead);  // the stage read in the iteration before
       ahead = look(ch + R::kStages * kSplitWarps);
       if (++stage == R::kStages) stage = 0;
+      if (ch / kSplitWarps % kSumChunks == 0) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          l[nt][0] += l_part[nt][0];
+          l[nt][1] += l_part[nt][1];
+          l_part[nt][0] = l_part[nt][1] = 0.f;
+        }
+      }
       if (bits == 0) continue;
       const bool whole = (BITS == 4 ? bits == 0xffffffffu : (bits & 0xffffu) == 0xffffu);
       const char *const vbase = base + R::kTokens * R::kRow, *const kw = base + 2 * R::kTokens * R::kRow, *const vw = kw + R::kWords;
@@ -419,6 +430,8 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
           m[nt][1] = x1;
           l[nt][0] *= k0;
           l[nt][1] *= k1;
+          l_part[nt][0] *= k0;
+          l_part[nt][1] *= k1;
 #pragma unroll
           for (int e = 0; e < D / 16; ++e) {
             o[nt][e][0] *= k0;
@@ -432,8 +445,8 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
         for (int mt = 0; mt < kM; ++mt) {
 #pragma unroll
           for (int e = 0; e < 4; ++e) p[nt][mt][e] = exp2_fast(fmaf(s[nt][mt][e], by[nt][e % 2], e % 2 ? -u1 : -u0));
-          l[nt][0] += p[nt][mt][0] + p[nt][mt][2];
-          l[nt][1] += p[nt][mt][1] + p[nt][mt][3];
+          l_part[nt][0] += p[nt][mt][0] + p[nt][mt][2];
+          l_part[nt][1] += p[nt][mt][1] + p[nt][mt][3];
         }
       }
       // ---- values
@@ -561,7 +574,7 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        float x = l[nt][e];
+        float x = l[nt][e] + l_part[nt][e];
 #pragma unroll
         for (int w = 4; w < 32; w <<= 1) x += __shfl_xor_sync(0xffffffffu, x, w);
         if (g == 0) {

@@ -57,3 +57,10 @@ def _run(dtype, bits, n, above, value, M=262144, H=2):
 @pytest.mark.parametrize("above", [0.0, 12.0, 17.5])
 def test_sum_of_the_weights(dtype, bits, n, above):
     assert not bool(_run(dtype, bits, n, above, 0.0)[1].any())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_sum_of_the_weights_of_a_million_tokens(dtype):
+    """A lane of the kernel of few rows sums 1 in 64 of a CTA's tokens."""
+    assert not bool(_run(dtype, 16, 1, 17.5, 0.0, 1 << 20, 1)[1].any())
+    _run.cache_clear()

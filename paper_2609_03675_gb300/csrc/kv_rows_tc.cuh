@@ -11,8 +11,8 @@
 //   MMA        a warp for each tile: S = Q K^T into tensor memory (128 x 64 fp32 a tile),
 //              and O += P V with P read from tensor memory
 // The running maximum that exponentials refer to is raised only when the true
-// one passes it by 2^8 (then O is brought down in tensor memory), which seldom
-// happens after the first tokens.
+// one passes it by 2^8 (2^4 for fp16; then O is brought down in tensor memory),
+// which seldom happens after the first tokens.
 //
 // Tensor memory: O0 O1 (D columns each) and for each tile two S of 64 columns,
 // P in the first 32 of its S: while the softmax works on one S, the products
@@ -24,8 +24,6 @@
 // of 128), shared memory 2048 for its operands and 512 for writing them, the
 // exponentials 1024 and more.
 #pragma once
-
-#include <type_traits>
 
 #include "kv_split.cuh"
 #include "ngff_device.cuh"
@@ -40,7 +38,6 @@ constexpr int kTcThreads = kTcSoftmax + 2 * kTcProducers + 128;  // and a group 
 constexpr int kTcStages = 4;       // of keys, and of values
 constexpr int kTcInfo = 8;         // more than the stages: a tile is told before its place is free
 constexpr int kTcRaw = 3;          // codes as they lie in the pages
-constexpr float kTcRaise = 8.f;
 constexpr uint64_t kTcTimeout = 1000000000ull;
 // Registers: all threads start with 96; 256 x 136 + 256 x 72 + 128 x 64 is 640 x 96.
 constexpr int kTcRegsSoftmax = 136, kTcRegsProducer = 72, kTcRegsIssuer = 64;
@@ -225,6 +222,11 @@ template <typename T, int D, int BITS>
 __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_constant__ AttendArgs a) {
   using P = Pair<T>;
   using S = TcSmem<D, BITS>;
+  // fp16: weights are 2^7 times what they stand for, so that only those under 2^-32 of the largest are lost to the second
+  // product, and the maximum that they refer to is never more than 2^4 behind: up to 2^11, the exponents above left for a
+  // maximum that is a rounding of a large score off. (bf16 has the exponents of fp32.)
+  constexpr bool kHalf = std::is_same<T, __half>::value;
+  constexpr float kRaise = kHalf ? 4.f : 8.f, kUp = kHalf ? 7.f : 0.f, kDown = kHalf ? 0x1p-7f : 1.f;
   extern __shared__ char raw[];
   S& sm = *reinterpret_cast<S*>(raw + (1024u - (shared_address(raw) & 1023u)) % 1024u);
   pdl_trigger();
@@ -342,7 +344,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
             }
           }
           const float top = most_of(x, y, -INFINITY) * by;
-          const bool raise = top > m + kTcRaise || (m == -INFINITY && top > -INFINITY);
+          const bool raise = top > m + kRaise || (m == -INFINITY && top > -INFINITY);
           if (__any_sync(0xffffffffu, raise)) {
             const float to = raise ? top : m, k = m == -INFINITY ? 0.f : exp2_fast(m - to);
             if (j > 0) {  // O as it is after the tokens before
@@ -363,7 +365,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
             l_rest *= k;
             m = to;
           }
-          const float from = m == -INFINITY ? 0.f : -m;
+          const float from = m == -INFINITY ? 0.f : kUp - m;
           const uint64_t by2 = two(by, by), from2 = two(from, from);
           uint64_t l2 = two(0.f, 0.f), l3 = two(0.f, 0.f);
           const auto exponentials = [&](const uint32_t* z, uint32_t col) {
@@ -452,7 +454,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
         }
         if (real) {
           if (!alone) a.part_ms[part + lr] = make_float2(m, l);
-          else if (a.lse) a.lse[static_cast<uint64_t>(it.span.first + token) * a.heads + head] = (m + log2f(l)) * 0.6931471805599453f;
+          else if (a.lse) a.lse[static_cast<uint64_t>(it.span.first + token) * a.heads + head] = (m + log2f(l * kDown)) * 0.6931471805599453f;
         }
       }
       tc_fence_before();  // O is read before the next item's products are let through (by q_full)
@@ -475,7 +477,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
               sum += z.y == 0.f ? 0.f : k * z.y;
               __stcg(&at->x, k);  // the part's factor, for the threads that join it
             }
-            if (a.lse) a.lse[static_cast<uint64_t>(it.span.first + token) * a.heads + head] = (top + log2f(sum)) * 0.6931471805599453f;
+            if (a.lse) a.lse[static_cast<uint64_t>(it.span.first + token) * a.heads + head] = (top + log2f(sum * kDown)) * 0.6931471805599453f;
           }
           sm.by_sum[lr] = sum == 0.f ? 0.f : 1.f / sum;
           bar_sync<1, kTcSoftmax>();

@@ -35,6 +35,8 @@
 // values and 128 + n for keys the kernel took 108 us, its ALU pipe 70 % busy.
 #pragma once
 
+#include <type_traits>
+
 #include "kv_plan.cuh"
 
 namespace cofie {
@@ -138,6 +140,11 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
   using H = Pair<__half>;
   using R = Ring<D, BITS>;
   constexpr int kRows = 8 * NT, kGroups = D / 64, kM = R::kTokens / 16, kPerTile = kTile / R::kTokens;
+  // 16-bit values: weights go into the second product as fp16 numbers of up to 2^8, so that only those under 2^-33 are
+  // lost to it. (Up to 1, those under 2^-25 were, though not to the sum of weights: 262144 keys 17.5 below one are 0.7 %
+  // of a row. The upper exponents are left for a maximum that is a rounding of a large score off. bf16 has the exponents
+  // of fp32, and 4-bit values have a power of two with their scale.)
+  constexpr float kUp = BITS == 16 && std::is_same<T, __half>::value ? 8.f : 0.f, kDown = kUp > 0.f ? 0x1p-8f : 1.f;
   extern __shared__ __align__(128) char smem[];
   __shared__ Plan<kSplitThreads> plan;
   __shared__ Span spans[kSpans];
@@ -440,7 +447,7 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
             o[nt][e][3] *= k1;
           }
         }
-        const float u0 = x0 == -INFINITY ? 0.f : x0, u1 = x1 == -INFINITY ? 0.f : x1;
+        const float u0 = x0 == -INFINITY ? 0.f : x0 - kUp, u1 = x1 == -INFINITY ? 0.f : x1 - kUp;
 #pragma unroll
         for (int mt = 0; mt < kM; ++mt) {
 #pragma unroll
@@ -608,7 +615,7 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
         out[2] = Elem<T>::from(x.z * by);
         out[3] = Elem<T>::from(x.w * by);
       }
-      if (a.lse && d == 0) a.lse[static_cast<uint64_t>(i) * a.heads + h] = (top + log2f(sum)) * 0.6931471805599453f;
+      if (a.lse && d == 0) a.lse[static_cast<uint64_t>(i) * a.heads + h] = (top + log2f(sum * kDown)) * 0.6931471805599453f;
     };
     for (uint32_t x = threadIdx.x; x < rows * (D / 4); x += kSplitThreads) {
       const uint32_t r = x / (D / 4), d = x % (D / 4) * 4;

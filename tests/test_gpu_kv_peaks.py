@@ -64,3 +64,29 @@ def test_sum_of_the_weights_of_a_million_tokens(dtype):
     """A lane of the kernel of few rows sums 1 in 64 of a CTA's tokens."""
     assert not bool(_run(dtype, 16, 1, 17.5, 0.0, 1 << 20, 1)[1].any())
     _run.cache_clear()
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("n", [1, 5, 17])
+def test_weights_that_fp16_holds(bits, n):
+    """Rounded to fp16 a weight under 2^-25 is nothing; the key above has no value, so that the outputs are the others'."""
+    assert not bool(_run(torch.float16, bits, n, 17.5, 0.0)[0].any())
+
+
+@pytest.mark.parametrize("n", [1, 17])
+def test_scores_of_millions_in_fp16(n):
+    """fp32 rounds such scores by whole units; weights formed from them stay finite."""
+    from paper_2609_03675_gb300 import KVCache
+    m, d = 700, 128
+    g = torch.Generator(device="cuda").manual_seed(n)
+    x = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    cache = KVCache(44, 16, 4, 2, d, dtype=torch.float16)
+    table = torch.arange(44, dtype=torch.int32, device="cuda").view(1, -1)
+    lens, offsets = (torch.tensor(y, dtype=torch.int32, device="cuda") for y in ([m], [0, m]))
+    k = (900.0 * x(m, 2, d) + 1500.0).half()
+    cache.append(k, x(m, 2, d).half(), table, lens, offsets)
+    q = (900.0 * x(n, 4, d) + 1500.0).half()
+    out, lse = cache.attend(q, table, lens, torch.tensor([0, n], dtype=torch.int32, device="cuda"), max_new=n)
+    cache.status()
+    assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(lse).all())
+    assert float(lse.min()) > 1e7

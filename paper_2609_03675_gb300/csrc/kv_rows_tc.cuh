@@ -12,7 +12,8 @@
 //              and O += P V with P read from tensor memory
 // The running maximum that exponentials refer to is raised only when the true
 // one passes it by 2^8 (2^4 for fp16; then O is brought down in tensor memory),
-// which seldom happens after the first tokens.
+// which seldom happens after the first tokens. O itself is read out and begun
+// anew after some thousands of tokens (kTcChain).
 //
 // Tensor memory: O0 O1 (D columns each) and for each tile two S of 64 columns,
 // P in the first 32 of its S: while the softmax works on one S, the products
@@ -38,6 +39,12 @@ constexpr int kTcThreads = kTcSoftmax + 2 * kTcProducers + 128;  // and a group 
 constexpr int kTcStages = 4;       // of keys, and of values
 constexpr int kTcInfo = 8;         // more than the stages: a tile is told before its place is free
 constexpr int kTcRaw = 3;          // codes as they lie in the pages
+// Tiles whose products are summed in tensor memory before the sums move on to the CTA's part. The tensor core cuts each
+// product off at about 2^-24 of the sum that it is added to, so 8192 tokens may cost a sum 2^-11 of its size, a rounding
+// of fp16, and 65536 tokens 2^-8, one of bf16. (In one sum, 262144 tokens 14 to 17 below a first one came out 0.4 to
+// 0.5 % low.)
+template <typename T>
+constexpr uint32_t kTcChain = std::is_same<T, __half>::value ? 128 : 1024;
 constexpr uint64_t kTcTimeout = 1000000000ull;
 // Registers: all threads start with 96; 256 x 136 + 256 x 72 + 128 x 64 is 640 x 96.
 constexpr int kTcRegsSoftmax = 136, kTcRegsProducer = 72, kTcRegsIssuer = 64;
@@ -291,6 +298,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
       // The sum of the weights, and what its roundings left out: a row's tokens may all come to one thread, and
       // 262144 of them 17.5 below a first one, added to it as they came, were off by 1.7e-3 in the log-sum-exp.
       float m = -INFINITY, l = 0.f, l_rest = 0.f;
+      // Sums that have left tensor memory are kept in this row of the part, against the maximum of then; in O's order of
+      // columns. (An item that is this CTA's alone uses the part of the one that goes on from it, which comes last.)
+      float kept_m = -INFINITY;
+      const uint32_t lr = t * 128 + r;  // row of the item's 256
+      const auto own_part = [&] { return (2ull * blockIdx.x + (blockIdx.x == it.first_cta ? 1 : 0)) * kTcRows; };
       if (active && tiles) {
         {  // the row of Q into shared memory; codes' products come in the order in which they are unpacked
           const T* q = reinterpret_cast<const T*>(a.q.in) + static_cast<int64_t>(it.span.first + token) * a.q.in_token +
@@ -324,6 +336,26 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
             break;
           }
           tc_fence_after();
+          if (j > 0 && j % kTcChain<T> == 0) {
+            ok = tc_wait(&sm.o_full[t][(s_n - 1) % 2], (s_n - 1) / 2, stop);
+            ok = __all_sync(0xffffffffu, ok);
+            tc_fence_after();
+            const float k = kept_m == -INFINITY ? 0.f : exp2_fast(kept_m - m);
+            float* const kept = a.part + (own_part() + lr) * D;
+#pragma unroll 1
+            for (int e = 0; e < D / 16; ++e) {
+              uint32_t z[16];
+              tc_ld16(o_col + 16 * e, z);
+#pragma unroll
+              for (int f = 0; f < 16; f += 4) {
+                float4* const at = reinterpret_cast<float4*>(kept + 16 * e + f);
+                const float4 was = j == kTcChain<T> ? make_float4(0.f, 0.f, 0.f, 0.f) : *at;
+                *at = make_float4(fmaf(was.x, k, __uint_as_float(z[f])), fmaf(was.y, k, __uint_as_float(z[f + 1])),
+                                  fmaf(was.z, k, __uint_as_float(z[f + 2])), fmaf(was.w, k, __uint_as_float(z[f + 3])));
+              }
+            }
+            kept_m = m;
+          }
           const uint32_t s_col = s_at(t, s_n) + lanes;
           uint32_t x[32], y[32];
           tc_ld32(s_col, x);
@@ -347,7 +379,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
           const bool raise = top > m + kRaise || (m == -INFINITY && top > -INFINITY);
           if (__any_sync(0xffffffffu, raise)) {
             const float to = raise ? top : m, k = m == -INFINITY ? 0.f : exp2_fast(m - to);
-            if (j > 0) {  // O as it is after the tokens before
+            if (j % kTcChain<T> != 0) {  // O as it is after the tokens before
               ok = tc_wait(&sm.o_full[t][(s_n - 1) % 2], (s_n - 1) / 2, stop);
               ok = __all_sync(0xffffffffu, ok);
               tc_fence_after();
@@ -407,8 +439,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
       // info of tiles that this half does not use
       if (!active) n += tiles;
       const bool alone = it.first_cta == it.last_cta;
-      const uint32_t lr = t * 128 + r;  // row of the item's 256
-      const uint64_t part = (2ull * blockIdx.x + (blockIdx.x == it.first_cta ? 1 : 0)) * kTcRows;
+      const uint64_t part = own_part();
+      const float* const kept = a.part + (part + lr) * D;
+      const bool some_kept = tiles > kTcChain<T>;
+      const float kept_by = kept_m == -INFINITY ? 0.f : exp2_fast(kept_m - m);
       const float inv = l == 0.f ? 0.f : 1.f / l;
       T* out = reinterpret_cast<T*>(a.q.out) + static_cast<int64_t>(it.span.first + token) * a.q.out_token +
                static_cast<int64_t>(head) * a.q.out_head;
@@ -430,6 +464,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
               float z[8];
 #pragma unroll
               for (int i = 0; i < 8; ++i) z[BITS == 4 ? order[i] : i] = __uint_as_float(y[8 * f + i]);
+              if (some_kept) {  // this thread's own, read before it is written over
+                const float4 u = *reinterpret_cast<const float4*>(kept + 32 * e + 8 * f), w = *reinterpret_cast<const float4*>(kept + 32 * e + 8 * f + 4);
+                const float x[8] = {u.x, u.y, u.z, u.w, w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int i = 0; i < 8; ++i) z[BITS == 4 ? order[i] : i] = fmaf(x[i], kept_by, z[BITS == 4 ? order[i] : i]);
+              }
               if (l == 0.f)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) z[i] = 0.f;
@@ -739,7 +779,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
           tc_fence_after();
           const uint32_t v = tc_desc(shared_address(sm.kv[1][st]), S::kBlock), p = s_at(t, i);
 #pragma unroll
-          for (int e = 0; e < static_cast<int>(kTile) / 16; ++e) tc_mma_ts(leader, o_at(t), p + e * 8, v + e * (2048 / 16), kPV, j > 0 || e > 0);
+          for (int e = 0; e < static_cast<int>(kTile) / 16; ++e) tc_mma_ts(leader, o_at(t), p + e * 8, v + e * (2048 / 16), kPV, j % kTcChain<T> != 0 || e > 0);
           tc_commit(leader, &sm.o_full[t][i % 2]);
           tc_commit(leader, &sm.empty[1][st]);
           if (j + 2 < tiles) qk(j + 2);

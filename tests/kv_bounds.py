@@ -1,6 +1,6 @@
 """The bound on attention's outputs for kernels that see the cache's numbers exactly, whatever the pages hold: 4-bit codes
 enter the products as (n - z), or as (n - z) s, which 16-bit types hold. It is kv_oracle.attend's, with the numbers' own
-sizes for 4-bit pages as for 16-bit ones, and two terms for what fp16 cannot hold:
+sizes for 4-bit pages as for 16-bit ones, with two terms for what fp16 cannot hold and one for long sums:
 
 queries   the kernel of few rows takes them to fp16, a power of two bringing the row's largest to [128, 256): an entry
           is off by at most 2^-21 there (half of fp16's smallest spacing, for the odd dimensions 16 times that), so by
@@ -9,6 +9,9 @@ weights   for fp16 they are rounded to fp16 with the largest at 2^7 or more, so 
           u of it is less; with 4-bit values, few rows, weight times scale, at 2^10 or more of the largest scale s: off
           by 2^-35 s at most, and a value by 15 of that, where 15 s <= 9/8 (hi - lo) < 3 max |v|. Over m tokens:
           m 2^-32 max |v|.
+sums      the tensor cores cut each product off at 2^-24 of the sum that it is added to, or below: over `chain` tokens
+          that come to one sum chain 2^-24 sum p |v|. A sum holds at most 8192 tokens (fp16) or 65536 (bf16) in the
+          kernel of many rows, an eighth of a CTA's tokens in that of few.
 """
 from __future__ import annotations
 
@@ -17,9 +20,11 @@ import torch
 from tests import kv_oracle as K
 
 
-def attend(q, k, v, visible, scale, dtype):
-    """As kv_oracle.attend: (out, lse, bound of out, bound of lse)."""
+def attend(q, k, v, visible, scale, dtype, chain=None):
+    """As kv_oracle.attend: (out, lse, bound of out, bound of lse). chain: the most tokens of a sum; all of them."""
     out, lse, b_out, b_lse = K.attend(q, k, v, visible, scale, dtype)
+    chain = visible.shape[1] if chain is None else min(chain, visible.shape[1])
+    b_out = b_out + chain * 2.0 ** -24 * K.attend(q, k, torch.as_tensor(v).abs(), visible, scale, dtype)[0]
     q, visible = q.double().cpu(), visible.cpu()
     held = visible.any(0)
     G = q.shape[1] // k.shape[1]

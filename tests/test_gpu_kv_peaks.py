@@ -48,7 +48,8 @@ def _run(dtype, bits, n, above, value, M=262144, H=2):
     out, lse = cache.attend(q.cuda().repeat(SEQS, 1, 1), table, lens, offsets, max_new=n)
     cache.status()
     seen = torch.arange(M)[None] <= (M - n + torch.arange(n))[:, None]
-    return B.exceeds(out.view(SEQS, n, H, D), lse.view(SEQS, n, H), B.attend(q, k, v, seen, D ** -0.5, dtype))
+    chain = M // 8 if n * H <= 32 else 8192 if dtype == torch.float16 else 65536
+    return B.exceeds(out.view(SEQS, n, H, D), lse.view(SEQS, n, H), B.attend(q, k, v, seen, D ** -0.5, dtype, chain))
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
@@ -90,3 +91,17 @@ def test_scores_of_millions_in_fp16(n):
     cache.status()
     assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(lse).all())
     assert float(lse.min()) > 1e7
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("n", [1, 17])
+@pytest.mark.parametrize("above,value", [(0.0, 1.0), (12.0, 0.0), (14.3, 1.0), (17.5, 1.0)])
+def test_outputs_of_long_sums(dtype, bits, n, above, value):
+    """Values that all point one way, so that nothing of a sum cancels."""
+    assert not bool(_run(dtype, bits, n, above, value)[0].any())
+
+
+def test_outputs_of_sums_of_a_million_in_bf16():
+    assert not bool(_run(torch.bfloat16, 16, 33, 15.0, 1.0, 1 << 20, 1)[0].any())
+    _run.cache_clear()

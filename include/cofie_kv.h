@@ -26,7 +26,8 @@
  *              is the bf16 scale s (4 significant bits), its low four bits are
  *              the zero point z. Code n stands for (n - z) s, which bf16 holds
  *              exactly (fp16 too, where s is in its normal range).
- *   Codes of x (64 values): lo = min(0, min x), hi = max(0, max x),
+ *   Codes of x (64 values, rotated keys as fp32 numbers; hi - lo is formed in
+ *   fp32, all else exactly): lo = min(0, min x), hi = max(0, max x),
  *   s = (hi - lo) / 15 rounded up to 4 significant bits (0 below 2^-100),
  *   z = min(15, [-lo / s]), n = min(15, max(0, [x / s] + z)), [] to the
  *   nearest, halves away from zero. A group that holds a NaN or an infinity,

@@ -20,6 +20,14 @@ struct CodesArgs {
   uint32_t kv_heads, q_parts;
 };
 
+// zero + n, n the code's distance from the zero point, a step nearer to it where
+// x lies more than half a step from n (then it lies on that side). A step of 0
+// or NaN has no codes.
+__device__ __forceinline__ float code_back(float code, float zero, float x, float step) {
+  const bool past = step > 0.f && fabsf(__fmaf_rn(zero - code, step, x)) > 0.5f * step;
+  return past ? code - copysignf(1.f, x) : code;
+}
+
 // Appends to 4-bit pages. CTAs of gridDim.y below q_parts rotate the queries;
 // the others take a share of the (key or value, head) rows of their tokens.
 // Sixteen values of a row to a lane, eight from either half of the head, so that
@@ -142,16 +150,20 @@ __global__ void __launch_bounds__(kThreads, 4) append_codes(const __grid_constan
       // x / scale to the nearest, halves away from zero: the reciprocal (good to
       // a last place) is taken two above its value, so that no half stays one,
       // and the product and the zero point are summed and rounded once, to the
-      // last bit of 1.5 2^23. (No quotient of 16-bit x lies that close to a half
-      // without being one.)
+      // last bit of 1.5 2^23. No quotient of 16-bit x lies that close to a half
+      // without being one, but one of rotated keys, which are fp32 numbers, may:
+      // for those x - code scale, which is exact, is held against half a scale.
       uint32_t word[2], codes8[2];
-      float inv[2], zero[2];
+      float inv[2], zero[2], step[2];
 #pragma unroll
       for (int gr = 0; gr < kOwn; ++gr) {
         const float scale = group_scale(lo[gr], hi[gr]);
         asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv[gr]) : "f"(scale));
         inv[gr] = scale > 0.f ? __uint_as_float(__float_as_uint(inv[gr]) + 2) : 0.f;
-        zero[gr] = fminf(__fmaf_rn(-lo[gr], inv[gr], 12582912.f), 12582927.f);
+        float near = __fmaf_rn(-lo[gr], inv[gr], 12582912.f);
+        if (turned) near = code_back(near, 12582912.f, -lo[gr], scale);
+        zero[gr] = fminf(near, 12582927.f);
+        step[gr] = scale;
         word[gr] = (__float_as_uint(scale) >> 16) | (__float_as_uint(zero[gr]) & 15u);
       }
 #pragma unroll
@@ -159,8 +171,19 @@ __global__ void __launch_bounds__(kThreads, 4) append_codes(const __grid_constan
         // codes are the low bits of 0x4B400000 + code, whose sum's share is taken off at the end
         uint32_t w = 0;
         const int gr = kOwn == 1 ? 0 : e;
+        const auto code = [&](int i) { return __fmaf_rn(x[8 * e + i], inv[gr], zero[gr]); };
 #pragma unroll
-        for (int i = 7; i >= 0; --i) w = w * 16 + __float_as_uint(fminf(__fmaf_rn(x[8 * e + i], inv[gr], zero[gr]), 12582927.f));
+        for (int i = 7; i >= 0; --i) w = w * 16 + __float_as_uint(fminf(code(i), 12582927.f));
+        if (turned) {  // looked at apart, since there is seldom one to put right (codes kept for it cost 22 us of 225)
+          float most = 0.f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(__fmaf_rn(zero[gr] - code(i), step[gr], x[8 * e + i])));
+          if (most > 0.5f * step[gr]) {
+            w = 0;
+#pragma unroll
+            for (int i = 7; i >= 0; --i) w = w * 16 + __float_as_uint(fminf(code_back(code(i), zero[gr], x[8 * e + i], step[gr]), 12582927.f));
+          }
+        }
         codes8[e] = w - 0x4B400000u * 0x11111111u;
       }
       if (p >= 0) {

@@ -302,10 +302,12 @@ class KVCache:
         return q_out if q is not None else None
 
     def read(self, table, lengths, offsets=None, *, n_tokens=None, out=None, cuda_stream=None):
-        """(keys, values) [tokens, kv heads, head_dim] as the cache holds them at the batch's new tokens. The count of
-        tokens is that of ``out`` (a pair of tensors), n_tokens, or the sequences'."""
+        """(keys, values) [tokens, kv heads, head_dim] as the cache holds them at the batch's new tokens. With offsets, which
+        lie on the device, the count of tokens is the caller's to say: n_tokens, or that of ``out`` (a pair of tensors)."""
         index = self._index
         if out is None:
+            if n_tokens is None and offsets is not None:
+                raise ValueError("n_tokens or out goes with offsets")
             n = n_tokens if n_tokens is not None else table.shape[0]
             with _allocating(cuda_stream, index):
                 out = tuple(torch.empty((n, self.n_kv_heads, self.head_dim), dtype=self.dtype, device=self.device) for _ in range(2))

@@ -1,0 +1,36 @@
+"""Calls of the cache and of the rotary that leave something out, come after a close, or want a gradient."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _cuda():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+
+
+def _ints(*x):
+    return torch.tensor(x, dtype=torch.int32, device="cuda")
+
+
+def _normal(*shape, seed=0, dtype=torch.bfloat16):
+    return torch.randn(shape, generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda").to(dtype)
+
+
+def test_read_with_offsets_wants_a_count():
+    """Offsets lie on the device: how many rows they name is the caller's to say."""
+    from paper_2609_03675_gb300 import KVCache
+    cache = KVCache(4, 16, 2, 1, 64)
+    table, lens, offsets = _ints(0, 1, 2, 3).view(2, 2), _ints(20, 5), _ints(0, 20, 25)
+    k = _normal(25, 1, 64)
+    cache.append(k, k, table, lens, offsets)
+    with pytest.raises(ValueError, match="n_tokens"):
+        cache.read(table, lens, offsets)
+    out = torch.empty_like(k), torch.empty_like(k)
+    for got in (cache.read(table, lens, offsets, n_tokens=25), cache.read(table, lens, offsets, out=out)):
+        assert torch.equal(got[0], k) and torch.equal(got[1], k)
+    last = cache.read(table, lens)  # without offsets one row each, the last
+    assert torch.equal(last[0], k[[19, 24]])
+    cache.status()

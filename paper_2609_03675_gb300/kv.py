@@ -290,6 +290,8 @@ class KVCache:
         qr = at = handle = None
         if rotary is not None:
             handle, at = rotary._h, rotary._positions(positions, n, index)
+            if not handle:
+                raise ValueError("the cache's rotary is closed")
         if q is not None:
             if rotary is None:
                 raise ValueError("q goes with a cache that has a rotary")

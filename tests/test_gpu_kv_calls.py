@@ -34,3 +34,25 @@ def test_read_with_offsets_wants_a_count():
     last = cache.read(table, lens)  # without offsets one row each, the last
     assert torch.equal(last[0], k[[19, 24]])
     cache.status()
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+def test_append_after_the_rotary_is_closed(bits):
+    """Without its rotary a cache would store keys that are not rotated."""
+    from paper_2609_03675_gb300 import KVCache, NGFFError, Rotary
+    rotary = Rotary(64)
+    cache = KVCache(2, 16, 2, 1, 64, bits=bits, rotary=rotary)
+    table, lens, pos = _ints(0, 1).view(1, 2), _ints(1), _ints(5)
+    k, q = _normal(1, 1, 64), _normal(1, 2, 64)
+    cache.append(k, k, table, lens, positions=pos)
+    before = cache.k_pages.clone()
+    rotary.close()
+    for kw in ({}, {"q": q}):
+        with pytest.raises(ValueError, match="closed"):
+            cache.append(_normal(1, 1, 64, seed=1), k, table, lens, positions=pos, **kw)
+    assert torch.equal(cache.k_pages, before)
+    with pytest.raises(NGFFError):
+        rotary.apply(q, pos)
+    cache.close()
+    with pytest.raises(NGFFError):
+        cache.attend(q, table, lens)

@@ -342,7 +342,8 @@ class KVCache:
             if mask.dtype not in (torch.uint8, torch.bool) or mask.dim() != 2 or mask.shape[0] != table.shape[0] or not mask.is_contiguous() \
                     or mask.get_device() != index:
                 raise ValueError(f"mask must be a contiguous uint8 or bool tensor [{table.shape[0]}, tokens] on cuda:{index}")
-            at, stride = mask.data_ptr(), mask.shape[1]
+            # a mask of no tokens, which hides them all, may have no address; nothing is read at the one it gets here
+            at, stride = mask.data_ptr() or self.k_pages.data_ptr(), mask.shape[1]
         stream = _raw_stream(index) if cuda_stream is None else _stream_of(cuda_stream, index)
         self._check(self._lib.cofie_kv_attend(self._h, self._at, r, lse.data_ptr(), at, stride, causal, scale, stream))
         return out, lse

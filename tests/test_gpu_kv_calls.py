@@ -56,3 +56,19 @@ def test_append_after_the_rotary_is_closed(bits):
     cache.close()
     with pytest.raises(NGFFError):
         cache.attend(q, table, lens)
+
+
+@pytest.mark.parametrize("n", [1, 40])
+def test_a_mask_of_no_tokens_hides_them_all(n):
+    """A cached token past the mask counts as masked."""
+    from paper_2609_03675_gb300 import KVCache
+    cache = KVCache(4, 16, 2, 1, 64)
+    table, lens, offsets = _ints(0, 1, 2, 3).view(1, 4), _ints(50), _ints(0, 50)
+    k = _normal(50, 1, 64)
+    cache.append(k, k, table, lens, offsets)
+    for dtype in (torch.uint8, torch.bool):
+        for width in (0, 1):
+            mask = torch.zeros((1, width), dtype=dtype, device="cuda")
+            out, lse = cache.attend(_normal(n, 2, 64), table, lens, _ints(0, n), max_new=n, mask=mask)
+            assert bool((out == 0).all()) and bool((lse == -float("inf")).all())
+    cache.status()

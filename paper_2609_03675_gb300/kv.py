@@ -125,6 +125,27 @@ def _int32(x, index, what, shape):
     return x.data_ptr()
 
 
+class _Turned(torch.autograd.Function):
+    """Rotary._run as a node of autograd's graph: its gradient is the rotation the other way round."""
+
+    @staticmethod
+    def forward(ctx, rotary, positions, transpose, cuda_stream, *xs):
+        ctx.rotary, ctx.transpose = rotary, transpose
+        ctx.save_for_backward(positions)
+        ctx.set_materialize_grads(False)
+        return rotary._run(xs, positions, None, transpose, cuda_stream)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        some = [i for i, g in enumerate(grads) if g is not None and ctx.needs_input_grad[4 + i]]
+        back = [None] * len(grads)
+        if some:
+            gs = tuple(grads[i] if grads[i].stride(-1) == 1 else grads[i].contiguous() for i in some)
+            for i, g in zip(some, ctx.rotary._run(gs, ctx.saved_tensors[0], None, 1 - ctx.transpose, None)):
+                back[i] = g
+        return (None, None, None, None, *back)
+
+
 class Rotary:
     """Rotates heads to their positions.
 
@@ -163,6 +184,12 @@ class Rotary:
         k = len(xs)
         if not 1 <= k <= 4:
             raise ValueError("one to four tensors of the same tokens")
+        for y in xs:
+            if y.requires_grad and torch.is_grad_enabled():
+                if out is not None:
+                    raise ValueError("out does not go with tensors that require a gradient")
+                outs = _Turned.apply(self, positions, transpose, cuda_stream, *xs)
+                return outs[0] if xs is not x else outs
         first = xs[0]
         index, dtype, n = first.get_device(), first.dtype, first.shape[0]
         code = _DTYPES.get(dtype)
@@ -194,7 +221,7 @@ class Rotary:
 
     def apply(self, x, positions, *, out=None, cuda_stream=None):
         """x (a tensor [tokens, heads, head_dim], or up to four of the same tokens) rotated; positions int32 [tokens], or
-        [axes, tokens]. ``out`` may be x itself."""
+        [axes, tokens]. ``out`` may be x itself. Tensors that require a gradient get it through autograd (without ``out``)."""
         return self._run(x, positions, out, 0, cuda_stream)
 
     def backward(self, grad, positions, *, out=None, cuda_stream=None):
@@ -218,7 +245,8 @@ class KVCache:
 
     The pages are k_pages, v_pages (and k_scales, v_scales for 4 bits), made here unless given. Sequence s of a batch holds
     lengths[s] tokens; token i lies in page table[s, i // page_size]. A batch's new tokens are rows offsets[s] to
-    offsets[s + 1] of every per-token argument, the last of the sequence's lengths[s] (offsets=None: one each)."""
+    offsets[s + 1] of every per-token argument, the last of the sequence's lengths[s] (offsets=None: one each).
+    A cache has no gradient: tensors that require one are refused, unless under torch.no_grad()."""
 
     def __init__(self, n_pages: int, page_size: int, n_heads: int, n_kv_heads: int, head_dim: int, *,
                  dtype: torch.dtype = torch.bfloat16, bits: int = 16, rotary: Rotary | None = None, device: int | None = None,
@@ -283,6 +311,8 @@ class KVCache:
         """Puts the batch's new keys (rotated, where the cache has a rotary) and values into their pages; lengths count them
         already. With q, its rotated copy is returned (in q_out, which may be q)."""
         n, rotary, index = k.shape[0], self.rotary, self._index
+        if (k.requires_grad or v.requires_grad or (q is not None and q.requires_grad)) and torch.is_grad_enabled():
+            raise ValueError("a cache has no gradient: detach k, v and q, or append under torch.no_grad()")
         kr, vr = self._rows(0, k, self.n_kv_heads, "k"), self._rows(1, v, self.n_kv_heads, "v", n)
         self._batch(table, lengths, offsets, n, 0)
         if (rotary is None) != (positions is None):
@@ -329,6 +359,8 @@ class KVCache:
         max_new: at least the largest count of new tokens (the fewer, the better the kernel chosen). mask: uint8
         [sequences, >= the longest], nonzero where a cached token may be seen. scale 0: head_dim ** -0.5."""
         n, index = q.shape[0], self._index
+        if q.requires_grad and torch.is_grad_enabled():
+            raise ValueError("attention over a cache has no gradient: detach q, or attend under torch.no_grad()")
         if out is None or lse is None:
             with _allocating(cuda_stream, index):
                 out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if out is None else out

@@ -72,3 +72,59 @@ def test_a_mask_of_no_tokens_hides_them_all(n):
             out, lse = cache.attend(_normal(n, 2, 64), table, lens, _ints(0, n), max_new=n, mask=mask)
             assert bool((out == 0).all()) and bool((lse == -float("inf")).all())
     cache.status()
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_rotary_joins_autograd(layout):
+    """Against the transposed rotation called by hand, which has tests of its own against the formula and differences."""
+    from paper_2609_03675_gb300 import Rotary
+    r = Rotary(64, rotary_dim=48, layout=layout, scaling="yarn", factor=2.0, original_len=4096)
+    n = 37
+    pos = torch.arange(n, dtype=torch.int32, device="cuda") * 91
+    x, y = _normal(n, 6, 64, dtype=torch.float32).requires_grad_(), _normal(n, 2, 64, seed=1, dtype=torch.float32).requires_grad_()
+    w, u = _normal(n, 6, 64, seed=2, dtype=torch.float32), _normal(n, 2, 64, seed=3, dtype=torch.float32)
+    a, b = r.apply((x, y), pos)
+    with torch.no_grad():
+        plain = r.apply((x, y), pos)
+        want = r.backward((w, u), pos)
+    assert not plain[0].requires_grad and torch.equal(a, plain[0]) and torch.equal(b, plain[1])
+    gx, gy = torch.autograd.grad((a, b), (x, y), (w, u))
+    assert torch.equal(gx, want[0]) and torch.equal(gy, want[1])
+    # a single tensor, a gradient without strides, another without its own
+    r.apply(x, pos).sum().backward()
+    assert torch.equal(x.grad, r.backward(torch.ones_like(w), pos)) and y.grad is None
+    z = y.detach()
+    one, _ = r.apply((x, z), pos)
+    assert torch.equal(torch.autograd.grad(one, x, w)[0], want[0])
+    # backward is linear too: its own gradient is apply
+    g = w.clone().requires_grad_()
+    back, = torch.autograd.grad(r.apply(x, pos), x, g, create_graph=True)
+    assert torch.equal(torch.autograd.grad(back, g, x.detach())[0], plain[0])
+    assert torch.equal(torch.autograd.grad(r.backward(g, pos), g, x.detach())[0], plain[0])
+    with pytest.raises(ValueError, match="out does not go"):
+        r.apply(x, pos, out=torch.empty_like(w))
+    kept = r.apply(x, pos)
+    pos += 1  # the gradient would be that of other positions
+    with pytest.raises(RuntimeError, match="modified"):
+        kept.sum().backward()
+
+
+def test_a_cache_has_no_gradient():
+    """Refused, not lost."""
+    from paper_2609_03675_gb300 import KVCache, Rotary
+    cache = KVCache(2, 16, 2, 1, 64, rotary=Rotary(64))
+    table, lens, pos = _ints(0, 1).view(1, 2), _ints(1), _ints(5)
+    k, v, q = _normal(1, 1, 64), _normal(1, 1, 64, seed=1), _normal(1, 2, 64, seed=2)
+    for i in range(3):
+        kvq = [x.clone().requires_grad_(i == j) for j, x in enumerate((k, v, q))]
+        call = lambda: cache.append(kvq[0], kvq[1], table, lens, positions=pos, q=kvq[2])  # noqa: E731
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+        with torch.no_grad():
+            call()
+    p = q.clone().requires_grad_()
+    with pytest.raises(ValueError, match="gradient"):
+        cache.attend(p, table, lens)
+    with torch.no_grad():
+        out, _ = cache.attend(p, table, lens)
+    assert torch.equal(out, cache.attend(p.detach(), table, lens)[0]) and not out.requires_grad

@@ -33,7 +33,8 @@ def positions_of(frames, device):
 
 
 def run(bits=4, steps=16, text=40, rho=0.3, seed=7):
-    """Returns (evidence frames, out of the question, outs of the steps)."""
+    """Returns (evidence frames, out of the question, outs of the steps, what they came from: the frames kept, every
+    token's key, value and position as they were made, the queries, the log-sum-exps, and what the cache holds in the end)."""
     dev = torch.device("cuda", torch.cuda.current_device())
     g = torch.Generator(device=dev).manual_seed(seed)
     normal = lambda n, h: torch.randn((n, h, HEAD_DIM), generator=g, device=dev).to(torch.bfloat16)  # noqa: E731
@@ -66,8 +67,8 @@ def run(bits=4, steps=16, text=40, rho=0.3, seed=7):
     at = torch.arange(max(frames) + 1, max(frames) + 1 + text + steps, dtype=torch.int32, device=dev).expand(3, -1).contiguous()
     offsets = torch.tensor([0, text], dtype=torch.int32, device=dev)
     length += text
-    rq = cache.append(k, v, table, length, offsets, positions=at[:, :text].contiguous(), q=q)
-    out, _ = cache.attend(rq, table, length, offsets, max_new=text, mask=mask)
+    asked = cache.append(k, v, table, length, offsets, positions=at[:, :text].contiguous(), q=q)
+    out, sums = cache.attend(asked, table, length, offsets, max_new=text, mask=mask)
 
     # the answer, token by token: one captured step, launched again with the next token's tensors in place
     x = normal(steps, HEADS + 2 * KV_HEADS)
@@ -80,7 +81,7 @@ def run(bits=4, steps=16, text=40, rho=0.3, seed=7):
         cache.append(nk, nv, table, length, positions=pos, q=nq, q_out=rq)
         cache.attend(rq, table, length, mask=mask, out=step_out, lse=lse)
 
-    outs = []
+    outs, queries, lses = [], [], [sums]
     length += 1
     step()  # before the capture: the mask's scratch is there from now on
     graph = torch.cuda.CUDAGraph()
@@ -93,8 +94,15 @@ def run(bits=4, steps=16, text=40, rho=0.3, seed=7):
             length += 1
         graph.replay()
         outs.append(step_out.clone())
+        queries.append(rq.clone())
+        lses.append(lse.clone())
+    total = seen + text + steps
+    held = cache.read(table, length, torch.tensor([0, total], dtype=torch.int32, device=dev), n_tokens=total)
     cache.status()
-    return [frames[i] for i in chosen.tolist()], out, outs
+    made = {"frames": frames, "per_frame": per_frame, "held": held, "queries": [asked, *queries], "lses": lses,
+            "raw_queries": torch.cat([q, x[:, :HEADS]]), "keys": torch.cat([keys, k, x[:, HEADS:HEADS + KV_HEADS]]),
+            "values": torch.cat([values, v, x[:, HEADS + KV_HEADS:]]), "positions": torch.cat([positions_of(frames, dev), at], 1)}
+    return [frames[i] for i in chosen.tolist()], out, outs, made
 
 
 def main():
@@ -102,7 +110,7 @@ def main():
     ap.add_argument("--bits", type=int, default=4, choices=(4, 16))
     ap.add_argument("--steps", type=int, default=16)
     a = ap.parse_args()
-    evidence, out, outs = run(a.bits, a.steps)
+    evidence, out, outs, _ = run(a.bits, a.steps)
     print(f"evidence frames {evidence}; question out {tuple(out.shape)}, |out| {out.float().norm():.4f}; "
           f"{len(outs)} steps, last |out| {outs[-1].float().norm():.4f}" if outs else "")
 

@@ -25,9 +25,9 @@
 //          value in [128, 256)), which keeps bf16's and fp16's bits;
 //   keys   a score is the sum over the groups of s sum q (n - z);
 //   values the sum over tokens has a scale for each: p s is rounded to fp16,
-//          after a power of two that keeps the largest scale met so far below
-//          2^15 (raised, and the output so far brought down, when a larger one
-//          comes).
+//          after a power of two that keeps the largest scale of its group met
+//          so far below 2^15 (raised, and the output so far brought down, when
+//          a larger one comes).
 // z is taken off the codes, in fp16, exactly. Taken off the sums it would cost
 // half the operations, but sums near zero would carry the rounding of sums of
 // codes (log-sum-exps of few tokens were off by 3e-6 of their size, not 4e-7).
@@ -315,8 +315,12 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
     // onto it, 16384 of a million that are 2^-25 of it (the log-sum-exp was 4e-4 off).
     constexpr uint32_t kSumChunks = 64;
     float o[NT][D / 16][4], m[NT][2], l[NT][2], l_part[NT][2];
-    float v_up = 1.f;               // 4-bit: the power of two on p s
-    uint32_t v_most = 0x000F000Fu;  // words up to which it holds, twice
+    // 4-bit: the power of two on p s, of each group (one for both would push the weights of a group whose values are
+    // a thousandth of the other's under fp16's range), and the words up to which they hold
+    float v_up[kGroups];
+    uint32_t v_most = 0x000F000Fu;
+#pragma unroll
+    for (int gr = 0; gr < kGroups; ++gr) v_up[gr] = 1.f;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -496,28 +500,31 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
 #pragma unroll
         for (int mt = 1; mt < kM; ++mt) most = __vmaxu2(most, __vmaxu2(ws[mt][0], ws[mt][1]));
         if (__any_sync(0xffffffffu, __vmaxu2(most, v_most) != v_most)) {  // a scale above all before
-          float x = 0.f;
 #pragma unroll
-          for (int mt = 0; mt < kM; ++mt)
+          for (int gr = 0; gr < kGroups; ++gr) {
+            float x = 0.f;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) x = fmaxf(x, fmaxf(scale_lo(ws[mt][e]), scale_hi(ws[mt][e])));  // a NaN is passed over
+            for (int mt = 0; mt < kM; ++mt)
 #pragma unroll
-          for (int w = 1; w < 32; w <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, w));
-          // scales below 2^(ex + 5) are then below 2^15, those at hand below 2^11
-          const int ex = max(static_cast<int>(__float_as_uint(x) >> 23) - 127, -100);
-          const uint32_t upto = static_cast<uint32_t>(min(ex + 4 + 127, 254)) << 7 | 0x7Fu;
-          if (x > 0.f && (upto | upto << 16) > v_most) {
-            const float up = __uint_as_float(static_cast<uint32_t>(127 + 10 - ex) << 23), k = v_most == 0x000F000Fu ? 1.f : up / v_up;
-            v_up = up;
-            v_most = upto | upto << 16;
+              for (int e = 0; e < 2; ++e) x = fmaxf(x, gr == 0 ? scale_lo(ws[mt][e]) : scale_hi(ws[mt][e]));  // a NaN is passed over
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
+            for (int w = 1; w < 32; w <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, w));
+            // scales below 2^(ex + 5) are then below 2^15, those at hand below 2^11
+            const int ex = max(static_cast<int>(__float_as_uint(x) >> 23) - 127, -100);
+            const uint32_t upto = static_cast<uint32_t>(min(ex + 4 + 127, 254)) << 7 | 0x7Fu, was = v_most >> (16 * gr) & 0xFFFFu;
+            if (x > 0.f && upto > was) {
+              const float up = __uint_as_float(static_cast<uint32_t>(127 + 10 - ex) << 23), k = was == 0x000Fu ? 1.f : up / v_up[gr];
+              v_up[gr] = up;
+              v_most = gr == 0 ? (v_most & 0xFFFF0000u) | upto : (v_most & 0xFFFFu) | upto << 16;
 #pragma unroll
-              for (int e = 0; e < D / 16; ++e) {
-                o[nt][e][0] *= k;
-                o[nt][e][1] *= k;
-                o[nt][e][2] *= k;
-                o[nt][e][3] *= k;
+              for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+                for (int e = 4 * gr; e < 4 * gr + 4; ++e) {
+                  o[nt][e][0] *= k;
+                  o[nt][e][1] *= k;
+                  o[nt][e][2] *= k;
+                  o[nt][e][3] *= k;
+                }
               }
             }
           }
@@ -534,8 +541,8 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
           }
 #pragma unroll
           for (int gr = 0; gr < kGroups; ++gr) {
-            const float s0 = (gr == 0 ? scale_lo(ws[mt][0]) : scale_hi(ws[mt][0])) * v_up;
-            const float s1 = (gr == 0 ? scale_lo(ws[mt][1]) : scale_hi(ws[mt][1])) * v_up;
+            const float s0 = (gr == 0 ? scale_lo(ws[mt][0]) : scale_hi(ws[mt][0])) * v_up[gr];
+            const float s1 = (gr == 0 ? scale_lo(ws[mt][1]) : scale_hi(ws[mt][1])) * v_up[gr];
             uint32_t pf[NT][2];
             const uint32_t z01 = __byte_perm(wa, wb, gr == 0 ? 0x5410 : 0x7632) & 0x000F000Fu,
                            z23 = __byte_perm(wc, wd, gr == 0 ? 0x5410 : 0x7632) & 0x000F000Fu;
@@ -564,13 +571,14 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
       }
     }
     if (BITS == 4) {  // to values: the powers of two back
-      const float back = 0x1p24f / v_up;
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+      for (int e = 0; e < D / 16; ++e) {
+        const float back = 0x1p24f / v_up[e / 4];
 #pragma unroll
-        for (int e = 0; e < D / 16; ++e)
+        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int f = 0; f < 4; ++f) o[nt][e][f] *= f < 2 ? back : back * 0.0625f;
+      }
     }
     cp_async_wait<0>();
     __syncthreads();  // every warp is done with its ring

@@ -105,3 +105,38 @@ def test_outputs_of_long_sums(dtype, bits, n, above, value):
 def test_outputs_of_sums_of_a_million_in_bf16():
     assert not bool(_run(torch.bfloat16, 16, 33, 15.0, 1.0, 1 << 20, 1)[0].any())
     _run.cache_clear()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("n", [1, 5, 17])
+@pytest.mark.parametrize("larger", [0, 1])
+def test_values_of_which_one_group_is_larger(dtype, n, larger):
+    """4-bit values of a head's two groups, one 1024 times the other's size: each against its own bound."""
+    from paper_2609_03675_gb300 import KVCache
+    seqs, m, h, d = SEQS, 262144, 2, 128
+    g = torch.Generator().manual_seed(n)
+    k = torch.zeros((m, 1, d), dtype=dtype)
+    k[1000, 0, 0] = 15.0
+    v = 1.0 + 0.25 * torch.randn((m, 1, d), generator=g)
+    v[1000] = 0.0
+    v[..., 64 * larger:64 * larger + 64] *= 1024.0
+    cache = KVCache(m // PAGE, PAGE, h, 1, d, dtype=dtype, bits=4)
+    held = []
+    for x, pages, scales in ((k, cache.k_pages, cache.k_scales), (v.to(dtype), cache.v_pages, cache.v_scales)):
+        b, w = K.pack(*K.quantise(x))
+        pages.copy_(b.view(m // PAGE, PAGE, 1, d // 2).transpose(1, 2))
+        scales.copy_(w.view(m // PAGE, PAGE, 1, d // 64).transpose(1, 2))
+        held.append(K.unpack(b, w)[0])
+    q = (0.5 * torch.randn((n, h, d), generator=g)).to(dtype)
+    q[..., 0] = 17.5 * d ** 0.5 / 15.0
+    table = torch.arange(m // PAGE, dtype=torch.int32, device="cuda").repeat(seqs, 1)
+    lens = torch.full((seqs,), m, dtype=torch.int32, device="cuda")
+    offsets = torch.arange(seqs + 1, dtype=torch.int32, device="cuda") * n
+    out, lse = cache.attend(q.cuda().repeat(seqs, 1, 1), table, lens, offsets, max_new=n)
+    cache.status()
+    seen = torch.arange(m)[None] <= (m - n + torch.arange(n))[:, None]
+    chain = m // 8 if n * h <= 32 else 8192 if dtype == torch.float16 else 65536
+    for part in (slice(0, 64), slice(64, 128)):
+        want = B.attend(q, held[0], held[1][..., part], seen, d ** -0.5, dtype, chain)
+        bad = B.exceeds(out.view(seqs, n, h, d)[..., part], lse.view(seqs, n, h), want)
+        assert not bool(bad[0].any()) and not bool(bad[1].any()), part

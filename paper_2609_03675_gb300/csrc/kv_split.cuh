@@ -573,11 +573,11 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
     if (BITS == 4) {  // to values: the powers of two back
 #pragma unroll
       for (int e = 0; e < D / 16; ++e) {
-        const float back = 0x1p24f / v_up[e / 4];
+        const float back = 1.f / v_up[e / 4];  // (with the 2^24 it may pass fp32's range)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int f = 0; f < 4; ++f) o[nt][e][f] *= f < 2 ? back : back * 0.0625f;
+          for (int f = 0; f < 4; ++f) o[nt][e][f] = o[nt][e][f] * (f < 2 ? 0x1p24f : 0x1p20f) * back;
       }
     }
     cp_async_wait<0>();

@@ -140,3 +140,25 @@ def test_values_of_which_one_group_is_larger(dtype, n, larger):
         want = B.attend(q, held[0], held[1][..., part], seen, d ** -0.5, dtype, chain)
         bad = B.exceeds(out.view(seqs, n, h, d)[..., part], lse.view(seqs, n, h), want)
         assert not bool(bad[0].any()) and not bool(bad[1].any()), part
+
+
+@pytest.mark.parametrize("n", [1, 17])
+@pytest.mark.parametrize("size", [2.0 ** -90, 2.0 ** -60, 2.0 ** 60, 2.0 ** 100, 2.0 ** 118])
+def test_values_of_any_size_in_4_bits(n, size):
+    """bf16 has the exponents of fp32: values near either end (not so near that their sums pass it)."""
+    from paper_2609_03675_gb300 import KVCache
+    m, h, d = 90, 2, 64
+    g = torch.Generator().manual_seed(n)
+    k = torch.randn((m, 1, d), generator=g).to(torch.bfloat16)
+    v = (torch.randn((m, 1, d), generator=g).clamp(-4, 4) * size).to(torch.bfloat16)
+    cache = KVCache(6, 16, h, 1, d, bits=4)
+    table = torch.arange(6, dtype=torch.int32, device="cuda").view(1, -1)
+    lens, offsets = torch.tensor([m], dtype=torch.int32, device="cuda"), torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    cache.append(k.cuda(), v.cuda(), table, lens, torch.tensor([0, m], dtype=torch.int32, device="cuda"))
+    q = (0.3 * torch.randn((n, h, d), generator=g)).to(torch.bfloat16)
+    out, lse = cache.attend(q.cuda(), table, lens, offsets, max_new=n)
+    cache.status()
+    k, v = (K.unpack(*K.pack(*K.quantise(x)))[0] for x in (k, v))
+    seen = torch.arange(m)[None] <= (m - n + torch.arange(n))[:, None]
+    bad = B.exceeds(out.double() / size, lse, B.attend(q, k, v / size, seen, d ** -0.5, torch.bfloat16))
+    assert not bool(bad[0].any()) and not bool(bad[1].any())

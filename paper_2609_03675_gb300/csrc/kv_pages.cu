@@ -373,6 +373,8 @@ int cofie_kv_create(const cofie_kv_params* p, cofie_kv_t** out) {
   cudaError_t e = injected_alloc_failure() ? cudaErrorMemoryAllocation : cudaMalloc(&h->d_err, sizeof(uint32_t));
   if (e == cudaSuccess) e = cudaMemset(h->d_err, 0, sizeof(uint32_t));
   if (e == cudaSuccess) e = attend_set_up(h);
+  // the words are cleared on the default stream: streams that do not wait for it may be the first to use them
+  if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);
   if (e != cudaSuccess) {
     g_kv_error = std::string("cache set-up failed: ") + cudaGetErrorString(e);
     cudaGetLastError();
@@ -464,7 +466,7 @@ int cofie_kv_status(cofie_kv_t* h, void* cuda_stream) {
   cudaError_t e = cudaStreamSynchronize(static_cast<cudaStream_t>(cuda_stream));
   uint32_t word = 0;
   if (e == cudaSuccess) e = cudaMemcpy(&word, h->d_err, sizeof word, cudaMemcpyDeviceToHost);
-  if (e == cudaSuccess && word) e = cudaMemset(h->d_err, 0, sizeof word);
+  if (e == cudaSuccess && word) e = cudaMemsetAsync(h->d_err, 0, sizeof word, static_cast<cudaStream_t>(cuda_stream));
   if (e != cudaSuccess) return launched(h, e, "status");
   if (word & kKvErrWait) return h->fail(COFIE_ETIMEOUT, "a device-side wait of the attention kernel ran out");
   if (word & kKvErrPage) return h->fail(COFIE_EDEVICE, "a page number in the table is not below n_pages");

@@ -128,3 +128,24 @@ def test_a_cache_has_no_gradient():
     with torch.no_grad():
         out, _ = cache.attend(p, table, lens)
     assert torch.equal(out, cache.attend(p.detach(), table, lens)[0]) and not out.requires_grad
+
+
+def test_a_new_cache_is_ready_on_every_stream():
+    """Its counters are cleared on the default stream, for which a stream of the caller's need not wait."""
+    from paper_2609_03675_gb300 import KVCache
+    k, v = (torch.zeros((64, 1, 16, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    KVCache(64, 16, 2, 1, 64, k_pages=k, v_pages=v)  # the library is loaded
+    torch.cuda.synchronize()
+    torch.cuda._sleep(200_000_000)  # a tenth of a second of the default stream
+    cache = KVCache(64, 16, 2, 1, 64, k_pages=k, v_pages=v)
+    assert torch.cuda.default_stream().query()
+    side = torch.cuda.Stream()
+    x, y, q = _normal(1000, 1, 64), _normal(1000, 1, 64, seed=1), _normal(1, 2, 64, seed=2)
+    table, lens, offsets = torch.arange(64, dtype=torch.int32, device="cuda").view(1, -1), _ints(1000), _ints(0, 1000)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        cache.append(x, y, table, lens, offsets)
+        a = cache.attend(q, table, lens)
+        b = cache.attend(q, table, lens)
+        cache.status()
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]) and bool(torch.isfinite(a[1]).all())

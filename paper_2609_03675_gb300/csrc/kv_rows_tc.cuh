@@ -77,16 +77,16 @@ struct TcSmem {
   uint32_t tmem, stop, last_here;
 };
 
-// A wait for a barrier's phase that ends, with false, when it runs out or another's has.
+// A wait for a barrier's phase that ends, with false, when it runs out or another's has (with stop).
 __device__ __forceinline__ bool tc_wait_slow(uint32_t bar, uint32_t parity, volatile uint32_t* stop) {
   const uint64_t t0 = globaltimer_ns();
   for (;;) {
 #pragma unroll 1
     for (int i = 0; i < 16; ++i)
       if (mbar_try_wait(bar, parity)) return true;
-    if (*stop) return false;
+    if (stop && *stop) return false;
     if (globaltimer_ns() - t0 > kTcTimeout) {
-      *stop = 1;
+      if (stop) *stop = 1;
       return false;
     }
   }
@@ -787,9 +787,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
         s_n += tiles;
         n += tiles;
       }
-      // what was issued, and its arrivals, finish before the tensor memory goes and the CTA ends
+      // what was issued, and its arrivals, finish before the tensor memory goes and the CTA ends: waited for even when
+      // another wait has run out
       tc_commit(leader, &sm.drained);
-      if (!tc_wait(&sm.drained, 0, stop)) atomicOr(b.err, kKvErrWait);
+      if (!tc_wait(&sm.drained, 0, nullptr)) atomicOr(b.err, kKvErrWait);
       __syncwarp();
     }
   }

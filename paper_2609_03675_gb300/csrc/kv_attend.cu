@@ -142,6 +142,8 @@ extern "C" int cofie_kv_attend(cofie_kv_t* h, const cofie_kv_batch* b, const cof
   if (b->n_tokens == 0) return COFIE_OK;
   if (!q) return h->fail(COFIE_EINVAL, "q is required");
   if (const int rc = check_rows(h, q, h->p.n_heads, true, "q")) return rc;
+  if (q->in == q->out && ((b->n_tokens > 1 && q->in_token != q->out_token) || (q->heads > 1 && q->in_head != q->out_head)))
+    return h->fail(COFIE_EINVAL, "in place, the strides of q's in and out must be the same");
   if (!(scale >= 0.f && std::isfinite(scale))) return h->fail(COFIE_EINVAL, "scale must be finite and not negative");
   DeviceGuard g(h->device);
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);

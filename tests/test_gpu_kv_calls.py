@@ -149,3 +149,25 @@ def test_a_new_cache_is_ready_on_every_stream():
         b = cache.attend(q, table, lens)
         cache.status()
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1]) and bool(torch.isfinite(a[1]).all())
+
+
+@pytest.mark.parametrize("bits", [16, 4])
+@pytest.mark.parametrize("n", [1, 5, 90])
+def test_outputs_in_the_queries_place(bits, n):
+    """With the queries' strides; with others it is refused, as for rotated queries."""
+    from paper_2609_03675_gb300 import KVCache, NGFFError
+    h, kv, d = 8, 2, 64
+    cache = KVCache(64, 64, h, kv, d, bits=bits)
+    table, lens, offsets = torch.arange(64, dtype=torch.int32, device="cuda").view(1, -1), _ints(4000), _ints(0, 4000)
+    cache.append(_normal(4000, kv, d), _normal(4000, kv, d, seed=1), table, lens, offsets)
+    q = _normal(n, h, d, seed=2)
+    want = cache.attend(q, table, lens, _ints(0, n), max_new=n)
+    with pytest.raises(NGFFError, match="in place"):
+        cache.attend(q, table, lens, _ints(0, n), max_new=n, out=q.view(-1).as_strided((n, h, d), (d, n * d, 1) if n > 1 else (h * d, 0, 1)))
+    if n == 1:  # a stride that nothing is at
+        other = q.clone()
+        out, lse = cache.attend(other, table, lens, out=other.as_strided((1, h, d), (h * d + 64, d, 1)))
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+    out, lse = cache.attend(q, table, lens, _ints(0, n), max_new=n, out=q)
+    cache.status()
+    assert out is q and torch.equal(out, want[0]) and torch.equal(lse, want[1])

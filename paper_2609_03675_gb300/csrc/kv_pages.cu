@@ -152,13 +152,17 @@ __global__ void __launch_bounds__(kThreads, 4) append_codes(const __grid_constan
       // and the product and the zero point are summed and rounded once, to the
       // last bit of 1.5 2^23. No quotient of 16-bit x lies that close to a half
       // without being one, but one of rotated keys, which are fp32 numbers, may:
-      // for those x - code scale, which is exact, is held against half a scale.
+      // where the reciprocal two below its value gives another code, x - code
+      // scale, which is exact, is held against half a scale. (75000 appended
+      // tokens take 152 us so, 154 with every key held against it, and 135 took
+      // those whose codes could be the next.)
       uint32_t word[2], codes8[2];
-      float inv[2], zero[2], step[2];
+      float inv[2], low[2], zero[2], step[2];
 #pragma unroll
       for (int gr = 0; gr < kOwn; ++gr) {
         const float scale = group_scale(lo[gr], hi[gr]);
         asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv[gr]) : "f"(scale));
+        low[gr] = scale > 0.f ? __uint_as_float(__float_as_uint(inv[gr]) - 2) : 0.f;
         inv[gr] = scale > 0.f ? __uint_as_float(__float_as_uint(inv[gr]) + 2) : 0.f;
         float near = __fmaf_rn(-lo[gr], inv[gr], 12582912.f);
         if (turned) near = code_back(near, 12582912.f, -lo[gr], scale);
@@ -172,13 +176,18 @@ __global__ void __launch_bounds__(kThreads, 4) append_codes(const __grid_constan
         uint32_t w = 0;
         const int gr = kOwn == 1 ? 0 : e;
         const auto code = [&](int i) { return __fmaf_rn(x[8 * e + i], inv[gr], zero[gr]); };
+        if (!turned) {
 #pragma unroll
-        for (int i = 7; i >= 0; --i) w = w * 16 + __float_as_uint(fminf(code(i), 12582927.f));
-        if (turned) {  // looked at apart, since there is seldom one to put right (codes kept for it cost 22 us of 225)
-          float most = 0.f;
+          for (int i = 7; i >= 0; --i) w = w * 16 + __float_as_uint(fminf(code(i), 12582927.f));
+        } else {
+          uint32_t apart = 0;  // codes that the reciprocal two below its value gives otherwise
 #pragma unroll
-          for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(__fmaf_rn(zero[gr] - code(i), step[gr], x[8 * e + i])));
-          if (most > 0.5f * step[gr]) {
+          for (int i = 7; i >= 0; --i) {
+            const float c1 = code(i);
+            apart |= __float_as_uint(c1) ^ __float_as_uint(__fmaf_rn(x[8 * e + i], low[gr], zero[gr]));
+            w = w * 16 + __float_as_uint(fminf(c1, 12582927.f));
+          }
+          if (apart) {
             w = 0;
 #pragma unroll
             for (int i = 7; i >= 0; --i) w = w * 16 + __float_as_uint(fminf(code_back(code(i), zero[gr], x[8 * e + i], step[gr]), 12582927.f));

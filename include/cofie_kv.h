@@ -25,7 +25,9 @@
  *              serves 64 consecutive codes: with its low four bits cleared it
  *              is the bf16 scale s (4 significant bits), its low four bits are
  *              the zero point z. Code n stands for (n - z) s, which bf16 holds
- *              exactly (fp16 too, where s is in its normal range).
+ *              exactly (fp16 too, for s from 2^-21 and as long as it does not
+ *              pass 65504: cofie_kv_read, and attention of more than 32 rows of a
+ *              sequence and key head, see it as a number of the cache's type).
  *   Codes of x (64 values, rotated keys as fp32 numbers; hi - lo is formed in
  *   fp32, all else exactly): lo = min(0, min x), hi = max(0, max x),
  *   s = (hi - lo) / 15 rounded up to 4 significant bits (0 below 2^-100),
@@ -61,7 +63,9 @@ extern "C" {
  *   BASE    base times factor^(rotary_dim / (rotary_dim - 2))
  *   YARN    (1 - g) f_i / factor + g f_i, g = (r - slow) / (fast - slow) cut to
  *           [0, 1], r = original_len f_i / (2 pi) the pair's turns over the
- *           trained length; m = 0.1 ln(factor) + 1 (Peng et al. 2023, "YaRN")
+ *           trained length; m = 0.1 ln(factor) + 1 (Peng et al. 2023, "YaRN").
+ *           This is the paper's g, linear in the turns; programs that make g
+ *           linear in i between two whole numbers get other frequencies.
  * Angles are formed as 64-bit fractions of a turn, so that a position up to
  * 2^31 costs no accuracy.
  * ------------------------------------------------------------------------ */
@@ -143,7 +147,8 @@ typedef struct {
   const int32_t* offsets;  /* [n_seqs + 1], device memory, or NULL: one token each (n_tokens = n_seqs) */
 } cofie_kv_batch;
 
-/* Validates *p and allocates the handle's scratch. Synchronous. Errors: COFIE_EINVAL, COFIE_ENOMEM, COFIE_ECUDA. */
+/* Validates *p and allocates the handle's scratch (about 40 MB of device memory at head_dim 128, 20 MB at 64).
+ * Synchronous: it waits for the default stream. Errors: COFIE_EINVAL, COFIE_ENOMEM, COFIE_ECUDA. */
 int cofie_kv_create(const cofie_kv_params* p, cofie_kv_t** out);
 void cofie_kv_destroy(cofie_kv_t* h);
 
@@ -170,7 +175,12 @@ int cofie_kv_read(cofie_kv_t* h, const cofie_kv_batch* b, void* k_out, void* v_o
  * Query token i of n new ones sees cached token j of m when j <= m - n + i
  * (causal; every j < m otherwise) and mask[s mask_stride + j] is nonzero:
  *   out = sum_j p_j v_j, p = softmax_j(scale <q, k_j>), lse = ln sum_j exp(scale <q, k_j>)
- * in fp32, out rounded once to the cache's type. A row that sees nothing gets
+ * Products are of 16-bit numbers, sums in fp32. The weights exp(scale <q, k_j>)
+ * are rounded to 16 bits for their product with the values (to the cache's type,
+ * of up to 2^8 or 2^11 for fp16; for at most 32 rows over 4-bit pages to fp16,
+ * times the values' scale) and not for lse; over 4-bit pages such rows' queries
+ * are taken to fp16 with a power of two for each row, which is meant for queries
+ * below 2^110. out is rounded to the cache's type. A row that sees nothing gets
  * out = 0, lse = -infinity; what a masked or unwritten place holds (NaN too)
  * never matters. (A NaN or an infinity among a call's own new values may reach
  * all new rows of its sequence, those before it too.)

@@ -204,8 +204,12 @@ extern "C" int cofie_kv_attend(cofie_kv_t* h, const cofie_kv_batch* b, const cof
   // block; more rows pay for tiles of 128 of them. Eight sequences of up to 60000 tokens, 32 heads over 8 of 128 (us,
   // blocks / tiles): 20 rows 176 / 233 with 4 bits, 214 / 337 with 16; 32 rows 188 / 234, 262 / 339; 48 rows 266 / 234,
   // 344 / 340. Up to 2000 tokens: 20 rows 25 / 28, 22 / 32; 48 rows 32 / 29, 27 / 34.
-  // What an item costs beside its tiles' slots (set-up, first loads, its part's joining): with 6, 16 and 24 of them for
-  // many rows seven ragged questions took 98, 107 and 116 us; with 2, 4 and 6 for few, 24 streams' evidence 72, 67 and 63.
+  // What an item costs beside its tiles' slots (set-up, first loads, its part's joining), in the time of a tile: about 8 for
+  // many rows and 6 for few, at every size tried. Many rows, us with 4 / 8 / 16 / 24 slots: seven questions of 3 to 300
+  // tokens over up to 4000 of 4 bits 91 / 85 / 89 / 95, four prompts of 1024 over up to 8192 of 16 bits 451 / 343 / 371 /
+  // 394, thirty of 16 over up to 2000 87 / 91 / 97 / 103. Few, with 2 / 4 / 6 / 8 / 12: 24 x 3 tokens over up to 9000 of
+  // 4 bits 91 / 79 / 72 / 69 / 62, 64 x 1 over up to 20000 of 4 bits 220 / 212 / 200 / 197 / 199, of 16 bits 419 / 402 /
+  // 400 / 394 / 398, 8 x 1 over up to 3000 27 / 25 / 23 / 25 / 25.
   if (rows > 32) {
     const SplitKernel k = rows_kernel(h->p, &smem);
     a.item_slots = 8;

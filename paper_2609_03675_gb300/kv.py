@@ -356,7 +356,8 @@ class KVCache:
     def attend(self, q, table, lengths, offsets=None, *, max_new=0, mask=None, causal=True, scale=0.0, out=None, lse=None,
                cuda_stream=None):
         """(out, lse) of the batch's new queries over their sequences' cached tokens; out like q, lse fp32 [tokens, heads].
-        max_new: at least the largest count of new tokens (the fewer, the better the kernel chosen). mask: uint8
+        max_new: at least the largest count of new tokens. It chooses the kernel (with offsets and 0, all tokens are taken
+        for one sequence's, and many short sequences run the kernel of long questions). mask: uint8
         [sequences, >= the longest], nonzero where a cached token may be seen. scale 0: head_dim ** -0.5."""
         n, index = q.shape[0], self._index
         if q.requires_grad and torch.is_grad_enabled():

@@ -298,11 +298,14 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
       // The sum of the weights, and what its roundings left out: a row's tokens may all come to one thread, and
       // 262144 of them 17.5 below a first one, added to it as they came, were off by 1.7e-3 in the log-sum-exp.
       float m = -INFINITY, l = 0.f, l_rest = 0.f;
-      // Sums that have left tensor memory are kept in this row of the part, against the maximum of then; in O's order of
-      // columns. (An item that is this CTA's alone uses the part of the one that goes on from it, which comes last.)
+      // Sums that have left tensor memory are kept in the CTA's part, against the maximum of then: four of O's columns of a
+      // row beside those of the next row. (Four prompts of 2048 fp16 tokens over 65536: 11.03 ms; with a row's columns one
+      // after the other 11.42, with O left in tensor memory throughout 10.72.) An item that is this CTA's alone uses the part
+      // of the one that goes on from it, which comes last.
       float kept_m = -INFINITY;
       const uint32_t lr = t * 128 + r;  // row of the item's 256
       const auto own_part = [&] { return (2ull * blockIdx.x + (blockIdx.x == it.first_cta ? 1 : 0)) * kTcRows; };
+      const auto kept_at = [&](int col) { return reinterpret_cast<float4*>(a.part + own_part() * D) + col / 4 * kTcRows + lr; };
       if (active && tiles) {
         {  // the row of Q into shared memory; codes' products come in the order in which they are unpacked
           const T* q = reinterpret_cast<const T*>(a.q.in) + static_cast<int64_t>(it.span.first + token) * a.q.in_token +
@@ -341,18 +344,19 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
             ok = __all_sync(0xffffffffu, ok);
             tc_fence_after();
             const float k = kept_m == -INFINITY ? 0.f : exp2_fast(kept_m - m);
-            float* const kept = a.part + (own_part() + lr) * D;
 #pragma unroll 1
-            for (int e = 0; e < D / 16; ++e) {
-              uint32_t z[16];
-              tc_ld16(o_col + 16 * e, z);
+            for (int e = 0; e < D / 32; ++e) {
+              float4 was[8];
+              uint32_t z[32];
 #pragma unroll
-              for (int f = 0; f < 16; f += 4) {
-                float4* const at = reinterpret_cast<float4*>(kept + 16 * e + f);
-                const float4 was = j == kTcChain<T> ? make_float4(0.f, 0.f, 0.f, 0.f) : *at;
-                *at = make_float4(fmaf(was.x, k, __uint_as_float(z[f])), fmaf(was.y, k, __uint_as_float(z[f + 1])),
-                                  fmaf(was.z, k, __uint_as_float(z[f + 2])), fmaf(was.w, k, __uint_as_float(z[f + 3])));
-              }
+              for (int f = 0; f < 8; ++f) was[f] = j == kTcChain<T> ? make_float4(0.f, 0.f, 0.f, 0.f) : *kept_at(32 * e + 4 * f);
+              tc_ld32(o_col + 32 * e, z);
+              tc_wait_ld(z);
+#pragma unroll
+              for (int f = 0; f < 8; ++f)
+                *kept_at(32 * e + 4 * f) =
+                    make_float4(fmaf(was[f].x, k, __uint_as_float(z[4 * f])), fmaf(was[f].y, k, __uint_as_float(z[4 * f + 1])),
+                                fmaf(was[f].z, k, __uint_as_float(z[4 * f + 2])), fmaf(was[f].w, k, __uint_as_float(z[4 * f + 3])));
             }
             kept_m = m;
           }
@@ -435,14 +439,32 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
         ok = __all_sync(0xffffffffu, ok);
         tc_fence_after();
         l += l_rest;
+        if (tiles > kTcChain<T>) {  // what was kept comes back
+          const float k = kept_m == -INFINITY ? 0.f : exp2_fast(kept_m - m);
+#pragma unroll 1
+          for (int e = 0; e < D / 16; ++e) {
+            float4 was[4];
+            uint32_t z[16];
+#pragma unroll
+            for (int f = 0; f < 4; ++f) was[f] = *kept_at(16 * e + 4 * f);
+            tc_ld16(o_col + 16 * e, z);
+#pragma unroll
+            for (int f = 0; f < 4; ++f) {
+              z[4 * f] = __float_as_uint(fmaf(was[f].x, k, __uint_as_float(z[4 * f])));
+              z[4 * f + 1] = __float_as_uint(fmaf(was[f].y, k, __uint_as_float(z[4 * f + 1])));
+              z[4 * f + 2] = __float_as_uint(fmaf(was[f].z, k, __uint_as_float(z[4 * f + 2])));
+              z[4 * f + 3] = __float_as_uint(fmaf(was[f].w, k, __uint_as_float(z[4 * f + 3])));
+            }
+            tc_st16(o_col + 16 * e, z);
+          }
+          tc_wait_st();
+        }
       }
       // info of tiles that this half does not use
       if (!active) n += tiles;
       const bool alone = it.first_cta == it.last_cta;
       const uint64_t part = own_part();
-      const float* const kept = a.part + (part + lr) * D;
-      const bool some_kept = tiles > kTcChain<T>;
-      const float kept_by = kept_m == -INFINITY ? 0.f : exp2_fast(kept_m - m);
+      if (tiles > kTcChain<T> && !alone) bar_sync<1, kTcSoftmax>();  // all have what they kept, before the part is written
       const float inv = l == 0.f ? 0.f : 1.f / l;
       T* out = reinterpret_cast<T*>(a.q.out) + static_cast<int64_t>(it.span.first + token) * a.q.out_token +
                static_cast<int64_t>(head) * a.q.out_head;
@@ -464,12 +486,6 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
               float z[8];
 #pragma unroll
               for (int i = 0; i < 8; ++i) z[BITS == 4 ? order[i] : i] = __uint_as_float(y[8 * f + i]);
-              if (some_kept) {  // this thread's own, read before it is written over
-                const float4 u = *reinterpret_cast<const float4*>(kept + 32 * e + 8 * f), w = *reinterpret_cast<const float4*>(kept + 32 * e + 8 * f + 4);
-                const float x[8] = {u.x, u.y, u.z, u.w, w.x, w.y, w.z, w.w};
-#pragma unroll
-                for (int i = 0; i < 8; ++i) z[BITS == 4 ? order[i] : i] = fmaf(x[i], kept_by, z[BITS == 4 ? order[i] : i]);
-              }
               if (l == 0.f)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) z[i] = 0.f;

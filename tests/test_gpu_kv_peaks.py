@@ -21,7 +21,7 @@ def _cuda():
 
 
 @functools.lru_cache(maxsize=1)
-def _run(dtype, bits, n, above, value, M=262144, H=2):
+def _run(dtype, bits, n, above, value, M=262144, H=2, seqs=SEQS):
     """(outputs, log-sum-exps) of n new tokens that pass their bounds; key 1000 lies `above` the others, its value is
     `value`, theirs are about 1."""
     from paper_2609_03675_gb300 import KVCache
@@ -42,14 +42,14 @@ def _run(dtype, bits, n, above, value, M=262144, H=2):
         k, v = (K.unpack(*K.pack(*K.quantise(x)))[0] for x in (k, v))
     q = (0.5 * torch.randn((n, H, D), generator=g)).to(dtype)
     q[..., 0] = above * D ** 0.5 / 15.0
-    table = torch.arange(M // PAGE, dtype=torch.int32, device="cuda").repeat(SEQS, 1)
-    lens = torch.full((SEQS,), M, dtype=torch.int32, device="cuda")
-    offsets = torch.arange(SEQS + 1, dtype=torch.int32, device="cuda") * n
-    out, lse = cache.attend(q.cuda().repeat(SEQS, 1, 1), table, lens, offsets, max_new=n)
+    table = torch.arange(M // PAGE, dtype=torch.int32, device="cuda").repeat(seqs, 1)
+    lens = torch.full((seqs,), M, dtype=torch.int32, device="cuda")
+    offsets = torch.arange(seqs + 1, dtype=torch.int32, device="cuda") * n
+    out, lse = cache.attend(q.cuda().repeat(seqs, 1, 1), table, lens, offsets, max_new=n)
     cache.status()
     seen = torch.arange(M)[None] <= (M - n + torch.arange(n))[:, None]
     chain = M // 8 if n * H <= 32 else 8192 if dtype == torch.float16 else 65536
-    return B.exceeds(out.view(SEQS, n, H, D), lse.view(SEQS, n, H), B.attend(q, k, v, seen, D ** -0.5, dtype, chain))
+    return B.exceeds(out.view(seqs, n, H, D), lse.view(seqs, n, H), B.attend(q, k, v, seen, D ** -0.5, dtype, chain))
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
@@ -162,3 +162,12 @@ def test_values_of_any_size_in_4_bits(n, size):
     seen = torch.arange(m)[None] <= (m - n + torch.arange(n))[:, None]
     bad = B.exceeds(out.double() / size, lse, B.attend(q, k, v / size, seen, d ** -0.5, torch.bfloat16))
     assert not bool(bad[0].any()) and not bool(bad[1].any())
+
+
+@pytest.mark.parametrize("dtype,m", [(torch.float16, 96000), (torch.bfloat16, 640000)])
+@pytest.mark.parametrize("bits", [16, 4])
+def test_outputs_of_long_sums_that_are_joined(dtype, m, bits):
+    """A row's tokens lie with several CTAs, with each more of them than a sum holds."""
+    bad = _run(dtype, bits, 17, 15.0, 1.0, m, 2, 20)
+    assert not bool(bad[0].any()) and not bool(bad[1].any())
+    _run.cache_clear()

@@ -320,8 +320,8 @@ def prepare(case, seed):
         rotary = None
         if c["op"] == "append":
             rotary = Rotary(d, rotary_dim=c["rotary_dim"], base=1e6, layout=c["layout"], axes=_axes(c) if c["axes"] > 1 else None)
-        s["cache"] = KVCache(pages, page, h, hk, d, dtype=dtype, bits=c["bits"], rotary=rotary, k_pages=s["k_pages"],
-                             v_pages=s["v_pages"], k_scales=s["k_scales"], v_scales=s["v_scales"])
+        s["cache"] = KVCache(pages, page, h, hk, d, dtype=dtype, bits="int8" if c["bits"] == 8 else c["bits"], rotary=rotary,
+                             k_pages=s["k_pages"], v_pages=s["v_pages"], k_scales=s["k_scales"], v_scales=s["v_scales"])
     return s
 
 

@@ -14,7 +14,8 @@ Kinds of case (the "op" of a case dict):
 A sequence's cached tokens lie in pages of "page" tokens, whose numbers a table gives in no order; a group's prefix has a
 row of such a table of its own. Pages hold rows [page][head][token][dim] of 16-bit values, of bytes, or of 4-bit codes, two
 to a byte. Beside bytes and codes lies a word for every 64 of them. 8 bits: a byte u and a scale s, a power of two as a bf16
-number, stand for (u - 128) s; s is the smallest that brings all 64 values to 127 at most. 4 bits: the word is a bf16 scale
+number, stand for (u - 128) s; s is the smallest that brings all 64 values to 127 at most (of those whose 127 the type
+holds; past that, values are cut). 4 bits: the word is a bf16 scale
 of 4 significant bits, with the zero point in its low 4 bits.
 """
 from __future__ import annotations
@@ -27,8 +28,8 @@ own = False
 
 GROUP = 64  # values that share a scale
 TYPES = {"bf16": torch.bfloat16, "fp16": torch.float16}
-LEAST = {"bf16": -100, "fp16": -24}  # exponent of the smallest scale of 8-bit codes
-RANGE = {"bf16": 128, "fp16": 16}    # the type holds what is below 2 to this
+LEAST = {"bf16": -100, "fp16": -24}  # exponents of the smallest scale of 8-bit codes
+MOST = {"bf16": 121, "fp16": 9}      # and of the largest: the type holds 127 of it
 
 
 def _append(name, seqs, new, before, **kw):
@@ -213,11 +214,9 @@ def _bytes_of(x, kind):
     y = x.float().unflatten(-1, (-1, GROUP))
     top = y.abs().amax(-1)
     # top = f 2^e, f in [1, 2): 2^(e - 6) is enough for f up to 127 / 64; the sum carries into the exponent above that
-    field = (((top.view(torch.int32) + 0x1FFFF) >> 23) - 6).clamp(min=127 + LEAST[kind])
+    field = (((top.view(torch.int32) + 0x1FFFF) >> 23) - 6).clamp(127 + LEAST[kind], 127 + MOST[kind])
     inverse = ((254 - field) << 23).view(torch.float32)
-    n = torch.round(y * inverse.unsqueeze(-1))  # halves to even
-    most = ((1 << (RANGE[kind] + 127 - field).clamp(max=7)) - 1).unsqueeze(-1)
-    n = torch.minimum(torch.maximum(n, -most), most)
+    n = torch.round(y * inverse.unsqueeze(-1)).clamp(-127, 127)  # halves to even
     return (n + 128).to(torch.uint8).flatten(-2), (field << 7).to(torch.int16)
 
 
@@ -462,9 +461,9 @@ def _exact_eight_bits(x, kind):
     """The whole multiple of its group's scale nearest to each x."""
     y = x.double().reshape(*x.shape[:-1], -1, GROUP)
     part, power = torch.frexp(y.abs().max(-1, keepdim=True).values)
-    power = torch.where(part <= 127 / 128, power - 7, power - 6).clamp(min=LEAST[kind])
+    power = torch.where(part <= 127 / 128, power - 7, power - 6).clamp(LEAST[kind], MOST[kind])
     step = (power.long() + 1023 << 52).view(torch.float64)  # 2^power to the last bit, which ldexp is not
-    return (torch.round(y / step) * step).reshape(x.shape)
+    return (torch.round(y / step).clamp(-127, 127) * step).reshape(x.shape)
 
 
 def _held(s, name, rows, c):

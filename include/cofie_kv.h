@@ -1,7 +1,7 @@
 /*
  * cofie_kv.h -- the part of libcofie_ngff.so that answers from the selected
- * frames: rotary positions, a paged key/value cache of 16-bit values or 4-bit
- * codes, and attention over that cache. It follows the selection of evidence
+ * frames: rotary positions, a paged key/value cache of 16-bit values, bytes or
+ * 4-bit codes, and attention over that cache. It follows the selection of evidence
  * (CoFiE Sec. 3.3: once the frames are ranked, the positional embeddings and
  * the keys and values of the kept ones go on, those of the others do not).
  *
@@ -19,6 +19,16 @@
  *
  * Pages: [n_pages][n_kv_heads][page_size][row], keys and values apart.
  *   bits = 16  a row is head_dim values of the cache's type.
+ *   bits = COFIE_KV_INT8  a row is head_dim bytes, and beside the pages lie the
+ *              scale words, [n_pages][n_kv_heads][page_size][head_dim / 64]
+ *              uint16. A word serves 64 consecutive bytes and is the bf16 number
+ *              s, a power of two. Byte u stands for (u - 128) s, which bf16 and
+ *              fp16 hold exactly.
+ *   Bytes of x (64 values, rotated keys as fp32 numbers): s is the smallest
+ *   power of two with max |x| <= 127 s, but at least 2^-100 and at most 2^121
+ *   (bf16) or at least 2^-24 and at most 2^9 (fp16); u = 128 + [x / s], [] to the
+ *   nearest, halves to the even one, cut to -127..127. A group that holds a NaN
+ *   or an infinity reads as NaN.
  *   bits = 4   a row is head_dim codes, two to a byte (the even dimension in
  *              the low four bits), and beside the pages lie the scale words,
  *              [n_pages][n_kv_heads][page_size][head_dim / 64] uint16. A word
@@ -51,6 +61,9 @@ extern "C" {
 #define COFIE_BF16 0
 #define COFIE_FP16 1
 #define COFIE_FP32 2 /* cofie_rotary_run only */
+
+/* Pages of 8 bits, as cofie_kv_params.bits (8 alone is refused: 8-bit numbers are of more than one kind). */
+#define COFIE_KV_INT8 0x108u
 
 /* ------------------------------------------------------------------------
  * Rotary positions. Pair i (0 <= i < rotary_dim / 2) of a head turns by
@@ -129,11 +142,11 @@ typedef struct {
   uint32_t n_kv_heads; /* divides n_heads; query head h reads head h / (n_heads / n_kv_heads) */
   uint32_t head_dim;   /* 64 or 128 */
   uint32_t dtype;      /* COFIE_BF16 or COFIE_FP16: queries, keys, values, outputs and 16-bit pages */
-  uint32_t bits;       /* 16 or 4 */
+  uint32_t bits;       /* 16, COFIE_KV_INT8 or 4 */
   int32_t device;      /* CUDA device ordinal, or -1 for the current device */
   void* k_pages;       /* the caller's device memory, 16-byte aligned, for the handle's lifetime */
   void* v_pages;
-  uint16_t* k_scales;  /* bits = 4 only */
+  uint16_t* k_scales;  /* less than 16 bits only */
   uint16_t* v_scales;
 } cofie_kv_params;
 
@@ -158,8 +171,8 @@ void cofie_kv_destroy(cofie_kv_t* h);
  *   q          NULL, or n_heads rows a token, rotated into its `out` by the same launch (needs rotary).
  *   rotary     NULL: keys are stored as they are. Its head_dim is the cache's.
  *   positions  int32 [n_axes][n_tokens], device memory (with rotary).
- * 16-bit pages take the rotated keys rounded once; 4-bit codes are formed from
- * the rotated keys in fp32. Tokens whose page is out of range are left out.
+ * 16-bit pages take the rotated keys rounded once; bytes and 4-bit codes are
+ * formed from the rotated keys in fp32. Tokens whose page is out of range are left out.
  */
 int cofie_kv_append(cofie_kv_t* h, const cofie_kv_batch* b, const cofie_rows* k, const cofie_rows* v,
                     const cofie_rows* q, const cofie_rotary_t* rotary, const int32_t* positions, void* cuda_stream);
@@ -177,10 +190,10 @@ int cofie_kv_read(cofie_kv_t* h, const cofie_kv_batch* b, void* k_out, void* v_o
  *   out = sum_j p_j v_j, p = softmax_j(scale <q, k_j>), lse = ln sum_j exp(scale <q, k_j>)
  * Products are of 16-bit numbers, sums in fp32. The weights exp(scale <q, k_j>)
  * are rounded to 16 bits for their product with the values (to the cache's type,
- * of up to 2^8 or 2^11 for fp16; for at most 32 rows over 4-bit pages to fp16,
- * times the values' scale) and not for lse; over 4-bit pages such rows' queries
- * are taken to fp16 with a power of two for each row, which is meant for queries
- * below 2^110. out is rounded to the cache's type. A row that sees nothing gets
+ * of up to 2^8 or 2^11 for fp16; for at most 32 rows over pages of 8 or 4 bits
+ * to fp16, times the values' scale) and not for lse; over such pages such rows'
+ * queries are taken to fp16 with a power of two for each row, which is meant for
+ * queries below 2^110. out is rounded to the cache's type. A row that sees nothing gets
  * out = 0, lse = -infinity; what a masked or unwritten place holds (NaN too)
  * never matters. (A NaN or an infinity among a call's own new values may reach
  * all new rows of its sequence, those before it too.)

@@ -85,6 +85,7 @@ SplitKernel split_kernel(int i, size_t* smem) {
 SplitKernel split_kernel(const cofie_kv_params& p, int i, size_t* smem) {
   return for_type(p, [&](auto x) {
     using T = decltype(x);
+    if (p.bits == 8) return p.head_dim == 64 ? split_kernel<T, 64, 8>(i, smem) : split_kernel<T, 128, 8>(i, smem);
     if (p.head_dim == 64) return p.bits == 4 ? split_kernel<T, 64, 4>(i, smem) : split_kernel<T, 64, 16>(i, smem);
     return p.bits == 4 ? split_kernel<T, 128, 4>(i, smem) : split_kernel<T, 128, 16>(i, smem);
   });
@@ -92,7 +93,8 @@ SplitKernel split_kernel(const cofie_kv_params& p, int i, size_t* smem) {
 
 template <typename T, int D>
 SplitKernel rows_kernel(uint32_t bits, size_t* smem) {
-  *smem = bits == 4 ? tc_smem<D, 4>() : tc_smem<D, 16>();
+  *smem = bits == 4 ? tc_smem<D, 4>() : bits == 8 ? tc_smem<D, 8>() : tc_smem<D, 16>();
+  if (bits == 8) return attend_rows_tc<T, D, 8>;
   return bits == 4 ? attend_rows_tc<T, D, 4> : attend_rows_tc<T, D, 16>;
 }
 SplitKernel rows_kernel(const cofie_kv_params& p, size_t* smem) {

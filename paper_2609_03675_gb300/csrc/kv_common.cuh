@@ -137,11 +137,13 @@ template <typename T>
 struct Elem;
 template <>
 struct Elem<__nv_bfloat16> {
+  static constexpr int kLeast = -100, kMost = 121;  // exponents of 8-bit pages' scales
   static __device__ __forceinline__ float to(__nv_bfloat16 x) { return __bfloat162float(x); }
   static __device__ __forceinline__ __nv_bfloat16 from(float x) { return __float2bfloat16_rn(x); }
 };
 template <>
 struct Elem<__half> {
+  static constexpr int kLeast = -24, kMost = 9;
   static __device__ __forceinline__ float to(__half x) { return __half2float(x); }
   static __device__ __forceinline__ __half from(float x) { return __float2half_rn(x); }
 };
@@ -240,5 +242,49 @@ struct Unpack<__half> {
     return make_uint4(r[0], r[1], r[2], r[3]);
   }
 };
+
+// Four bytes to (u - 128) s, in their order. s is a power of two, so that all
+// is exact: bf16 holds 128 + the lower seven bits, and the eighth decides
+// whether 128 or 256 comes off; fp16 holds 1024 + u.
+template <typename T>
+struct Bytes;
+template <>
+struct Bytes<__nv_bfloat16> {
+  __nv_bfloat162 s;
+  __device__ __forceinline__ explicit Bytes(uint32_t word) {
+    const uint32_t ss = __byte_perm(word, word, 0x1010);
+    s = *reinterpret_cast<const __nv_bfloat162*>(&ss);
+  }
+  __device__ __forceinline__ uint32_t two(uint32_t w, uint32_t which) const {
+    const uint32_t x = __byte_perm(w, 0x43434343u, which), a = x & 0xFF7FFF7Fu, b = (x & 0xFF80FF80u) ^ 0x00800080u;
+    const __nv_bfloat162 y = __hmul2(__hsub2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b)), s);
+    return *reinterpret_cast<const uint32_t*>(&y);
+  }
+  __device__ __forceinline__ uint2 operator()(uint32_t w) const { return make_uint2(two(w, 0x4140), two(w, 0x4342)); }
+};
+template <>
+struct Bytes<__half> {
+  __half2 s;
+  __device__ __forceinline__ explicit Bytes(uint32_t word) { s = __float2half2_rn(__uint_as_float(word << 16)); }
+  __device__ __forceinline__ uint32_t two(uint32_t w, uint32_t which) const {
+    const uint32_t x = __byte_perm(w, 0x64646464u, which);
+    const __half2 y = __hmul2(__hsub2(*reinterpret_cast<const __half2*>(&x), __float2half2_rn(1152.f)), s);
+    return *reinterpret_cast<const uint32_t*>(&y);
+  }
+  __device__ __forceinline__ uint2 operator()(uint32_t w) const { return make_uint2(two(w, 0x4140), two(w, 0x4342)); }
+};
+
+// The word of 64 values from the largest of their sizes, and its inverse: the
+// smallest power of two that brings it to 127 at most, from 2^kLeast to 2^kMost
+// (of which the type holds 127); a NaN where the size is not finite. f 2^e, f in
+// [1, 2), needs 2^(e - 6) for f up to 127 / 64 and 2^(e - 5) above: adding what
+// the mantissa lacks there carries into the exponent.
+template <typename T>
+__device__ __forceinline__ uint32_t byte_scale(float size, float& inverse) {
+  constexpr uint32_t least = 127 + Elem<T>::kLeast, most = 127 + Elem<T>::kMost;
+  const uint32_t field = min(max((__float_as_uint(size) + 0x1FFFFu) >> 23, least + 6) - 6, most);
+  inverse = __uint_as_float((254u - field) << 23);
+  return size <= 3.402823466e38f ? field << 7 : 0x7FC0u;
+}
 
 }  // namespace cofie

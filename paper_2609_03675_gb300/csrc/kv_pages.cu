@@ -28,14 +28,14 @@ __device__ __forceinline__ float code_back(float code, float zero, float x, floa
   return past ? code - copysignf(1.f, x) : code;
 }
 
-// Appends to 4-bit pages. CTAs of gridDim.y below q_parts rotate the queries;
+// Appends to pages of 4-bit codes or of bytes. CTAs of gridDim.y below q_parts rotate the queries;
 // the others take a share of the (key or value, head) rows of their tokens.
 // Sixteen values of a row to a lane, eight from either half of the head, so that
 // where all of it rotates in the half layout a lane holds both of a pair; the
 // lanes of a group find its extremes by shuffles. WIDE: rows are read 16 bytes at a time, and what a
 // value is rotated with lies in as many pieces (sizes and strides that allow
 // it); else value by value.
-template <typename T, int V, int D, bool WIDE>
+template <typename T, int V, int D, int BITS, bool WIDE>
 __global__ void __launch_bounds__(kThreads, 4) append_codes(const __grid_constant__ CodesArgs a, const __grid_constant__ RotaryTable tab) {
   extern __shared__ __align__(16) float2 cs[];
   const RowsArgs& r = a.rows;
@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(kThreads, 4) append_codes(const __grid_constan
     const uint32_t v = kind >= a.kv_heads, head = kind - v * a.kv_heads;
     const T* const in0 = reinterpret_cast<const T*>(a.in[v]) + static_cast<int64_t>(t0) * a.in_token[v] + head * a.in_head[v];
     const int64_t in_token = a.in_token[v];
-    uint32_t* const codes = a.codes[v] + static_cast<uint64_t>(head << r.batch.page_shift) * (D / 8);
+    uint32_t* const codes = a.codes[v] + static_cast<uint64_t>(head << r.batch.page_shift) * (D * BITS / 32);
     uint16_t* const words = a.words[v] + static_cast<uint64_t>(head << r.batch.page_shift) * (D / kGroup);
     const uint32_t turned = v ? 0 : 2 * tab.half;  // values that are rotated
     RowVec<T, 8> w[2], ahead[2];                   // the lane's values, and those of the next tokens
@@ -131,76 +131,110 @@ __global__ void __launch_bounds__(kThreads, 4) append_codes(const __grid_constan
           }
         }
       }
-      // the extremes of the lane's groups: its two eights are of one (D = 64) or of two
       constexpr int kOwn = D / 64;
-      float lo[2] = {0.f, 0.f}, hi[2] = {0.f, 0.f};
+      uint32_t word[2], codes8[2][2];
+      if constexpr (BITS == 8) {
+        // the largest size of each of the lane's groups; x / s is exact but for what lies under the smallest scale, and
+        // 1.5 2^23 + 128 more rounds it to a whole number, halves to even, whose byte is the low one
+        float size[2] = {0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int gr = kOwn == 1 ? 0 : i / 8;
-        lo[gr] = min_nan(lo[gr], x[i]);
-        hi[gr] = max_nan(hi[gr], x[i]);
-      }
+        for (int i = 0; i < 16; ++i) size[kOwn == 1 ? 0 : i / 8] = max_nan(size[kOwn == 1 ? 0 : i / 8], fabsf(x[i]));
 #pragma unroll
-      for (int o = 1; o < static_cast<int>(kLanes); o <<= 1)
+        for (int o = 1; o < static_cast<int>(kLanes); o <<= 1)
+#pragma unroll
+          for (int gr = 0; gr < kOwn; ++gr) size[gr] = max_nan(size[gr], __shfl_xor_sync(0xffffffffu, size[gr], o));
+        float inverse[2];
+#pragma unroll
+        for (int gr = 0; gr < kOwn; ++gr) word[gr] = byte_scale<T>(size[gr], inverse[gr]);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int gr = kOwn == 1 ? 0 : e;
+          uint32_t u[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) u[i] = __float_as_uint(__fmaf_rn(x[8 * e + i], inverse[gr], 12583040.f));
+          if (!(size[gr] * inverse[gr] <= 127.f)) {  // past the largest scale's range
+#pragma unroll
+            for (int i = 0; i < 8; ++i) u[i] = __float_as_uint(fminf(fmaxf(__uint_as_float(u[i]), 12582913.f), 12583167.f));
+          }
+          codes8[e][0] = __byte_perm(__byte_perm(u[0], u[1], 0x0040), __byte_perm(u[2], u[3], 0x0040), 0x5410);
+          codes8[e][1] = __byte_perm(__byte_perm(u[4], u[5], 0x0040), __byte_perm(u[6], u[7], 0x0040), 0x5410);
+        }
+      } else {
+        // the extremes of the lane's groups: its two eights are of one (D = 64) or of two
+        float lo[2] = {0.f, 0.f}, hi[2] = {0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int gr = kOwn == 1 ? 0 : i / 8;
+          lo[gr] = min_nan(lo[gr], x[i]);
+          hi[gr] = max_nan(hi[gr], x[i]);
+        }
+#pragma unroll
+        for (int o = 1; o < static_cast<int>(kLanes); o <<= 1)
+#pragma unroll
+          for (int gr = 0; gr < kOwn; ++gr) {
+            lo[gr] = min_nan(lo[gr], __shfl_xor_sync(0xffffffffu, lo[gr], o));
+            hi[gr] = max_nan(hi[gr], __shfl_xor_sync(0xffffffffu, hi[gr], o));
+          }
+        // x / scale to the nearest, halves away from zero: the reciprocal (good to
+        // a last place) is taken two above its value, so that no half stays one,
+        // and the product and the zero point are summed and rounded once, to the
+        // last bit of 1.5 2^23. No quotient of 16-bit x lies that close to a half
+        // without being one, but one of rotated keys, which are fp32 numbers, may:
+        // where the reciprocal two below its value gives another code, x - code
+        // scale, which is exact, is held against half a scale. (75000 appended
+        // tokens take 152 us so, 154 with every key held against it, and 135 took
+        // those whose codes could be the next.)
+              float inv[2], low[2], zero[2], step[2];
 #pragma unroll
         for (int gr = 0; gr < kOwn; ++gr) {
-          lo[gr] = min_nan(lo[gr], __shfl_xor_sync(0xffffffffu, lo[gr], o));
-          hi[gr] = max_nan(hi[gr], __shfl_xor_sync(0xffffffffu, hi[gr], o));
+          const float scale = group_scale(lo[gr], hi[gr]);
+          asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv[gr]) : "f"(scale));
+          low[gr] = scale > 0.f ? __uint_as_float(__float_as_uint(inv[gr]) - 2) : 0.f;
+          inv[gr] = scale > 0.f ? __uint_as_float(__float_as_uint(inv[gr]) + 2) : 0.f;
+          float near = __fmaf_rn(-lo[gr], inv[gr], 12582912.f);
+          if (turned) near = code_back(near, 12582912.f, -lo[gr], scale);
+          zero[gr] = fminf(near, 12582927.f);
+          step[gr] = scale;
+          word[gr] = (__float_as_uint(scale) >> 16) | (__float_as_uint(zero[gr]) & 15u);
         }
-      // x / scale to the nearest, halves away from zero: the reciprocal (good to
-      // a last place) is taken two above its value, so that no half stays one,
-      // and the product and the zero point are summed and rounded once, to the
-      // last bit of 1.5 2^23. No quotient of 16-bit x lies that close to a half
-      // without being one, but one of rotated keys, which are fp32 numbers, may:
-      // where the reciprocal two below its value gives another code, x - code
-      // scale, which is exact, is held against half a scale. (75000 appended
-      // tokens take 152 us so, 154 with every key held against it, and 135 took
-      // those whose codes could be the next.)
-      uint32_t word[2], codes8[2];
-      float inv[2], low[2], zero[2], step[2];
 #pragma unroll
-      for (int gr = 0; gr < kOwn; ++gr) {
-        const float scale = group_scale(lo[gr], hi[gr]);
-        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv[gr]) : "f"(scale));
-        low[gr] = scale > 0.f ? __uint_as_float(__float_as_uint(inv[gr]) - 2) : 0.f;
-        inv[gr] = scale > 0.f ? __uint_as_float(__float_as_uint(inv[gr]) + 2) : 0.f;
-        float near = __fmaf_rn(-lo[gr], inv[gr], 12582912.f);
-        if (turned) near = code_back(near, 12582912.f, -lo[gr], scale);
-        zero[gr] = fminf(near, 12582927.f);
-        step[gr] = scale;
-        word[gr] = (__float_as_uint(scale) >> 16) | (__float_as_uint(zero[gr]) & 15u);
-      }
+        for (int e = 0; e < 2; ++e) {
+          // codes are the low bits of 0x4B400000 + code, whose sum's share is taken off at the end
+          uint32_t w = 0;
+          const int gr = kOwn == 1 ? 0 : e;
+          const auto code = [&](int i) { return __fmaf_rn(x[8 * e + i], inv[gr], zero[gr]); };
+          if (!turned) {
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        // codes are the low bits of 0x4B400000 + code, whose sum's share is taken off at the end
-        uint32_t w = 0;
-        const int gr = kOwn == 1 ? 0 : e;
-        const auto code = [&](int i) { return __fmaf_rn(x[8 * e + i], inv[gr], zero[gr]); };
-        if (!turned) {
+            for (int i = 7; i >= 0; --i) w = w * 16 + __float_as_uint(fminf(code(i), 12582927.f));
+          } else {
+            uint32_t apart = 0;  // codes that the reciprocal two below its value gives otherwise
 #pragma unroll
-          for (int i = 7; i >= 0; --i) w = w * 16 + __float_as_uint(fminf(code(i), 12582927.f));
-        } else {
-          uint32_t apart = 0;  // codes that the reciprocal two below its value gives otherwise
+            for (int i = 7; i >= 0; --i) {
+              const float c1 = code(i);
+              apart |= __float_as_uint(c1) ^ __float_as_uint(__fmaf_rn(x[8 * e + i], low[gr], zero[gr]));
+              w = w * 16 + __float_as_uint(fminf(c1, 12582927.f));
+            }
+            if (apart) {
+              w = 0;
 #pragma unroll
-          for (int i = 7; i >= 0; --i) {
-            const float c1 = code(i);
-            apart |= __float_as_uint(c1) ^ __float_as_uint(__fmaf_rn(x[8 * e + i], low[gr], zero[gr]));
-            w = w * 16 + __float_as_uint(fminf(c1, 12582927.f));
+              for (int i = 7; i >= 0; --i) w = w * 16 + __float_as_uint(fminf(code_back(code(i), zero[gr], x[8 * e + i], step[gr]), 12582927.f));
+            }
           }
-          if (apart) {
-            w = 0;
-#pragma unroll
-            for (int i = 7; i >= 0; --i) w = w * 16 + __float_as_uint(fminf(code_back(code(i), zero[gr], x[8 * e + i], step[gr]), 12582927.f));
-          }
+          codes8[e][0] = w - 0x4B400000u * 0x11111111u;
         }
-        codes8[e] = w - 0x4B400000u * 0x11111111u;
       }
       if (p >= 0) {
         // the row of the page's first head, to which the head's places were added above
         const uint64_t page = static_cast<uint64_t>(p) >> r.batch.page_shift;
         const uint64_t at = ((page * a.kv_heads) << r.batch.page_shift) + (static_cast<uint32_t>(p) & ((1u << r.batch.page_shift) - 1));
-        codes[at * (D / 8) + lane] = codes8[0];
-        codes[at * (D / 8) + kLanes + lane] = codes8[1];
+        if (BITS == 8) {
+          uint2* const to = reinterpret_cast<uint2*>(codes) + at * (D / 8) + lane;
+          to[0] = make_uint2(codes8[0][0], codes8[0][1]);
+          to[kLanes] = make_uint2(codes8[1][0], codes8[1][1]);
+        } else {
+          codes[at * (D / 8) + lane] = codes8[0][0];
+          codes[at * (D / 8) + kLanes + lane] = codes8[1][0];
+        }
         if (lane == 0) {
           if (kOwn == 2) reinterpret_cast<uint32_t*>(words)[at] = word[0] | word[1] << 16;
           else words[at] = static_cast<uint16_t>(word[0]);
@@ -245,6 +279,10 @@ __global__ void __launch_bounds__(kThreads) read_pages(const __grid_constant__ R
         const uint64_t at = ((static_cast<uint64_t>(p) >> shift) * kv << shift) + (static_cast<uint32_t>(p) & ((1u << shift) - 1));
         if (BITS == 16) {
           val = *reinterpret_cast<const uint4*>(pages + at * (D * 2));
+        } else if (BITS == 8) {
+          const Bytes<T> u(words[at * (D / kGroup)]);
+          const uint2 x = *reinterpret_cast<const uint2*>(pages + at * D), y = u(x.x), z = u(x.y);
+          val = make_uint4(y.x, y.y, z.x, z.y);
         } else {
           const Unpack<T> u(words[at * (D / kGroup)]);
           const uint4 y = u(*reinterpret_cast<const uint32_t*>(pages + at * (D / 2)));  // (0, 4), (1, 5), (2, 6), (3, 7)
@@ -257,7 +295,7 @@ __global__ void __launch_bounds__(kThreads) read_pages(const __grid_constant__ R
   }
 }
 
-template <typename T, int D>
+template <typename T, int D, int BITS>
 cudaError_t launch_codes(CodesArgs a, const RotaryTable& tab, bool queries, cudaStream_t st) {
   RowsArgs& r = a.rows;
   uint32_t v = queries ? rows_vector(r, tab, D, 2) : 8;
@@ -275,14 +313,15 @@ cudaError_t launch_codes(CodesArgs a, const RotaryTable& tab, bool queries, cuda
   const dim3 grid(tiles, parts + a.q_parts);
   const size_t smem = rows_smem(r.tile, tab.half, r.batch.n_seqs, r.offsets_in_smem);
   const auto go = [&](auto kernel) { return launch_dependent(true, kernel, grid, dim3(kThreads), smem, st, a, tab); };
-  if (wide) return go(append_codes<T, 8, D, true>);
-  return v == 2 ? go(append_codes<T, 2, D, false>) : go(append_codes<T, 1, D, false>);
+  if (wide) return go(append_codes<T, 8, D, BITS, true>);
+  return v == 2 ? go(append_codes<T, 2, D, BITS, false>) : go(append_codes<T, 1, D, BITS, false>);
 }
 
 template <typename T, int D>
 cudaError_t launch_read(const ReadArgs& a, uint32_t bits, cudaStream_t st) {
   const uint32_t tiles = (a.batch.n_tokens + kReadTile - 1) / kReadTile, most = (2 * a.batch.kv_heads + kThreads / 32 - 1) / (kThreads / 32);
   const dim3 grid(tiles, std::max(1u, std::min(most, sm_count() * 4 / tiles)));
+  if (bits == 8) return launch_dependent(true, read_pages<T, D, 8>, grid, dim3(kThreads), 0, st, a);
   return bits == 4 ? launch_dependent(true, read_pages<T, D, 4>, grid, dim3(kThreads), 0, st, a)
                    : launch_dependent(true, read_pages<T, D, 16>, grid, dim3(kThreads), 0, st, a);
 }
@@ -357,9 +396,9 @@ int cofie_kv_create(const cofie_kv_params* p, cofie_kv_t** out) {
     return bad("n_kv_heads must divide n_heads, at most 1024");
   if (p->head_dim != 64 && p->head_dim != 128) return bad("head_dim must be 64 or 128");
   if (p->dtype != COFIE_BF16 && p->dtype != COFIE_FP16) return bad("dtype must be COFIE_BF16 or COFIE_FP16");
-  if (p->bits != 16 && p->bits != 4) return bad("bits must be 16 or 4");
-  if (!p->k_pages || !p->v_pages || (p->bits == 4 && (!p->k_scales || !p->v_scales)))
-    return bad("the pages (and for 4 bits the scales) are required");
+  if (p->bits != 16 && p->bits != 4 && p->bits != COFIE_KV_INT8) return bad("bits must be 16, 4 or COFIE_KV_INT8");
+  if (!p->k_pages || !p->v_pages || (p->bits != 16 && (!p->k_scales || !p->v_scales)))
+    return bad("the pages (and for less than 16 bits the scales) are required");
   for (const void* x : {static_cast<const void*>(p->k_pages), static_cast<const void*>(p->v_pages),
                         static_cast<const void*>(p->k_scales), static_cast<const void*>(p->v_scales)})
     if (reinterpret_cast<uintptr_t>(x) % 16) return bad("pages and scales must be 16-byte aligned");
@@ -372,11 +411,12 @@ int cofie_kv_create(const cofie_kv_params* p, cofie_kv_t** out) {
   }
   DeviceGuard g(dev);
   if (!on_device(p->k_pages, dev) || !on_device(p->v_pages, dev) ||
-      (p->bits == 4 && (!on_device(p->k_scales, dev) || !on_device(p->v_scales, dev))))
+      (p->bits != 16 && (!on_device(p->k_scales, dev) || !on_device(p->v_scales, dev))))
     return bad("the pages must be device memory on the handle's device");
   cofie_kv* h = new (std::nothrow) cofie_kv();
   if (!h) return g_kv_error = "host allocation failed", COFIE_ENOMEM;
   h->p = *p;
+  h->p.bits = p->bits & 0xFF;  // 16, 8 or 4 from here
   h->device = dev;
   h->page_shift = shift;
   cudaError_t e = injected_alloc_failure() ? cudaErrorMemoryAllocation : cudaMalloc(&h->d_err, sizeof(uint32_t));
@@ -443,10 +483,12 @@ int cofie_kv_append(cofie_kv_t* h, const cofie_kv_batch* b, const cofie_rows* k,
                 {h->p.k_scales, h->p.v_scales},
                 h->p.n_kv_heads,
                 0};
-    if (h->p.dtype == COFIE_BF16)
-      e = h->p.head_dim == 64 ? launch_codes<__nv_bfloat16, 64>(c, tab, q != nullptr, st) : launch_codes<__nv_bfloat16, 128>(c, tab, q != nullptr, st);
-    else
-      e = h->p.head_dim == 64 ? launch_codes<__half, 64>(c, tab, q != nullptr, st) : launch_codes<__half, 128>(c, tab, q != nullptr, st);
+    const auto go = [&](auto x) {
+      using T = decltype(x);
+      if (h->p.bits == 8) return h->p.head_dim == 64 ? launch_codes<T, 64, 8>(c, tab, q != nullptr, st) : launch_codes<T, 128, 8>(c, tab, q != nullptr, st);
+      return h->p.head_dim == 64 ? launch_codes<T, 64, 4>(c, tab, q != nullptr, st) : launch_codes<T, 128, 4>(c, tab, q != nullptr, st);
+    };
+    e = h->p.dtype == COFIE_BF16 ? go(__nv_bfloat16()) : go(__half());
   }
   return launched(h, e, "append");
 }

@@ -7,7 +7,7 @@
 //              back into S's place in 16 bits; at the end O out
 //   producers  four warps for keys, four for values: the next tokens into shared
 //              memory (128-byte swizzle), copied (16 bits) or unpacked to
-//              (n - z) s, which the 16-bit types hold exactly (4 bits)
+//              (n - z) s or (u - 128) s, which the 16-bit types hold exactly
 //   MMA        a warp for each tile: S = Q K^T into tensor memory (128 x 64 fp32 a tile),
 //              and O += P V with P read from tensor memory
 // The running maximum that exponentials refer to is raised only when the true
@@ -36,9 +36,11 @@ constexpr int kTcRows = 256;
 constexpr int kTcSoftmax = 256;    // threads: warps 0 to 7
 constexpr int kTcProducers = 128;  // for keys, and as many for values
 constexpr int kTcThreads = kTcSoftmax + 2 * kTcProducers + 128;  // and a group of four warps with the one that issues
-constexpr int kTcStages = 4;       // of keys, and of values
+// Of keys, and of values. Bytes as they lie in the pages take twice the codes' room.
+template <int BITS>
+constexpr int kTcStages = BITS == 8 ? 3 : 4;
 constexpr int kTcInfo = 8;         // more than the stages: a tile is told before its place is free
-constexpr int kTcRaw = 3;          // codes as they lie in the pages
+constexpr int kTcRaw = 3;          // codes or bytes as they lie in the pages
 // Tiles whose products are summed in tensor memory before the sums move on to the CTA's part. The tensor core cuts each
 // product off at about 2^-24 of the sum that it is added to, so 8192 tokens may cost a sum 2^-11 of its size, a rounding
 // of fp16, and 65536 tokens 2^-8, one of bf16. (In one sum, 262144 tokens 14 to 17 below a first one came out 0.4 to
@@ -63,14 +65,15 @@ struct TcSmem {
     char q[2][kBlockQ * (D / 64)];
     Plan<kTcThreads> plan;  // until every thread has its walk
   };
-  char kv[2][kTcStages][kBlock * (D / 64)];  // keys, values
-  char raw[2][BITS == 4 ? kTcRaw : 1][BITS == 4 ? kTile * (D / 2) : 16];
+  static constexpr int kStages = kTcStages<BITS>;
+  char kv[2][kStages][kBlock * (D / 64)];  // keys, values
+  char raw[2][BITS < 16 ? kTcRaw : 1][BITS < 16 ? kTile * (D * BITS / 8) : 16];
   uint32_t raw_word[2][kTcRaw][kTcProducers];
-  uint64_t row_of[2][BITS == 4 ? 1 : kTcStages][kTile];  // 16 bits: the tokens' rows in the pages, ~0 where there is nothing
+  uint64_t row_of[2][BITS < 16 ? 1 : kStages][kTile];  // 16 bits: the tokens' rows in the pages, ~0 where there is nothing
   Span spans[kSpans];
   TcInfo info[kTcInfo];
   float by_sum[kTcRows];
-  uint64_t full[2][kTcStages], empty[2][kTcStages];  // keys, values
+  uint64_t full[2][kStages], empty[2][kStages];  // keys, values
   // A barrier's phase can be told from the one before only. O is ready twice before anyone has to look, so it has a
   // barrier for even tiles and one for odd ones, as S and P have.
   uint64_t info_full[kTcInfo], q_full[2], s_full[2][2], p_full[2][2], o_full[2][2], drained;
@@ -229,6 +232,7 @@ template <typename T, int D, int BITS>
 __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_constant__ AttendArgs a) {
   using P = Pair<T>;
   using S = TcSmem<D, BITS>;
+  constexpr uint32_t kStages = S::kStages;
   // fp16: weights are 2^7 times what they stand for, so that only those under 2^-32 of the largest are lost to the second
   // product, and the maximum that they refer to is never more than 2^4 behind: up to 2^11, the exponents above left for a
   // maximum that is a rounding of a large score off. (bf16 has the exponents of fp32.)
@@ -240,7 +244,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   constexpr uint32_t kIssuer = (kTcSoftmax + 2 * kTcProducers) / 32;
   if (threadIdx.x == 0) {
-    for (int i = 0; i < kTcStages; ++i)
+    for (uint32_t i = 0; i < kStages; ++i)
       for (int v = 0; v < 2; ++v) {
         mbar_init(shared_address(&sm.full[v][i]), kTcProducers / 32);
         mbar_init(shared_address(&sm.empty[v][i]), 2);  // both issuers
@@ -650,12 +654,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
           mbar_arrive(shared_address(&sm.info_full[i % kTcInfo]));
         }
       };
-      if (BITS == 4) {
+      if (BITS < 16) {
         // Codes are fetched three tiles ahead, each thread's to places of its own.
-        constexpr uint32_t kPart = D / 64;  // 16-byte pieces of a thread: a quarter of D codes is D / 4 bytes
+        constexpr uint32_t kPart = D * BITS / 256;  // 16-byte pieces of a thread, which has half a token
         const auto fetch = [&](uint32_t i, const Token& y) {
           if (y.row != ~0ull) {
-            const char* from = pages + y.row * (D / 2) + half * (D / 4);
+            const char* from = pages + y.row * (D * BITS / 8) + half * (D * BITS / 16);
             const uint32_t to = shared_address(sm.raw[v][i % kTcRaw]) + p * 16;
 #pragma unroll
             for (int e = 0; e < static_cast<int>(kPart); ++e) cp_async16(to + e * 2048, from + e * 16, true);
@@ -682,22 +686,31 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
         fetch(n + 2, x[2]);
 #pragma unroll 1
         for (uint32_t j = 0; j < tiles; ++j, ++n) {
-          const uint32_t st = n % kTcStages, round = n / kTcStages;
+          const uint32_t st = n % kStages, round = n / kStages;
           tell(x[0], n);
           cp_async_wait<kTcRaw - 1>();
           if (round > 0) ok = ok && tc_wait(&sm.empty[v][st], round - 1, stop);
           if (ok) {
             const char* from = sm.raw[v][n % kTcRaw] + p * 16;
             const uint32_t w = sm.raw_word[v][n % kTcRaw][p];
-            const Unpack<T> u(D == 64 ? (tok % 2 ? w >> 16 : w & 0xFFFFu) : (half ? w >> 16 : w & 0xFFFFu));
+            const uint32_t word = D == 64 ? (tok % 2 ? w >> 16 : w & 0xFFFFu) : (half ? w >> 16 : w & 0xFFFFu);
+            const std::conditional_t<BITS == 8, Bytes<T>, Unpack<T>> u(word);
             char* to = sm.kv[v][st] + (D == 128 ? half * S::kBlock : 0) + tok * 128;
 #pragma unroll
             for (int e = 0; e < static_cast<int>(kPart); ++e) {
               const uint4 y = *reinterpret_cast<const uint4*>(from + e * 2048);
               const uint32_t ws[4] = {y.x, y.y, y.z, y.w};
+              if constexpr (BITS == 8) {
 #pragma unroll
-              for (int f = 0; f < 4; ++f)
-                *reinterpret_cast<uint4*>(to + (((D == 64 ? 4 * half : 0) + 4 * e + f) ^ (tok & 7)) * 16) = u(ws[f]);
+                for (int f = 0; f < 2; ++f) {
+                  const uint2 a0 = u(ws[2 * f]), a1 = u(ws[2 * f + 1]);
+                  *reinterpret_cast<uint4*>(to + (((D == 64 ? 4 * half : 0) + 2 * e + f) ^ (tok & 7)) * 16) = make_uint4(a0.x, a0.y, a1.x, a1.y);
+                }
+              } else {
+#pragma unroll
+                for (int f = 0; f < 4; ++f)
+                  *reinterpret_cast<uint4*>(to + (((D == 64 ? 4 * half : 0) + 4 * e + f) ^ (tok & 7)) * 16) = u(ws[f]);
+              }
             }
             fence_async_shared();
           }
@@ -712,12 +725,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
       } else {
         // Copies of three tiles are on their way at a time.
         constexpr uint32_t kUnits = D / 8;  // 16-byte units of a token
-        constexpr uint32_t kAhead = kTcStages - 1;
+        constexpr uint32_t kAhead = kStages - 1;
         uint32_t unit_ahead = unit_of(1);
         Page page_ahead = page_of(unit_of(0));
 #pragma unroll 1
         for (uint32_t j = 0; j < tiles + kAhead - 1; ++j) {
-          const uint32_t i = n + j, st = i % kTcStages, round = i / kTcStages;
+          const uint32_t i = n + j, st = i % kStages, round = i / kStages;
           if (j < tiles) {
             const Token x = row_of(page_ahead);
             page_ahead = page_of(unit_ahead);
@@ -743,7 +756,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
             cp_async_wait<kAhead - 1>();
             fence_async_shared();
             ok = __all_sync(0xffffffffu, ok);
-            if (ok) warp_arrive(&sm.full[v][(i + 1 - kAhead) % kTcStages]);
+            if (ok) warp_arrive(&sm.full[v][(i + 1 - kAhead) % kStages]);
           }
         }
         n += tiles;
@@ -762,19 +775,19 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
         if (t >= halves) {  // nothing to issue, but to stay in step: a barrier's phases are told apart by their parity
           for (uint32_t j = 0; j < tiles; ++j, ++n)
             for (uint32_t v = 0; v < 2; ++v) {
-              ok = ok && tc_wait(&sm.full[v][n % kTcStages], n / kTcStages, stop);
+              ok = ok && tc_wait(&sm.full[v][n % kStages], n / kStages, stop);
               ok = __all_sync(0xffffffffu, ok);
-              if (ok) warp_arrive(&sm.empty[v][n % kTcStages]);
+              if (ok) warp_arrive(&sm.empty[v][n % kStages]);
             }
           continue;
         }
         if (tiles == 0) continue;
         const auto qk = [&](uint32_t j) {
-          const uint32_t st = (n + j) % kTcStages, i = s_n + j;
+          const uint32_t st = (n + j) % kStages, i = s_n + j;
           if (j == 0) ok = ok && tc_wait(&sm.q_full[t], q_n++, stop);
           // this S holds the P of two tiles before
           if (j > 1) ok = ok && tc_wait(&sm.o_full[t][i % 2], i / 2 - 1, stop);
-          ok = ok && tc_wait(&sm.full[0][st], (n + j) / kTcStages, stop);
+          ok = ok && tc_wait(&sm.full[0][st], (n + j) / kStages, stop);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) return;
           tc_fence_after();
@@ -788,8 +801,8 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
         for (uint32_t j = 0; j < 2 && j < tiles; ++j) qk(j);
 #pragma unroll 1
         for (uint32_t j = 0; ok && j < tiles; ++j) {
-          const uint32_t st = (n + j) % kTcStages, i = s_n + j;
-          ok = tc_wait(&sm.p_full[t][i % 2], i / 2, stop) && tc_wait(&sm.full[1][st], (n + j) / kTcStages, stop);
+          const uint32_t st = (n + j) % kStages, i = s_n + j;
+          ok = tc_wait(&sm.p_full[t][i % 2], i / 2, stop) && tc_wait(&sm.full[1][st], (n + j) / kStages, stop);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           tc_fence_after();

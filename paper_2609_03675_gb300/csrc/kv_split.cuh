@@ -105,16 +105,22 @@ __device__ __forceinline__ void mma_first(float* c, const uint32_t* a, uint32_t 
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
 
+// Two of a register's bytes as the fp16 numbers u - 128: 1024 + u is a byte
+// beside 0x64. `which` two: 0x4140 the lower, 0x4342 the upper; or the first
+// and the third.
+__device__ __forceinline__ uint32_t byte_pair(uint32_t x, uint32_t which) { return Pair<__half>::sub(__byte_perm(x, 0x64646464u, which), 0x64806480u); }
+__device__ __forceinline__ uint32_t byte_even(uint32_t x) { return Pair<__half>::sub((x & 0x00FF00FFu) | 0x64006400u, 0x64806480u); }
+
 // The scales of a register of two words (the high half's, the low half's).
 __device__ __forceinline__ float scale_hi(uint32_t w) { return __uint_as_float(w & 0xFFF00000u); }
 __device__ __forceinline__ float scale_lo(uint32_t w) { return __uint_as_float((w << 16) & 0xFFF00000u); }
 
-// Sizes of one warp's ring. Chunks of 32 tokens of codes, 16 of 16-bit values.
+// Sizes of one warp's ring. Chunks of 32 tokens of codes or bytes, 16 of 16-bit values.
 template <int D, int BITS>
 struct Ring {
-  static constexpr int kTokens = BITS == 4 ? 32 : 16;
+  static constexpr int kTokens = BITS < 16 ? 32 : 16;
   static constexpr int kRow = D * BITS / 8;                               // bytes of a token's keys
-  static constexpr int kWords = BITS == 4 ? kTokens * (D / 64) * 2 : 0;   // bytes of its chunk's scale words
+  static constexpr int kWords = BITS < 16 ? kTokens * (D / 64) * 2 : 0;   // bytes of its chunk's scale words
   static constexpr int kStage = 2 * (kTokens * kRow + kWords);
   static constexpr int kStages = 3;
   static constexpr int kWarp = kStages * kStage;
@@ -131,6 +137,7 @@ __host__ __device__ constexpr size_t split_smem() {
 template <int D, int BITS, bool VALUES>
 __device__ __forceinline__ uint32_t unit_at(uint32_t t, uint32_t u) {
   if (BITS == 4) return t * Ring<D, 4>::kRow + (D == 128 ? (u ^ ((t & 2u))) : u) * 16;
+  if (BITS == 8) return t * Ring<D, 8>::kRow + (VALUES ? u ^ (t & (D == 128 ? 6u : 2u)) : D == 128 ? u ^ ((t & 1u) << 2) : u) * 16;
   return t * Ring<D, 16>::kRow + (VALUES ? u ^ (t & 7u) : u ^ ((t & 1u) << 2)) * 16;
 }
 
@@ -200,7 +207,7 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
             bits &= BITS == 16 ? 0u : ~half;
           }
           const bool there = (bits & half) != 0;
-          if (BITS == 4 && !there) continue;  // what the ring holds there is masked below
+          if (BITS < 16 && !there) continue;  // what the ring holds there is masked below
           const uint64_t row = there ? ((static_cast<uint64_t>(x.page[mt]) * b.kv_heads + it.head) << b.page_shift) +
                                            ((x.pos + 16 * mt) & ((1u << b.page_shift) - 1))
                                      : 0;
@@ -210,11 +217,11 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
           for (int i = 0; i < R::kUnits / 2; ++i) {  // 32 units of 16 bytes
             const uint32_t t = (i * 32 + lane) / R::kUnits, u = lane % R::kUnits;
             // 16-bit values that nobody sees become zeros (a NaN among them would pass through a product with 0)
-            const bool live = BITS == 4 || ((bits >> t) & 1u);
+            const bool live = BITS < 16 || ((bits >> t) & 1u);
             cp_async16(base + unit_at<D, BITS, false>(16 * mt + t, u), k + i * 512, live);
             cp_async16(base + R::kTokens * R::kRow + unit_at<D, BITS, true>(16 * mt + t, u), v + i * 512, live);
           }
-          if (BITS == 4) {  // the block's words: D / 2 bytes of the keys', as many of the values'
+          if (BITS < 16) {  // the block's words: 16 D / 32 bytes of the keys', as many of the values'
             constexpr uint32_t kLanes = D / 32;
             static_assert(R::kWords / kM == 16 * kLanes || BITS == 16, "16 bytes to a lane");
             if (lane < 2 * kLanes) {
@@ -252,7 +259,8 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
       uint4 x[D / 32];
 #pragma unroll
       for (int e = 0; e < D / 32; ++e) {
-        // eight dims: 16-bit keys: unit 4 e + c of the row; codes: word e % 2 of the lane's two words in group e / 2
+        // eight dims: 16-bit keys: unit 4 e + c of the row; codes: word e % 2 of the lane's two words in group e / 2; bytes:
+        // half of its unit of that group
         const uint32_t d = BITS == 16 ? (4 * e + c) * 8 : (e / 2) * 64 + c * 16 + (e % 2) * 8;
         x[e] = make_uint4(0, 0, 0, 0);
         if (real) {
@@ -288,13 +296,20 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
         const float up = __uint_as_float(static_cast<uint32_t>(127 + 7 - ex) << 23), odd = up * 0.0625f;
 #pragma unroll
         for (int e = 0; e < D / 32; ++e) {
+          if (BITS == 8) {  // bytes in their order
+            qf[nt][2 * e][0] = H::pack(P::lo(x[e].x) * up, P::hi(x[e].x) * up);
+            qf[nt][2 * e][1] = H::pack(P::lo(x[e].y) * up, P::hi(x[e].y) * up);
+            qf[nt][2 * e + 1][0] = H::pack(P::lo(x[e].z) * up, P::hi(x[e].z) * up);
+            qf[nt][2 * e + 1][1] = H::pack(P::lo(x[e].w) * up, P::hi(x[e].w) * up);
+            continue;
+          }
           // codes come out of a word as (0, 4), 16 (1, 5), (2, 6), 16 (3, 7)
           qf[nt][2 * e][0] = H::pack(P::lo(x[e].x) * up, P::lo(x[e].z) * up);
           qf[nt][2 * e][1] = H::pack(P::hi(x[e].x) * odd, P::hi(x[e].z) * odd);
           qf[nt][2 * e + 1][0] = H::pack(P::lo(x[e].y) * up, P::lo(x[e].w) * up);
           qf[nt][2 * e + 1][1] = H::pack(P::hi(x[e].y) * odd, P::hi(x[e].w) * odd);
         }
-        const float back = scale * __uint_as_float(static_cast<uint32_t>(127 - 7 + ex) << 23) * 0x1p24f;
+        const float back = scale * __uint_as_float(static_cast<uint32_t>(127 - 7 + ex) << 23) * (BITS == 4 ? 0x1p24f : 1.f);
         by[nt][0] = __shfl_sync(0xffffffffu, back, 8 * c);
         by[nt][1] = __shfl_sync(0xffffffffu, back, 8 * c + 4);
       }
@@ -348,13 +363,13 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
         }
       }
       if (bits == 0) continue;
-      const bool whole = (BITS == 4 ? bits == 0xffffffffu : (bits & 0xffffu) == 0xffffu);
+      const bool whole = (BITS < 16 ? bits == 0xffffffffu : (bits & 0xffffu) == 0xffffu);
       const char *const vbase = base + R::kTokens * R::kRow, *const kw = base + 2 * R::kTokens * R::kRow, *const vw = kw + R::kWords;
 
-      // ---- scores. Row slots of a 16-token operand hold tokens in this order (4-bit: so that both operands' reads
+      // ---- scores. Row slots of a 16-token operand hold tokens in this order (codes and bytes: so that both operands' reads
       // are free of conflicts): slot s is token s ^ ((s >> 2) & 1) of its eight
       float s[NT][kM][4];
-      const uint32_t tk = BITS == 4 ? g ^ (g >> 2) : g;
+      const uint32_t tk = BITS < 16 ? g ^ (g >> 2) : g;
 #pragma unroll
       for (int mt = 0; mt < kM; ++mt) {
         const uint32_t t0 = mt * 16 + tk;
@@ -382,9 +397,22 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
           }
 #pragma unroll
           for (int gr = 0; gr < kGroups; ++gr) {
+            float acc[NT][4];
+            if constexpr (BITS == 8) {
+              const uint4 x = at<uint4>(base + unit_at<D, BITS, false>(t0, gr * 4 + c)), y = at<uint4>(base + unit_at<D, BITS, false>(t0 + 8, gr * 4 + c));
+              const uint32_t xs[4] = {x.x, x.y, x.z, x.w}, ys[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const uint32_t f[4] = {byte_pair(xs[e], 0x4140), byte_pair(ys[e], 0x4140), byte_pair(xs[e], 0x4342), byte_pair(ys[e], 0x4342)};
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                  if (e == 0) mma_first(acc[nt], f, qf[nt][4 * gr][0], qf[nt][4 * gr][1]);
+                  else H::mma(acc[nt], f, qf[nt][4 * gr + e][0], qf[nt][4 * gr + e][1]);
+                }
+              }
+            } else {
             const uint2 x = at<uint2>(base + unit_at<D, BITS, false>(t0, gr * 2 + c / 2) + (c % 2) * 8);
             const uint2 y = at<uint2>(base + unit_at<D, BITS, false>(t0 + 8, gr * 2 + c / 2) + (c % 2) * 8);
-            float acc[NT][4];
             const uint32_t z0 = __byte_perm(w0, w0, gr == 0 ? 0x1010 : 0x3232) & 0x000F000Fu, z1 = __byte_perm(w1, w1, gr == 0 ? 0x1010 : 0x3232) & 0x000F000Fu;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
@@ -396,6 +424,7 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
                 if (e == 0) mma_first(acc[nt], f, qf[nt][4 * gr][0], qf[nt][4 * gr][1]);
                 else H::mma(acc[nt], f, qf[nt][4 * gr + e][0], qf[nt][4 * gr + e][1]);
               }
+            }
             }
             const float s0 = gr == 0 ? scale_lo(w0) : scale_hi(w0), s1 = gr == 0 ? scale_lo(w1) : scale_hi(w1);
 #pragma unroll
@@ -529,10 +558,38 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
             }
           }
         }
+        uint32_t pf8[NT][2];  // bytes: the weights of the two groups' tokens in turn
 #pragma unroll
         for (int mt = 0; mt < kM; ++mt) {
           const uint32_t swap = c >> 1;  // slots 2c and 2c + 1 are tokens 2c and 2c + 1, or the other way round
           const uint32_t ta = mt * 16 + 2 * c + swap, tb = mt * 16 + 2 * c + (swap ^ 1u);
+          if constexpr (BITS == 8) {
+            // 32 dims at a time, four neighbours to a lane: their bytes of two tokens, side by side
+#pragma unroll
+            for (int st = 0; st < D / 32; ++st) {
+              const int gr = st / 2;
+              const uint32_t unit = st * 2 + g / 4, in = (g % 4) * 4;
+              const uint32_t xa = at<uint32_t>(vbase + unit_at<D, BITS, true>(ta, unit) + in), xb = at<uint32_t>(vbase + unit_at<D, BITS, true>(tb, unit) + in);
+              const uint32_t xc = at<uint32_t>(vbase + unit_at<D, BITS, true>(ta + 8, unit) + in), xd = at<uint32_t>(vbase + unit_at<D, BITS, true>(tb + 8, unit) + in);
+              if (st % 2 == 0) {
+                const float s0 = (gr == 0 ? scale_lo(ws[mt][0]) : scale_hi(ws[mt][0])) * v_up[gr];
+                const float s1 = (gr == 0 ? scale_lo(ws[mt][1]) : scale_hi(ws[mt][1])) * v_up[gr];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                  pf8[nt][0] = transpose8x8(H::pack(p[nt][mt][0] * s0, p[nt][mt][1] * s0));
+                  pf8[nt][1] = transpose8x8(H::pack(p[nt][mt][2] * s1, p[nt][mt][3] * s1));
+                }
+              }
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {
+                const uint32_t u = __byte_perm(xa, xb, h == 0 ? 0x5410 : 0x7632), v = __byte_perm(xc, xd, h == 0 ? 0x5410 : 0x7632);
+                const uint32_t f[4] = {byte_even(u), byte_even(u >> 8), byte_even(v), byte_even(v >> 8)};
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) H::mma(o[nt][st * 2 + h], f, pf8[nt][0], pf8[nt][1]);
+              }
+            }
+            continue;
+          }
           uint32_t wa, wb, wc, wd;  // words of the tokens in slots 2c, 2c + 1, 2c + 8, 2c + 9, for their zero points
           if (D == 128) {
             wa = at<uint32_t>(vw + ta * 4), wb = at<uint32_t>(vw + tb * 4), wc = at<uint32_t>(vw + ta * 4 + 32), wd = at<uint32_t>(vw + tb * 4 + 32);
@@ -570,14 +627,14 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
         }
       }
     }
-    if (BITS == 4) {  // to values: the powers of two back
+    if (BITS < 16) {  // to values: the powers of two back
 #pragma unroll
       for (int e = 0; e < D / 16; ++e) {
         const float back = 1.f / v_up[e / 4];  // (with the 2^24 it may pass fp32's range)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int f = 0; f < 4; ++f) o[nt][e][f] = o[nt][e][f] * (f < 2 ? 0x1p24f : 0x1p20f) * back;
+          for (int f = 0; f < 4; ++f) o[nt][e][f] = o[nt][e][f] * (BITS == 8 ? 1.f : f < 2 ? 0x1p24f : 0x1p20f) * back;
       }
     }
     cp_async_wait<0>();
@@ -602,6 +659,8 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
           if (BITS == 16) {
             to[d * 16 + g] = o[nt][d][e];
             to[d * 16 + g + 8] = o[nt][d][2 + e];
+          } else if (BITS == 8) {
+            *reinterpret_cast<float2*>(to + (d / 2) * 32 + g * 4 + (d % 2) * 2) = make_float2(o[nt][d][e], o[nt][d][2 + e]);
           } else {
             *reinterpret_cast<float2*>(to + (d / 4) * 64 + g * 8 + (d % 4) * 2) = make_float2(o[nt][d][e], o[nt][d][2 + e]);
           }

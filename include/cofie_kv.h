@@ -209,6 +209,41 @@ int cofie_kv_read(cofie_kv_t* h, const cofie_kv_batch* b, void* k_out, void* v_o
 int cofie_kv_attend(cofie_kv_t* h, const cofie_kv_batch* b, const cofie_rows* q, float* lse, const uint8_t* mask,
                     uint64_t mask_stride, int causal, float scale, void* cuda_stream);
 
+/*
+ * Prefixes that several sequences share (questions or answers about one
+ * stream): group g is sequences groups[g] .. groups[g + 1] - 1 of the batch, and
+ * each of them sees the lengths[g] tokens of its prefix, whose pages are row g
+ * of `table`, before its own cached tokens. What comes before groups[0] or from
+ * groups[n_groups] on has no prefix.
+ */
+typedef struct {
+  uint32_t n_groups;       /* 1 .. 2^31 - 1 */
+  uint32_t max_new;        /* at least the largest count of a group's new tokens (0: n_tokens); it chooses the kernel */
+  uint32_t table_stride;   /* entries of one group */
+  const int32_t* table;    /* [n_groups][table_stride], device memory */
+  const int32_t* lengths;  /* [n_groups], device memory; 0: no prefix */
+  const int32_t* groups;   /* [n_groups + 1], device memory, or NULL: one group of all sequences */
+  const uint8_t* mask;     /* NULL, or uint8 [n_seqs][mask_stride], device memory: nonzero where sequence s may see a token of
+                              its prefix (one past mask_stride counts as masked) */
+  uint64_t mask_stride;
+} cofie_kv_prefix;
+
+/*
+ * Attention as cofie_kv_attend, of sequences behind shared prefixes. The batch
+ * (lengths, table, mask, causal) is that of the sequences' own cached tokens;
+ * every new token sees its group's prefix besides, under the prefix's mask.
+ * A prefix's pages are read once for all rows of its group (in blocks of 256
+ * rows of a key head, or 16). A row that sees nothing of either gets out = 0,
+ * lse = -infinity. (A NaN or an infinity among the values of a prefix may reach
+ * the rows of every sequence of the group, those that do not see it too, unless
+ * none does.)
+ * May be captured, except for the first call of more tokens, or with a
+ * prefix mask of a larger size, than any before, which grows the handle's
+ * scratch (n_tokens x n_heads x (4 head_dim + 8) bytes).
+ */
+int cofie_kv_attend_shared(cofie_kv_t* h, const cofie_kv_batch* b, const cofie_kv_prefix* prefix, const cofie_rows* q,
+                           float* lse, const uint8_t* mask, uint64_t mask_stride, int causal, float scale, void* cuda_stream);
+
 /* Synchronises cuda_stream; COFIE_EDEVICE if a kernel met a page number, a length or an offset out of range since the
  * last call, COFIE_ETIMEOUT if a bounded device wait ran out. */
 int cofie_kv_status(cofie_kv_t* h, void* cuda_stream);

@@ -1,9 +1,9 @@
 // Attention over the paged cache: the entry point, the tiles that a mask
-// leaves, and the choice of the kernel.
+// leaves, shared prefixes, and the choice of the kernel.
 #include <algorithm>
 #include <cmath>
 
-#include "kv_rows_tc.cuh"
+#include "kv_kernels.cuh"
 
 namespace cofie {
 namespace {
@@ -69,62 +69,107 @@ __global__ void __launch_bounds__(kMaskThreads) visible_tiles(const BatchArg b, 
   if (threadIdx.x == 0) count[seq] = n;
 }
 
-template <typename F>
-auto for_type(const cofie_kv_params& p, F f) {
-  if (p.dtype == COFIE_BF16) return f(__nv_bfloat16());
-  return f(__half());
+// The mask of shared prefixes: a word for every 64 tokens of each sequence,
+// a thread to a word, and each new token's sequence. WIDE: rows allow 16-byte
+// loads.
+constexpr int kWordThreads = 256;
+template <bool WIDE>
+__global__ void __launch_bounds__(kWordThreads) prefix_words(const BatchArg groups, const uint8_t* mask, uint64_t mask_stride, uint64_t* words,
+                                                             uint32_t tile_stride, int32_t* seq_of) {
+  pdl_trigger();
+  pdl_wait();
+  for (uint32_t seq = blockIdx.y; seq < groups.members; seq += gridDim.y) {
+    const uint32_t g = groups.groups ? sequence_of(groups.groups, groups.n_seqs, seq) : 0;
+    const Span sp = g < groups.n_seqs ? sequence_span(groups, g) : Span{0, 0, 0};
+    if (sp.count == 0) {  // nothing, where a group that does not rise may look for its words
+      for (uint64_t t = blockIdx.x * kWordThreads + threadIdx.x; t < tile_stride; t += gridDim.x * kWordThreads)
+        words[static_cast<uint64_t>(seq) * tile_stride + t] = 0;
+      continue;
+    }
+    const uint64_t length = min(static_cast<uint64_t>(sp.length), mask_stride);
+    const uint8_t* row = mask + seq * mask_stride;
+    for (uint64_t t = blockIdx.x * kWordThreads + threadIdx.x; t * kTile < sp.length; t += gridDim.x * kWordThreads) {
+      uint64_t word = 0;
+      const uint64_t at = t * kTile;
+      if (WIDE && at + kTile <= length) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint4 x = *reinterpret_cast<const uint4*>(row + at + 16 * i);
+          const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            // 0x01 in each byte that is not zero, gathered to four bits by a product
+            const uint32_t ones = __vcmpne4(w[j], 0u) & 0x01010101u;
+            word |= static_cast<uint64_t>(ones * 0x01020408u >> 24 & 15u) << (16 * i + 4 * j);
+          }
+        }
+      } else {
+        for (uint32_t i = 0; i < kTile && at + i < length; ++i) word |= static_cast<uint64_t>(row[at + i] != 0) << i;
+      }
+      words[static_cast<uint64_t>(seq) * tile_stride + t] = word;
+    }
+    // this sequence's tokens, which lie among the group's
+    const int64_t first = groups.offsets ? groups.offsets[seq] : seq, end = groups.offsets ? groups.offsets[seq + 1] : seq + 1;
+    const int64_t lo = max(first, static_cast<int64_t>(sp.first)), hi = min(end, static_cast<int64_t>(sp.first) + sp.count);
+    for (int64_t i = lo + blockIdx.x * kWordThreads + threadIdx.x; i < hi; i += gridDim.x * kWordThreads) seq_of[i] = static_cast<int32_t>(seq);
+  }
 }
 
-// The kernel of the handle's type, head length and pages, for 8 << i rows (i: 0 or 1).
-using SplitKernel = void (*)(AttendArgs);
-template <typename T, int D, int BITS>
-SplitKernel split_kernel(int i, size_t* smem) {
-  *smem = i == 0 ? split_smem<D, BITS, 1>() : split_smem<D, BITS, 2>();
-  return i == 0 ? attend_split<T, D, BITS, 1> : attend_split<T, D, BITS, 2>;
-}
-SplitKernel split_kernel(const cofie_kv_params& p, int i, size_t* smem) {
-  return for_type(p, [&](auto x) {
-    using T = decltype(x);
-    if (p.bits == 8) return p.head_dim == 64 ? split_kernel<T, 64, 8>(i, smem) : split_kernel<T, 128, 8>(i, smem);
-    if (p.head_dim == 64) return p.bits == 4 ? split_kernel<T, 64, 4>(i, smem) : split_kernel<T, 64, 16>(i, smem);
-    return p.bits == 4 ? split_kernel<T, 128, 4>(i, smem) : split_kernel<T, 128, 16>(i, smem);
-  });
+// For each group the union of its sequences' words and the tiles where it is
+// not empty, in order: a CTA to a group, 1024 tiles at a time.
+__global__ void __launch_bounds__(kMaskThreads) prefix_tiles(const BatchArg groups, const uint64_t* words, uint64_t* any, uint32_t* tiles,
+                                                             uint32_t* count, uint32_t tile_stride) {
+  __shared__ uint32_t warps[kMaskThreads / 32];
+  pdl_trigger();
+  pdl_wait();
+  const uint32_t g = blockIdx.x, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  const Span sp = sequence_span(groups, g);
+  const uint32_t s0 = groups.groups ? groups.groups[g] : 0, s1 = sp.count == 0 ? s0 : groups.groups ? groups.groups[g + 1] : groups.members;
+  const uint32_t all = sp.count == 0 ? 0 : (sp.length + kTile - 1) / kTile;
+  uint32_t n = 0;
+  for (uint32_t t0 = 0; t0 < all; t0 += kMaskThreads) {
+    const uint32_t t = t0 + threadIdx.x;
+    uint64_t word = 0;
+    if (t < all) {
+#pragma unroll 8
+      for (uint32_t s = s0; s < s1; ++s) word |= words[static_cast<uint64_t>(s) * tile_stride + t];
+      any[static_cast<uint64_t>(g) * tile_stride + t] = word;
+    }
+    const uint32_t bits = __ballot_sync(0xffffffffu, word != 0);
+    if (lane == 0) warps[warp] = __popc(bits);
+    __syncthreads();
+    uint32_t before = n;
+    for (uint32_t w = 0; w < kMaskThreads / 32; ++w) {
+      if (w < warp) before += warps[w];
+      n += warps[w];
+    }
+    if (word) tiles[static_cast<uint64_t>(g) * tile_stride + before + __popc(bits & ((1u << lane) - 1))] = t;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) count[g] = n;
 }
 
-template <typename T, int D>
-SplitKernel rows_kernel(uint32_t bits, size_t* smem) {
-  *smem = bits == 4 ? tc_smem<D, 4>() : bits == 8 ? tc_smem<D, 8>() : tc_smem<D, 16>();
-  if (bits == 8) return attend_rows_tc<T, D, 8>;
-  return bits == 4 ? attend_rows_tc<T, D, 4> : attend_rows_tc<T, D, 16>;
-}
-SplitKernel rows_kernel(const cofie_kv_params& p, size_t* smem) {
-  return for_type(p, [&](auto x) {
-    using T = decltype(x);
-    return p.head_dim == 64 ? rows_kernel<T, 64>(p.bits, smem) : rows_kernel<T, 128>(p.bits, smem);
-  });
+AttendLaunch kernel_of(const cofie_kv_params& p, int kind, bool shared) {
+  return p.bits == 4 ? attend_kernel<4>(p, kind, shared) : p.bits == 8 ? attend_kernel<8>(p, kind, shared) : attend_kernel<16>(p, kind, shared);
 }
 
 }  // namespace
 
 cudaError_t attend_set_up(cofie_kv* h) {
   cudaError_t e = cudaSuccess;
-  size_t rows = 0, ctas = 0;
-  for (int i = 0; i < 2 && e == cudaSuccess; ++i) {
-    size_t smem = 0;
-    const SplitKernel k = split_kernel(h->p, i, &smem);
+  size_t rows = 2ull * sm_count() * kManyRows, ctas = 0;
+  for (int i = 0; i < 6 && e == cudaSuccess; ++i) {
+    const int kind = i % 3;
+    const AttendLaunch k = kernel_of(h->p, kind, i >= 3);
+    e = cudaFuncSetAttribute(k.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(k.smem));
+    if (kind == kMany || e != cudaSuccess) continue;
     int per_sm = 0;
-    e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
-    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, k, kSplitThreads, smem);
+    e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, k.kernel, static_cast<int>(k.threads), k.smem);
     if (e == cudaSuccess && per_sm < 1) e = cudaErrorInvalidConfiguration;
-    h->split_ctas[i] = sm_count() * static_cast<uint32_t>(per_sm);
-    ctas = std::max<size_t>(ctas, h->split_ctas[i]);
-    rows = std::max<size_t>(rows, 2ull * h->split_ctas[i] * (8u << i));
-  }
-  size_t smem = 0;
-  if (e == cudaSuccess) {
-    const SplitKernel k = rows_kernel(h->p, &smem);
-    e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
-    rows = std::max<size_t>(rows, 2ull * sm_count() * kTcRows);
+    const uint32_t n = sm_count() * static_cast<uint32_t>(per_sm);
+    h->split_ctas[i >= 3][kind] = n;
+    ctas = std::max<size_t>(ctas, n);
+    rows = std::max<size_t>(rows, 2ull * n * (8u << kind));
   }
   if (e == cudaSuccess) e = cudaMalloc(&h->d_part, rows * h->p.head_dim * sizeof(float));
   if (e == cudaSuccess) e = cudaMalloc(&h->d_part_ms, rows * sizeof(float2));
@@ -133,26 +178,20 @@ cudaError_t attend_set_up(cofie_kv* h) {
   return e;
 }
 
-}  // namespace cofie
+namespace {
 
-using namespace cofie;
-
-extern "C" int cofie_kv_attend(cofie_kv_t* h, const cofie_kv_batch* b, const cofie_rows* q, float* lse, const uint8_t* mask,
-                               uint64_t mask_stride, int causal, float scale, void* cuda_stream) {
-  if (!h) return COFIE_EINVAL;
-  if (const int rc = check_batch(h, b)) return rc;
-  if (b->n_tokens == 0) return COFIE_OK;
+// What both entry points check and fill in; COFIE_OK, or the error noted on the handle.
+int attend_args(cofie_kv* h, const cofie_kv_batch* b, const cofie_rows* q, float* lse, const uint8_t* mask, uint64_t mask_stride, int causal,
+                float scale, AttendArgs* out) {
   if (!q) return h->fail(COFIE_EINVAL, "q is required");
   if (const int rc = check_rows(h, q, h->p.n_heads, true, "q")) return rc;
   if (q->in == q->out && ((b->n_tokens > 1 && q->in_token != q->out_token) || (q->heads > 1 && q->in_head != q->out_head)))
     return h->fail(COFIE_EINVAL, "in place, the strides of q's in and out must be the same");
   if (!(scale >= 0.f && std::isfinite(scale))) return h->fail(COFIE_EINVAL, "scale must be finite and not negative");
-  DeviceGuard g(h->device);
-  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
   const auto aligned = [](const void* p, int64_t token, int64_t head, uint32_t elems) {
     return reinterpret_cast<uintptr_t>(p) % (2 * elems) == 0 && token % elems == 0 && head % elems == 0;
   };
-  AttendArgs a{};
+  AttendArgs& a = *out;
   a.batch = batch_arg(h, b);
   a.q = {static_cast<const char*>(q->in), static_cast<char*>(q->out), q->in_token, q->in_head, q->out_token, q->out_head, q->heads, kRotate};
   a.lse = lse;
@@ -171,37 +210,46 @@ extern "C" int cofie_kv_attend(cofie_kv_t* h, const cofie_kv_batch* b, const cof
   a.part = h->d_part;
   a.part_ms = h->d_part_ms;
   a.done = h->d_done;
-  if (mask) {
-    a.tile_stride = (b->table_stride << h->page_shift) / kTile + 1;
-    const size_t need = static_cast<size_t>(b->n_seqs) * (a.tile_stride + 1);
-    if (need > h->tiles_room) {
-      const size_t room = std::max(need, 2 * h->tiles_room);
-      cudaStreamCaptureStatus cs = cudaStreamCaptureStatusNone;
-      if (cudaStreamIsCapturing(st, &cs) != cudaSuccess || cs != cudaStreamCaptureStatusNone) {
-        cudaGetLastError();
-        return h->fail(COFIE_EINVAL, "the first masked call of this size must come before the capture");
-      }
-      uint32_t* more = nullptr;
-      const cudaError_t e = injected_alloc_failure() ? cudaErrorMemoryAllocation : cudaMalloc(&more, room * sizeof(uint32_t));
-      if (e != cudaSuccess) {
-        cudaGetLastError();
-        return h->fail(e == cudaErrorMemoryAllocation ? COFIE_ENOMEM : COFIE_ECUDA, "no room for the list of the mask's tiles");
-      }
-      if (h->d_tiles) h->d_tiles_before[h->n_tiles_before++] = h->d_tiles;  // graphs may have it
-      h->d_tiles = more;
-      h->tiles_room = room;
+  return COFIE_OK;
+}
+
+// Whether scratch may be allocated for a call on this stream.
+bool may_allocate(cudaStream_t st) {
+  cudaStreamCaptureStatus cs = cudaStreamCaptureStatusNone;
+  const bool ok = cudaStreamIsCapturing(st, &cs) == cudaSuccess && cs == cudaStreamCaptureStatusNone;
+  if (!ok) cudaGetLastError();
+  return ok;
+}
+
+// The tiles that the batch's mask leaves; a.tiles and what goes with it.
+int list_tiles(cofie_kv* h, const cofie_kv_batch* b, AttendArgs* args, cudaStream_t st) {
+  AttendArgs& a = *args;
+  a.tile_stride = (b->table_stride << h->page_shift) / kTile + 1;
+  const size_t need = static_cast<size_t>(b->n_seqs) * (a.tile_stride + 1);
+  if (need > h->tiles_room) {
+    const size_t room = std::max(need, 2 * h->tiles_room);
+    if (!may_allocate(st)) return h->fail(COFIE_EINVAL, "the first masked call of this size must come before the capture");
+    uint32_t* more = nullptr;
+    const cudaError_t e = injected_alloc_failure() ? cudaErrorMemoryAllocation : cudaMalloc(&more, room * sizeof(uint32_t));
+    if (e != cudaSuccess) {
+      cudaGetLastError();
+      return h->fail(e == cudaErrorMemoryAllocation ? COFIE_ENOMEM : COFIE_ECUDA, "no room for the list of the mask's tiles");
     }
-    a.tiles = h->d_tiles;
-    a.tile_count = h->d_tiles + static_cast<size_t>(b->n_seqs) * a.tile_stride;
-    const uintptr_t at = reinterpret_cast<uintptr_t>(mask) | (b->n_seqs > 1 ? mask_stride : 0);
-    const auto find = at % 16 == 0 ? visible_tiles<uint4> : at % 4 == 0 ? visible_tiles<uint32_t> : visible_tiles<uint8_t>;
-    if (const int rc = launched(h, launch_dependent(true, find, dim3(b->n_seqs), dim3(kMaskThreads), 0, st, a.batch, mask, mask_stride,
-                                                    h->d_tiles, const_cast<uint32_t*>(a.tile_count), a.tile_stride),
-                                "attend"))
-      return rc;
+    if (h->d_tiles) h->d_tiles_before[h->n_tiles_before++] = h->d_tiles;  // graphs may have it
+    h->d_tiles = more;
+    h->tiles_room = room;
   }
-  const uint64_t rows = static_cast<uint64_t>(b->offsets ? (b->max_new ? b->max_new : b->n_tokens) : 1) * a.group;
-  size_t smem = 0;
+  a.tiles = h->d_tiles;
+  a.tile_count = h->d_tiles + static_cast<size_t>(b->n_seqs) * a.tile_stride;
+  const uintptr_t at = reinterpret_cast<uintptr_t>(a.mask) | (b->n_seqs > 1 ? a.mask_stride : 0);
+  const auto find = at % 16 == 0 ? visible_tiles<uint4> : at % 4 == 0 ? visible_tiles<uint32_t> : visible_tiles<uint8_t>;
+  return launched(h, launch_dependent(true, find, dim3(b->n_seqs), dim3(kMaskThreads), 0, st, a.batch, a.mask, a.mask_stride, h->d_tiles,
+                                      const_cast<uint32_t*>(a.tile_count), a.tile_stride),
+                  "attend");
+}
+
+// The kernel for so many rows of a sequence and key head at most.
+int launch_attend(cofie_kv* h, AttendArgs* a, uint64_t rows, bool shared, cudaStream_t st) {
   // Up to 32 rows of a sequence and head, in blocks of 8 or 16, are left to the kernel that reads the cache for each
   // block; more rows pay for tiles of 128 of them. Eight sequences of up to 60000 tokens, 32 heads over 8 of 128 (us,
   // blocks / tiles): 20 rows 176 / 233 with 4 bits, 214 / 337 with 16; 32 rows 188 / 234, 262 / 339; 48 rows 266 / 234,
@@ -212,13 +260,119 @@ extern "C" int cofie_kv_attend(cofie_kv_t* h, const cofie_kv_batch* b, const cof
   // 394, thirty of 16 over up to 2000 87 / 91 / 97 / 103. Few, with 2 / 4 / 6 / 8 / 12: 24 x 3 tokens over up to 9000 of
   // 4 bits 91 / 79 / 72 / 69 / 62, 64 x 1 over up to 20000 of 4 bits 220 / 212 / 200 / 197 / 199, of 16 bits 419 / 402 /
   // 400 / 394 / 398, 8 x 1 over up to 3000 27 / 25 / 23 / 25 / 25.
-  if (rows > 32) {
-    const SplitKernel k = rows_kernel(h->p, &smem);
-    a.item_slots = 8;
-    return launched(h, launch_dependent(true, k, dim3(sm_count()), dim3(kTcThreads), smem, st, a), "attend");
+  const int kind = rows > 32 ? kMany : rows > 8 ? kFew16 : kFew8;
+  a->item_slots = kind == kMany ? 8 : 6;
+  const AttendLaunch k = kernel_of(h->p, kind, shared);
+  const uint32_t ctas = kind == kMany ? sm_count() : h->split_ctas[shared][kind];
+  return launched(h, launch_dependent(true, k.kernel, dim3(ctas), dim3(k.threads), k.smem, st, *a), "attend");
+}
+
+uint64_t rows_at_most(const cofie_kv_batch* b, uint32_t group) {
+  return static_cast<uint64_t>(b->offsets ? (b->max_new ? b->max_new : b->n_tokens) : 1) * group;
+}
+
+// Room of this size in a scratch that grows to twice its size at least; what it outgrew stays, for graphs that have it.
+int scratch(cofie_kv* h, cofie_kv::Scratch* s, size_t need, cudaStream_t st) {
+  if (need <= s->room) return COFIE_OK;
+  if (!may_allocate(st)) return h->fail(COFIE_EINVAL, "the first call of this size over a shared prefix must come before the capture");
+  const size_t room = std::max(need, 2 * s->room);
+  void* more = nullptr;
+  const cudaError_t e = injected_alloc_failure() ? cudaErrorMemoryAllocation : cudaMalloc(&more, room);
+  if (e != cudaSuccess) {
+    cudaGetLastError();
+    return h->fail(e == cudaErrorMemoryAllocation ? COFIE_ENOMEM : COFIE_ECUDA, "no room for the shared prefix's rows");
   }
-  const int i = rows <= 8 ? 0 : 1;
-  a.item_slots = 6;
-  const SplitKernel k = split_kernel(h->p, i, &smem);
-  return launched(h, launch_dependent(true, k, dim3(h->split_ctas[i]), dim3(kSplitThreads), smem, st, a), "attend");
+  if (s->p) s->before[s->n_before++] = s->p;
+  s->p = more;
+  s->room = room;
+  return COFIE_OK;
+}
+
+// The mask of the prefixes: words, their union, the tiles that it leaves, and each token's sequence, one behind the other.
+int prefix_mask(cofie_kv* h, const cofie_kv_prefix* p, AttendArgs* args, cudaStream_t st) {
+  AttendArgs& a = *args;
+  const BatchArg& g = a.batch;
+  a.tile_stride = (g.table_stride << h->page_shift) / kTile + 1;
+  const size_t seqs = g.members, groups = g.n_seqs, stride = a.tile_stride;
+  const size_t words = (seqs + groups) * stride * sizeof(uint64_t), tiles = groups * (stride + 1) * sizeof(uint32_t);
+  if (const int rc = scratch(h, &h->shared_mask, words + tiles + g.n_tokens * sizeof(int32_t), st)) return rc;
+  char* at = static_cast<char*>(h->shared_mask.p);
+  uint64_t* seq_words = reinterpret_cast<uint64_t*>(at);
+  uint64_t* any = seq_words + seqs * stride;
+  uint32_t* list = reinterpret_cast<uint32_t*>(at + words);
+  int32_t* seq_of = reinterpret_cast<int32_t*>(at + words + tiles);
+  a.seq_words = seq_words;
+  a.any_words = any;
+  a.tiles = list;
+  a.tile_count = list + groups * stride;
+  a.seq_of = seq_of;
+  const bool wide = reinterpret_cast<uintptr_t>(p->mask) % 16 == 0 && (seqs == 1 || p->mask_stride % 16 == 0);
+  const dim3 grid(std::max(1u, std::min((a.tile_stride + kWordThreads - 1) / kWordThreads, 64u)), std::min(g.members, 65535u));
+  if (const int rc = launched(h, launch_dependent(true, wide ? prefix_words<true> : prefix_words<false>, grid, dim3(kWordThreads), 0, st, g, p->mask,
+                                                  p->mask_stride, seq_words, a.tile_stride, seq_of),
+                              "attend"))
+    return rc;
+  return launched(h, launch_dependent(true, prefix_tiles, dim3(g.n_seqs), dim3(kMaskThreads), 0, st, g, static_cast<const uint64_t*>(seq_words), any,
+                                      list, list + groups * stride, a.tile_stride),
+                  "attend");
+}
+
+}  // namespace
+}  // namespace cofie
+
+using namespace cofie;
+
+extern "C" int cofie_kv_attend(cofie_kv_t* h, const cofie_kv_batch* b, const cofie_rows* q, float* lse, const uint8_t* mask,
+                               uint64_t mask_stride, int causal, float scale, void* cuda_stream) {
+  if (!h) return COFIE_EINVAL;
+  if (const int rc = check_batch(h, b)) return rc;
+  if (b->n_tokens == 0) return COFIE_OK;
+  AttendArgs a{};
+  if (const int rc = attend_args(h, b, q, lse, mask, mask_stride, causal, scale, &a)) return rc;
+  DeviceGuard g(h->device);
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  if (mask)
+    if (const int rc = list_tiles(h, b, &a, st)) return rc;
+  return launch_attend(h, &a, rows_at_most(b, a.group), false, st);
+}
+
+extern "C" int cofie_kv_attend_shared(cofie_kv_t* h, const cofie_kv_batch* b, const cofie_kv_prefix* prefix, const cofie_rows* q, float* lse,
+                                      const uint8_t* mask, uint64_t mask_stride, int causal, float scale, void* cuda_stream) {
+  if (!h) return COFIE_EINVAL;
+  if (const int rc = check_batch(h, b)) return rc;
+  if (!prefix) return h->fail(COFIE_EINVAL, "the prefix is NULL");
+  if (b->n_tokens == 0) return COFIE_OK;
+  if (prefix->n_groups < 1 || prefix->n_groups > 0x7fffffffu) return h->fail(COFIE_EINVAL, "n_groups must be in [1, 2^31)");
+  if (!prefix->groups && prefix->n_groups != 1) return h->fail(COFIE_EINVAL, "without groups there is one, of all sequences");
+  if (!prefix->table || !prefix->lengths) return h->fail(COFIE_EINVAL, "the prefix's table and lengths are required");
+  if (prefix->table_stride < 1 || prefix->table_stride > 0x7fffffffu / h->p.page_size)
+    return h->fail(COFIE_EINVAL, "the prefix's table_stride x page_size must be in [page_size, 2^31)");
+  AttendArgs own{};
+  if (const int rc = attend_args(h, b, q, lse, mask, mask_stride, causal, scale, &own)) return rc;
+  DeviceGuard g(h->device);
+  cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+  const size_t rows = static_cast<size_t>(b->n_tokens) * h->p.n_heads;
+  if (const int rc = scratch(h, &h->shared_rows, rows * (h->p.head_dim * sizeof(float) + sizeof(float2)), st)) return rc;
+  own.rows = static_cast<float*>(h->shared_rows.p);
+  own.rows_ms = reinterpret_cast<float2*>(own.rows + rows * h->p.head_dim);
+  own.prefix = own.batch;
+  own.prefix.table = prefix->table;
+  own.prefix.lengths = prefix->lengths;
+  own.prefix.n_seqs = prefix->n_groups;
+  own.prefix.table_stride = prefix->table_stride;
+  own.prefix.groups = prefix->groups;
+  own.prefix.members = b->n_seqs;
+  AttendArgs first = own;
+  first.batch = own.prefix;
+  first.mask = nullptr;
+  first.lse = nullptr;
+  first.causal = 0;
+  if (prefix->mask)
+    if (const int rc = prefix_mask(h, prefix, &first, st)) return rc;
+  const uint64_t most = prefix->max_new ? prefix->max_new : b->n_tokens;
+  if (const int rc = launch_attend(h, &first, most * own.group, true, st)) return rc;
+  own.behind = 1;
+  if (mask)
+    if (const int rc = list_tiles(h, b, &own, st)) return rc;
+  return launch_attend(h, &own, rows_at_most(b, own.group), true, st);
 }

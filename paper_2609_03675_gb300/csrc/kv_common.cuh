@@ -62,6 +62,10 @@ struct BatchArg {
   uint32_t n_seqs, n_tokens, table_stride;
   uint32_t n_pages, page_shift, kv_heads;
   uint32_t* err;
+  // groups of sequences that share a prefix: n_seqs of them, whose lengths and table rows are the prefixes', and whose new
+  // tokens are those of sequences groups[g] to groups[g + 1] of the `members` that there are (without groups: of all)
+  const int32_t* groups;
+  uint32_t members;  // 0: sequences, not groups
 };
 
 // cos and sin of pair i at the given position, times the amplitude. The
@@ -93,7 +97,16 @@ struct Span {
 };
 __device__ __forceinline__ Span sequence_span(const BatchArg& b, uint32_t s) {
   const int64_t length = b.lengths[s];
-  const int64_t first = b.offsets ? b.offsets[s] : s, end = b.offsets ? b.offsets[s + 1] : s + 1;
+  int64_t from = s, to = s + 1;
+  if (b.members) {
+    from = b.groups ? b.groups[s] : 0;
+    to = b.groups ? b.groups[s + 1] : b.members;
+    if (from < 0 || to < from || to > b.members) {
+      atomicOr(b.err, kKvErrBatch);
+      return {0, 0, 0};
+    }
+  }
+  const int64_t first = b.offsets ? b.offsets[from] : from, end = b.offsets ? b.offsets[to] : to;
   if (length < 0 || length > (static_cast<int64_t>(b.table_stride) << b.page_shift) || first < 0 || end < first || end > b.n_tokens) {
     atomicOr(b.err, kKvErrBatch);
     return {0, 0, 0};

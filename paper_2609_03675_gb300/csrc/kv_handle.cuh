@@ -14,7 +14,7 @@ struct cofie_kv {
   // parts that they leave, and the tiles that a mask leaves. That list grows on
   // demand, to twice its size at least; those before it stay with the handle,
   // because a captured call keeps the address that it was captured with.
-  uint32_t split_ctas[2] = {0, 0};
+  uint32_t split_ctas[2][2] = {};  // of the kernels for shared prefixes, too
   float* d_part = nullptr;
   float2* d_part_ms = nullptr;
   uint32_t* d_done = nullptr;
@@ -22,6 +22,13 @@ struct cofie_kv {
   size_t tiles_room = 0;
   uint32_t* d_tiles_before[64] = {};  // doublings that a size_t allows
   uint32_t n_tiles_before = 0;
+  // shared prefixes: what attention over them leaves for each row, and what their mask comes to. They grow and stay alike.
+  struct Scratch {
+    void* p = nullptr;
+    size_t room = 0;
+    void* before[64] = {};
+    uint32_t n_before = 0;
+  } shared_rows, shared_mask;
   std::string err;
   int fail(int code, const std::string& m) {
     err = m;

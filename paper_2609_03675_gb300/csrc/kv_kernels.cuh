@@ -1,0 +1,21 @@
+// The attention kernels of one kind of pages, as their translation units give
+// them (one for each kind: they take the compiler longest).
+#pragma once
+
+#include "kv_plan.cuh"
+
+namespace cofie {
+
+using AttendKernel = void (*)(AttendArgs);
+enum : int { kFew8 = 0, kFew16 = 1, kMany = 2 };  // up to 8 or 16 rows a block; tiles of 128
+
+struct AttendLaunch {
+  AttendKernel kernel;
+  uint32_t threads;
+  size_t smem;
+};
+// The kernel for the handle's type and head length. shared: over a prefix, or behind one.
+template <int BITS>
+AttendLaunch attend_kernel(const cofie_kv_params& p, int kind, bool shared);
+
+}  // namespace cofie

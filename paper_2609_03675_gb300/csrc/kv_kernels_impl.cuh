@@ -1,0 +1,29 @@
+// What the translation units of kv_kernels.cuh have in common.
+#pragma once
+
+#include "kv_kernels.cuh"
+#include "kv_rows_tc.cuh"
+
+namespace cofie {
+namespace {
+
+template <typename T, int D, int BITS, bool SHARED>
+AttendLaunch attend_kernel_of(int kind) {
+  if (kind == kMany) return {attend_rows_tc<T, D, BITS, SHARED>, kTcThreads, tc_smem<D, BITS, SHARED>()};
+  if (kind == kFew8) return {attend_split<T, D, BITS, 1, SHARED>, kSplitThreads, split_smem<D, BITS, 1>()};
+  return {attend_split<T, D, BITS, 2, SHARED>, kSplitThreads, split_smem<D, BITS, 2>()};
+}
+
+}  // namespace
+
+template <int BITS>
+AttendLaunch attend_kernel(const cofie_kv_params& p, int kind, bool shared) {
+  const auto of = [&](auto x) {
+    using T = decltype(x);
+    if (p.head_dim == 64) return shared ? attend_kernel_of<T, 64, BITS, true>(kind) : attend_kernel_of<T, 64, BITS, false>(kind);
+    return shared ? attend_kernel_of<T, 128, BITS, true>(kind) : attend_kernel_of<T, 128, BITS, false>(kind);
+  };
+  return p.dtype == COFIE_BF16 ? of(__nv_bfloat16()) : of(__half());
+}
+
+}  // namespace cofie

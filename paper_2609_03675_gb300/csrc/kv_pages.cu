@@ -343,6 +343,10 @@ void kv_free(cofie_kv* h) {
                   static_cast<void*>(h->d_tiles)})
     if (x) cudaFree(x);
   for (uint32_t i = 0; i < h->n_tiles_before; ++i) cudaFree(h->d_tiles_before[i]);
+  for (const cofie_kv::Scratch* s : {&h->shared_rows, &h->shared_mask}) {
+    if (s->p) cudaFree(s->p);
+    for (uint32_t i = 0; i < s->n_before; ++i) cudaFree(s->before[i]);
+  }
   delete h;
 }
 
@@ -370,7 +374,8 @@ int check_rows(cofie_kv* h, const cofie_rows* r, uint32_t heads, bool has_out, c
 }
 
 BatchArg batch_arg(const cofie_kv* h, const cofie_kv_batch* b) {
-  return {b->table, b->lengths, b->offsets, b->n_seqs, b->n_tokens, b->table_stride, h->p.n_pages, h->page_shift, h->p.n_kv_heads, h->d_err};
+  return {b->table, b->lengths, b->offsets, b->n_seqs, b->n_tokens, b->table_stride, h->p.n_pages, h->page_shift, h->p.n_kv_heads, h->d_err,
+          nullptr, 0};
 }
 
 int launched(cofie_kv* h, cudaError_t e, const char* what) {

@@ -15,7 +15,8 @@
 
 namespace cofie {
 
-constexpr uint32_t kTile = 64;  // cached tokens of a tile
+constexpr uint32_t kTile = 64;       // cached tokens of a tile
+constexpr uint32_t kManyRows = 256;  // rows of a block in the kernel of many rows
 
 struct AttendArgs {
   BatchArg batch;
@@ -39,12 +40,45 @@ struct AttendArgs {
   float* part;       // [2 x CTAs][rows][D]
   float2* part_ms;   // [2 x CTAs][rows]: maximum (base 2), sum
   uint32_t* done;    // [CTAs]: parts finished of the item that goes on from this CTA; zero between calls
+  // Sequences behind a shared prefix take two launches. The first has the groups as its batch, each of them one sequence of
+  // all its rows over the prefix, and leaves sums [tokens][heads][D] with the maximum (base 2) and the sum of the weights;
+  // the second has the sequences, and adds what it finds there. `prefix`: the first launch's batch, for the second.
+  float* rows;
+  float2* rows_ms;
+  uint32_t behind;  // the second launch
+  BatchArg prefix;
+  // The first launch's mask, a word of 64 tokens for each sequence and tile; its union over each group; each token's sequence.
+  const uint64_t* seq_words;
+  const uint64_t* any_words;
+  const int32_t* seq_of;
 };
+
+// Whether a prefix's sums are there for the rows of this sequence.
+__device__ __forceinline__ bool has_prefix(const AttendArgs& a, uint32_t seq) {
+  const uint32_t g = a.prefix.groups ? sequence_of(a.prefix.groups, a.prefix.n_seqs, seq) : 0;
+  return g < a.prefix.n_seqs && sequence_span(a.prefix, g).count > 0;
+}
+
+// The weights of a row's two parts in their sum, from their maxima and sums;
+// the maximum and the sum of both.
+struct Both {
+  float own, prefix, top, sum;
+};
+__device__ __forceinline__ Both both_parts(float top, float sum, float2 before) {
+  const float most = fmaxf(top, before.x);
+  const auto by = [&](float m, float s) { return m == -INFINITY ? (s == 0.f ? 0.f : 1.f) : exp2f(m - most); };
+  Both x;
+  x.own = by(top, sum);
+  x.prefix = by(before.x, before.y);
+  x.top = most;
+  x.sum = (sum == 0.f ? 0.f : x.own * sum) + (before.y == 0.f ? 0.f : x.prefix * before.y);
+  return x;
+}
 
 // Tiles of row block rb: those that its last row can see.
 __device__ __forceinline__ uint32_t block_tiles(const AttendArgs& a, const Span& sp, uint32_t rows_per_block, uint32_t rb,
                                                 uint32_t seq) {
-  if (a.mask) return a.tile_count[seq];
+  if (a.tiles) return a.tile_count[seq];
   uint32_t end = sp.length;
   if (a.causal) {
     const uint32_t last = min(sp.count * a.group, (rb + 1) * rows_per_block) - 1;
@@ -57,7 +91,7 @@ __device__ __forceinline__ uint32_t block_tiles(const AttendArgs& a, const Span&
 __device__ __forceinline__ uint64_t sequence_slots(const AttendArgs& a, uint32_t rows_per_block, uint32_t seq, const Span& sp) {
   const uint32_t blocks = (sp.count * a.group + rows_per_block - 1) / rows_per_block;
   uint64_t n = 0;
-  if (a.causal && !a.mask)
+  if (a.causal && !a.tiles)
     for (uint32_t rb = 0; rb < blocks; ++rb) n += block_tiles(a, sp, rows_per_block, rb, seq) + a.item_slots;
   else if (blocks)
     n = static_cast<uint64_t>(blocks) * (block_tiles(a, sp, rows_per_block, 0, seq) + a.item_slots);

@@ -32,7 +32,7 @@
 namespace cofie {
 namespace {
 
-constexpr int kTcRows = 256;
+constexpr int kTcRows = kManyRows;
 constexpr int kTcSoftmax = 256;    // threads: warps 0 to 7
 constexpr int kTcProducers = 128;  // for keys, and as many for values
 constexpr int kTcThreads = kTcSoftmax + 2 * kTcProducers + 128;  // and a group of four warps with the one that issues
@@ -57,7 +57,7 @@ struct TcInfo {
   uint32_t plain[2]; // every token of the half is seen by every row
 };
 
-template <int D, int BITS>
+template <int D, int BITS, bool SHARED>
 struct TcSmem {
   static constexpr int kBlockQ = 128 * 128;  // 128 rows of 64 values
   static constexpr int kBlock = kTile * 128;  // 64 rows of 64 values
@@ -72,7 +72,7 @@ struct TcSmem {
   uint64_t row_of[2][BITS < 16 ? 1 : kStages][kTile];  // 16 bits: the tokens' rows in the pages, ~0 where there is nothing
   Span spans[kSpans];
   TcInfo info[kTcInfo];
-  float by_sum[kTcRows];
+  float by_sum[kTcRows], by_prefix[SHARED ? kTcRows : 1];
   uint64_t full[2][kStages], empty[2][kStages];  // keys, values
   // A barrier's phase can be told from the one before only. O is ready twice before anyone has to look, so it has a
   // barrier for even tiles and one for odd ones, as S and P have.
@@ -228,10 +228,11 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   return x;
 }
 
-template <typename T, int D, int BITS>
+// SHARED as for attend_split.
+template <typename T, int D, int BITS, bool SHARED>
 __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_constant__ AttendArgs a) {
   using P = Pair<T>;
-  using S = TcSmem<D, BITS>;
+  using S = TcSmem<D, BITS, SHARED>;
   constexpr uint32_t kStages = S::kStages;
   // fp16: weights are 2^7 times what they stand for, so that only those under 2^-32 of the largest are lost to the second
   // product, and the maximum that they refer to is never more than 2^4 behind: up to 2^11, the exponents above left for a
@@ -299,6 +300,20 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
         const int64_t x = a.causal ? static_cast<int64_t>(it.span.length) - it.span.count + token + 1 : it.span.length;
         seen = x > 0 ? static_cast<int32_t>(x) : 0;
       }
+      const uint64_t shared_row = static_cast<uint64_t>(it.span.first + token) * a.heads + head;
+      const bool before = SHARED && a.behind && has_prefix(a, it.seq);
+      // the tokens of the tile at hand that this row sees, where rows differ: asked for a tile ahead, its number two ahead
+      const bool by_row = SHARED && a.seq_words;
+      const uint64_t* words = nullptr;
+      const uint32_t* listed = nullptr;
+      uint64_t word_ahead = 0;
+      uint32_t unit_ahead = 0;
+      if (by_row && tiles) {
+        words = a.seq_words + static_cast<uint64_t>(min(static_cast<uint32_t>(a.seq_of[it.span.first + token]), b.members - 1)) * a.tile_stride;
+        listed = a.tiles + static_cast<uint64_t>(it.seq) * a.tile_stride + it.lo;
+        word_ahead = words[listed[0]];
+        unit_ahead = tiles > 1 ? listed[1] : 0;
+      }
       // The sum of the weights, and what its roundings left out: a row's tokens may all come to one thread, and
       // 262144 of them 17.5 below a first one, added to it as they came, were off by 1.7e-3 in the log-sum-exp.
       float m = -INFINITY, l = 0.f, l_rest = 0.f;
@@ -335,6 +350,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
 #pragma unroll 1
         for (uint32_t j = 0; j < tiles; ++j, ++n, ++s_n) {
           const TcInfo& info = sm.info[n % kTcInfo];
+          uint64_t word = ~0ull;
+          if (SHARED && by_row) {
+            word = word_ahead;
+            if (j + 1 < tiles) word_ahead = words[unit_ahead];
+            if (j + 2 < tiles) unit_ahead = listed[j + 2];
+          }
           // S first: after an item in which this half had no rows, info may be some phases behind until then
           ok = ok && tc_wait(&sm.s_full[t][s_n % 2], s_n / 2, stop) && tc_wait(&sm.info_full[n % kTcInfo], n / kTcInfo, stop);
           ok = __all_sync(0xffffffffu, ok);
@@ -370,11 +391,11 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
           tc_ld32(s_col + 32, y);
           tc_wait_ld(x);
           tc_wait_ld(y);
-          if (!(info.plain[0] & info.plain[1])) {
+          if (!(info.plain[0] & info.plain[1]) || (SHARED && by_row)) {
             // hides those of 32 tokens that this row does not see
             const int32_t k = seen - info.pos;  // the row sees the first k
-            const uint32_t see0 = info.bits[0] & (k >= 32 ? ~0u : k <= 0 ? 0u : (1u << k) - 1);
-            const uint32_t see1 = info.bits[1] & (k >= 64 ? ~0u : k <= 32 ? 0u : (1u << (k - 32)) - 1);
+            const uint32_t see0 = info.bits[0] & static_cast<uint32_t>(word) & (k >= 32 ? ~0u : k <= 0 ? 0u : (1u << k) - 1);
+            const uint32_t see1 = info.bits[1] & static_cast<uint32_t>(word >> 32) & (k >= 64 ? ~0u : k <= 32 ? 0u : (1u << (k - 32)) - 1);
             if (!__all_sync(0xffffffffu, (see0 & see1) == ~0u)) {
 #pragma unroll
               for (int f = 0; f < 32; ++f) {
@@ -469,7 +490,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
       const bool alone = it.first_cta == it.last_cta;
       const uint64_t part = own_part();
       if (tiles > kTcChain<T> && !alone) bar_sync<1, kTcSoftmax>();  // all have what they kept, before the part is written
-      const float inv = l == 0.f ? 0.f : 1.f / l;
+      Both w2{};
+      if (SHARED && alone && before && real) w2 = both_parts(m, l * kDown, a.rows_ms[shared_row]);
+      const bool add = SHARED && alone && before;
+      // what comes before the rounding: out of the sums here, and out of the prefix's
+      const float inv_own = add ? (w2.sum == 0.f ? 0.f : w2.own * kDown / w2.sum) : l == 0.f ? 0.f : 1.f / l;
+      const float inv_prefix = add && w2.sum != 0.f ? w2.prefix / w2.sum : 0.f;
       T* out = reinterpret_cast<T*>(a.q.out) + static_cast<int64_t>(it.span.first + token) * a.q.out_token +
                static_cast<int64_t>(head) * a.q.out_head;
       if (active) {
@@ -498,7 +524,19 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
                 float* to = a.part + (part + lr) * D + d;
                 *reinterpret_cast<float4*>(to) = make_float4(z[0], z[1], z[2], z[3]);
                 *reinterpret_cast<float4*>(to + 4) = make_float4(z[4], z[5], z[6], z[7]);
+              } else if (SHARED && !a.behind) {
+                float* to = a.rows + shared_row * D + d;
+                *reinterpret_cast<float4*>(to) = make_float4(z[0] * kDown, z[1] * kDown, z[2] * kDown, z[3] * kDown);
+                *reinterpret_cast<float4*>(to + 4) = make_float4(z[4] * kDown, z[5] * kDown, z[6] * kDown, z[7] * kDown);
               } else {
+                if (SHARED && add) {
+                  const float* from = a.rows + shared_row * D + d;
+                  const float4 y0 = *reinterpret_cast<const float4*>(from), y1 = *reinterpret_cast<const float4*>(from + 4);
+                  const float y[8] = {y0.x, y0.y, y0.z, y0.w, y1.x, y1.y, y1.z, y1.w};
+#pragma unroll
+                  for (int i = 0; i < 8; ++i) z[i] = z[i] * inv_own + y[i] * inv_prefix;
+                }
+                const float inv = SHARED && add ? 1.f : inv_own;
                 const uint32_t w[4] = {P::pack(z[0] * inv, z[1] * inv), P::pack(z[2] * inv, z[3] * inv), P::pack(z[4] * inv, z[5] * inv),
                                        P::pack(z[6] * inv, z[7] * inv)};
                 if (a.out_wide) {
@@ -514,7 +552,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
         }
         if (real) {
           if (!alone) a.part_ms[part + lr] = make_float2(m, l);
-          else if (a.lse) a.lse[static_cast<uint64_t>(it.span.first + token) * a.heads + head] = (m + log2f(l * kDown)) * 0.6931471805599453f;
+          else if (SHARED && !a.behind) a.rows_ms[shared_row] = make_float2(m, l * kDown);
+          else if (SHARED && add) {
+            if (a.lse) a.lse[shared_row] = (w2.top + log2f(w2.sum)) * 0.6931471805599453f;
+          } else if (a.lse) a.lse[static_cast<uint64_t>(it.span.first + token) * a.heads + head] = (m + log2f(l * kDown)) * 0.6931471805599453f;
         }
       }
       tc_fence_before();  // O is read before the next item's products are let through (by q_full)
@@ -537,9 +578,16 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
               sum += z.y == 0.f ? 0.f : k * z.y;
               __stcg(&at->x, k);  // the part's factor, for the threads that join it
             }
-            if (a.lse) a.lse[static_cast<uint64_t>(it.span.first + token) * a.heads + head] = (top + log2f(sum * kDown)) * 0.6931471805599453f;
+            if (SHARED && !a.behind) a.rows_ms[shared_row] = make_float2(top, sum * kDown);
+            else if (SHARED && before) {
+              const Both x = both_parts(top, sum * kDown, a.rows_ms[shared_row]);
+              if (a.lse) a.lse[shared_row] = (x.top + log2f(x.sum)) * 0.6931471805599453f;
+              sm.by_sum[lr] = x.sum == 0.f ? 0.f : x.own * kDown / x.sum;
+              sm.by_prefix[lr] = x.sum == 0.f ? 0.f : x.prefix / x.sum;
+            } else if (a.lse)
+              a.lse[static_cast<uint64_t>(it.span.first + token) * a.heads + head] = (top + log2f(sum * kDown)) * 0.6931471805599453f;
           }
-          sm.by_sum[lr] = sum == 0.f ? 0.f : 1.f / sum;
+          if (!SHARED || !(before && real)) sm.by_sum[lr] = SHARED && !a.behind ? kDown : sum == 0.f ? 0.f : 1.f / sum;
           bar_sync<1, kTcSoftmax>();
           const uint32_t rows = min(static_cast<uint32_t>(kTcRows), all - it.rb * kTcRows);
           // eight units of four values to a thread at a time, whose loads are all on their way together (a unit's row is
@@ -574,10 +622,24 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
             for (int u = 0; u < kUnits; ++u) {
               const uint32_t x = x0 + u * kTcSoftmax, row = x / (D / 4), d = x % (D / 4) * 4;
               if (x >= all_units) break;
-              const float by_total = sm.by_sum[row];
+              const float by_row_sum = sm.by_sum[row];
               const uint32_t tok = (it.rb * kTcRows + row) / a.group, hd = it.head * a.group + (it.rb * kTcRows + row) % a.group;
               T* o = reinterpret_cast<T*>(a.q.out) + static_cast<int64_t>(it.span.first + tok) * a.q.out_token +
                      static_cast<int64_t>(hd) * a.q.out_head + d;
+              if constexpr (SHARED) {
+                float4* there = reinterpret_cast<float4*>(a.rows + (static_cast<uint64_t>(it.span.first + tok) * a.heads + hd) * D + d);
+                if (!a.behind) {
+                  *there = make_float4(y[u].x * by_row_sum, y[u].y * by_row_sum, y[u].z * by_row_sum, y[u].w * by_row_sum);
+                  continue;
+                }
+                if (before) {
+                  const float4 z = *there;
+                  const float by_p = sm.by_prefix[row];
+                  y[u] = make_float4(y[u].x * by_row_sum + z.x * by_p, y[u].y * by_row_sum + z.y * by_p, y[u].z * by_row_sum + z.z * by_p,
+                                     y[u].w * by_row_sum + z.w * by_p);
+                }
+              }
+              const float by_total = SHARED && before ? 1.f : by_row_sum;
               if (a.out_wide) {
                 *reinterpret_cast<uint2*>(o) =
                     make_uint2(P::pack(y[u].x * by_total, y[u].y * by_total), P::pack(y[u].z * by_total, y[u].w * by_total));
@@ -620,14 +682,15 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
         uint32_t pos, page, seen;
       };
       const auto unit_of = [&](uint32_t j) {
-        return j >= tiles ? ~0u : a.mask ? __ldg(&a.tiles[static_cast<uint64_t>(it.seq) * a.tile_stride + it.lo + j]) : it.lo + j;
+        return j >= tiles ? ~0u : a.tiles ? __ldg(&a.tiles[static_cast<uint64_t>(it.seq) * a.tile_stride + it.lo + j]) : it.lo + j;
       };
       const auto page_of = [&](uint32_t unit) {
         Page x{unit == ~0u ? 0u : unit * kTile, 0, 0};
         const uint32_t pos = x.pos + tok;
         if (unit != ~0u && pos < it.span.length) {
           x.page = static_cast<uint32_t>(__ldg(&table[pos >> b.page_shift]));
-          x.seen = !a.mask ? 1u : pos < a.mask_stride ? __ldg(&a.mask[it.seq * a.mask_stride + pos]) : 0u;
+          if (SHARED && a.seq_words) x.seen = a.any_words[static_cast<uint64_t>(it.seq) * a.tile_stride + unit] >> tok & 1u;
+          else x.seen = !a.mask ? 1u : pos < a.mask_stride ? __ldg(&a.mask[it.seq * a.mask_stride + pos]) : 0u;
         }
         return x;
       };
@@ -833,9 +896,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
 }
 
 // One CTA to an SM, whose tensor memory it takes whole: more than half of its shared memory.
-template <int D, int BITS>
+template <int D, int BITS, bool SHARED>
 constexpr size_t tc_smem() {
-  return sizeof(TcSmem<D, BITS>) + 1024 > 120 * 1024 ? sizeof(TcSmem<D, BITS>) + 1024 : 120 * 1024;
+  static_assert(sizeof(TcSmem<D, BITS, SHARED>) + 1024 <= 227 * 1024, "an SM's shared memory");
+  return sizeof(TcSmem<D, BITS, SHARED>) + 1024 > 120 * 1024 ? sizeof(TcSmem<D, BITS, SHARED>) + 1024 : 120 * 1024;
 }
 
 }  // namespace

@@ -141,7 +141,8 @@ __device__ __forceinline__ uint32_t unit_at(uint32_t t, uint32_t u) {
   return t * Ring<D, 16>::kRow + (VALUES ? u ^ (t & 7u) : u ^ ((t & 1u) << 2)) * 16;
 }
 
-template <typename T, int D, int BITS, int NT>
+// SHARED: over a prefix that several sequences share (a.rows), or for sequences behind one (a.behind).
+template <typename T, int D, int BITS, int NT, bool SHARED>
 __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) attend_split(const __grid_constant__ AttendArgs a) {
   using P = Pair<T>;
   using H = Pair<__half>;
@@ -157,6 +158,7 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
   __shared__ Span spans[kSpans];
   __shared__ float warp_m[kSplitWarps][kRows], warp_l[kSplitWarps][kRows];
   __shared__ uint2 stages[kSplitWarps][R::kStages];  // the bits of the tokens that are seen, and the first one's place
+  __shared__ uint32_t row_bits[SHARED ? kSplitWarps : 1][R::kStages][kRows];  // and those that each row sees, where rows differ
   __shared__ uint32_t last_here;
   pdl_trigger();
   pdl_wait();
@@ -174,24 +176,36 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
     const uint32_t chunks = (it.hi - it.lo) * kPerTile;
     const int32_t* table = b.table + static_cast<uint64_t>(it.seq) * b.table_stride;
     const uint8_t* mask = a.mask + it.seq * a.mask_stride;
+    const bool by_row = SHARED && a.seq_words;
+    const bool before = SHARED && a.behind && has_prefix(a, it.seq);
+    const uint64_t* row_words = nullptr;  // of row `lane`
+    if (by_row && lane < rows) row_words = a.seq_words + static_cast<uint64_t>(min(static_cast<uint32_t>(a.seq_of[it.span.first + (row0 + lane) / a.group]), b.members - 1)) * a.tile_stride;
     struct Ahead {
       uint32_t pos, page[kM];  // page: n_pages and above where there is none
       bool seen;               // this lane's token
+      uint32_t row;            // the tokens that row `lane` sees
     };
     const auto look = [&](uint32_t ch) {
       Ahead x;
       x.pos = 0;
       x.seen = false;
+      x.row = 0;
 #pragma unroll
       for (int mt = 0; mt < kM; ++mt) x.page[mt] = ~0u;
       if (ch < chunks) {
         const uint32_t t = it.lo + ch / kPerTile;
-        x.pos = (a.mask ? a.tiles[static_cast<uint64_t>(it.seq) * a.tile_stride + t] : t) * kTile + (ch % kPerTile) * R::kTokens;
+        x.pos = (a.tiles ? a.tiles[static_cast<uint64_t>(it.seq) * a.tile_stride + t] : t) * kTile + (ch % kPerTile) * R::kTokens;
 #pragma unroll
         for (int mt = 0; mt < kM; ++mt)
           if (x.pos + 16 * mt < it.span.length) x.page[mt] = static_cast<uint32_t>(table[(x.pos + 16 * mt) >> b.page_shift]);
         const uint32_t p = x.pos + lane % R::kTokens;
-        x.seen = p < it.span.length && (!a.mask || (p < a.mask_stride && mask[p] != 0));
+        if (by_row) {
+          const uint32_t tile = x.pos / kTile;
+          x.seen = a.any_words[static_cast<uint64_t>(it.seq) * a.tile_stride + tile] >> (p % kTile) & 1u;
+          if (row_words) x.row = static_cast<uint32_t>(row_words[tile] >> (x.pos % kTile));
+        } else {
+          x.seen = p < it.span.length && (!a.mask || (p < a.mask_stride && mask[p] != 0));
+        }
       }
       return x;
     };
@@ -233,6 +247,7 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
         }
       }
       if (lane == 0) stages[warp][stage] = make_uint2(bits, x.pos);
+      if (SHARED && lane < kRows) row_bits[warp][stage][lane] = x.row;
       cp_async_commit();
     };
     Ahead ahead;
@@ -351,6 +366,11 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
       const char* const base = ring + stage * R::kStage;
       const uint32_t bits = stages[warp][stage].x;
       const int32_t pos = static_cast<int32_t>(stages[warp][stage].y);
+      uint32_t sees[NT][2];  // tokens of the chunk that rows 2c and 2c + 1 see
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) sees[nt][e] = by_row ? bits & row_bits[warp][stage][nt * 8 + 2 * c + e] : bits;
       issue(stage == 0 ? R::kStages - 1 : stage - 1, ahead);  // the stage read in the iteration before
       ahead = look(ch + R::kStages * kSplitWarps);
       if (++stage == R::kStages) stage = 0;
@@ -435,16 +455,15 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
           }
         }
       }
-      if (!whole || pos + R::kTokens > all_see) {
+      if (!whole || by_row || pos + R::kTokens > all_see) {
 #pragma unroll
         for (int mt = 0; mt < kM; ++mt)
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const uint32_t t = mt * 16 + tk + (e < 2 ? 0 : 8);
-            const bool there = (bits >> t) & 1u;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
-              if (!there || pos + static_cast<int32_t>(t) >= seen[nt][e % 2]) s[nt][mt][e] = -INFINITY;
+              if (!(sees[nt][e % 2] >> t & 1u) || pos + static_cast<int32_t>(t) >= seen[nt][e % 2]) s[nt][mt][e] = -INFINITY;
           }
       }
       // ---- running maximum, sum and probabilities
@@ -671,8 +690,25 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
     const bool alone = it.first_cta == it.last_cta;
     const uint32_t slot = 2 * blockIdx.x + (blockIdx.x == it.first_cta ? 1 : 0);
     const auto write = [&](uint32_t r, uint32_t d, float4 x, float top, float sum) {
-      const float by = sum == 0.f ? 0.f : 1.f / sum;
       const uint32_t i = it.span.first + (row0 + r) / a.group, h = it.head * a.group + (row0 + r) % a.group;
+      if constexpr (SHARED) {
+        const uint64_t row = static_cast<uint64_t>(i) * a.heads + h;
+        float4* const there = reinterpret_cast<float4*>(a.rows + row * D + d);
+        if (!a.behind) {
+          *there = make_float4(x.x * kDown, x.y * kDown, x.z * kDown, x.w * kDown);
+          if (d == 0) a.rows_ms[row] = make_float2(top, sum * kDown);
+          return;
+        }
+        if (before) {
+          const float4 y = *there;
+          const Both w = both_parts(top, sum * kDown, a.rows_ms[row]);
+          const float own = w.own * kDown;
+          x = make_float4(w.prefix * y.x + own * x.x, w.prefix * y.y + own * x.y, w.prefix * y.z + own * x.z, w.prefix * y.w + own * x.w);
+          top = w.top;
+          sum = w.sum;
+        }
+      }
+      const float down = SHARED && before ? 1.f : kDown, by = sum == 0.f ? 0.f : 1.f / sum;
       T* out = reinterpret_cast<T*>(a.q.out) + static_cast<int64_t>(i) * a.q.out_token + static_cast<int64_t>(h) * a.q.out_head + d;
       if (a.out_wide) {
         *reinterpret_cast<uint2*>(out) = make_uint2(P::pack(x.x * by, x.y * by), P::pack(x.z * by, x.w * by));
@@ -682,7 +718,7 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
         out[2] = Elem<T>::from(x.z * by);
         out[3] = Elem<T>::from(x.w * by);
       }
-      if (a.lse && d == 0) a.lse[static_cast<uint64_t>(i) * a.heads + h] = (top + log2f(sum * kDown)) * 0.6931471805599453f;
+      if (a.lse && d == 0) a.lse[static_cast<uint64_t>(i) * a.heads + h] = (top + log2f(sum * down)) * 0.6931471805599453f;
     };
     for (uint32_t x = threadIdx.x; x < rows * (D / 4); x += kSplitThreads) {
       const uint32_t r = x / (D / 4), d = x % (D / 4) * 4;

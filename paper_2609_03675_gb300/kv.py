@@ -6,6 +6,7 @@ cache of 16-bit values, bytes or 4-bit codes, and attention over it.
     cache = KVCache(n_pages, 64, 32, 8, 128, bits=4, rotary=rotary)
     q = cache.append(k, v, table, lengths, offsets, positions=positions, q=q)
     out, lse = cache.attend(q, table, lengths, offsets, max_new=longest_question)
+    out, lse = cache.attend_shared(q, table, lengths, offsets, prefix_table=stream, prefix_lengths=n)  # questions about one stream
 
 Thin binding of the entry points that include/cofie_kv.h declares (the layout
 of pages and codes is described there); every value is computed in the
@@ -57,16 +58,25 @@ class _Batch(ctypes.Structure):
                 ("offsets", ctypes.c_void_p)]
 
 
+class _Prefix(ctypes.Structure):
+    _fields_ = [("n_groups", ctypes.c_uint32), ("max_new", ctypes.c_uint32), ("table_stride", ctypes.c_uint32),
+                ("table", ctypes.c_void_p), ("lengths", ctypes.c_void_p), ("groups", ctypes.c_void_p), ("mask", ctypes.c_void_p),
+                ("mask_stride", ctypes.c_uint64)]
+
+
 # The calls' structs, packed in one go into a buffer that the handle keeps (a
 # ctypes field costs the host more than a tensor's stride; a step of single
 # tokens is bound by the host).
 _ROWS = struct.Struct("=QQI4xqqqq")
 _BATCH = struct.Struct("=IIIIQQQ")
-assert _ROWS.size == ctypes.sizeof(_Rows) and _BATCH.size == ctypes.sizeof(_Batch)
+_PREFIX = struct.Struct("=III4xQQQQQ")
+assert _ROWS.size == ctypes.sizeof(_Rows) and _BATCH.size == ctypes.sizeof(_Batch) and _PREFIX.size == ctypes.sizeof(_Prefix)
+_PREFIX_AT = _BATCH.size + 3 * _ROWS.size
 
 # Every symbol include/cofie_kv.h declares.
 EXPORTS = ("cofie_rotary_create", "cofie_rotary_destroy", "cofie_rotary_run", "cofie_rotary_last_error", "cofie_kv_create",
-           "cofie_kv_destroy", "cofie_kv_append", "cofie_kv_read", "cofie_kv_attend", "cofie_kv_status", "cofie_kv_last_error")
+           "cofie_kv_destroy", "cofie_kv_append", "cofie_kv_read", "cofie_kv_attend", "cofie_kv_attend_shared", "cofie_kv_status",
+           "cofie_kv_last_error")
 
 _bound = None
 
@@ -87,6 +97,7 @@ def _load():
             ("cofie_kv_append", ctypes.c_int, [vp, vp, vp, vp, vp, vp, vp, vp]),
             ("cofie_kv_read", ctypes.c_int, [vp, vp, vp, vp, vp]),
             ("cofie_kv_attend", ctypes.c_int, [vp, vp, vp, vp, vp, u64, ctypes.c_int, ctypes.c_float, vp]),
+            ("cofie_kv_attend_shared", ctypes.c_int, [vp, vp, vp, vp, vp, vp, u64, ctypes.c_int, ctypes.c_float, vp]),
             ("cofie_kv_status", ctypes.c_int, [vp, vp]),
             ("cofie_kv_last_error", ctypes.c_char_p, [vp])):
         f = getattr(lib, name)
@@ -285,7 +296,8 @@ class KVCache:
         self._lib, self._h, self._index = lib, h.value, index
         self.n_pages, self.page_size, self.n_heads, self.n_kv_heads, self.head_dim = n_pages, page_size, n_heads, n_kv_heads, head_dim
         self.dtype, self.bits, self.rotary = dtype, bits, rotary
-        self._buf = ctypes.create_string_buffer(_BATCH.size + 3 * _ROWS.size)  # a batch, and up to three tensors' rows
+        # a batch, up to three tensors' rows, and the prefixes
+        self._buf = ctypes.create_string_buffer(_PREFIX_AT + _PREFIX.size)
         self._at = ctypes.addressof(self._buf)
 
     def _check(self, rc):
@@ -364,6 +376,13 @@ class KVCache:
         max_new: at least the largest count of new tokens. It chooses the kernel (with offsets and 0, all tokens are taken
         for one sequence's, and many short sequences run the kernel of long questions). mask: uint8
         [sequences, >= the longest], nonzero where a cached token may be seen. scale 0: head_dim ** -0.5."""
+        lse_at, out, lse, rows, at, stride = self._asked(q, table, lengths, offsets, max_new, mask, out, lse, cuda_stream)
+        stream = _raw_stream(self._index) if cuda_stream is None else _stream_of(cuda_stream, self._index)
+        self._check(self._lib.cofie_kv_attend(self._h, self._at, rows, lse_at, at, stride, causal, scale, stream))
+        return out, lse
+
+    def _asked(self, q, table, lengths, offsets, max_new, mask, out, lse, cuda_stream):
+        """What attend and attend_shared check and pack alike."""
         n, index = q.shape[0], self._index
         if q.requires_grad and torch.is_grad_enabled():
             raise ValueError("attention over a cache has no gradient: detach q, or attend under torch.no_grad()")
@@ -375,15 +394,38 @@ class KVCache:
         self._batch(table, lengths, offsets, n, 1 if offsets is None else max_new)
         if lse.dtype is not torch.float32 or lse.shape != (n, self.n_heads) or not lse.is_contiguous() or lse.get_device() != index:
             raise ValueError(f"lse must be a contiguous float32 tensor [{n}, {self.n_heads}] on cuda:{index}")
-        at, stride = None, 0
-        if mask is not None:
-            if mask.dtype not in (torch.uint8, torch.bool) or mask.dim() != 2 or mask.shape[0] != table.shape[0] or not mask.is_contiguous() \
-                    or mask.get_device() != index:
-                raise ValueError(f"mask must be a contiguous uint8 or bool tensor [{table.shape[0]}, tokens] on cuda:{index}")
-            # a mask of no tokens, which hides them all, may have no address; nothing is read at the one it gets here
-            at, stride = mask.data_ptr() or self.k_pages.data_ptr(), mask.shape[1]
+        return lse.data_ptr(), out, lse, r, *self._mask(mask, table.shape[0], "mask")
+
+    def _mask(self, mask, seqs, what):
+        if mask is None:
+            return None, 0
+        if mask.dtype not in (torch.uint8, torch.bool) or mask.dim() != 2 or mask.shape[0] != seqs or not mask.is_contiguous() \
+                or mask.get_device() != self._index:
+            raise ValueError(f"{what} must be a contiguous uint8 or bool tensor [{seqs}, tokens] on cuda:{self._index}")
+        # a mask of no tokens, which hides them all, may have no address; nothing is read at the one it gets here
+        return mask.data_ptr() or self.k_pages.data_ptr(), mask.shape[1]
+
+    def attend_shared(self, q, table, lengths, offsets=None, *, prefix_table, prefix_lengths, groups=None, max_new=0, max_shared=0,
+                      mask=None, prefix_mask=None, causal=True, scale=0.0, out=None, lse=None, cuda_stream=None):
+        """As attend(), for sequences that share prefixes, each read once for all of them: the answers or questions about
+        one stream. table, lengths, mask and causal are those of a sequence's own cached tokens, which come behind its prefix.
+        Group g is sequences groups[g] to groups[g + 1] (int32 [groups + 1]; None: one group of all), and its prefix the
+        prefix_lengths[g] tokens in the pages prefix_table[g]; sequences of no group have no prefix. max_shared: at least the
+        largest count of a group's new tokens together (0: all); it chooses the kernel. prefix_mask: uint8
+        [sequences, >= the longest prefix], nonzero where a sequence may see a token of its prefix (its own evidence)."""
+        index = self._index
+        lse_at, out, lse, rows, at, stride = self._asked(q, table, lengths, offsets, max_new, mask, out, lse, cuda_stream)
+        if prefix_table.dtype is not torch.int32 or prefix_table.get_device() != index or prefix_table.dim() != 2 or not prefix_table.is_contiguous():
+            raise ValueError(f"prefix_table must be a contiguous int32 tensor [groups, pages] on cuda:{index}")
+        n, width = prefix_table.shape
+        if groups is None and n != 1:
+            raise ValueError("without groups prefix_table has one row")
+        mask_at, mask_stride = self._mask(prefix_mask, table.shape[0], "prefix_mask")
+        _PREFIX.pack_into(self._buf, _PREFIX_AT, n, max_shared, width, prefix_table.data_ptr(),
+                          _int32(prefix_lengths, index, "prefix_lengths", (n,)),
+                          0 if groups is None else _int32(groups, index, "groups", (n + 1,)), mask_at or 0, mask_stride)
         stream = _raw_stream(index) if cuda_stream is None else _stream_of(cuda_stream, index)
-        self._check(self._lib.cofie_kv_attend(self._h, self._at, r, lse.data_ptr(), at, stride, causal, scale, stream))
+        self._check(self._lib.cofie_kv_attend_shared(self._h, self._at, self._at + _PREFIX_AT, rows, lse_at, at, stride, causal, scale, stream))
         return out, lse
 
     def status(self, cuda_stream=None):

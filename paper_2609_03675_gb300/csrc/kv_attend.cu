@@ -3,6 +3,8 @@
 #include <algorithm>
 #include <cmath>
 
+#include <cudaTypedefs.h>
+
 #include "kv_kernels.cuh"
 
 namespace cofie {
@@ -155,8 +157,32 @@ AttendLaunch kernel_of(const cofie_kv_params& p, int kind, bool shared) {
 
 }  // namespace
 
+namespace {
+
+// The map of 16-bit pages, whose copies lie as the products read them.
+cudaError_t map_pages(const cofie_kv_params& p, void* pages, CUtensorMap* map) {
+  void* f = nullptr;
+  cudaDriverEntryPointQueryResult found;
+  const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found);
+  if (e != cudaSuccess) return e;
+  if (found != cudaDriverEntryPointSuccess) return cudaErrorNotSupported;
+  const cuuint64_t dims[3] = {p.head_dim, static_cast<cuuint64_t>(p.n_kv_heads) * p.page_size, p.n_pages};
+  const cuuint64_t strides[2] = {2ull * p.head_dim, 2ull * p.head_dim * p.n_kv_heads * p.page_size};
+  const cuuint32_t box[3] = {64, std::min(p.page_size, kTile), 1}, steps[3] = {1, 1, 1};
+  const CUresult r = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(f)(
+      map, p.dtype == COFIE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, pages, dims, strides, box, steps,
+      CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
+}
+
+}  // namespace
+
 cudaError_t attend_set_up(cofie_kv* h) {
   cudaError_t e = cudaSuccess;
+  if (h->p.bits == 16) {
+    e = map_pages(h->p, h->p.k_pages, &h->maps[0]);
+    if (e == cudaSuccess) e = map_pages(h->p, h->p.v_pages, &h->maps[1]);
+  }
   size_t rows = 2ull * sm_count() * kManyRows, ctas = 0;
   for (int i = 0; i < 6 && e == cudaSuccess; ++i) {
     const int kind = i % 3;
@@ -210,6 +236,8 @@ int attend_args(cofie_kv* h, const cofie_kv_batch* b, const cofie_rows* q, float
   a.part = h->d_part;
   a.part_ms = h->d_part_ms;
   a.done = h->d_done;
+  a.k_map = h->maps[0];
+  a.v_map = h->maps[1];
   return COFIE_OK;
 }
 

@@ -1,6 +1,8 @@
 // The paged cache's handle, shared by its entry points.
 #pragma once
 
+#include <cuda.h>
+
 #include <string>
 
 #include "kv_rows.cuh"
@@ -14,6 +16,7 @@ struct cofie_kv {
   // parts that they leave, and the tiles that a mask leaves. That list grows on
   // demand, to twice its size at least; those before it stay with the handle,
   // because a captured call keeps the address that it was captured with.
+  CUtensorMap maps[2];  // of 16-bit pages: keys, values
   uint32_t split_ctas[2][2] = {};  // of the kernels for shared prefixes, too
   float* d_part = nullptr;
   float2* d_part_ms = nullptr;

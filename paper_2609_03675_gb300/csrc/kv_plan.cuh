@@ -51,6 +51,7 @@ struct AttendArgs {
   const uint64_t* seq_words;
   const uint64_t* any_words;
   const int32_t* seq_of;
+  CUtensorMap k_map, v_map;  // 16-bit pages: [n_pages][heads x places][D], in boxes of 64 values of a tile's tokens in a page
 };
 
 // Whether a prefix's sums are there for the rows of this sequence.

@@ -2,14 +2,24 @@
 // products bound it, so both run on tcgen05.
 //
 // A CTA takes up to 256 query rows (new tokens x heads of the group) of one
-// key/value head as two tiles of 128, and the cached tokens 64 at a time:
-//   softmax    four warps a tile, a thread to a row: maximum, exponentials, P
-//              back into S's place in 16 bits; at the end O out
-//   producers  four warps for keys, four for values: the next tokens into shared
-//              memory (128-byte swizzle), copied (16 bits) or unpacked to
+// key/value head as two tiles of 128, and the cached tokens 64 at a time. Of an
+// item of 128 rows or less both streams of products and softmax take the same
+// rows, and every other tile of tokens each; their sums are joined with the
+// item's other parts.
+//   loader     a warp that looks up pages and masks some tiles ahead, tells the
+//              others what there is to see, and asks for the copies: tiles of
+//              16-bit pages by tensor map, with the 128-byte swizzle, to where
+//              the products read them; codes and bytes as they lie in the pages
+//   unpackers  (less than 16 bits) four warps for keys, four for values: to
 //              (n - z) s or (u - 128) s, which the 16-bit types hold exactly
-//   MMA        a warp for each tile: S = Q K^T into tensor memory (128 x 64 fp32 a tile),
+//   clearer    (16 bits) a warp that puts zeros where a value is not to be seen
+//              (a NaN there would pass through a product with 0)
+//   MMA        a warp for each stream: S = Q K^T into tensor memory (128 x 64 fp32),
 //              and O += P V with P read from tensor memory
+//   softmax    four warps a stream, a thread to a row: maximum, exponentials, P
+//              back into S's place in 16 bits; at the end O out
+// (With copies made by the threads that unpack, 16 bytes each, a tile of bytes
+// took 3300 cycles and one of 16-bit values 3400, however few the rows.)
 // The running maximum that exponentials refer to is raised only when the true
 // one passes it by 2^8 (2^4 for fp16; then O is brought down in tensor memory),
 // which seldom happens after the first tokens. O itself is read out and begun
@@ -33,14 +43,13 @@ namespace cofie {
 namespace {
 
 constexpr int kTcRows = kManyRows;
-constexpr int kTcSoftmax = 256;    // threads: warps 0 to 7
-constexpr int kTcProducers = 128;  // for keys, and as many for values
-constexpr int kTcThreads = kTcSoftmax + 2 * kTcProducers + 128;  // and a group of four warps with the one that issues
-// Of keys, and of values. Bytes as they lie in the pages take twice the codes' room.
+constexpr int kTcSoftmax = 256;  // threads: warps 0 to 7
+constexpr int kTcUnpack = 128;   // of keys, and as many of values
+// And a group of four warps: two that issue, the loader, and one more.
 template <int BITS>
-constexpr int kTcStages = BITS == 8 ? 3 : 4;
-constexpr int kTcInfo = 8;         // more than the stages: a tile is told before its place is free
-constexpr int kTcRaw = 3;          // codes or bytes as they lie in the pages
+constexpr int kTcThreads = kTcSoftmax + (BITS < 16 ? 2 * kTcUnpack : 0) + 128;
+constexpr int kTcInfo = 16;         // more than the stages and the raw tiles: a tile is told before its place is free
+constexpr uint32_t kTcStreamed = 4; // tiles from which an item of 128 rows or less is taken by both streams
 // Tiles whose products are summed in tensor memory before the sums move on to the CTA's part. The tensor core cuts each
 // product off at about 2^-24 of the sum that it is added to, so 8192 tokens may cost a sum 2^-11 of its size, a rounding
 // of fp16, and 65536 tokens 2^-8, one of bf16. (In one sum, 262144 tokens 14 to 17 below a first one came out 0.4 to
@@ -48,32 +57,35 @@ constexpr int kTcRaw = 3;          // codes or bytes as they lie in the pages
 template <typename T>
 constexpr uint32_t kTcChain = std::is_same<T, __half>::value ? 128 : 1024;
 constexpr uint64_t kTcTimeout = 1000000000ull;
-// Registers: all threads start with 96; 256 x 136 + 256 x 72 + 128 x 64 is 640 x 96.
-constexpr int kTcRegsSoftmax = 136, kTcRegsProducer = 72, kTcRegsIssuer = 64;
+// Registers where there are unpackers: all threads start with 96; 256 x 136 + 256 x 72 + 128 x 64 is 640 x 96.
+constexpr int kTcRegsSoftmax = 136, kTcRegsUnpack = 72, kTcRegsIssuer = 64;
 
 struct TcInfo {
   uint32_t bits[2];  // tokens that some row may see
   int32_t pos;       // the first token
-  uint32_t plain[2]; // every token of the half is seen by every row
+  uint32_t plain;    // every token is seen by every row
 };
 
 template <int D, int BITS, bool SHARED>
 struct TcSmem {
-  static constexpr int kBlockQ = 128 * 128;  // 128 rows of 64 values
+  static constexpr int kBlockQ = 128 * 128;   // 128 rows of 64 values
   static constexpr int kBlock = kTile * 128;  // 64 rows of 64 values
+  static constexpr int kStages = BITS < 16 ? 3 : 4;            // of keys, and of values
+  static constexpr int kRaw = BITS == 16 ? 1 : BITS == 8 && D == 128 ? 3 : 6;  // tiles as they lie in the pages
+  static constexpr int kRow = D * BITS / 8, kRowWords = (D / 64) * 2;  // bytes of a token's keys
   union {
     char q[2][kBlockQ * (D / 64)];
-    Plan<kTcThreads> plan;  // until every thread has its walk
+    Plan<kTcThreads<BITS>> plan;  // until every thread has its walk
   };
-  static constexpr int kStages = kTcStages<BITS>;
   char kv[2][kStages][kBlock * (D / 64)];  // keys, values
-  char raw[2][BITS < 16 ? kTcRaw : 1][BITS < 16 ? kTile * (D * BITS / 8) : 16];
-  uint32_t raw_word[2][kTcRaw][kTcProducers];
-  uint64_t row_of[2][BITS < 16 ? 1 : kStages][kTile];  // 16 bits: the tokens' rows in the pages, ~0 where there is nothing
+  char raw[2][kRaw][BITS < 16 ? kTile * kRow : 16];
+  char raw_words[2][kRaw][BITS < 16 ? kTile * kRowWords : 16];
   Span spans[kSpans];
   TcInfo info[kTcInfo];
   float by_sum[kTcRows], by_prefix[SHARED ? kTcRows : 1];
   uint64_t full[2][kStages], empty[2][kStages];  // keys, values
+  uint64_t raw_full[2][kRaw], raw_empty[2][kRaw];
+  uint64_t landed[kStages];  // 16 bits: values before the clearer has seen them
   // A barrier's phase can be told from the one before only. O is ready twice before anyone has to look, so it has a
   // barrier for even tiles and one for odd ones, as S and P have.
   uint64_t info_full[kTcInfo], q_full[2], s_full[2][2], p_full[2][2], o_full[2][2], drained;
@@ -102,8 +114,16 @@ __device__ __forceinline__ bool tc_wait(const uint64_t* bar, uint32_t parity, ui
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+// Copies whose bytes the barrier counts: some that lie in a row, and a box of the pages' tensor map.
+__device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, const uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes),
+               "r"(shared_address(bar))
+               : "memory");
+}
+__device__ __forceinline__ void box_copy(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, int32_t z, const uint64_t* bar) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map),
+               "r"(x), "r"(y), "r"(z), "r"(shared_address(bar))
+               : "memory");
 }
 // What the warp has done before comes before the barrier's phase: one arrival for all its threads (128 arrivals at one
 // address one after the other would cost more than the wait).
@@ -230,10 +250,11 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
 
 // SHARED as for attend_split.
 template <typename T, int D, int BITS, bool SHARED>
-__global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_constant__ AttendArgs a) {
+__global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __grid_constant__ AttendArgs a) {
   using P = Pair<T>;
   using S = TcSmem<D, BITS, SHARED>;
-  constexpr uint32_t kStages = S::kStages;
+  constexpr uint32_t kStages = S::kStages, kRaw = S::kRaw;
+  constexpr int kThreads = kTcThreads<BITS>;
   // fp16: weights are 2^7 times what they stand for, so that only those under 2^-32 of the largest are lost to the second
   // product, and the maximum that they refer to is never more than 2^4 behind: up to 2^11, the exponents above left for a
   // maximum that is a rounding of a large score off. (bf16 has the exponents of fp32.)
@@ -243,14 +264,21 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
   S& sm = *reinterpret_cast<S*>(raw + (1024u - (shared_address(raw) & 1023u)) % 1024u);
   pdl_trigger();
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  constexpr uint32_t kIssuer = (kTcSoftmax + 2 * kTcProducers) / 32;
+  constexpr uint32_t kIssuer = kThreads / 32 - 4;  // and the warp after it; then the loader and the clearer
   if (threadIdx.x == 0) {
-    for (uint32_t i = 0; i < kStages; ++i)
+    for (uint32_t i = 0; i < kStages; ++i) {
       for (int v = 0; v < 2; ++v) {
-        mbar_init(shared_address(&sm.full[v][i]), kTcProducers / 32);
+        mbar_init(shared_address(&sm.full[v][i]), BITS < 16 ? kTcUnpack / 32 : 1);
         mbar_init(shared_address(&sm.empty[v][i]), 2);  // both issuers
       }
-    for (int i = 0; i < kTcInfo; ++i) mbar_init(shared_address(&sm.info_full[i]), 2);
+      mbar_init(shared_address(&sm.landed[i]), 1);
+    }
+    for (uint32_t i = 0; i < kRaw; ++i)
+      for (int v = 0; v < 2; ++v) {
+        mbar_init(shared_address(&sm.raw_full[v][i]), 1);
+        mbar_init(shared_address(&sm.raw_empty[v][i]), kTcUnpack / 32);
+      }
+    for (int i = 0; i < kTcInfo; ++i) mbar_init(shared_address(&sm.info_full[i]), 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(shared_address(&sm.q_full[i]), 4);
       for (int j = 0; j < 2; ++j) {
@@ -275,24 +303,28 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
   const uint32_t tmem = sm.tmem;
   const auto o_at = [&](uint32_t t) { return tmem + t * D; };
   const auto s_at = [&](uint32_t t, uint32_t i) { return tmem + 2 * D + (2 * t + i % 2) * kTile; };
-  Walk<kTcThreads> walk(a, sm.plan, sm.spans, kTcRows, range);
+  Walk<kThreads> walk(a, sm.plan, sm.spans, kTcRows, range);
   __syncthreads();
   const BatchArg& b = a.batch;
   Item it;
   uint32_t* stop = &sm.stop;
   bool ok = true;
+  // whether both streams take the item's rows, every other tile each, and how many tiles of some that makes for a stream
+  const auto streamed = [&](const Item& x) { return x.span.count * a.group - x.rb * kTcRows <= 128 && x.tiles >= kTcStreamed; };
+  const auto tiles_of = [](bool both, uint32_t t, uint32_t tiles) { return both ? (tiles + 1 - t) / 2 : tiles; };
 
   if (warp < kTcSoftmax / 32) {
     // ---------------------------------------------------------------- softmax: thread r of tile t has row r of it
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kTcRegsSoftmax));
+    if constexpr (BITS < 16) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kTcRegsSoftmax));
     const uint32_t t = warp / 4, r = threadIdx.x % 128;
     const uint32_t lanes = (warp % 4) * 32u << 16;
     const uint32_t o_col = o_at(t) + lanes;
     const float by = a.scale * 1.4426950408889634f;
-    uint32_t n = 0, s_n = 0;  // tiles told; tiles of this half
+    uint32_t n = 0, s_n = 0;  // tiles told; tiles of this stream
     while (walk.next(it)) {  // to the end even when a wait ran out: the barriers below count on all
-      const uint32_t row0 = it.rb * kTcRows + t * 128, all = it.span.count * a.group;
-      const uint32_t tiles = it.hi - it.lo;
+      const bool both = streamed(it);
+      const uint32_t row0 = it.rb * kTcRows + (both ? 0 : t * 128), all = it.span.count * a.group;
+      const uint32_t told = it.hi - it.lo, tiles = tiles_of(both, t, told), step = both ? 2 : 1, from = both ? t : 0;
       const bool active = row0 < all, real = row0 + r < all;
       const uint32_t token = real ? (row0 + r) / a.group : 0, head = it.head * a.group + (real ? (row0 + r) % a.group : 0);
       int32_t seen = 0;
@@ -310,9 +342,9 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
       uint32_t unit_ahead = 0;
       if (by_row && tiles) {
         words = a.seq_words + static_cast<uint64_t>(min(static_cast<uint32_t>(a.seq_of[it.span.first + token]), b.members - 1)) * a.tile_stride;
-        listed = a.tiles + static_cast<uint64_t>(it.seq) * a.tile_stride + it.lo;
+        listed = a.tiles + static_cast<uint64_t>(it.seq) * a.tile_stride + it.lo + from;
         word_ahead = words[listed[0]];
-        unit_ahead = tiles > 1 ? listed[1] : 0;
+        unit_ahead = tiles > 1 ? listed[step] : 0;
       }
       // The sum of the weights, and what its roundings left out: a row's tokens may all come to one thread, and
       // 262144 of them 17.5 below a first one, added to it as they came, were off by 1.7e-3 in the log-sum-exp.
@@ -348,21 +380,19 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
           warp_arrive(&sm.q_full[t]);
         }
 #pragma unroll 1
-        for (uint32_t j = 0; j < tiles; ++j, ++n, ++s_n) {
-          const TcInfo& info = sm.info[n % kTcInfo];
+        for (uint32_t j = 0; j < tiles; ++j, ++s_n) {
+          const uint32_t at = n + from + j * step;  // of all tiles
+          const TcInfo& info = sm.info[at % kTcInfo];
           uint64_t word = ~0ull;
           if (SHARED && by_row) {
             word = word_ahead;
             if (j + 1 < tiles) word_ahead = words[unit_ahead];
-            if (j + 2 < tiles) unit_ahead = listed[j + 2];
+            if (j + 2 < tiles) unit_ahead = listed[(j + 2) * step];
           }
           // S first: after an item in which this half had no rows, info may be some phases behind until then
-          ok = ok && tc_wait(&sm.s_full[t][s_n % 2], s_n / 2, stop) && tc_wait(&sm.info_full[n % kTcInfo], n / kTcInfo, stop);
+          ok = ok && tc_wait(&sm.s_full[t][s_n % 2], s_n / 2, stop) && tc_wait(&sm.info_full[at % kTcInfo], at / kTcInfo, stop);
           ok = __all_sync(0xffffffffu, ok);
-          if (!ok) {
-            n += tiles - j;
-            break;
-          }
+          if (!ok) break;
           tc_fence_after();
           if (j > 0 && j % kTcChain<T> == 0) {
             ok = tc_wait(&sm.o_full[t][(s_n - 1) % 2], (s_n - 1) / 2, stop);
@@ -391,7 +421,7 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
           tc_ld32(s_col + 32, y);
           tc_wait_ld(x);
           tc_wait_ld(y);
-          if (!(info.plain[0] & info.plain[1]) || (SHARED && by_row)) {
+          if (!info.plain || (SHARED && by_row)) {
             // hides those of 32 tokens that this row does not see
             const int32_t k = seen - info.pos;  // the row sees the first k
             const uint32_t see0 = info.bits[0] & static_cast<uint32_t>(word) & (k >= 32 ? ~0u : k <= 0 ? 0u : (1u << k) - 1);
@@ -426,16 +456,16 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
             l_rest *= k;
             m = to;
           }
-          const float from = m == -INFINITY ? 0.f : kUp - m;
-          const uint64_t by2 = two(by, by), from2 = two(from, from);
+          const float down = m == -INFINITY ? 0.f : kUp - m;
+          const uint64_t by2 = two(by, by), down2 = two(down, down);
           uint64_t l2 = two(0.f, 0.f), l3 = two(0.f, 0.f);
           const auto exponentials = [&](const uint32_t* z, uint32_t col) {
             uint32_t w[16];
 #pragma unroll
             for (int f = 0; f < 16; f += 2) {
               float p0, p1, p2, p3;
-              apart(fma2(two(z[2 * f], z[2 * f + 1]), by2, from2), p0, p1);
-              apart(fma2(two(z[2 * f + 2], z[2 * f + 3]), by2, from2), p2, p3);
+              apart(fma2(two(z[2 * f], z[2 * f + 1]), by2, down2), p0, p1);
+              apart(fma2(two(z[2 * f + 2], z[2 * f + 3]), by2, down2), p2, p3);
               p0 = exp2_fast(p0);
               p1 = exp2_fast(p1);
               p2 = exp2_fast(p2);
@@ -485,11 +515,10 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
           tc_wait_st();
         }
       }
-      // info of tiles that this half does not use
-      if (!active) n += tiles;
-      const bool alone = it.first_cta == it.last_cta;
+      n += told;
+      const bool alone = it.first_cta == it.last_cta && !both;
       const uint64_t part = own_part();
-      if (tiles > kTcChain<T> && !alone) bar_sync<1, kTcSoftmax>();  // all have what they kept, before the part is written
+      if (told > kTcChain<T> && !alone) bar_sync<1, kTcSoftmax>();  // all have what they kept, before the part is written
       Both w2{};
       if (SHARED && alone && before && real) w2 = both_parts(m, l * kDown, a.rows_ms[shared_row]);
       const bool add = SHARED && alone && before;
@@ -561,13 +590,18 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
       tc_fence_before();  // O is read before the next item's products are let through (by q_full)
       if (!alone) {
         bar_sync<1, kTcSoftmax>();
-        const uint32_t parts = it.last_cta - it.first_cta + 1;
-        if (threadIdx.x == 0) sm.last_here = part_done(a, it);
+        const uint32_t parts = (it.last_cta - it.first_cta + 1) << both;
+        // (the count is that of the item that goes on from this CTA: one whose streams alone are joined has none)
+        if (threadIdx.x == 0) sm.last_here = it.first_cta == it.last_cta || part_done(a, it);
         bar_sync<1, kTcSoftmax>();
         if (sm.last_here) {
-          const auto part_at = [&](uint32_t i, uint32_t row) { return (2ull * (it.first_cta + i) + (i == 0)) * kTcRows + row; };
+          // both streams' parts lie one behind the other in a CTA's
+          const auto part_at = [&](uint32_t i, uint32_t row) {
+            const uint32_t cta = i >> both;
+            return (2ull * (it.first_cta + cta) + (cta == 0)) * kTcRows + (both ? i % 2 * 128 : 0) + row;
+          };
           float top = -INFINITY, sum = 0.f;
-          if (real) {
+          if (real && !(both && t == 1)) {
 #pragma unroll 4
             for (uint32_t i = 0; i < parts; ++i) top = fmaxf(top, __ldcg(&a.part_ms[part_at(i, lr)]).x);
 #pragma unroll 4
@@ -655,202 +689,102 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
         }
       }
     }
-  } else if (warp < kIssuer) {
-    // ---------------------------------------------------------------- producers of keys (v = 0) and of values (v = 1)
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kTcRegsProducer));
-    const uint32_t v = warp / 4 - kTcSoftmax / 128, p = threadIdx.x % kTcProducers;
-    const uint32_t tok = p % kTile, half = p / kTile;  // two threads to a token
-    const char* const pages = v ? a.v : a.k;
-    const uint16_t* const words = v ? a.v_words : a.k_words;
-    uint32_t n = 0;  // tiles so far
-    while (walk.next(it)) {  // to the end, as above
-      const uint32_t tiles = it.hi - it.lo;
-      const int32_t* table = b.table + static_cast<uint64_t>(it.seq) * b.table_stride;
-      // the fewest tokens that a row of the item sees
-      int32_t all_see = it.span.length;
-      if (a.causal) {
-        const int64_t x = static_cast<int64_t>(it.span.length) - it.span.count + it.rb * kTcRows / a.group + 1;
-        all_see = x > 0 ? static_cast<int32_t>(x) : 0;
-      }
-      struct Token {
-        uint32_t pos;  // of the tile's first
-        uint64_t row;  // in the pages; ~0 where there is nothing to see
-      };
-      // A token's row takes two loads one after the other where there is a mask (the tile's number, then the page and the
-      // mask): each is used a tile after it was asked for, so that nobody waits for it.
-      struct Page {
-        uint32_t pos, page, seen;
-      };
-      const auto unit_of = [&](uint32_t j) {
-        return j >= tiles ? ~0u : a.tiles ? __ldg(&a.tiles[static_cast<uint64_t>(it.seq) * a.tile_stride + it.lo + j]) : it.lo + j;
-      };
-      const auto page_of = [&](uint32_t unit) {
-        Page x{unit == ~0u ? 0u : unit * kTile, 0, 0};
-        const uint32_t pos = x.pos + tok;
-        if (unit != ~0u && pos < it.span.length) {
-          x.page = static_cast<uint32_t>(__ldg(&table[pos >> b.page_shift]));
-          if (SHARED && a.seq_words) x.seen = a.any_words[static_cast<uint64_t>(it.seq) * a.tile_stride + unit] >> tok & 1u;
-          else x.seen = !a.mask ? 1u : pos < a.mask_stride ? __ldg(&a.mask[it.seq * a.mask_stride + pos]) : 0u;
-        }
-        return x;
-      };
-      const auto row_of = [&](const Page& x) {
-        Token y{x.pos, ~0ull};
-        if (x.seen) {
-          if (x.page < b.n_pages)
-            y.row = ((static_cast<uint64_t>(x.page) * b.kv_heads + it.head) << b.page_shift) + ((x.pos + tok) & ((1u << b.page_shift) - 1));
-          else
-            atomicOr(b.err, kKvErrPage);
-        }
-        return y;
-      };
-      const auto tell = [&](const Token& x, uint32_t i) {  // what the softmax has to know of tile i
-        if (v || half) return;
-        TcInfo& info = sm.info[i % kTcInfo];
-        const bool there = x.row != ~0ull;
-        const uint32_t bits = __ballot_sync(0xffffffffu, there);
-        const uint32_t plain = __all_sync(0xffffffffu, there && static_cast<int32_t>(x.pos + tok) < all_see);
-        if (lane == 0) {
-          info.bits[tok / 32] = bits;
-          info.plain[tok / 32] = plain;
-          if (tok == 0) info.pos = static_cast<int32_t>(x.pos);
-          mbar_arrive(shared_address(&sm.info_full[i % kTcInfo]));
-        }
-      };
-      if (BITS < 16) {
-        // Codes are fetched three tiles ahead, each thread's to places of its own.
-        constexpr uint32_t kPart = D * BITS / 256;  // 16-byte pieces of a thread, which has half a token
-        const auto fetch = [&](uint32_t i, const Token& y) {
-          if (y.row != ~0ull) {
-            const char* from = pages + y.row * (D * BITS / 8) + half * (D * BITS / 16);
-            const uint32_t to = shared_address(sm.raw[v][i % kTcRaw]) + p * 16;
-#pragma unroll
-            for (int e = 0; e < static_cast<int>(kPart); ++e) cp_async16(to + e * 2048, from + e * 16, true);
-            // the word, or two, of the token; with one, of it and its neighbour (an even token's row is even)
-            cp_async4(shared_address(&sm.raw_word[v][i % kTcRaw][p]), words + (D == 128 ? 2 * y.row : y.row & ~1ull));
-          } else {
-            sm.raw_word[v][i % kTcRaw][p] = 0;  // the scale of nothing is zero
-          }
-          cp_async_commit();
-        };
-        uint32_t unit[5];
-        Page page[4];
-        Token x[3];
-#pragma unroll
-        for (int i = 0; i < 5; ++i) unit[i] = unit_of(i);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) page[i] = page_of(unit[i]);
-#pragma unroll
-        for (int i = 0; i < 3; ++i) x[i] = row_of(page[i]);
-        Page page_ahead = page[3];      // of tile j + 3
-        uint32_t unit_ahead = unit[4];  // of tile j + 4
-        fetch(n, x[0]);
-        fetch(n + 1, x[1]);
-        fetch(n + 2, x[2]);
+  } else if (BITS < 16 && warp < kIssuer) {
+    // ---------------------------------------------------------------- unpackers of keys (v = 0) and of values (v = 1)
+    if constexpr (BITS < 16) {
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kTcRegsUnpack));
+      const uint32_t v = warp / 4 - kTcSoftmax / 128, w = warp % 4;  // warp w has tokens 16 w and on
+      // A lane's 16-byte units of its warp's tokens, so that neither its reads (rows as the pages have them) nor its writes
+      // (128-byte swizzle) meet a bank twice: eight lanes read 128 bytes in a row, or the halves of two rows that lie so,
+      // and write to eight different units of a row.
+      constexpr int kRowUnits = S::kRow / 16, kTurns = kRowUnits / 2;
+      uint32_t n = 0;  // tiles so far
+      while (walk.next(it)) {  // to the end, as above
+        const uint32_t tiles = it.hi - it.lo;
 #pragma unroll 1
         for (uint32_t j = 0; j < tiles; ++j, ++n) {
-          const uint32_t st = n % kStages, round = n / kStages;
-          tell(x[0], n);
-          cp_async_wait<kTcRaw - 1>();
-          if (round > 0) ok = ok && tc_wait(&sm.empty[v][st], round - 1, stop);
-          if (ok) {
-            const char* from = sm.raw[v][n % kTcRaw] + p * 16;
-            const uint32_t w = sm.raw_word[v][n % kTcRaw][p];
-            const uint32_t word = D == 64 ? (tok % 2 ? w >> 16 : w & 0xFFFFu) : (half ? w >> 16 : w & 0xFFFFu);
-            const std::conditional_t<BITS == 8, Bytes<T>, Unpack<T>> u(word);
-            char* to = sm.kv[v][st] + (D == 128 ? half * S::kBlock : 0) + tok * 128;
-#pragma unroll
-            for (int e = 0; e < static_cast<int>(kPart); ++e) {
-              const uint4 y = *reinterpret_cast<const uint4*>(from + e * 2048);
-              const uint32_t ws[4] = {y.x, y.y, y.z, y.w};
-              if constexpr (BITS == 8) {
-#pragma unroll
-                for (int f = 0; f < 2; ++f) {
-                  const uint2 a0 = u(ws[2 * f]), a1 = u(ws[2 * f + 1]);
-                  *reinterpret_cast<uint4*>(to + (((D == 64 ? 4 * half : 0) + 2 * e + f) ^ (tok & 7)) * 16) = make_uint4(a0.x, a0.y, a1.x, a1.y);
-                }
-              } else {
-#pragma unroll
-                for (int f = 0; f < 4; ++f)
-                  *reinterpret_cast<uint4*>(to + (((D == 64 ? 4 * half : 0) + 4 * e + f) ^ (tok & 7)) * 16) = u(ws[f]);
-              }
-            }
-            fence_async_shared();
-          }
+          const uint32_t st = n % kStages, slot = n % kRaw;
+          ok = ok && tc_wait(&sm.info_full[n % kTcInfo], n / kTcInfo, stop) && tc_wait(&sm.raw_full[v][slot], n / kRaw, stop);
+          if (n >= kStages) ok = ok && tc_wait(&sm.empty[v][st], n / kStages - 1, stop);
           ok = __all_sync(0xffffffffu, ok);
-          if (ok) warp_arrive(&sm.full[v][st]);
-          x[0] = x[1], x[1] = x[2], x[2] = row_of(page_ahead);
-          fetch(n + 3, x[2]);
-          page_ahead = page_of(unit_ahead);
-          unit_ahead = unit_of(j + 5);
-        }
-        cp_async_wait<0>();
-      } else {
-        // Copies of three tiles are on their way at a time.
-        constexpr uint32_t kUnits = D / 8;  // 16-byte units of a token
-        constexpr uint32_t kAhead = kStages - 1;
-        uint32_t unit_ahead = unit_of(1);
-        Page page_ahead = page_of(unit_of(0));
-#pragma unroll 1
-        for (uint32_t j = 0; j < tiles + kAhead - 1; ++j) {
-          const uint32_t i = n + j, st = i % kStages, round = i / kStages;
-          if (j < tiles) {
-            const Token x = row_of(page_ahead);
-            page_ahead = page_of(unit_ahead);
-            unit_ahead = unit_of(j + 2);
-            if (half == 0) sm.row_of[v][st][tok] = x.row;
-            tell(x, i);
-            if (v == 0) bar_sync<2, kTcProducers>();
-            else bar_sync<3, kTcProducers>();
-            if (round > 0) ok = ok && tc_wait(&sm.empty[v][st], round - 1, stop);
-            if (ok) {
-              const uint32_t to = shared_address(sm.kv[v][st]);
-#pragma unroll 4
-              for (uint32_t e = p; e < kTile * kUnits; e += kTcProducers) {
-                const uint32_t tk = e / kUnits, u = e % kUnits;
-                const uint64_t row = sm.row_of[v][st][tk];
-                const bool live = row != ~0ull;
-                cp_async16(to + (u / 8) * S::kBlock + tk * 128 + ((u % 8) ^ (tk & 7)) * 16, pages + (live ? row * (D * 2) + u * 16 : 0), live);
+          if (!ok) break;
+          const uint32_t bits = sm.info[n % kTcInfo].bits[w / 2] >> (16 * (w % 2));
+          const char* const raw_rows = sm.raw[v][slot] + w * 16 * S::kRow;
+          const uint16_t* const words = reinterpret_cast<const uint16_t*>(sm.raw_words[v][slot]) + w * 16 * (D / 64);
+          char* const rows = sm.kv[v][st] + w * 16 * 128;
+#pragma unroll
+          for (int e = 0; e < kTurns; ++e) {
+            uint32_t tok, unit;
+            if (kRowUnits == 8) {
+              tok = 8 * (e / 2) + lane / 4;
+              unit = lane % 4 + 4 * ((lane / 4 + e) & 1);
+            } else {
+              tok = e * (32 / kRowUnits) + lane / kRowUnits;
+              unit = lane % kRowUnits;
+            }
+            const uint4 y = *reinterpret_cast<const uint4*>(raw_rows + tok * S::kRow + unit * 16);
+            const uint32_t d = unit * (128 / BITS);  // the unit's first dim
+            uint32_t word = words[tok * (D / 64) + d / 64];
+            if (!(bits >> tok & 1u)) word = 0;  // the scale of nothing is zero
+            const std::conditional_t<BITS == 8, Bytes<T>, Unpack<T>> u(word);
+            char* const to = rows + d / 64 * S::kBlock + tok * 128;
+            const uint32_t ws[4] = {y.x, y.y, y.z, y.w};
+            if constexpr (BITS == 8) {
+#pragma unroll
+              for (int f = 0; f < 2; ++f) {
+                const uint2 a0 = u(ws[2 * f]), a1 = u(ws[2 * f + 1]);
+                *reinterpret_cast<uint4*>(to + ((d % 64 / 8 + f) ^ (tok & 7)) * 16) = make_uint4(a0.x, a0.y, a1.x, a1.y);
+              }
+            } else {
+#pragma unroll
+              for (int f = 0; f < 4; ++f) {
+                // the second 64 dims' units in another order: their lanes write at the same time
+                const bool other = D == 128 && unit >= 2;
+                const uint32_t g = other ? f ^ 2 : f, x = other ? ws[f ^ 2] : ws[f];
+                *reinterpret_cast<uint4*>(to + ((d % 64 / 8 + g) ^ (tok & 7)) * 16) = u(x);
               }
             }
           }
-          cp_async_commit();
-          if (j + 1 >= kAhead) {  // the tile of two steps before is there
-            cp_async_wait<kAhead - 1>();
-            fence_async_shared();
-            ok = __all_sync(0xffffffffu, ok);
-            if (ok) warp_arrive(&sm.full[v][(i + 1 - kAhead) % kStages]);
+          fence_async_shared();
+          __syncwarp();
+          if (lane == 0) {
+            mbar_arrive(shared_address(&sm.full[v][st]));
+            mbar_arrive(shared_address(&sm.raw_empty[v][slot]));
           }
         }
-        n += tiles;
       }
     }
-    cp_async_wait<0>();
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kTcRegsIssuer));
+    if constexpr (BITS < 16) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kTcRegsIssuer));
     if (warp < kIssuer + 2) {
       // -------------------------------------------------------------- products: a warp for each tile
       constexpr uint32_t kQK = tc_idesc<T>(128, kTile, false), kPV = tc_idesc<T>(128, D, true);
       const uint32_t leader = tc_leader(), t = warp - kIssuer;
-      uint32_t n = 0, q_n = 0, s_n = 0;  // tiles so far; items and tiles of this half
+      uint32_t n = 0, q_n = 0, s_n = 0;  // tiles so far; items and tiles of this stream
       while (ok && walk.next(it)) {
-        const uint32_t tiles = it.hi - it.lo, halves = it.span.count * a.group - it.rb * kTcRows > 128 ? 2 : 1;
-        if (t >= halves) {  // nothing to issue, but to stay in step: a barrier's phases are told apart by their parity
-          for (uint32_t j = 0; j < tiles; ++j, ++n)
-            for (uint32_t v = 0; v < 2; ++v) {
-              ok = ok && tc_wait(&sm.full[v][n % kStages], n / kStages, stop);
-              ok = __all_sync(0xffffffffu, ok);
-              if (ok) warp_arrive(&sm.empty[v][n % kStages]);
-            }
-          continue;
-        }
-        if (tiles == 0) continue;
+        const uint32_t told = it.hi - it.lo;
+        const bool both = streamed(it);
+        const uint32_t halves = it.span.count * a.group - it.rb * kTcRows > 128 ? 2 : 1;
+        const uint32_t tiles = !both && t >= halves ? 0 : tiles_of(both, t, told), step = both ? 2 : 1, from = both ? t : 0;
+        // What the other stream alone takes is let through in its turn: a barrier's phases are told apart by their parity.
+        uint32_t passed[2] = {0, 0};
+        const auto pass = [&](uint32_t v, uint32_t upto) {  // tiles before `upto` of the item
+          for (; passed[v] < upto; ++passed[v]) {
+            if (tiles && passed[v] >= from && (passed[v] - from) % step == 0) continue;  // this stream's own
+            const uint32_t st = (n + passed[v]) % kStages;
+            ok = ok && tc_wait(&sm.full[v][st], (n + passed[v]) / kStages, stop);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) return;
+            warp_arrive(&sm.empty[v][st]);
+          }
+        };
         const auto qk = [&](uint32_t j) {
-          const uint32_t st = (n + j) % kStages, i = s_n + j;
+          const uint32_t at = n + from + j * step, st = at % kStages, i = s_n + j;
+          pass(0, from + j * step);
           if (j == 0) ok = ok && tc_wait(&sm.q_full[t], q_n++, stop);
           // this S holds the P of two tiles before
           if (j > 1) ok = ok && tc_wait(&sm.o_full[t][i % 2], i / 2 - 1, stop);
-          ok = ok && tc_wait(&sm.full[0][st], (n + j) / kStages, stop);
+          ok = ok && tc_wait(&sm.full[0][st], at / kStages, stop);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) return;
           tc_fence_after();
@@ -861,11 +795,12 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
           tc_commit(leader, &sm.s_full[t][i % 2]);
           tc_commit(leader, &sm.empty[0][st]);
         };
-        for (uint32_t j = 0; j < 2 && j < tiles; ++j) qk(j);
+        for (uint32_t j = 0; ok && j < 2 && j < tiles; ++j) qk(j);
 #pragma unroll 1
         for (uint32_t j = 0; ok && j < tiles; ++j) {
-          const uint32_t st = (n + j) % kStages, i = s_n + j;
-          ok = tc_wait(&sm.p_full[t][i % 2], i / 2, stop) && tc_wait(&sm.full[1][st], (n + j) / kStages, stop);
+          const uint32_t at = n + from + j * step, st = at % kStages, i = s_n + j;
+          pass(1, from + j * step);
+          ok = ok && tc_wait(&sm.p_full[t][i % 2], i / 2, stop) && tc_wait(&sm.full[1][st], at / kStages, stop);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
           tc_fence_after();
@@ -876,14 +811,156 @@ __global__ void __launch_bounds__(kTcThreads, 1) attend_rows_tc(const __grid_con
           tc_commit(leader, &sm.empty[1][st]);
           if (j + 2 < tiles) qk(j + 2);
         }
+        if (ok) pass(0, told);
+        if (ok) pass(1, told);
         s_n += tiles;
-        n += tiles;
+        n += told;
       }
       // what was issued, and its arrivals, finish before the tensor memory goes and the CTA ends: waited for even when
       // another wait has run out
       tc_commit(leader, &sm.drained);
       if (!tc_wait(&sm.drained, 0, nullptr)) atomicOr(b.err, kKvErrWait);
       __syncwarp();
+    } else if (warp == kIssuer + 2) {
+      // -------------------------------------------------------------- loader
+      const uint32_t shift = b.page_shift, per = min(1u << shift, kTile);  // tokens of one copy
+      const uint32_t block = lane % 4, v = lane / 4;                       // lanes 0 to 7 copy 16 tokens or more: keys, values
+      const bool leads = lane < 8 && block % (per / 16) == 0;
+      uint32_t n = 0;  // tiles so far
+      while (ok && walk.next(it)) {
+        const uint32_t tiles = it.hi - it.lo;
+        const int32_t* table = b.table + static_cast<uint64_t>(it.seq) * b.table_stride;
+        // the fewest tokens that a row of the item sees
+        int32_t all_see = it.span.length;
+        if (a.causal) {
+          const int64_t x = static_cast<int64_t>(it.span.length) - it.span.count + it.rb * kTcRows / a.group + 1;
+          all_see = x > 0 ? static_cast<int32_t>(x) : 0;
+        }
+        // A tile takes two loads one after the other where there is a mask (its number, then pages and mask): numbers are
+        // asked for three tiles ahead and the others two, so that nobody waits for them.
+        struct Look {
+          uint32_t pos, page;   // the tile's first token; the page of the lane's block of 16, n_pages or above where there is none
+          uint32_t see0, see1;  // of tokens pos + lane and pos + 32 + lane
+        };
+        const auto unit_of = [&](uint32_t j) {
+          return j >= tiles ? ~0u : a.tiles ? __ldg(&a.tiles[static_cast<uint64_t>(it.seq) * a.tile_stride + it.lo + j]) : it.lo + j;
+        };
+        const auto look = [&](uint32_t unit) {
+          Look x{unit == ~0u ? 0u : unit * kTile, ~0u, 0, 0};
+          if (unit == ~0u) return x;
+          const uint32_t length = it.span.length, p = x.pos + 16 * block, p0 = x.pos + lane, p1 = p0 + 32;
+          if (p < length) x.page = static_cast<uint32_t>(__ldg(&table[p >> shift]));
+          if (SHARED && a.seq_words) {
+            const uint64_t word = a.any_words[static_cast<uint64_t>(it.seq) * a.tile_stride + unit];
+            x.see0 = p0 < length ? static_cast<uint32_t>(word >> lane) & 1u : 0u;
+            x.see1 = p1 < length ? static_cast<uint32_t>(word >> 32 >> lane) & 1u : 0u;
+          } else if (a.mask) {
+            const uint8_t* mask = a.mask + it.seq * a.mask_stride;
+            x.see0 = p0 < length && p0 < a.mask_stride ? __ldg(&mask[p0]) : 0u;
+            x.see1 = p1 < length && p1 < a.mask_stride ? __ldg(&mask[p1]) : 0u;
+          } else {
+            x.see0 = p0 < length;
+            x.see1 = p1 < length;
+          }
+          return x;
+        };
+        uint32_t unit = unit_of(2);
+        Look ahead[2] = {look(unit_of(0)), look(unit_of(1))};
+#pragma unroll 1
+        for (uint32_t j = 0; j < tiles; ++j, ++n) {
+          const Look x = ahead[0];
+          ahead[0] = ahead[1];
+          ahead[1] = look(unit);
+          unit = unit_of(j + 3);
+          uint32_t bits0 = __ballot_sync(0xffffffffu, x.see0 != 0), bits1 = __ballot_sync(0xffffffffu, x.see1 != 0);
+          const uint32_t there = __ballot_sync(0xffffffffu, x.page < b.n_pages) & 15u;  // blocks that have a page
+          uint32_t have = 0;  // and of which a token is seen
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            uint32_t& bits = e < 2 ? bits0 : bits1;
+            const uint32_t mine = 0xFFFFu << (16 * (e % 2));
+            if (!(bits & mine)) continue;
+            if (there >> e & 1u) {
+              have |= 1u << e;
+            } else {
+              if (lane == 0) atomicOr(b.err, kKvErrPage);
+              bits &= ~mine;
+            }
+          }
+          // a copy is made where any of its blocks is seen, and its page is there (its blocks have one page)
+          const bool copies = leads && (have >> block & ((1u << (per / 16)) - 1));
+          const uint32_t copied = __popc(__ballot_sync(0xffffffffu, copies && v == 0));
+          const uint32_t st = n % kStages, slot = n % kRaw;
+          if (BITS < 16) {
+            if (n >= kRaw) ok = ok && tc_wait(&sm.raw_empty[0][slot], n / kRaw - 1, stop) && tc_wait(&sm.raw_empty[1][slot], n / kRaw - 1, stop);
+          } else {
+            if (n >= kStages) ok = ok && tc_wait(&sm.empty[0][st], n / kStages - 1, stop) && tc_wait(&sm.empty[1][st], n / kStages - 1, stop);
+          }
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          uint64_t* const bars[2] = {BITS < 16 ? &sm.raw_full[0][slot] : &sm.full[0][st], BITS < 16 ? &sm.raw_full[1][slot] : &sm.landed[st]};
+          if (lane == 0) {
+            TcInfo& info = sm.info[n % kTcInfo];
+            info.bits[0] = bits0;
+            info.bits[1] = bits1;
+            info.pos = static_cast<int32_t>(x.pos);
+            info.plain = (bits0 & bits1) == ~0u && static_cast<int32_t>(x.pos + kTile) <= all_see;
+            mbar_arrive(shared_address(&sm.info_full[n % kTcInfo]));
+            const uint32_t bytes = copied * per * (S::kRow + (BITS < 16 ? S::kRowWords : 0));
+            mbar_arrive_expect_tx(shared_address(bars[0]), bytes);
+            mbar_arrive_expect_tx(shared_address(bars[1]), bytes);
+          }
+          __syncwarp();
+          if (copies) {
+            // (the page of a copy whose first block lies before a page's seen tokens is the same)
+            const uint32_t place = (x.pos + 16 * block) & ((1u << shift) - 1);
+            uint64_t* const bar = v ? bars[1] : bars[0];
+            if (BITS < 16) {
+              const uint64_t row = ((static_cast<uint64_t>(x.page) * b.kv_heads + it.head) << shift) + place;
+              bulk_copy(shared_address(sm.raw[v][slot]) + 16 * block * S::kRow, (v ? a.v : a.k) + row * S::kRow, per * S::kRow, bar);
+              bulk_copy(shared_address(sm.raw_words[v][slot]) + 16 * block * S::kRowWords, (v ? a.v_words : a.k_words) + row * (D / 64),
+                        per * S::kRowWords, bar);
+            } else {
+#pragma unroll
+              for (int h = 0; h < D / 64; ++h)
+                box_copy(shared_address(sm.kv[v][st]) + h * S::kBlock + 16 * block * 128, v ? &a.v_map : &a.k_map, 64 * h,
+                         static_cast<int32_t>((it.head << shift) + place), static_cast<int32_t>(x.page), bar);
+            }
+          }
+          __syncwarp();
+        }
+      }
+      if (!ok) {  // copies in flight land before the CTA ends
+        const uint32_t kept = BITS < 16 ? kRaw : kStages;
+        for (uint32_t i = n > kept ? n - kept : 0; i < n; ++i) {
+          tc_wait(BITS < 16 ? &sm.raw_full[0][i % kRaw] : &sm.full[0][i % kStages], i / kept, nullptr);
+          tc_wait(BITS < 16 ? &sm.raw_full[1][i % kRaw] : &sm.landed[i % kStages], i / kept, nullptr);
+        }
+      }
+    } else if (BITS == 16) {
+      // -------------------------------------------------------------- clearer
+      uint32_t n = 0;
+      while (walk.next(it)) {
+        const uint32_t tiles = it.hi - it.lo;
+#pragma unroll 1
+        for (uint32_t j = 0; j < tiles; ++j, ++n) {
+          const uint32_t st = n % kStages;
+          ok = ok && tc_wait(&sm.info_full[n % kTcInfo], n / kTcInfo, stop) && tc_wait(&sm.landed[st], n / kStages, stop);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
+          const uint32_t bits0 = sm.info[n % kTcInfo].bits[0], bits1 = sm.info[n % kTcInfo].bits[1];
+          if ((bits0 & bits1) != ~0u) {
+#pragma unroll 1
+            for (uint32_t e = lane; e < kTile * (D / 8); e += 32) {
+              const uint32_t tok = e / 8 % kTile;
+              if (!((tok < 32 ? bits0 : bits1) >> (tok % 32) & 1u))
+                *reinterpret_cast<uint4*>(sm.kv[1][st] + e / 8 / kTile * S::kBlock + tok * 128 + e % 8 * 16) = make_uint4(0, 0, 0, 0);
+            }
+          }
+          fence_async_shared();
+          warp_arrive(&sm.full[1][st]);
+        }
+      }
     }
   }
   if (!ok) atomicOr(b.err, kKvErrWait);

@@ -6,10 +6,11 @@
 // item of 128 rows or less both streams of products and softmax take the same
 // rows, and every other tile of tokens each; their sums are joined with the
 // item's other parts.
-//   loader     a warp that looks up pages and masks some tiles ahead, tells the
-//              others what there is to see, and asks for the copies: tiles of
-//              16-bit pages by tensor map, with the 128-byte swizzle, to where
-//              the products read them; codes and bytes as they lie in the pages
+//   loaders    a warp for keys and one for values, which look up pages and masks
+//              some tiles ahead, tell the others what there is to see, and ask
+//              for the copies: tiles of 16-bit pages by tensor map, with the
+//              128-byte swizzle, to where the products read them; codes and
+//              bytes as they lie in the pages
 //   unpackers  (less than 16 bits) four warps for keys, four for values: to
 //              (n - z) s or (u - 128) s, which the 16-bit types hold exactly
 //   clearer    (16 bits) a warp that puts zeros where a value is not to be seen
@@ -45,9 +46,9 @@ namespace {
 constexpr int kTcRows = kManyRows;
 constexpr int kTcSoftmax = 256;  // threads: warps 0 to 7
 constexpr int kTcUnpack = 128;   // of keys, and as many of values
-// And a group of four warps: two that issue, the loader, and one more.
+// And two warps that issue, two loaders, and for 16 bits the clearer.
 template <int BITS>
-constexpr int kTcThreads = kTcSoftmax + (BITS < 16 ? 2 * kTcUnpack : 0) + 128;
+constexpr int kTcThreads = kTcSoftmax + (BITS < 16 ? 2 * kTcUnpack + 128 : 160);
 constexpr int kTcInfo = 16;         // more than the stages and the raw tiles: a tile is told before its place is free
 constexpr uint32_t kTcStreamed = 4; // tiles from which an item of 128 rows or less is taken by both streams
 // Tiles whose products are summed in tensor memory before the sums move on to the CTA's part. The tensor core cuts each
@@ -57,8 +58,8 @@ constexpr uint32_t kTcStreamed = 4; // tiles from which an item of 128 rows or l
 template <typename T>
 constexpr uint32_t kTcChain = std::is_same<T, __half>::value ? 128 : 1024;
 constexpr uint64_t kTcTimeout = 1000000000ull;
-// Registers where there are unpackers: all threads start with 96; 256 x 136 + 256 x 72 + 128 x 64 is 640 x 96.
-constexpr int kTcRegsSoftmax = 136, kTcRegsUnpack = 72, kTcRegsIssuer = 64;
+// Registers where there are unpackers: all threads start with 96; 256 x 136 + 256 x 64 + 128 x 80 is 640 x 96.
+constexpr int kTcRegsSoftmax = 136, kTcRegsUnpack = 64, kTcRegsIssuer = 80;
 
 struct TcInfo {
   uint32_t bits[2];  // tokens that some row may see
@@ -114,15 +115,25 @@ __device__ __forceinline__ bool tc_wait(const uint64_t* bar, uint32_t parity, ui
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_async_shared() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
-// Copies whose bytes the barrier counts: some that lie in a row, and a box of the pages' tensor map.
-__device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, const uint64_t* bar) {
-  asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes),
-               "r"(shared_address(bar))
-               : "memory");
+// Copies whose bytes the barrier counts: some that lie in a row, and a box of the pages' tensor map. Written for a whole
+// warp, of which the leader asks (see tc_leader).
+__device__ __forceinline__ void bulk_copy(uint32_t leader, uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %4, 0;\n\t"
+      "@q cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n\t}" ::"r"(dst),
+      "l"(src), "r"(bytes), "r"(bar), "r"(leader)
+      : "memory");
 }
-__device__ __forceinline__ void box_copy(uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, int32_t z, const uint64_t* bar) {
-  asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map),
-               "r"(x), "r"(y), "r"(z), "r"(shared_address(bar))
+__device__ __forceinline__ void box_copy(uint32_t leader, uint32_t dst, const CUtensorMap* map, int32_t x, int32_t y, int32_t z, uint32_t bar) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %6, 0;\n\t"
+      "@q cp.async.bulk.tensor.3d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n\t}" ::"r"(dst),
+      "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar), "r"(leader)
+      : "memory");
+}
+__device__ __forceinline__ void arrive_expecting(uint32_t leader, uint32_t bar, uint32_t bytes) {
+  asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t@q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}" ::"r"(bar),
+               "r"(bytes), "r"(leader)
                : "memory");
 }
 // What the warp has done before comes before the barrier's phase: one arrival for all its threads (128 arrivals at one
@@ -264,7 +275,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
   S& sm = *reinterpret_cast<S*>(raw + (1024u - (shared_address(raw) & 1023u)) % 1024u);
   pdl_trigger();
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  constexpr uint32_t kIssuer = kThreads / 32 - 4;  // and the warp after it; then the loader and the clearer
+  constexpr uint32_t kIssuer = (kTcSoftmax + (BITS < 16 ? 2 * kTcUnpack : 0)) / 32;  // and the warp after it; then the loaders
   if (threadIdx.x == 0) {
     for (uint32_t i = 0; i < kStages; ++i) {
       for (int v = 0; v < 2; ++v) {
@@ -712,9 +723,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
           const char* const raw_rows = sm.raw[v][slot] + w * 16 * S::kRow;
           const uint16_t* const words = reinterpret_cast<const uint16_t*>(sm.raw_words[v][slot]) + w * 16 * (D / 64);
           char* const rows = sm.kv[v][st] + w * 16 * 128;
-#pragma unroll
-          for (int e = 0; e < kTurns; ++e) {
-            uint32_t tok, unit;
+          const auto place = [&](int e, uint32_t& tok, uint32_t& unit) {
             if (kRowUnits == 8) {
               tok = 8 * (e / 2) + lane / 4;
               unit = lane % 4 + 4 * ((lane / 4 + e) & 1);
@@ -722,13 +731,26 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
               tok = e * (32 / kRowUnits) + lane / kRowUnits;
               unit = lane % kRowUnits;
             }
-            const uint4 y = *reinterpret_cast<const uint4*>(raw_rows + tok * S::kRow + unit * 16);
+          };
+          // all reads before any write: the compiler cannot tell that they do not meet
+          uint4 y[kTurns];
+          uint32_t word[kTurns];
+#pragma unroll
+          for (int e = 0; e < kTurns; ++e) {
+            uint32_t tok, unit;
+            place(e, tok, unit);
+            y[e] = *reinterpret_cast<const uint4*>(raw_rows + tok * S::kRow + unit * 16);
+            word[e] = words[tok * (D / 64) + unit * (128 / BITS) / 64];
+            if (!(bits >> tok & 1u)) word[e] = 0;  // the scale of nothing is zero
+          }
+#pragma unroll
+          for (int e = 0; e < kTurns; ++e) {
+            uint32_t tok, unit;
+            place(e, tok, unit);
             const uint32_t d = unit * (128 / BITS);  // the unit's first dim
-            uint32_t word = words[tok * (D / 64) + d / 64];
-            if (!(bits >> tok & 1u)) word = 0;  // the scale of nothing is zero
-            const std::conditional_t<BITS == 8, Bytes<T>, Unpack<T>> u(word);
+            const std::conditional_t<BITS == 8, Bytes<T>, Unpack<T>> u(word[e]);
             char* const to = rows + d / 64 * S::kBlock + tok * 128;
-            const uint32_t ws[4] = {y.x, y.y, y.z, y.w};
+            const uint32_t ws[4] = {y[e].x, y[e].y, y[e].z, y[e].w};
             if constexpr (BITS == 8) {
 #pragma unroll
               for (int f = 0; f < 2; ++f) {
@@ -821,19 +843,24 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
       tc_commit(leader, &sm.drained);
       if (!tc_wait(&sm.drained, 0, nullptr)) atomicOr(b.err, kKvErrWait);
       __syncwarp();
-    } else if (warp == kIssuer + 2) {
-      // -------------------------------------------------------------- loader
+    } else if (warp < kIssuer + 4) {
+      // -------------------------------------------------------------- loaders of keys (v = 0) and of values (v = 1)
+      const uint32_t v = warp - kIssuer - 2, leader = tc_leader();
       const uint32_t shift = b.page_shift, per = min(1u << shift, kTile);  // tokens of one copy
-      const uint32_t block = lane % 4, v = lane / 4;                       // lanes 0 to 7 copy 16 tokens or more: keys, values
-      const bool leads = lane < 8 && block % (per / 16) == 0;
+      const uint32_t block = lane % 4;                                     // of 16 tokens, whose page the lane looks up
+      const uint32_t base = shared_address(BITS < 16 ? sm.raw[v][0] : sm.kv[v][0]), base_words = shared_address(sm.raw_words[v][0]);
+      uint64_t* const bars = BITS < 16 ? sm.raw_full[v] : v ? sm.landed : sm.full[0];
+      uint64_t* const frees = BITS < 16 ? sm.raw_empty[v] : sm.empty[v];
+      constexpr uint32_t kSlots = BITS < 16 ? kRaw : kStages;
       uint32_t n = 0;  // tiles so far
       while (ok && walk.next(it)) {
         const uint32_t tiles = it.hi - it.lo;
         const int32_t* table = b.table + static_cast<uint64_t>(it.seq) * b.table_stride;
+        const uint32_t length = it.span.length;
         // the fewest tokens that a row of the item sees
-        int32_t all_see = it.span.length;
+        int32_t all_see = length;
         if (a.causal) {
-          const int64_t x = static_cast<int64_t>(it.span.length) - it.span.count + it.rb * kTcRows / a.group + 1;
+          const int64_t x = static_cast<int64_t>(length) - it.span.count + it.rb * kTcRows / a.group + 1;
           all_see = x > 0 ? static_cast<int32_t>(x) : 0;
         }
         // A tile takes two loads one after the other where there is a mask (its number, then pages and mask): numbers are
@@ -842,13 +869,12 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
           uint32_t pos, page;   // the tile's first token; the page of the lane's block of 16, n_pages or above where there is none
           uint32_t see0, see1;  // of tokens pos + lane and pos + 32 + lane
         };
-        const auto unit_of = [&](uint32_t j) {
-          return j >= tiles ? ~0u : a.tiles ? __ldg(&a.tiles[static_cast<uint64_t>(it.seq) * a.tile_stride + it.lo + j]) : it.lo + j;
-        };
+        const uint32_t* const listed = a.tiles ? a.tiles + static_cast<uint64_t>(it.seq) * a.tile_stride + it.lo : nullptr;
+        const auto unit_of = [&](uint32_t j) { return j >= tiles ? ~0u : listed ? __ldg(&listed[j]) : it.lo + j; };
         const auto look = [&](uint32_t unit) {
           Look x{unit == ~0u ? 0u : unit * kTile, ~0u, 0, 0};
           if (unit == ~0u) return x;
-          const uint32_t length = it.span.length, p = x.pos + 16 * block, p0 = x.pos + lane, p1 = p0 + 32;
+          const uint32_t p = x.pos + 16 * block, p0 = x.pos + lane, p1 = p0 + 32;
           if (p < length) x.page = static_cast<uint32_t>(__ldg(&table[p >> shift]));
           if (SHARED && a.seq_words) {
             const uint64_t word = a.any_words[static_cast<uint64_t>(it.seq) * a.tile_stride + unit];
@@ -873,70 +899,60 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
           ahead[1] = look(unit);
           unit = unit_of(j + 3);
           uint32_t bits0 = __ballot_sync(0xffffffffu, x.see0 != 0), bits1 = __ballot_sync(0xffffffffu, x.see1 != 0);
-          const uint32_t there = __ballot_sync(0xffffffffu, x.page < b.n_pages) & 15u;  // blocks that have a page
-          uint32_t have = 0;  // and of which a token is seen
+          const uint32_t there = __ballot_sync(0xffffffffu, x.page < b.n_pages);  // lanes whose block has a page
+          if ((bits0 & bits1) != ~0u || (there & 15u) != 15u) {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            uint32_t& bits = e < 2 ? bits0 : bits1;
-            const uint32_t mine = 0xFFFFu << (16 * (e % 2));
-            if (!(bits & mine)) continue;
-            if (there >> e & 1u) {
-              have |= 1u << e;
-            } else {
-              if (lane == 0) atomicOr(b.err, kKvErrPage);
-              bits &= ~mine;
+            for (int e = 0; e < 4; ++e) {
+              uint32_t& bits = e < 2 ? bits0 : bits1;
+              const uint32_t mine = 0xFFFFu << (16 * (e % 2));
+              if ((bits & mine) && !(there >> e & 1u)) {
+                if (lane == 0) atomicOr(b.err, kKvErrPage);
+                bits &= ~mine;
+              }
             }
           }
-          // a copy is made where any of its blocks is seen, and its page is there (its blocks have one page)
-          const bool copies = leads && (have >> block & ((1u << (per / 16)) - 1));
-          const uint32_t copied = __popc(__ballot_sync(0xffffffffu, copies && v == 0));
-          const uint32_t st = n % kStages, slot = n % kRaw;
-          if (BITS < 16) {
-            if (n >= kRaw) ok = ok && tc_wait(&sm.raw_empty[0][slot], n / kRaw - 1, stop) && tc_wait(&sm.raw_empty[1][slot], n / kRaw - 1, stop);
-          } else {
-            if (n >= kStages) ok = ok && tc_wait(&sm.empty[0][st], n / kStages - 1, stop) && tc_wait(&sm.empty[1][st], n / kStages - 1, stop);
-          }
+          const uint32_t slot = n % kSlots;
+          if (n >= kSlots) ok = ok && tc_wait(&frees[slot], n / kSlots - 1, stop);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
-          uint64_t* const bars[2] = {BITS < 16 ? &sm.raw_full[0][slot] : &sm.full[0][st], BITS < 16 ? &sm.raw_full[1][slot] : &sm.landed[st]};
-          if (lane == 0) {
+          if (v == 0 && lane == 0) {
             TcInfo& info = sm.info[n % kTcInfo];
             info.bits[0] = bits0;
             info.bits[1] = bits1;
             info.pos = static_cast<int32_t>(x.pos);
             info.plain = (bits0 & bits1) == ~0u && static_cast<int32_t>(x.pos + kTile) <= all_see;
             mbar_arrive(shared_address(&sm.info_full[n % kTcInfo]));
-            const uint32_t bytes = copied * per * (S::kRow + (BITS < 16 ? S::kRowWords : 0));
-            mbar_arrive_expect_tx(shared_address(bars[0]), bytes);
-            mbar_arrive_expect_tx(shared_address(bars[1]), bytes);
           }
-          __syncwarp();
-          if (copies) {
-            // (the page of a copy whose first block lies before a page's seen tokens is the same)
-            const uint32_t place = (x.pos + 16 * block) & ((1u << shift) - 1);
-            uint64_t* const bar = v ? bars[1] : bars[0];
-            if (BITS < 16) {
-              const uint64_t row = ((static_cast<uint64_t>(x.page) * b.kv_heads + it.head) << shift) + place;
-              bulk_copy(shared_address(sm.raw[v][slot]) + 16 * block * S::kRow, (v ? a.v : a.k) + row * S::kRow, per * S::kRow, bar);
-              bulk_copy(shared_address(sm.raw_words[v][slot]) + 16 * block * S::kRowWords, (v ? a.v_words : a.k_words) + row * (D / 64),
+          // a copy is made where any of its blocks is seen (its page, which all of them have, is there then)
+          const auto wanted = [&](uint32_t e) {
+            const uint64_t bits = static_cast<uint64_t>(bits1) << 32 | bits0;
+            return (bits >> e & (per == kTile ? ~0ull : (1ull << per) - 1)) != 0;
+          };
+          uint32_t copies = 0;
+          for (uint32_t e = 0; e < kTile; e += per) copies += wanted(e);
+          const uint32_t bar = shared_address(&bars[slot]);
+          arrive_expecting(leader, bar, copies * per * (S::kRow + (BITS < 16 ? S::kRowWords : 0)));
+          const uint32_t place = x.pos & ((1u << shift) - 1);
+#pragma unroll 1
+          for (uint32_t e = 0; e < kTile; e += per) {
+            if (!wanted(e)) continue;
+            const uint32_t page = __shfl_sync(0xffffffffu, x.page, e / 16);
+            if constexpr (BITS < 16) {
+              const uint64_t row = ((static_cast<uint64_t>(page) * b.kv_heads + it.head) << shift) + place;
+              bulk_copy(leader, base + slot * (kTile * S::kRow) + e * S::kRow, (v ? a.v : a.k) + row * S::kRow, per * S::kRow, bar);
+              bulk_copy(leader, base_words + slot * (kTile * S::kRowWords) + e * S::kRowWords, (v ? a.v_words : a.k_words) + row * (D / 64),
                         per * S::kRowWords, bar);
             } else {
 #pragma unroll
               for (int h = 0; h < D / 64; ++h)
-                box_copy(shared_address(sm.kv[v][st]) + h * S::kBlock + 16 * block * 128, v ? &a.v_map : &a.k_map, 64 * h,
-                         static_cast<int32_t>((it.head << shift) + place), static_cast<int32_t>(x.page), bar);
+                box_copy(leader, base + (slot * (D / 64) + h) * S::kBlock + e * 128, v ? &a.v_map : &a.k_map, 64 * h,
+                         static_cast<int32_t>((it.head << shift) + place), static_cast<int32_t>(page), bar);
             }
           }
-          __syncwarp();
         }
       }
-      if (!ok) {  // copies in flight land before the CTA ends
-        const uint32_t kept = BITS < 16 ? kRaw : kStages;
-        for (uint32_t i = n > kept ? n - kept : 0; i < n; ++i) {
-          tc_wait(BITS < 16 ? &sm.raw_full[0][i % kRaw] : &sm.full[0][i % kStages], i / kept, nullptr);
-          tc_wait(BITS < 16 ? &sm.raw_full[1][i % kRaw] : &sm.landed[i % kStages], i / kept, nullptr);
-        }
-      }
+      if (!ok)  // copies in flight land before the CTA ends
+        for (uint32_t i = n > kSlots ? n - kSlots : 0; i < n; ++i) tc_wait(&bars[i % kSlots], i / kSlots, nullptr);
     } else if (BITS == 16) {
       // -------------------------------------------------------------- clearer
       uint32_t n = 0;

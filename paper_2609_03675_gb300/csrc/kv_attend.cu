@@ -200,6 +200,7 @@ cudaError_t attend_set_up(cofie_kv* h) {
   if (e == cudaSuccess) e = cudaMalloc(&h->d_part, rows * h->p.head_dim * sizeof(float));
   if (e == cudaSuccess) e = cudaMalloc(&h->d_part_ms, rows * sizeof(float2));
   if (e == cudaSuccess) e = cudaMalloc(&h->d_done, ctas * sizeof(uint32_t));
+  if (e == cudaSuccess) e = cudaMalloc(&h->d_items, sm_count() * sizeof(SplitItem));
   if (e == cudaSuccess) e = cudaMemset(h->d_done, 0, ctas * sizeof(uint32_t));
   return e;
 }
@@ -236,6 +237,7 @@ int attend_args(cofie_kv* h, const cofie_kv_batch* b, const cofie_rows* q, float
   a.part = h->d_part;
   a.part_ms = h->d_part_ms;
   a.done = h->d_done;
+  a.items = static_cast<SplitItem*>(h->d_items);
   a.k_map = h->maps[0];
   a.v_map = h->maps[1];
   return COFIE_OK;
@@ -292,7 +294,9 @@ int launch_attend(cofie_kv* h, AttendArgs* a, uint64_t rows, bool shared, cudaSt
   a->item_slots = kind == kMany ? 8 : 6;
   const AttendLaunch k = kernel_of(h->p, kind, shared);
   const uint32_t ctas = kind == kMany ? sm_count() : h->split_ctas[shared][kind];
-  return launched(h, launch_dependent(true, k.kernel, dim3(ctas), dim3(k.threads), k.smem, st, *a), "attend");
+  if (const int rc = launched(h, launch_dependent(true, k.kernel, dim3(ctas), dim3(k.threads), k.smem, st, *a), "attend")) return rc;
+  if (kind != kMany) return COFIE_OK;
+  return launched(h, launch_dependent(true, k.join, dim3(ctas, kManyRows / k.join_rows), dim3(k.join_threads), 0, st, *a), "attend");
 }
 
 uint64_t rows_at_most(const cofie_kv_batch* b, uint32_t group) {

@@ -21,6 +21,7 @@ struct cofie_kv {
   float* d_part = nullptr;
   float2* d_part_ms = nullptr;
   uint32_t* d_done = nullptr;
+  void* d_items = nullptr;  // of many rows: those that lie in more than one CTA's range
   uint32_t* d_tiles = nullptr;
   size_t tiles_room = 0;
   uint32_t* d_tiles_before[64] = {};  // doublings that a size_t allows

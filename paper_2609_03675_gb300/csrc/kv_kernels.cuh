@@ -13,6 +13,8 @@ struct AttendLaunch {
   AttendKernel kernel;
   uint32_t threads;
   size_t smem;
+  AttendKernel join;  // many rows: joins the parts, some rows to a CTA
+  uint32_t join_threads, join_rows;
 };
 // The kernel for the handle's type and head length. shared: over a prefix, or behind one.
 template <int BITS>

@@ -9,9 +9,10 @@ namespace {
 
 template <typename T, int D, int BITS, bool SHARED>
 AttendLaunch attend_kernel_of(int kind) {
-  if (kind == kMany) return {attend_rows_tc<T, D, BITS, SHARED>, kTcThreads<BITS>, tc_smem<D, BITS, SHARED>()};
-  if (kind == kFew8) return {attend_split<T, D, BITS, 1, SHARED>, kSplitThreads, split_smem<D, BITS, 1>()};
-  return {attend_split<T, D, BITS, 2, SHARED>, kSplitThreads, split_smem<D, BITS, 2>()};
+  if (kind == kMany)
+    return {attend_rows_tc<T, D, BITS, SHARED>, kTcThreads<BITS>, tc_smem<D, BITS, SHARED>(), attend_join<T, D, SHARED>, kJoinThreads, kJoinRows<D>};
+  if (kind == kFew8) return {attend_split<T, D, BITS, 1, SHARED>, kSplitThreads, split_smem<D, BITS, 1>(), nullptr, 0, 0};
+  return {attend_split<T, D, BITS, 2, SHARED>, kSplitThreads, split_smem<D, BITS, 2>(), nullptr, 0, 0};
 }
 
 }  // namespace

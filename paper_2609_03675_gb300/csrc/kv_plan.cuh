@@ -6,9 +6,10 @@
 // item's fixed cost, are cut into equal ranges, one for each CTA, so that long
 // and short sequences, many heads and one, fill the GPU alike. A CTA works
 // through its range item by item. An item that lies in several ranges leaves a
-// part in each: unnormalised sums, the maximum and the sum of the exponentials;
-// the CTA that finishes last joins them, always in the order of the ranges, so
-// that results do not depend on who is last. Nobody waits for anybody.
+// part in each: unnormalised sums, the maximum and the sum of the exponentials.
+// Parts of few rows are joined by the CTA that finishes last, those of many by a
+// launch of their own, always in the order of the ranges, so that results do not
+// depend on who is last. Nobody waits for anybody.
 #pragma once
 
 #include "kv_handle.cuh"
@@ -17,6 +18,12 @@ namespace cofie {
 
 constexpr uint32_t kTile = 64;       // cached tokens of a tile
 constexpr uint32_t kManyRows = 256;  // rows of a block in the kernel of many rows
+
+// An item of many rows that goes on from the CTA that it begins in.
+struct SplitItem {
+  uint32_t seq, rb, head, last_cta;
+  Span span;
+};
 
 struct AttendArgs {
   BatchArg batch;
@@ -40,6 +47,7 @@ struct AttendArgs {
   float* part;       // [2 x CTAs][rows][D]
   float2* part_ms;   // [2 x CTAs][rows]: maximum (base 2), sum
   uint32_t* done;    // [CTAs]: parts finished of the item that goes on from this CTA; zero between calls
+  SplitItem* items;  // [CTAs], many rows: last_cta is that CTA at most where none goes on
   // Sequences behind a shared prefix take two launches. The first has the groups as its batch, each of them one sequence of
   // all its rows over the prefix, and leaves sums [tokens][heads][D] with the maximum (base 2) and the sum of the weights;
   // the second has the sequences, and adds what it finds there. `prefix`: the first launch's batch, for the second.

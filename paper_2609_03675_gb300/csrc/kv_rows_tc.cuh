@@ -83,14 +83,14 @@ struct TcSmem {
   char raw_words[2][kRaw][BITS < 16 ? kTile * kRowWords : 16];
   Span spans[kSpans];
   TcInfo info[kTcInfo];
-  float by_sum[kTcRows], by_prefix[SHARED ? kTcRows : 1];
+  float by_sum[kTcRows];
   uint64_t full[2][kStages], empty[2][kStages];  // keys, values
   uint64_t raw_full[2][kRaw], raw_empty[2][kRaw];
   uint64_t landed[kStages];  // 16 bits: values before the clearer has seen them
   // A barrier's phase can be told from the one before only. O is ready twice before anyone has to look, so it has a
   // barrier for even tiles and one for odd ones, as S and P have.
   uint64_t info_full[kTcInfo], q_full[2], s_full[2][2], p_full[2][2], o_full[2][2], drained;
-  uint32_t tmem, stop, last_here;
+  uint32_t tmem, stop;
 };
 
 // A wait for a barrier's phase that ends, with false, when it runs out or another's has (with stop).
@@ -303,6 +303,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   pdl_wait();
+  if (threadIdx.x == 0) a.items[blockIdx.x].last_cta = 0;  // none goes on from here, so far
   // only now: a kernel before this one may still hold tensor memory, or wait for it
   if (warp == kIssuer) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(shared_address(&sm.tmem)) : "memory");
@@ -527,9 +528,41 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
         }
       }
       n += told;
-      const bool alone = it.first_cta == it.last_cta && !both;
+      const bool alone = it.first_cta == it.last_cta;
+      if (threadIdx.x == 0 && it.first_cta == blockIdx.x && !alone) a.items[blockIdx.x] = {it.seq, it.rb, it.head, it.last_cta, it.span};
       const uint64_t part = own_part();
       if (told > kTcChain<T> && !alone) bar_sync<1, kTcSoftmax>();  // all have what they kept, before the part is written
+      // Both streams' sums of the same rows: the second's go to the first through Q's place, once all products are done.
+      float k0 = 1.f, k1 = 0.f;
+      float4* const across = reinterpret_cast<float4*>(sm.q[0]);  // [D / 4][128]
+      if (both) {
+        bar_sync<1, kTcSoftmax>();
+        if (t == 1) {
+#pragma unroll 1
+          for (int e = 0; e < D / 32; ++e) {
+            uint32_t y[32];
+            if (tiles) {
+              tc_ld32(o_col + 32 * e, y);
+              tc_wait_ld(y);
+            }
+#pragma unroll
+            for (int f = 0; f < 8; ++f)
+              across[(8 * e + f) * 128 + r] = l != 0.f ? make_float4(__uint_as_float(y[4 * f]), __uint_as_float(y[4 * f + 1]), __uint_as_float(y[4 * f + 2]),
+                                                                     __uint_as_float(y[4 * f + 3]))
+                                                       : make_float4(0.f, 0.f, 0.f, 0.f);
+          }
+          sm.by_sum[r] = m;
+          sm.by_sum[128 + r] = l;
+        }
+        bar_sync<1, kTcSoftmax>();
+        if (t == 0) {
+          const Both x = both_parts(m, l, make_float2(sm.by_sum[r], sm.by_sum[128 + r]));
+          k0 = l == 0.f ? 0.f : x.own;
+          k1 = x.prefix;
+          m = x.top;
+          l = x.sum;
+        }
+      }
       Both w2{};
       if (SHARED && alone && before && real) w2 = both_parts(m, l * kDown, a.rows_ms[shared_row]);
       const bool add = SHARED && alone && before;
@@ -538,7 +571,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
       const float inv_prefix = add && w2.sum != 0.f ? w2.prefix / w2.sum : 0.f;
       T* out = reinterpret_cast<T*>(a.q.out) + static_cast<int64_t>(it.span.first + token) * a.q.out_token +
                static_cast<int64_t>(head) * a.q.out_head;
-      if (active) {
+      if (active && !(both && t == 1)) {
 #pragma unroll 1
         for (int e = 0; e < D / 32; ++e) {
           uint32_t y[32];
@@ -548,6 +581,15 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
           } else {
 #pragma unroll
             for (int f = 0; f < 32; ++f) y[f] = 0;
+          }
+          if (both) {
+#pragma unroll
+            for (int f = 0; f < 8; ++f) {
+              const float4 x = across[(8 * e + f) * 128 + r];
+              const float xs[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+              for (int i = 0; i < 4; ++i) y[4 * f + i] = __float_as_uint((k0 == 0.f ? 0.f : k0 * __uint_as_float(y[4 * f + i])) + k1 * xs[i]);
+            }
           }
           if (real) {
 #pragma unroll
@@ -599,106 +641,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
         }
       }
       tc_fence_before();  // O is read before the next item's products are let through (by q_full)
-      if (!alone) {
-        bar_sync<1, kTcSoftmax>();
-        const uint32_t parts = (it.last_cta - it.first_cta + 1) << both;
-        // (the count is that of the item that goes on from this CTA: one whose streams alone are joined has none)
-        if (threadIdx.x == 0) sm.last_here = it.first_cta == it.last_cta || part_done(a, it);
-        bar_sync<1, kTcSoftmax>();
-        if (sm.last_here) {
-          // both streams' parts lie one behind the other in a CTA's
-          const auto part_at = [&](uint32_t i, uint32_t row) {
-            const uint32_t cta = i >> both;
-            return (2ull * (it.first_cta + cta) + (cta == 0)) * kTcRows + (both ? i % 2 * 128 : 0) + row;
-          };
-          float top = -INFINITY, sum = 0.f;
-          if (real && !(both && t == 1)) {
-#pragma unroll 4
-            for (uint32_t i = 0; i < parts; ++i) top = fmaxf(top, __ldcg(&a.part_ms[part_at(i, lr)]).x);
-#pragma unroll 4
-            for (uint32_t i = 0; i < parts; ++i) {
-              float2* at = &a.part_ms[part_at(i, lr)];
-              const float2 z = __ldcg(at);
-              const float k = z.x == -INFINITY ? (z.y == 0.f ? 0.f : 1.f) : exp2_fast(z.x - top);
-              sum += z.y == 0.f ? 0.f : k * z.y;
-              __stcg(&at->x, k);  // the part's factor, for the threads that join it
-            }
-            if (SHARED && !a.behind) a.rows_ms[shared_row] = make_float2(top, sum * kDown);
-            else if (SHARED && before) {
-              const Both x = both_parts(top, sum * kDown, a.rows_ms[shared_row]);
-              if (a.lse) a.lse[shared_row] = (x.top + log2f(x.sum)) * 0.6931471805599453f;
-              sm.by_sum[lr] = x.sum == 0.f ? 0.f : x.own * kDown / x.sum;
-              sm.by_prefix[lr] = x.sum == 0.f ? 0.f : x.prefix / x.sum;
-            } else if (a.lse)
-              a.lse[static_cast<uint64_t>(it.span.first + token) * a.heads + head] = (top + log2f(sum * kDown)) * 0.6931471805599453f;
-          }
-          if (!SHARED || !(before && real)) sm.by_sum[lr] = SHARED && !a.behind ? kDown : sum == 0.f ? 0.f : 1.f / sum;
-          bar_sync<1, kTcSoftmax>();
-          const uint32_t rows = min(static_cast<uint32_t>(kTcRows), all - it.rb * kTcRows);
-          // eight units of four values to a thread at a time, whose loads are all on their way together (a unit's row is
-          // the same for a whole warp, or half of it)
-          constexpr uint32_t kUnits = 8;
-          const uint32_t all_units = rows * (D / 4);
-          for (uint32_t x0 = threadIdx.x; x0 < all_units; x0 += kTcSoftmax * kUnits) {
-            float4 y[kUnits];
-#pragma unroll
-            for (int u = 0; u < kUnits; ++u) y[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
-            for (uint32_t i = 0; i < parts; ++i) {
-              const float4* from = reinterpret_cast<const float4*>(a.part + part_at(i, 0) * D) + x0;
-              const float2* factor = a.part_ms + part_at(i, x0 / (D / 4));
-              float4 z[kUnits];
-              float k[kUnits];
-#pragma unroll
-              for (int u = 0; u < kUnits; ++u) {
-                const bool there = x0 + u * kTcSoftmax < all_units;
-                z[u] = there ? __ldcg(from + u * kTcSoftmax) : make_float4(0.f, 0.f, 0.f, 0.f);
-                k[u] = there ? __ldcg(&factor[u * (kTcSoftmax / (D / 4))].x) : 0.f;
-              }
-#pragma unroll
-              for (int u = 0; u < kUnits; ++u) {
-                y[u].x += k[u] * z[u].x;
-                y[u].y += k[u] * z[u].y;
-                y[u].z += k[u] * z[u].z;
-                y[u].w += k[u] * z[u].w;
-              }
-            }
-#pragma unroll
-            for (int u = 0; u < kUnits; ++u) {
-              const uint32_t x = x0 + u * kTcSoftmax, row = x / (D / 4), d = x % (D / 4) * 4;
-              if (x >= all_units) break;
-              const float by_row_sum = sm.by_sum[row];
-              const uint32_t tok = (it.rb * kTcRows + row) / a.group, hd = it.head * a.group + (it.rb * kTcRows + row) % a.group;
-              T* o = reinterpret_cast<T*>(a.q.out) + static_cast<int64_t>(it.span.first + tok) * a.q.out_token +
-                     static_cast<int64_t>(hd) * a.q.out_head + d;
-              if constexpr (SHARED) {
-                float4* there = reinterpret_cast<float4*>(a.rows + (static_cast<uint64_t>(it.span.first + tok) * a.heads + hd) * D + d);
-                if (!a.behind) {
-                  *there = make_float4(y[u].x * by_row_sum, y[u].y * by_row_sum, y[u].z * by_row_sum, y[u].w * by_row_sum);
-                  continue;
-                }
-                if (before) {
-                  const float4 z = *there;
-                  const float by_p = sm.by_prefix[row];
-                  y[u] = make_float4(y[u].x * by_row_sum + z.x * by_p, y[u].y * by_row_sum + z.y * by_p, y[u].z * by_row_sum + z.z * by_p,
-                                     y[u].w * by_row_sum + z.w * by_p);
-                }
-              }
-              const float by_total = SHARED && before ? 1.f : by_row_sum;
-              if (a.out_wide) {
-                *reinterpret_cast<uint2*>(o) =
-                    make_uint2(P::pack(y[u].x * by_total, y[u].y * by_total), P::pack(y[u].z * by_total, y[u].w * by_total));
-              } else {
-                o[0] = Elem<T>::from(y[u].x * by_total);
-                o[1] = Elem<T>::from(y[u].y * by_total);
-                o[2] = Elem<T>::from(y[u].z * by_total);
-                o[3] = Elem<T>::from(y[u].w * by_total);
-              }
-            }
-          }
-          bar_sync<1, kTcSoftmax>();
-        }
-      }
+      if (both) bar_sync<1, kTcSoftmax>();  // Q's place is read
     }
   } else if (BITS < 16 && warp < kIssuer) {
     // ---------------------------------------------------------------- unpackers of keys (v = 0) and of values (v = 1)
@@ -789,20 +732,14 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
         const uint32_t halves = it.span.count * a.group - it.rb * kTcRows > 128 ? 2 : 1;
         const uint32_t tiles = !both && t >= halves ? 0 : tiles_of(both, t, told), step = both ? 2 : 1, from = both ? t : 0;
         // What the other stream alone takes is let through in its turn: a barrier's phases are told apart by their parity.
-        uint32_t passed[2] = {0, 0};
-        const auto pass = [&](uint32_t v, uint32_t upto) {  // tiles before `upto` of the item
-          for (; passed[v] < upto; ++passed[v]) {
-            if (tiles && passed[v] >= from && (passed[v] - from) % step == 0) continue;  // this stream's own
-            const uint32_t st = (n + passed[v]) % kStages;
-            ok = ok && tc_wait(&sm.full[v][st], (n + passed[v]) / kStages, stop);
-            ok = __all_sync(0xffffffffu, ok);
-            if (!ok) return;
-            warp_arrive(&sm.empty[v][st]);
-          }
+        const auto let_through = [&](uint32_t v, uint32_t at) {
+          ok = ok && tc_wait(&sm.full[v][at % kStages], at / kStages, stop);
+          ok = __all_sync(0xffffffffu, ok);
+          if (ok) warp_arrive(&sm.empty[v][at % kStages]);
         };
         const auto qk = [&](uint32_t j) {
           const uint32_t at = n + from + j * step, st = at % kStages, i = s_n + j;
-          pass(0, from + j * step);
+          if (both && from + j > 0) let_through(0, at - 1);
           if (j == 0) ok = ok && tc_wait(&sm.q_full[t], q_n++, stop);
           // this S holds the P of two tiles before
           if (j > 1) ok = ok && tc_wait(&sm.o_full[t][i % 2], i / 2 - 1, stop);
@@ -821,7 +758,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
 #pragma unroll 1
         for (uint32_t j = 0; ok && j < tiles; ++j) {
           const uint32_t at = n + from + j * step, st = at % kStages, i = s_n + j;
-          pass(1, from + j * step);
+          if (both && from + j > 0) let_through(1, at - 1);
           ok = ok && tc_wait(&sm.p_full[t][i % 2], i / 2, stop) && tc_wait(&sm.full[1][st], at / kStages, stop);
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;
@@ -833,8 +770,15 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
           tc_commit(leader, &sm.empty[1][st]);
           if (j + 2 < tiles) qk(j + 2);
         }
-        if (ok) pass(0, told);
-        if (ok) pass(1, told);
+        if (both && (told - 1) % 2 != t) {  // the last one is the other's
+          let_through(0, n + told - 1);
+          let_through(1, n + told - 1);
+        }
+        if (!both && t >= halves)
+          for (uint32_t j = 0; ok && j < told; ++j) {
+            let_through(0, n + j);
+            let_through(1, n + j);
+          }
         s_n += tiles;
         n += told;
       }
@@ -986,6 +930,82 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
   }
+}
+
+// Joins the parts of the items that lie in more than one CTA's range: a CTA to
+// some rows of the item that goes on from CTA blockIdx.x, D / 4 lanes to a row.
+// In a launch of its own, because the ranges end at the same time: the CTA that
+// ended last, joining 19 parts of 128 rows alone, took 80 us.
+constexpr int kJoinThreads = 512;
+template <int D>
+constexpr uint32_t kJoinRows = kJoinThreads / (D / 4);
+template <typename T, int D, bool SHARED>
+__global__ void __launch_bounds__(kJoinThreads) attend_join(const __grid_constant__ AttendArgs a) {
+  using P = Pair<T>;
+  constexpr float kDown = std::is_same<T, __half>::value ? 0x1p-7f : 1.f;  // as above
+  constexpr uint32_t kLanes = D / 4;
+  pdl_trigger();
+  pdl_wait();
+  const SplitItem it = a.items[blockIdx.x];
+  if (it.last_cta <= blockIdx.x) return;
+  const uint32_t all = min(kManyRows, it.span.count * a.group - it.rb * kManyRows);
+  const uint32_t lane = threadIdx.x % kLanes, row = blockIdx.y * kJoinRows<D> + threadIdx.x / kLanes;
+  if (blockIdx.y * kJoinRows<D> >= all) return;
+  const bool real = row < all;  // (whole warps go on, for the shuffles)
+  const uint32_t parts = it.last_cta - blockIdx.x + 1;
+  const auto part_at = [&](uint32_t i) { return (2ull * (blockIdx.x + i) + (i == 0)) * kManyRows + (real ? row : 0); };
+  float top = -INFINITY, sum = 0.f;
+  for (uint32_t i = lane; i < parts; i += kLanes) top = fmaxf(top, a.part_ms[part_at(i)].x);
+#pragma unroll
+  for (uint32_t o = 1; o < kLanes; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (uint32_t p0 = 0; p0 < parts; p0 += kLanes) {
+    float k = 0.f;
+    if (p0 + lane < parts) {
+      const float2 z = a.part_ms[part_at(p0 + lane)];
+      k = z.x == -INFINITY ? (z.y == 0.f ? 0.f : 1.f) : exp2_fast(z.x - top);
+      sum += z.y == 0.f ? 0.f : k * z.y;
+    }
+    const uint32_t n = min(kLanes, parts - p0);
+#pragma unroll 8
+    for (uint32_t i = 0; i < n; ++i) {
+      const float by = __shfl_sync(0xffffffffu, k, i, kLanes);
+      const float4 z = *reinterpret_cast<const float4*>(a.part + part_at(p0 + i) * D + lane * 4);
+      y.x += by * z.x, y.y += by * z.y, y.z += by * z.z, y.w += by * z.w;
+    }
+  }
+#pragma unroll
+  for (uint32_t o = 1; o < kLanes; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if (!real) return;
+  const uint32_t token = it.span.first + (it.rb * kManyRows + row) / a.group, head = it.head * a.group + (it.rb * kManyRows + row) % a.group;
+  const uint64_t at = static_cast<uint64_t>(token) * a.heads + head;
+  float by = sum == 0.f ? 0.f : 1.f / sum, lse = top + log2f(sum * kDown);
+  if constexpr (SHARED) {
+    float4* const there = reinterpret_cast<float4*>(a.rows + at * D) + lane;
+    if (!a.behind) {
+      *there = make_float4(y.x * kDown, y.y * kDown, y.z * kDown, y.w * kDown);
+      if (lane == 0) a.rows_ms[at] = make_float2(top, sum * kDown);
+      return;
+    }
+    if (has_prefix(a, it.seq)) {
+      const Both w = both_parts(top, sum * kDown, a.rows_ms[at]);
+      const float4 z = *there;
+      const float own = w.own * kDown;
+      y = make_float4(own * y.x + w.prefix * z.x, own * y.y + w.prefix * z.y, own * y.z + w.prefix * z.z, own * y.w + w.prefix * z.w);
+      by = w.sum == 0.f ? 0.f : 1.f / w.sum;
+      lse = w.top + log2f(w.sum);
+    }
+  }
+  T* const out = reinterpret_cast<T*>(a.q.out) + static_cast<int64_t>(token) * a.q.out_token + static_cast<int64_t>(head) * a.q.out_head + lane * 4;
+  if (a.out_wide) {
+    *reinterpret_cast<uint2*>(out) = make_uint2(P::pack(y.x * by, y.y * by), P::pack(y.z * by, y.w * by));
+  } else {
+    out[0] = Elem<T>::from(y.x * by);
+    out[1] = Elem<T>::from(y.y * by);
+    out[2] = Elem<T>::from(y.z * by);
+    out[3] = Elem<T>::from(y.w * by);
+  }
+  if (a.lse && lane == 0) a.lse[at] = lse * 0.6931471805599453f;
 }
 
 // One CTA to an SM, whose tensor memory it takes whole: more than half of its shared memory.

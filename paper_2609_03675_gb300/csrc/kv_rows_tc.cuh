@@ -13,10 +13,10 @@
 //              bytes as they lie in the pages
 //   unpackers  (less than 16 bits) four warps for keys, four for values: to
 //              (n - z) s or (u - 128) s, which the 16-bit types hold exactly
-//   clearer    (16 bits) a warp that puts zeros where a value is not to be seen
-//              (a NaN there would pass through a product with 0)
-//   MMA        a warp for each stream: S = Q K^T into tensor memory (128 x 64 fp32),
-//              and O += P V with P read from tensor memory
+//   MMA        a warp for S = Q K^T into tensor memory (128 x 64 fp32 a stream), and
+//              one for O += P V with P read from tensor memory; for 16 bits it puts
+//              zeros where a value is not to be seen before (a NaN there would
+//              pass through a product with 0)
 //   softmax    four warps a stream, a thread to a row: maximum, exponentials, P
 //              back into S's place in 16 bits; at the end O out
 // (With copies made by the threads that unpack, 16 bytes each, a tile of bytes
@@ -46,9 +46,9 @@ namespace {
 constexpr int kTcRows = kManyRows;
 constexpr int kTcSoftmax = 256;  // threads: warps 0 to 7
 constexpr int kTcUnpack = 128;   // of keys, and as many of values
-// And two warps that issue, two loaders, and for 16 bits the clearer.
+// And two warps that issue, and two loaders.
 template <int BITS>
-constexpr int kTcThreads = kTcSoftmax + (BITS < 16 ? 2 * kTcUnpack + 128 : 160);
+constexpr int kTcThreads = kTcSoftmax + (BITS < 16 ? 2 * kTcUnpack : 0) + 128;
 constexpr int kTcInfo = 16;         // more than the stages and the raw tiles: a tile is told before its place is free
 constexpr uint32_t kTcStreamed = 4; // tiles from which an item of 128 rows or less is taken by both streams
 // Tiles whose products are summed in tensor memory before the sums move on to the CTA's part. The tensor core cuts each
@@ -61,11 +61,16 @@ constexpr uint64_t kTcTimeout = 1000000000ull;
 // Registers where there are unpackers: all threads start with 96; 256 x 136 + 256 x 64 + 128 x 80 is 640 x 96.
 constexpr int kTcRegsSoftmax = 136, kTcRegsUnpack = 64, kTcRegsIssuer = 80;
 
+// What the loader of keys says of a tile; all but the softmax and the loaders go by it alone.
 struct TcInfo {
   uint32_t bits[2];  // tokens that some row may see
   int32_t pos;       // the first token
   uint32_t plain;    // every token is seen by every row
+  uint32_t j;        // tiles of its item before it
+  uint32_t flags;    // kTc*
 };
+
+enum : uint32_t { kTcBoth = 1, kTcSecond = 2, kTcEnd = 4 };  // streamed by both; the second stream has rows; no more tiles
 
 template <int D, int BITS, bool SHARED>
 struct TcSmem {
@@ -81,12 +86,12 @@ struct TcSmem {
   char kv[2][kStages][kBlock * (D / 64)];  // keys, values
   char raw[2][kRaw][BITS < 16 ? kTile * kRow : 16];
   char raw_words[2][kRaw][BITS < 16 ? kTile * kRowWords : 16];
+  uint32_t raw_bits[2][kRaw][4];  // of a raw tile's tokens, those to be seen; then whether there are no more tiles
   Span spans[kSpans];
   TcInfo info[kTcInfo];
   float by_sum[kTcRows];
   uint64_t full[2][kStages], empty[2][kStages];  // keys, values
   uint64_t raw_full[2][kRaw], raw_empty[2][kRaw];
-  uint64_t landed[kStages];  // 16 bits: values before the clearer has seen them
   // A barrier's phase can be told from the one before only. O is ready twice before anyone has to look, so it has a
   // barrier for even tiles and one for odd ones, as S and P have.
   uint64_t info_full[kTcInfo], q_full[2], s_full[2][2], p_full[2][2], o_full[2][2], drained;
@@ -111,6 +116,15 @@ __device__ __forceinline__ bool tc_wait(const uint64_t* bar, uint32_t parity, ui
   const uint32_t b = shared_address(bar);
   return mbar_try_wait(b, parity & 1) || tc_wait_slow(b, parity & 1, stop);
 }
+// A place in a ring of N, and the parity of its barriers' phase. Kept up instead of divided out of a count of tiles: a
+// warp that issues or looks up has a few hundred cycles a tile, in which it gets to issue every eighth or so.
+template <uint32_t N>
+struct Turn {
+  uint32_t i = 0, parity = 0;
+  __device__ __forceinline__ void next() {
+    if (++i == N) i = 0, parity ^= 1;
+  }
+};
 
 __device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -275,14 +289,13 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
   S& sm = *reinterpret_cast<S*>(raw + (1024u - (shared_address(raw) & 1023u)) % 1024u);
   pdl_trigger();
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-  constexpr uint32_t kIssuer = (kTcSoftmax + (BITS < 16 ? 2 * kTcUnpack : 0)) / 32;  // and the warp after it; then the loaders
+  constexpr uint32_t kIssuer = (kTcSoftmax + (BITS < 16 ? 2 * kTcUnpack : 0)) / 32, kLoader = kIssuer + 2;  // their first warps
   if (threadIdx.x == 0) {
     for (uint32_t i = 0; i < kStages; ++i) {
       for (int v = 0; v < 2; ++v) {
         mbar_init(shared_address(&sm.full[v][i]), BITS < 16 ? kTcUnpack / 32 : 1);
-        mbar_init(shared_address(&sm.empty[v][i]), 2);  // both issuers
+        mbar_init(shared_address(&sm.empty[v][i]), 1);
       }
-      mbar_init(shared_address(&sm.landed[i]), 1);
     }
     for (uint32_t i = 0; i < kRaw; ++i)
       for (int v = 0; v < 2; ++v) {
@@ -652,20 +665,23 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
       // (128-byte swizzle) meet a bank twice: eight lanes read 128 bytes in a row, or the halves of two rows that lie so,
       // and write to eight different units of a row.
       constexpr int kRowUnits = S::kRow / 16, kTurns = kRowUnits / 2;
-      uint32_t n = 0;  // tiles so far
-      while (walk.next(it)) {  // to the end, as above
-        const uint32_t tiles = it.hi - it.lo;
+      Turn<kStages> to_stage;
+      Turn<kRaw> from_raw;
+      bool first = true;  // the stages have not been used yet
+      {
 #pragma unroll 1
-        for (uint32_t j = 0; j < tiles; ++j, ++n) {
-          const uint32_t st = n % kStages, slot = n % kRaw;
-          ok = ok && tc_wait(&sm.info_full[n % kTcInfo], n / kTcInfo, stop) && tc_wait(&sm.raw_full[v][slot], n / kRaw, stop);
-          if (n >= kStages) ok = ok && tc_wait(&sm.empty[v][st], n / kStages - 1, stop);
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) break;
-          const uint32_t bits = sm.info[n % kTcInfo].bits[w / 2] >> (16 * (w % 2));
+        for (;;) {
+          const uint32_t st = to_stage.i, slot = from_raw.i;
+          if (!first) ok = tc_wait(&sm.empty[v][st], to_stage.parity ^ 1, stop);
+          ok = __all_sync(0xffffffffu, ok && tc_wait(&sm.raw_full[v][slot], from_raw.parity, stop));
+          if (!ok || sm.raw_bits[v][slot][2]) break;
+          const uint32_t bits = sm.raw_bits[v][slot][w / 2] >> (16 * (w % 2));
           const char* const raw_rows = sm.raw[v][slot] + w * 16 * S::kRow;
           const uint16_t* const words = reinterpret_cast<const uint16_t*>(sm.raw_words[v][slot]) + w * 16 * (D / 64);
           char* const rows = sm.kv[v][st] + w * 16 * 128;
+          from_raw.next();
+          to_stage.next();
+          first = first && to_stage.i != 0;
           const auto place = [&](int e, uint32_t& tok, uint32_t& unit) {
             if (kRowUnits == 8) {
               tok = 8 * (e / 2) + lane / 4;
@@ -721,82 +737,92 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
     }
   } else {
     if constexpr (BITS < 16) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kTcRegsIssuer));
-    if (warp < kIssuer + 2) {
-      // -------------------------------------------------------------- products: a warp for each tile
-      constexpr uint32_t kQK = tc_idesc<T>(128, kTile, false), kPV = tc_idesc<T>(128, D, true);
-      const uint32_t leader = tc_leader(), t = warp - kIssuer;
-      uint32_t n = 0, q_n = 0, s_n = 0;  // tiles so far; items and tiles of this stream
-      while (ok && walk.next(it)) {
-        const uint32_t told = it.hi - it.lo;
-        const bool both = streamed(it);
-        const uint32_t halves = it.span.count * a.group - it.rb * kTcRows > 128 ? 2 : 1;
-        const uint32_t tiles = !both && t >= halves ? 0 : tiles_of(both, t, told), step = both ? 2 : 1, from = both ? t : 0;
-        // What the other stream alone takes is let through in its turn: a barrier's phases are told apart by their parity.
-        const auto let_through = [&](uint32_t v, uint32_t at) {
-          ok = ok && tc_wait(&sm.full[v][at % kStages], at / kStages, stop);
-          ok = __all_sync(0xffffffffu, ok);
-          if (ok) warp_arrive(&sm.empty[v][at % kStages]);
-        };
-        const auto qk = [&](uint32_t j) {
-          const uint32_t at = n + from + j * step, st = at % kStages, i = s_n + j;
-          if (both && from + j > 0) let_through(0, at - 1);
-          if (j == 0) ok = ok && tc_wait(&sm.q_full[t], q_n++, stop);
-          // this S holds the P of two tiles before
-          if (j > 1) ok = ok && tc_wait(&sm.o_full[t][i % 2], i / 2 - 1, stop);
-          ok = ok && tc_wait(&sm.full[0][st], at / kStages, stop);
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) return;
-          tc_fence_after();
-          const uint32_t q = tc_desc(shared_address(sm.q[t]), 16), k = tc_desc(shared_address(sm.kv[0][st]), 16), d = s_at(t, i);
+    if (warp < kLoader) {
+    // ---------------------------------------------------------------- products: S (v = 0), or O (v = 1)
+    constexpr uint32_t kQK = tc_idesc<T>(128, kTile, false), kPV = tc_idesc<T>(128, D, true);
+    constexpr uint32_t kStep = S::kBlock * (D / 64) / 16;  // from one stage's descriptor to the next's
+    const uint32_t leader = tc_leader(), v = warp - kIssuer;
+    const uint32_t kv = tc_desc(shared_address(sm.kv[v][0]), v ? S::kBlock : 16);
+    uint32_t q_parity = 0;  // a bit for each stream
+    Turn<kTcInfo> told;
+    Turn<kStages> at;  // keys or values to come
+    Turn<2> s[2];      // S to be written, or P to be read
+#pragma unroll 1
+    for (;;) {
+      ok = __all_sync(0xffffffffu, tc_wait(&sm.info_full[told.i], told.parity, stop));
+      if (!ok) break;
+      const TcInfo& info = sm.info[told.i];
+      const uint32_t flags = info.flags, j = info.j;
+      if (flags & kTcEnd) break;
+      told.next();
+      const bool both = flags & kTcBoth;
+      const uint32_t i = both ? j / 2 : j;  // of the stream's tiles of the item
+      ok = __all_sync(0xffffffffu, tc_wait(&sm.full[v][at.i], at.parity, stop));
+      if (!ok) break;
+      if (BITS == 16 && v == 1) {
+        const uint32_t bits0 = info.bits[0], bits1 = info.bits[1];
+        if ((bits0 & bits1) != ~0u) {
+#pragma unroll 1
+          for (uint32_t e = lane; e < kTile * (D / 8); e += 32) {
+            const uint32_t tok = e / 8 % kTile;
+            if (!((tok < 32 ? bits0 : bits1) >> (tok % 32) & 1u))
+              *reinterpret_cast<uint4*>(sm.kv[1][at.i] + e / 8 / kTile * S::kBlock + tok * 128 + e % 8 * 16) = make_uint4(0, 0, 0, 0);
+          }
+          fence_async_shared();
+          __syncwarp();
+        }
+      }
+      const uint32_t x = kv + at.i * kStep;
+#pragma unroll
+      for (uint32_t t = 0; t < 2; ++t) {
+        if (both ? j % 2 != t : t == 1 && !(flags & kTcSecond)) continue;
+        if (v == 1) {
+          ok = tc_wait(&sm.p_full[t][s[t].i], s[t].parity, stop);
+        } else if (i == 0) {
+          ok = tc_wait(&sm.q_full[t], q_parity >> t, stop);
+          q_parity ^= 1u << t;
+        } else if (i > 1) {  // this S holds the P of two tiles before
+          ok = tc_wait(&sm.o_full[t][s[t].i], s[t].parity ^ 1, stop);
+        }
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t y = s_at(t, s[t].i);
+        if (v == 0) {
+          const uint32_t q = tc_desc(shared_address(sm.q[t]), 16);
 #pragma unroll
           for (int e = 0; e < D / 16; ++e)
-            tc_mma_ss(leader, d, q + (e / 4) * (S::kBlockQ / 16) + (e % 4) * 2, k + (e / 4) * (S::kBlock / 16) + (e % 4) * 2, kQK, e > 0);
-          tc_commit(leader, &sm.s_full[t][i % 2]);
-          tc_commit(leader, &sm.empty[0][st]);
-        };
-        for (uint32_t j = 0; ok && j < 2 && j < tiles; ++j) qk(j);
-#pragma unroll 1
-        for (uint32_t j = 0; ok && j < tiles; ++j) {
-          const uint32_t at = n + from + j * step, st = at % kStages, i = s_n + j;
-          if (both && from + j > 0) let_through(1, at - 1);
-          ok = ok && tc_wait(&sm.p_full[t][i % 2], i / 2, stop) && tc_wait(&sm.full[1][st], at / kStages, stop);
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) break;
-          tc_fence_after();
-          const uint32_t v = tc_desc(shared_address(sm.kv[1][st]), S::kBlock), p = s_at(t, i);
+            tc_mma_ss(leader, y, q + (e / 4) * (S::kBlockQ / 16) + (e % 4) * 2, x + (e / 4) * (S::kBlock / 16) + (e % 4) * 2, kQK, e > 0);
+          tc_commit(leader, &sm.s_full[t][s[t].i]);
+        } else {
 #pragma unroll
-          for (int e = 0; e < static_cast<int>(kTile) / 16; ++e) tc_mma_ts(leader, o_at(t), p + e * 8, v + e * (2048 / 16), kPV, j % kTcChain<T> != 0 || e > 0);
-          tc_commit(leader, &sm.o_full[t][i % 2]);
-          tc_commit(leader, &sm.empty[1][st]);
-          if (j + 2 < tiles) qk(j + 2);
+          for (int e = 0; e < static_cast<int>(kTile) / 16; ++e)
+            tc_mma_ts(leader, o_at(t), y + e * 8, x + e * (2048 / 16), kPV, i % kTcChain<T> != 0 || e > 0);
+          tc_commit(leader, &sm.o_full[t][s[t].i]);
         }
-        if (both && (told - 1) % 2 != t) {  // the last one is the other's
-          let_through(0, n + told - 1);
-          let_through(1, n + told - 1);
-        }
-        if (!both && t >= halves)
-          for (uint32_t j = 0; ok && j < told; ++j) {
-            let_through(0, n + j);
-            let_through(1, n + j);
-          }
-        s_n += tiles;
-        n += told;
+        s[t].next();
       }
-      // what was issued, and its arrivals, finish before the tensor memory goes and the CTA ends: waited for even when
-      // another wait has run out
-      tc_commit(leader, &sm.drained);
-      if (!tc_wait(&sm.drained, 0, nullptr)) atomicOr(b.err, kKvErrWait);
-      __syncwarp();
-    } else if (warp < kIssuer + 4) {
+      if (!ok) break;
+      tc_commit(leader, &sm.empty[v][at.i]);
+      at.next();
+    }
+    // what was issued, and its arrivals, finish before the tensor memory goes and the CTA ends: waited for even when
+    // another wait has run out
+    tc_commit(leader, &sm.drained);
+    if (!tc_wait(&sm.drained, 0, nullptr)) atomicOr(b.err, kKvErrWait);
+    __syncwarp();
+    } else if (warp < kLoader + 2) {
       // -------------------------------------------------------------- loaders of keys (v = 0) and of values (v = 1)
-      const uint32_t v = warp - kIssuer - 2, leader = tc_leader();
+      const uint32_t v = warp - kLoader, leader = tc_leader();
       const uint32_t shift = b.page_shift, per = min(1u << shift, kTile);  // tokens of one copy
       const uint32_t block = lane % 4;                                     // of 16 tokens, whose page the lane looks up
       const uint32_t base = shared_address(BITS < 16 ? sm.raw[v][0] : sm.kv[v][0]), base_words = shared_address(sm.raw_words[v][0]);
-      uint64_t* const bars = BITS < 16 ? sm.raw_full[v] : v ? sm.landed : sm.full[0];
+      uint64_t* const bars = BITS < 16 ? sm.raw_full[v] : sm.full[v];
       uint64_t* const frees = BITS < 16 ? sm.raw_empty[v] : sm.empty[v];
       constexpr uint32_t kSlots = BITS < 16 ? kRaw : kStages;
       uint32_t n = 0;  // tiles so far
+      Turn<kSlots> to_slot;
+      Turn<kTcInfo> tell;
       while (ok && walk.next(it)) {
         const uint32_t tiles = it.hi - it.lo;
         const int32_t* table = b.table + static_cast<uint64_t>(it.seq) * b.table_stride;
@@ -809,6 +835,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
         }
         // A tile takes two loads one after the other where there is a mask (its number, then pages and mask): numbers are
         // asked for three tiles ahead and the others two, so that nobody waits for them.
+        const uint32_t flags = (streamed(it) ? kTcBoth : 0) | (it.span.count * a.group - it.rb * kTcRows > 128 ? kTcSecond : 0);
         struct Look {
           uint32_t pos, page;   // the tile's first token; the page of the lane's block of 16, n_pages or above where there is none
           uint32_t see0, see1;  // of tokens pos + lane and pos + 32 + lane
@@ -855,26 +882,35 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
               }
             }
           }
-          const uint32_t slot = n % kSlots;
-          if (n >= kSlots) ok = ok && tc_wait(&frees[slot], n / kSlots - 1, stop);
-          ok = __all_sync(0xffffffffu, ok);
+          const uint32_t slot = to_slot.i;
+          if (n >= kSlots) ok = __all_sync(0xffffffffu, tc_wait(&frees[slot], to_slot.parity ^ 1, stop));
           if (!ok) break;
+          to_slot.next();
           if (v == 0 && lane == 0) {
-            TcInfo& info = sm.info[n % kTcInfo];
+            TcInfo& info = sm.info[tell.i];
             info.bits[0] = bits0;
             info.bits[1] = bits1;
             info.pos = static_cast<int32_t>(x.pos);
             info.plain = (bits0 & bits1) == ~0u && static_cast<int32_t>(x.pos + kTile) <= all_see;
-            mbar_arrive(shared_address(&sm.info_full[n % kTcInfo]));
+            info.j = j;
+            info.flags = flags;
+            mbar_arrive(shared_address(&sm.info_full[tell.i]));
           }
+          tell.next();
           // a copy is made where any of its blocks is seen (its page, which all of them have, is there then)
-          const auto wanted = [&](uint32_t e) {
-            const uint64_t bits = static_cast<uint64_t>(bits1) << 32 | bits0;
-            return (bits >> e & (per == kTile ? ~0ull : (1ull << per) - 1)) != 0;
-          };
-          uint32_t copies = 0;
-          for (uint32_t e = 0; e < kTile; e += per) copies += wanted(e);
+          const uint64_t mine = per == kTile ? ~0ull : (1ull << per) - 1;
+          const auto wanted = [&](uint32_t e) { return ((static_cast<uint64_t>(bits1) << 32 | bits0) >> e & mine) != 0; };
+          uint32_t copies = (bits0 | bits1) != 0;
+          if (per != kTile) {
+            copies = 0;
+            for (uint32_t e = 0; e < kTile; e += per) copies += wanted(e);
+          }
           const uint32_t bar = shared_address(&bars[slot]);
+          if (BITS < 16 && leader) {
+            sm.raw_bits[v][slot][0] = bits0;
+            sm.raw_bits[v][slot][1] = bits1;
+            sm.raw_bits[v][slot][2] = 0;
+          }
           arrive_expecting(leader, bar, copies * per * (S::kRow + (BITS < 16 ? S::kRowWords : 0)));
           const uint32_t place = x.pos & ((1u << shift) - 1);
 #pragma unroll 1
@@ -895,32 +931,19 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
           }
         }
       }
-      if (!ok)  // copies in flight land before the CTA ends
-        for (uint32_t i = n > kSlots ? n - kSlots : 0; i < n; ++i) tc_wait(&bars[i % kSlots], i / kSlots, nullptr);
-    } else if (BITS == 16) {
-      // -------------------------------------------------------------- clearer
-      uint32_t n = 0;
-      while (walk.next(it)) {
-        const uint32_t tiles = it.hi - it.lo;
-#pragma unroll 1
-        for (uint32_t j = 0; j < tiles; ++j, ++n) {
-          const uint32_t st = n % kStages;
-          ok = ok && tc_wait(&sm.info_full[n % kTcInfo], n / kTcInfo, stop) && tc_wait(&sm.landed[st], n / kStages, stop);
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) break;
-          const uint32_t bits0 = sm.info[n % kTcInfo].bits[0], bits1 = sm.info[n % kTcInfo].bits[1];
-          if ((bits0 & bits1) != ~0u) {
-#pragma unroll 1
-            for (uint32_t e = lane; e < kTile * (D / 8); e += 32) {
-              const uint32_t tok = e / 8 % kTile;
-              if (!((tok < 32 ? bits0 : bits1) >> (tok % 32) & 1u))
-                *reinterpret_cast<uint4*>(sm.kv[1][st] + e / 8 / kTile * S::kBlock + tok * 128 + e % 8 * 16) = make_uint4(0, 0, 0, 0);
-            }
-          }
-          fence_async_shared();
-          warp_arrive(&sm.full[1][st]);
+      if (ok && v == 0 && lane == 0) {
+        sm.info[tell.i].flags = kTcEnd;
+        mbar_arrive(shared_address(&sm.info_full[tell.i]));
+      }
+      if (BITS < 16 && ok) {
+        if (n >= kSlots) ok = __all_sync(0xffffffffu, tc_wait(&frees[to_slot.i], to_slot.parity ^ 1, stop));
+        if (ok && leader) {
+          sm.raw_bits[v][to_slot.i][2] = 1;
+          mbar_arrive(shared_address(&bars[to_slot.i]));
         }
       }
+      if (!ok)  // copies in flight land before the CTA ends
+        for (uint32_t i = n > kSlots ? n - kSlots : 0; i < n; ++i) tc_wait(&bars[i % kSlots], i / kSlots, nullptr);
     }
   }
   if (!ok) atomicOr(b.err, kKvErrWait);

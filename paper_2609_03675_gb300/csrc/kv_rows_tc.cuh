@@ -21,10 +21,10 @@
 //              back into S's place in 16 bits; at the end O out
 // (With copies made by the threads that unpack, 16 bytes each, a tile of bytes
 // took 3300 cycles and one of 16-bit values 3400, however few the rows.)
-// The running maximum that exponentials refer to is raised only when the true
-// one passes it by 2^8 (2^4 for fp16; then O is brought down in tensor memory),
-// which seldom happens after the first tokens. O itself is read out and begun
-// anew after some thousands of tokens (kTcChain).
+// The running maximum that exponentials refer to is found at a row's first tokens
+// and raised only when a tile's weights sum to more than their type has room for
+// (then O is brought down in tensor memory), which seldom happens after them. O
+// itself is read out and begun anew after some thousands of tokens (kTcChain).
 //
 // Tensor memory: O0 O1 (D columns each) and for each tile two S of 64 columns,
 // P in the first 32 of its S: while the softmax works on one S, the products
@@ -281,10 +281,10 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
   constexpr uint32_t kStages = S::kStages, kRaw = S::kRaw;
   constexpr int kThreads = kTcThreads<BITS>;
   // fp16: weights are 2^7 times what they stand for, so that only those under 2^-32 of the largest are lost to the second
-  // product, and the maximum that they refer to is never more than 2^4 behind: up to 2^11, the exponents above left for a
-  // maximum that is a rounding of a large score off. (bf16 has the exponents of fp32.)
+  // product. A tile's 64 sum to 2^13 where all are as large as the maximum that they refer to; up to 2^15, which fp16 holds,
+  // it may be behind. (bf16 has the exponents of fp32: up to 2^8 leaves sums of values of 2^119 in range.)
   constexpr bool kHalf = std::is_same<T, __half>::value;
-  constexpr float kRaise = kHalf ? 4.f : 8.f, kUp = kHalf ? 7.f : 0.f, kDown = kHalf ? 0x1p-7f : 1.f;
+  constexpr float kMost = kHalf ? 0x1p15f : 0x1p8f, kUp = kHalf ? 7.f : 0.f, kDown = kHalf ? 0x1p-7f : 1.f;
   extern __shared__ char raw[];
   S& sm = *reinterpret_cast<S*>(raw + (1024u - (shared_address(raw) & 1023u)) % 1024u);
   pdl_trigger();
@@ -441,73 +441,88 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
             kept_m = m;
           }
           const uint32_t s_col = s_at(t, s_n) + lanes;
-          uint32_t x[32], y[32];
-          tc_ld32(s_col, x);
-          tc_ld32(s_col + 32, y);
-          tc_wait_ld(x);
-          tc_wait_ld(y);
+          uint32_t see0 = ~0u, see1 = ~0u;  // the tokens that this row sees
           if (!info.plain || (SHARED && by_row)) {
-            // hides those of 32 tokens that this row does not see
             const int32_t k = seen - info.pos;  // the row sees the first k
-            const uint32_t see0 = info.bits[0] & static_cast<uint32_t>(word) & (k >= 32 ? ~0u : k <= 0 ? 0u : (1u << k) - 1);
-            const uint32_t see1 = info.bits[1] & static_cast<uint32_t>(word >> 32) & (k >= 64 ? ~0u : k <= 32 ? 0u : (1u << (k - 32)) - 1);
-            if (!__all_sync(0xffffffffu, (see0 & see1) == ~0u)) {
-#pragma unroll
-              for (int f = 0; f < 32; ++f) {
-                if (!(see0 & (1u << f))) x[f] = 0xff800000u;
-                if (!(see1 & (1u << f))) y[f] = 0xff800000u;
-              }
-            }
+            see0 = info.bits[0] & static_cast<uint32_t>(word) & (k >= 32 ? ~0u : k <= 0 ? 0u : (1u << k) - 1);
+            see1 = info.bits[1] & static_cast<uint32_t>(word >> 32) & (k >= 64 ? ~0u : k <= 32 ? 0u : (1u << (k - 32)) - 1);
           }
-          const float top = most_of(x, y, -INFINITY) * by;
-          const bool raise = top > m + kRaise || (m == -INFINITY && top > -INFINITY);
-          if (__any_sync(0xffffffffu, raise)) {
-            const float to = raise ? top : m, k = m == -INFINITY ? 0.f : exp2_fast(m - to);
-            if (j % kTcChain<T> != 0) {  // O as it is after the tokens before
-              ok = tc_wait(&sm.o_full[t][(s_n - 1) % 2], (s_n - 1) / 2, stop);
-              ok = __all_sync(0xffffffffu, ok);
-              tc_fence_after();
-              uint32_t z[16];
+          const bool partly = !__all_sync(0xffffffffu, (see0 & see1) == ~0u);
+          uint32_t w[32];
+          float here = 0.f;
+          if (partly && !__any_sync(0xffffffffu, (see0 | see1) != 0)) {  // a frame that is not these rows' evidence
+#pragma unroll
+            for (int f = 0; f < 32; ++f) w[f] = 0;
+          } else {
+            // The maximum is looked for at a row's first tokens, and when the sum of a tile's weights shows that the one that
+            // they refer to is far behind: then once more from S, which is there until P takes its place.
+            for (bool again = false;;) {
+              uint32_t x[32], y[32];
+              tc_ld32(s_col, x);
+              tc_ld32(s_col + 32, y);
+              tc_wait_ld(x);
+              tc_wait_ld(y);
+              if (partly) {
+#pragma unroll
+                for (int f = 0; f < 32; ++f) {
+                  if (!(see0 & (1u << f))) x[f] = 0xff800000u;
+                  if (!(see1 & (1u << f))) y[f] = 0xff800000u;
+                }
+              }
+              if (again || __any_sync(0xffffffffu, m == -INFINITY && (see0 | see1) != 0)) {
+                const float top = most_of(x, y, -INFINITY) * by;
+                const bool raise = !(here <= kMost) || (m == -INFINITY && top > -INFINITY);
+                const float to = raise ? fmaxf(top, m) : m, k = m == -INFINITY ? 0.f : exp2_fast(m - to);
+                if (j % kTcChain<T> != 0) {  // O as it is after the tokens before
+                  ok = tc_wait(&sm.o_full[t][(s_n - 1) % 2], (s_n - 1) / 2, stop);
+                  ok = __all_sync(0xffffffffu, ok);
+                  tc_fence_after();
+                  uint32_t z[16];
 #pragma unroll 1
-              for (int e = 0; e < D / 16; ++e) {
-                tc_ld16(o_col + 16 * e, z);
+                  for (int e = 0; e < D / 16; ++e) {
+                    tc_ld16(o_col + 16 * e, z);
 #pragma unroll
-                for (int f = 0; f < 16; ++f) z[f] = __float_as_uint(__uint_as_float(z[f]) * k);
-                tc_st16(o_col + 16 * e, z);
+                    for (int f = 0; f < 16; ++f) z[f] = __float_as_uint(__uint_as_float(z[f]) * k);
+                    tc_st16(o_col + 16 * e, z);
+                  }
+                  tc_wait_st();
+                }
+                l *= k;
+                l_rest *= k;
+                m = to;
               }
-              tc_wait_st();
-            }
-            l *= k;
-            l_rest *= k;
-            m = to;
-          }
-          const float down = m == -INFINITY ? 0.f : kUp - m;
-          const uint64_t by2 = two(by, by), down2 = two(down, down);
-          uint64_t l2 = two(0.f, 0.f), l3 = two(0.f, 0.f);
-          const auto exponentials = [&](const uint32_t* z, uint32_t col) {
-            uint32_t w[16];
+              const float down = m == -INFINITY ? 0.f : kUp - m;
+              const uint64_t by2 = two(by, by), down2 = two(down, down);
+              uint64_t l2 = two(0.f, 0.f), l3 = two(0.f, 0.f);
+              const auto exponentials = [&](const uint32_t* z, uint32_t* w) {
 #pragma unroll
-            for (int f = 0; f < 16; f += 2) {
-              float p0, p1, p2, p3;
-              apart(fma2(two(z[2 * f], z[2 * f + 1]), by2, down2), p0, p1);
-              apart(fma2(two(z[2 * f + 2], z[2 * f + 3]), by2, down2), p2, p3);
-              p0 = exp2_fast(p0);
-              p1 = exp2_fast(p1);
-              p2 = exp2_fast(p2);
-              p3 = exp2_fast(p3);
-              l2 = add2(l2, two(p0, p1));
-              l3 = add2(l3, two(p2, p3));
-              w[f] = P::pack(p0, p1);
-              w[f + 1] = P::pack(p2, p3);
+                for (int f = 0; f < 16; f += 2) {
+                  float p0, p1, p2, p3;
+                  apart(fma2(two(z[2 * f], z[2 * f + 1]), by2, down2), p0, p1);
+                  apart(fma2(two(z[2 * f + 2], z[2 * f + 3]), by2, down2), p2, p3);
+                  p0 = exp2_fast(p0);
+                  p1 = exp2_fast(p1);
+                  p2 = exp2_fast(p2);
+                  p3 = exp2_fast(p3);
+                  l2 = add2(l2, two(p0, p1));
+                  l3 = add2(l3, two(p2, p3));
+                  w[f] = P::pack(p0, p1);
+                  w[f + 1] = P::pack(p2, p3);
+                }
+              };
+              exponentials(x, w);
+              exponentials(y, w + 16);
+              float l0, l1;
+              apart(add2(l2, l3), l0, l1);
+              here = l0 + l1;
+              if (again || __all_sync(0xffffffffu, here <= kMost)) break;
+              again = true;
             }
-            tc_st16(col, w);
-          };
-          exponentials(x, s_col);
-          exponentials(y, s_col + 16);
-          float l0, l1;
-          apart(add2(l2, l3), l0, l1);
+          }
+          tc_st16(s_col, w);
+          tc_st16(s_col + 16, w + 16);
           {  // l + here, whose rounding is l - (sum - took) + (here - took) to the last bit
-            const float here = l0 + l1, sum = l + here, took = sum - l;
+            const float sum = l + here, took = sum - l;
             l_rest += (l - (sum - took)) + (here - took);
             l = sum;
           }

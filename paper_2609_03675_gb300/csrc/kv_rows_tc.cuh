@@ -58,8 +58,8 @@ constexpr uint32_t kTcStreamed = 4; // tiles from which an item of 128 rows or l
 template <typename T>
 constexpr uint32_t kTcChain = std::is_same<T, __half>::value ? 128 : 1024;
 constexpr uint64_t kTcTimeout = 1000000000ull;
-// Registers where there are unpackers: all threads start with 96; 256 x 136 + 256 x 64 + 128 x 80 is 640 x 96.
-constexpr int kTcRegsSoftmax = 136, kTcRegsUnpack = 64, kTcRegsIssuer = 80;
+// Registers where there are unpackers: all threads start with 96; 256 x 144 + 256 x 56 + 128 x 80 is 640 x 96.
+constexpr int kTcRegsSoftmax = 144, kTcRegsUnpack = 56, kTcRegsIssuer = 80;
 
 // What the loader of keys says of a tile; all but the softmax and the loaders go by it alone.
 struct TcInfo {
@@ -753,79 +753,82 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
   } else {
     if constexpr (BITS < 16) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kTcRegsIssuer));
     if (warp < kLoader) {
-    // ---------------------------------------------------------------- products: S (v = 0), or O (v = 1)
-    constexpr uint32_t kQK = tc_idesc<T>(128, kTile, false), kPV = tc_idesc<T>(128, D, true);
-    constexpr uint32_t kStep = S::kBlock * (D / 64) / 16;  // from one stage's descriptor to the next's
-    const uint32_t leader = tc_leader(), v = warp - kIssuer;
-    const uint32_t kv = tc_desc(shared_address(sm.kv[v][0]), v ? S::kBlock : 16);
-    uint32_t q_parity = 0;  // a bit for each stream
-    Turn<kTcInfo> told;
-    Turn<kStages> at;  // keys or values to come
-    Turn<2> s[2];      // S to be written, or P to be read
+      // -------------------------------------------------------------- products: S (v = 0), or O (v = 1)
+      // What the warp goes by is brought to where all lanes' common values live (by reductions over them), so that the
+      // operands of a product take an addition there and no way of their own.
+      const uint32_t leader = tc_leader(), t_mem = __reduce_max_sync(0xffffffffu, tmem);
+      const auto products = [&](auto kind) {
+        constexpr uint32_t v = decltype(kind)::value;
+        constexpr uint32_t kQK = tc_idesc<T>(128, kTile, false), kPV = tc_idesc<T>(128, D, true);
+        constexpr uint32_t kStep = S::kBlock * (D / 64) / 16;  // from one stage's descriptor to the next's
+        const uint32_t kv = tc_desc(shared_address(sm.kv[v][0]), v ? S::kBlock : 16);
+        uint32_t q_parity = 0;  // a bit for each stream
+        Turn<kTcInfo> told;
+        Turn<kStages> at;  // keys or values to come
+        Turn<2> s[2];      // S to be written, or P to be read
 #pragma unroll 1
-    for (;;) {
-      ok = __all_sync(0xffffffffu, tc_wait(&sm.info_full[told.i], told.parity, stop));
-      if (!ok) break;
-      const TcInfo& info = sm.info[told.i];
-      const uint32_t flags = info.flags, j = info.j;
-      if (flags & kTcEnd) break;
-      told.next();
-      const bool both = flags & kTcBoth;
-      const uint32_t i = both ? j / 2 : j;  // of the stream's tiles of the item
-      ok = __all_sync(0xffffffffu, tc_wait(&sm.full[v][at.i], at.parity, stop));
-      if (!ok) break;
-      if (BITS == 16 && v == 1) {
-        const uint32_t bits0 = info.bits[0], bits1 = info.bits[1];
-        if ((bits0 & bits1) != ~0u) {
+        for (;;) {
+          if (!__all_sync(0xffffffffu, tc_wait(&sm.info_full[told.i], told.parity, stop))) return false;
+          const TcInfo& info = sm.info[told.i];
+          const uint32_t flags = __reduce_or_sync(0xffffffffu, info.flags), j = __reduce_max_sync(0xffffffffu, info.j);
+          if (flags & kTcEnd) return true;
+          const bool both = flags & kTcBoth;
+          const uint32_t i = both ? j / 2 : j;  // of the stream's tiles of the item
+          if (!__all_sync(0xffffffffu, tc_wait(&sm.full[v][at.i], at.parity, stop))) return false;
+          if (BITS == 16 && v == 1) {
+            const uint32_t bits0 = info.bits[0], bits1 = info.bits[1];
+            if (__any_sync(0xffffffffu, (bits0 & bits1) != ~0u)) {
 #pragma unroll 1
-          for (uint32_t e = lane; e < kTile * (D / 8); e += 32) {
-            const uint32_t tok = e / 8 % kTile;
-            if (!((tok < 32 ? bits0 : bits1) >> (tok % 32) & 1u))
-              *reinterpret_cast<uint4*>(sm.kv[1][at.i] + e / 8 / kTile * S::kBlock + tok * 128 + e % 8 * 16) = make_uint4(0, 0, 0, 0);
+              for (uint32_t e = lane; e < kTile * (D / 8); e += 32) {
+                const uint32_t tok = e / 8 % kTile;
+                if (!((tok < 32 ? bits0 : bits1) >> (tok % 32) & 1u))
+                  *reinterpret_cast<uint4*>(sm.kv[1][at.i] + e / 8 / kTile * S::kBlock + tok * 128 + e % 8 * 16) = make_uint4(0, 0, 0, 0);
+              }
+              fence_async_shared();
+              __syncwarp();
+            }
           }
-          fence_async_shared();
-          __syncwarp();
-        }
-      }
-      const uint32_t x = kv + at.i * kStep;
+          told.next();
+          const uint32_t x = kv + at.i * kStep;
 #pragma unroll
-      for (uint32_t t = 0; t < 2; ++t) {
-        if (both ? j % 2 != t : t == 1 && !(flags & kTcSecond)) continue;
-        if (v == 1) {
-          ok = tc_wait(&sm.p_full[t][s[t].i], s[t].parity, stop);
-        } else if (i == 0) {
-          ok = tc_wait(&sm.q_full[t], q_parity >> t, stop);
-          q_parity ^= 1u << t;
-        } else if (i > 1) {  // this S holds the P of two tiles before
-          ok = tc_wait(&sm.o_full[t][s[t].i], s[t].parity ^ 1, stop);
-        }
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-        tc_fence_after();
-        const uint32_t y = s_at(t, s[t].i);
-        if (v == 0) {
-          const uint32_t q = tc_desc(shared_address(sm.q[t]), 16);
+          for (uint32_t t = 0; t < 2; ++t) {
+            if (both ? j % 2 != t : t == 1 && !(flags & kTcSecond)) continue;
+            bool there = true;
+            if (v == 1) {
+              there = tc_wait(&sm.p_full[t][s[t].i], s[t].parity, stop);
+            } else if (i == 0) {
+              there = tc_wait(&sm.q_full[t], q_parity >> t, stop);
+              q_parity ^= 1u << t;
+            } else if (i > 1) {  // this S holds the P of two tiles before
+              there = tc_wait(&sm.o_full[t][s[t].i], s[t].parity ^ 1, stop);
+            }
+            if (!__all_sync(0xffffffffu, there)) return false;
+            tc_fence_after();
+            const uint32_t y = t_mem + 2 * D + (2 * t + s[t].i) * kTile;
+            if (v == 0) {
+              const uint32_t q = tc_desc(shared_address(sm.q[t]), 16);
 #pragma unroll
-          for (int e = 0; e < D / 16; ++e)
-            tc_mma_ss(leader, y, q + (e / 4) * (S::kBlockQ / 16) + (e % 4) * 2, x + (e / 4) * (S::kBlock / 16) + (e % 4) * 2, kQK, e > 0);
-          tc_commit(leader, &sm.s_full[t][s[t].i]);
-        } else {
+              for (int e = 0; e < D / 16; ++e)
+                tc_mma_ss(leader, y, q + (e / 4) * (S::kBlockQ / 16) + (e % 4) * 2, x + (e / 4) * (S::kBlock / 16) + (e % 4) * 2, kQK, e > 0);
+              tc_commit(leader, &sm.s_full[t][s[t].i]);
+            } else {
 #pragma unroll
-          for (int e = 0; e < static_cast<int>(kTile) / 16; ++e)
-            tc_mma_ts(leader, o_at(t), y + e * 8, x + e * (2048 / 16), kPV, i % kTcChain<T> != 0 || e > 0);
-          tc_commit(leader, &sm.o_full[t][s[t].i]);
+              for (int e = 0; e < static_cast<int>(kTile) / 16; ++e)
+                tc_mma_ts(leader, t_mem + t * D, y + e * 8, x + e * (2048 / 16), kPV, i % kTcChain<T> != 0 || e > 0);
+              tc_commit(leader, &sm.o_full[t][s[t].i]);
+            }
+            s[t].next();
+          }
+          tc_commit(leader, &sm.empty[v][at.i]);
+          at.next();
         }
-        s[t].next();
-      }
-      if (!ok) break;
-      tc_commit(leader, &sm.empty[v][at.i]);
-      at.next();
-    }
-    // what was issued, and its arrivals, finish before the tensor memory goes and the CTA ends: waited for even when
-    // another wait has run out
-    tc_commit(leader, &sm.drained);
-    if (!tc_wait(&sm.drained, 0, nullptr)) atomicOr(b.err, kKvErrWait);
-    __syncwarp();
+      };
+      ok = warp == kIssuer ? products(std::integral_constant<uint32_t, 0>()) : products(std::integral_constant<uint32_t, 1>());
+      // what was issued, and its arrivals, finish before the tensor memory goes and the CTA ends: waited for even when
+      // another wait has run out
+      tc_commit(leader, &sm.drained);
+      if (!tc_wait(&sm.drained, 0, nullptr)) atomicOr(b.err, kKvErrWait);
+      __syncwarp();
     } else if (warp < kLoader + 2) {
       // -------------------------------------------------------------- loaders of keys (v = 0) and of values (v = 1)
       const uint32_t v = warp - kLoader, leader = tc_leader();

@@ -11,6 +11,7 @@ namespace cofie {
 namespace {
 
 constexpr int kMaskThreads = 1024;
+constexpr uint64_t kShortTokens = 1024;
 
 // The tiles of 64 cached tokens of which the mask leaves one at least, in
 // order, a CTA to a sequence, 1024 tiles at a time: neighbouring lanes look at
@@ -184,11 +185,11 @@ cudaError_t attend_set_up(cofie_kv* h) {
     if (e == cudaSuccess) e = map_pages(h->p, h->p.v_pages, &h->maps[1]);
   }
   size_t rows = 2ull * sm_count() * kManyRows, ctas = 0;
-  for (int i = 0; i < 6 && e == cudaSuccess; ++i) {
-    const int kind = i % 3;
+  for (int i = 0; i < 8 && e == cudaSuccess; ++i) {
+    const int kind = i < 3 ? i : i - 3;
     const AttendLaunch k = kernel_of(h->p, kind, i >= 3);
     e = cudaFuncSetAttribute(k.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(k.smem));
-    if (kind == kMany || e != cudaSuccess) continue;
+    if (kind >= kMany || e != cudaSuccess) continue;
     int per_sm = 0;
     e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, k.kernel, static_cast<int>(k.threads), k.smem);
     if (e == cudaSuccess && per_sm < 1) e = cudaErrorInvalidConfiguration;
@@ -290,10 +291,15 @@ int launch_attend(cofie_kv* h, AttendArgs* a, uint64_t rows, bool shared, cudaSt
   // 394, thirty of 16 over up to 2000 87 / 91 / 97 / 103. Few, with 2 / 4 / 6 / 8 / 12: 24 x 3 tokens over up to 9000 of
   // 4 bits 91 / 79 / 72 / 69 / 62, 64 x 1 over up to 20000 of 4 bits 220 / 212 / 200 / 197 / 199, of 16 bits 419 / 402 /
   // 400 / 394 / 398, 8 x 1 over up to 3000 27 / 25 / 23 / 25 / 25.
-  const int kind = rows > 32 ? kMany : rows > 8 ? kFew16 : kFew8;
+  // Own tokens behind a prefix are few as a rule: up to kShortTokens, as the table's width bounds them, a sequence and key
+  // head are left to one CTA.
+  int kind = rows > 32 ? kMany : rows > 8 ? kFew16 : kFew8;
+  const uint64_t items = static_cast<uint64_t>(a->batch.n_seqs) * a->batch.kv_heads;
+  if (a->behind && kind != kMany && (static_cast<uint64_t>(a->batch.table_stride) << h->page_shift) <= kShortTokens && items <= 0x7fffffffu)
+    kind = kind == kFew8 ? kShort8 : kShort16;
   a->item_slots = kind == kMany ? 8 : 6;
   const AttendLaunch k = kernel_of(h->p, kind, shared);
-  const uint32_t ctas = kind == kMany ? sm_count() : h->split_ctas[shared][kind];
+  const uint32_t ctas = kind == kMany ? sm_count() : kind >= kShort8 ? static_cast<uint32_t>(items) : h->split_ctas[shared][kind];
   if (const int rc = launched(h, launch_dependent(true, k.kernel, dim3(ctas), dim3(k.threads), k.smem, st, *a), "attend")) return rc;
   if (kind != kMany) return COFIE_OK;
   return launched(h, launch_dependent(true, k.join, dim3(ctas, kManyRows / k.join_rows), dim3(k.join_threads), 0, st, *a), "attend");

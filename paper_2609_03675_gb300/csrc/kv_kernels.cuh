@@ -7,7 +7,8 @@
 namespace cofie {
 
 using AttendKernel = void (*)(AttendArgs);
-enum : int { kFew8 = 0, kFew16 = 1, kMany = 2 };  // up to 8 or 16 rows a block; tiles of 128
+// Up to 8 or 16 rows a block; tiles of 128; up to 8 or 16, a CTA to each sequence and key head (shared prefixes only).
+enum : int { kFew8 = 0, kFew16 = 1, kMany = 2, kShort8 = 3, kShort16 = 4 };
 
 struct AttendLaunch {
   AttendKernel kernel;

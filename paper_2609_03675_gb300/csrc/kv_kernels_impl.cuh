@@ -11,8 +11,12 @@ template <typename T, int D, int BITS, bool SHARED>
 AttendLaunch attend_kernel_of(int kind) {
   if (kind == kMany)
     return {attend_rows_tc<T, D, BITS, SHARED>, kTcThreads<BITS>, tc_smem<D, BITS, SHARED>(), attend_join<T, D, SHARED>, kJoinThreads, kJoinRows<D>};
-  if (kind == kFew8) return {attend_split<T, D, BITS, 1, SHARED>, kSplitThreads, split_smem<D, BITS, 1>(), nullptr, 0, 0};
-  return {attend_split<T, D, BITS, 2, SHARED>, kSplitThreads, split_smem<D, BITS, 2>(), nullptr, 0, 0};
+  if constexpr (SHARED) {
+    if (kind == kShort8) return {attend_split<T, D, BITS, 1, true, true>, kSplitThreads<true>, split_smem<D, BITS, 1, true>(), nullptr, 0, 0};
+    if (kind == kShort16) return {attend_split<T, D, BITS, 2, true, true>, kSplitThreads<true>, split_smem<D, BITS, 2, true>(), nullptr, 0, 0};
+  }
+  if (kind == kFew8) return {attend_split<T, D, BITS, 1, SHARED, false>, kSplitThreads<false>, split_smem<D, BITS, 1, false>(), nullptr, 0, 0};
+  return {attend_split<T, D, BITS, 2, SHARED, false>, kSplitThreads<false>, split_smem<D, BITS, 2, false>(), nullptr, 0, 0};
 }
 
 }  // namespace

@@ -42,8 +42,12 @@
 namespace cofie {
 namespace {
 
-constexpr int kSplitWarps = 8;
-constexpr int kSplitThreads = 32 * kSplitWarps;
+// SHORT: a CTA of half the warps to each sequence, key head and block of rows, so that none of them is cut and two CTAs fit
+// an SM.
+template <bool SHORT>
+constexpr int kSplitWarps = SHORT ? 4 : 8;
+template <bool SHORT>
+constexpr int kSplitThreads = 32 * kSplitWarps<SHORT>;
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool live) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
@@ -127,11 +131,30 @@ struct Ring {
   static constexpr int kUnits = kRow / 16;                                // 16-byte units of a token
 };
 
-template <int D, int BITS, int NT>
+template <int D, int BITS, int NT, bool SHORT>
 __host__ __device__ constexpr size_t split_smem() {
-  const size_t ring = static_cast<size_t>(kSplitWarps) * Ring<D, BITS>::kWarp, join = static_cast<size_t>(kSplitWarps) * 8 * NT * D * 4;
+  const size_t warps = kSplitWarps<SHORT>, ring = warps * Ring<D, BITS>::kWarp, join = warps * 8 * NT * D * 4;
   return ring > join ? ring : join;
 }
+
+// The one sequence and key head of a SHORT CTA, block of rows by block.
+struct ShortWalk {
+  const AttendArgs& a;
+  const uint32_t rows_per_block;
+  uint32_t rb = 0;
+  __device__ __forceinline__ ShortWalk(const AttendArgs& args, uint32_t rows) : a(args), rows_per_block(rows) {}
+  __device__ __forceinline__ bool next(Item& it) {
+    it.seq = blockIdx.x / a.batch.kv_heads;
+    it.head = blockIdx.x % a.batch.kv_heads;
+    if (rb == 0) it.span = sequence_span(a.batch, it.seq);
+    if (static_cast<uint64_t>(rb) * rows_per_block >= static_cast<uint64_t>(it.span.count) * a.group) return false;
+    it.rb = rb++;
+    it.tiles = it.hi = block_tiles(a, it.span, rows_per_block, it.rb, it.seq);
+    it.lo = 0;
+    it.first_cta = it.last_cta = blockIdx.x;
+    return true;
+  }
+};
 
 // Where unit u of token t lies in its chunk, such that the reads below meet no bank twice.
 template <int D, int BITS, bool VALUES>
@@ -142,11 +165,12 @@ __device__ __forceinline__ uint32_t unit_at(uint32_t t, uint32_t u) {
 }
 
 // SHARED: over a prefix that several sequences share (a.rows), or for sequences behind one (a.behind).
-template <typename T, int D, int BITS, int NT, bool SHARED>
-__global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) attend_split(const __grid_constant__ AttendArgs a) {
+template <typename T, int D, int BITS, int NT, bool SHARED, bool SHORT>
+__global__ void __launch_bounds__(kSplitThreads<SHORT>, SHORT || (NT == 1 && BITS == 4) ? 2 : 1) attend_split(const __grid_constant__ AttendArgs a) {
   using P = Pair<T>;
   using H = Pair<__half>;
   using R = Ring<D, BITS>;
+  constexpr int kWarps = kSplitWarps<SHORT>, kThreads = kSplitThreads<SHORT>;
   constexpr int kRows = 8 * NT, kGroups = D / 64, kM = R::kTokens / 16, kPerTile = kTile / R::kTokens;
   // 16-bit values: weights go into the second product as fp16 numbers of up to 2^8, so that only those under 2^-33 are
   // lost to it. (Up to 1, those under 2^-25 were, though not to the sum of weights: 262144 keys 17.5 below one are 0.7 %
@@ -154,17 +178,23 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
   // of fp32, and 4-bit values have a power of two with their scale.)
   constexpr float kUp = BITS == 16 && std::is_same<T, __half>::value ? 8.f : 0.f, kDown = kUp > 0.f ? 0x1p-8f : 1.f;
   extern __shared__ __align__(128) char smem[];
-  __shared__ Plan<kSplitThreads> plan;
-  __shared__ Span spans[kSpans];
-  __shared__ float warp_m[kSplitWarps][kRows], warp_l[kSplitWarps][kRows];
-  __shared__ uint2 stages[kSplitWarps][R::kStages];  // the bits of the tokens that are seen, and the first one's place
-  __shared__ uint32_t row_bits[SHARED ? kSplitWarps : 1][R::kStages][kRows];  // and those that each row sees, where rows differ
+  __shared__ std::conditional_t<SHORT, char, Plan<kThreads>> plan;
+  __shared__ Span spans[SHORT ? 1 : kSpans];
+  __shared__ float warp_m[kWarps][kRows], warp_l[kWarps][kRows];
+  __shared__ uint2 stages[kWarps][R::kStages];  // the bits of the tokens that are seen, and the first one's place
+  __shared__ uint32_t row_bits[SHARED ? kWarps : 1][R::kStages][kRows];  // and those that each row sees, where rows differ
   __shared__ uint32_t last_here;
   pdl_trigger();
   pdl_wait();
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, c = lane % 4;
-  const uint64_t range = plan.set_up(a, kRows, spans);
-  Walk<kSplitThreads> walk(a, plan, spans, kRows, range);
+  auto walk = [&] {
+    if constexpr (SHORT) {
+      return ShortWalk(a, kRows);
+    } else {
+      const uint64_t range = plan.set_up(a, kRows, spans);
+      return Walk<kThreads>(a, plan, spans, kRows, range);
+    }
+  }();
   const char* const ring = smem + warp * R::kWarp;
   const BatchArg& b = a.batch;
   Item it;
@@ -254,8 +284,8 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
     {
       Ahead first[R::kStages - 1];
 #pragma unroll
-      for (int s = 0; s < R::kStages - 1; ++s) first[s] = look(warp + s * kSplitWarps);
-      ahead = look(warp + (R::kStages - 1) * kSplitWarps);
+      for (int s = 0; s < R::kStages - 1; ++s) first[s] = look(warp + s * kWarps);
+      ahead = look(warp + (R::kStages - 1) * kWarps);
 #pragma unroll
       for (int s = 0; s < R::kStages - 1; ++s) issue(s, first[s]);
     }
@@ -360,7 +390,7 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
     }
 
     uint32_t stage = 0;
-    for (uint32_t ch = warp; ch < chunks; ch += kSplitWarps) {
+    for (uint32_t ch = warp; ch < chunks; ch += kWarps) {
       cp_async_wait<R::kStages - 2>();
       __syncwarp();
       const char* const base = ring + stage * R::kStage;
@@ -372,9 +402,9 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
 #pragma unroll
         for (int e = 0; e < 2; ++e) sees[nt][e] = by_row ? bits & row_bits[warp][stage][nt * 8 + 2 * c + e] : bits;
       issue(stage == 0 ? R::kStages - 1 : stage - 1, ahead);  // the stage read in the iteration before
-      ahead = look(ch + R::kStages * kSplitWarps);
+      ahead = look(ch + R::kStages * kWarps);
       if (++stage == R::kStages) stage = 0;
-      if (ch / kSplitWarps % kSumChunks == 0) {
+      if (ch / kWarps % kSumChunks == 0) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           l[nt][0] += l_part[nt][0];
@@ -720,14 +750,14 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
       }
       if (a.lse && d == 0) a.lse[static_cast<uint64_t>(i) * a.heads + h] = (top + log2f(sum * down)) * 0.6931471805599453f;
     };
-    for (uint32_t x = threadIdx.x; x < rows * (D / 4); x += kSplitThreads) {
+    for (uint32_t x = threadIdx.x; x < rows * (D / 4); x += kThreads) {
       const uint32_t r = x / (D / 4), d = x % (D / 4) * 4;
       float top = -INFINITY, sum = 0.f;
 #pragma unroll
-      for (int w = 0; w < kSplitWarps; ++w) top = fmaxf(top, warp_m[w][r]);
+      for (int w = 0; w < kWarps; ++w) top = fmaxf(top, warp_m[w][r]);
       float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int w = 0; w < kSplitWarps; ++w) {
+      for (int w = 0; w < kWarps; ++w) {
         const float k = warp_m[w][r] == -INFINITY ? 0.f : exp2_fast(warp_m[w][r] - top);
         if (warp_m[w][r] == -INFINITY && warp_l[w][r] == 0.f) continue;
         const float4 z = *reinterpret_cast<const float4*>(buf + (w * kRows + r) * D + d);
@@ -750,25 +780,25 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
         const uint32_t parts = it.last_cta - it.first_cta + 1;
         const auto part_at = [&](uint32_t i, uint32_t r) { return (2ull * (it.first_cta + i) + (i == 0)) * kRows + r; };
         float2* ms = reinterpret_cast<float2*>(smem);  // [part][row]
-        constexpr uint32_t kJoin = split_smem<D, BITS, NT>() / (kRows * sizeof(float2));
+        constexpr uint32_t kJoin = split_smem<D, BITS, NT, SHORT>() / (kRows * sizeof(float2));
         float top = -INFINITY, sum = 0.f;  // of row threadIdx.x
         for (uint32_t p0 = 0; p0 < parts; p0 += kJoin) {
           const uint32_t n = min(kJoin, parts - p0);
           __syncthreads();
-          for (uint32_t x = threadIdx.x; x < n * kRows; x += kSplitThreads) ms[x] = __ldcg(&a.part_ms[part_at(p0 + x / kRows, x % kRows)]);
+          for (uint32_t x = threadIdx.x; x < n * kRows; x += kThreads) ms[x] = __ldcg(&a.part_ms[part_at(p0 + x / kRows, x % kRows)]);
           __syncthreads();
           if (threadIdx.x < rows)
             for (uint32_t i = 0; i < n; ++i) top = fmaxf(top, ms[i * kRows + threadIdx.x].x);
         }
         if (threadIdx.x < kRows) warp_m[0][threadIdx.x] = top;
-        constexpr int kMost = (kRows * (D / 4) + kSplitThreads - 1) / kSplitThreads;
+        constexpr int kMost = (kRows * (D / 4) + kThreads - 1) / kThreads;
         float4 y[kMost];
 #pragma unroll
         for (int q = 0; q < kMost; ++q) y[q] = make_float4(0.f, 0.f, 0.f, 0.f);
         for (uint32_t p0 = 0; p0 < parts; p0 += kJoin) {
           const uint32_t n = min(kJoin, parts - p0);
           __syncthreads();
-          for (uint32_t x = threadIdx.x; x < n * kRows; x += kSplitThreads) {
+          for (uint32_t x = threadIdx.x; x < n * kRows; x += kThreads) {
             const float2 z = parts <= kJoin ? ms[x] : __ldcg(&a.part_ms[part_at(p0 + x / kRows, x % kRows)]);
             const float k = z.x == -INFINITY ? (z.y == 0.f ? 0.f : 1.f) : exp2_fast(z.x - warp_m[0][x % kRows]);
             ms[x] = make_float2(k, z.y == 0.f ? 0.f : k * z.y);
@@ -778,7 +808,7 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
             for (uint32_t i = 0; i < n; ++i) sum += ms[i * kRows + threadIdx.x].y;
 #pragma unroll
           for (int q = 0; q < kMost; ++q) {
-            const uint32_t x = threadIdx.x + q * kSplitThreads, r = x / (D / 4), d = x % (D / 4) * 4;
+            const uint32_t x = threadIdx.x + q * kThreads, r = x / (D / 4), d = x % (D / 4) * 4;
             if (r >= rows) break;
 #pragma unroll 8
             for (uint32_t i = 0; i < n; ++i) {
@@ -792,7 +822,7 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 && BITS == 4 ? 2 : 1) a
         __syncthreads();
 #pragma unroll
         for (int q = 0; q < kMost; ++q) {
-          const uint32_t x = threadIdx.x + q * kSplitThreads, r = x / (D / 4), d = x % (D / 4) * 4;
+          const uint32_t x = threadIdx.x + q * kThreads, r = x / (D / 4), d = x % (D / 4) * 4;
           if (r < rows) write(r, d, y[q], warp_m[0][r], warp_l[0][r]);
         }
       }

@@ -2,6 +2,7 @@
 #include <algorithm>
 #include <cstring>
 #include <new>
+#include <type_traits>
 
 #include "kv_handle.cuh"
 
@@ -44,6 +45,17 @@ __global__ void __launch_bounds__(kThreads, 4) append_codes(const __grid_constan
   const uint32_t t0 = blockIdx.x * r.tile, n = min(r.tile, r.n_tokens - t0);
   pdl_trigger();
   pdl_wait();
+  if (WIDE && blockIdx.y >= a.q_parts) {  // the CTA's rows are asked for before its angles and places are formed
+    const uint32_t parts0 = gridDim.y - a.q_parts, part0 = blockIdx.y - a.q_parts;
+    const uint32_t per0 = (2 * a.kv_heads + parts0 - 1) / parts0, first = part0 * per0, many = min(per0, 2 * a.kv_heads - min(first, 2 * a.kv_heads));
+    constexpr uint32_t kLines = D * 2 / 128;
+    for (uint32_t e = threadIdx.x; e < many * n * kLines; e += kThreads) {
+      const uint32_t line = e % kLines, row = e / kLines, kind0 = first + row % many, t = row / many;
+      const uint32_t v0 = kind0 >= a.kv_heads, head0 = kind0 - v0 * a.kv_heads;
+      const char* p = a.in[v0] + 2 * (static_cast<int64_t>(t0 + t) * a.in_token[v0] + head0 * a.in_head[v0]) + line * 128;
+      asm volatile("prefetch.global.L2 [%0];" ::"l"(p));
+    }
+  }
   rows_set_up(r, tab, t0, n, cs, place, offs);
   if (blockIdx.y < a.q_parts) {
     const uint32_t per = (r.heads + a.q_parts - 1) / a.q_parts, h0 = blockIdx.y * per;
@@ -156,8 +168,11 @@ __global__ void __launch_bounds__(kThreads, 4) append_codes(const __grid_constan
 #pragma unroll
             for (int i = 0; i < 8; ++i) u[i] = __float_as_uint(fminf(fmaxf(__uint_as_float(u[i]), 12582913.f), 12583167.f));
           }
-          codes8[e][0] = __byte_perm(__byte_perm(u[0], u[1], 0x0040), __byte_perm(u[2], u[3], 0x0040), 0x5410);
-          codes8[e][1] = __byte_perm(__byte_perm(u[4], u[5], 0x0040), __byte_perm(u[6], u[7], 0x0040), 0x5410);
+          // the bytes are the low bits of 0x4B400000 + byte, whose sum's share is taken off at the end (products and sums
+          // where byte permutations would wait for the pipe that the extremes keep busy)
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            codes8[e][i] = ((u[4 * i + 3] * 256 + u[4 * i + 2]) * 256 + u[4 * i + 1]) * 256 + u[4 * i] - 0x4B400000u * 0x01010101u;
         }
       } else {
         // the extremes of the lane's groups: its two eights are of one (D = 64) or of two
@@ -254,10 +269,10 @@ struct ReadArgs {
 constexpr uint32_t kReadTile = 16;  // tokens of a CTA
 
 // A warp takes the keys or the values of a head, some tokens at a time, eight
-// values of a row to a lane.
+// values of a row to a lane, or 16 bytes.
 template <typename T, int D, int BITS>
 __global__ void __launch_bounds__(kThreads) read_pages(const __grid_constant__ ReadArgs a) {
-  constexpr uint32_t kLanes = D / 8, kStep = 32 / kLanes;
+  constexpr uint32_t kValues = BITS == 8 ? 16 : 8, kLanes = D / kValues, kStep = 32 / kLanes;
   __shared__ int64_t place[kReadTile];
   pdl_trigger();
   pdl_wait();
@@ -268,29 +283,49 @@ __global__ void __launch_bounds__(kThreads) read_pages(const __grid_constant__ R
   for (uint32_t kind = blockIdx.y * (kThreads / 32) + threadIdx.x / 32; kind < 2 * kv; kind += gridDim.y * (kThreads / 32)) {
     const uint32_t v = kind >= kv, head = kind - v * kv;
     // from the head's place in a page
-    const char* const pages = a.pages[v] + static_cast<uint64_t>(head << shift) * (D * BITS / 8) + lane * BITS;
-    const uint16_t* const words = a.words[v] + static_cast<uint64_t>(head << shift) * (D / kGroup) + lane / 8;
-    uint4* const out = a.out[v] + (static_cast<uint64_t>(t0) * kv + head) * kLanes + lane;
-#pragma unroll 4
-    for (uint32_t t = mine; t < n; t += kStep) {
-      const int64_t p = place[t];
-      uint4 val = make_uint4(0, 0, 0, 0);
-      if (p >= 0) {
-        const uint64_t at = ((static_cast<uint64_t>(p) >> shift) * kv << shift) + (static_cast<uint32_t>(p) & ((1u << shift) - 1));
-        if (BITS == 16) {
-          val = *reinterpret_cast<const uint4*>(pages + at * (D * 2));
-        } else if (BITS == 8) {
-          const Bytes<T> u(words[at * (D / kGroup)]);
-          const uint2 x = *reinterpret_cast<const uint2*>(pages + at * D), y = u(x.x), z = u(x.y);
-          val = make_uint4(y.x, y.y, z.x, z.y);
-        } else {
-          const Unpack<T> u(words[at * (D / kGroup)]);
-          const uint4 y = u(*reinterpret_cast<const uint32_t*>(pages + at * (D / 2)));  // (0, 4), (1, 5), (2, 6), (3, 7)
-          val = make_uint4(__byte_perm(y.x, y.y, 0x5410), __byte_perm(y.z, y.w, 0x5410), __byte_perm(y.x, y.y, 0x7632),
-                           __byte_perm(y.z, y.w, 0x7632));
-        }
+    const char* const pages = a.pages[v] + static_cast<uint64_t>(head << shift) * (D * BITS / 8) + lane * (kValues * BITS / 8);
+    const uint16_t* const words = a.words[v] + static_cast<uint64_t>(head << shift) * (D / kGroup) + lane * kValues / kGroup;
+    uint4* const out = a.out[v] + (static_cast<uint64_t>(t0) * kv + head) * (D / 8) + lane * (kValues / 8);
+    using Raw = std::conditional_t<BITS == 4, uint32_t, uint4>;
+    constexpr int kAtOnce = kReadTile / kStep < 4 ? kReadTile / kStep : 4;  // rows whose loads are on their way together
+    for (uint32_t t1 = mine; t1 < n; t1 += kAtOnce * kStep) {
+      int64_t p[kAtOnce];
+      Raw x[kAtOnce];
+      uint32_t word[kAtOnce];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const uint32_t t = t1 + i * kStep;
+        p[i] = t < n ? place[t] : -1;
+        // (the pages' first row is there to be read where the batch gives the token no place)
+        const int64_t q = max(p[i], static_cast<int64_t>(0));
+        const uint64_t at = ((static_cast<uint64_t>(q) >> shift) * kv << shift) + (static_cast<uint32_t>(q) & ((1u << shift) - 1));
+        x[i] = *reinterpret_cast<const Raw*>(pages + at * (D * BITS / 8));
+        word[i] = BITS < 16 ? words[at * (D / kGroup)] : 0;
       }
-      out[static_cast<uint64_t>(t) * kv * kLanes] = val;
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const uint32_t t = t1 + i * kStep;
+        if (t >= n) continue;
+        uint4 val = make_uint4(0, 0, 0, 0), more = val;
+        if (p[i] >= 0) {
+          if constexpr (BITS == 16) {
+            val = x[i];
+          } else if constexpr (BITS == 8) {
+            const Bytes<T> u(word[i]);
+            const uint2 y0 = u(x[i].x), y1 = u(x[i].y), y2 = u(x[i].z), y3 = u(x[i].w);
+            val = make_uint4(y0.x, y0.y, y1.x, y1.y);
+            more = make_uint4(y2.x, y2.y, y3.x, y3.y);
+          } else {
+            const Unpack<T> u(word[i]);
+            const uint4 y = u(x[i]);  // (0, 4), (1, 5), (2, 6), (3, 7)
+            val = make_uint4(__byte_perm(y.x, y.y, 0x5410), __byte_perm(y.z, y.w, 0x5410), __byte_perm(y.x, y.y, 0x7632),
+                             __byte_perm(y.z, y.w, 0x7632));
+          }
+        }
+        uint4* const to = out + static_cast<uint64_t>(t) * kv * (D / 8);
+        to[0] = val;
+        if (BITS == 8) to[1] = more;
+      }
     }
   }
 }

@@ -413,7 +413,7 @@ __global__ void __launch_bounds__(kSplitThreads<SHORT>, SHORT || (NT == 1 && BIT
         }
       }
       if (bits == 0) continue;
-      const bool whole = (BITS < 16 ? bits == 0xffffffffu : (bits & 0xffffu) == 0xffffu);
+      const bool whole = (R::kTokens == 32 ? bits == 0xffffffffu : (bits & 0xffffu) == 0xffffu);
       const char *const vbase = base + R::kTokens * R::kRow, *const kw = base + 2 * R::kTokens * R::kRow, *const vw = kw + R::kWords;
 
       // ---- scores. Row slots of a 16-token operand hold tokens in this order (codes and bytes: so that both operands' reads

@@ -24,7 +24,8 @@
  *              uint16. A word serves 64 consecutive bytes and is the bf16 number
  *              s, a power of two. Byte u stands for (u - 128) s, which bf16 and
  *              fp16 hold exactly.
- *   Bytes of x (64 values, rotated keys as fp32 numbers): s is the smallest
+ *   Bytes of x (64 values, rotated keys as fp32 numbers, but those that fp32's
+ *   error leaves open between two bytes turned in 64 bits): s is the smallest
  *   power of two with max |x| <= 127 s, but at least 2^-100 and at most 2^121
  *   (bf16) or at least 2^-24 and at most 2^9 (fp16); u = 128 + [x / s], [] to the
  *   nearest, halves to the even one, cut to -127..127. A group that holds a NaN

@@ -29,6 +29,17 @@ __device__ __forceinline__ float code_back(float code, float zero, float x, floa
   return past ? code - copysignf(1.f, x) : code;
 }
 
+// Value d of a head, turned in 64 bits, as a byte's sum (see below): for the few
+// that lie closer to a half than fp32 tells.
+template <typename T>
+__device__ __noinline__ float exact_byte(const T* in, uint32_t d, uint32_t half, bool by_half, uint64_t turn, int32_t pos, float amplitude, float inverse) {
+  const bool second = by_half ? d >= half : d & 1;
+  const double x = Elem<T>::to(in[d]), y = Elem<T>::to(in[by_half ? (second ? d - half : d + half) : d ^ 1]);
+  double s, c;
+  sincospi(static_cast<double>(static_cast<int64_t>(turn * static_cast<uint64_t>(static_cast<int64_t>(pos)))) * 0x1p-63, &s, &c);
+  return static_cast<float>(rint((x * c + (second ? y * s : -y * s)) * amplitude * inverse) + 12583040.0);
+}
+
 // Appends to pages of 4-bit codes or of bytes. CTAs of gridDim.y below q_parts rotate the queries;
 // the others take a share of the (key or value, head) rows of their tokens.
 // Sixteen values of a row to a lane, eight from either half of the head, so that
@@ -147,15 +158,20 @@ __global__ void __launch_bounds__(kThreads, 4) append_codes(const __grid_constan
       uint32_t word[2], codes8[2][2];
       if constexpr (BITS == 8) {
         // the largest size of each of the lane's groups; x / s is exact but for what lies under the smallest scale, and
-        // 1.5 2^23 + 128 more rounds it to a whole number, halves to even, whose byte is the low one
+        // 1.5 2^23 + 128 more rounds it to a whole number, halves to even, whose byte is the low one. A rotated key is off by
+        // 2.8e-7 (|x| + |y|) of its pair (angle 9.4e-8, cos and sin 6e-8, products and sum 1.2e-7), so by 5.6e-7 of the
+        // largest turned value of the pair at most: one that lies so close to a half is turned once more in 64 bits. (One in
+        // 10^4; without that one in 3 10^5 bytes of rotated keys was its neighbour.)
         float size[2] = {0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < 16; ++i) size[kOwn == 1 ? 0 : i / 8] = max_nan(size[kOwn == 1 ? 0 : i / 8], fabsf(x[i]));
+        // (where a pair's other value is another lane's, the row's largest stands for the lane's)
+        float inverse[2], reach = fmaxf(size[0], size[1]);
 #pragma unroll
         for (int o = 1; o < static_cast<int>(kLanes); o <<= 1)
 #pragma unroll
           for (int gr = 0; gr < kOwn; ++gr) size[gr] = max_nan(size[gr], __shfl_xor_sync(0xffffffffu, size[gr], o));
-        float inverse[2];
+        if (by_half && turned != D) reach = fmaxf(size[0], size[1]);
 #pragma unroll
         for (int gr = 0; gr < kOwn; ++gr) word[gr] = byte_scale<T>(size[gr], inverse[gr]);
 #pragma unroll
@@ -164,6 +180,31 @@ __global__ void __launch_bounds__(kThreads, 4) append_codes(const __grid_constan
           uint32_t u[8];
 #pragma unroll
           for (int i = 0; i < 8; ++i) u[i] = __float_as_uint(__fmaf_rn(x[8 * e + i], inverse[gr], 12583040.f));
+          if (turned) {
+            float near = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              near = fmaxf(near, fabsf(__fmaf_rn(x[8 * e + i], inverse[gr], 12583040.f - __uint_as_float(u[i]))));
+            const float off = 6e-7f * reach * inverse[gr];
+            if (p >= 0 && near > 0.5f - off) {
+              const T* in = in0 + t * in_token;
+              uint32_t close = 0;
+#pragma unroll
+              for (int i = 0; i < 8; ++i)
+                close |= (fabsf(__fmaf_rn(x[8 * e + i], inverse[gr], 12583040.f - __uint_as_float(u[i]))) > 0.5f - off ? 1u : 0u) << i;
+#pragma unroll 1
+              for (; close; close &= close - 1) {
+                const uint32_t i = __ffs(close) - 1, d = e * (D / 2) + lane * 8 + i;
+                if (d >= turned) break;
+                const uint32_t pair = by_half ? (d >= tab.half ? d - tab.half : d) : d / 2;
+                const int32_t pos = r.positions[static_cast<uint64_t>(tab.axis[pair]) * r.n_tokens + t0 + t];
+                const float exact = exact_byte(in, d, tab.half, by_half, tab.turn[pair], pos, tab.amplitude, inverse[gr]);
+#pragma unroll
+                for (uint32_t f = 0; f < 8; ++f)
+                  if (f == i) u[f] = __float_as_uint(exact);
+              }
+            }
+          }
           if (!(size[gr] * inverse[gr] <= 127.f)) {  // past the largest scale's range
 #pragma unroll
             for (int i = 0; i < 8; ++i) u[i] = __float_as_uint(fminf(fmaxf(__uint_as_float(u[i]), 12582913.f), 12583167.f));

@@ -118,17 +118,30 @@ __global__ void __launch_bounds__(kWordThreads) prefix_words(const BatchArg grou
   }
 }
 
-// For each group the union of its sequences' words and the tiles where it is
-// not empty, in order: a CTA to a group, 1024 tiles at a time.
+// For each group the union of its sequences' words, and for each block of its
+// rows (the last list: for that block and all after it) the tiles where the
+// union of the sequences that have rows there is not empty, in order: a CTA to a
+// list, 1024 tiles at a time. (By lists of the group alone, blocks of 256 rows of
+// 16 questions that see 0.3 of 400 frames each took 594 us, so 458.)
 __global__ void __launch_bounds__(kMaskThreads) prefix_tiles(const BatchArg groups, const uint64_t* words, uint64_t* any, uint32_t* tiles,
-                                                             uint32_t* count, uint32_t tile_stride) {
+                                                             uint32_t* count, uint32_t tile_stride, const int32_t* seq_of, uint32_t block_rows,
+                                                             uint32_t group) {
   __shared__ uint32_t warps[kMaskThreads / 32];
   pdl_trigger();
   pdl_wait();
-  const uint32_t g = blockIdx.x, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  const uint32_t g = blockIdx.x, rb = blockIdx.y, lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  const uint64_t list = static_cast<uint64_t>(g) * gridDim.y + rb;
   const Span sp = sequence_span(groups, g);
-  const uint32_t s0 = groups.groups ? groups.groups[g] : 0, s1 = sp.count == 0 ? s0 : groups.groups ? groups.groups[g + 1] : groups.members;
-  const uint32_t all = sp.count == 0 ? 0 : (sp.length + kTile - 1) / kTile;
+  const uint64_t rows = static_cast<uint64_t>(sp.count) * group, row0 = static_cast<uint64_t>(rb) * block_rows;
+  const uint32_t all = row0 >= rows ? 0 : (sp.length + kTile - 1) / kTile;
+  uint32_t s0 = 0, s1 = 0, g0 = 0, g1 = 0;  // the block's sequences, and the group's
+  if (all) {
+    g0 = groups.groups ? groups.groups[g] : 0;
+    g1 = groups.groups ? groups.groups[g + 1] : groups.members;
+    const uint64_t last = rb + 1 == gridDim.y ? rows : min(rows, row0 + block_rows);
+    s0 = min(static_cast<uint32_t>(seq_of[sp.first + row0 / group]), groups.members - 1);
+    s1 = min(static_cast<uint32_t>(seq_of[sp.first + (last - 1) / group]), groups.members - 1) + 1;
+  }
   uint32_t n = 0;
   for (uint32_t t0 = 0; t0 < all; t0 += kMaskThreads) {
     const uint32_t t = t0 + threadIdx.x;
@@ -136,7 +149,13 @@ __global__ void __launch_bounds__(kMaskThreads) prefix_tiles(const BatchArg grou
     if (t < all) {
 #pragma unroll 8
       for (uint32_t s = s0; s < s1; ++s) word |= words[static_cast<uint64_t>(s) * tile_stride + t];
-      any[static_cast<uint64_t>(g) * tile_stride + t] = word;
+      if (rb == 0) {
+        uint64_t both = word;
+        if (s0 != g0 || s1 != g1)
+#pragma unroll 8
+          for (uint32_t s = g0; s < g1; ++s) both |= words[static_cast<uint64_t>(s) * tile_stride + t];
+        any[static_cast<uint64_t>(g) * tile_stride + t] = both;
+      }
     }
     const uint32_t bits = __ballot_sync(0xffffffffu, word != 0);
     if (lane == 0) warps[warp] = __popc(bits);
@@ -146,10 +165,10 @@ __global__ void __launch_bounds__(kMaskThreads) prefix_tiles(const BatchArg grou
       if (w < warp) before += warps[w];
       n += warps[w];
     }
-    if (word) tiles[static_cast<uint64_t>(g) * tile_stride + before + __popc(bits & ((1u << lane) - 1))] = t;
+    if (word) tiles[list * tile_stride + before + __popc(bits & ((1u << lane) - 1))] = t;
     __syncthreads();
   }
-  if (threadIdx.x == 0) count[g] = n;
+  if (threadIdx.x == 0) count[list] = n;
 }
 
 AttendLaunch kernel_of(const cofie_kv_params& p, int kind, bool shared) {
@@ -256,6 +275,7 @@ bool may_allocate(cudaStream_t st) {
 int list_tiles(cofie_kv* h, const cofie_kv_batch* b, AttendArgs* args, cudaStream_t st) {
   AttendArgs& a = *args;
   a.tile_stride = (b->table_stride << h->page_shift) / kTile + 1;
+  a.list_blocks = 1;
   const size_t need = static_cast<size_t>(b->n_seqs) * (a.tile_stride + 1);
   if (need > h->tiles_room) {
     const size_t room = std::max(need, 2 * h->tiles_room);
@@ -279,12 +299,19 @@ int list_tiles(cofie_kv* h, const cofie_kv_batch* b, AttendArgs* args, cudaStrea
                   "attend");
 }
 
-// The kernel for so many rows of a sequence and key head at most.
+// The kernel for so many rows of a sequence and key head at most: up to 16 rows, in blocks of 8 or 16, are left to the kernel
+// that reads the cache for each block; more rows pay for tiles of 128 of them. Eight sequences of up to 60000 tokens, 32
+// heads over 8 of 128 (us, blocks / tiles): 16 rows of 16 bits 178 / 174, of 8 bits 132 / 235, of 4 bits 123 / 186; 20 rows
+// 332 / 175, 239 / 236, 224 / 186. 32 sequences of up to 6000: 16 rows 85 / 92, 86 / 121, 81 / 102; 20 rows 137 / 94, 139 /
+// 121, 137 / 103. Eight of up to 2000: 16 rows 21 / 23, 24 / 28, 23 / 27; 20 rows 27 / 23, 29 / 29, 29 / 27. Without a shared
+// prefix 4-bit pages go by blocks up to 32 rows, though tiles would be quicker from 17: rows of tiles see values past fp16's
+// range as infinite, those of blocks do not, and calls of 17 to 32 rows have counted on that.
+int kind_of(const cofie_kv* h, uint64_t rows, bool shared) {
+  const uint64_t few = h->p.bits == 4 && !shared ? 32 : 16;
+  return rows > few ? kMany : rows > 8 ? kFew16 : kFew8;
+}
+
 int launch_attend(cofie_kv* h, AttendArgs* a, uint64_t rows, bool shared, cudaStream_t st) {
-  // Up to 32 rows of a sequence and head, in blocks of 8 or 16, are left to the kernel that reads the cache for each
-  // block; more rows pay for tiles of 128 of them. Eight sequences of up to 60000 tokens, 32 heads over 8 of 128 (us,
-  // blocks / tiles): 20 rows 176 / 233 with 4 bits, 214 / 337 with 16; 32 rows 188 / 234, 262 / 339; 48 rows 266 / 234,
-  // 344 / 340. Up to 2000 tokens: 20 rows 25 / 28, 22 / 32; 48 rows 32 / 29, 27 / 34.
   // What an item costs beside its tiles' slots (set-up, first loads, its part's joining), in the time of a tile: about 8 for
   // many rows and 6 for few, at every size tried. Many rows, us with 4 / 8 / 16 / 24 slots: seven questions of 3 to 300
   // tokens over up to 4000 of 4 bits 91 / 85 / 89 / 95, four prompts of 1024 over up to 8192 of 16 bits 451 / 343 / 371 /
@@ -293,7 +320,7 @@ int launch_attend(cofie_kv* h, AttendArgs* a, uint64_t rows, bool shared, cudaSt
   // 400 / 394 / 398, 8 x 1 over up to 3000 27 / 25 / 23 / 25 / 25.
   // Own tokens behind a prefix are few as a rule: up to kShortTokens, as the table's width bounds them, a sequence and key
   // head are left to one CTA.
-  int kind = rows > 32 ? kMany : rows > 8 ? kFew16 : kFew8;
+  int kind = kind_of(h, rows, shared);
   const uint64_t items = static_cast<uint64_t>(a->batch.n_seqs) * a->batch.kv_heads;
   if (a->behind && kind != kMany && (static_cast<uint64_t>(a->batch.table_stride) << h->page_shift) <= kShortTokens && items <= 0x7fffffffu)
     kind = kind == kFew8 ? kShort8 : kShort16;
@@ -327,12 +354,15 @@ int scratch(cofie_kv* h, cofie_kv::Scratch* s, size_t need, cudaStream_t st) {
 }
 
 // The mask of the prefixes: words, their union, the tiles that it leaves, and each token's sequence, one behind the other.
-int prefix_mask(cofie_kv* h, const cofie_kv_prefix* p, AttendArgs* args, cudaStream_t st) {
+int prefix_mask(cofie_kv* h, const cofie_kv_prefix* p, AttendArgs* args, uint64_t rows, cudaStream_t st) {
   AttendArgs& a = *args;
   const BatchArg& g = a.batch;
   a.tile_stride = (g.table_stride << h->page_shift) / kTile + 1;
-  const size_t seqs = g.members, groups = g.n_seqs, stride = a.tile_stride;
-  const size_t words = (seqs + groups) * stride * sizeof(uint64_t), tiles = groups * (stride + 1) * sizeof(uint32_t);
+  // lists for so many rows of a group; 256 of them at most, and with many groups one each
+  const uint32_t block_rows = kind_of(h, rows, true) == kMany ? kManyRows : kind_of(h, rows, true) == kFew16 ? 16u : 8u;
+  a.list_blocks = g.n_seqs > 256 ? 1u : static_cast<uint32_t>(std::min<uint64_t>((rows + block_rows - 1) / block_rows, 256 / g.n_seqs));
+  const size_t seqs = g.members, groups = g.n_seqs, stride = a.tile_stride, lists = groups * a.list_blocks;
+  const size_t words = (seqs + groups) * stride * sizeof(uint64_t), tiles = lists * (stride + 1) * sizeof(uint32_t);
   if (const int rc = scratch(h, &h->shared_mask, words + tiles + g.n_tokens * sizeof(int32_t), st)) return rc;
   char* at = static_cast<char*>(h->shared_mask.p);
   uint64_t* seq_words = reinterpret_cast<uint64_t*>(at);
@@ -342,7 +372,7 @@ int prefix_mask(cofie_kv* h, const cofie_kv_prefix* p, AttendArgs* args, cudaStr
   a.seq_words = seq_words;
   a.any_words = any;
   a.tiles = list;
-  a.tile_count = list + groups * stride;
+  a.tile_count = list + lists * stride;
   a.seq_of = seq_of;
   const bool wide = reinterpret_cast<uintptr_t>(p->mask) % 16 == 0 && (seqs == 1 || p->mask_stride % 16 == 0);
   const dim3 grid(std::max(1u, std::min((a.tile_stride + kWordThreads - 1) / kWordThreads, 64u)), std::min(g.members, 65535u));
@@ -350,8 +380,9 @@ int prefix_mask(cofie_kv* h, const cofie_kv_prefix* p, AttendArgs* args, cudaStr
                                                   p->mask_stride, seq_words, a.tile_stride, seq_of),
                               "attend"))
     return rc;
-  return launched(h, launch_dependent(true, prefix_tiles, dim3(g.n_seqs), dim3(kMaskThreads), 0, st, g, static_cast<const uint64_t*>(seq_words), any,
-                                      list, list + groups * stride, a.tile_stride),
+  return launched(h, launch_dependent(true, prefix_tiles, dim3(g.n_seqs, a.list_blocks), dim3(kMaskThreads), 0, st, g,
+                                      static_cast<const uint64_t*>(seq_words), any, list, list + lists * stride, a.tile_stride,
+                                      static_cast<const int32_t*>(seq_of), block_rows, a.group),
                   "attend");
 }
 
@@ -405,9 +436,9 @@ extern "C" int cofie_kv_attend_shared(cofie_kv_t* h, const cofie_kv_batch* b, co
   first.mask = nullptr;
   first.lse = nullptr;
   first.causal = 0;
-  if (prefix->mask)
-    if (const int rc = prefix_mask(h, prefix, &first, st)) return rc;
   const uint64_t most = prefix->max_new ? prefix->max_new : b->n_tokens;
+  if (prefix->mask)
+    if (const int rc = prefix_mask(h, prefix, &first, most * own.group, st)) return rc;
   if (const int rc = launch_attend(h, &first, most * own.group, true, st)) return rc;
   own.behind = 1;
   if (mask)

@@ -39,10 +39,11 @@ struct AttendArgs {
   uint32_t item_slots;  // slots that an item costs beside those of its tiles
   uint32_t q_wide, out_wide;  // rows of q (16-byte vectors) and of the output (8-byte) are aligned
   float scale;
-  // tiles that the mask leaves, in order, and their count, for each sequence (with a mask)
+  // tiles that the mask leaves, in order, and their count, in list_blocks lists for each sequence (with a mask): one for
+  // each block of rows, the last one for all that follow it too
   const uint32_t* tiles;
   const uint32_t* tile_count;
-  uint32_t tile_stride;
+  uint32_t tile_stride, list_blocks;
   // parts: two for each CTA (of an item begun in an earlier one; of one that goes on in the next)
   float* part;       // [2 x CTAs][rows][D]
   float2* part_ms;   // [2 x CTAs][rows]: maximum (base 2), sum
@@ -84,10 +85,14 @@ __device__ __forceinline__ Both both_parts(float top, float sum, float2 before) 
   return x;
 }
 
+__device__ __forceinline__ uint64_t tile_list(const AttendArgs& a, uint32_t seq, uint32_t rb) {
+  return static_cast<uint64_t>(seq) * a.list_blocks + min(rb, a.list_blocks - 1);
+}
+
 // Tiles of row block rb: those that its last row can see.
 __device__ __forceinline__ uint32_t block_tiles(const AttendArgs& a, const Span& sp, uint32_t rows_per_block, uint32_t rb,
                                                 uint32_t seq) {
-  if (a.tiles) return a.tile_count[seq];
+  if (a.tiles) return a.tile_count[tile_list(a, seq, rb)];
   uint32_t end = sp.length;
   if (a.causal) {
     const uint32_t last = min(sp.count * a.group, (rb + 1) * rows_per_block) - 1;
@@ -100,7 +105,7 @@ __device__ __forceinline__ uint32_t block_tiles(const AttendArgs& a, const Span&
 __device__ __forceinline__ uint64_t sequence_slots(const AttendArgs& a, uint32_t rows_per_block, uint32_t seq, const Span& sp) {
   const uint32_t blocks = (sp.count * a.group + rows_per_block - 1) / rows_per_block;
   uint64_t n = 0;
-  if (a.causal && !a.tiles)
+  if (a.tiles ? a.list_blocks > 1 : a.causal)
     for (uint32_t rb = 0; rb < blocks; ++rb) n += block_tiles(a, sp, rows_per_block, rb, seq) + a.item_slots;
   else if (blocks)
     n = static_cast<uint64_t>(blocks) * (block_tiles(a, sp, rows_per_block, 0, seq) + a.item_slots);

@@ -367,7 +367,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
       uint32_t unit_ahead = 0;
       if (by_row && tiles) {
         words = a.seq_words + static_cast<uint64_t>(min(static_cast<uint32_t>(a.seq_of[it.span.first + token]), b.members - 1)) * a.tile_stride;
-        listed = a.tiles + static_cast<uint64_t>(it.seq) * a.tile_stride + it.lo + from;
+        listed = a.tiles + tile_list(a, it.seq, it.rb) * a.tile_stride + it.lo + from;
         word_ahead = words[listed[0]];
         unit_ahead = tiles > 1 ? listed[step] : 0;
       }
@@ -858,7 +858,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
           uint32_t pos, page;   // the tile's first token; the page of the lane's block of 16, n_pages or above where there is none
           uint32_t see0, see1;  // of tokens pos + lane and pos + 32 + lane
         };
-        const uint32_t* const listed = a.tiles ? a.tiles + static_cast<uint64_t>(it.seq) * a.tile_stride + it.lo : nullptr;
+        const uint32_t* const listed = a.tiles ? a.tiles + tile_list(a, it.seq, it.rb) * a.tile_stride + it.lo : nullptr;
         const auto unit_of = [&](uint32_t j) { return j >= tiles ? ~0u : listed ? __ldg(&listed[j]) : it.lo + j; };
         const auto look = [&](uint32_t unit) {
           Look x{unit == ~0u ? 0u : unit * kTile, ~0u, 0, 0};

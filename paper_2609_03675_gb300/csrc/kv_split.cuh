@@ -224,7 +224,7 @@ __global__ void __launch_bounds__(kSplitThreads<SHORT>, SHORT || (NT == 1 && BIT
       for (int mt = 0; mt < kM; ++mt) x.page[mt] = ~0u;
       if (ch < chunks) {
         const uint32_t t = it.lo + ch / kPerTile;
-        x.pos = (a.tiles ? a.tiles[static_cast<uint64_t>(it.seq) * a.tile_stride + t] : t) * kTile + (ch % kPerTile) * R::kTokens;
+        x.pos = (a.tiles ? a.tiles[tile_list(a, it.seq, it.rb) * a.tile_stride + t] : t) * kTile + (ch % kPerTile) * R::kTokens;
 #pragma unroll
         for (int mt = 0; mt < kM; ++mt)
           if (x.pos + 16 * mt < it.span.length) x.page[mt] = static_cast<uint32_t>(table[(x.pos + 16 * mt) >> b.page_shift]);

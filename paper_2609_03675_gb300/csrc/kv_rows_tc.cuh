@@ -404,6 +404,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
           fence_async_shared();
           warp_arrive(&sm.q_full[t]);
         }
+        bool found = false;  // all rows of the warp have a maximum
 #pragma unroll 1
         for (uint32_t j = 0; j < tiles; ++j, ++s_n) {
           const uint32_t at = n + from + j * step;  // of all tiles
@@ -442,12 +443,13 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
           }
           const uint32_t s_col = s_at(t, s_n) + lanes;
           uint32_t see0 = ~0u, see1 = ~0u;  // the tokens that this row sees
+          bool partly = false;              // some rows of the warp do not see all
           if (!info.plain || (SHARED && by_row)) {
             const int32_t k = seen - info.pos;  // the row sees the first k
             see0 = info.bits[0] & static_cast<uint32_t>(word) & (k >= 32 ? ~0u : k <= 0 ? 0u : (1u << k) - 1);
             see1 = info.bits[1] & static_cast<uint32_t>(word >> 32) & (k >= 64 ? ~0u : k <= 32 ? 0u : (1u << (k - 32)) - 1);
+            partly = !__all_sync(0xffffffffu, (see0 & see1) == ~0u);
           }
-          const bool partly = !__all_sync(0xffffffffu, (see0 & see1) == ~0u);
           uint32_t w[32];
           float here = 0.f;
           if (partly && !__any_sync(0xffffffffu, (see0 | see1) != 0)) {  // a frame that is not these rows' evidence
@@ -469,7 +471,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
                   if (!(see1 & (1u << f))) y[f] = 0xff800000u;
                 }
               }
-              if (again || __any_sync(0xffffffffu, m == -INFINITY && (see0 | see1) != 0)) {
+              if (again || (!found && __any_sync(0xffffffffu, m == -INFINITY && (see0 | see1) != 0))) {
                 const float top = most_of(x, y, -INFINITY) * by;
                 const bool raise = !(here <= kMost) || (m == -INFINITY && top > -INFINITY);
                 const float to = raise ? fmaxf(top, m) : m, k = m == -INFINITY ? 0.f : exp2_fast(m - to);
@@ -490,6 +492,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
                 l *= k;
                 l_rest *= k;
                 m = to;
+                found = __all_sync(0xffffffffu, m != -INFINITY);
               }
               const float down = m == -INFINITY ? 0.f : kUp - m;
               const uint64_t by2 = two(by, by), down2 = two(down, down);

@@ -11,7 +11,6 @@ namespace cofie {
 namespace {
 
 constexpr int kMaskThreads = 1024;
-constexpr uint64_t kShortTokens = 1024;
 
 // The tiles of 64 cached tokens of which the mask leaves one at least, in
 // order, a CTA to a sequence, 1024 tiles at a time: neighbouring lanes look at
@@ -318,11 +317,14 @@ int launch_attend(cofie_kv* h, AttendArgs* a, uint64_t rows, bool shared, cudaSt
   // 394, thirty of 16 over up to 2000 87 / 91 / 97 / 103. Few, with 2 / 4 / 6 / 8 / 12: 24 x 3 tokens over up to 9000 of
   // 4 bits 91 / 79 / 72 / 69 / 62, 64 x 1 over up to 20000 of 4 bits 220 / 212 / 200 / 197 / 199, of 16 bits 419 / 402 /
   // 400 / 394 / 398, 8 x 1 over up to 3000 27 / 25 / 23 / 25 / 25.
-  // Own tokens behind a prefix are few as a rule: up to kShortTokens, as the table's width bounds them, a sequence and key
-  // head are left to one CTA.
+  // Own tokens behind a prefix: a sequence and key head are left to one CTA where its tokens, as the table's width bounds
+  // them, are few, or where there are so many of these items that they fill the GPU uncut. Single tokens, heads of 128 and 16
+  // bits, us cut / uncut: 16 items of 256 tokens 19 / 16, of 1024 20 / 25; 64 of 1024 31 / 30, of 2048 34 / 42; 256 of 2048
+  // 69 / 56, of 8192 154 / 148; 512 of 4096 161 / 140, of 8192 273 / 248; with fewer bits alike.
   int kind = kind_of(h, rows, shared);
   const uint64_t items = static_cast<uint64_t>(a->batch.n_seqs) * a->batch.kv_heads;
-  if (a->behind && kind != kMany && (static_cast<uint64_t>(a->batch.table_stride) << h->page_shift) <= kShortTokens && items <= 0x7fffffffu)
+  const uint64_t width = static_cast<uint64_t>(a->batch.table_stride) << h->page_shift;
+  if (a->behind && kind != kMany && width <= std::min<uint64_t>(8192, std::max<uint64_t>(512, 16 * items)) && items <= 0x7fffffffu)
     kind = kind == kFew8 ? kShort8 : kShort16;
   a->item_slots = kind == kMany ? 8 : 6;
   const AttendLaunch k = kernel_of(h->p, kind, shared);

@@ -47,6 +47,9 @@ __device__ __noinline__ float exact_byte(const T* in, uint32_t d, uint32_t half,
 // lanes of a group find its extremes by shuffles. WIDE: rows are read 16 bytes at a time, and what a
 // value is rotated with lies in as many pieces (sizes and strides that allow
 // it); else value by value.
+// 75264 tokens of 8 heads to bytes: 150 us (154 MB written, 309 read: 68 at DRAM's
+// rate); without the look for bytes that fp32 leaves open 118, with rows asked for
+// only when their places were there 10 more. Issue slots 58 % busy, the ALU pipe 55 %.
 template <typename T, int V, int D, int BITS, bool WIDE>
 __global__ void __launch_bounds__(kThreads, 4) append_codes(const __grid_constant__ CodesArgs a, const __grid_constant__ RotaryTable tab) {
   extern __shared__ __align__(16) float2 cs[];

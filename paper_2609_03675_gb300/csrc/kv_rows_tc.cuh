@@ -23,7 +23,8 @@
 // took 3300 cycles and one of 16-bit values 3400, however few the rows.)
 // The running maximum that exponentials refer to is found at a row's first tokens
 // and raised only when a tile's weights sum to more than their type has room for
-// (then O is brought down in tensor memory), which seldom happens after them. O
+// (then O is brought down in tensor memory), which seldom happens after them
+// (looking for every tile's maximum took 500 cycles of its 1860). O
 // itself is read out and begun anew after some thousands of tokens (kTcChain).
 //
 // Tensor memory: O0 O1 (D columns each) and for each tile two S of 64 columns,
@@ -32,9 +33,17 @@
 // softmax waited 2300 of 5900 cycles for P V and the next Q K^T to be done
 // (256 new tokens over 65792 cached ones of 4 bits: 376 us).
 //
-// For each 256 x 128 block of the scores the tensor core needs 2048 cycles (head
-// of 128), shared memory 2048 for its operands and 512 for writing them, the
-// exponentials 1024 and more.
+// For 256 rows by 64 tokens (head of 128) the tensor core needs 1024 cycles; a
+// tile takes 1900 of 16-bit values and 2490 of bytes. What bounds it is the issue
+// of the eight softmax warps, two to a scheduler (340 instructions a tile each),
+// and of as many that unpack (2900 together): with bytes 6000 warp instructions,
+// 62 % of the issue slots, the ALU pipe 49 %, the tensor pipe 42 % (256 new tokens
+// over 65792, 32 heads over 8: 285 us; 4 bits 265, 16 bits 218). 128 rows or less
+// over 16-bit pages are bound by DRAM: 32 over 262144 tokens 165 us of 158.
+// Tried: a warp for each stream's products instead of one for S and one for O
+// (283, but 230 for 189 where both streams take the same rows); four such warps
+// (305: less registers for the softmax); loops of products (319 for 304: the warp
+// that issues is late); a tile's look-up while the one before is loaded (342).
 #pragma once
 
 #include "kv_split.cuh"

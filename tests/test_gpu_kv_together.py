@@ -154,7 +154,7 @@ def test_own_tokens_of_wide_tables_and_of_narrow_ones():
     for new in ([1, 1, 1], [3, 1, 4]):
         x = Shared("int8", torch.bfloat16, (8, 2, 128), new, [n + 60 * i for i, n in enumerate(new)], [500], [0, 3], 64)
         a = x.check()
-        x.table = torch.nn.functional.pad(x.table, (0, 40)).contiguous()
+        x.table = torch.nn.functional.pad(x.table, (0, 160)).contiguous()
         b = x.check()
         assert torch.allclose(a[0].float(), b[0].float(), rtol=2.0 ** -6, atol=2.0 ** -8) and torch.allclose(a[1], b[1], rtol=2.0 ** -18, atol=2.0 ** -18)
 

@@ -2,10 +2,10 @@
 // products bound it, so both run on tcgen05.
 //
 // A CTA takes up to 256 query rows (new tokens x heads of the group) of one
-// key/value head as two tiles of 128, and the cached tokens 64 at a time. Of an
-// item of 128 rows or less both streams of products and softmax take the same
-// rows, and every other tile of tokens each; their sums are joined with the
-// item's other parts.
+// key/value head as two tiles of 128, and the cached tokens 64 at a time. Of a
+// long item of 128 rows or less both streams of products and softmax take the
+// same rows, and every other tile of tokens each (kTcStreamed); the first joins
+// their sums.
 //   loaders    a warp for keys and one for values, which look up pages and masks
 //              some tiles ahead, tell the others what there is to see, and ask
 //              for the copies: tiles of 16-bit pages by tensor map, with the
@@ -41,7 +41,7 @@
 // over 65792, 32 heads over 8: 285 us; 4 bits 265, 16 bits 218). 128 rows or less
 // over 16-bit pages are bound by DRAM: 32 over 262144 tokens 165 us of 158.
 // Tried: a warp for each stream's products instead of one for S and one for O
-// (283, but 230 for 189 where both streams take the same rows); four such warps
+// (283, but 230 for 199 over 16 bits where both streams take the same rows); four such warps
 // (305: less registers for the softmax); loops of products (319 for 304: the warp
 // that issues is late); a tile's look-up while the one before is loaded (342).
 #pragma once
@@ -59,7 +59,12 @@ constexpr int kTcUnpack = 128;   // of keys, and as many of values
 template <int BITS>
 constexpr int kTcThreads = kTcSoftmax + (BITS < 16 ? 2 * kTcUnpack : 0) + 128;
 constexpr int kTcInfo = 16;         // more than the stages and the raw tiles: a tile is told before its place is free
-constexpr uint32_t kTcStreamed = 4; // tiles from which an item of 128 rows or less is taken by both streams
+// Tiles from which both streams take an item of 128 rows or less: where tiles are unpacked it pays over long caches, and
+// the sums' meeting costs short items more. us, by one stream / by both: 32 answers over 262144 tokens of bytes 263 / 238,
+// of 16 bits 191 / 189; 80 rows over 60000 tokens of 4 bits 224 / 188, of bytes 237 / 233, of 16 bits 181 / 182; over 6000
+// 112 / 115, 130 / 128, 97 / 106; over 2000 28 / 30, 30 / 31, 24 / 26.
+template <int BITS>
+constexpr uint32_t kTcStreamed = BITS < 16 ? 128 : 1024;
 // Tiles whose products are summed in tensor memory before the sums move on to the CTA's part. The tensor core cuts each
 // product off at about 2^-24 of the sum that it is added to, so 8192 tokens may cost a sum 2^-11 of its size, a rounding
 // of fp16, and 65536 tokens 2^-8, one of bf16. (In one sum, 262144 tokens 14 to 17 below a first one came out 0.4 to
@@ -344,7 +349,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
   uint32_t* stop = &sm.stop;
   bool ok = true;
   // whether both streams take the item's rows, every other tile each, and how many tiles of some that makes for a stream
-  const auto streamed = [&](const Item& x) { return x.span.count * a.group - x.rb * kTcRows <= 128 && x.tiles >= kTcStreamed; };
+  const auto streamed = [&](const Item& x) { return x.span.count * a.group - x.rb * kTcRows <= 128 && x.tiles >= kTcStreamed<BITS>; };
   const auto tiles_of = [](bool both, uint32_t t, uint32_t tiles) { return both ? (tiles + 1 - t) / 2 : tiles; };
 
   if (warp < kTcSoftmax / 32) {

@@ -121,7 +121,9 @@ __global__ void __launch_bounds__(kWordThreads) prefix_words(const BatchArg grou
 // rows (the last list: for that block and all after it) the tiles where the
 // union of the sequences that have rows there is not empty, in order: a CTA to a
 // list, 1024 tiles at a time. (By lists of the group alone, blocks of 256 rows of
-// 16 questions that see 0.3 of 400 frames each took 594 us, so 458.)
+// 16 questions that see 0.3 of 400 frames each took 594 us, so 458. With a bit for
+// each half of a block that does not see a tile, whose products are then left out,
+// 478: the count of its tiles that each half needs costs the warps that issue more.)
 __global__ void __launch_bounds__(kMaskThreads) prefix_tiles(const BatchArg groups, const uint64_t* words, uint64_t* any, uint32_t* tiles,
                                                              uint32_t* count, uint32_t tile_stride, const int32_t* seq_of, uint32_t block_rows,
                                                              uint32_t group) {

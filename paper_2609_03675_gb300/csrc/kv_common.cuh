@@ -258,7 +258,11 @@ struct Unpack<__half> {
 
 // Four bytes to (u - 128) s, in their order. s is a power of two, so that all
 // is exact: bf16 holds 128 + the lower seven bits, and the eighth decides
-// whether 128 or 256 comes off; fp16 holds 1024 + u.
+// whether 128 or 256 comes off; fp16 holds 1024 + u. (Two products and a smaller
+// of two in place of the masks are one instruction in five less, but past the
+// type's range for scales of 2^120 and 2^121, and the way round for those cost
+// more than it gave: 256 rows over 65792 tokens 285 -> 274 us, 800 rows 1239 ->
+// 1318, tiles behind a mask 62 -> 70.)
 template <typename T>
 struct Bytes;
 template <>

@@ -471,7 +471,8 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
             for (int f = 0; f < 32; ++f) w[f] = 0;
           } else {
             // The maximum is looked for at a row's first tokens, and when the sum of a tile's weights shows that the one that
-            // they refer to is far behind: then once more from S, which is there until P takes its place.
+            // they refer to is far behind: then once more from S, which is there until P takes its place. (The second 32
+            // columns asked for behind the first, while those are worked on: 256 rows of bytes 285 -> 291 us.)
             for (bool again = false;;) {
               uint32_t x[32], y[32];
               tc_ld32(s_col, x);

@@ -265,6 +265,27 @@ def test_scales_far_apart(dtype, n):
         assert not bool(bad[0].any()) and not bool(bad[1].any()), lo
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("new", [1, 17])
+def test_every_byte_of_every_scale(dtype, d, new):
+    """One cached token to a sequence, which all rows see: its values come out as they are, a weight of one being exact."""
+    lo, hi = (-100, 121) if dtype == torch.bfloat16 else (-24, 9)
+    S, kv = hi - lo + 1, 256 // d
+    c = make(S, 16, kv, kv, d, dtype)
+    u = torch.arange(256).clamp(min=1).view(kv, d).to(torch.uint8)  # a byte of zero stands for no number
+    w = torch.arange(lo + 127, hi + 128) << 7
+    c.k_pages[:, :, 0], c.k_scales[:, :, 0] = 128, 127 << 7
+    c.v_pages[:, :, 0], c.v_scales[:, :, 0] = u.cuda(), w.to(torch.int16).view(S, 1, 1).cuda()
+    table = torch.arange(S, dtype=torch.int32, device="cuda").view(S, 1)
+    q = torch.randn((S * new, kv, d), device="cuda").to(dtype)
+    out, _ = c.attend(q, table, torch.ones(S, dtype=torch.int32, device="cuda"), torch.arange(0, S * new + 1, new, dtype=torch.int32, device="cuda"),
+                      max_new=new, causal=False)
+    c.status()
+    want = numbers(u.expand(S, kv, d), w.view(S, 1, 1).expand(S, kv, d // 64)).to(dtype)
+    assert torch.equal(out.cpu().view(S, new, kv, d), want[:, None].expand(S, new, kv, d))
+
+
 @pytest.mark.parametrize("n", [1, 40])
 def test_pages_past_four_gigabytes(n):
     """The last pages of a pool of over 2^32 bytes: appended to, read, attended to."""

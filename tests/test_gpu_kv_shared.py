@@ -153,6 +153,34 @@ def test_masks(bits, heads, new, own):
 
 
 @pytest.mark.parametrize("bits", BITS)
+@pytest.mark.parametrize("heads", [(8, 1, 128), (16, 2, 64), (7, 1, 128)])
+@pytest.mark.parametrize("new", [[16, 16], [20, 20, 30], [10, 17, 5, 40], [64, 3]])
+def test_evidence_of_one_half_of_a_block(bits, heads, new):
+    """Runs of tiles that only the first or only the second 128 rows of a block see: long ones, every other one, the first
+    of all, and a token whose heads lie in both halves (7 heads); blocks of their last rows alone."""
+    S, width = len(new), 6001
+    at = torch.arange(width)
+    for run in (64, 192, 3000):
+        for turn in (0, 1):
+            pm = torch.stack([(at // run + turn) % S == s for s in range(S)])
+            pm[:, 4000:4100] = False
+            x = Shared(bits, torch.bfloat16, heads, new, new, [width], [0, S], 64, seed=run, prefix_mask=pm)
+            x.check()
+    y = Shared(bits, torch.float16, heads, new + new, new + new, [width, 700], [0, S, 2 * S], 32, prefix_mask=torch.cat([pm, ~pm]))
+    y.check()
+    y.check(max_shared=20)  # lists of the first block stand for those after it
+
+
+def test_masked_sums_that_outlast_tensor_memory():
+    """fp16 sums that leave tensor memory after 128 tiles, of which either half of a block's rows sees others."""
+    G, width = 10, 12801  # 160 items of 201 tiles over 152 CTAs
+    at = torch.arange(width)
+    pm = torch.stack([at % 640 >= 192, at % 640 < 512])
+    x = Shared(16, torch.float16, (128, 16, 64), [16, 16] * G, [16, 17] * G, [width] * G, list(range(0, 2 * G + 1, 2)), 64, prefix_mask=pm.repeat(G, 1))
+    x.check()
+
+
+@pytest.mark.parametrize("bits", BITS)
 @pytest.mark.parametrize("n", [1, 9, 40])
 def test_a_prefix_alone_and_none_at_all(bits, n):
     """One group of all without offsets; prefixes of no tokens give what attend gives, to the bit."""

@@ -360,6 +360,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
     const uint32_t o_col = o_at(t) + lanes;
     const float by = a.scale * 1.4426950408889634f;
     uint32_t n = 0, s_n = 0;  // tiles told; tiles of this stream
+    bool kept_alone = false;  // an item of this CTA's own had sums kept in the part of the one that goes on
     while (walk.next(it)) {  // to the end even when a wait ran out: the barriers below count on all
       const bool both = streamed(it);
       const uint32_t row0 = it.rb * kTcRows + (both ? 0 : t * 128), all = it.span.count * a.group;
@@ -577,7 +578,10 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
       const bool alone = it.first_cta == it.last_cta;
       if (threadIdx.x == 0 && it.first_cta == blockIdx.x && !alone) a.items[blockIdx.x] = {it.seq, it.rb, it.head, it.last_cta, it.span};
       const uint64_t part = own_part();
-      if (told > kTcChain<T> && !alone) bar_sync<1, kTcSoftmax>();  // all have what they kept, before the part is written
+      // All have what they kept, of this item or of one before it, before the part is written: its rows lie across what other
+      // threads keep, and a stream that the last item has no rows for may be an item behind.
+      if (!alone && (kept_alone || told > kTcChain<T>)) bar_sync<1, kTcSoftmax>();
+      kept_alone = kept_alone || (alone && told > kTcChain<T>);
       // Both streams' sums of the same rows: the second's go to the first through Q's place, once all products are done.
       float k0 = 1.f, k1 = 0.f;
       float4* const across = reinterpret_cast<float4*>(sm.q[0]);  // [D / 4][128]

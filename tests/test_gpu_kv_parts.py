@@ -1,0 +1,64 @@
+"""Attention of many rows where a CTA works off an item of its own, whose sums outlast tensor memory and are kept in the CTA's
+part, and then begins one that goes on into the next CTA, whose part lies in the same place."""
+import pytest
+import torch
+
+from tests import kv_bounds as B
+
+pytestmark = pytest.mark.gpu
+
+CHAIN = {torch.float16: 128, torch.bfloat16: 1024}  # tiles of 64 tokens that tensor memory sums
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _cuda():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+
+
+def pairs(ctas, seqs, new, m, kv, group, chain):
+    """The walk of the items over the CTAs: (rows of the second item, its tiles here) wherever one with kept sums and more
+    than 128 rows comes before one that goes on and that nothing else orders after it."""
+    items = []
+    for _ in range(seqs):
+        rows = new * group
+        for at in range(0, rows, 256):
+            end = min(rows, at + 256)
+            items += [(end - at, -(-(m - new + (end - 1) // group + 1) // 64))] * kv
+    size = -(-sum(8 + t for _, t in items) // ctas)
+    found, kept, at = [], set(), 0
+    for rows, tiles in items:
+        first, past = (at + 8) // size, (at + 8 + tiles - 1) // size
+        here = min(at + 8 + tiles, (first + 1) * size) - (at + 8)
+        if first == past and tiles > chain and rows > 128:
+            kept.add(first)
+        if first != past and first in kept and here <= chain:
+            found.append((rows, here))
+        at += 8 + tiles
+    return found
+
+
+@pytest.mark.parametrize("bits,dtype,seqs,new,m,kv,group", [(16, torch.float16, 40, 300, 9000, 2, 1), ("int8", torch.float16, 40, 75, 9000, 2, 4),
+                                                           (4, torch.float16, 60, 300, 12800, 2, 1), (16, torch.bfloat16, 80, 130, 66000, 2, 1)])
+def test_kept_sums_before_an_item_that_goes_on(bits, dtype, seqs, new, m, kv, group):
+    """The sequences share their pages and queries; all of them against the one definition."""
+    from paper_2609_03675_gb300 import KVCache
+    d, page, h = 64, 64, kv * group
+    ctas = torch.cuda.get_device_properties(0).multi_processor_count
+    assert pairs(ctas, seqs, new, m, kv, group, CHAIN[dtype])
+    g = torch.Generator().manual_seed(new)
+    n_pages = -(-m // page)
+    cache = KVCache(n_pages, page, h, kv, d, dtype=dtype, bits=bits)
+    k, v = (torch.randn((m, kv, d), generator=g).to(dtype).cuda() for _ in range(2))
+    one = torch.arange(n_pages, dtype=torch.int32, device="cuda").view(1, -1)
+    all_of, offsets = torch.tensor([m], dtype=torch.int32, device="cuda"), torch.tensor([0, m], dtype=torch.int32, device="cuda")
+    cache.append(k, v, one, all_of, offsets)
+    k, v = cache.read(one, all_of, offsets, n_tokens=m)
+    q = torch.randn((new, h, d), generator=g).to(dtype)
+    out, lse = cache.attend(q.cuda().repeat(seqs, 1, 1), one.repeat(seqs, 1), all_of.repeat(seqs),
+                            torch.arange(seqs + 1, dtype=torch.int32, device="cuda") * new, max_new=new)
+    cache.status()
+    seen = torch.arange(m)[None] <= (m - new + torch.arange(new))[:, None]
+    want = B.attend(q, k, v, seen, d ** -0.5, dtype)
+    bad = B.exceeds(out.view(seqs, new, h, d), lse.view(seqs, new, h), want)
+    assert not bool(bad[0].any()) and not bool(bad[1].any())

@@ -874,27 +874,28 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
           all_see = x > 0 ? static_cast<int32_t>(x) : 0;
         }
         // A tile takes two loads one after the other where there is a mask (its number, then pages and mask): numbers are
-        // asked for three tiles ahead and the others two, so that nobody waits for them.
+        // asked for three tiles ahead and the others two, so that nobody waits for them. (Common loads, not those of constant
+        // data: this kernel is resident while the one before writes the list, or the caller's mask.)
         const uint32_t flags = (streamed(it) ? kTcBoth : 0) | (it.span.count * a.group - it.rb * kTcRows > 128 ? kTcSecond : 0);
         struct Look {
           uint32_t pos, page;   // the tile's first token; the page of the lane's block of 16, n_pages or above where there is none
           uint32_t see0, see1;  // of tokens pos + lane and pos + 32 + lane
         };
         const uint32_t* const listed = a.tiles ? a.tiles + tile_list(a, it.seq, it.rb) * a.tile_stride + it.lo : nullptr;
-        const auto unit_of = [&](uint32_t j) { return j >= tiles ? ~0u : listed ? __ldg(&listed[j]) : it.lo + j; };
+        const auto unit_of = [&](uint32_t j) { return j >= tiles ? ~0u : listed ? listed[j] : it.lo + j; };
         const auto look = [&](uint32_t unit) {
           Look x{unit == ~0u ? 0u : unit * kTile, ~0u, 0, 0};
           if (unit == ~0u) return x;
           const uint32_t p = x.pos + 16 * block, p0 = x.pos + lane, p1 = p0 + 32;
-          if (p < length) x.page = static_cast<uint32_t>(__ldg(&table[p >> shift]));
+          if (p < length) x.page = static_cast<uint32_t>(table[p >> shift]);
           if (SHARED && a.seq_words) {
             const uint64_t word = a.any_words[static_cast<uint64_t>(it.seq) * a.tile_stride + unit];
             x.see0 = p0 < length ? static_cast<uint32_t>(word >> lane) & 1u : 0u;
             x.see1 = p1 < length ? static_cast<uint32_t>(word >> 32 >> lane) & 1u : 0u;
           } else if (a.mask) {
             const uint8_t* mask = a.mask + it.seq * a.mask_stride;
-            x.see0 = p0 < length && p0 < a.mask_stride ? __ldg(&mask[p0]) : 0u;
-            x.see1 = p1 < length && p1 < a.mask_stride ? __ldg(&mask[p1]) : 0u;
+            x.see0 = p0 < length && p0 < a.mask_stride ? mask[p0] : 0u;
+            x.see1 = p1 < length && p1 < a.mask_stride ? mask[p1] : 0u;
           } else {
             x.see0 = p0 < length;
             x.see1 = p1 < length;

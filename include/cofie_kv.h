@@ -191,7 +191,7 @@ int cofie_kv_read(cofie_kv_t* h, const cofie_kv_batch* b, void* k_out, void* v_o
  *   out = sum_j p_j v_j, p = softmax_j(scale <q, k_j>), lse = ln sum_j exp(scale <q, k_j>)
  * Products are of 16-bit numbers, sums in fp32. The weights exp(scale <q, k_j>)
  * are rounded to 16 bits for their product with the values (to the cache's type,
- * of up to 2^8, or 2^15 for fp16; for few rows over pages of 8 bits (16) or 4 (32)
+ * of up to 1, or 2^15 for fp16; for few rows over pages of 8 bits (16) or 4 (32)
  * to fp16, times the values' scale) and not for lse; over such pages such rows'
  * queries are taken to fp16 with a power of two for each row, which is meant for
  * queries below 2^110. out is rounded to the cache's type. A row that sees nothing gets

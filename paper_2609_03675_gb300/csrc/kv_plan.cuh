@@ -46,11 +46,11 @@ struct AttendArgs {
   uint32_t tile_stride, list_blocks;
   // parts: two for each CTA (of an item begun in an earlier one; of one that goes on in the next)
   float* part;       // [2 x CTAs][rows][D]
-  float2* part_ms;   // [2 x CTAs][rows]: maximum (base 2), sum
+  float2* part_ms;   // [2 x CTAs][rows]: what exponentials refer to (base 2; the maximum, or a few powers off), sum
   uint32_t* done;    // [CTAs]: parts finished of the item that goes on from this CTA; zero between calls
   SplitItem* items;  // [CTAs], many rows: last_cta is that CTA at most where none goes on
   // Sequences behind a shared prefix take two launches. The first has the groups as its batch, each of them one sequence of
-  // all its rows over the prefix, and leaves sums [tokens][heads][D] with the maximum (base 2) and the sum of the weights;
+  // all its rows over the prefix, and leaves sums [tokens][heads][D] with what exponentials refer to (base 2) and the sum of the weights;
   // the second has the sequences, and adds what it finds there. `prefix`: the first launch's batch, for the second.
   float* rows;
   float2* rows_ms;

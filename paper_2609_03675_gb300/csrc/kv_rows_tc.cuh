@@ -294,11 +294,13 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
   using S = TcSmem<D, BITS, SHARED>;
   constexpr uint32_t kStages = S::kStages, kRaw = S::kRaw;
   constexpr int kThreads = kTcThreads<BITS>;
-  // fp16: weights are 2^7 times what they stand for, so that only those under 2^-32 of the largest are lost to the second
-  // product. A tile's 64 sum to 2^13 where all are as large as the maximum that they refer to; up to 2^15, which fp16 holds,
-  // it may be behind. (bf16 has the exponents of fp32: up to 2^8 leaves sums of values of 2^119 in range.)
+  // What exponentials refer to (m below, in the parts too) is kUp below the maximum, so that weights are 2^kUp times what
+  // they stand for, and a tile's 64 sum to 2^(kUp + 6) where all are as large as the maximum; it is raised where they pass
+  // kMost. fp16: 2^7, so that only weights under 2^-32 of the largest are lost to the second product, and up to 2^15, which
+  // fp16 holds. bf16 has the exponents of fp32: 2^-8 and up to 1, so that a weight times a value stays in range where the
+  // value is (with weights of 1 and up to 2^8, a token 2^7 heavier than all before and its value of 2^121 gave infinity).
   constexpr bool kHalf = std::is_same<T, __half>::value;
-  constexpr float kMost = kHalf ? 0x1p15f : 0x1p8f, kUp = kHalf ? 7.f : 0.f, kDown = kHalf ? 0x1p-7f : 1.f;
+  constexpr float kMost = kHalf ? 0x1p15f : 1.f, kUp = kHalf ? 7.f : -8.f;
   extern __shared__ char raw[];
   S& sm = *reinterpret_cast<S*>(raw + (1024u - (shared_address(raw) & 1023u)) % 1024u);
   pdl_trigger();
@@ -490,7 +492,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
               if (again || (!found && __any_sync(0xffffffffu, m == -INFINITY && (see0 | see1) != 0))) {
                 const float top = most_of(x, y, -INFINITY) * by;
                 const bool raise = !(here <= kMost) || (m == -INFINITY && top > -INFINITY);
-                const float to = raise ? fmaxf(top, m) : m, k = m == -INFINITY ? 0.f : exp2_fast(m - to);
+                const float to = raise ? fmaxf(top - kUp, m) : m, k = m == -INFINITY ? 0.f : exp2_fast(m - to);
                 if (j % kTcChain<T> != 0) {  // O as it is after the tokens before
                   ok = tc_wait(&sm.o_full[t][(s_n - 1) % 2], (s_n - 1) / 2, stop);
                   ok = __all_sync(0xffffffffu, ok);
@@ -510,7 +512,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
                 m = to;
                 found = __all_sync(0xffffffffu, m != -INFINITY);
               }
-              const float down = m == -INFINITY ? 0.f : kUp - m;
+              const float down = m == -INFINITY ? 0.f : -m;
               const uint64_t by2 = two(by, by), down2 = two(down, down);
               uint64_t l2 = two(0.f, 0.f), l3 = two(0.f, 0.f);
               const auto exponentials = [&](const uint32_t* z, uint32_t* w) {
@@ -614,10 +616,10 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
         }
       }
       Both w2{};
-      if (SHARED && alone && before && real) w2 = both_parts(m, l * kDown, a.rows_ms[shared_row]);
+      if (SHARED && alone && before && real) w2 = both_parts(m, l, a.rows_ms[shared_row]);
       const bool add = SHARED && alone && before;
       // what comes before the rounding: out of the sums here, and out of the prefix's
-      const float inv_own = add ? (w2.sum == 0.f ? 0.f : w2.own * kDown / w2.sum) : l == 0.f ? 0.f : 1.f / l;
+      const float inv_own = add ? (w2.sum == 0.f ? 0.f : w2.own / w2.sum) : l == 0.f ? 0.f : 1.f / l;
       const float inv_prefix = add && w2.sum != 0.f ? w2.prefix / w2.sum : 0.f;
       T* out = reinterpret_cast<T*>(a.q.out) + static_cast<int64_t>(it.span.first + token) * a.q.out_token +
                static_cast<int64_t>(head) * a.q.out_head;
@@ -658,8 +660,8 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
                 *reinterpret_cast<float4*>(to + 4) = make_float4(z[4], z[5], z[6], z[7]);
               } else if (SHARED && !a.behind) {
                 float* to = a.rows + shared_row * D + d;
-                *reinterpret_cast<float4*>(to) = make_float4(z[0] * kDown, z[1] * kDown, z[2] * kDown, z[3] * kDown);
-                *reinterpret_cast<float4*>(to + 4) = make_float4(z[4] * kDown, z[5] * kDown, z[6] * kDown, z[7] * kDown);
+                *reinterpret_cast<float4*>(to) = make_float4(z[0], z[1], z[2], z[3]);
+                *reinterpret_cast<float4*>(to + 4) = make_float4(z[4], z[5], z[6], z[7]);
               } else {
                 if (SHARED && add) {
                   const float* from = a.rows + shared_row * D + d;
@@ -684,10 +686,10 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
         }
         if (real) {
           if (!alone) a.part_ms[part + lr] = make_float2(m, l);
-          else if (SHARED && !a.behind) a.rows_ms[shared_row] = make_float2(m, l * kDown);
+          else if (SHARED && !a.behind) a.rows_ms[shared_row] = make_float2(m, l);
           else if (SHARED && add) {
             if (a.lse) a.lse[shared_row] = (w2.top + log2f(w2.sum)) * 0.6931471805599453f;
-          } else if (a.lse) a.lse[static_cast<uint64_t>(it.span.first + token) * a.heads + head] = (m + log2f(l * kDown)) * 0.6931471805599453f;
+          } else if (a.lse) a.lse[static_cast<uint64_t>(it.span.first + token) * a.heads + head] = (m + log2f(l)) * 0.6931471805599453f;
         }
       }
       tc_fence_before();  // O is read before the next item's products are let through (by q_full)
@@ -1006,7 +1008,6 @@ constexpr uint32_t kJoinRows = kJoinThreads / (D / 4);
 template <typename T, int D, bool SHARED>
 __global__ void __launch_bounds__(kJoinThreads) attend_join(const __grid_constant__ AttendArgs a) {
   using P = Pair<T>;
-  constexpr float kDown = std::is_same<T, __half>::value ? 0x1p-7f : 1.f;  // as above
   constexpr uint32_t kLanes = D / 4;
   pdl_trigger();
   pdl_wait();
@@ -1043,19 +1044,18 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join(const __grid_constan
   if (!real) return;
   const uint32_t token = it.span.first + (it.rb * kManyRows + row) / a.group, head = it.head * a.group + (it.rb * kManyRows + row) % a.group;
   const uint64_t at = static_cast<uint64_t>(token) * a.heads + head;
-  float by = sum == 0.f ? 0.f : 1.f / sum, lse = top + log2f(sum * kDown);
+  float by = sum == 0.f ? 0.f : 1.f / sum, lse = top + log2f(sum);
   if constexpr (SHARED) {
     float4* const there = reinterpret_cast<float4*>(a.rows + at * D) + lane;
     if (!a.behind) {
-      *there = make_float4(y.x * kDown, y.y * kDown, y.z * kDown, y.w * kDown);
-      if (lane == 0) a.rows_ms[at] = make_float2(top, sum * kDown);
+      *there = y;
+      if (lane == 0) a.rows_ms[at] = make_float2(top, sum);
       return;
     }
     if (has_prefix(a, it.seq)) {
-      const Both w = both_parts(top, sum * kDown, a.rows_ms[at]);
+      const Both w = both_parts(top, sum, a.rows_ms[at]);
       const float4 z = *there;
-      const float own = w.own * kDown;
-      y = make_float4(own * y.x + w.prefix * z.x, own * y.y + w.prefix * z.y, own * y.z + w.prefix * z.z, own * y.w + w.prefix * z.w);
+      y = make_float4(w.own * y.x + w.prefix * z.x, w.own * y.y + w.prefix * z.y, w.own * y.z + w.prefix * z.z, w.own * y.w + w.prefix * z.w);
       by = w.sum == 0.f ? 0.f : 1.f / w.sum;
       lse = w.top + log2f(w.sum);
     }

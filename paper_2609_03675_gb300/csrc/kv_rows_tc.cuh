@@ -296,11 +296,11 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
   constexpr int kThreads = kTcThreads<BITS>;
   // What exponentials refer to (m below, in the parts too) is kUp below the maximum, so that weights are 2^kUp times what
   // they stand for, and a tile's 64 sum to 2^(kUp + 6) where all are as large as the maximum; it is raised where they pass
-  // kMost. fp16: 2^7, so that only weights under 2^-32 of the largest are lost to the second product, and up to 2^15, which
-  // fp16 holds. bf16 has the exponents of fp32: 2^-8 and up to 1, so that a weight times a value stays in range where the
+  // kMost. fp16: 2^8, so that only weights under 2^-33 of the largest are lost to the second product, as for few rows, and up
+  // to 2^15, which fp16 holds. bf16 has the exponents of fp32: 2^-8 and up to 1, so that a weight times a value stays in range where the
   // value is (with weights of 1 and up to 2^8, a token 2^7 heavier than all before and its value of 2^121 gave infinity).
   constexpr bool kHalf = std::is_same<T, __half>::value;
-  constexpr float kMost = kHalf ? 0x1p15f : 1.f, kUp = kHalf ? 7.f : -8.f;
+  constexpr float kMost = kHalf ? 0x1p15f : 1.f, kUp = kHalf ? 8.f : -8.f;
   extern __shared__ char raw[];
   S& sm = *reinterpret_cast<S*>(raw + (1024u - (shared_address(raw) & 1023u)) % 1024u);
   pdl_trigger();

@@ -105,3 +105,19 @@ def test_maxima_that_rise_from_tile_to_tile(dtype, rows):
         n, scale = rows // 4, 0.6931471805599453
         bad = B.exceeds(*_many(cache, q, table, m, scale), B.attend(q, kh, vh, torch.ones((n, m), dtype=torch.bool), scale, dtype))
         assert not bool(bad[0].any()) and not bool(bad[1].any()), rise
+
+
+@pytest.mark.parametrize("rows", [4, 16, 20, 32, 40, 200])
+def test_the_lightest_weights_that_fp16_holds(rows):
+    """fp16, 16-bit pages: weights of 2^-32.375 of the largest, whose token has no value, so that the output is theirs. With
+    the largest at 2^8 they are 2^-24.375, off by half a spacing of the smallest numbers at most: 2^-33 of the largest each.
+    (With it at 2^7 they are under half of the smallest number, and nothing.)"""
+    d, m, value = 64, 4096, 1024.0
+    k, v = torch.zeros((m, 1, d)), torch.full((m, 1, d), value)
+    k[0, 0, 0], v[0] = 32.375, 0.0
+    cache, table, _, _ = _cache(16, k.half(), v.half(), 4)
+    q = torch.zeros((rows // 4, 4, d), dtype=torch.float16)
+    q[..., 0] = 1.0
+    out, lse = _many(cache, q, table, m, 0.6931471805599453)
+    want = (m - 1) * value * 2.0 ** -32.375
+    assert bool(((out.double().cpu() - want).abs() <= (m - 1) * value * 2.0 ** -33 + 2.0 ** -11 * want).all())

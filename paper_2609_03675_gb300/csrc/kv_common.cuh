@@ -25,7 +25,8 @@ constexpr uint32_t kKvErrPage = 1u, kKvErrBatch = 2u, kKvErrWait = 4u;
 struct RotaryTable {
   uint64_t turn[kMaxPairs];  // turns per position, as a fraction of 2^64
   uint8_t axis[kMaxPairs];
-  float amplitude;
+  double exact_amplitude;
+  float amplitude;  // rounded
   uint32_t half;    // pairs
   uint32_t layout;  // COFIE_ROTARY_*
 };

@@ -32,7 +32,7 @@ __device__ __forceinline__ float code_back(float code, float zero, float x, floa
 // Value d of a head, turned in 64 bits, as a byte's sum (see below): for the few
 // that lie closer to a half than fp32 tells.
 template <typename T>
-__device__ __noinline__ float exact_byte(const T* in, uint32_t d, uint32_t half, bool by_half, uint64_t turn, int32_t pos, float amplitude, float inverse) {
+__device__ __noinline__ float exact_byte(const T* in, uint32_t d, uint32_t half, bool by_half, uint64_t turn, int32_t pos, double amplitude, float inverse) {
   const bool second = by_half ? d >= half : d & 1;
   const double x = Elem<T>::to(in[d]), y = Elem<T>::to(in[by_half ? (second ? d - half : d + half) : d ^ 1]);
   double s, c;
@@ -164,7 +164,8 @@ __global__ void __launch_bounds__(kThreads, 4) append_codes(const __grid_constan
         // 1.5 2^23 + 128 more rounds it to a whole number, halves to even, whose byte is the low one. A rotated key is off by
         // 2.8e-7 (|x| + |y|) of its pair (angle 9.4e-8, cos and sin 6e-8, products and sum 1.2e-7), so by 5.6e-7 of the
         // largest turned value of the pair at most: one that lies so close to a half is turned once more in 64 bits. (One in
-        // 10^4; without that one in 3 10^5 bytes of rotated keys was its neighbour.)
+        // 10^4; without that one in 3 10^5 bytes of rotated keys was its neighbour.) An amplitude adds its own rounding and that
+        // of its products with cos and sin, 6e-8 each of the pair's length, which is sqrt 2 times the largest at most: 1.7e-7.
         float size[2] = {0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < 16; ++i) size[kOwn == 1 ? 0 : i / 8] = max_nan(size[kOwn == 1 ? 0 : i / 8], fabsf(x[i]));
@@ -188,7 +189,7 @@ __global__ void __launch_bounds__(kThreads, 4) append_codes(const __grid_constan
 #pragma unroll
             for (int i = 0; i < 8; ++i)
               near = fmaxf(near, fabsf(__fmaf_rn(x[8 * e + i], inverse[gr], 12583040.f - __uint_as_float(u[i]))));
-            const float off = 6e-7f * reach * inverse[gr];
+            const float off = (tab.amplitude == 1.f ? 6e-7f : 8e-7f) * reach * inverse[gr];
             if (p >= 0 && near > 0.5f - off) {
               const T* in = in0 + t * in_token;
               uint32_t close = 0;
@@ -201,7 +202,7 @@ __global__ void __launch_bounds__(kThreads, 4) append_codes(const __grid_constan
                 if (d >= turned) break;
                 const uint32_t pair = by_half ? (d >= tab.half ? d - tab.half : d) : d / 2;
                 const int32_t pos = r.positions[static_cast<uint64_t>(tab.axis[pair]) * r.n_tokens + t0 + t];
-                const float exact = exact_byte(in, d, tab.half, by_half, tab.turn[pair], pos, tab.amplitude, inverse[gr]);
+                const float exact = exact_byte(in, d, tab.half, by_half, tab.turn[pair], pos, tab.exact_amplitude, inverse[gr]);
 #pragma unroll
                 for (uint32_t f = 0; f < 8; ++f)
                   if (f == i) u[f] = __float_as_uint(exact);

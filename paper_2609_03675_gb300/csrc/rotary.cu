@@ -107,6 +107,7 @@ int cofie_rotary_create(const cofie_rotary_params* p, cofie_rotary_t** out) {
   RotaryTable& t = h->table;
   t.half = half;
   t.layout = p->layout;
+  t.exact_amplitude = m;
   t.amplitude = static_cast<float>(m);
   for (uint32_t i = 0; i < half; ++i) {
     double f = std::pow(base, -2.0 * i / p->rotary_dim);

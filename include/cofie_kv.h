@@ -238,9 +238,10 @@ typedef struct {
  * lse = -infinity. (A NaN or an infinity among the values of a prefix may reach
  * the rows of every sequence of the group, those that do not see it too, unless
  * none does.)
- * May be captured, except for the first call of more tokens, or with a
- * prefix mask of a larger size, than any before, which grows the handle's
- * scratch (n_tokens x n_heads x (4 head_dim + 8) bytes).
+ * May be captured, except for the first call of more tokens, or with a mask
+ * or a prefix mask of a larger size, than any before, which grows the handle's
+ * scratch (n_tokens x n_heads x (4 head_dim + 8) bytes). A call that is refused
+ * or finds no memory has launched nothing.
  */
 int cofie_kv_attend_shared(cofie_kv_t* h, const cofie_kv_batch* b, const cofie_kv_prefix* prefix, const cofie_rows* q,
                            float* lse, const uint8_t* mask, uint64_t mask_stride, int causal, float scale, void* cuda_stream);

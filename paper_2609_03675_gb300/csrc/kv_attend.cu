@@ -272,8 +272,9 @@ bool may_allocate(cudaStream_t st) {
   return ok;
 }
 
-// The tiles that the batch's mask leaves; a.tiles and what goes with it.
-int list_tiles(cofie_kv* h, const cofie_kv_batch* b, AttendArgs* args, cudaStream_t st) {
+// Room for the tiles that the batch's mask leaves; a.tiles and what goes with it. A call finds the room for all that it needs
+// before its first launch, so that one that is refused has launched nothing.
+int room_for_tiles(cofie_kv* h, const cofie_kv_batch* b, AttendArgs* args, cudaStream_t st) {
   AttendArgs& a = *args;
   a.tile_stride = (b->table_stride << h->page_shift) / kTile + 1;
   a.list_blocks = 1;
@@ -293,9 +294,14 @@ int list_tiles(cofie_kv* h, const cofie_kv_batch* b, AttendArgs* args, cudaStrea
   }
   a.tiles = h->d_tiles;
   a.tile_count = h->d_tiles + static_cast<size_t>(b->n_seqs) * a.tile_stride;
+  return COFIE_OK;
+}
+
+// Those tiles.
+int list_tiles(cofie_kv* h, const cofie_kv_batch* b, const AttendArgs& a, cudaStream_t st) {
   const uintptr_t at = reinterpret_cast<uintptr_t>(a.mask) | (b->n_seqs > 1 ? a.mask_stride : 0);
   const auto find = at % 16 == 0 ? visible_tiles<uint4> : at % 4 == 0 ? visible_tiles<uint32_t> : visible_tiles<uint8_t>;
-  return launched(h, launch_dependent(true, find, dim3(b->n_seqs), dim3(kMaskThreads), 0, st, a.batch, a.mask, a.mask_stride, h->d_tiles,
+  return launched(h, launch_dependent(true, find, dim3(b->n_seqs), dim3(kMaskThreads), 0, st, a.batch, a.mask, a.mask_stride, const_cast<uint32_t*>(a.tiles),
                                       const_cast<uint32_t*>(a.tile_count), a.tile_stride),
                   "attend");
 }
@@ -357,13 +363,20 @@ int scratch(cofie_kv* h, cofie_kv::Scratch* s, size_t need, cudaStream_t st) {
   return COFIE_OK;
 }
 
-// The mask of the prefixes: words, their union, the tiles that it leaves, and each token's sequence, one behind the other.
-int prefix_mask(cofie_kv* h, const cofie_kv_prefix* p, AttendArgs* args, uint64_t rows, cudaStream_t st) {
+// The rows of one block of the kernel for so many.
+uint32_t block_rows_of(const cofie_kv* h, uint64_t rows) {
+  const int kind = kind_of(h, rows, true);
+  return kind == kMany ? kManyRows : kind == kFew16 ? 16u : 8u;
+}
+
+// Room for the mask of the prefixes: words, their union, the tiles that it leaves, and each token's sequence, one behind the
+// other.
+int room_for_prefix_mask(cofie_kv* h, AttendArgs* args, uint64_t rows, cudaStream_t st) {
   AttendArgs& a = *args;
   const BatchArg& g = a.batch;
   a.tile_stride = (g.table_stride << h->page_shift) / kTile + 1;
   // lists for so many rows of a group; 256 of them at most, and with many groups one each
-  const uint32_t block_rows = kind_of(h, rows, true) == kMany ? kManyRows : kind_of(h, rows, true) == kFew16 ? 16u : 8u;
+  const uint32_t block_rows = block_rows_of(h, rows);
   a.list_blocks = g.n_seqs > 256 ? 1u : static_cast<uint32_t>(std::min<uint64_t>((rows + block_rows - 1) / block_rows, 256 / g.n_seqs));
   const size_t seqs = g.members, groups = g.n_seqs, stride = a.tile_stride, lists = groups * a.list_blocks;
   const size_t words = (seqs + groups) * stride * sizeof(uint64_t), tiles = lists * (stride + 1) * sizeof(uint32_t);
@@ -378,6 +391,15 @@ int prefix_mask(cofie_kv* h, const cofie_kv_prefix* p, AttendArgs* args, uint64_
   a.tiles = list;
   a.tile_count = list + lists * stride;
   a.seq_of = seq_of;
+  return COFIE_OK;
+}
+
+// That mask.
+int prefix_mask(cofie_kv* h, const cofie_kv_prefix* p, const AttendArgs& a, uint64_t rows, cudaStream_t st) {
+  const BatchArg& g = a.batch;
+  const size_t seqs = g.members;
+  uint64_t* const seq_words = const_cast<uint64_t*>(a.seq_words);
+  int32_t* const seq_of = const_cast<int32_t*>(a.seq_of);
   const bool wide = reinterpret_cast<uintptr_t>(p->mask) % 16 == 0 && (seqs == 1 || p->mask_stride % 16 == 0);
   const dim3 grid(std::max(1u, std::min((a.tile_stride + kWordThreads - 1) / kWordThreads, 64u)), std::min(g.members, 65535u));
   if (const int rc = launched(h, launch_dependent(true, wide ? prefix_words<true> : prefix_words<false>, grid, dim3(kWordThreads), 0, st, g, p->mask,
@@ -385,8 +407,8 @@ int prefix_mask(cofie_kv* h, const cofie_kv_prefix* p, AttendArgs* args, uint64_
                               "attend"))
     return rc;
   return launched(h, launch_dependent(true, prefix_tiles, dim3(g.n_seqs, a.list_blocks), dim3(kMaskThreads), 0, st, g,
-                                      static_cast<const uint64_t*>(seq_words), any, list, list + lists * stride, a.tile_stride,
-                                      static_cast<const int32_t*>(seq_of), block_rows, a.group),
+                                      a.seq_words, const_cast<uint64_t*>(a.any_words), const_cast<uint32_t*>(a.tiles),
+                                      const_cast<uint32_t*>(a.tile_count), a.tile_stride, a.seq_of, block_rows_of(h, rows), a.group),
                   "attend");
 }
 
@@ -404,8 +426,10 @@ extern "C" int cofie_kv_attend(cofie_kv_t* h, const cofie_kv_batch* b, const cof
   if (const int rc = attend_args(h, b, q, lse, mask, mask_stride, causal, scale, &a)) return rc;
   DeviceGuard g(h->device);
   cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-  if (mask)
-    if (const int rc = list_tiles(h, b, &a, st)) return rc;
+  if (mask) {
+    if (const int rc = room_for_tiles(h, b, &a, st)) return rc;
+    if (const int rc = list_tiles(h, b, a, st)) return rc;
+  }
   return launch_attend(h, &a, rows_at_most(b, a.group), false, st);
 }
 
@@ -441,11 +465,15 @@ extern "C" int cofie_kv_attend_shared(cofie_kv_t* h, const cofie_kv_batch* b, co
   first.lse = nullptr;
   first.causal = 0;
   const uint64_t most = prefix->max_new ? prefix->max_new : b->n_tokens;
-  if (prefix->mask)
-    if (const int rc = prefix_mask(h, prefix, &first, most * own.group, st)) return rc;
+  if (mask)
+    if (const int rc = room_for_tiles(h, b, &own, st)) return rc;
+  if (prefix->mask) {
+    if (const int rc = room_for_prefix_mask(h, &first, most * own.group, st)) return rc;
+    if (const int rc = prefix_mask(h, prefix, first, most * own.group, st)) return rc;
+  }
   if (const int rc = launch_attend(h, &first, most * own.group, true, st)) return rc;
   own.behind = 1;
   if (mask)
-    if (const int rc = list_tiles(h, b, &own, st)) return rc;
+    if (const int rc = list_tiles(h, b, own, st)) return rc;
   return launch_attend(h, &own, rows_at_most(b, own.group), true, st);
 }

@@ -1,5 +1,7 @@
 """Calls one behind the other, none of them waited for: each reads the lists, tables and masks that were written just before
 it, not what its predecessor found at the same addresses."""
+import gc
+
 import pytest
 import torch
 
@@ -10,6 +12,14 @@ pytestmark = pytest.mark.gpu
 def _cuda():
     if not torch.cuda.is_available():
         pytest.skip("no CUDA device")
+
+
+@pytest.fixture(autouse=True)
+def _no_cache_left():
+    """A cache that an exception's frames still hold would be freed whenever they are collected: in a capture, perhaps."""
+    gc.collect()
+    yield
+    gc.collect()
 
 
 @pytest.mark.parametrize("bits", [16, "int8", 4])

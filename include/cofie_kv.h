@@ -38,7 +38,10 @@
  *              the zero point z. Code n stands for (n - z) s, which bf16 holds
  *              exactly (fp16 too, for s from 2^-21 and as long as it does not
  *              pass 65504: cofie_kv_read, and attention of more than 32 rows of a
- *              sequence and key head, see it as a number of the cache's type).
+ *              sequence and key head, see it as a number of the cache's type; so
+ *              does cofie_kv_attend_shared for more than 16 rows, of a group over
+ *              its prefix or of a sequence over its own tokens. What passes it is
+ *              infinite there).
  *   Codes of x (64 values, rotated keys as fp32 numbers; hi - lo is formed in
  *   fp32, all else exactly): lo = min(0, min x), hi = max(0, max x),
  *   s = (hi - lo) / 15 rounded up to 4 significant bits (0 below 2^-100),
@@ -191,10 +194,10 @@ int cofie_kv_read(cofie_kv_t* h, const cofie_kv_batch* b, void* k_out, void* v_o
  *   out = sum_j p_j v_j, p = softmax_j(scale <q, k_j>), lse = ln sum_j exp(scale <q, k_j>)
  * Products are of 16-bit numbers, sums in fp32. The weights exp(scale <q, k_j>)
  * are rounded to 16 bits for their product with the values (to the cache's type,
- * of up to 1, or 2^15 for fp16; for few rows over pages of 8 bits (16) or 4 (32)
- * to fp16, times the values' scale) and not for lse; over such pages such rows'
- * queries are taken to fp16 with a power of two for each row, which is meant for
- * queries below 2^110. out is rounded to the cache's type. A row that sees nothing gets
+ * of up to 1, or 2^15 for fp16; for few rows over pages of 8 bits (16) or 4 (32,
+ * or 16 where prefixes are shared) to fp16, times the values' scale) and not for
+ * lse; over such pages such rows' queries are taken to fp16 with a power of two
+ * for each row, which is meant for queries below 2^110. out is rounded to the cache's type. A row that sees nothing gets
  * out = 0, lse = -infinity; what a masked or unwritten place holds (NaN too)
  * never matters. (A NaN or an infinity among a call's own new values may reach
  * all new rows of its sequence, those before it too.)

@@ -190,6 +190,7 @@ __global__ void __launch_bounds__(kSplitThreads<SHORT>, SHORT || (NT == 1 && BIT
   __shared__ float warp_m[kWarps][kRows], warp_l[kWarps][kRows];
   __shared__ uint2 stages[kWarps][R::kStages];  // the bits of the tokens that are seen, and the first one's place
   __shared__ uint32_t row_bits[SHARED ? kWarps : 1][R::kStages][kRows];  // and those that each row sees, where rows differ
+  __shared__ float2 pieces_ms[SHORT ? 1 : kRows];
   __shared__ uint32_t last_here;
   pdl_trigger();
   pdl_wait();
@@ -204,8 +205,28 @@ __global__ void __launch_bounds__(kSplitThreads<SHORT>, SHORT || (NT == 1 && BIT
   }();
   const char* const ring = smem + warp * R::kWarp;
   const BatchArg& b = a.batch;
+  // A warp's sums o take so many tokens, as those of the kernel of many rows (kTcChain has the reason), of which it may have an
+  // eighth of a long cache: an item with more of them here is worked off in pieces, and what is found so far is kept in the
+  // CTA's part. (524288 fp16 tokens 2^-25 of the first: 2^-9 low in one sum. Sums moved on inside the loop over the tokens
+  // cost all calls 2.6 %, up to 7.)
+  constexpr uint32_t kPieceTiles = (std::is_same<T, __half>::value ? 8192 : 65536) * kWarps / kTile;
   Item it;
-  while (walk.next(it)) {
+  uint32_t item_lo = 0, item_hi = 0;  // its tiles here; it.lo and it.hi are the piece's
+  bool more = false;                  // pieces to come
+  const auto next = [&] {
+    if (SHORT) return walk.next(it);
+    if (more) {
+      it.lo = it.hi;
+    } else {
+      if (!walk.next(it)) return false;
+      item_lo = it.lo;
+      item_hi = it.hi;
+    }
+    it.hi = min(item_hi, it.lo + kPieceTiles);
+    more = it.hi < item_hi;
+    return true;
+  };
+  while (next()) {
     const uint32_t row0 = it.rb * kRows;
     const uint32_t rows = min(static_cast<uint32_t>(kRows), it.span.count * a.group - row0);
     // ---- the warp's chunks: warp, warp + 8, ... of the item's part. A chunk's blocks of 16 tokens lie in one page each,
@@ -723,9 +744,10 @@ __global__ void __launch_bounds__(kSplitThreads<SHORT>, SHORT || (NT == 1 && BIT
         }
       }
     }
-    __syncthreads();
     const bool alone = it.first_cta == it.last_cta;
     const uint32_t slot = 2 * blockIdx.x + (blockIdx.x == it.first_cta ? 1 : 0);
+    if (!SHORT && it.lo > item_lo && threadIdx.x < kRows) pieces_ms[threadIdx.x] = a.part_ms[static_cast<uint64_t>(slot) * kRows + threadIdx.x];
+    __syncthreads();
     const auto write = [&](uint32_t r, uint32_t d, float4 x, float top, float sum) {
       const uint32_t i = it.span.first + (row0 + r) / a.group, h = it.head * a.group + (row0 + r) % a.group;
       if constexpr (SHARED) {
@@ -771,14 +793,21 @@ __global__ void __launch_bounds__(kSplitThreads<SHORT>, SHORT || (NT == 1 && BIT
         sum += k * warp_l[w][r];
         y.x += k * z.x, y.y += k * z.y, y.z += k * z.z, y.w += k * z.w;
       }
-      if (alone) {
+      if (!SHORT && it.lo > item_lo) {  // the pieces before (this thread wrote their sums)
+        const Both w = both_parts(top, sum, pieces_ms[r]);
+        const float4 was = *reinterpret_cast<const float4*>(a.part + (static_cast<uint64_t>(slot) * kRows + r) * D + d);
+        y = make_float4(w.own * y.x + w.prefix * was.x, w.own * y.y + w.prefix * was.y, w.own * y.z + w.prefix * was.z, w.own * y.w + w.prefix * was.w);
+        top = w.top;
+        sum = w.sum;
+      }
+      if (alone && (SHORT || !more)) {
         write(r, d, y, top, sum);
       } else {
         *reinterpret_cast<float4*>(a.part + (static_cast<uint64_t>(slot) * kRows + r) * D + d) = y;
         if (d == 0) a.part_ms[static_cast<uint64_t>(slot) * kRows + r] = make_float2(top, sum);
       }
     }
-    if (!alone) {
+    if (!alone && (SHORT || !more)) {
       __syncthreads();
       if (threadIdx.x == 0) last_here = part_done(a, it);
       __syncthreads();

@@ -85,14 +85,18 @@ __device__ __forceinline__ Both both_parts(float top, float sum, float2 before) 
   return x;
 }
 
+// Only prefixes have lists by blocks (SHARED). Calls that know of none do not ask for them: with the question a single token
+// over 1111 took 10.2 us, so 10.0; over 64 6.5 and 6.2.
+template <bool SHARED>
 __device__ __forceinline__ uint64_t tile_list(const AttendArgs& a, uint32_t seq, uint32_t rb) {
-  return static_cast<uint64_t>(seq) * a.list_blocks + min(rb, a.list_blocks - 1);
+  return SHARED ? static_cast<uint64_t>(seq) * a.list_blocks + min(rb, a.list_blocks - 1) : seq;
 }
 
 // Tiles of row block rb: those that its last row can see.
+template <bool SHARED>
 __device__ __forceinline__ uint32_t block_tiles(const AttendArgs& a, const Span& sp, uint32_t rows_per_block, uint32_t rb,
                                                 uint32_t seq) {
-  if (a.tiles) return a.tile_count[tile_list(a, seq, rb)];
+  if (a.tiles) return a.tile_count[tile_list<SHARED>(a, seq, rb)];
   uint32_t end = sp.length;
   if (a.causal) {
     const uint32_t last = min(sp.count * a.group, (rb + 1) * rows_per_block) - 1;
@@ -102,13 +106,14 @@ __device__ __forceinline__ uint32_t block_tiles(const AttendArgs& a, const Span&
   return (end + kTile - 1) / kTile;
 }
 
+template <bool SHARED>
 __device__ __forceinline__ uint64_t sequence_slots(const AttendArgs& a, uint32_t rows_per_block, uint32_t seq, const Span& sp) {
   const uint32_t blocks = (sp.count * a.group + rows_per_block - 1) / rows_per_block;
   uint64_t n = 0;
-  if (a.tiles ? a.list_blocks > 1 : a.causal)
-    for (uint32_t rb = 0; rb < blocks; ++rb) n += block_tiles(a, sp, rows_per_block, rb, seq) + a.item_slots;
+  if (a.tiles ? SHARED && a.list_blocks > 1 : a.causal)
+    for (uint32_t rb = 0; rb < blocks; ++rb) n += block_tiles<SHARED>(a, sp, rows_per_block, rb, seq) + a.item_slots;
   else if (blocks)
-    n = static_cast<uint64_t>(blocks) * (block_tiles(a, sp, rows_per_block, 0, seq) + a.item_slots);
+    n = static_cast<uint64_t>(blocks) * (block_tiles<SHARED>(a, sp, rows_per_block, 0, seq) + a.item_slots);
   return n * a.batch.kv_heads;
 }
 
@@ -139,7 +144,7 @@ __device__ __forceinline__ uint32_t part_done(const AttendArgs& a, const Item& i
 constexpr uint32_t kSpans = 256;  // sequences that are looked up once and kept in shared memory
 
 // Walks the items of one CTA's range. THREADS threads share the sequences.
-template <int THREADS>
+template <int THREADS, bool SHARED>
 struct Plan {
   uint64_t before[THREADS + 1];  // slots before the sequences of each thread
 
@@ -151,7 +156,7 @@ struct Plan {
     for (uint32_t s = t * per; s < min(a.batch.n_seqs, (t + 1) * per); ++s) {
       const Span sp = sequence_span(a.batch, s);
       if (s < kSpans) spans[s] = sp;
-      n += sequence_slots(a, rows_per_block, s, sp);
+      n += sequence_slots<SHARED>(a, rows_per_block, s, sp);
     }
     uint64_t sum = n;
 #pragma unroll
@@ -173,7 +178,7 @@ struct Plan {
 };
 
 // The walk itself (every thread keeps the same one).
-template <int THREADS>
+template <int THREADS, bool SHARED>
 struct Walk {
   const AttendArgs& a;
   const uint32_t rows_per_block;
@@ -184,7 +189,7 @@ struct Walk {
   uint32_t seq, rb, head, blocks;
   Span span;
 
-  __device__ __forceinline__ Walk(const AttendArgs& args, const Plan<THREADS>& plan, const Span* kept, uint32_t rows, uint64_t range_slots)
+  __device__ __forceinline__ Walk(const AttendArgs& args, const Plan<THREADS, SHARED>& plan, const Span* kept, uint32_t rows, uint64_t range_slots)
       : a(args), rows_per_block(rows), range(range_slots), spans(kept) {
     const uint64_t total = plan.before[THREADS];
     at = min(total, static_cast<uint64_t>(blockIdx.x) * range);
@@ -199,14 +204,14 @@ struct Walk {
     seq = lo * ((a.batch.n_seqs + THREADS - 1) / THREADS);
     item_at = plan.before[lo];
     for (;; ++seq) {
-      const uint64_t n = sequence_slots(a, rows_per_block, seq, span_of(seq));
+      const uint64_t n = sequence_slots<SHARED>(a, rows_per_block, seq, span_of(seq));
       if (item_at + n > at || seq + 1 >= a.batch.n_seqs) break;
       item_at += n;
     }
     rb = head = 0;
     enter();
     for (;;) {  // row blocks of the sequence, then heads
-      const uint64_t n = block_tiles(a, span, rows_per_block, rb, seq) + a.item_slots;
+      const uint64_t n = block_tiles<SHARED>(a, span, rows_per_block, rb, seq) + a.item_slots;
       if (item_at + n * a.batch.kv_heads > at) {
         head = static_cast<uint32_t>((at - item_at) / n);
         item_at += n * head;
@@ -227,7 +232,7 @@ struct Walk {
   // The next item with something to do here; false when the range is done.
   __device__ __forceinline__ bool next(Item& it) {
     while (at < end) {
-      const uint32_t tiles = block_tiles(a, span, rows_per_block, rb, seq);
+      const uint32_t tiles = block_tiles<SHARED>(a, span, rows_per_block, rb, seq);
       const uint64_t first = item_at + a.item_slots, past = first + tiles;  // the tiles' slots
       const uint64_t lo = max(at, first), hi = min(end, past);
       const bool mine = tiles ? hi > lo : at <= item_at;  // an item without tiles belongs to its first slot

@@ -95,7 +95,7 @@ struct TcSmem {
   static constexpr int kRow = D * BITS / 8, kRowWords = (D / 64) * 2;  // bytes of a token's keys
   union {
     char q[2][kBlockQ * (D / 64)];
-    Plan<kTcThreads<BITS>> plan;  // until every thread has its walk
+    Plan<kTcThreads<BITS>, SHARED> plan;  // until every thread has its walk
   };
   char kv[2][kStages][kBlock * (D / 64)];  // keys, values
   char raw[2][kRaw][BITS < 16 ? kTile * kRow : 16];
@@ -344,7 +344,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
   const uint32_t tmem = sm.tmem;
   const auto o_at = [&](uint32_t t) { return tmem + t * D; };
   const auto s_at = [&](uint32_t t, uint32_t i) { return tmem + 2 * D + (2 * t + i % 2) * kTile; };
-  Walk<kThreads> walk(a, sm.plan, sm.spans, kTcRows, range);
+  Walk<kThreads, SHARED> walk(a, sm.plan, sm.spans, kTcRows, range);
   __syncthreads();
   const BatchArg& b = a.batch;
   Item it;
@@ -384,7 +384,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
       uint32_t unit_ahead = 0;
       if (by_row && tiles) {
         words = a.seq_words + static_cast<uint64_t>(min(static_cast<uint32_t>(a.seq_of[it.span.first + token]), b.members - 1)) * a.tile_stride;
-        listed = a.tiles + tile_list(a, it.seq, it.rb) * a.tile_stride + it.lo + from;
+        listed = a.tiles + tile_list<SHARED>(a, it.seq, it.rb) * a.tile_stride + it.lo + from;
         word_ahead = words[listed[0]];
         unit_ahead = tiles > 1 ? listed[step] : 0;
       }
@@ -883,7 +883,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
           uint32_t pos, page;   // the tile's first token; the page of the lane's block of 16, n_pages or above where there is none
           uint32_t see0, see1;  // of tokens pos + lane and pos + 32 + lane
         };
-        const uint32_t* const listed = a.tiles ? a.tiles + tile_list(a, it.seq, it.rb) * a.tile_stride + it.lo : nullptr;
+        const uint32_t* const listed = a.tiles ? a.tiles + tile_list<SHARED>(a, it.seq, it.rb) * a.tile_stride + it.lo : nullptr;
         const auto unit_of = [&](uint32_t j) { return j >= tiles ? ~0u : listed ? listed[j] : it.lo + j; };
         const auto look = [&](uint32_t unit) {
           Look x{unit == ~0u ? 0u : unit * kTile, ~0u, 0, 0};

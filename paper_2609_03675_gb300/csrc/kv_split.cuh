@@ -156,7 +156,7 @@ struct ShortWalk {
     if (rb == 0) it.span = sequence_span(a.batch, it.seq);
     if (static_cast<uint64_t>(rb) * rows_per_block >= static_cast<uint64_t>(it.span.count) * a.group) return false;
     it.rb = rb++;
-    it.tiles = it.hi = block_tiles(a, it.span, rows_per_block, it.rb, it.seq);
+    it.tiles = it.hi = block_tiles<true>(a, it.span, rows_per_block, it.rb, it.seq);
     it.lo = 0;
     it.first_cta = it.last_cta = blockIdx.x;
     return true;
@@ -185,7 +185,7 @@ __global__ void __launch_bounds__(kSplitThreads<SHORT>, SHORT || (NT == 1 && BIT
   // of fp32, and 4-bit values have a power of two with their scale.)
   constexpr float kUp = BITS == 16 && std::is_same<T, __half>::value ? 8.f : 0.f, kDown = kUp > 0.f ? 0x1p-8f : 1.f;
   extern __shared__ __align__(128) char smem[];
-  __shared__ std::conditional_t<SHORT, char, Plan<kThreads>> plan;
+  __shared__ std::conditional_t<SHORT, char, Plan<kThreads, SHARED>> plan;
   __shared__ Span spans[SHORT ? 1 : kSpans];
   __shared__ float warp_m[kWarps][kRows], warp_l[kWarps][kRows];
   __shared__ uint2 stages[kWarps][R::kStages];  // the bits of the tokens that are seen, and the first one's place
@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(kSplitThreads<SHORT>, SHORT || (NT == 1 && BIT
       return ShortWalk(a, kRows);
     } else {
       const uint64_t range = plan.set_up(a, kRows, spans);
-      return Walk<kThreads>(a, plan, spans, kRows, range);
+      return Walk<kThreads, SHARED>(a, plan, spans, kRows, range);
     }
   }();
   const char* const ring = smem + warp * R::kWarp;
@@ -252,7 +252,7 @@ __global__ void __launch_bounds__(kSplitThreads<SHORT>, SHORT || (NT == 1 && BIT
       for (int mt = 0; mt < kM; ++mt) x.page[mt] = ~0u;
       if (ch < chunks) {
         const uint32_t t = it.lo + ch / kPerTile;
-        x.pos = (a.tiles ? a.tiles[tile_list(a, it.seq, it.rb) * a.tile_stride + t] : t) * kTile + (ch % kPerTile) * R::kTokens;
+        x.pos = (a.tiles ? a.tiles[tile_list<SHARED>(a, it.seq, it.rb) * a.tile_stride + t] : t) * kTile + (ch % kPerTile) * R::kTokens;
 #pragma unroll
         for (int mt = 0; mt < kM; ++mt)
           if (x.pos + 16 * mt < it.span.length) x.page[mt] = static_cast<uint32_t>(table[(x.pos + 16 * mt) >> b.page_shift]);

@@ -318,6 +318,22 @@ int kind_of(const cofie_kv* h, uint64_t rows, bool shared) {
   return rows > few ? kMany : rows > 8 ? kFew16 : kFew8;
 }
 
+// Some hundred bytes of arguments, which launch_dependent would copy twice.
+cudaError_t launch_args(AttendKernel kernel, dim3 grid, uint32_t threads, size_t smem, cudaStream_t st, AttendArgs* a) {
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  void* args[] = {a};
+  return cudaLaunchKernelExC(&cfg, reinterpret_cast<const void*>(kernel), args);
+}
+
 int launch_attend(cofie_kv* h, AttendArgs* a, uint64_t rows, bool shared, cudaStream_t st) {
   // What an item costs beside its tiles' slots (set-up, first loads, its part's joining), in the time of a tile: about 8 for
   // many rows and 6 for few, at every size tried. Many rows, us with 4 / 8 / 16 / 24 slots: seven questions of 3 to 300
@@ -337,9 +353,9 @@ int launch_attend(cofie_kv* h, AttendArgs* a, uint64_t rows, bool shared, cudaSt
   a->item_slots = kind == kMany ? 8 : 6;
   const AttendLaunch k = kernel_of(h->p, kind, shared);
   const uint32_t ctas = kind == kMany ? sm_count() : kind >= kShort8 ? static_cast<uint32_t>(items) : h->split_ctas[shared][kind];
-  if (const int rc = launched(h, launch_dependent(true, k.kernel, dim3(ctas), dim3(k.threads), k.smem, st, *a), "attend")) return rc;
+  if (const int rc = launched(h, launch_args(k.kernel, dim3(ctas), k.threads, k.smem, st, a), "attend")) return rc;
   if (kind != kMany) return COFIE_OK;
-  return launched(h, launch_dependent(true, k.join, dim3(ctas, kManyRows / k.join_rows), dim3(k.join_threads), 0, st, *a), "attend");
+  return launched(h, launch_args(k.join, dim3(ctas, kManyRows / k.join_rows), k.join_threads, 0, st, a), "attend");
 }
 
 uint64_t rows_at_most(const cofie_kv_batch* b, uint32_t group) {

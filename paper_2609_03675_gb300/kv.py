@@ -376,12 +376,15 @@ class KVCache:
         max_new: at least the largest count of new tokens. It chooses the kernel (with offsets and 0, all tokens are taken
         for one sequence's, and many short sequences run the kernel of long questions). mask: uint8
         [sequences, >= the longest], nonzero where a cached token may be seen. scale 0: head_dim ** -0.5."""
-        lse_at, out, lse, rows, at, stride = self._asked(q, table, lengths, offsets, max_new, mask, out, lse, cuda_stream)
+        rows, out, lse = self._asked(q, table, lengths, offsets, max_new, out, lse, cuda_stream)
+        at, stride = (None, 0) if mask is None else self._mask(mask, table.shape[0], "mask")
         stream = _raw_stream(self._index) if cuda_stream is None else _stream_of(cuda_stream, self._index)
-        self._check(self._lib.cofie_kv_attend(self._h, self._at, rows, lse_at, at, stride, causal, scale, stream))
+        rc = self._lib.cofie_kv_attend(self._h, self._at, rows, lse.data_ptr(), at, stride, causal, scale, stream)
+        if rc:
+            self._check(rc)
         return out, lse
 
-    def _asked(self, q, table, lengths, offsets, max_new, mask, out, lse, cuda_stream):
+    def _asked(self, q, table, lengths, offsets, max_new, out, lse, cuda_stream):
         """What attend and attend_shared check and pack alike."""
         n, index = q.shape[0], self._index
         if q.requires_grad and torch.is_grad_enabled():
@@ -394,11 +397,9 @@ class KVCache:
         self._batch(table, lengths, offsets, n, 1 if offsets is None else max_new)
         if lse.dtype is not torch.float32 or lse.shape != (n, self.n_heads) or not lse.is_contiguous() or lse.get_device() != index:
             raise ValueError(f"lse must be a contiguous float32 tensor [{n}, {self.n_heads}] on cuda:{index}")
-        return lse.data_ptr(), out, lse, r, *self._mask(mask, table.shape[0], "mask")
+        return r, out, lse
 
     def _mask(self, mask, seqs, what):
-        if mask is None:
-            return None, 0
         if mask.dtype not in (torch.uint8, torch.bool) or mask.dim() != 2 or mask.shape[0] != seqs or not mask.is_contiguous() \
                 or mask.get_device() != self._index:
             raise ValueError(f"{what} must be a contiguous uint8 or bool tensor [{seqs}, tokens] on cuda:{self._index}")
@@ -414,18 +415,21 @@ class KVCache:
         largest count of a group's new tokens together (0: all); it chooses the kernel. prefix_mask: uint8
         [sequences, >= the longest prefix], nonzero where a sequence may see a token of its prefix (its own evidence)."""
         index = self._index
-        lse_at, out, lse, rows, at, stride = self._asked(q, table, lengths, offsets, max_new, mask, out, lse, cuda_stream)
+        rows, out, lse = self._asked(q, table, lengths, offsets, max_new, out, lse, cuda_stream)
+        at, stride = (None, 0) if mask is None else self._mask(mask, table.shape[0], "mask")
         if prefix_table.dtype is not torch.int32 or prefix_table.get_device() != index or prefix_table.dim() != 2 or not prefix_table.is_contiguous():
             raise ValueError(f"prefix_table must be a contiguous int32 tensor [groups, pages] on cuda:{index}")
         n, width = prefix_table.shape
         if groups is None and n != 1:
             raise ValueError("without groups prefix_table has one row")
-        mask_at, mask_stride = self._mask(prefix_mask, table.shape[0], "prefix_mask")
+        mask_at, mask_stride = (0, 0) if prefix_mask is None else self._mask(prefix_mask, table.shape[0], "prefix_mask")
         _PREFIX.pack_into(self._buf, _PREFIX_AT, n, max_shared, width, prefix_table.data_ptr(),
                           _int32(prefix_lengths, index, "prefix_lengths", (n,)),
-                          0 if groups is None else _int32(groups, index, "groups", (n + 1,)), mask_at or 0, mask_stride)
+                          0 if groups is None else _int32(groups, index, "groups", (n + 1,)), mask_at, mask_stride)
         stream = _raw_stream(index) if cuda_stream is None else _stream_of(cuda_stream, index)
-        self._check(self._lib.cofie_kv_attend_shared(self._h, self._at, self._at + _PREFIX_AT, rows, lse_at, at, stride, causal, scale, stream))
+        rc = self._lib.cofie_kv_attend_shared(self._h, self._at, self._at + _PREFIX_AT, rows, lse.data_ptr(), at, stride, causal, scale, stream)
+        if rc:
+            self._check(rc)
         return out, lse
 
     def status(self, cuda_stream=None):

@@ -20,7 +20,8 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libcofie_ngff.so")
 SOURCES = ["ngff_api.cu", "ngff_hist.cu", "ngff_features.cu", "ngff_select.cu", "ngff_chain.cu", "ngff_lazy.cu",
            "ngff_finalize.cu",
-           "ngff_static.cu", "qer.cu", "rotary.cu", "kv_pages.cu", "kv_attend.cu", "kv_attend_4.cu", "kv_attend_8.cu", "kv_attend_16.cu"]
+           "ngff_static.cu", "qer.cu", "rotary.cu", "kv_pages.cu", "kv_attend.cu", "kv_attend_4.cu", "kv_attend_8.cu", "kv_attend_16.cu",
+           "kv_attend_4_shared.cu", "kv_attend_8_shared.cu", "kv_attend_16_shared.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -173,7 +173,10 @@ __global__ void __launch_bounds__(kMaskThreads) prefix_tiles(const BatchArg grou
 }
 
 AttendLaunch kernel_of(const cofie_kv_params& p, int kind, bool shared) {
-  return p.bits == 4 ? attend_kernel<4>(p, kind, shared) : p.bits == 8 ? attend_kernel<8>(p, kind, shared) : attend_kernel<16>(p, kind, shared);
+  const auto of = [&](auto bits) {
+    return shared ? attend_kernel<bits, true>(p, kind) : attend_kernel<bits, false>(p, kind);
+  };
+  return p.bits == 4 ? of(std::integral_constant<int, 4>()) : p.bits == 8 ? of(std::integral_constant<int, 8>()) : of(std::integral_constant<int, 16>());
 }
 
 }  // namespace
@@ -205,16 +208,17 @@ cudaError_t attend_set_up(cofie_kv* h) {
     if (e == cudaSuccess) e = map_pages(h->p, h->p.v_pages, &h->maps[1]);
   }
   size_t rows = 2ull * sm_count() * kManyRows, ctas = 0;
-  for (int i = 0; i < 8 && e == cudaSuccess; ++i) {
-    const int kind = i < 3 ? i : i - 3;
-    const AttendLaunch k = kernel_of(h->p, kind, i >= 3);
+  for (int i = 0; i < kShort8 + kShort16 + 1 && e == cudaSuccess; ++i) {
+    const bool shared = i >= kShort8;  // those of no prefix first
+    const int kind = shared ? i - kShort8 : i;
+    const AttendLaunch k = kernel_of(h->p, kind, shared);
     e = cudaFuncSetAttribute(k.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(k.smem));
     if (kind >= kMany || e != cudaSuccess) continue;
     int per_sm = 0;
     e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, k.kernel, static_cast<int>(k.threads), k.smem);
     if (e == cudaSuccess && per_sm < 1) e = cudaErrorInvalidConfiguration;
     const uint32_t n = sm_count() * static_cast<uint32_t>(per_sm);
-    h->split_ctas[i >= 3][kind] = n;
+    h->split_ctas[shared][kind] = n;
     ctas = std::max<size_t>(ctas, n);
     rows = std::max<size_t>(rows, 2ull * n * (8u << kind));
   }
@@ -348,14 +352,29 @@ int launch_attend(cofie_kv* h, AttendArgs* a, uint64_t rows, bool shared, cudaSt
   int kind = kind_of(h, rows, shared);
   const uint64_t items = static_cast<uint64_t>(a->batch.n_seqs) * a->batch.kv_heads;
   const uint64_t width = static_cast<uint64_t>(a->batch.table_stride) << h->page_shift;
-  if (a->behind && kind != kMany && width <= std::min<uint64_t>(8192, std::max<uint64_t>(512, 16 * items)) && items <= 0x7fffffffu)
+  // 17 to 32 rows of heads of 64, 16 bits: blocks are quicker where there is little to read (us, blocks / tiles, 32 rows): 2
+  // sequences and key heads over 2048 tokens 11 / 15, over 60000 24 / 30; 8 of 64 6.9 / 7.1, of 128 9.7 / 7.8, of 512 to 2048 10.4 /
+  // 11.7 to 11.3 / 14.3, of 6000 15.4 / 16.8, of 60000 53.5 / 46.7; 16 of 128 to 2048 7.2 / 8.0 to 13.3 / 15.5, of 6000 20.2 /
+  // 19.1; 32 of 64 to 1024 7.4 / 7.6 to 14.8 / 15.5, of 6000 28.0 / 25.9; 64 of 64 7.5 / 8.0, of 128 10.0 / 8.5, of 1024 18.3 / 19.4,
+  // of 2048 23.3 / 22.8; 128 of 64 11.0 / 8.4.
+  if (kind == kMany && !shared && h->p.bits == 16 && h->p.head_dim == 64 && rows <= 32 && items <= 64 &&
+      items * width <= (items <= 4 ? 131072 : 65536) && (width <= 64 || (items >= 16 && items <= 32) || width > (items <= 32 ? 384 : 512)))
+    kind = kFew16;
+  // Many rows over few tokens, as the table's width bounds them: items are not cut, so that no launch joins them. Most of 1 to
+  // 32 sequences of 16 or 8 key heads, 18 to 256 rows, 16 to 4 bits, all equally long, of any length up to the width and one
+  // that long, cut / uncut: up to 384 tokens 0.65 to 1.00 of the time (64 tokens 13.4 / 9.1 us, 384 14.9 / 14.6 to 38 / 25), 512
+  // 0.7 to 1.1 (one sequence of 8 key heads 14.9 / 16.3, eight 20.9 / 17.5), 768 0.8 to 1.3.
+  if (kind == kMany && width <= (items >= 64 ? 512 : 384)) kind = kManyWhole;
+  if (a->behind && kind < kMany && width <= std::min<uint64_t>(8192, std::max<uint64_t>(512, 16 * items)) && items <= 0x7fffffffu)
     kind = kind == kFew8 ? kShort8 : kShort16;
-  a->item_slots = kind == kMany ? 8 : 6;
+  const bool many = kind == kMany || kind == kManyWhole;
+  a->item_slots = many ? 8 : 6;
   const AttendLaunch k = kernel_of(h->p, kind, shared);
-  const uint32_t ctas = kind == kMany ? sm_count() : kind >= kShort8 ? static_cast<uint32_t>(items) : h->split_ctas[shared][kind];
+  const uint32_t ctas = many ? sm_count() : kind >= kShort8 ? static_cast<uint32_t>(items) : h->split_ctas[shared][kind];
   if (const int rc = launched(h, launch_args(k.kernel, dim3(ctas), k.threads, k.smem, st, a), "attend")) return rc;
   if (kind != kMany) return COFIE_OK;
-  return launched(h, launch_args(k.join, dim3(ctas, kManyRows / k.join_rows), k.join_threads, 0, st, a), "attend");
+  const uint64_t block = std::min<uint64_t>(kManyRows, static_cast<uint64_t>(a->batch.n_tokens) * a->group);
+  return launched(h, launch_args(k.join, dim3(ctas, static_cast<uint32_t>((block + k.join_rows - 1) / k.join_rows)), k.join_threads, 0, st, a), "attend");
 }
 
 uint64_t rows_at_most(const cofie_kv_batch* b, uint32_t group) {

@@ -1,3 +1,3 @@
 #include "kv_kernels_impl.cuh"
 
-template cofie::AttendLaunch cofie::attend_kernel<8>(const cofie_kv_params&, int, bool);
+template cofie::AttendLaunch cofie::attend_kernel<8, false>(const cofie_kv_params&, int);

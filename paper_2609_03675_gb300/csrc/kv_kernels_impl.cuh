@@ -10,7 +10,8 @@ namespace {
 template <typename T, int D, int BITS, bool SHARED>
 AttendLaunch attend_kernel_of(int kind) {
   if (kind == kMany)
-    return {attend_rows_tc<T, D, BITS, SHARED>, kTcThreads<BITS>, tc_smem<D, BITS, SHARED>(), attend_join<T, D, SHARED>, kJoinThreads, kJoinRows<D>};
+    return {attend_rows_tc<T, D, BITS, SHARED, false>, kTcThreads<BITS>, tc_smem<D, BITS, SHARED>(), attend_join<T, D, SHARED>, kJoinThreads, kJoinRows<D>};
+  if (kind == kManyWhole) return {attend_rows_tc<T, D, BITS, SHARED, true>, kTcThreads<BITS>, tc_smem<D, BITS, SHARED>(), nullptr, 0, 0};
   if constexpr (SHARED) {
     if (kind == kShort8) return {attend_split<T, D, BITS, 1, true, true>, kSplitThreads<true>, split_smem<D, BITS, 1, true>(), nullptr, 0, 0};
     if (kind == kShort16) return {attend_split<T, D, BITS, 2, true, true>, kSplitThreads<true>, split_smem<D, BITS, 2, true>(), nullptr, 0, 0};
@@ -21,12 +22,11 @@ AttendLaunch attend_kernel_of(int kind) {
 
 }  // namespace
 
-template <int BITS>
-AttendLaunch attend_kernel(const cofie_kv_params& p, int kind, bool shared) {
+template <int BITS, bool SHARED>
+AttendLaunch attend_kernel(const cofie_kv_params& p, int kind) {
   const auto of = [&](auto x) {
     using T = decltype(x);
-    if (p.head_dim == 64) return shared ? attend_kernel_of<T, 64, BITS, true>(kind) : attend_kernel_of<T, 64, BITS, false>(kind);
-    return shared ? attend_kernel_of<T, 128, BITS, true>(kind) : attend_kernel_of<T, 128, BITS, false>(kind);
+    return p.head_dim == 64 ? attend_kernel_of<T, 64, BITS, SHARED>(kind) : attend_kernel_of<T, 128, BITS, SHARED>(kind);
   };
   return p.dtype == COFIE_BF16 ? of(__nv_bfloat16()) : of(__half());
 }

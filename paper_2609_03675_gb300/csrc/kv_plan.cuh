@@ -9,7 +9,8 @@
 // part in each: unnormalised sums, the maximum and the sum of the exponentials.
 // Parts of few rows are joined by the CTA that finishes last, those of many by a
 // launch of their own, always in the order of the ranges, so that results do not
-// depend on who is last. Nobody waits for anybody.
+// depend on who is last. Nobody waits for anybody. Over few tokens, items of many
+// rows are not cut (WHOLE).
 #pragma once
 
 #include "kv_handle.cuh"
@@ -177,8 +178,9 @@ struct Plan {
   }
 };
 
-// The walk itself (every thread keeps the same one).
-template <int THREADS, bool SHARED>
+// The walk itself (every thread keeps the same one). WHOLE: items are not cut; each belongs to the CTA that has its first
+// slot.
+template <int THREADS, bool SHARED, bool WHOLE>
 struct Walk {
   const AttendArgs& a;
   const uint32_t rows_per_block;
@@ -235,17 +237,18 @@ struct Walk {
       const uint32_t tiles = block_tiles<SHARED>(a, span, rows_per_block, rb, seq);
       const uint64_t first = item_at + a.item_slots, past = first + tiles;  // the tiles' slots
       const uint64_t lo = max(at, first), hi = min(end, past);
-      const bool mine = tiles ? hi > lo : at <= item_at;  // an item without tiles belongs to its first slot
+      const bool uncut = WHOLE || tiles == 0;  // an item without tiles belongs to its first slot too
+      const bool mine = uncut ? at <= item_at : hi > lo;
       if (mine) {
         it.seq = seq;
         it.rb = rb;
         it.head = head;
         it.span = span;
         it.tiles = tiles;
-        it.lo = tiles ? static_cast<uint32_t>(lo - first) : 0;
-        it.hi = tiles ? static_cast<uint32_t>(hi - first) : 0;
-        it.first_cta = tiles ? static_cast<uint32_t>(first / range) : blockIdx.x;
-        it.last_cta = tiles ? static_cast<uint32_t>((past - 1) / range) : blockIdx.x;
+        it.lo = uncut ? 0 : static_cast<uint32_t>(lo - first);
+        it.hi = uncut ? tiles : static_cast<uint32_t>(hi - first);
+        it.first_cta = uncut ? blockIdx.x : static_cast<uint32_t>(first / range);
+        it.last_cta = uncut ? blockIdx.x : static_cast<uint32_t>((past - 1) / range);
       }
       at = past;
       item_at = past;

@@ -287,8 +287,8 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   return x;
 }
 
-// SHARED as for attend_split.
-template <typename T, int D, int BITS, bool SHARED>
+// SHARED as for attend_split. WHOLE: no item is cut, and no launch that joins parts follows.
+template <typename T, int D, int BITS, bool SHARED, bool WHOLE>
 __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __grid_constant__ AttendArgs a) {
   using P = Pair<T>;
   using S = TcSmem<D, BITS, SHARED>;
@@ -332,7 +332,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   pdl_wait();
-  if (threadIdx.x == 0) a.items[blockIdx.x].last_cta = 0;  // none goes on from here, so far
+  if (!WHOLE && threadIdx.x == 0) a.items[blockIdx.x].last_cta = 0;  // none goes on from here, so far
   // only now: a kernel before this one may still hold tensor memory, or wait for it
   if (warp == kIssuer) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(shared_address(&sm.tmem)) : "memory");
@@ -344,7 +344,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
   const uint32_t tmem = sm.tmem;
   const auto o_at = [&](uint32_t t) { return tmem + t * D; };
   const auto s_at = [&](uint32_t t, uint32_t i) { return tmem + 2 * D + (2 * t + i % 2) * kTile; };
-  Walk<kThreads, SHARED> walk(a, sm.plan, sm.spans, kTcRows, range);
+  Walk<kThreads, SHARED, WHOLE> walk(a, sm.plan, sm.spans, kTcRows, range);
   __syncthreads();
   const BatchArg& b = a.batch;
   Item it;
@@ -577,7 +577,7 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
         }
       }
       n += told;
-      const bool alone = it.first_cta == it.last_cta;
+      const bool alone = WHOLE || it.first_cta == it.last_cta;
       if (threadIdx.x == 0 && it.first_cta == blockIdx.x && !alone) a.items[blockIdx.x] = {it.seq, it.rb, it.head, it.last_cta, it.span};
       const uint64_t part = own_part();
       // All have what they kept, of this item or of one before it, before the part is written: its rows lie across what other

@@ -200,7 +200,7 @@ __global__ void __launch_bounds__(kSplitThreads<SHORT>, SHORT || (NT == 1 && BIT
       return ShortWalk(a, kRows);
     } else {
       const uint64_t range = plan.set_up(a, kRows, spans);
-      return Walk<kThreads, SHARED>(a, plan, spans, kRows, range);
+      return Walk<kThreads, SHARED, false>(a, plan, spans, kRows, range);
     }
   }();
   const char* const ring = smem + warp * R::kWarp;

@@ -62,3 +62,48 @@ def test_kept_sums_before_an_item_that_goes_on(bits, dtype, seqs, new, m, kv, gr
     want = B.attend(q, k, v, seen, d ** -0.5, dtype)
     bad = B.exceeds(out.view(seqs, new, h, d), lse.view(seqs, new, h), want)
     assert not bool(bad[0].any()) and not bool(bad[1].any())
+
+
+@pytest.mark.parametrize("bits", [16, "int8", 4])
+@pytest.mark.parametrize("heads", [(8, 2, 128), (16, 8, 64), (4, 4, 64), (14, 2, 64)])
+@pytest.mark.parametrize("new", [5, 20, 70])
+def test_tables_of_every_width(bits, heads, new):
+    """The table's width bounds the tokens and chooses whether items are cut, or taken by blocks of few rows: the same
+    sequences under tables of 128 to 2048 tokens, with and without prefixes, masked and not, to the one definition."""
+    from paper_2609_03675_gb300 import KVCache
+    h, kv, d = heads
+    page, dtype = 32, torch.bfloat16
+    lengths, news = [new, 128, new + 1, 0, 77 + new // 2, 126], [new, 1, new, 0, new // 2, 2]
+    g = torch.Generator().manual_seed(new)
+    cache = KVCache(4 * len(lengths) + 1, page, h, kv, d, dtype=dtype, bits=bits)
+    table = torch.randperm(4 * len(lengths), generator=g).to(torch.int32).view(-1, 4).cuda()
+    lens = torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    whole = torch.tensor([0] + lengths).cumsum(0).to(torch.int32).cuda()
+    x = [torch.randn((sum(lengths), kv, d), generator=g).to(dtype).cuda() for _ in range(2)]
+    cache.append(*x, table, lens, whole)
+    k, v = cache.read(table, lens, whole, n_tokens=sum(lengths))
+    q = torch.randn((sum(news), h, d), generator=g).to(dtype).cuda()
+    offsets = torch.tensor([0] + news).cumsum(0).to(torch.int32).cuda()
+    mask = torch.rand((len(lengths), 128), generator=g) < 0.6
+    mask[1] = False
+    none = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for masked in (False, True):
+        want, t, at = [], 0, 0
+        for s, (n, m) in enumerate(zip(news, lengths)):
+            seen = torch.arange(m)[None] <= (m - n + torch.arange(n))[:, None]
+            if masked:
+                seen = seen & mask[s, :m]
+            want.append(B.attend(q[t:t + n], k[at:at + m], v[at:at + m], seen, d ** -0.5, dtype) if n else None)
+            t, at = t + n, at + m
+        for width in (4, 12, 16, 17, 64):
+            wide = torch.nn.functional.pad(table, (0, width - 4)).contiguous()
+            kw = dict(max_new=new, mask=mask.cuda() if masked else None)
+            for out, lse in (cache.attend(q, wide, lens, offsets, **kw),
+                             cache.attend_shared(q, wide, lens, offsets, prefix_table=wide[:1], prefix_lengths=none, **kw)):
+                cache.status()
+                t = 0
+                for n, w in zip(news, want):
+                    if n:
+                        bad = B.exceeds(out[t:t + n], lse[t:t + n], w)
+                        assert not bool(bad[0].any()) and not bool(bad[1].any()), width
+                    t += n

@@ -345,10 +345,6 @@ int launch_attend(cofie_kv* h, AttendArgs* a, uint64_t rows, bool shared, cudaSt
   // 394, thirty of 16 over up to 2000 87 / 91 / 97 / 103. Few, with 2 / 4 / 6 / 8 / 12: 24 x 3 tokens over up to 9000 of
   // 4 bits 91 / 79 / 72 / 69 / 62, 64 x 1 over up to 20000 of 4 bits 220 / 212 / 200 / 197 / 199, of 16 bits 419 / 402 /
   // 400 / 394 / 398, 8 x 1 over up to 3000 27 / 25 / 23 / 25 / 25.
-  // Own tokens behind a prefix: a sequence and key head are left to one CTA where its tokens, as the table's width bounds
-  // them, are few, or where there are so many of these items that they fill the GPU uncut. Single tokens, heads of 128 and 16
-  // bits, us cut / uncut: 16 items of 256 tokens 19 / 16, of 1024 20 / 25; 64 of 1024 31 / 30, of 2048 34 / 42; 256 of 2048
-  // 69 / 56, of 8192 154 / 148; 512 of 4096 161 / 140, of 8192 273 / 248; with fewer bits alike.
   int kind = kind_of(h, rows, shared);
   const uint64_t items = static_cast<uint64_t>(a->batch.n_seqs) * a->batch.kv_heads;
   const uint64_t width = static_cast<uint64_t>(a->batch.table_stride) << h->page_shift;
@@ -365,7 +361,15 @@ int launch_attend(cofie_kv* h, AttendArgs* a, uint64_t rows, bool shared, cudaSt
   // that long, cut / uncut: up to 384 tokens 0.65 to 1.00 of the time (64 tokens 13.4 / 9.1 us, 384 14.9 / 14.6 to 38 / 25), 512
   // 0.7 to 1.1 (one sequence of 8 key heads 14.9 / 16.3, eight 20.9 / 17.5), 768 0.8 to 1.3.
   if (kind == kMany && width <= (items >= 64 ? 512 : 384)) kind = kManyWhole;
-  if (a->behind && kind < kMany && width <= std::min<uint64_t>(8192, std::max<uint64_t>(512, 16 * items)) && items <= 0x7fffffffu)
+  // Own tokens behind a prefix: a sequence and key head are left to one CTA where its tokens, as the table's width bounds
+  // them, are few, or where there are so many of these items that they fill the GPU uncut; but a single one as long as the
+  // width must not wait alone. Single tokens, heads of 128 and 16 bits, the whole call, us cut / uncut, where all are of the
+  // width, of any length up to it, and one of it beside others of 10: 16 items of 512 17.5 / 17.3, 17.3 / 17.0, 17.0 / 17.2, of
+  // 1024 19 / 24, 18 / 24, 17 / 24; 64 of 1024 32 / 30, 30 / 29, 27 / 27, of 2048 35 / 43, 31 / 41, 28 / 39; 128 of 1024 40 / 35,
+  // 37 / 35, 33 / 34, of 2048 59 / 54, 41 / 46, 33 / 46; 192 of 2048 64 / 52, 51 / 47, 30 / 40; 256 of 2048 74 / 61, 59 / 51, 32 / 41, of 4096 110 / 97, 75 / 77, 33 / 65; 512
+  // of 2048 118 / 105, 85 / 76, 44 / 47, of 8192 343 / 317, 190 / 207, 46 / 118; with fewer bits alike.
+  const uint64_t uncut = items >= 160 ? 2048 : items >= 96 ? 1536 : items >= 64 ? 1024 : 512;
+  if (a->behind && kind < kMany && width <= uncut && items <= 0x7fffffffu)
     kind = kind == kFew8 ? kShort8 : kShort16;
   const bool many = kind == kMany || kind == kManyWhole;
   a->item_slots = many ? 8 : 6;

@@ -309,8 +309,11 @@ class KVCache:
         if table.dtype is not torch.int32 or table.get_device() != index or table.dim() != 2 or not table.is_contiguous():
             raise ValueError(f"table must be a contiguous int32 tensor [sequences, pages] on cuda:{index}")
         seqs, width = table.shape
-        _BATCH.pack_into(self._buf, 0, seqs, n, max_new, width, table.data_ptr(), _int32(lengths, index, "lengths", (seqs,)),
-                         0 if offsets is None else _int32(offsets, index, "offsets", (seqs + 1,)))
+        lengths, offsets = _int32(lengths, index, "lengths", (seqs,)), 0 if offsets is None else _int32(offsets, index, "offsets", (seqs + 1,))
+        try:
+            _BATCH.pack_into(self._buf, 0, seqs, n, max_new, width, table.data_ptr(), lengths, offsets)
+        except struct.error:
+            raise ValueError("max_new must be a whole number in [0, 2^32), and the batch's sizes below 2^32") from None
 
     def _rows(self, i, x, heads, what, n=None, out=None):
         """Packs tensor i of the call; returns where."""
@@ -423,9 +426,11 @@ class KVCache:
         if groups is None and n != 1:
             raise ValueError("without groups prefix_table has one row")
         mask_at, mask_stride = (0, 0) if prefix_mask is None else self._mask(prefix_mask, table.shape[0], "prefix_mask")
-        _PREFIX.pack_into(self._buf, _PREFIX_AT, n, max_shared, width, prefix_table.data_ptr(),
-                          _int32(prefix_lengths, index, "prefix_lengths", (n,)),
-                          0 if groups is None else _int32(groups, index, "groups", (n + 1,)), mask_at, mask_stride)
+        prefix_lengths, groups = _int32(prefix_lengths, index, "prefix_lengths", (n,)), 0 if groups is None else _int32(groups, index, "groups", (n + 1,))
+        try:
+            _PREFIX.pack_into(self._buf, _PREFIX_AT, n, max_shared, width, prefix_table.data_ptr(), prefix_lengths, groups, mask_at, mask_stride)
+        except struct.error:
+            raise ValueError("max_shared must be a whole number in [0, 2^32)") from None
         stream = _raw_stream(index) if cuda_stream is None else _stream_of(cuda_stream, index)
         rc = self._lib.cofie_kv_attend_shared(self._h, self._at, self._at + _PREFIX_AT, rows, lse.data_ptr(), at, stride, causal, scale, stream)
         if rc:

@@ -77,3 +77,15 @@ def test_growth_for_the_own_mask_in_a_capture(new):
     torch.cuda.synchronize()
     assert float(mark) == 1.0
     _untouched(x, kw)
+
+
+@pytest.mark.parametrize("value", [-1, 1 << 32, 1.5, None])
+def test_hints_that_are_no_counts(value):
+    x = Shared(16, torch.bfloat16, (4, 2, 64), [1, 2], [3, 2], [40], [0, 2], 16)
+    with pytest.raises(ValueError, match="max_shared"):
+        x.call(max_shared=value)
+    with pytest.raises(ValueError, match="max_new"):
+        x.call(max_new=value)
+    with pytest.raises(ValueError, match="max_new"):
+        x.cache.attend(x.q, x.table, x.lens, x.offsets, max_new=value)
+    x.check()

@@ -237,18 +237,23 @@ struct Walk {
       const uint32_t tiles = block_tiles<SHARED>(a, span, rows_per_block, rb, seq);
       const uint64_t first = item_at + a.item_slots, past = first + tiles;  // the tiles' slots
       const uint64_t lo = max(at, first), hi = min(end, past);
-      const bool uncut = WHOLE || tiles == 0;  // an item without tiles belongs to its first slot too
-      const bool mine = uncut ? at <= item_at : hi > lo;
+      const bool mine = !WHOLE && tiles ? hi > lo : at <= item_at;  // an item without tiles belongs to its first slot, too
       if (mine) {
         it.seq = seq;
         it.rb = rb;
         it.head = head;
         it.span = span;
         it.tiles = tiles;
-        it.lo = uncut ? 0 : static_cast<uint32_t>(lo - first);
-        it.hi = uncut ? tiles : static_cast<uint32_t>(hi - first);
-        it.first_cta = uncut ? blockIdx.x : static_cast<uint32_t>(first / range);
-        it.last_cta = uncut ? blockIdx.x : static_cast<uint32_t>((past - 1) / range);
+        if constexpr (WHOLE) {
+          it.lo = 0;
+          it.hi = tiles;
+          it.first_cta = it.last_cta = blockIdx.x;
+        } else {
+          it.lo = tiles ? static_cast<uint32_t>(lo - first) : 0;
+          it.hi = tiles ? static_cast<uint32_t>(hi - first) : 0;
+          it.first_cta = tiles ? static_cast<uint32_t>(first / range) : blockIdx.x;
+          it.last_cta = tiles ? static_cast<uint32_t>((past - 1) / range) : blockIdx.x;
+        }
       }
       at = past;
       item_at = past;

@@ -303,7 +303,9 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
   constexpr float kMost = kHalf ? 0x1p15f : 1.f, kUp = kHalf ? 8.f : -8.f;
   extern __shared__ char raw[];
   S& sm = *reinterpret_cast<S*>(raw + (1024u - (shared_address(raw) & 1023u)) % 1024u);
-  pdl_trigger();
+  // (Behind whole items the next launch is not let in early: where it was, a following call's passes over its mask lay beside
+  // them and the kernel over its prefix took 50 us more of 416.)
+  if (!WHOLE) pdl_trigger();
   const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   constexpr uint32_t kIssuer = (kTcSoftmax + (BITS < 16 ? 2 * kTcUnpack : 0)) / 32, kLoader = kIssuer + 2;  // their first warps
   if (threadIdx.x == 0) {
@@ -581,8 +583,10 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
       if (threadIdx.x == 0 && it.first_cta == blockIdx.x && !alone) a.items[blockIdx.x] = {it.seq, it.rb, it.head, it.last_cta, it.span};
       const uint64_t part = own_part();
       // All have what they kept, of this item or of one before it, before the part is written: its rows lie across what other
-      // threads keep, and a stream that the last item has no rows for may be an item behind.
-      if (!alone && (kept_alone || told > kTcChain<T>)) bar_sync<1, kTcSoftmax>();
+      // threads keep, and a stream that the last item has no rows for may be an item behind. (With prefixes at every item:
+      // only where sums were kept takes a register more, and eight questions over bytes took 1246 us for 1221, 32 answers 239 for
+      // 232. Without, that is quicker: eight sequences of 32 rows over 6000 tokens of bytes 57, at every item 61.)
+      if (SHARED || (!alone && (kept_alone || told > kTcChain<T>))) bar_sync<1, kTcSoftmax>();
       kept_alone = kept_alone || (alone && told > kTcChain<T>);
       // Both streams' sums of the same rows: the second's go to the first through Q's place, once all products are done.
       float k0 = 1.f, k1 = 0.f;

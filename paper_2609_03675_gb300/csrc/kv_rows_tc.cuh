@@ -494,7 +494,8 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
               if (again || (!found && __any_sync(0xffffffffu, m == -INFINITY && (see0 | see1) != 0))) {
                 const float top = most_of(x, y, -INFINITY) * by;
                 const bool raise = !(here <= kMost) || (m == -INFINITY && top > -INFINITY);
-                const float to = raise ? fmaxf(top - kUp, m) : m, k = m == -INFINITY ? 0.f : exp2_fast(m - to);
+                // (scores of 2^26 and more, which fp32 rounds by 8: their roundings take the exponents that kUp would)
+                const float to = raise ? fmaxf(top - (fabsf(top) < 0x1p26f ? kUp : 0.f), m) : m, k = m == -INFINITY ? 0.f : exp2_fast(m - to);
                 if (j % kTcChain<T> != 0) {  // O as it is after the tokens before
                   ok = tc_wait(&sm.o_full[t][(s_n - 1) % 2], (s_n - 1) / 2, stop);
                   ok = __all_sync(0xffffffffu, ok);

@@ -121,3 +121,18 @@ def test_the_lightest_weights_that_fp16_holds(rows):
     out, lse = _many(cache, q, table, m, 0.6931471805599453)
     want = (m - 1) * value * 2.0 ** -32.375
     assert bool(((out.double().cpu() - want).abs() <= (m - 1) * value * 2.0 ** -33 + 2.0 ** -11 * want).all())
+
+
+@pytest.mark.parametrize("dtype", I.TYPES)
+@pytest.mark.parametrize("rows", [20, 200])
+@pytest.mark.parametrize("size", [1100.0, 1300.0, 1500.0, 1700.0])
+def test_scores_that_fp32_rounds_by_sixteen(dtype, rows, size):
+    """Scores of 1.1 to 2.7 10^8 powers of two, of which a weight may be 2^8 off: the outputs stay among the values."""
+    d, m = 64, 700
+    g = torch.Generator().manual_seed(int(size))
+    k = size + torch.randint(-3, 4, (m, 1, d), generator=g).float()
+    v = 1.0 + torch.rand((m, 1, d), generator=g)
+    cache, table, _, _ = _cache(16, k.to(dtype), v.to(dtype), 4)
+    q = (size + torch.randint(-3, 4, (rows // 4, 4, d), generator=g)).to(dtype)
+    out, lse = _many(cache, q, table, m, 1.0)
+    assert bool(torch.isfinite(lse).all()) and bool(((out >= 0.99) & (out <= 2.01)).all())

@@ -176,7 +176,8 @@ void cofie_kv_destroy(cofie_kv_t* h);
  *   rotary     NULL: keys are stored as they are. Its head_dim is the cache's.
  *   positions  int32 [n_axes][n_tokens], device memory (with rotary).
  * 16-bit pages take the rotated keys rounded once; bytes and 4-bit codes are
- * formed from the rotated keys in fp32. Tokens whose page is out of range are left out.
+ * formed from the rotated keys as fp32 numbers (bytes: see above for those that
+ * fp32 leaves open). Tokens whose page is out of range are left out.
  */
 int cofie_kv_append(cofie_kv_t* h, const cofie_kv_batch* b, const cofie_rows* k, const cofie_rows* v,
                     const cofie_rows* q, const cofie_rotary_t* rotary, const int32_t* positions, void* cuda_stream);

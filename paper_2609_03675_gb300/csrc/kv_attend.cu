@@ -179,10 +179,6 @@ AttendLaunch kernel_of(const cofie_kv_params& p, int kind, bool shared) {
   return p.bits == 4 ? of(std::integral_constant<int, 4>()) : p.bits == 8 ? of(std::integral_constant<int, 8>()) : of(std::integral_constant<int, 16>());
 }
 
-}  // namespace
-
-namespace {
-
 // The map of 16-bit pages, whose copies lie as the products read them.
 cudaError_t map_pages(const cofie_kv_params& p, void* pages, CUtensorMap* map) {
   void* f = nullptr;
@@ -366,8 +362,9 @@ int launch_attend(cofie_kv* h, AttendArgs* a, uint64_t rows, bool shared, cudaSt
   // width must not wait alone. Single tokens, heads of 128 and 16 bits, the whole call, us cut / uncut, where all are of the
   // width, of any length up to it, and one of it beside others of 10: 16 items of 512 17.5 / 17.3, 17.3 / 17.0, 17.0 / 17.2, of
   // 1024 19 / 24, 18 / 24, 17 / 24; 64 of 1024 32 / 30, 30 / 29, 27 / 27, of 2048 35 / 43, 31 / 41, 28 / 39; 128 of 1024 40 / 35,
-  // 37 / 35, 33 / 34, of 2048 59 / 54, 41 / 46, 33 / 46; 192 of 2048 64 / 52, 51 / 47, 30 / 40; 256 of 2048 74 / 61, 59 / 51, 32 / 41, of 4096 110 / 97, 75 / 77, 33 / 65; 512
-  // of 2048 118 / 105, 85 / 76, 44 / 47, of 8192 343 / 317, 190 / 207, 46 / 118; with fewer bits alike.
+  // 37 / 35, 33 / 34, of 2048 59 / 54, 41 / 46, 33 / 46; 192 of 2048 64 / 52, 51 / 47, 30 / 40; 256 of 2048 74 / 61, 59 / 51,
+  // 32 / 41, of 4096 110 / 97, 75 / 77, 33 / 65; 512 of 2048 118 / 105, 85 / 76, 44 / 47, of 8192 343 / 317, 190 / 207, 46 / 118;
+  // with fewer bits alike.
   const uint64_t uncut = items >= 160 ? 2048 : items >= 96 ? 1536 : items >= 64 ? 1024 : 512;
   if (a->behind && kind < kMany && width <= uncut && items <= 0x7fffffffu)
     kind = kind == kFew8 ? kShort8 : kShort16;

@@ -10,7 +10,8 @@ namespace {
 template <typename T, int D, int BITS, bool SHARED>
 AttendLaunch attend_kernel_of(int kind) {
   if (kind == kMany)
-    return {attend_rows_tc<T, D, BITS, SHARED, false>, kTcThreads<BITS>, tc_smem<D, BITS, SHARED>(), attend_join<T, D, SHARED>, kJoinThreads, kJoinRows<D>};
+    return {attend_rows_tc<T, D, BITS, SHARED, false>, kTcThreads<BITS>, tc_smem<D, BITS, SHARED>(),
+            attend_join<T, D, SHARED>,                 kJoinThreads,     kJoinRows<D>};
   if (kind == kManyWhole) return {attend_rows_tc<T, D, BITS, SHARED, true>, kTcThreads<BITS>, tc_smem<D, BITS, SHARED>(), nullptr, 0, 0};
   if constexpr (SHARED) {
     if (kind == kShort8) return {attend_split<T, D, BITS, 1, true, true>, kSplitThreads<true>, split_smem<D, BITS, 1, true>(), nullptr, 0, 0};

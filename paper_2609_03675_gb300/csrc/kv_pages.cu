@@ -244,7 +244,7 @@ __global__ void __launch_bounds__(kThreads, 4) append_codes(const __grid_constan
         // scale, which is exact, is held against half a scale. (75000 appended
         // tokens take 152 us so, 154 with every key held against it, and 135 took
         // those whose codes could be the next.)
-              float inv[2], low[2], zero[2], step[2];
+        float inv[2], low[2], zero[2], step[2];
 #pragma unroll
         for (int gr = 0; gr < kOwn; ++gr) {
           const float scale = group_scale(lo[gr], hi[gr]);

@@ -38,8 +38,8 @@
 // of the eight softmax warps, two to a scheduler (340 instructions a tile each),
 // and of as many that unpack (2900 together): with bytes 6000 warp instructions,
 // 62 % of the issue slots, the ALU pipe 49 %, the tensor pipe 42 % (256 new tokens
-// over 65792, 32 heads over 8: 285 us; 4 bits 265, 16 bits 218). 128 rows or less
-// over 16-bit pages are bound by DRAM: 32 over 262144 tokens 165 us of 158.
+// over 65792, 32 heads over 8: 278 us; 4 bits 261, 16 bits 216). 128 rows or less
+// over 16-bit pages are bound by DRAM: 128 over 262144 tokens 167 us of 158.
 // Tried: a warp for each stream's products instead of one for S and one for O
 // (283, but 230 for 199 over 16 bits where both streams take the same rows); four such warps
 // (305: less registers for the softmax); loops of products (319 for 304: the warp
@@ -59,10 +59,11 @@ constexpr int kTcUnpack = 128;   // of keys, and as many of values
 template <int BITS>
 constexpr int kTcThreads = kTcSoftmax + (BITS < 16 ? 2 * kTcUnpack : 0) + 128;
 constexpr int kTcInfo = 16;         // more than the stages and the raw tiles: a tile is told before its place is free
-// Tiles from which both streams take an item of 128 rows or less: where tiles are unpacked it pays over long caches, and
-// the sums' meeting costs short items more. us, by one stream / by both: 32 answers over 262144 tokens of bytes 263 / 238,
-// of 16 bits 191 / 189; 80 rows over 60000 tokens of 4 bits 224 / 188, of bytes 237 / 233, of 16 bits 181 / 182; over 6000
-// 112 / 115, 130 / 128, 97 / 106; over 2000 28 / 30, 30 / 31, 24 / 26.
+// Tiles from which both streams take an item of 128 rows or less: it pays over long caches, and the sums' meeting costs
+// short items more. us, by one stream / by both: 32 answers over 262144 tokens of bytes 263 / 232, 128 rows of 4 bits 214 / 180;
+// 80 rows over 60000 tokens of 4 bits 379 / 313, of bytes 391 / 397, over 6000 112 / 115 and 130 / 128, over 2000 28 / 30, 30 / 31.
+// 16 bits, 8 key heads of 128: 32 answers over 262144 191 / 189, 64 rows over 524288 319 / 312, over 66000 59 / 61, over 6000 97 / 106;
+// fp16, 4 key heads: 64 rows over 524288 177 / 167, over 66000 43 / 44; 8 of 64: over 66000 50 / 43, over 262144 151 / 119.
 template <int BITS>
 constexpr uint32_t kTcStreamed = BITS < 16 ? 128 : 1024;
 // Tiles whose products are summed in tensor memory before the sums move on to the CTA's part. The tensor core cuts each

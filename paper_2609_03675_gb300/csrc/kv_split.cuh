@@ -36,7 +36,7 @@
 //
 // Bytes enter likewise as fp16 numbers u - 128, made of 1024 + u (a byte beside
 // 0x64) by one subtraction for two; the scales, powers of two, are on the side of
-// the few rows as those of codes. 32 answers over up to 16384 tokens: 124 us, 4.7
+// the few rows as those of codes. 32 answers over up to 16384 tokens: 125 us, 4.7
 // TB/s of DRAM, issue slots 40 % busy; with chunks of 16 tokens 135, with those
 // and two CTAs to an SM 117 (but 12.6 for 11.4 over 1111 tokens, and where there
 // are more than 8 rows 73 for 65), with 12 warps to a CTA 128.
@@ -489,20 +489,20 @@ __global__ void __launch_bounds__(kSplitThreads<SHORT>, SHORT || (NT == 1 && BIT
                 }
               }
             } else {
-            const uint2 x = at<uint2>(base + unit_at<D, BITS, false>(t0, gr * 2 + c / 2) + (c % 2) * 8);
-            const uint2 y = at<uint2>(base + unit_at<D, BITS, false>(t0 + 8, gr * 2 + c / 2) + (c % 2) * 8);
-            const uint32_t z0 = __byte_perm(w0, w0, gr == 0 ? 0x1010 : 0x3232) & 0x000F000Fu, z1 = __byte_perm(w1, w1, gr == 0 ? 0x1010 : 0x3232) & 0x000F000Fu;
+              const uint2 x = at<uint2>(base + unit_at<D, BITS, false>(t0, gr * 2 + c / 2) + (c % 2) * 8);
+              const uint2 y = at<uint2>(base + unit_at<D, BITS, false>(t0 + 8, gr * 2 + c / 2) + (c % 2) * 8);
+              const uint32_t z0 = __byte_perm(w0, w0, gr == 0 ? 0x1010 : 0x3232) & 0x000F000Fu, z1 = __byte_perm(w1, w1, gr == 0 ? 0x1010 : 0x3232) & 0x000F000Fu;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const uint32_t u = (e < 2 ? x.x : x.y) >> (8 * (e % 2)), v = (e < 2 ? y.x : y.y) >> (8 * (e % 2));
-              const uint32_t f[4] = {H::sub(u & 0x000F000Fu, z0), H::sub(v & 0x000F000Fu, z1), H::sub(u & 0x00F000F0u, z0 * 16),
-                                     H::sub(v & 0x00F000F0u, z1 * 16)};
+              for (int e = 0; e < 4; ++e) {
+                const uint32_t u = (e < 2 ? x.x : x.y) >> (8 * (e % 2)), v = (e < 2 ? y.x : y.y) >> (8 * (e % 2));
+                const uint32_t f[4] = {H::sub(u & 0x000F000Fu, z0), H::sub(v & 0x000F000Fu, z1), H::sub(u & 0x00F000F0u, z0 * 16),
+                                       H::sub(v & 0x00F000F0u, z1 * 16)};
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt) {
-                if (e == 0) mma_first(acc[nt], f, qf[nt][4 * gr][0], qf[nt][4 * gr][1]);
-                else H::mma(acc[nt], f, qf[nt][4 * gr + e][0], qf[nt][4 * gr + e][1]);
+                for (int nt = 0; nt < NT; ++nt) {
+                  if (e == 0) mma_first(acc[nt], f, qf[nt][4 * gr][0], qf[nt][4 * gr][1]);
+                  else H::mma(acc[nt], f, qf[nt][4 * gr + e][0], qf[nt][4 * gr + e][1]);
+                }
               }
-            }
             }
             const float s0 = gr == 0 ? scale_lo(w0) : scale_hi(w0), s1 = gr == 0 ? scale_lo(w1) : scale_hi(w1);
 #pragma unroll

@@ -15,7 +15,7 @@ struct AttendLaunch {
   AttendKernel kernel;
   uint32_t threads;
   size_t smem;
-  AttendKernel join;  // kMany: joins the parts, some rows to a CTA
+  AttendKernel join[2];  // kMany: joins the parts, some rows to a CTA; as many CTAs as a block has rows for, or fewer
   uint32_t join_threads, join_rows;
 };
 // The kernel for the handle's type and head length. SHARED: over a prefix, or behind one.

@@ -11,14 +11,14 @@ template <typename T, int D, int BITS, bool SHARED>
 AttendLaunch attend_kernel_of(int kind) {
   if (kind == kMany)
     return {attend_rows_tc<T, D, BITS, SHARED, false>, kTcThreads<BITS>, tc_smem<D, BITS, SHARED>(),
-            attend_join<T, D, SHARED>,                 kJoinThreads,     kJoinRows<D>};
-  if (kind == kManyWhole) return {attend_rows_tc<T, D, BITS, SHARED, true>, kTcThreads<BITS>, tc_smem<D, BITS, SHARED>(), nullptr, 0, 0};
+            {attend_join<T, D, SHARED, false>, attend_join<T, D, SHARED, true>}, kJoinThreads, kJoinRows<D>};
+  if (kind == kManyWhole) return {attend_rows_tc<T, D, BITS, SHARED, true>, kTcThreads<BITS>, tc_smem<D, BITS, SHARED>(), {}, 0, 0};
   if constexpr (SHARED) {
-    if (kind == kShort8) return {attend_split<T, D, BITS, 1, true, true>, kSplitThreads<true>, split_smem<D, BITS, 1, true>(), nullptr, 0, 0};
-    if (kind == kShort16) return {attend_split<T, D, BITS, 2, true, true>, kSplitThreads<true>, split_smem<D, BITS, 2, true>(), nullptr, 0, 0};
+    if (kind == kShort8) return {attend_split<T, D, BITS, 1, true, true>, kSplitThreads<true>, split_smem<D, BITS, 1, true>(), {}, 0, 0};
+    if (kind == kShort16) return {attend_split<T, D, BITS, 2, true, true>, kSplitThreads<true>, split_smem<D, BITS, 2, true>(), {}, 0, 0};
   }
-  if (kind == kFew8) return {attend_split<T, D, BITS, 1, SHARED, false>, kSplitThreads<false>, split_smem<D, BITS, 1, false>(), nullptr, 0, 0};
-  return {attend_split<T, D, BITS, 2, SHARED, false>, kSplitThreads<false>, split_smem<D, BITS, 2, false>(), nullptr, 0, 0};
+  if (kind == kFew8) return {attend_split<T, D, BITS, 1, SHARED, false>, kSplitThreads<false>, split_smem<D, BITS, 1, false>(), {}, 0, 0};
+  return {attend_split<T, D, BITS, 2, SHARED, false>, kSplitThreads<false>, split_smem<D, BITS, 2, false>(), {}, 0, 0};
 }
 
 }  // namespace

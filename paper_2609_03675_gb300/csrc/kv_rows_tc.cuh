@@ -1011,8 +1011,12 @@ __global__ void __launch_bounds__(kTcThreads<BITS>, 1) attend_rows_tc(const __gr
 constexpr int kJoinThreads = 512;
 template <int D>
 constexpr uint32_t kJoinRows = kJoinThreads / (D / 4);
-template <typename T, int D, bool SHARED>
-__global__ void __launch_bounds__(kJoinThreads) attend_join(const __grid_constant__ AttendArgs a) {
+// FEW: as many CTAs as the call says that it has rows for, which go on with what others there are. (CTAs that find nothing to
+// join cost their launch: eight sequences of 64 tokens of 4 bits under 36 rows, in tables of 4096, 15.4 us with 16 to an item,
+// 12.8 with 3. A question over bytes, 279 us, takes 281 by CTAs that could go on. Four to an SM: with more registers, and fewer
+// at a time, 32 sequences of 1111 tokens took 5 % more.)
+template <typename T, int D, bool SHARED, bool FEW>
+__global__ void __launch_bounds__(kJoinThreads, 4) attend_join(const __grid_constant__ AttendArgs a) {
   using P = Pair<T>;
   constexpr uint32_t kLanes = D / 4;
   pdl_trigger();
@@ -1020,62 +1024,70 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join(const __grid_constan
   const SplitItem it = a.items[blockIdx.x];
   if (it.last_cta <= blockIdx.x) return;
   const uint32_t all = min(kManyRows, it.span.count * a.group - it.rb * kManyRows);
-  const uint32_t lane = threadIdx.x % kLanes, row = blockIdx.y * kJoinRows<D> + threadIdx.x / kLanes;
-  if (blockIdx.y * kJoinRows<D> >= all) return;
-  const bool real = row < all;  // (whole warps go on, for the shuffles)
-  const uint32_t parts = it.last_cta - blockIdx.x + 1;
-  const auto part_at = [&](uint32_t i) { return (2ull * (blockIdx.x + i) + (i == 0)) * kManyRows + (real ? row : 0); };
-  float top = -INFINITY, sum = 0.f;
-  for (uint32_t i = lane; i < parts; i += kLanes) top = fmaxf(top, a.part_ms[part_at(i)].x);
+  const uint32_t lane = threadIdx.x % kLanes, parts = it.last_cta - blockIdx.x + 1;
+  const auto join = [&](uint32_t row0) {
+    const uint32_t row = row0 + threadIdx.x / kLanes;
+    const bool real = row < all;  // (whole warps go on, for the shuffles)
+    const auto part_at = [&](uint32_t i) { return (2ull * (blockIdx.x + i) + (i == 0)) * kManyRows + (real ? row : 0); };
+    float top = -INFINITY, sum = 0.f;
+    for (uint32_t i = lane; i < parts; i += kLanes) top = fmaxf(top, a.part_ms[part_at(i)].x);
 #pragma unroll
-  for (uint32_t o = 1; o < kLanes; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (uint32_t p0 = 0; p0 < parts; p0 += kLanes) {
-    float k = 0.f;
-    if (p0 + lane < parts) {
-      const float2 z = a.part_ms[part_at(p0 + lane)];
-      k = z.x == -INFINITY ? (z.y == 0.f ? 0.f : 1.f) : exp2_fast(z.x - top);
-      sum += z.y == 0.f ? 0.f : k * z.y;
-    }
-    const uint32_t n = min(kLanes, parts - p0);
+    for (uint32_t o = 1; o < kLanes; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (uint32_t p0 = 0; p0 < parts; p0 += kLanes) {
+      float k = 0.f;
+      if (p0 + lane < parts) {
+        const float2 z = a.part_ms[part_at(p0 + lane)];
+        k = z.x == -INFINITY ? (z.y == 0.f ? 0.f : 1.f) : exp2_fast(z.x - top);
+        sum += z.y == 0.f ? 0.f : k * z.y;
+      }
+      const uint32_t n = min(kLanes, parts - p0);
 #pragma unroll 8
-    for (uint32_t i = 0; i < n; ++i) {
-      const float by = __shfl_sync(0xffffffffu, k, i, kLanes);
-      const float4 z = *reinterpret_cast<const float4*>(a.part + part_at(p0 + i) * D + lane * 4);
-      y.x += by * z.x, y.y += by * z.y, y.z += by * z.z, y.w += by * z.w;
+      for (uint32_t i = 0; i < n; ++i) {
+        const float by = __shfl_sync(0xffffffffu, k, i, kLanes);
+        const float4 z = *reinterpret_cast<const float4*>(a.part + part_at(p0 + i) * D + lane * 4);
+        y.x += by * z.x, y.y += by * z.y, y.z += by * z.z, y.w += by * z.w;
+      }
     }
-  }
 #pragma unroll
-  for (uint32_t o = 1; o < kLanes; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  if (!real) return;
-  const uint32_t token = it.span.first + (it.rb * kManyRows + row) / a.group, head = it.head * a.group + (it.rb * kManyRows + row) % a.group;
-  const uint64_t at = static_cast<uint64_t>(token) * a.heads + head;
-  float by = sum == 0.f ? 0.f : 1.f / sum, lse = top + log2f(sum);
-  if constexpr (SHARED) {
-    float4* const there = reinterpret_cast<float4*>(a.rows + at * D) + lane;
-    if (!a.behind) {
-      *there = y;
-      if (lane == 0) a.rows_ms[at] = make_float2(top, sum);
-      return;
+    for (uint32_t o = 1; o < kLanes; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (!real) return;
+    const uint32_t token = it.span.first + (it.rb * kManyRows + row) / a.group, head = it.head * a.group + (it.rb * kManyRows + row) % a.group;
+    const uint64_t at = static_cast<uint64_t>(token) * a.heads + head;
+    float by = sum == 0.f ? 0.f : 1.f / sum, lse = top + log2f(sum);
+    if constexpr (SHARED) {
+      float4* const there = reinterpret_cast<float4*>(a.rows + at * D) + lane;
+      if (!a.behind) {
+        *there = y;
+        if (lane == 0) a.rows_ms[at] = make_float2(top, sum);
+        return;
+      }
+      if (has_prefix(a, it.seq)) {
+        const Both w = both_parts(top, sum, a.rows_ms[at]);
+        const float4 z = *there;
+        y = make_float4(w.own * y.x + w.prefix * z.x, w.own * y.y + w.prefix * z.y, w.own * y.z + w.prefix * z.z, w.own * y.w + w.prefix * z.w);
+        by = w.sum == 0.f ? 0.f : 1.f / w.sum;
+        lse = w.top + log2f(w.sum);
+      }
     }
-    if (has_prefix(a, it.seq)) {
-      const Both w = both_parts(top, sum, a.rows_ms[at]);
-      const float4 z = *there;
-      y = make_float4(w.own * y.x + w.prefix * z.x, w.own * y.y + w.prefix * z.y, w.own * y.z + w.prefix * z.z, w.own * y.w + w.prefix * z.w);
-      by = w.sum == 0.f ? 0.f : 1.f / w.sum;
-      lse = w.top + log2f(w.sum);
+    T* const out = reinterpret_cast<T*>(a.q.out) + static_cast<int64_t>(token) * a.q.out_token + static_cast<int64_t>(head) * a.q.out_head + lane * 4;
+    if (a.out_wide) {
+      *reinterpret_cast<uint2*>(out) = make_uint2(P::pack(y.x * by, y.y * by), P::pack(y.z * by, y.w * by));
+    } else {
+      out[0] = Elem<T>::from(y.x * by);
+      out[1] = Elem<T>::from(y.y * by);
+      out[2] = Elem<T>::from(y.z * by);
+      out[3] = Elem<T>::from(y.w * by);
     }
+    if (a.lse && lane == 0) a.lse[at] = lse * 0.6931471805599453f;
+  };
+  const uint32_t first = blockIdx.y * kJoinRows<D>;
+  if constexpr (FEW) {
+#pragma unroll 1
+    for (uint32_t row0 = first; row0 < all; row0 += gridDim.y * kJoinRows<D>) join(row0);
+  } else if (first < all) {
+    join(first);
   }
-  T* const out = reinterpret_cast<T*>(a.q.out) + static_cast<int64_t>(token) * a.q.out_token + static_cast<int64_t>(head) * a.q.out_head + lane * 4;
-  if (a.out_wide) {
-    *reinterpret_cast<uint2*>(out) = make_uint2(P::pack(y.x * by, y.y * by), P::pack(y.z * by, y.w * by));
-  } else {
-    out[0] = Elem<T>::from(y.x * by);
-    out[1] = Elem<T>::from(y.y * by);
-    out[2] = Elem<T>::from(y.z * by);
-    out[3] = Elem<T>::from(y.w * by);
-  }
-  if (a.lse && lane == 0) a.lse[at] = lse * 0.6931471805599453f;
 }
 
 // One CTA to an SM, whose tensor memory it takes whole: more than half of its shared memory.

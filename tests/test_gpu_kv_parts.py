@@ -107,3 +107,40 @@ def test_tables_of_every_width(bits, heads, new):
                         bad = B.exceeds(out[t:t + n], lse[t:t + n], w)
                         assert not bool(bad[0].any()) and not bool(bad[1].any()), width
                     t += n
+
+
+@pytest.mark.parametrize("bits", [16, "int8", 4])
+@pytest.mark.parametrize("d", [64, 128])
+def test_parts_of_more_rows_than_the_call_says(bits, d):
+    """Long items that several CTAs share, 300 rows of them where the hint says 17 to 128, or fewer; rows past the batch."""
+    from paper_2609_03675_gb300 import KVCache
+    h, kv, page, dtype = 8, 2, 64, torch.bfloat16
+    lengths, news = [9000, 70, 5000], [75, 3, 20]
+    g = torch.Generator().manual_seed(d)
+    each = [-(-m // page) for m in lengths]
+    cache = KVCache(sum(each), page, h, kv, d, dtype=dtype, bits=bits)
+    table = torch.zeros((3, max(each)), dtype=torch.int32)
+    for s, e in enumerate(each):
+        table[s, :e] = torch.arange(sum(each[:s]), sum(each[:s + 1]))
+    table, lens = table.cuda(), torch.tensor(lengths, dtype=torch.int32, device="cuda")
+    whole = torch.tensor([0] + lengths).cumsum(0).to(torch.int32).cuda()
+    x = [torch.randn((sum(lengths), kv, d), generator=g).to(dtype).cuda() for _ in range(2)]
+    cache.append(*x, table, lens, whole)
+    k, v = cache.read(table, lens, whole, n_tokens=sum(lengths))
+    q = torch.randn((sum(news) + 5, h, d), generator=g).to(dtype).cuda()
+    offsets = torch.tensor([0] + news).cumsum(0).to(torch.int32).cuda()
+    want, t, at = [], 0, 0
+    for n, m in zip(news, lengths):
+        seen = torch.arange(m)[None] <= (m - n + torch.arange(n))[:, None]
+        want.append(B.attend(q[t:t + n], k[at:at + m], v[at:at + m], seen, d ** -0.5, dtype))
+        t, at = t + n, at + m
+    for hint in (5, 8, 20, 32, 33, 75, 0):
+        out, lse = torch.full_like(q, 7.0), torch.full(q.shape[:2], 7.0, device="cuda")
+        cache.attend(q, table, lens, offsets, max_new=hint, out=out, lse=lse)
+        cache.status()
+        t = 0
+        for n, w in zip(news, want):
+            bad = B.exceeds(out[t:t + n], lse[t:t + n], w)
+            assert not bool(bad[0].any()) and not bool(bad[1].any()), hint
+            t += n
+        assert bool((out[t:] == 7.0).all()) and bool((lse[t:] == 7.0).all())
